@@ -6,7 +6,9 @@
  *   - the per-channel long convolution of length L via FFT       (Eq. 6, Sec. 2.2),
  *   - chunked ("tiled, divide-and-conquer") causal linear attention with a carried
  *     d_k x d_v state and a row normaliser                       (Eq. 2, Sec. 4.1),
- *   - their composition with the Q/K/V formation                 (Eqs. 8, 10-12).
+ *   - their composition with the Q/K/V formation                 (Eqs. 8, 10-12),
+ * and, for layers built around the same short convolution, a selective state space scan, the short convolution with
+ * carried inputs and the norms between two blocks, each for prompts, single tokens and training.
  *
  * Conventions common to every entry point
  *   - Every data pointer is a DEVICE pointer owned by the caller; the library never frees or
@@ -48,8 +50,9 @@ typedef enum {
 typedef enum { CHELA_F32 = 0, CHELA_BF16 = 1, CHELA_BF16_PAIR = 2 } chela_dtype_t;
 
 /* CHELA_NORM_RMS: o = r * (mean_j r_j^2 + eps)^(-1/2) over the d_v entries of one head's output
- * row, no learnable gain -- the library's reading of "Norm" in Eq. 2.  CHELA_NORM_NONE: o = r. */
-typedef enum { CHELA_NORM_NONE = 0, CHELA_NORM_RMS = 1 } chela_norm_t;
+ * row, no learnable gain -- the library's reading of "Norm" in Eq. 2.  CHELA_NORM_NONE: o = r.
+ * CHELA_NORM_LAYER: the row minus its mean, then as CHELA_NORM_RMS (chela_blocknorm_fwd / _bwd only). */
+typedef enum { CHELA_NORM_NONE = 0, CHELA_NORM_RMS = 1, CHELA_NORM_LAYER = 2 } chela_norm_t;
 
 const char *chela_status_string(chela_status_t status);
 int chela_version(void);
@@ -319,6 +322,138 @@ chela_status_t chela_mixer_prepared_fwd(const void *x, const float *w_short, int
                                         int L, int D, int H, int chunk, chela_dtype_t in_dtype, chela_dtype_t out_dtype,
                                         chela_norm_t norm, float norm_eps, void *workspace, size_t workspace_bytes,
                                         cudaStream_t stream);
+
+/*
+ * Packed sequences.  The entry points below take S sequences laid one behind the other along one token axis of T
+ * tokens (token-major: one token's channels are contiguous).  Sequence s owns the tokens seq_offsets[s] <= t <
+ * seq_offsets[s + 1]; seq_offsets is a device array of S + 1 int32, not decreasing, seq_offsets[0] = 0.  With
+ * seq_offsets = NULL all sequences have T / S tokens (T a multiple of S).  Sequences may be empty: their state passes
+ * through unchanged.  Tokens from seq_offsets[S] to T belong to no sequence: they are not read and their output rows are
+ * left as they were.  The offsets are read on the device; out of range values are clamped to [0, T], so that a bad array
+ * gives undefined results but no access outside the tensors.
+ * Token strides (`*_stride`, in elements) are the distance between consecutive tokens and at least the row's length,
+ * so that an operand can be a column slice of a wider projection; they must be multiples of 8.  Outputs without a
+ * stride argument are contiguous.
+ *
+ * Short depthwise causal convolution (chela_shortconv_fwd) over packed sequences with the inputs before the first
+ * token carried in and the last ones carried out, for evaluation in segments and for decoding:
+ *   u[t,c] = bias[c] + sum_{j=0}^{width-1} w[c,j] * x[t-j,c],   y = act(u)      (act: 0 identity, 1 SiLU)
+ * where x[-1], x[-2], ... of sequence s are state_in[s, width-2], state_in[s, width-3], ... (zero if state_in is NULL).
+ * state_out[s] = the last width - 1 inputs of (state_in[s] | the sequence), oldest first.
+ * x, y : [T, D] io_dtype.  w : [D, width] fp32.  bias : [D] fp32 or NULL.  state_in, state_out : [S, width-1, D] io_dtype,
+ * nullable, may be the same buffer; no other operands may overlap.  Supported: 1 <= width <= 16, D a multiple of 8
+ * (width = 1 has no state: both state pointers are ignored).  No workspace.
+ *
+ * chela_shortconv_step: one new token per sequence, x, y : [S, D]; state_in is required unless width = 1; state_out as
+ * above (the same buffer for an update in place).
+ */
+chela_status_t chela_shortconv_carry_fwd(const void *x, long long x_stride, const float *w, const float *bias, void *y,
+                                         const void *state_in, void *state_out, const int *seq_offsets, int S, int T, int D,
+                                         int width, int act, chela_dtype_t io_dtype, cudaStream_t stream);
+chela_status_t chela_shortconv_step(const void *x, long long x_stride, const float *w, const float *bias, void *y,
+                                    const void *state_in, void *state_out, int S, int D, int width, int act,
+                                    chela_dtype_t io_dtype, cudaStream_t stream);
+
+/*
+ * Backward of chela_shortconv_carry_fwd.  d_y : [T, D] io_dtype, d_state_out : gradient of state_out, [S, width-1, D]
+ * io_dtype, or NULL (zero).  d_x : [T, D] grad_dtype; d_w : [D, width] and d_bias : [D] fp32, each nullable;
+ * d_state_in : [S, width-1, D] grad_dtype or NULL.  The sums over tokens are taken in a fixed order: equal calls give
+ * equal bits.  workspace: chela_shortconv_bwd_workspace_bytes.
+ */
+size_t chela_shortconv_bwd_workspace_bytes(int T, int D, int width);
+chela_status_t chela_shortconv_bwd(const void *x, long long x_stride, const float *w, const float *bias, const void *d_y,
+                                   long long d_y_stride, const void *state_in, const void *d_state_out, void *d_x, float *d_w,
+                                   float *d_bias, void *d_state_in, const int *seq_offsets, int S, int T, int D, int width,
+                                   int act, chela_dtype_t io_dtype, chela_dtype_t grad_dtype, void *workspace,
+                                   size_t workspace_bytes, cudaStream_t stream);
+
+/*
+ * Selective state space scan over packed sequences: per channel c a recurrence over N states whose decay and input
+ * depend on the token,
+ *   dt_t = softplus(dt[t,c] + dt_bias[c])   (softplus = 0: dt[t,c] + dt_bias[c]),
+ *   h_t[n] = exp(dt_t a[c,n]) h_{t-1}[n] + dt_t b[t,g,n] x[t,c],
+ *   y[t,c] = (sum_n c[t,g,n] h_t[n] + d_skip[c] x[t,c]) * silu(z[t,c]),
+ * with g = c / (D / G) the channel's group and h_{-1} = state_in[s,c] (zero if NULL).  It takes the long convolution's
+ * place behind the short one (Eq. 7) where the kernel shall depend on the tokens and a state shall be carried.
+ * x, dt, z : [T, D] in_dtype (F32 or BF16); z, d_skip, dt_bias nullable (no gate, 0, 0).  b, c : [T, G, N] in_dtype, a
+ * token's G * N values contiguous.  a : [D, N], d_skip, dt_bias : [D] fp32.  Supported: N in {8, 16, 32, 64}, D a multiple of
+ * 8, G = 1 or D / G a multiple of 32.  States are held in fp32 throughout.
+ */
+typedef struct {
+    const void *x, *dt, *b, *c, *z;
+    long long x_stride, dt_stride, b_stride, c_stride, z_stride;
+    const float *a, *d_skip, *dt_bias;
+    const float *state_in;          /* [S, D, N] fp32 or NULL */
+    const int *seq_offsets;         /* S + 1 int32 on the device, or NULL */
+    int S, T, D, N, G, softplus;
+    chela_dtype_t in_dtype;
+} chela_selscan_args_t;
+
+/*
+ * y : [T, D] out_dtype.  state_out : [S, D, N] fp32 or NULL, may be state_in's buffer.  checkpoints: NULL, or a device
+ * buffer of chela_selscan_checkpoint_bytes that receives the states at every 32nd token of each sequence, which
+ * chela_selscan_bwd then need not compute again.  y may be NULL when only state_out or checkpoints are wanted.
+ * No workspace.
+ */
+size_t chela_selscan_checkpoint_bytes(int T, int S, int D, int N);
+chela_status_t chela_selscan_fwd(const chela_selscan_args_t *args, void *y, float *state_out, void *checkpoints,
+                                 chela_dtype_t out_dtype, cudaStream_t stream);
+
+/* One new token per sequence (T = S, seq_offsets NULL): reads and writes the state once.  state_in is required;
+ * state_out (required) may be state_in's buffer. */
+chela_status_t chela_selscan_step(const chela_selscan_args_t *args, void *y, float *state_out, chela_dtype_t out_dtype,
+                                  cudaStream_t stream);
+
+/*
+ * Backward of chela_selscan_fwd for the same args.  d_y : [T, D] in_dtype; d_state_out : [S, D, N] fp32 or NULL (zero).
+ * checkpoints : as written by chela_selscan_fwd for these args, or NULL (computed again in the workspace).
+ * d_x, d_dt, d_z : [T, D] and d_b, d_c : [T, G, N] of grad_dtype (F32 or BF16); d_a : [D, N], d_skip, d_dt_bias : [D] fp32;
+ * d_state_in : [S, D, N] fp32 or NULL.  d_z is required exactly when z is given; d_skip_grad and d_dt_bias are nullable.
+ * d_dt is the gradient of dt as given, through softplus.  Sums over tokens and channels are taken in a fixed order.
+ */
+size_t chela_selscan_bwd_workspace_bytes(int T, int S, int D, int N, int have_checkpoints);
+chela_status_t chela_selscan_bwd(const chela_selscan_args_t *args, const void *d_y, long long d_y_stride,
+                                 const float *d_state_out, const void *checkpoints, void *d_x, void *d_dt, float *d_a, void *d_b,
+                                 void *d_c, float *d_skip_grad, void *d_z, float *d_dt_bias, float *d_state_in,
+                                 chela_dtype_t grad_dtype, void *workspace, size_t workspace_bytes, cudaStream_t stream);
+
+/*
+ * The junction of two blocks: one block's output is gated, normalised, scaled and added to the residual stream, and the
+ * sum is normalised for the next block.  Per token row of D values,
+ *   v = y * act(gate)  (gate_after = 0)  or  y;      n = Norm_post(v) * w_post + b_post;
+ *   m = n  or  n * act(gate)  (gate_after = 1);      r' = res + scale * m;      o = Norm_pre(r') * w_pre + b_pre,
+ * gate_act 0 identity, 1 SiLU, 2 sigmoid; norms CHELA_NORM_NONE, _RMS or _LAYER with eps inside the square root.
+ * y = NULL leaves out everything up to r' (r' = res; res_out must be NULL): the norm before a first block.  o = NULL leaves
+ * out the last norm: the norm behind a last block.  res = NULL counts as zero.
+ * res, res_out : [T, D] res_dtype, may be the same buffer.  y, gate : [T, D] in_dtype with token strides.  o : [T, D]
+ * out_dtype.  w_post, b_post, scale, w_pre, b_pre : [D] fp32, each nullable (1, 0, 1, 1, 0).  All dtypes F32 or BF16.
+ * o is taken from r' before its rounding to res_dtype.  Supported: D a multiple of 8, D <= 8192.  No workspace.
+ */
+typedef struct {
+    const void *res, *y, *gate;     /* for chela_blocknorm_bwd, res is r' as chela_blocknorm_fwd wrote it */
+    long long res_stride, y_stride, gate_stride;
+    const float *w_post, *b_post, *scale, *w_pre, *b_pre;
+    int T, D, gate_act, gate_after;
+    chela_norm_t norm_post, norm_pre;
+    float eps;
+    chela_dtype_t in_dtype, res_dtype;
+} chela_blocknorm_args_t;
+
+chela_status_t chela_blocknorm_fwd(const chela_blocknorm_args_t *args, void *res_out, void *o, chela_dtype_t out_dtype,
+                                   cudaStream_t stream);
+
+/*
+ * Backward of chela_blocknorm_fwd; statistics are recomputed from r' and y.  d_o : [T, D] in_dtype or NULL (zero),
+ * d_res_out : [T, D] res_dtype or NULL (zero), not both NULL.  d_res : [T, D] res_dtype, the gradient of res, which is also
+ * that of r'.  d_y, d_gate : [T, D] grad_dtype, required exactly when y, gate are given.  d_w_post, d_b_post, d_scale,
+ * d_w_pre, d_b_pre : [D] fp32, each nullable; a gradient of a part that the call leaves out is zero.  d_res may be
+ * d_res_out's buffer.  Sums over tokens are taken in a fixed order.
+ */
+size_t chela_blocknorm_bwd_workspace_bytes(int T, int D);
+chela_status_t chela_blocknorm_bwd(const chela_blocknorm_args_t *args, const void *d_o, const void *d_res_out, void *d_res,
+                                   void *d_y, void *d_gate, float *d_w_post, float *d_b_post, float *d_scale, float *d_w_pre,
+                                   float *d_b_pre, chela_dtype_t grad_dtype, void *workspace, size_t workspace_bytes,
+                                   cudaStream_t stream);
 
 #ifdef __cplusplus
 }

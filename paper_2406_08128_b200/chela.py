@@ -8,6 +8,7 @@ loading fails with an error.
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 import os
 
@@ -18,12 +19,30 @@ LIB_PATH = os.path.join(_HERE, "libchela.so")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = range(6)
 F32, BF16, BF16_PAIR = 0, 1, 2
-NORM_NONE, NORM_RMS = 0, 1
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 _lib = None
 
 _c_int, _c_float, _c_size_t, _vp = ctypes.c_int, ctypes.c_float, ctypes.c_size_t, ctypes.c_void_p
+_c_ll = ctypes.c_longlong
+
+
+class SelscanArgs(ctypes.Structure):
+    """chela_selscan_args_t"""
+    _fields_ = [(n, _vp) for n in ("x", "dt", "b", "c", "z")] \
+        + [(n, _c_ll) for n in ("x_stride", "dt_stride", "b_stride", "c_stride", "z_stride")] \
+        + [(n, _vp) for n in ("a", "d_skip", "dt_bias", "state_in", "seq_offsets")] \
+        + [(n, _c_int) for n in ("S", "T", "D", "N", "G", "softplus", "in_dtype")]
+
+
+class BlocknormArgs(ctypes.Structure):
+    """chela_blocknorm_args_t"""
+    _fields_ = [(n, _vp) for n in ("res", "y", "gate")] + [(n, _c_ll) for n in ("res_stride", "y_stride", "gate_stride")] \
+        + [(n, _vp) for n in ("w_post", "b_post", "scale", "w_pre", "b_pre")] \
+        + [(n, _c_int) for n in ("T", "D", "gate_act", "gate_after", "norm_post", "norm_pre")] + [("eps", _c_float)] \
+        + [(n, _c_int) for n in ("in_dtype", "res_dtype")]
+
 
 _SIGNATURES = {
     "chela_status_string": (ctypes.c_char_p, [_c_int]),
@@ -67,6 +86,18 @@ _SIGNATURES = {
     "chela_mixer_fwd": (_c_int, [_vp, _vp, _c_int, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _c_int, _c_int, _vp,
                                  _c_int, _c_int, _c_int, _c_int, _c_int, _c_int, _c_int, _c_int, _c_float,
                                  _vp, _c_size_t, _vp]),
+    "chela_shortconv_carry_fwd": (_c_int, [_vp, _c_ll] + [_vp] * 6 + [_c_int] * 5 + [_c_int, _vp]),
+    "chela_shortconv_step": (_c_int, [_vp, _c_ll] + [_vp] * 5 + [_c_int] * 4 + [_c_int, _vp]),
+    "chela_shortconv_bwd_workspace_bytes": (_c_size_t, [_c_int] * 3),
+    "chela_shortconv_bwd": (_c_int, [_vp, _c_ll, _vp, _vp, _vp, _c_ll] + [_vp] * 7 + [_c_int] * 7 + [_vp, _c_size_t, _vp]),
+    "chela_selscan_checkpoint_bytes": (_c_size_t, [_c_int] * 4),
+    "chela_selscan_fwd": (_c_int, [_vp] * 4 + [_c_int, _vp]),
+    "chela_selscan_step": (_c_int, [_vp] * 3 + [_c_int, _vp]),
+    "chela_selscan_bwd_workspace_bytes": (_c_size_t, [_c_int] * 5),
+    "chela_selscan_bwd": (_c_int, [_vp, _vp, _c_ll] + [_vp] * 11 + [_c_int, _vp, _c_size_t, _vp]),
+    "chela_blocknorm_fwd": (_c_int, [_vp] * 3 + [_c_int, _vp]),
+    "chela_blocknorm_bwd_workspace_bytes": (_c_size_t, [_c_int] * 2),
+    "chela_blocknorm_bwd": (_c_int, [_vp] * 11 + [_c_int, _vp, _c_size_t, _vp]),
 }
 
 
@@ -368,3 +399,297 @@ def mixer_gated_fwd(x, w_short, k_long, w_q, w_k, w_v, w_a, w_o, H, chunk=64, b_
                                        int(norm), float(eps), _ptr(workspace), workspace.numel(), _stream()),
            "chela_mixer_gated_fwd")
     return u
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# Operators over packed sequences.  Token tensors are [T, D] (sequences one behind the other, with seq_offsets) or
+# [B, L, D] (B sequences of L tokens); the channel axis must be contiguous and consecutive tokens a fixed distance
+# apart, so column slices of a wider projection are taken as they are.  All tensors of a call live on one CUDA device;
+# the call runs on that device's current stream.
+
+ShortconvGrads = collections.namedtuple("ShortconvGrads", "d_x d_w d_bias d_state_in")
+SelscanGrads = collections.namedtuple("SelscanGrads", "d_x d_dt d_a d_b d_c d_skip d_z d_dt_bias d_state_in")
+BlocknormGrads = collections.namedtuple("BlocknormGrads", "d_res d_y d_gate d_w_post d_b_post d_scale d_w_pre d_b_pre")
+
+
+def _need(ok, where, what):
+    if not ok:
+        err = ChelaError(ERR_INVALID_ARG, where)
+        err.args = ("%s: %s" % (err.args[0], what),)
+        raise err
+
+
+def _rows(t, where, name, lead, dtype, device, inner):
+    """Pointer and token stride of a token tensor [*lead, *inner]; the inner axes contiguous, one step between tokens."""
+    n = len(lead)
+    _need(t.dtype == dtype and t.device == device and tuple(t.shape) == (*lead, *inner), where,
+          "%s must be a %s tensor %s on %s" % (name, dtype, (*lead, *inner), device))
+    strides, step = t.stride(), 1
+    for i in range(len(t.shape) - 1, n - 1, -1):
+        _need(t.shape[i] == 1 or strides[i] == step, where, "%s: a token's values must be contiguous" % name)
+        step *= t.shape[i]
+    if n == 1:
+        stride = strides[0] if lead[0] > 1 else -(-step // 8) * 8
+    else:
+        stride = strides[1] if lead[1] > 1 else (strides[0] if lead[0] > 1 else -(-step // 8) * 8)
+        _need(lead[0] == 1 or strides[0] == lead[1] * stride, where, "%s: tokens must be a fixed distance apart" % name)
+    return _vp(t.data_ptr()), stride
+
+
+def _flat(t, where, name, shape, dtype, device):
+    """Pointer of an optional contiguous tensor of the given shape."""
+    if t is None:
+        return None
+    _need(t.dtype == dtype and t.device == device and tuple(t.shape) == tuple(shape) and t.is_contiguous(), where,
+          "%s must be a contiguous %s tensor %s on %s" % (name, dtype, tuple(shape), device))
+    return _vp(t.data_ptr())
+
+
+def _seqs(x, seq_offsets, where):
+    """(leading shape, S, T, offsets pointer) of a token tensor."""
+    _need(x.dtype in _DTYPES and x.dim() in (2, 3), where, "tokens must be [T, D] or [B, L, D] of float32 or bfloat16")
+    _need(x.is_cuda, where, "tensors must be on a CUDA device (there is no CPU fallback)")
+    lead = tuple(x.shape[:-1])
+    if seq_offsets is None:
+        return lead, lead[0] if len(lead) == 2 else 1, lead[0] * lead[1] if len(lead) == 2 else lead[0], None
+    _need(len(lead) == 1 and seq_offsets.dim() == 1 and seq_offsets.shape[0] >= 2, where,
+          "seq_offsets [S + 1] goes with packed tokens [T, D]")
+    return lead, seq_offsets.shape[0] - 1, lead[0], _flat(seq_offsets, where, "seq_offsets", (seq_offsets.shape[0],), torch.int32, x.device)
+
+
+class _on:
+    """The device of a call's tensors as the current one (no switch where it is already)."""
+
+    def __init__(self, device):
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard:
+            self.guard.__exit__(*exc)
+
+
+def _new(out, where, name, shape, dtype, device):
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _flat(out, where, name, shape, dtype, device)
+    return out
+
+
+def shortconv_carry_fwd(x, w, bias=None, act=True, state_in=None, state_out=None, seq_offsets=None, out=None):
+    """chela_shortconv_carry_fwd: (y, state_out).  x [T,D] or [B,L,D]; w [D,width] f32; states [S,width-1,D] like x."""
+    where = "chela_shortconv_carry_fwd"
+    lead, S, T, off = _seqs(x, seq_offsets, where)
+    D, width, dev = x.shape[-1], w.shape[-1], x.device
+    px, xs = _rows(x, where, "x", lead, x.dtype, dev, (D,))
+    y = _new(out, where, "out", x.shape, x.dtype, dev)
+    state_out = _new(state_out, where, "state_out", (S, width - 1, D), x.dtype, dev)
+    with _on(dev):
+        _check(lib().chela_shortconv_carry_fwd(
+            px, xs, _flat(w, where, "w", (D, width), torch.float32, dev), _flat(bias, where, "bias", (D,), torch.float32, dev),
+            _ptr(y), _flat(state_in, where, "state_in", (S, width - 1, D), x.dtype, dev), _ptr(state_out), off, S, T, D, width,
+            int(bool(act)), _dt(x), _stream()), where)
+    return y, state_out
+
+
+def shortconv_step(x, w, state, bias=None, act=True, state_out=None, out=None):
+    """chela_shortconv_step: y [S,D] for one new token per sequence; state [S,width-1,D] is updated in place unless
+    state_out is given."""
+    where = "chela_shortconv_step"
+    lead, _, S, _ = _seqs(x, None, where)
+    _need(len(lead) == 1, where, "x must be [S, D]")
+    D, width, dev = x.shape[-1], w.shape[-1], x.device
+    px, xs = _rows(x, where, "x", lead, x.dtype, dev, (D,))
+    y = _new(out, where, "out", x.shape, x.dtype, dev)
+    state_out = state if state_out is None else state_out
+    with _on(dev):
+        _check(lib().chela_shortconv_step(
+            px, xs, _flat(w, where, "w", (D, width), torch.float32, dev), _flat(bias, where, "bias", (D,), torch.float32, dev),
+            _ptr(y), _flat(state, where, "state", (S, width - 1, D), x.dtype, dev),
+            _flat(state_out, where, "state_out", (S, width - 1, D), x.dtype, dev), S, D, width, int(bool(act)), _dt(x), _stream()), where)
+    return y
+
+
+def shortconv_bwd(x, w, d_y, bias=None, act=True, state_in=None, d_state_out=None, seq_offsets=None, grad_dtype=F32,
+                  want_d_state=False, workspace=None):
+    """chela_shortconv_bwd: ShortconvGrads; d_x (and d_state_in, if wanted) of grad_dtype, d_w and d_bias f32."""
+    where = "chela_shortconv_bwd"
+    lead, S, T, off = _seqs(x, seq_offsets, where)
+    D, width, dev, gt = x.shape[-1], w.shape[-1], x.device, _tdtype(grad_dtype)
+    px, xs = _rows(x, where, "x", lead, x.dtype, dev, (D,))
+    pdy, dys = _rows(d_y, where, "d_y", lead, x.dtype, dev, (D,))
+    d_x = torch.empty(x.shape, dtype=gt, device=dev)
+    d_w = torch.empty((D, width), dtype=torch.float32, device=dev)
+    d_bias = torch.empty((D,), dtype=torch.float32, device=dev)
+    held = (S, width - 1, D)
+    d_state = torch.empty(held, dtype=gt, device=dev) if want_d_state else None
+    if workspace is None:
+        workspace = _workspace(int(lib().chela_shortconv_bwd_workspace_bytes(T, D, width)), dev)
+    with _on(dev):
+        _check(lib().chela_shortconv_bwd(
+            px, xs, _flat(w, where, "w", (D, width), torch.float32, dev), _flat(bias, where, "bias", (D,), torch.float32, dev), pdy, dys,
+            _flat(state_in, where, "state_in", held, x.dtype, dev), _flat(d_state_out, where, "d_state_out", held, x.dtype, dev),
+            _ptr(d_x), _ptr(d_w), _ptr(d_bias), _ptr(d_state), off, S, T, D, width, int(bool(act)), _dt(x), int(grad_dtype),
+            _ptr(workspace), workspace.numel(), _stream()), where)
+    return ShortconvGrads(d_x, d_w, d_bias, d_state)
+
+
+def _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state_in, seq_offsets):
+    lead, S, T, off = _seqs(x, seq_offsets, where)
+    D, dev, f32 = x.shape[-1], x.device, torch.float32
+    _need(a.dim() == 2 and b.dim() == len(lead) + 2, where, "a is [D, N], b and c are [..., G, N]")
+    G, N = b.shape[-2], b.shape[-1]
+    r = SelscanArgs()
+    r.x, r.x_stride = _rows(x, where, "x", lead, x.dtype, dev, (D,))
+    r.dt, r.dt_stride = _rows(dt, where, "dt", lead, x.dtype, dev, (D,))
+    r.b, r.b_stride = _rows(b, where, "b", lead, x.dtype, dev, (G, N))
+    r.c, r.c_stride = _rows(c, where, "c", lead, x.dtype, dev, (G, N))
+    if z is not None:
+        r.z, r.z_stride = _rows(z, where, "z", lead, x.dtype, dev, (D,))
+    r.a = _flat(a, where, "a", (D, N), f32, dev)
+    r.d_skip, r.dt_bias = _flat(d_skip, where, "d_skip", (D,), f32, dev), _flat(dt_bias, where, "dt_bias", (D,), f32, dev)
+    r.state_in, r.seq_offsets = _flat(state_in, where, "state_in", (S, D, N), f32, dev), off
+    r.S, r.T, r.D, r.N, r.G, r.softplus, r.in_dtype = S, T, D, N, G, int(bool(softplus)), _dt(x)
+    return r
+
+
+def selscan_checkpoints(T, S, D, N, device):
+    """A buffer for the states that selscan_fwd saves for selscan_bwd."""
+    return torch.empty(int(lib().chela_selscan_checkpoint_bytes(T, S, D, N)) // 4, dtype=torch.float32, device=device)
+
+
+def _checkpoints(t, where, r, device):
+    if t is None:
+        return None
+    need = int(lib().chela_selscan_checkpoint_bytes(r.T, r.S, r.D, r.N)) // 4
+    _need(t.dim() == 1 and t.shape[0] >= need, where, "checkpoints must come from selscan_checkpoints for these sizes")
+    return _flat(t, where, "checkpoints", (t.shape[0],), torch.float32, device)
+
+
+def selscan_fwd(x, dt, a, b, c, d_skip=None, z=None, dt_bias=None, softplus=True, state_in=None, state_out=None,
+                seq_offsets=None, checkpoints=None, out_dtype=None, out=None):
+    """chela_selscan_fwd: (y, state_out).  x, dt, z [T,D] or [B,L,D]; a [D,N] f32; b, c [...,G,N]; states [S,D,N] f32."""
+    where = "chela_selscan_fwd"
+    r = _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state_in, seq_offsets)
+    y = _new(out, where, "out", x.shape, x.dtype if out_dtype is None else _tdtype(out_dtype), x.device)
+    state_out = _new(state_out, where, "state_out", (r.S, r.D, r.N), torch.float32, x.device)
+    ckpt = _checkpoints(checkpoints, where, r, x.device)
+    with _on(x.device):
+        _check(lib().chela_selscan_fwd(ctypes.byref(r), _ptr(y), _ptr(state_out), ckpt, _dt(y), _stream()), where)
+    return y, state_out
+
+
+def selscan_step(x, dt, a, b, c, state, d_skip=None, z=None, dt_bias=None, softplus=True, state_out=None, out_dtype=None,
+                 out=None):
+    """chela_selscan_step: y [S,D] for one new token per sequence; state [S,D,N] f32 is updated in place unless state_out
+    is given."""
+    where = "chela_selscan_step"
+    _need(x.dim() == 2, where, "x must be [S, D]")
+    r = _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, None, None)
+    r.S = r.T
+    held = (r.S, r.D, r.N)
+    r.state_in = _flat(state, where, "state", held, torch.float32, x.device)
+    y = _new(out, where, "out", x.shape, x.dtype if out_dtype is None else _tdtype(out_dtype), x.device)
+    state_out = state if state_out is None else state_out
+    with _on(x.device):
+        _check(lib().chela_selscan_step(ctypes.byref(r), _ptr(y), _flat(state_out, where, "state_out", held, torch.float32, x.device),
+                                        _dt(y), _stream()), where)
+    return y
+
+
+def selscan_bwd(x, dt, a, b, c, d_y, d_skip=None, z=None, dt_bias=None, softplus=True, state_in=None, seq_offsets=None,
+                checkpoints=None, d_state_out=None, grad_dtype=F32, want_d_state=False, workspace=None):
+    """chela_selscan_bwd: SelscanGrads; d_x, d_dt, d_b, d_c, d_z of grad_dtype, the others f32 (None where not given)."""
+    where = "chela_selscan_bwd"
+    r = _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state_in, seq_offsets)
+    dev, gt, f32, held = x.device, _tdtype(grad_dtype), torch.float32, (r.S, r.D, r.N)
+    pdy, dys = _rows(d_y, where, "d_y", tuple(x.shape[:-1]), x.dtype, dev, (r.D,))
+    ckpt = _checkpoints(checkpoints, where, r, dev)
+    g = SelscanGrads(d_x=torch.empty(x.shape, dtype=gt, device=dev), d_dt=torch.empty(x.shape, dtype=gt, device=dev),
+                     d_a=torch.empty(a.shape, dtype=f32, device=dev), d_b=torch.empty(b.shape, dtype=gt, device=dev),
+                     d_c=torch.empty(c.shape, dtype=gt, device=dev),
+                     d_skip=None if d_skip is None else torch.empty((r.D,), dtype=f32, device=dev),
+                     d_z=None if z is None else torch.empty(x.shape, dtype=gt, device=dev),
+                     d_dt_bias=None if dt_bias is None else torch.empty((r.D,), dtype=f32, device=dev),
+                     d_state_in=torch.empty(held, dtype=f32, device=dev) if want_d_state else None)
+    if workspace is None:
+        workspace = _workspace(int(lib().chela_selscan_bwd_workspace_bytes(r.T, r.S, r.D, r.N, int(ckpt is not None))), dev)
+    with _on(dev):
+        _check(lib().chela_selscan_bwd(ctypes.byref(r), pdy, dys, _flat(d_state_out, where, "d_state_out", held, f32, dev), ckpt,
+                                       _ptr(g.d_x), _ptr(g.d_dt), _ptr(g.d_a), _ptr(g.d_b), _ptr(g.d_c), _ptr(g.d_skip), _ptr(g.d_z),
+                                       _ptr(g.d_dt_bias), _ptr(g.d_state_in), int(grad_dtype), _ptr(workspace), workspace.numel(),
+                                       _stream()), where)
+    return g
+
+
+def _blocknorm_args(where, res, y, gate, w_post, b_post, norm_post, scale, w_pre, b_pre, norm_pre, gate_act, gate_after, eps, in_dtype):
+    first = res if res is not None else y
+    _need(first is not None, where, "res or y must be given")
+    lead, _, _, _ = _seqs(first, None, where)
+    D, dev, f32 = first.shape[-1], first.device, torch.float32
+    r = BlocknormArgs()
+    if res is not None:
+        _need(res.dtype in _DTYPES, where, "res must be float32 or bfloat16")
+        r.res, r.res_stride = _rows(res, where, "res", lead, res.dtype, dev, (D,))
+    if y is not None:
+        _need(y.dtype in _DTYPES, where, "y must be float32 or bfloat16")
+        r.y, r.y_stride = _rows(y, where, "y", lead, y.dtype, dev, (D,))
+    if gate is not None:
+        _need(y is not None, where, "gate goes with y")
+        r.gate, r.gate_stride = _rows(gate, where, "gate", lead, y.dtype, dev, (D,))
+    for name, t in (("w_post", w_post), ("b_post", b_post), ("scale", scale), ("w_pre", w_pre), ("b_pre", b_pre)):
+        setattr(r, name, _flat(t, where, name, (D,), f32, dev))
+    r.T, r.D = first.numel() // D if D else 0, D
+    r.gate_act, r.gate_after, r.norm_post, r.norm_pre, r.eps = int(gate_act), int(bool(gate_after)), int(norm_post), int(norm_pre), float(eps)
+    r.in_dtype = _dt(y) if y is not None else in_dtype
+    r.res_dtype = _dt(first)
+    return r, first
+
+
+def blocknorm_fwd(res, y=None, gate=None, w_post=None, b_post=None, norm_post=NORM_RMS, scale=None, w_pre=None, b_pre=None,
+                  norm_pre=NORM_RMS, gate_act=1, gate_after=False, eps=1e-6, pre=True, out_dtype=None, res_out=None, out=None):
+    """chela_blocknorm_fwd: (r', o).  y=None: only the norm before a block (r' is res itself); pre=False: only gate, norm,
+    scale and residual behind one (o is None).  o is of out_dtype, or y's (without y: res's) dtype."""
+    where = "chela_blocknorm_fwd"
+    r, first = _blocknorm_args(where, res, y, gate, w_post, b_post, norm_post, scale, w_pre, b_pre, norm_pre, gate_act, gate_after, eps,
+                               F32 if res is None or res.dtype == torch.float32 else BF16)
+    _need(pre or y is not None, where, "nothing to compute")
+    dev = first.device
+    if y is not None:
+        res_out = _new(res_out, where, "res_out", first.shape, first.dtype, dev)
+    else:
+        _need(res_out is None, where, "res_out goes with y")
+    o = None
+    if pre:
+        o = _new(out, where, "out", first.shape, (y.dtype if y is not None else res.dtype) if out_dtype is None else _tdtype(out_dtype), dev)
+    with _on(dev):
+        _check(lib().chela_blocknorm_fwd(ctypes.byref(r), _ptr(res_out), _ptr(o), F32 if o is None else _dt(o), _stream()), where)
+    return res_out if y is not None else res, o
+
+
+def blocknorm_bwd(res_out, y=None, gate=None, d_o=None, d_res_out=None, w_post=None, b_post=None, norm_post=NORM_RMS, scale=None,
+                  w_pre=None, b_pre=None, norm_pre=NORM_RMS, gate_act=1, gate_after=False, eps=1e-6, grad_dtype=F32, workspace=None):
+    """chela_blocknorm_bwd: BlocknormGrads from r' (as blocknorm_fwd returned it), y and gate; d_o of y's dtype (without y:
+    res_out's), d_res_out of res_out's dtype, either may be None.  d_res is of res_out's dtype, d_y and d_gate of grad_dtype."""
+    where = "chela_blocknorm_bwd"
+    r, first = _blocknorm_args(where, res_out, y, gate, w_post, b_post, norm_post, scale, w_pre, b_pre, norm_pre, gate_act, gate_after, eps,
+                               F32 if res_out.dtype == torch.float32 else BF16)
+    dev, shape, gt, D = first.device, first.shape, _tdtype(grad_dtype), r.D
+    in_dtype = torch.float32 if r.in_dtype == F32 else torch.bfloat16
+    vec = lambda on: torch.empty((D,), dtype=torch.float32, device=dev) if on else None  # noqa: E731
+    g = BlocknormGrads(d_res=torch.empty(shape, dtype=first.dtype, device=dev),
+                       d_y=None if y is None else torch.empty(shape, dtype=gt, device=dev),
+                       d_gate=None if gate is None else torch.empty(shape, dtype=gt, device=dev),
+                       d_w_post=vec(w_post is not None), d_b_post=vec(b_post is not None), d_scale=vec(scale is not None),
+                       d_w_pre=vec(w_pre is not None), d_b_pre=vec(b_pre is not None))
+    if workspace is None:
+        workspace = _workspace(int(lib().chela_blocknorm_bwd_workspace_bytes(r.T, D)), dev)
+    with _on(dev):
+        _check(lib().chela_blocknorm_bwd(ctypes.byref(r), _flat(d_o, where, "d_o", shape, in_dtype, dev),
+                                         _flat(d_res_out, where, "d_res_out", shape, first.dtype, dev), _ptr(g.d_res), _ptr(g.d_y),
+                                         _ptr(g.d_gate), _ptr(g.d_w_post), _ptr(g.d_b_post), _ptr(g.d_scale), _ptr(g.d_w_pre),
+                                         _ptr(g.d_b_pre), int(grad_dtype), _ptr(workspace), workspace.numel(), _stream()), where)
+    return g

@@ -145,4 +145,30 @@ chela_status_t launch_affine_pair(const void *z, const void *alpha, const float 
 chela_status_t launch_gate_combine(const float *o, const void *g_a, const void *g_o, chela_dtype_t gate_dtype, const void *x,
                                    chela_dtype_t x_dtype, void *u, chela_dtype_t u_dtype, size_t n, cudaStream_t stream);
 
+// ---- operators over packed sequences (shortconv_carry.cu, selscan.cu, blocknorm.cu) -------------------------------
+
+chela_status_t launch_shortconv_carry(const void *x, long long x_stride, const float *w, const float *bias, void *y,
+                                      const void *state_in, void *state_out, const int *seq_offsets, int S, int T, int D, int width,
+                                      int act, chela_dtype_t io_dtype, cudaStream_t stream);
+size_t shortconv_bwd_workspace_bytes(int T, int D, int width);
+chela_status_t launch_shortconv_bwd(const void *x, long long x_stride, const float *w, const float *bias, const void *d_y,
+                                    long long d_y_stride, const void *state_in, const void *d_state_out, void *d_x, float *d_w,
+                                    float *d_bias, void *d_state_in, const int *seq_offsets, int S, int T, int D, int width, int act,
+                                    chela_dtype_t io_dtype, chela_dtype_t grad_dtype, void *workspace, cudaStream_t stream);
+
+size_t selscan_checkpoint_bytes(int T, int S, int D, int N);
+chela_status_t launch_selscan_fwd(const chela_selscan_args_t &a, void *y, float *state_out, void *ckpt, chela_dtype_t out_dtype,
+                                  cudaStream_t stream);
+chela_status_t launch_selscan_step(const chela_selscan_args_t &a, void *y, float *state_out, chela_dtype_t out_dtype, cudaStream_t stream);
+size_t selscan_bwd_workspace_bytes(int T, int S, int D, int N, bool have_ckpt);
+chela_status_t launch_selscan_bwd(const chela_selscan_args_t &a, const void *d_y, long long d_y_stride, const float *d_state_out,
+                                  const void *ckpt, void *d_x, void *d_dt, float *d_a, void *d_b, void *d_c, float *d_skip, void *d_z,
+                                  float *d_bias, float *d_state_in, chela_dtype_t grad_dtype, void *workspace, cudaStream_t stream);
+
+chela_status_t launch_blocknorm_fwd(const chela_blocknorm_args_t &a, void *res_out, void *o, chela_dtype_t out_dtype, cudaStream_t stream);
+size_t blocknorm_bwd_workspace_bytes(int T, int D);
+chela_status_t launch_blocknorm_bwd(const chela_blocknorm_args_t &a, const void *d_o, const void *d_res_out, void *d_res, void *d_y,
+                                    void *d_gate, float *d_w_post, float *d_b_post, float *d_scale, float *d_w_pre, float *d_b_pre,
+                                    chela_dtype_t grad_dtype, void *workspace, cudaStream_t stream);
+
 }  // namespace chela

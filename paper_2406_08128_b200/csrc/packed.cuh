@@ -1,0 +1,107 @@
+// Helpers of the operators over packed sequences (short convolution with carried inputs, selective scan, block norms).
+#pragma once
+#include "common.cuh"
+
+namespace chela {
+
+// Tokens of one sequence.  Offsets come from the device unchecked by the host, so they are clamped to [0, T] here:
+// a bad array then gives wrong results, never an access outside the tensors.
+struct SeqRange {
+    int start, len;
+};
+__device__ __forceinline__ int seq_start(const int *off, int s, int S, int T)
+{
+    return off ? min(max(off[s], 0), T) : (int)((long long)T / S * s);
+}
+__device__ __forceinline__ SeqRange seq_range(const int *off, int s, int S, int T)
+{
+    SeqRange r;
+    r.start = seq_start(off, s, S, T);
+    r.len = max(seq_start(off, s + 1, S, T) - r.start, 0);
+    return r;
+}
+
+// Blocks of K tokens that do not cross sequences, numbered without knowing the lengths on the host: sequence s owns the
+// blocks start_s / K + s ... start_{s+1} / K + s.  That is at least one and at least ceil(len / K) blocks, and there are
+// at most T / K + S in all.
+inline size_t packed_blocks(int T, int S, int K) { return (size_t)T / K + S; }
+__device__ __forceinline__ int packed_block_seq(const int *off, int S, int T, int K, long long block)
+{
+    int lo = 0, hi = S - 1;   // the last s with start_s / K + s <= block
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if ((long long)(seq_start(off, mid, S, T) / K) + mid <= block) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp_approx(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// e^x with the product x log2(e) kept to more than 32 bits: its rounding alone would cost |x| 2^-24.
+__device__ __forceinline__ float exp_acc(float x)
+{
+    const float p = x * kLog2e;
+    const float lo = fmaf(x, kLog2e, -p) + x * 1.925963033500e-8f;   // log2(e) - (float)log2(e)
+    const float e = ex2(p);
+    return (fabsf(p) < 1000.f) ? fmaf(e, lo * 0.6931471805599453f, e) : e;   // infinities and NaN: p alone
+}
+// sigmoid; for u far below zero the reciprocal of infinity is 0
+__device__ __forceinline__ float sigmoid_acc(float u) { return rcp_approx(1.0f + ex2(-u * kLog2e)); }
+
+// log(1 + e^v) = max(v, 0) + log1p(e^-|v|).  log1p(e)/e on [0, 1] is a polynomial of degree 9 fitted for this file
+// (weighted least squares iterated to equal ripple, relative error 5e-9; 1.6e-7 with fp32 Horner steps): the logarithm
+// of the rounded sum 1 + e would lose the small time steps (e = 1e-3 .. 1e-1) that these models work with.
+__device__ __forceinline__ float softplus_acc(float v)
+{
+    const float e = exp_acc(-fabsf(v));
+    float p = -3.244025400e-03f;
+    p = fmaf(p, e, 1.985146478e-02f);
+    p = fmaf(p, e, -5.695954338e-02f);
+    p = fmaf(p, e, 1.060365662e-01f);
+    p = fmaf(p, e, -1.530559361e-01f);
+    p = fmaf(p, e, 1.967594028e-01f);
+    p = fmaf(p, e, -2.495413423e-01f);
+    p = fmaf(p, e, 3.332996368e-01f);
+    p = fmaf(p, e, -4.999990165e-01f);
+    p = fmaf(p, e, 1.0f);
+    return fmaxf(v, 0.f) + (v == v ? p * e : v);
+}
+
+// pairs of fp32 values in one instruction
+__device__ __forceinline__ float2 mul2v(float2 a, float2 b)
+{
+    float2 d;
+    asm("{ .reg .b64 x, y; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mul.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x; }"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2v(float2 a, float2 b)
+{
+    float2 d;
+    asm("{ .reg .b64 x, y; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; add.rn.f32x2 x, x, y; mov.b64 {%0, %1}, x; }"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 fma2v(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{ .reg .b64 x, y, z; mov.b64 x, {%2, %3}; mov.b64 y, {%4, %5}; mov.b64 z, {%6, %7}; fma.rn.f32x2 x, x, y, z;"
+        " mov.b64 {%0, %1}, x; }"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 splat2(float a) { return make_float2(a, a); }
+
+}  // namespace chela

@@ -1,0 +1,349 @@
+// Short depthwise causal convolution over packed sequences with the last width - 1 inputs carried between calls, its
+// single-token form and its backward pass.  u_t = bias + sum_j w_j x_{t-j}, y = act(u).
+//
+// Bound by HBM: 2 bytes in and 2 out per bf16 element for 2 width flops.  A thread owns 4 channels (one 8-byte access
+// for bf16, a warp reads 256 contiguous bytes of a token) and kTok consecutive tokens of one sequence with the taps and the
+// previous inputs in registers, so every input is read once plus a halo of width - 1 rows per kTok.
+#include "packed.cuh"
+
+namespace chela {
+namespace {
+
+constexpr int kTok = 32;      // tokens of one forward work item
+constexpr int kBwdTok = 32;   // tokens of one backward work item
+
+struct ConvParams {
+    const void *x;
+    long long xs;
+    const float *w, *bias;
+    void *y;
+    const void *state_in;
+    void *state_out;
+    const int *off;
+    int S, T, D, width, act;
+};
+
+__device__ __forceinline__ float4 fma4(float4 a, float4 b, float4 c)
+{
+    return make_float4(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y), fmaf(a.z, b.z, c.z), fmaf(a.w, b.w, c.w));
+}
+__device__ __forceinline__ float4 add4(float4 a, float4 b) { return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w); }
+__device__ __forceinline__ float4 zero4() { return make_float4(0.f, 0.f, 0.f, 0.f); }
+__device__ __forceinline__ float silu_acc(float u) { return u * sigmoid_acc(u); }
+__device__ __forceinline__ float d_silu(float u)
+{
+    const float s = sigmoid_acc(u);
+    return s * fmaf(u, 1.f - s, 1.f);
+}
+
+// Input row at position t of a sequence that starts at row `start`: carried rows stand before position 0.
+template <typename T>
+__device__ __forceinline__ float4 row_at(const ConvParams &p, int s, int start, int len, int t, int c)
+{
+    if (t >= 0) return t < len ? load4(static_cast<const T *>(p.x) + (size_t)(start + t) * p.xs + c) : zero4();
+    const int r = p.width - 1 + t;
+    if (!p.state_in || r < 0) return zero4();
+    return load4(static_cast<const T *>(p.state_in) + ((size_t)s * (p.width - 1) + r) * p.D + c);
+}
+
+// The last width - 1 inputs of (carried rows | sequence).  Called by the one thread that owns these channels of the
+// sequence's first work item, after all its own reads of state_in, so both states may be the same buffer: state_out row r
+// comes from a row of state_in with an index >= r, so going upwards no row is written before it is read.
+template <typename T>
+__device__ __forceinline__ void store_state(const ConvParams &p, int s, const SeqRange &sr, int c)
+{
+    const int n = p.width - 1;
+    for (int r = 0; r < n; ++r) {
+        const float4 v = row_at<T>(p, s, sr.start, sr.len, sr.len - n + r, c);
+        store4(static_cast<T *>(p.state_out) + ((size_t)s * n + r) * p.D + c, v);
+    }
+}
+
+template <int W>
+__device__ __forceinline__ void load_taps(const float *w, int width, int c, float4 (&taps)[W])
+{
+#pragma unroll
+    for (int j = 0; j < W; ++j)
+        taps[j] = j < width ? make_float4(w[(size_t)c * width + j], w[(size_t)(c + 1) * width + j], w[(size_t)(c + 2) * width + j],
+                                          w[(size_t)(c + 3) * width + j])
+                            : zero4();
+}
+
+// W: taps held in registers (the width itself up to 4; 8 and 16 for the widths up to those, their extra taps zero).
+template <typename T, int W>
+__global__ void __launch_bounds__(256) conv_carry_kernel(const ConvParams p, long long items)
+{
+    constexpr int SUB = 4;
+    const int nvec = p.D / 4;
+    for (long long idx = blockIdx.x * (long long)blockDim.x + threadIdx.x; idx < items; idx += (long long)gridDim.x * blockDim.x) {
+        const int c = 4 * (int)(idx % nvec);
+        const long long blk = idx / nvec;
+        const int s = packed_block_seq(p.off, p.S, p.T, kTok, blk);
+        const SeqRange sr = seq_range(p.off, s, p.S, p.T);
+        const int b = (int)(blk - (sr.start / kTok + s)), t0 = b * kTok;
+        if (b < 0) continue;
+        if (t0 < sr.len) {
+            float4 taps[W], in[SUB + W - 1];
+            load_taps<W>(p.w, p.width, c, taps);
+            const float4 bias = p.bias ? load4(p.bias + c) : zero4();
+#pragma unroll
+            for (int i = 0; i < W - 1; ++i) in[i] = row_at<T>(p, s, sr.start, sr.len, t0 - (W - 1) + i, c);
+#pragma unroll 1
+            for (int t = t0; t < min(t0 + kTok, sr.len); t += SUB) {
+#pragma unroll
+                for (int i = 0; i < SUB; ++i) in[W - 1 + i] = row_at<T>(p, s, sr.start, sr.len, t + i, c);
+#pragma unroll
+                for (int i = 0; i < SUB; ++i) {
+                    if (t + i < sr.len) {
+                        float4 u = bias;
+#pragma unroll
+                        for (int j = 0; j < W; ++j) u = fma4(taps[j], in[W - 1 + i - j], u);
+                        if (p.act) u = make_float4(silu_acc(u.x), silu_acc(u.y), silu_acc(u.z), silu_acc(u.w));
+                        store4(static_cast<T *>(p.y) + (size_t)(sr.start + t + i) * p.D + c, u);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < W - 1; ++i) in[i] = in[SUB + i];
+            }
+        }
+        if (b == 0 && p.state_out) store_state<T>(p, s, sr, c);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ backward
+
+struct ConvBwdParams {
+    ConvParams f;
+    const void *dy;
+    long long dys;
+    const void *d_state_out;
+    void *d_x, *d_state_in;
+    float *part;   // [gridDim.y][width + 1][D]: taps, bias
+};
+
+// d_u at position t: d_y act'(u), zero outside the sequence
+template <typename T, int W>
+__device__ __forceinline__ float4 d_u_at(const ConvBwdParams &q, const SeqRange &sr, int t, int c, const float4 (&taps)[W], float4 bias,
+                                         const float4 *in /* in[j] = x_{t-W+1+j} */)
+{
+    if (t >= sr.len) return zero4();
+    float4 d = load4(static_cast<const T *>(q.dy) + (size_t)(sr.start + t) * q.dys + c);
+    if (q.f.act) {
+        float4 u = bias;
+#pragma unroll
+        for (int j = 0; j < W; ++j) u = fma4(taps[j], in[W - 1 - j], u);
+        d = make_float4(d.x * d_silu(u.x), d.y * d_silu(u.y), d.z * d_silu(u.z), d.w * d_silu(u.w));
+    }
+    return d;
+}
+
+// A CTA: 32 lanes x 4 channels, 8 warps that walk work items of kBwdTok tokens; the taps' gradients stay in registers until
+// the end, are added over the warps in shared memory and leave as one partial sum per CTA row (a fixed order, no atomics).
+// d_x_t = sum_j w_j d_u_{t+j}: a thread evaluates the d_u of its tokens and of the W - 1 behind them.
+template <typename T, typename TG, int W>
+__global__ void __launch_bounds__(256) conv_bwd_kernel(const ConvBwdParams q, long long nblocks)
+{
+    const ConvParams &p = q.f;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c = (blockIdx.x * 32 + lane) * 4;
+    const bool live = c < p.D;
+    float4 taps[W], dw[W], db = zero4(), bias = zero4();
+#pragma unroll
+    for (int j = 0; j < W; ++j) dw[j] = zero4();
+    if (live) {
+        load_taps<W>(p.w, p.width, c, taps);
+        if (p.bias) bias = load4(p.bias + c);
+        for (long long blk = (long long)blockIdx.y * 8 + warp; blk < nblocks; blk += (long long)gridDim.y * 8) {
+            const int s = packed_block_seq(p.off, p.S, p.T, kBwdTok, blk);
+            const SeqRange sr = seq_range(p.off, s, p.S, p.T);
+            const int b = (int)(blk - (sr.start / kBwdTok + s)), t0 = b * kBwdTok;
+            if (b < 0 || t0 >= sr.len) continue;
+            const int end = min(t0 + kBwdTok, sr.len);
+            float4 in[W], du[W];   // in[j] = x_{t-W+1+j}; du[j] = d_u_{t-j}
+#pragma unroll
+            for (int j = 0; j < W; ++j) du[j] = zero4();
+#pragma unroll
+            for (int j = 1; j < W; ++j) in[j] = row_at<T>(p, s, sr.start, sr.len, t0 - W + j, c);
+            in[0] = zero4();
+#pragma unroll 2
+            for (int t = t0; t < end + W - 1; ++t) {
+#pragma unroll
+                for (int j = 0; j < W - 1; ++j) in[j] = in[j + 1];
+                in[W - 1] = row_at<T>(p, s, sr.start, sr.len, t, c);
+#pragma unroll
+                for (int j = W - 1; j > 0; --j) du[j] = du[j - 1];
+                du[0] = d_u_at<T, W>(q, sr, t, c, taps, bias, in);
+                if (t < end) {
+#pragma unroll
+                    for (int j = 0; j < W; ++j) dw[j] = fma4(du[0], in[W - 1 - j], dw[j]);
+                    db = add4(db, du[0]);
+                }
+                const int tx = t - (W - 1);   // all terms of d_x at this position are there now
+                if (tx >= t0) {
+                    float4 dx = zero4();
+#pragma unroll
+                    for (int j = 0; j < W; ++j) dx = fma4(taps[j], du[W - 1 - j], dx);
+                    const int r = tx - (sr.len - (p.width - 1));
+                    if (q.d_state_out && r >= 0)
+                        dx = add4(dx, load4(static_cast<const T *>(q.d_state_out) + ((size_t)s * (p.width - 1) + r) * p.D + c));
+                    store4(static_cast<TG *>(q.d_x) + (size_t)(sr.start + tx) * p.D + c, dx);
+                }
+            }
+        }
+    }
+    if (!q.part) return;
+    __shared__ float4 red[8][32];
+#pragma unroll 1
+    for (int j = 0; j <= p.width; ++j) {
+        float4 v = db;
+#pragma unroll
+        for (int k = 0; k < W; ++k)
+            if (k == j && j < p.width) v = dw[k];
+        __syncthreads();
+        red[warp][lane] = v;
+        __syncthreads();
+        if (warp == 0 && live) {
+            float4 o = zero4();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o = add4(o, red[k][lane]);
+            *reinterpret_cast<float4 *>(q.part + ((size_t)blockIdx.y * (p.width + 1) + j) * p.D + c) = o;
+        }
+    }
+}
+
+// d_state_in row r is position r - (width - 1): sum_j w_j d_u of the tokens it reached, plus what passes straight through
+// to state_out where the sequence is shorter than the state.
+template <typename T, typename TG>
+__global__ void __launch_bounds__(128) conv_bwd_state_kernel(const ConvBwdParams q)
+{
+    const ConvParams &p = q.f;
+    const int n = p.width - 1, nvec = p.D / 4;
+    const long long idx = blockIdx.x * (long long)blockDim.x + threadIdx.x;
+    if (idx >= (long long)p.S * n * nvec) return;
+    const int c = 4 * (int)(idx % nvec), r = (int)(idx / nvec % n), s = (int)(idx / nvec / n);
+    const SeqRange sr = seq_range(p.off, s, p.S, p.T);
+    const int pos = r - n;
+    float4 acc = zero4();
+    const float4 bias = p.bias ? load4(p.bias + c) : zero4();
+    auto tap = [&](int j) {
+        return make_float4(p.w[(size_t)c * p.width + j], p.w[(size_t)(c + 1) * p.width + j], p.w[(size_t)(c + 2) * p.width + j],
+                           p.w[(size_t)(c + 3) * p.width + j]);
+    };
+    for (int t = 0; t <= pos + n && t < sr.len; ++t) {
+        float4 d = load4(static_cast<const T *>(q.dy) + (size_t)(sr.start + t) * q.dys + c);
+        if (p.act) {
+            float4 u = bias;
+            for (int j = 0; j < p.width; ++j) u = fma4(tap(j), row_at<T>(p, s, sr.start, sr.len, t - j, c), u);
+            d = make_float4(d.x * d_silu(u.x), d.y * d_silu(u.y), d.z * d_silu(u.z), d.w * d_silu(u.w));
+        }
+        acc = fma4(tap(t - pos), d, acc);
+    }
+    const int k = pos - (sr.len - n);
+    if (q.d_state_out && k >= 0) acc = add4(acc, load4(static_cast<const T *>(q.d_state_out) + ((size_t)s * n + k) * p.D + c));
+    store4(static_cast<TG *>(q.d_state_in) + ((size_t)s * n + r) * p.D + c, acc);
+}
+
+__global__ void __launch_bounds__(256) conv_bwd_sum_kernel(const float *part, float *d_w, float *d_bias, int nparts, int D, int width)
+{
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;   // j * D + c
+    if (i >= (width + 1) * D) return;
+    float o = 0.f;
+    for (int k = 0; k < nparts; ++k) o += part[(size_t)k * (width + 1) * D + i];
+    const int j = i / D, c = i % D;
+    if (j < width) {
+        if (d_w) d_w[(size_t)c * width + j] = o;
+    } else if (d_bias) {
+        d_bias[c] = o;
+    }
+}
+
+int conv_bwd_rows(int T, int D)
+{
+    // CTA rows that walk the work items: about four CTAs per SM over all channel columns, no more than there are items
+    const int cols = (D / 4 + 31) / 32;
+    const int want = (148 * 4 + cols - 1) / cols, most = (T / kBwdTok + 8) / 8;
+    return want < most ? want : (most < 1 ? 1 : most);
+}
+
+template <typename T>
+chela_status_t fwd_w(const ConvParams &p, cudaStream_t stream)
+{
+    const long long items = (long long)packed_blocks(p.T, p.S, kTok) * (p.D / 4);
+    const long long need = (items + 255) / 256;
+    const unsigned grid = (unsigned)(need < 148 * 64 ? need : 148 * 64);
+    switch (p.width) {
+    case 1: conv_carry_kernel<T, 1><<<grid, 256, 0, stream>>>(p, items); break;
+    case 2: conv_carry_kernel<T, 2><<<grid, 256, 0, stream>>>(p, items); break;
+    case 3: conv_carry_kernel<T, 3><<<grid, 256, 0, stream>>>(p, items); break;
+    case 4: conv_carry_kernel<T, 4><<<grid, 256, 0, stream>>>(p, items); break;
+    case 5: case 6: case 7: case 8: conv_carry_kernel<T, 8><<<grid, 256, 0, stream>>>(p, items); break;
+    default: conv_carry_kernel<T, 16><<<grid, 256, 0, stream>>>(p, items); break;
+    }
+    return last_launch_status();
+}
+
+template <typename T, typename TG>
+chela_status_t bwd_w(const ConvBwdParams &q, float *d_w, float *d_bias, cudaStream_t stream)
+{
+    const ConvParams &p = q.f;
+    const long long nblocks = (long long)packed_blocks(p.T, p.S, kBwdTok);
+    const int rows = conv_bwd_rows(p.T, p.D);
+    const dim3 grid((p.D / 4 + 31) / 32, rows);
+    switch (p.width) {
+    case 1: conv_bwd_kernel<T, TG, 1><<<grid, 256, 0, stream>>>(q, nblocks); break;
+    case 2: conv_bwd_kernel<T, TG, 2><<<grid, 256, 0, stream>>>(q, nblocks); break;
+    case 3: conv_bwd_kernel<T, TG, 3><<<grid, 256, 0, stream>>>(q, nblocks); break;
+    case 4: conv_bwd_kernel<T, TG, 4><<<grid, 256, 0, stream>>>(q, nblocks); break;
+    case 5: case 6: case 7: case 8: conv_bwd_kernel<T, TG, 8><<<grid, 256, 0, stream>>>(q, nblocks); break;
+    default: conv_bwd_kernel<T, TG, 16><<<grid, 256, 0, stream>>>(q, nblocks); break;
+    }
+    chela_status_t st = last_launch_status();
+    if (st == CHELA_OK && q.part) {
+        conv_bwd_sum_kernel<<<((p.width + 1) * p.D + 255) / 256, 256, 0, stream>>>(q.part, d_w, d_bias, rows, p.D, p.width);
+        st = last_launch_status();
+    }
+    if (st == CHELA_OK && q.d_state_in) {
+        const long long n = (long long)p.S * (p.width - 1) * (p.D / 4);
+        conv_bwd_state_kernel<T, TG><<<(unsigned)((n + 127) / 128), 128, 0, stream>>>(q);
+        st = last_launch_status();
+    }
+    return st;
+}
+
+}  // namespace
+
+chela_status_t launch_shortconv_carry(const void *x, long long x_stride, const float *w, const float *bias, void *y,
+                                      const void *state_in, void *state_out, const int *seq_offsets, int S, int T, int D, int width,
+                                      int act, chela_dtype_t io_dtype, cudaStream_t stream)
+{
+    const bool held = width > 1;
+    const ConvParams p = {x, x_stride, w, bias, y, held ? state_in : nullptr, held ? state_out : nullptr, seq_offsets, S, T, D, width, act};
+    return io_dtype == CHELA_F32 ? fwd_w<float>(p, stream) : fwd_w<__nv_bfloat16>(p, stream);
+}
+
+size_t shortconv_bwd_workspace_bytes(int T, int D, int width)
+{
+    return align_up((size_t)conv_bwd_rows(T, D) * (width + 1) * D * sizeof(float), 256);
+}
+
+chela_status_t launch_shortconv_bwd(const void *x, long long x_stride, const float *w, const float *bias, const void *d_y,
+                                    long long d_y_stride, const void *state_in, const void *d_state_out, void *d_x, float *d_w,
+                                    float *d_bias, void *d_state_in, const int *seq_offsets, int S, int T, int D, int width, int act,
+                                    chela_dtype_t io_dtype, chela_dtype_t grad_dtype, void *workspace, cudaStream_t stream)
+{
+    const bool held = width > 1;
+    ConvBwdParams q = {};
+    q.f = ConvParams{x, x_stride, w, bias, nullptr, held ? state_in : nullptr, nullptr, seq_offsets, S, T, D, width, act};
+    q.dy = d_y;
+    q.dys = d_y_stride;
+    q.d_state_out = held ? d_state_out : nullptr;
+    q.d_x = d_x;
+    q.d_state_in = held ? d_state_in : nullptr;
+    q.part = d_w || d_bias ? static_cast<float *>(workspace) : nullptr;
+    if (io_dtype == CHELA_F32)
+        return grad_dtype == CHELA_F32 ? bwd_w<float, float>(q, d_w, d_bias, stream) : bwd_w<float, __nv_bfloat16>(q, d_w, d_bias, stream);
+    return grad_dtype == CHELA_F32 ? bwd_w<__nv_bfloat16, float>(q, d_w, d_bias, stream)
+                                   : bwd_w<__nv_bfloat16, __nv_bfloat16>(q, d_w, d_bias, stream);
+}
+
+}  // namespace chela

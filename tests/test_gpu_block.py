@@ -1,0 +1,555 @@
+"""GPU parity of the operators over packed sequences (short convolution with carried inputs, selective scan, block norms)
+against plain float64 forms.
+
+Tolerances are factors of the sums' majorants (block_ref, ``mag=True``).  A single precision operation is off by at most
+2^-24 of its result, the approximate exponential by 2^-22; a recurrence over L tokens multiplies L such decays, each off
+by at most 2^-21 (exponential, rounding of the exponent, time step), so states are within (L + 4) 2^-21 of their majorant and
+gradients, which chain two recurrences, within twice that.  Sums over T tokens or D channels add at most their count times
+2^-24.  bf16 outputs add half a step, 2^-8 of the value.
+"""
+import numpy as np
+import pytest
+
+import block_ref as ref
+from paper_2406_08128_b200 import chela, inputs
+from util import to_device, to_numpy
+
+pytestmark = pytest.mark.gpu
+
+BF16_HALF = 2.0 ** -8
+DT = {"f32": chela.F32, "bf16": chela.BF16}
+
+
+def f32(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).cuda()
+
+
+def i32(a):
+    import torch
+    return torch.from_numpy(np.asarray(a, dtype=np.int32)).cuda()
+
+
+def dev(a, dtype, extra=0):
+    """Device tensor; with ``extra`` a column slice of a wider one, so that its token stride is not its width."""
+    import torch
+    if a is None:
+        return None
+    if not extra:
+        return to_device(a, dtype)
+    flat = a.reshape(a.shape[0], -1)
+    wide = np.concatenate([np.full((flat.shape[0], extra), np.nan, np.float32), flat, np.full((flat.shape[0], extra), np.nan, np.float32)], 1)
+    t = to_device(np.ascontiguousarray(wide, dtype=np.float32), dtype)[:, extra:extra + flat.shape[1]]
+    return t if a.ndim == 2 else t.unflatten(1, a.shape[1:])
+
+
+def close(got, want, mag, factor, dtype="f32", extra=0.0):
+    got = to_numpy(got) if not isinstance(got, np.ndarray) else got
+    assert got.shape == want.shape
+    tol = factor * mag + (BF16_HALF * np.abs(want) if dtype == "bf16" else 0.0) + extra + 1e-30
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (np.argwhere(bad)[:3], got[bad][:3], want[bad][:3], np.max(np.abs(got - want) / tol))
+
+
+LENGTHS = [[1], [0, 1, 2, 0], [5, 0, 33, 1, 64], [16, 17, 15], [31, 32, 33], [127, 128, 129, 3], [300]]
+
+
+# ------------------------------------------------------------------------------------------------ short convolution
+
+def conv_inputs(seed, lengths, D, W, dtype, pad=0):
+    rng = np.random.default_rng(seed)
+    T = sum(lengths) + pad
+    r = lambda *s: inputs.round_storage(rng.standard_normal(s, dtype=np.float32), dtype)  # noqa: E731
+    x, dy = r(T, D), r(T, D)
+    w = (rng.standard_normal((D, W), dtype=np.float32) / np.sqrt(W)).astype(np.float32)
+    bias = rng.standard_normal(D, dtype=np.float32)
+    return x, w, bias, r(len(lengths), W - 1, D), dy, r(len(lengths), W - 1, D)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("W,D,act", [(1, 8, True), (2, 40, True), (3, 64, False), (4, 136, True), (7, 24, True), (16, 16, True)])
+@pytest.mark.parametrize("lengths", LENGTHS, ids=str)
+@pytest.mark.parametrize("carry", [True, False])
+def test_conv_forward_backward(dtype, W, D, act, lengths, carry):
+    pad = 3
+    x, w, bias, state, dy, d_so = conv_inputs(W * 100 + len(lengths), lengths, D, W, dtype, pad)
+    n = sum(lengths)
+    x[n:] = dy[n:] = np.nan   # no sequence's tokens
+    b = bias if D != 24 else None
+    st = state if carry else None
+    off = i32(ref.offsets(lengths))
+    out = dev(np.full((n + pad, D), 7.0, np.float32), dtype)
+    extra = 8 if D != 64 else 0
+    y, so = chela.shortconv_carry_fwd(dev(x, dtype, extra), f32(w), None if b is None else f32(b), act=act, state_in=dev(st, dtype),
+                                      seq_offsets=off, out=out)
+    want, want_s = ref.conv(x, w, b, lengths, st, act)
+    mag = ref.conv(np.abs(x), np.abs(w), None if b is None else np.abs(b), lengths, None if st is None else np.abs(st), False)[0]
+    # W + 1 roundings of the sum, silu with its exponential and reciprocal (slope at most 1.1)
+    close(y[:n], want[:n], mag[:n], (W + 8) * 2.0 ** -23, dtype)
+    assert np.all(to_numpy(y[n:]) == 7.0)
+    assert np.array_equal(to_numpy(so), want_s)
+
+    g = chela.shortconv_bwd(dev(x, dtype, extra), f32(w), dev(dy, dtype, extra), None if b is None else f32(b), act=act,
+                            state_in=dev(st, dtype), d_state_out=dev(d_so, dtype) if carry else None, seq_offsets=off,
+                            grad_dtype=DT[dtype], want_d_state=True)
+    args = (x, w, b, dy, lengths, st, d_so if carry else None, act)
+    r, m = ref.conv_bwd(*args), ref.conv_bwd(*args, mag=True)
+    sums = (W + 16 + n) * 2.0 ** -23
+    close(g.d_x[:n], r[0][:n], m[0][:n], (2 * W + 16) * 2.0 ** -23, dtype)
+    close(g.d_w, r[1], m[1], sums)
+    close(g.d_bias, r[2], m[2], sums)
+    close(g.d_state_in, r[3], m[3], (2 * W + 16) * 2.0 ** -23, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_conv_steps_continue_a_prompt(dtype):
+    """A prompt, then single tokens with the state updated in place, give the longer prompt's rows bit for bit; so does the
+    prompt cut into segments whose state is carried in place."""
+    import torch
+    S, L, D, W = 3, 41, 72, 4
+    x, w, bias, *_ = conv_inputs(5, [L] * S, D, W, dtype)
+    xd, wd, bd = dev(x, dtype).view(S, L, D), f32(w), f32(bias)
+    full, last = chela.shortconv_carry_fwd(xd, wd, bd)
+    cut = 30
+    y, state = chela.shortconv_carry_fwd(xd[:, :cut].contiguous(), wd, bd)
+    assert torch.equal(y, full[:, :cut])
+    for t in range(cut, L):
+        y = chela.shortconv_step(xd[:, t], wd, state, bd)
+        assert torch.equal(y, full[:, t])
+    assert torch.equal(state, last)
+    state = torch.zeros_like(state)
+    at = 0
+    for n in (1, 2, 7, 31):
+        y, state = chela.shortconv_carry_fwd(xd[:, at:at + n].contiguous(), wd, bd, state_in=state, state_out=state)
+        assert torch.equal(y, full[:, at:at + n])
+        at += n
+    assert torch.equal(state, last)
+
+
+# ------------------------------------------------------------------------------------------------ selective scan
+
+def scan_inputs(seed, lengths, D, N, G, dtype, pad=0):
+    rng = np.random.default_rng(seed)
+    T, S = sum(lengths) + pad, len(lengths)
+    r = lambda *s: inputs.round_storage(rng.standard_normal(s, dtype=np.float32), dtype)  # noqa: E731
+    v = {"x": r(T, D), "dt": r(T, D), "b": r(T, G, N), "c": r(T, G, N), "z": r(T, D)}
+    v["a"] = (-np.arange(1, N + 1, dtype=np.float32) * np.exp(0.3 * rng.standard_normal((D, N), dtype=np.float32))).astype(np.float32)
+    v["d_skip"] = rng.standard_normal(D, dtype=np.float32)
+    v["dt_bias"] = (-3.0 + rng.standard_normal(D, dtype=np.float32)).astype(np.float32)
+    v["state"] = rng.standard_normal((S, D, N), dtype=np.float32)
+    v["d_y"] = r(T, D)
+    v["d_state_out"] = rng.standard_normal((S, D, N), dtype=np.float32)
+    return v
+
+
+def scan_call(v, lengths, dtype, form, extra=0, **more):
+    z, skip, bias, carry, soft = form
+    args = [dev(v["x"], dtype, extra), dev(v["dt"], dtype, extra), f32(v["a"]), dev(v["b"], dtype, extra), dev(v["c"], dtype, extra)]
+    kw = {"d_skip": f32(v["d_skip"]) if skip else None, "z": dev(v["z"], dtype, extra) if z else None,
+          "dt_bias": f32(v["dt_bias"]) if bias else None, "softplus": soft, "state_in": f32(v["state"]) if carry else None,
+          "seq_offsets": i32(ref.offsets(lengths))}
+    return args, kw | more
+
+
+def scan_ref(v, lengths, form, mag=False, bwd=False):
+    z, skip, bias, carry, soft = form
+    kw = {"d_skip": v["d_skip"] if skip else None, "z": v["z"] if z else None, "dt_bias": v["dt_bias"] if bias else None,
+          "soft": soft, "state": v["state"] if carry else None, "mag": mag}
+    if bwd:
+        return ref.scan_bwd(v["x"], v["dt"], v["a"], v["b"], v["c"], v["d_y"], lengths,
+                            d_state_out=v["d_state_out"] if carry else None, **kw)
+    return ref.scan(v["x"], v["dt"], v["a"], v["b"], v["c"], lengths, **kw)
+
+
+FORMS = [(True, True, True, True, True), (False, False, False, False, True), (True, False, True, True, False)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,D,G", [(8, 24, 1), (16, 40, 1), (16, 128, 2), (32, 72, 1), (64, 64, 2), (64, 8, 1)])
+@pytest.mark.parametrize("lengths", LENGTHS, ids=str)
+@pytest.mark.parametrize("form", FORMS, ids=["all", "bare", "rawdt"])
+def test_scan_forward_backward(dtype, N, D, G, lengths, form):
+    import torch
+    pad = 2
+    v = scan_inputs(N + D + len(lengths), lengths, D, N, G, dtype, pad)
+    if not form[4]:   # time steps as they are
+        v["dt"] = inputs.round_storage(np.abs(v["dt"]) * np.float32(0.1), dtype)
+        v["dt_bias"] = np.abs(v["dt_bias"]) * np.float32(0.01)
+    n = sum(lengths)
+    for k in ("x", "dt", "b", "c", "z", "d_y"):
+        v[k][n:] = np.nan
+    extra = 8 if D != 40 else 0
+    out = dev(np.full((n + pad, D), 7.0, np.float32), dtype)
+    args, kw = scan_call(v, lengths, dtype, form, extra)
+    ckpt = chela.selscan_checkpoints(n + pad, len(lengths), D, N, "cuda")
+    y, last = chela.selscan_fwd(*args, **kw, out=out, checkpoints=ckpt)
+    want, want_s = scan_ref(v, lengths, form)
+    mag, mag_s = scan_ref(v, lengths, form, mag=True)
+    L = max(lengths)
+    tol = (L + 8) * 2.0 ** -21
+    close(y[:n], want[:n], mag[:n], tol, dtype)
+    close(last, want_s, mag_s, tol)
+    assert np.all(to_numpy(y[n:]) == 7.0)
+
+    d_so = f32(v["d_state_out"]) if form[3] else None
+    bw = lambda c: chela.selscan_bwd(*args, dev(v["d_y"], dtype, extra), **kw, checkpoints=c, d_state_out=d_so, grad_dtype=DT[dtype],  # noqa: E731
+                                     want_d_state=True)
+    g = bw(ckpt)
+    r, m = scan_ref(v, lengths, form, bwd=True), scan_ref(v, lengths, form, mag=True, bwd=True)
+    tol = 2 * (L + 8) * 2.0 ** -21
+    for k, more, dt in (("d_x", 0, dtype), ("d_dt", 0, dtype), ("d_z", 0, dtype), ("d_b", D // G, dtype), ("d_c", D // G, dtype),
+                        ("d_a", n, "f32"), ("d_skip", n, "f32"), ("d_dt_bias", n, "f32"), ("d_state_in", 0, "f32")):
+        got = getattr(g, k)
+        if got is None:
+            assert (k == "d_z" and not form[0]) or (k == "d_skip" and not form[1]) or (k == "d_dt_bias" and not form[2])
+            continue
+        sl = slice(0, n) if k in ("d_x", "d_dt", "d_z", "d_b", "d_c") else slice(None)
+        close(got[sl], r[k][sl], m[k][sl], tol + more * 2.0 ** -24, dt)
+    again = bw(None)   # checkpoints computed again, sums in the same order
+    for p, q in zip(g, again):
+        assert p is None or torch.equal(p[:n] if p.shape[0] == n + pad else p, q[:n] if q.shape[0] == n + pad else q)
+
+
+def test_scan_gradients_against_differences():
+    """Central differences of the float64 forward form along random directions."""
+    lengths, D, N, G = [37, 5], 16, 16, 1
+    form = FORMS[0]
+    v = scan_inputs(3, lengths, D, N, G, "f32")
+    args, kw = scan_call(v, lengths, "f32", form)
+    g = chela.selscan_bwd(*args, f32(v["d_y"]), **kw, d_state_out=f32(v["d_state_out"]), want_d_state=True)
+    rng = np.random.default_rng(4)
+
+    def loss(u):
+        y, last = scan_ref(u, lengths, form)
+        return (y * v["d_y"]).sum() + (last * v["d_state_out"]).sum()
+
+    for name, grad in (("x", g.d_x), ("dt", g.d_dt), ("a", g.d_a), ("b", g.d_b), ("c", g.d_c), ("d_skip", g.d_skip), ("z", g.d_z),
+                       ("dt_bias", g.d_dt_bias), ("state", g.d_state_in)):
+        way = rng.standard_normal(v[name].shape)
+        hi, lo = dict(v), dict(v)
+        step = 1e-4
+        hi[name], lo[name] = v[name].astype(np.float64) + step * way, v[name].astype(np.float64) - step * way
+        want = (loss(hi) - loss(lo)) / (2 * step)
+        got = (to_numpy(grad) * way).sum()
+        # second-order term of the difference (1e-8 x third derivatives) and single precision gradients
+        assert abs(got - want) <= 1e-4 * np.abs(to_numpy(grad) * way).sum(), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [8, 16, 32, 64])
+def test_scan_step_against_the_formula(dtype, N):
+    S, D, G = 5, 64, 2
+    form = FORMS[0]
+    v = scan_inputs(N, [1] * S, D, N, G, dtype)
+    args, kw = scan_call(v, [1] * S, dtype, form, 8)
+    kw.pop("seq_offsets")
+    state = kw.pop("state_in")
+    y = chela.selscan_step(*args, state, **kw, out_dtype=chela.F32)
+    want, want_s = scan_ref(v, [1] * S, form)
+    mag, mag_s = scan_ref(v, [1] * S, form, mag=True)
+    close(y, want, mag, 2.0 ** -18)
+    close(state, want_s, mag_s, 2.0 ** -18)
+
+
+def test_scan_segments_and_steps_continue_a_prompt():
+    """Segments with the state carried in place, then single tokens, against one call."""
+    S, L, D, N = 2, 150, 40, 16
+    form = FORMS[0]
+    v = scan_inputs(8, [L] * S, D, N, 1, "f32")
+    v["state"][:] = 0
+    args, kw = scan_call(v, [L] * S, "f32", form)
+    for k in ("seq_offsets", "state_in"):
+        kw.pop(k)
+    cut3 = lambda t, i, j: t.view(S, L, *t.shape[1:])[:, i:j].contiguous()  # noqa: E731
+    full, last = chela.selscan_fwd(*[t if k == 2 else cut3(t, 0, L) for k, t in enumerate(args)],
+                                   **{k: (cut3(t, 0, L) if k == "z" else t) for k, t in kw.items()})
+    import torch
+    state = torch.zeros(S, D, N, device="cuda")
+    mag, mag_s = scan_ref(v, [L] * S, form, mag=True)
+    mag = mag.reshape(S, L, D)
+    at = 0
+    for n in (1, 63, 64, 12):
+        seg = [t if k == 2 else cut3(t, at, at + n) for k, t in enumerate(args)]
+        y, state = chela.selscan_fwd(*seg, **{k: (cut3(t, at, at + n) if k == "z" else t) for k, t in kw.items()}, state_in=state,
+                                     state_out=state)
+        close(y, to_numpy(full[:, at:at + n]), mag[:, at:at + n], 2 * (L + 8) * 2.0 ** -21)
+        at += n
+    for t in range(at, L):
+        one = [u if k == 2 else u.view(S, L, *u.shape[1:])[:, t] for k, u in enumerate(args)]
+        y = chela.selscan_step(*one, state, **{k: (u.view(S, L, D)[:, t] if k == "z" else u) for k, u in kw.items()})
+        close(y, to_numpy(full[:, t]), mag[:, t], 2 * (L + 8) * 2.0 ** -21)
+    close(state, to_numpy(last), mag_s, 2 * (L + 8) * 2.0 ** -21)
+
+
+def test_scan_keeps_what_is_not_finite_where_it_is():
+    """NaN and infinities of one sequence stay in it; an infinitely fast decay forgets the state and nothing else."""
+    lengths, D, N = [20, 33, 9], 16, 16
+    form = FORMS[0]
+    v = scan_inputs(11, lengths, D, N, 1, "f32")
+    v["a"][3, 2] = -np.inf
+    clean_args, kw = scan_call(v, lengths, "f32", form)
+    clean, clean_s = chela.selscan_fwd(*clean_args, **kw)
+    fast = dict(v)
+    fast["a"] = v["a"].copy()
+    fast["a"][3, 2] = -1e30
+    want, want_s = scan_ref(fast, lengths, form)
+    mag, mag_s = scan_ref(fast, lengths, form, mag=True)
+    close(clean, want, mag, 50 * 2.0 ** -21)
+    close(clean_s, want_s, mag_s, 50 * 2.0 ** -21)
+    import torch
+    for value in (np.nan, np.inf):
+        u = {k: a.copy() for k, a in v.items()}
+        u["x"][25, 5] = value
+        u["b"][30] = value
+        args, kw = scan_call(u, lengths, "f32", form)
+        y, s = chela.selscan_fwd(*args, **kw)
+        assert torch.equal(y[:25], clean[:25]) and torch.equal(y[53:], clean[53:])
+        assert torch.equal(s[0], clean_s[0]) and torch.equal(s[2], clean_s[2])
+        assert torch.equal(y[25:30, :5], clean[25:30, :5]) and not torch.isfinite(y[31:53]).any()
+
+
+def test_scan_time_steps_down_to_tiny_ones():
+    """softplus far below and above zero keeps its relative precision: one token from a zero state gives dt x b."""
+    raw = np.array([-40.0, -20.0, -12.0, -7.0, -2.0, -0.5, 0.0, 0.5, 3.0, 19.0, 30.0, 88.0, -80.0, 1e-3, -1e-3, 100.0], dtype=np.float32)
+    D = raw.size
+    x = np.ones((1, D), np.float32)
+    a = -np.ones((D, 8), np.float32)
+    bc = np.ones((1, 1, 8), np.float32)
+    _, s = chela.selscan_fwd(f32(x), f32(raw[None]), f32(a), f32(bc), f32(bc))
+    want = np.repeat(ref.softplus(raw.astype(np.float64))[None, :, None], 8, 2)
+    assert np.max(np.abs(to_numpy(s) / want - 1)) <= 2.0 ** -21
+
+
+def test_many_sequences_and_offsets_beyond_32_bits_of_elements():
+    """70000 sequences (more than a grid's second axis could hold), and token strides that put the last rows more than 2^31
+    elements behind the first."""
+    import torch
+    S, D, N = 70000, 8, 8
+    rng = np.random.default_rng(2)
+    lengths = rng.integers(0, 3, S)
+    v = scan_inputs(6, [int(lengths.sum())], D, N, 1, "f32")
+    off = i32(ref.offsets(lengths))
+    args, kw = scan_call(v, [1], "f32", (False, True, True, False, True))
+    kw["seq_offsets"] = off
+    y, s = chela.selscan_fwd(*args, **kw)
+    want, want_s = ref.scan(v["x"], v["dt"], v["a"], v["b"], v["c"], lengths, d_skip=v["d_skip"], dt_bias=v["dt_bias"])
+    mag, mag_s = ref.scan(v["x"], v["dt"], v["a"], v["b"], v["c"], lengths, d_skip=v["d_skip"], dt_bias=v["dt_bias"], mag=True)
+    close(y, want, mag, 2.0 ** -18)
+    close(s, want_s, mag_s, 2.0 ** -18)
+
+    T, stride = 1100, 1 << 21   # 1100 rows x 2^21 elements = 4.6 GB of bf16
+    wide = torch.empty(T * stride, dtype=torch.bfloat16, device="cuda")
+    x = wide.as_strided((T, 64), (stride, 1))
+    x.copy_(torch.randn(T, 64, device="cuda"))
+    w = torch.randn(64, 4, device="cuda")
+    y, st = chela.shortconv_carry_fwd(x, w, seq_offsets=i32([0, T]))
+    y2, st2 = chela.shortconv_carry_fwd(x.contiguous(), w, seq_offsets=i32([0, T]))
+    assert torch.equal(y, y2) and torch.equal(st, st2)
+    bc = torch.randn(T, 1, 16, device="cuda").bfloat16()
+    a = -torch.rand(64, 16, device="cuda")
+    r1 = chela.selscan_fwd(x, x, a, bc, bc, z=x, seq_offsets=i32([0, 500, T]))
+    r2 = chela.selscan_fwd(x.contiguous(), x.contiguous(), a, bc, bc, z=x.contiguous(), seq_offsets=i32([0, 500, T]))
+    assert torch.equal(r1[0], r2[0]) and torch.equal(r1[1], r2[1])
+    n1 = chela.blocknorm_fwd(x, x)
+    n2 = chela.blocknorm_fwd(x.contiguous(), x.contiguous())
+    assert torch.equal(n1[0], n2[0]) and torch.equal(n1[1], n2[1])
+
+
+# ------------------------------------------------------------------------------------------------ block norms
+
+def norm_inputs(seed, T, D, dtype, res_dtype):
+    rng = np.random.default_rng(seed)
+    r = lambda dt, *s: inputs.round_storage(rng.standard_normal(s, dtype=np.float32), dt)  # noqa: E731
+    v = {"res": r(res_dtype, T, D), "y": r(dtype, T, D), "gate": r(dtype, T, D), "d_o": r(dtype, T, D), "d_r": r(res_dtype, T, D)}
+    for k in ("w_post", "b_post", "scale", "w_pre", "b_pre"):
+        v[k] = (1.0 + 0.3 * rng.standard_normal(D, dtype=np.float32)).astype(np.float32)
+    return v
+
+
+@pytest.mark.parametrize("dtype,res_dtype", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("T,D", [(1, 8), (3, 40), (7, 256), (5, 264), (9, 512), (33, 1000), (4, 1032), (5, 2048), (3, 4104), (2, 8192)])
+@pytest.mark.parametrize("post,pre", [(1, 1), (2, 2), (1, 2), (0, 1), (2, 0)])
+@pytest.mark.parametrize("gate_act,after", [(None, False), (1, False), (2, True), (0, True)])
+def test_block_norms(dtype, res_dtype, T, D, post, pre, gate_act, after):
+    v = norm_inputs(T + D + post, T, D, dtype, res_dtype)
+    eps = 1e-6
+    gate = None if gate_act is None else v["gate"]
+    kw = {"w_post": v["w_post"], "b_post": v["b_post"] if post == 2 else None, "norm_post": post, "scale": v["scale"],
+          "w_pre": v["w_pre"], "b_pre": v["b_pre"] if pre == 2 else None, "norm_pre": pre, "gate_act": gate_act or 0, "gate_after": after,
+          "eps": eps}
+    dkw = {k: (f32(a) if isinstance(a, np.ndarray) else a) for k, a in kw.items()}
+    r, o = chela.blocknorm_fwd(dev(v["res"], res_dtype, 8), dev(v["y"], dtype, 8), dev(gate, dtype, 16), **dkw)
+    want_r, want_o, keep = ref.junction(v["res"], v["y"], gate, **kw)
+    # row sums of D squares: D/32 roundings a lane and a tree; every factor a few roundings; terms at most a few units large
+    tol = (D / 32 + 64) * 2.0 ** -24
+    size_r = np.abs(v["res"]) + np.abs(v["scale"]) * (np.abs(keep["m"]) + np.abs(keep["ga"]) * 4)
+    close(r, want_r, size_r, tol, res_dtype)
+    _, inv = ref.normalised(want_r, pre, eps)
+    close(o, want_o, np.abs(want_o) + np.abs(v["w_pre"]) * (size_r * inv + 1) + np.abs(v["b_pre"]), 2 * tol, dtype)
+
+    rb = inputs.round_storage(want_r.astype(np.float32), res_dtype)   # r' as it is stored
+    g = chela.blocknorm_bwd(dev(rb, res_dtype), dev(v["y"], dtype, 8), dev(gate, dtype, 16), dev(v["d_o"], dtype), dev(v["d_r"], res_dtype),
+                            **dkw, grad_dtype=DT[dtype])
+    w = ref.junction_bwd(rb, v["y"], gate, v["d_o"], v["d_r"], **kw)
+    _, inv2 = ref.normalised(rb.astype(np.float64), pre, eps)
+    hat2 = np.abs(ref.normalised(rb.astype(np.float64), pre, eps)[0])
+    # majorants: |d| plus its projections on the row, whose means are at most the row's largest terms
+    top = lambda a: np.abs(a).max(1, keepdims=True)  # noqa: E731
+    do = np.abs(v["d_o"] * v["w_pre"])
+    size = np.abs(v["d_r"]) + inv2 * (do + (hat2 * top(hat2) + 1) * top(do))
+    close(g.d_res, w["d_res"], size, 4 * tol, res_dtype)
+    ga, hat, inv1 = np.abs(keep["ga"]), np.abs(keep["hat"]), keep["inv"]
+    dm = size * np.abs(v["scale"])
+    dn = dm * (ga if after else 1) * np.abs(v["w_post"])
+    dv = inv1 * (dn + (hat * top(hat) + 1) * top(dn))
+    close(g.d_y, w["d_y"], dv * (1 if after else ga), 8 * tol, dtype)
+    n_abs = hat * np.abs(v["w_post"]) + np.abs(v["b_post"])
+    if gate is not None:
+        slope = 1.0 + np.abs(v["gate"])
+        close(g.d_gate, w["d_gate"], (dm * n_abs if after else dv * np.abs(v["y"])) * slope, 8 * tol, dtype)
+    many = 8 * tol + T * 2.0 ** -24
+    close(g.d_w_pre, w["d_w_pre"], (np.abs(v["d_o"]) * (hat2 + 1)).sum(0), many)
+    close(g.d_scale, w["d_scale"], (size * n_abs * (ga if after else 1) + size).sum(0), many)
+    close(g.d_w_post, w["d_w_post"], (dm * (ga if after else 1) * (hat + 1)).sum(0), many)
+    if pre == 2:
+        close(g.d_b_pre, w["d_b_pre"], np.abs(v["d_o"]).sum(0), many)
+    if post == 2:
+        close(g.d_b_post, w["d_b_post"], (dm * (ga if after else 1)).sum(0), many)
+
+
+def test_block_norm_parts_alone():
+    """The norm before a first block, the norm behind a last one, no residual, one gradient missing, weights left out."""
+    T, D, eps = 6, 48, 1e-5
+    v = norm_inputs(2, T, D, "f32", "f32")
+    none = {"w_post": None, "b_post": None, "norm_post": 1, "scale": None, "w_pre": None, "b_pre": None, "norm_pre": 1, "gate_act": 1,
+            "gate_after": False, "eps": eps}
+    res, y = f32(v["res"]), f32(v["y"])
+    r, o = chela.blocknorm_fwd(res, eps=eps)
+    assert r is res
+    close(o, ref.junction(v["res"], None, None, **none)[1], 1.0, 1e-5)
+    r, o = chela.blocknorm_fwd(res, y, eps=eps, pre=False)
+    assert o is None
+    close(r, ref.junction(v["res"], v["y"], None, **none)[0], 1.0, 1e-5)
+    r, o = chela.blocknorm_fwd(None, y, f32(v["gate"]), eps=eps, pre=False)
+    close(r, ref.junction(None, v["y"], v["gate"], **none)[0], 1.0, 1e-5)
+    for d_o, d_r in ((v["d_o"], None), (None, v["d_r"])):
+        g = chela.blocknorm_bwd(res, y, None, None if d_o is None else f32(d_o), None if d_r is None else f32(d_r), eps=eps)
+        w = ref.junction_bwd(v["res"], v["y"], None, d_o, d_r, **none)
+        close(g.d_res, w["d_res"], 1.0, 1e-4)
+        close(g.d_y, w["d_y"], 1.0, 1e-4)
+    g = chela.blocknorm_bwd(res, d_o=f32(v["d_o"]), w_pre=f32(v["w_pre"]), eps=eps)
+    w = ref.junction_bwd(v["res"], None, None, v["d_o"], None, **{**none, "w_pre": v["w_pre"]})
+    close(g.d_res, w["d_res"], 1.0, 1e-4)
+    close(g.d_w_pre, w["d_w_pre"], 1.0, 1e-4)
+    assert g.d_y is None and g.d_scale is None
+
+
+def test_block_norm_in_place_constant_and_extreme_rows():
+    """res_out = res; rows of zeros and of one value, a large mean (its square alone would lose the deviation), a NaN row."""
+    import torch
+    D = 64
+    rows = np.zeros((5, D), np.float32)
+    rows[1] = 3.0
+    rows[2] = 4096.0 + np.arange(D) % 3
+    rows[3, 7] = np.nan
+    rows[4] = np.arange(D)
+    for kind in (1, 2):
+        _, o = chela.blocknorm_fwd(f32(rows), norm_pre=kind)
+        want = ref.junction(rows, None, None, None, None, 0, None, None, None, kind, 0, False, 1e-6)[1]
+        got = to_numpy(o)
+        assert np.isnan(got[3]).all()
+        ok = [0, 1, 2, 4]
+        # one part in 2^-24 of the largest value over the deviation (0.8 where the mean is 4097)
+        assert np.all(np.abs(got[ok] - want[ok]) <= 4097 * 2.0 ** -22)
+    res, y = torch.randn(9, D, device="cuda"), torch.randn(9, D, device="cuda")
+    want, o1 = chela.blocknorm_fwd(res, y)
+    got, o2 = chela.blocknorm_fwd(res, y, res_out=res)
+    assert got is res and torch.equal(got, want) and torch.equal(o1, o2)
+
+
+# ------------------------------------------------------------------------------------------------ calls
+
+def test_graph_replay_streams_and_repeated_calls_give_equal_bits():
+    import torch
+    lengths, D, N = [40, 0, 25, 90], 64, 16
+    v = scan_inputs(21, lengths, D, N, 1, "bf16")
+    args, kw = scan_call(v, lengths, "bf16", FORMS[0])
+    dy = dev(v["d_y"], "bf16")
+    xs, w, bias, cst, cdy, _ = (dev(a, "bf16") if i in (0, 3, 4) else f32(a) if i in (1, 2) else None
+                                for i, a in enumerate(conv_inputs(3, lengths, D, 4, "bf16")))
+    nv = norm_inputs(4, sum(lengths), D, "bf16", "f32")
+    res, ny, ngate, nd_o, nd_r = f32(nv["res"]), dev(nv["y"], "bf16"), dev(nv["gate"], "bf16"), dev(nv["d_o"], "bf16"), f32(nv["d_r"])
+    wp = f32(nv["w_pre"])
+
+    def run():
+        y, s = chela.selscan_fwd(*args, **kw)
+        g = chela.selscan_bwd(*args, dy, **kw, want_d_state=True)
+        cy, cs = chela.shortconv_carry_fwd(xs, w, bias, state_in=cst, seq_offsets=kw["seq_offsets"])
+        cg = chela.shortconv_bwd(xs, w, cdy, bias, state_in=cst, seq_offsets=kw["seq_offsets"])
+        r, o = chela.blocknorm_fwd(res, ny, ngate, w_pre=wp)
+        ng = chela.blocknorm_bwd(r, ny, ngate, nd_o, nd_r, w_pre=wp)
+        return [t for t in (y, s, *g, cy, cs, *cg, r, o, *ng) if t is not None]
+
+    first = [t.clone() for t in run()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        second = run()
+    torch.cuda.current_stream().wait_stream(side)
+    for p, q in zip(first, second):
+        assert torch.equal(p, q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = run()
+    for t in held:
+        t.fill_(3.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    for p, q in zip(first, held):
+        assert torch.equal(p, q)
+    # the graph reads its inputs when it runs
+    args[0].zero_()
+    graph.replay()
+    want = chela.selscan_fwd(*args, **kw)[0]
+    assert torch.equal(held[0], want) and not torch.equal(held[0], first[0])
+
+
+def test_a_selective_block_decodes_what_its_prompt_computed():
+    """norm -> projection -> short convolution -> x and dt projections -> scan -> projection -> junction with the next
+    block's norm, over a prompt with the states carried and then token by token, against one longer prompt."""
+    import torch
+    torch.manual_seed(0)
+    S, L, cut, D, inner, N, rank = 3, 40, 33, 128, 256, 16, 32
+    p = lambda *s, scale=1.0: torch.randn(*s, device="cuda") * scale  # noqa: E731
+    w_in, w_x, w_dt, w_out = p(D, 2 * inner, scale=D ** -0.5), p(inner, rank + 2 * N, scale=inner ** -0.5), p(rank, inner, scale=rank ** -0.5), \
+        p(inner, D, scale=inner ** -0.5)
+    conv_w, conv_b, a = p(inner, 4, scale=0.5), p(inner, scale=0.1), -torch.arange(1, N + 1, device="cuda").float().repeat(inner, 1)
+    bias, skip, n1, n2, s1 = p(inner) - 4.0, p(inner), 1 + p(D, scale=0.1), 1 + p(D, scale=0.1), torch.full((D,), 0.5, device="cuda")
+    x = p(S, L, D)
+    dense = lambda t, w: chela.dense_fwd(t.reshape(-1, t.shape[-1]), w, y_dtype=chela.F32).view(*t.shape[:-1], w.shape[1])  # noqa: E731
+
+    def block(res, conv_state, scan_state, step):
+        _, h = chela.blocknorm_fwd(res, w_pre=n1)
+        xz = dense(h, w_in)
+        u, z = xz[..., :inner], xz[..., inner:]
+        if step:
+            u = chela.shortconv_step(u, conv_w, conv_state, conv_b)
+        else:
+            u, conv_state = chela.shortconv_carry_fwd(u, conv_w, conv_b, state_in=conv_state)
+        proj = dense(u, w_x)
+        dt = dense(proj[..., :rank].contiguous(), w_dt)
+        b, c = (proj[..., k:k + N].unflatten(-1, (1, N)) for k in (rank, rank + N))
+        if step:
+            y = chela.selscan_step(u, dt, a, b, c, scan_state, d_skip=skip, z=z, dt_bias=bias)
+        else:
+            y, scan_state = chela.selscan_fwd(u, dt, a, b, c, d_skip=skip, z=z, dt_bias=bias, state_in=scan_state)
+        r, o = chela.blocknorm_fwd(res, dense(y, w_out), w_post=n2, scale=s1, w_pre=n1)
+        return r, o, conv_state, scan_state
+
+    full_r, full_o, *_ = block(x, None, None, False)
+    r, o, cs, ss = block(x[:, :cut].contiguous(), None, None, False)
+    bound = 2e-5 * full_o.abs().max().item()   # single precision projections of 256 terms summed in other orders
+    assert (o - full_o[:, :cut]).abs().max().item() <= bound
+    for t in range(cut, L):
+        r, o, cs, ss = block(x[:, t].contiguous(), cs, ss, True)
+        assert (r - full_r[:, t]).abs().max().item() <= bound and (o - full_o[:, t]).abs().max().item() <= bound
