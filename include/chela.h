@@ -393,11 +393,13 @@ typedef struct {
  * y : [T, D] out_dtype.  state_out : [S, D, N] fp32 or NULL, may be state_in's buffer.  checkpoints: NULL, or a device
  * buffer of chela_selscan_checkpoint_bytes that receives the states at every 32nd token of each sequence, which
  * chela_selscan_bwd then need not compute again.  y may be NULL when only state_out or checkpoints are wanted.
- * No workspace.
+ * workspace: chela_selscan_workspace_bytes (0 unless there are so few sequences and channels that the sequences are split
+ * into segments, whose states it holds).
  */
 size_t chela_selscan_checkpoint_bytes(int T, int S, int D, int N);
+size_t chela_selscan_workspace_bytes(int T, int S, int D, int N);
 chela_status_t chela_selscan_fwd(const chela_selscan_args_t *args, void *y, float *state_out, void *checkpoints,
-                                 chela_dtype_t out_dtype, cudaStream_t stream);
+                                 chela_dtype_t out_dtype, void *workspace, size_t workspace_bytes, cudaStream_t stream);
 
 /* One new token per sequence (T = S, seq_offsets NULL): reads and writes the state once.  state_in is required;
  * state_out (required) may be state_in's buffer. */

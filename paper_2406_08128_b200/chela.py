@@ -91,7 +91,8 @@ _SIGNATURES = {
     "chela_shortconv_bwd_workspace_bytes": (_c_size_t, [_c_int] * 3),
     "chela_shortconv_bwd": (_c_int, [_vp, _c_ll, _vp, _vp, _vp, _c_ll] + [_vp] * 7 + [_c_int] * 7 + [_vp, _c_size_t, _vp]),
     "chela_selscan_checkpoint_bytes": (_c_size_t, [_c_int] * 4),
-    "chela_selscan_fwd": (_c_int, [_vp] * 4 + [_c_int, _vp]),
+    "chela_selscan_workspace_bytes": (_c_size_t, [_c_int] * 4),
+    "chela_selscan_fwd": (_c_int, [_vp] * 4 + [_c_int, _vp, _c_size_t, _vp]),
     "chela_selscan_step": (_c_int, [_vp] * 3 + [_c_int, _vp]),
     "chela_selscan_bwd_workspace_bytes": (_c_size_t, [_c_int] * 5),
     "chela_selscan_bwd": (_c_int, [_vp, _vp, _c_ll] + [_vp] * 11 + [_c_int, _vp, _c_size_t, _vp]),
@@ -570,15 +571,19 @@ def _checkpoints(t, where, r, device):
 
 
 def selscan_fwd(x, dt, a, b, c, d_skip=None, z=None, dt_bias=None, softplus=True, state_in=None, state_out=None,
-                seq_offsets=None, checkpoints=None, out_dtype=None, out=None):
+                seq_offsets=None, checkpoints=None, out_dtype=None, out=None, workspace=None):
     """chela_selscan_fwd: (y, state_out).  x, dt, z [T,D] or [B,L,D]; a [D,N] f32; b, c [...,G,N]; states [S,D,N] f32."""
     where = "chela_selscan_fwd"
     r = _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state_in, seq_offsets)
     y = _new(out, where, "out", x.shape, x.dtype if out_dtype is None else _tdtype(out_dtype), x.device)
     state_out = _new(state_out, where, "state_out", (r.S, r.D, r.N), torch.float32, x.device)
     ckpt = _checkpoints(checkpoints, where, r, x.device)
+    if workspace is None:
+        need = int(lib().chela_selscan_workspace_bytes(r.T, r.S, r.D, r.N))
+        workspace = _workspace(need, x.device) if need else None
     with _on(x.device):
-        _check(lib().chela_selscan_fwd(ctypes.byref(r), _ptr(y), _ptr(state_out), ckpt, _dt(y), _stream()), where)
+        _check(lib().chela_selscan_fwd(ctypes.byref(r), _ptr(y), _ptr(state_out), ckpt, _dt(y), _ptr(workspace),
+                                       0 if workspace is None else workspace.numel(), _stream()), where)
     return y, state_out
 
 

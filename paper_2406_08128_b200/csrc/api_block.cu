@@ -119,14 +119,23 @@ size_t chela_selscan_checkpoint_bytes(int T, int S, int D, int N)
     return selscan_checkpoint_bytes(T, S, D, N);
 }
 
+size_t chela_selscan_workspace_bytes(int T, int S, int D, int N)
+{
+    if (T < 1 || S < 1 || D < 1 || D % 8 != 0 || (N != 8 && N != 16 && N != 32 && N != 64)) return 0;
+    return selscan_workspace_bytes(T, S, D, N);
+}
+
 chela_status_t chela_selscan_fwd(const chela_selscan_args_t *args, void *y, float *state_out, void *checkpoints,
-                                 chela_dtype_t out_dtype, cudaStream_t stream)
+                                 chela_dtype_t out_dtype, void *workspace, size_t workspace_bytes, cudaStream_t stream)
 {
     const chela_status_t st = check_scan(args);
     if (st != CHELA_OK) return st;
-    if (!dtype_ok(out_dtype) || (!y && !state_out && !checkpoints) || !aligned16(y) || !aligned16(state_out) || !aligned16(checkpoints))
+    if (!dtype_ok(out_dtype) || (!y && !state_out && !checkpoints) || !aligned16(y) || !aligned16(state_out) || !aligned16(checkpoints) ||
+        !aligned16(workspace))
         return CHELA_ERR_INVALID_ARG;
-    return launch_selscan_fwd(*args, y, state_out, checkpoints, out_dtype, stream);
+    const size_t need = selscan_workspace_bytes(args->T, args->S, args->D, args->N);
+    if (need && (!workspace || workspace_bytes < need)) return CHELA_ERR_WORKSPACE;
+    return launch_selscan_fwd(*args, y, state_out, checkpoints, out_dtype, workspace, stream);
 }
 
 chela_status_t chela_selscan_step(const chela_selscan_args_t *args, void *y, float *state_out, chela_dtype_t out_dtype,

@@ -157,8 +157,9 @@ chela_status_t launch_shortconv_bwd(const void *x, long long x_stride, const flo
                                     chela_dtype_t io_dtype, chela_dtype_t grad_dtype, void *workspace, cudaStream_t stream);
 
 size_t selscan_checkpoint_bytes(int T, int S, int D, int N);
+size_t selscan_workspace_bytes(int T, int S, int D, int N);
 chela_status_t launch_selscan_fwd(const chela_selscan_args_t &a, void *y, float *state_out, void *ckpt, chela_dtype_t out_dtype,
-                                  cudaStream_t stream);
+                                  void *workspace, cudaStream_t stream);
 chela_status_t launch_selscan_step(const chela_selscan_args_t &a, void *y, float *state_out, chela_dtype_t out_dtype, cudaStream_t stream);
 size_t selscan_bwd_workspace_bytes(int T, int S, int D, int N, bool have_ckpt);
 chela_status_t launch_selscan_bwd(const chela_selscan_args_t &a, const void *d_y, long long d_y_stride, const float *d_state_out,

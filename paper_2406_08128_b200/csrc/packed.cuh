@@ -49,35 +49,8 @@ __device__ __forceinline__ float rcp_approx(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// e^x with the product x log2(e) kept to more than 32 bits: its rounding alone would cost |x| 2^-24.
-__device__ __forceinline__ float exp_acc(float x)
-{
-    const float p = x * kLog2e;
-    const float lo = fmaf(x, kLog2e, -p) + x * 1.925963033500e-8f;   // log2(e) - (float)log2(e)
-    const float e = ex2(p);
-    return (fabsf(p) < 1000.f) ? fmaf(e, lo * 0.6931471805599453f, e) : e;   // infinities and NaN: p alone
-}
 // sigmoid; for u far below zero the reciprocal of infinity is 0
 __device__ __forceinline__ float sigmoid_acc(float u) { return rcp_approx(1.0f + ex2(-u * kLog2e)); }
-
-// log(1 + e^v) = max(v, 0) + log1p(e^-|v|).  log1p(e)/e on [0, 1] is a polynomial of degree 9 fitted for this file
-// (weighted least squares iterated to equal ripple, relative error 5e-9; 1.6e-7 with fp32 Horner steps): the logarithm
-// of the rounded sum 1 + e would lose the small time steps (e = 1e-3 .. 1e-1) that these models work with.
-__device__ __forceinline__ float softplus_acc(float v)
-{
-    const float e = exp_acc(-fabsf(v));
-    float p = -3.244025400e-03f;
-    p = fmaf(p, e, 1.985146478e-02f);
-    p = fmaf(p, e, -5.695954338e-02f);
-    p = fmaf(p, e, 1.060365662e-01f);
-    p = fmaf(p, e, -1.530559361e-01f);
-    p = fmaf(p, e, 1.967594028e-01f);
-    p = fmaf(p, e, -2.495413423e-01f);
-    p = fmaf(p, e, 3.332996368e-01f);
-    p = fmaf(p, e, -4.999990165e-01f);
-    p = fmaf(p, e, 1.0f);
-    return fmaxf(v, 0.f) + (v == v ? p * e : v);
-}
 
 // pairs of fp32 values in one instruction
 __device__ __forceinline__ float2 mul2v(float2 a, float2 b)
@@ -103,5 +76,30 @@ __device__ __forceinline__ float2 fma2v(float2 a, float2 b, float2 c)
     return d;
 }
 __device__ __forceinline__ float2 splat2(float a) { return make_float2(a, a); }
+
+// log(1 + e^v) = max(v, 0) + log1p(e^-|v|).  log1p(e)/e on [0, 1] is a polynomial of degree 9 fitted for this file
+// (weighted least squares iterated to equal ripple, relative error 5e-9; 1.6e-7 with fp32 Horner steps): the logarithm
+// of the rounded sum 1 + e would lose the small time steps (e = 1e-3 .. 1e-1) that these models work with.  The
+// exponential's argument |v| log2(e) is rounded to p; what p lost, |v| - p ln 2, is put back to first order.
+__device__ __forceinline__ float2 softplus_acc(float2 v)
+{
+    // NaN stays; above 100 the exponential is below every normal number
+    const float2 x = make_float2(fabsf(v.x) > 100.f ? 100.f : fabsf(v.x), fabsf(v.y) > 100.f ? 100.f : fabsf(v.y));
+    const float2 t = mul2v(x, splat2(kLog2e)), r = fma2v(t, splat2(0.6931471805599453f), make_float2(-x.x, -x.y));
+    float2 e = make_float2(ex2(-t.x), ex2(-t.y));
+    e = fma2v(e, r, e);
+    float2 p = splat2(-3.244025400e-03f);
+    p = fma2v(p, e, splat2(1.985146478e-02f));
+    p = fma2v(p, e, splat2(-5.695954338e-02f));
+    p = fma2v(p, e, splat2(1.060365662e-01f));
+    p = fma2v(p, e, splat2(-1.530559361e-01f));
+    p = fma2v(p, e, splat2(1.967594028e-01f));
+    p = fma2v(p, e, splat2(-2.495413423e-01f));
+    p = fma2v(p, e, splat2(3.332996368e-01f));
+    p = fma2v(p, e, splat2(-4.999990165e-01f));
+    p = fma2v(p, e, splat2(1.0f));
+    return fma2v(p, e, make_float2(fmaxf(v.x, 0.f), fmaxf(v.y, 0.f)));
+}
+__device__ __forceinline__ float softplus_acc(float v) { return softplus_acc(splat2(v)).x; }
 
 }  // namespace chela

@@ -26,6 +26,10 @@ struct ScanParams {
     int S, T, D, G, softplus;
     void *y;
     float *state_out, *ckpt;
+    // a sequence split into segments of seg tokens (0: not split): seg_state [segments][D][N]; seg_sum [segments][D] is
+    // given in the pass that finds the segments' ends from zero states
+    int seg;
+    float *seg_state, *seg_sum;
 };
 
 __device__ __forceinline__ float4 zero4() { return make_float4(0.f, 0.f, 0.f, 0.f); }
@@ -44,164 +48,343 @@ __device__ __forceinline__ float gate_f(float z) { return z * sigmoid_acc(z); }
 
 // ------------------------------------------------------------------------------------------------ forward
 
-template <typename TI, typename TO, int N, int WD, int WT>
-__global__ void __launch_bounds__(32 * WD * WT) selscan_fwd_kernel(const ScanParams p)
+__device__ __forceinline__ void named_sync(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ void named_arrive(int id) { asm volatile("bar.arrive %0, 64;" ::"r"(id) : "memory"); }
+// 16 bytes from global to shared memory, zeros where ok is false (the address is then not read)
+__device__ __forceinline__ void copy16(void *dst, const void *src, bool ok)
 {
-    constexpr int R = N / 4, CPW = 32 / R, DC = CPW * WD, TOK = 16, TILE = TOK * WT, NT = 32 * WD * WT;
-    constexpr int NV = TILE * DC / 4, VPT = (NV + NT - 1) / NT;        // 4-channel vectors of x, dt, z a tile and a thread
-    constexpr int NB = TILE * N / 4, BPT = (NB + NT - 1) / NT;         // 4-state vectors of b, c
-    extern __shared__ __align__(16) unsigned char smem[];
-    float2 *s_in = reinterpret_cast<float2 *>(smem);                   // [TILE][DC] dt, dt x
-    float *s_b = reinterpret_cast<float *>(s_in + TILE * DC);          // [TILE][N]
-    float *s_c = s_b + TILE * N;                                       // [TILE][N]
-    constexpr int YP = TILE * DC + 8;
-    float *s_y = s_c + TILE * N;                                       // [R][YP] partial outputs
-    float4 *s_p = reinterpret_cast<float4 *>(s_y + R * YP);            // [WT][WD * 32] decay of a slice
-    float4 *s_h = s_p + WT * WD * 32;                                  // [WT][WD * 32] its state from zero
+    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int wd = warp % WD, wt = warp / WD;
-    const int nblk = (p.D + DC - 1) / DC;
-    const int s = blockIdx.x / nblk, c0 = (blockIdx.x % nblk) * DC;
-    const int chl = wd * CPW + lane / R, r = lane % R, ch = c0 + chl;
+// NS = 8 states and CH channels a lane; R = N / 8 lanes share CH channels.
+template <typename TI, int N, int CH, int TOK>
+struct FwdShape {
+    static constexpr int NS = 8, NP = 4, R = N / NS, CPW = 32 / R * CH, E16 = 16 / (int)sizeof(TI);
+    static constexpr int PT = TOK * CH / R;                              // tokens a lane prepares, of one channel
+    static constexpr int XC = CPW / E16, BC = N / E16;                   // 16-byte pieces of a token's x, b
+    static constexpr int CHUNKS = TOK * (3 * XC + 2 * BC), CPL = (CHUNKS + 31) / 32;   // of a slice, a lane
+    static constexpr int RAW_E = CHUNKS * E16;                           // elements of a raw slice
+    static constexpr int HAND_B = 32 * CH * NS * 4;
+    static constexpr int BC_F = 2 * TOK * N;                             // b, c of a slice in fp32
+    static constexpr int WARP_B = 2 * RAW_E * (int)sizeof(TI) + BC_F * 4 + HAND_B;
+};
+
+// One CTA: WT warps that take turns with the slices of TOK tokens of one chain: CPW channels of a sequence, or of a
+// segment of one.  A warp fetches its slice (asynchronously, one slice ahead), evaluates its decays, waits for the state
+// from the warp before it, runs the recurrence, hands the state on and forms the outputs; only the recurrence is serial.
+// A lane prepares (time step, gate, output) PT tokens of one channel, "its" channel, and runs 8 states of all CH
+// channels of its R lanes: slot 0 is its own channel, slot 1 its neighbour's, so that one exchange with lane ^ 1 turns
+// partial outputs around, and one 16-byte read of b or c (2 cycles an SM for 16 broadcast bytes) serves CH channels.
+// Two pools of work run beside each other here and are about equally long, which is why taking away any one part changes
+// the time by a few per cent only: exponentials (8 cycles a warp instruction) with the shared memory traffic behind the
+// same queue, and the multiply-adds.  Two-wide multiply-adds of three different register pairs take 4.2 cycles of a
+// scheduler, two single ones 2.6 but twice the issue slots; as a whole the two-wide form is 10 % faster.
+template <typename TI, typename TO, int N, int CH, int TOK, int WT, int OCC>
+__global__ void __launch_bounds__(32 * WT, OCC) selscan_fwd_kernel(const ScanParams p)
+{
+    using Sh = FwdShape<TI, N, CH, TOK>;
+    constexpr int NS = Sh::NS, R = Sh::R, NP = Sh::NP, CPW = Sh::CPW, E16 = Sh::E16, XC = Sh::XC, BC = Sh::BC, CPL = Sh::CPL, PT = Sh::PT;
+    static_assert(XC >= 1 && BC >= 1 && kCkptTok % TOK == 0 && PT >= 1 && WT > 1 && WT <= 15 && R >= CH, "shapes");
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ longlong2 s_src[5];                                       // address of token 0, bytes between a warp's slices
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    unsigned char *s_mine = smem + warp * Sh::WARP_B;
+    TI *s_raw = reinterpret_cast<TI *>(s_mine);                          // two slices: x, dt, z [TOK][CPW], b, c [TOK][N]
+    float *s_f = reinterpret_cast<float *>(s_mine + 2 * Sh::RAW_E * sizeof(TI));   // b, c [TOK][N] in fp32
+    float4 *s_hand = reinterpret_cast<float4 *>(s_mine + Sh::WARP_B - Sh::HAND_B);   // [CH NS / 4][32] the state handed on
+
+    const int nblk = (p.D + CPW - 1) / CPW;
+    const long long blk = blockIdx.x / nblk;
+    const int c0 = (blockIdx.x % nblk) * CPW;
+    int s, b = 0;
+    SeqRange sr;
+    if (p.seg) {
+        s = packed_block_seq(p.off, p.S, p.T, p.seg, blk);
+        sr = seq_range(p.off, s, p.S, p.T);
+        b = (int)(blk - (sr.start / p.seg + s));
+        if (b < 0 || (b > 0 && b * p.seg >= sr.len)) return;
+    } else {
+        s = (int)blk;
+        sr = seq_range(p.off, s, p.S, p.T);
+    }
+    const int begin = b * p.seg, end = p.seg ? min(begin + p.seg, sr.len) : sr.len;   // tokens of the sequence
+    const bool final = end == sr.len;
+    const int q = lane % R, grp = lane / R;
+    const int chl = grp * CH + q % CH, ch = c0 + chl, tok0 = (q / CH) * PT;   // this lane's channel, its first token of a slice
+    const int n0 = NS * q;
     const bool live = ch < p.D;
-    const SeqRange sr = seq_range(p.off, s, p.S, p.T);
     const int g = p.G == 1 ? 0 : c0 / (p.D / p.G);
 
-    const TI *px = static_cast<const TI *>(p.x), *pdt = static_cast<const TI *>(p.dt), *pz = static_cast<const TI *>(p.z);
-    const TI *pb = static_cast<const TI *>(p.b) + g * N, *pc = static_cast<const TI *>(p.c) + g * N;
-
-    float2 a01 = make_float2(0.f, 0.f), a23 = a01;
-    float4 carry = zero4();
-    const size_t st = ((size_t)s * p.D + ch) * N + 4 * r;
-    if (live) {
-        const float4 av = *reinterpret_cast<const float4 *>(p.a + (size_t)ch * N + 4 * r);
-        a01 = make_float2(decay_rate(av.x), decay_rate(av.y));
-        a23 = make_float2(decay_rate(av.z), decay_rate(av.w));
-        if (p.state_in) carry = *reinterpret_cast<const float4 *>(p.state_in + st);
+    if (threadIdx.x < 5) {
+        const int w = threadIdx.x;
+        const void *base = w == 0 ? p.x : w == 1 ? p.dt : w == 2 ? p.z : w == 3 ? p.b : p.c;
+        const long long stride = w == 0 ? p.xs : w == 1 ? p.dts : w == 2 ? p.zs : w == 3 ? p.bs : p.cs;
+        const long long at = ((long long)sr.start + begin) * stride + (w < 3 ? c0 : g * N);
+        s_src[w] = base ? make_longlong2((long long)base + at * (long long)sizeof(TI), stride * (long long)sizeof(TI)) : make_longlong2(0, 0);
     }
 
-    float4 rx[VPT], rdt[VPT], rz[VPT], rb[BPT], rc[BPT];
-    auto fetch = [&](int t0) {
+    // decay rates in shared memory, [CH NS / 4][32]: they are wanted before the state is, so that one takes the other's
+    // registers
+    __shared__ float4 s_a[CH * NP / 2][32];
+    float2 h[CH][NP];
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const int v = tid + i * NT, t = t0 + v / (DC / 4), c = c0 + 4 * (v % (DC / 4));
-            rx[i] = rdt[i] = rz[i] = zero4();
-            if (v < NV && t < sr.len && c < p.D) {
-                const size_t row = (size_t)(sr.start + t);
-                rx[i] = load4(px + row * p.xs + c);
-                rdt[i] = load4(pdt + row * p.dts + c);
-                if (pz) rz[i] = load4(pz + row * p.zs + c);
+    for (int j = 0; j < CH; ++j) {
+        const int cj = ch ^ j;   // pairs of channels start at even ones, so the neighbour is ch ^ 1
+        const bool ok = cj < p.D;
+        const size_t at = (size_t)cj * N + n0;
+        const float *init = p.seg_sum ? nullptr : (b > 0 ? p.seg_state + (size_t)blk * p.D * N : (p.state_in ? p.state_in + (size_t)s * p.D * N : nullptr));
+#pragma unroll
+        for (int k = 0; k < NP; k += 2) {
+            float4 av = zero4(), hv = zero4();
+            if (ok) {
+                av = *reinterpret_cast<const float4 *>(p.a + at + 2 * k);
+                av = make_float4(decay_rate(av.x), decay_rate(av.y), decay_rate(av.z), decay_rate(av.w));
+                if (init) hv = *reinterpret_cast<const float4 *>(init + at + 2 * k);
             }
+            h[j][k] = make_float2(hv.x, hv.y);
+            h[j][k + 1] = make_float2(hv.z, hv.w);
+            if (warp == 0) s_a[j * NP / 2 + k / 2][lane] = av;
         }
+    }
+    auto keep = [&](float *to, const float2 (&v)[CH][NP]) {   // states of this lane to a [D][N] array
 #pragma unroll
-        for (int i = 0; i < BPT; ++i) {
-            const int v = tid + i * NT, t = t0 + v / (N / 4), n = 4 * (v % (N / 4));
-            rb[i] = rc[i] = zero4();
-            if (v < NB && t < sr.len) {
-                const size_t row = (size_t)(sr.start + t);
-                rb[i] = load4(pb + row * p.bs + n);
-                rc[i] = load4(pc + row * p.cs + n);
+        for (int j = 0; j < CH; ++j) {
+            if ((ch ^ j) < p.D) {
+                float4 *o = reinterpret_cast<float4 *>(to + (size_t)(ch ^ j) * N + n0);
+                o[0] = make_float4(v[j][0].x, v[j][0].y, v[j][1].x, v[j][1].y);
+                o[1] = make_float4(v[j][2].x, v[j][2].y, v[j][3].x, v[j][3].y);
             }
         }
     };
+    const float bias = live && p.bias ? p.bias[ch] : 0.f, skip = live && p.dsk ? p.dsk[ch] : 0.f;
+    __syncthreads();
 
-    fetch(0);
-    for (int t0 = 0; t0 < sr.len; t0 += TILE) {
-        float4 kx[VPT], kz[VPT];   // this thread's x and z, for the epilogue of the tile
+    // this lane's 16-byte pieces of a slice
+    const char *src[CPL];
+    int tok[CPL];
+    long long step[CPL];
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const int v = tid + i * NT, t = t0 + v / (DC / 4), cl = 4 * (v % (DC / 4));
-            kx[i] = rx[i];
-            kz[i] = rz[i];
-            if (v < NV) {
-                float4 d = zero4();
-                if (t < sr.len && c0 + cl < p.D) {
-                    const float4 bias = opt4(p.bias, c0 + cl, 0.f);
-                    d = make_float4(rdt[i].x + bias.x, rdt[i].y + bias.y, rdt[i].z + bias.z, rdt[i].w + bias.w);
-                    if (p.softplus) d = make_float4(softplus_acc(d.x), softplus_acc(d.y), softplus_acc(d.z), softplus_acc(d.w));
+    for (int i = 0; i < CPL; ++i) {
+        int id = lane + 32 * i;
+        const bool in_x = id < 3 * TOK * XC;
+        int which = in_x ? id / (TOK * XC) : 3 + (id - 3 * TOK * XC) / (TOK * BC);
+        id = in_x ? id % (TOK * XC) : (id - 3 * TOK * XC) % (TOK * BC);
+        const int per = in_x ? XC : BC;
+        tok[i] = id / per;
+        const bool used = lane + 32 * i < Sh::CHUNKS;
+        if (!used) which = 0;
+        const longlong2 from = s_src[which];
+        const bool ok = used && from.x && (!in_x || c0 + (id % per) * E16 < p.D);
+        src[i] = reinterpret_cast<const char *>(ok ? from.x + (long long)(warp * TOK + tok[i]) * from.y + (id % per) * 16 : (long long)p.x);
+        step[i] = ok ? from.y * (WT * TOK) : 0;
+        if (!ok) tok[i] = 0x40000000;   // never inside; the address stays where it is
+    }
+    auto fetch = [&](int t0, int to) {
+#pragma unroll
+        for (int i = 0; i < CPL; ++i) {
+            if (lane + 32 * i < Sh::CHUNKS) copy16(s_raw + to * Sh::RAW_E + (lane + 32 * i) * E16, src[i], tok[i] < end - t0);
+            src[i] += step[i];
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+
+    if (begin >= end && warp == 0 && p.state_out && !p.seg_sum) keep(p.state_out + (size_t)s * p.D * N, h);
+    TO *py = static_cast<TO *>(p.y) + (p.y ? ((size_t)sr.start + begin + warp * TOK + tok0) * p.D + ch : 0);
+    float all_dt = 0.f;
+    int stage = 0;
+    fetch(begin + warp * TOK, 0);
+    for (int t0 = begin + warp * TOK; t0 < end; t0 += WT * TOK) {
+        fetch(t0 + WT * TOK, stage ^ 1);
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncwarp();
+        const TI *raw = s_raw + stage * Sh::RAW_E;
+#pragma unroll
+        for (int i = 0; i < (Sh::BC_F / 4 + 31) / 32; ++i)
+            if (lane + 32 * i < Sh::BC_F / 4) reinterpret_cast<float4 *>(s_f)[lane + 32 * i] = load4(raw + 3 * TOK * CPW + 4 * (lane + 32 * i));
+        const float *s_b = s_f + n0, *s_c = s_b + TOK * N;
+        auto row_of = [&](const float *m, float2 (&o)[NP]) {
+            const float4 u = reinterpret_cast<const float4 *>(m)[0], v = reinterpret_cast<const float4 *>(m)[1];
+            o[0] = make_float2(u.x, u.y);
+            o[1] = make_float2(u.z, u.w);
+            o[2] = make_float2(v.x, v.y);
+            o[3] = make_float2(v.z, v.w);
+        };
+        float dt[PT], dx[PT];
+#pragma unroll
+        for (int i = 0; i < PT; ++i) dt[i] = load1(raw + (TOK + tok0 + i) * CPW + chl) + bias;
+        if (p.softplus) {
+#pragma unroll
+            for (int i = 0; i < PT; i += 2) {
+                const float2 v = softplus_acc(make_float2(dt[i], dt[i + 1 < PT ? i + 1 : i]));
+                dt[i] = v.x;
+                if (i + 1 < PT) dt[i + 1] = v.y;
+            }
+        }
+        if (t0 + TOK > end) {   // past the end: decay 1, no input
+#pragma unroll
+            for (int i = 0; i < PT; ++i)
+                if (t0 + tok0 + i >= end) dt[i] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < PT; ++i) dx[i] = dt[i] * load1(raw + (tok0 + i) * CPW + chl);
+        if (p.seg_sum) {
+#pragma unroll
+            for (int i = 0; i < PT; ++i) all_dt += dt[i];
+        }
+        __syncwarp();
+        // value of the token i, slot j, from the lane that prepared it
+        auto of = [&](const float (&v)[PT], int i, int j) -> float {
+            if (R == 1) return v[i % PT];
+            if (R == 2) return j == 0 ? v[i % PT] : __shfl_xor_sync(0xffffffffu, v[i % PT], 1);
+            return __shfl_sync(0xffffffffu, v[i % PT], (lane & ~(R - 1)) + ((q % CH) ^ j) + CH * (i / PT));
+        };
+        float2 e[TOK][CH][NP];
+        auto rates = [&](int j, float2 (&o)[NP]) {
+            const float4 u = s_a[j * NP / 2][lane], v = s_a[j * NP / 2 + 1][lane];
+            o[0] = make_float2(u.x, u.y);
+            o[1] = make_float2(u.z, u.w);
+            o[2] = make_float2(v.x, v.y);
+            o[3] = make_float2(v.z, v.w);
+        };
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            float2 a[NP];
+            rates(j, a);
+#pragma unroll
+            for (int i = 0; i < TOK; ++i) {
+                const float d = of(dt, i, j);
+#pragma unroll
+                for (int k = 0; k < NP; ++k) {
+                    const float2 v = mul2v(a[k], splat2(d));
+                    e[i][j][k] = make_float2(ex2(v.x), ex2(v.y));
                 }
-                float4 *o = reinterpret_cast<float4 *>(s_in + (v / (DC / 4)) * DC + cl);
-                o[0] = make_float4(d.x, d.x * rx[i].x, d.y, d.y * rx[i].y);
-                o[1] = make_float4(d.z, d.z * rx[i].z, d.w, d.w * rx[i].w);
             }
         }
+        float dxs[TOK][CH];
 #pragma unroll
-        for (int i = 0; i < BPT; ++i) {
-            const int v = tid + i * NT;
-            if (v < NB) {
-                reinterpret_cast<float4 *>(s_b)[v] = rb[i];
-                reinterpret_cast<float4 *>(s_c)[v] = rc[i];
+        for (int i = 0; i < TOK; ++i)
+#pragma unroll
+            for (int j = 0; j < CH; ++j) dxs[i][j] = of(dx, i, j);
+        const bool last = t0 + TOK >= end;
+        if (t0 > begin) {
+            const int from = (warp + WT - 1) % WT;
+            named_sync(1 + from);
+            const float4 *m = reinterpret_cast<const float4 *>(smem + from * Sh::WARP_B + Sh::WARP_B - Sh::HAND_B);
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+#pragma unroll
+                for (int k = 0; k < NP; k += 2) {
+                    const float4 v = m[(j * NP / 2 + k / 2) * 32 + lane];
+                    h[j][k] = make_float2(v.x, v.y);
+                    h[j][k + 1] = make_float2(v.z, v.w);
+                }
+        }
+        auto hand_on = [&](const float2 (&v)[CH][NP]) {
+            if (!last) {
+#pragma unroll
+                for (int j = 0; j < CH; ++j)
+#pragma unroll
+                    for (int k = 0; k < NP; k += 2)
+                        s_hand[(j * NP / 2 + k / 2) * 32 + lane] = make_float4(v[j][k].x, v[j][k].y, v[j][k + 1].x, v[j][k + 1].y);
+                named_arrive(1 + warp);
+            } else if (p.seg_sum) {
+                keep(p.seg_state + (size_t)blk * p.D * N, v);
+            } else if (final && p.state_out) {
+                keep(p.state_out + (size_t)s * p.D * N, v);
             }
-        }
-        __syncthreads();
-        fetch(t0 + TILE);
-
-        // this slice from a zero state: outputs, and c times the decay since the slice's start
-        float2 h01 = make_float2(0.f, 0.f), h23 = h01, p01 = make_float2(1.f, 1.f), p23 = p01;
-        float2 q01[TOK], q23[TOK];
-        float y[TOK];
+        };
+        if (p.ckpt && t0 % kCkptTok == 0) keep(p.ckpt + ((size_t)(sr.start / kCkptTok) + s + t0 / kCkptTok) * p.D * N, h);
 #pragma unroll
         for (int i = 0; i < TOK; ++i) {
-            const int t = wt * TOK + i;
-            const float2 in = s_in[t * DC + chl];
-            const float4 bv = *reinterpret_cast<const float4 *>(s_b + t * N + 4 * r);
-            const float4 cv = *reinterpret_cast<const float4 *>(s_c + t * N + 4 * r);
-            float2 e01 = mul2v(a01, splat2(in.x)), e23 = mul2v(a23, splat2(in.x));
-            e01 = make_float2(ex2(e01.x), ex2(e01.y));
-            e23 = make_float2(ex2(e23.x), ex2(e23.y));
-            h01 = fma2v(e01, h01, mul2v(splat2(in.y), make_float2(bv.x, bv.y)));
-            h23 = fma2v(e23, h23, mul2v(splat2(in.y), make_float2(bv.z, bv.w)));
-            const float2 c01 = make_float2(cv.x, cv.y), c23 = make_float2(cv.z, cv.w);
-            const float2 yy = fma2v(c23, h23, mul2v(c01, h01));
-            y[i] = yy.x + yy.y;
-            p01 = mul2v(p01, e01);
-            p23 = mul2v(p23, e23);
-            q01[i] = mul2v(c01, p01);
-            q23[i] = mul2v(c23, p23);
-        }
-        s_p[wt * (WD * 32) + wd * 32 + lane] = make_float4(p01.x, p01.y, p23.x, p23.y);
-        s_h[wt * (WD * 32) + wd * 32 + lane] = make_float4(h01.x, h01.y, h23.x, h23.y);
-        __syncthreads();
-        float4 mine = carry;
+            float2 bv[NP];
+            row_of(s_b + i * N, bv);
 #pragma unroll
-        for (int w = 0; w < WT; ++w) {
-            if (w == wt) mine = carry;
-            const float4 pw = s_p[w * (WD * 32) + wd * 32 + lane], hw = s_h[w * (WD * 32) + wd * 32 + lane];
-            carry = make_float4(fmaf(pw.x, carry.x, hw.x), fmaf(pw.y, carry.y, hw.y), fmaf(pw.z, carry.z, hw.z),
-                                fmaf(pw.w, carry.w, hw.w));
-        }
-        if (p.ckpt && live && (wt * TOK) % kCkptTok == 0 && t0 + wt * TOK < sr.len) {
-            const size_t k = (size_t)(sr.start / kCkptTok) + s + (t0 + wt * TOK) / kCkptTok;
-            *reinterpret_cast<float4 *>(p.ckpt + (k * p.D + ch) * N + 4 * r) = mine;
-        }
+            for (int j = 0; j < CH; ++j)
 #pragma unroll
-        for (int i = 0; i < TOK; ++i) {
-            const float2 yy = fma2v(q23[i], make_float2(mine.z, mine.w), mul2v(q01[i], make_float2(mine.x, mine.y)));
-            s_y[r * YP + (wt * TOK + i) * DC + chl] = y[i] + (yy.x + yy.y);
+                for (int k = 0; k < NP; ++k) {
+                    h[j][k] = fma2v(e[i][j][k], h[j][k], mul2v(splat2(dxs[i][j]), bv[k]));
+                    e[i][j][k] = h[j][k];
+                }
         }
-        __syncthreads();
+        hand_on(h);
         if (p.y) {
+            float y[TOK];   // of this lane's channel, after its neighbour's share has come in
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                const int v = tid + i * NT, t = t0 + v / (DC / 4), cl = 4 * (v % (DC / 4));
-                if (v < NV && t < sr.len && c0 + cl < p.D) {
-                    const float4 dv = opt4(p.dsk, c0 + cl, 0.f);
-                    float4 o = make_float4(dv.x * kx[i].x, dv.y * kx[i].y, dv.z * kx[i].z, dv.w * kx[i].w);
+            for (int i = 0; i < TOK; ++i) {
+                float2 cv[NP];
+                row_of(s_c + i * N, cv);
+                float part[CH];
 #pragma unroll
-                    for (int j = 0; j < R; ++j) {
-                        const float4 part = *reinterpret_cast<const float4 *>(s_y + j * YP + 4 * v);
-                        o.x += part.x; o.y += part.y; o.z += part.z; o.w += part.w;
+                for (int j = 0; j < CH; ++j) {
+                    float2 u = mul2v(cv[0], e[i][j][0]);
+#pragma unroll
+                    for (int k = 1; k < NP; ++k) u = fma2v(cv[k], e[i][j][k], u);
+                    part[j] = u.x + u.y;
+                }
+                y[i] = CH == 1 ? part[0] : part[0] + __shfl_xor_sync(0xffffffffu, part[CH - 1], 1);
+            }
+            // R > CH: the other lanes of this channel hold other states; halve the tokens at each exchange
+            if (R > CH) {
+                int n = TOK;
+#pragma unroll
+                for (int o = R / 2; o >= CH; o >>= 1) {
+                    n >>= 1;
+                    const bool up = lane & o;
+#pragma unroll
+                    for (int i = 0; i < TOK / 2; ++i) {
+                        if (i < n) {
+                            const float send = up ? y[i] : y[i + n], mine = up ? y[i + n] : y[i];
+                            y[i] = mine + __shfl_xor_sync(0xffffffffu, send, o);
+                        }
                     }
-                    if (pz) {
-                        o.x *= gate_f(kz[i].x); o.y *= gate_f(kz[i].y); o.z *= gate_f(kz[i].z); o.w *= gate_f(kz[i].w);
-                    }
-                    store4(static_cast<TO *>(p.y) + (size_t)(sr.start + t) * p.D + c0 + cl, o);
                 }
             }
+#pragma unroll
+            for (int i = 0; i < PT; ++i) {
+                float v = fmaf(skip, load1(raw + (tok0 + i) * CPW + chl), y[i]);
+                if (p.z) v *= gate_f(load1(raw + (2 * TOK + tok0 + i) * CPW + chl));
+                if (live && t0 + tok0 + i < end) store1(py + (size_t)i * p.D, v);
+            }
+            py += (size_t)(WT * TOK) * p.D;
+        }
+        stage ^= 1;
+        __syncwarp();
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (p.seg_sum) {   // the segment's whole time, for its decay
+        __syncthreads();
+        float *s_dt = reinterpret_cast<float *>(smem);
+        s_dt[warp * 32 + lane] = all_dt;
+        __syncthreads();
+        if (warp == 0 && live && q < CH) {
+            float t = 0.f;
+            for (int w = 0; w < WT; ++w)
+#pragma unroll
+                for (int o = 0; o < R; o += CH) t += s_dt[w * 32 + lane + o];
+            p.seg_sum[(size_t)blk * p.D + ch] = t;
         }
     }
-    if (p.state_out && live && wt == 0) *reinterpret_cast<float4 *>(p.state_out + st) = carry;
+}
+
+// Segments of a sequence in turn: the state each ends with becomes the state it starts with.
+template <int N>
+__global__ void __launch_bounds__(128) selscan_segments_kernel(const ScanParams p)
+{
+    const size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x;   // (s, channel, state)
+    const size_t per = (size_t)p.D * N;
+    if (i >= per * p.S) return;
+    const int s = (int)(i / per), ch = (int)(i % per / N), n = (int)(i % N);
+    const SeqRange sr = seq_range(p.off, s, p.S, p.T);
+    const float a = decay_rate(p.a[(size_t)ch * N + n]);
+    float h = p.state_in ? p.state_in[i] : 0.f;
+    size_t k = (size_t)(sr.start / p.seg) + s;
+    for (int t = 0; t < sr.len; t += p.seg, ++k) {
+        float *m = p.seg_state + (k * p.D + ch) * N + n;
+        const float own = *m;
+        *m = h;
+        h = fmaf(ex2(a * p.seg_sum[k * p.D + ch]), h, own);
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ single token
@@ -598,19 +781,42 @@ __global__ void __launch_bounds__(256) sum_rows_kernel(const float *part, float 
 
 // ------------------------------------------------------------------------------------------------ launches
 
-template <typename TI, typename TO, int N, int WD, int WT>
-chela_status_t fwd_launch(const ScanParams &p, cudaStream_t stream)
+// Tokens of a segment, 0 = whole sequences.  A split costs a second pass over x, dt, b (their decays evaluated twice, 1.9
+// times the exponentials), so it pays only where the chains leave more than half of the SMs without work.
+int fwd_segment(int T, int S, int D, int N)
 {
-    constexpr int R = N / 4, DC = 32 / R * WD, TILE = 16 * WT;
-    constexpr size_t smem = (size_t)TILE * DC * 8 + 2 * TILE * N * 4 + R * (TILE * DC + 8) * 4 + 2 * WT * WD * 32 * 16;
-    const auto kern = selscan_fwd_kernel<TI, TO, N, WD, WT>;
-    if (smem > 48 * 1024) {
+    const int cpw = N <= 16 ? 32 : 512 / N;
+    const long long cols = (D + cpw - 1) / cpw, chains = cols * S;
+    if (chains * 2 > 148 || T / S < 512) return 0;
+    const long long want = (2 * 148 + cols - 1) / cols;   // segments in all
+    const long long seg = (T + want - 1) / want;
+    return (int)((seg < 256 ? 256 : seg + 127) / 128 * 128);
+}
+
+template <typename TI, typename TO, int N, int CH, int TOK, int WT, int OCC>
+chela_status_t fwd_launch(ScanParams p, cudaStream_t stream)
+{
+    using Sh = FwdShape<TI, N, CH, TOK>;
+    constexpr size_t smem = (size_t)WT * Sh::WARP_B;
+    const auto kern = selscan_fwd_kernel<TI, TO, N, CH, TOK, WT, OCC>;
+    if (smem > 47 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return cuda_status(e);
     }
-    const long long blocks = (long long)p.S * ((p.D + DC - 1) / DC);
+    const long long chains = p.seg ? (long long)packed_blocks(p.T, p.S, p.seg) : p.S;
+    const long long blocks = chains * ((p.D + Sh::CPW - 1) / Sh::CPW);
     if (blocks > 0x7fffffffLL) return CHELA_ERR_UNSUPPORTED;
-    kern<<<(unsigned)blocks, 32 * WD * WT, smem, stream>>>(p);
+    if (p.seg) {
+        ScanParams q = p;
+        q.y = nullptr;
+        q.ckpt = q.state_out = nullptr;
+        kern<<<(unsigned)blocks, 32 * WT, smem, stream>>>(q);
+        const long long n = ((long long)p.S * p.D * N + 127) / 128;
+        if (n > 0x7fffffffLL) return CHELA_ERR_UNSUPPORTED;
+        selscan_segments_kernel<N><<<(unsigned)n, 128, 0, stream>>>(p);
+        p.seg_sum = nullptr;
+    }
+    kern<<<(unsigned)blocks, 32 * WT, smem, stream>>>(p);
     return last_launch_status();
 }
 
@@ -618,10 +824,10 @@ template <typename TI, typename TO>
 chela_status_t fwd_n(const ScanParams &p, int N, cudaStream_t stream)
 {
     switch (N) {
-    case 8: return fwd_launch<TI, TO, 8, 1, 8>(p, stream);
-    case 16: return fwd_launch<TI, TO, 16, 1, 8>(p, stream);
-    case 32: return fwd_launch<TI, TO, 32, 2, 4>(p, stream);
-    default: return fwd_launch<TI, TO, 64, 4, 2>(p, stream);
+    case 8: return fwd_launch<TI, TO, 8, 1, 8, 8, 2>(p, stream);
+    case 16: return fwd_launch<TI, TO, 16, 2, 4, 8, 2>(p, stream);
+    case 32: return fwd_launch<TI, TO, 32, 2, 4, 8, 2>(p, stream);
+    default: return fwd_launch<TI, TO, 64, 2, 4, 8, 2>(p, stream);
     }
 }
 
@@ -698,14 +904,15 @@ ScanParams scan_params(const chela_selscan_args_t &a)
 }
 
 struct ScanBwdPlan {
-    size_t off_ckpt, off_bc, off_a, off_d, total;
+    size_t off_ckpt, off_fwd, off_bc, off_a, off_d, total;
 };
 ScanBwdPlan bwd_plan(int T, int S, int D, int N, bool have_ckpt)
 {
     ScanBwdPlan p;
     const int dc = bwd_channels(N);
     p.off_ckpt = 0;
-    p.off_bc = have_ckpt ? 0 : align_up(selscan_checkpoint_bytes(T, S, D, N), 256);
+    p.off_fwd = have_ckpt ? 0 : align_up(selscan_checkpoint_bytes(T, S, D, N), 256);
+    p.off_bc = p.off_fwd + (have_ckpt ? 0 : selscan_workspace_bytes(T, S, D, N));
     p.off_a = p.off_bc + align_up((size_t)((D + dc - 1) / dc) * T * 2 * N * sizeof(float), 256);
     p.off_d = p.off_a + align_up((size_t)S * D * N * sizeof(float), 256);
     p.total = p.off_d + align_up((size_t)S * 2 * D * sizeof(float), 256);
@@ -719,13 +926,24 @@ size_t selscan_checkpoint_bytes(int T, int S, int D, int N)
     return (packed_blocks(T, S, kCkptTok)) * D * N * sizeof(float);
 }
 
+size_t selscan_workspace_bytes(int T, int S, int D, int N)
+{
+    const int seg = fwd_segment(T, S, D, N);
+    return seg ? align_up(packed_blocks(T, S, seg) * D * (N + 1) * sizeof(float), 256) : 0;
+}
+
 chela_status_t launch_selscan_fwd(const chela_selscan_args_t &a, void *y, float *state_out, void *ckpt, chela_dtype_t out_dtype,
-                                  cudaStream_t stream)
+                                  void *workspace, cudaStream_t stream)
 {
     ScanParams p = scan_params(a);
     p.y = y;
     p.state_out = state_out;
     p.ckpt = static_cast<float *>(ckpt);
+    p.seg = fwd_segment(a.T, a.S, a.D, a.N);
+    if (p.seg) {
+        p.seg_state = static_cast<float *>(workspace);
+        p.seg_sum = p.seg_state + packed_blocks(a.T, a.S, p.seg) * a.D * a.N;
+    }
     if (a.in_dtype == CHELA_F32)
         return out_dtype == CHELA_F32 ? fwd_n<float, float>(p, a.N, stream) : fwd_n<float, __nv_bfloat16>(p, a.N, stream);
     return out_dtype == CHELA_F32 ? fwd_n<__nv_bfloat16, float>(p, a.N, stream) : fwd_n<__nv_bfloat16, __nv_bfloat16>(p, a.N, stream);
@@ -754,7 +972,7 @@ chela_status_t launch_selscan_bwd(const chela_selscan_args_t &a, const void *d_y
     q.f.ckpt = static_cast<float *>(const_cast<void *>(ckpt));
     if (!ckpt) {
         q.f.ckpt = reinterpret_cast<float *>(ws + w.off_ckpt);
-        const chela_status_t st = launch_selscan_fwd(a, nullptr, nullptr, q.f.ckpt, CHELA_F32, stream);
+        const chela_status_t st = launch_selscan_fwd(a, nullptr, nullptr, q.f.ckpt, CHELA_F32, ws + w.off_fwd, stream);
         if (st != CHELA_OK) return st;
     }
     q.dy = d_y;

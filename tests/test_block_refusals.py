@@ -60,14 +60,17 @@ def test_short_convolution_refusals(lib):
 
 def test_selective_scan_refusals(lib):
     bad, no = chela.ERR_INVALID_ARG, chela.ERR_UNSUPPORTED
-    fwd = lambda y=two, so=null, ck=null, odt=0, **kw: lib.chela_selscan_fwd(scan_args(**kw), y, so, ck, odt, null)  # noqa: E731
-    assert lib.chela_selscan_fwd(null, two, null, null, 0, null) == bad
+    fwd = lambda y=two, so=null, ck=null, odt=0, ws=one, n=BIG, **kw: lib.chela_selscan_fwd(scan_args(**kw), y, so, ck, odt, ws, n, null)  # noqa: E731
+    assert lib.chela_selscan_fwd(null, two, null, null, 0, one, BIG, null) == bad
     for k in ("x", "dt", "a", "b", "c"):
         assert fwd(**{k: 0}) == fwd(**{k: 260}) == bad
     assert fwd(z=512, z_stride=8) == fwd(z=260, z_stride=64) == fwd(state_in=260) == fwd(d_skip=260) == fwd(dt_bias=260) == bad
     assert fwd(x_stride=63) == fwd(x_stride=68) == fwd(b_stride=8) == fwd(c_stride=20) == bad
     assert fwd(S=0) == fwd(T=0) == fwd(S=3) == fwd(G=0) == fwd(in_dtype=2) == fwd(odt=2) == fwd(softplus=2) == bad
     assert fwd(y=null) == fwd(y=odd) == fwd(so=odd) == fwd(ck=odd) == bad
+    assert fwd(ws=odd) == bad
+    assert fwd(T=4096, ws=null) == fwd(T=4096, n=64) == chela.ERR_WORKSPACE   # two chains of 32 channels: split into segments
+    assert lib.chela_selscan_workspace_bytes(4096, 1, 64, 16) > 0 == lib.chela_selscan_workspace_bytes(4096, 64, 1024, 16)
     assert fwd(N=24, b_stride=24, c_stride=24) == fwd(D=60, x_stride=64) == no
     assert fwd(G=4, b_stride=64, c_stride=64) == no   # 16 channels a group
     step = lambda y=two, so=two, odt=0, **kw: lib.chela_selscan_step(scan_args(**({"S": 4, "state_in": 256} | kw)), y, so, odt, null)  # noqa: E731
