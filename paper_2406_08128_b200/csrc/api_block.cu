@@ -88,7 +88,7 @@ chela_status_t chela_shortconv_step(const void *x, long long x_stride, const flo
     const chela_status_t st = check_conv(x, x_stride, w, bias, state_in, state_out, nullptr, S, S, D, width, act, io_dtype);
     if (st != CHELA_OK) return st;
     if (!y || y == x || !aligned16(y) || (width > 1 && (!state_in || !state_out))) return CHELA_ERR_INVALID_ARG;
-    return launch_shortconv_carry(x, x_stride, w, bias, y, state_in, state_out, nullptr, S, S, D, width, act, io_dtype, stream);
+    return launch_shortconv_step(x, x_stride, w, bias, y, state_in, state_out, S, D, width, act, io_dtype, stream);
 }
 
 size_t chela_shortconv_bwd_workspace_bytes(int T, int D, int width)

@@ -3,9 +3,10 @@
 //   v = y act(g) | y,  n = Norm(v) w_post + b_post,  m = n | n act(g),  r' = res + scale m,  o = Norm(r') w_pre + b_pre.
 //
 // Bound by HBM: every operand is read once and every result written once; rows stay in registers between the two norms.
-// A lane holds 8 consecutive channels a vector (16 bytes of bf16), WPR warps share a row; sums over a row are fp32
-// shuffles and, for WPR > 1, one exchange through shared memory.  Layer statistics are two-pass (mean first) on the
-// registers, so a large mean costs no digits.
+// A lane holds 8 consecutive channels (16 bytes of bf16), WPR warps share a row; sums over a row are fp32 shuffles and, for
+// WPR > 1, one exchange through shared memory.  The next row's operands are loaded while a row is worked on, and the
+// per-channel weights wait in shared memory.  Layer statistics are two-pass (mean first) on the registers, so a large
+// mean costs no digits.
 #include "packed.cuh"
 
 namespace chela {
@@ -23,24 +24,36 @@ struct NormParams {
 struct Vec8 {
     float v[8];
 };
+// 8 elements as they lie in memory
 template <typename T>
-__device__ __forceinline__ Vec8 load8(const T *p)
+struct Raw8 {
+    Raw4<T> lo, hi;
+    __device__ __forceinline__ void load(const T *p)
+    {
+        if constexpr (sizeof(T) == 2) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(p);
+            lo.v = make_uint2(u.x, u.y);
+            hi.v = make_uint2(u.z, u.w);
+        } else {
+            lo.load(p);
+            hi.load(p + 4);
+        }
+    }
+    __device__ __forceinline__ void zero()
+    {
+        lo.zero();
+        hi.zero();
+    }
+    __device__ __forceinline__ Vec8 get() const
+    {
+        const float4 a = lo.get(), b = hi.get();
+        return Vec8{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+    }
+};
+__device__ __forceinline__ Vec8 load8(const float *p)
 {
     const float4 a = load4(p), b = load4(p + 4);
     return Vec8{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
-}
-template <>
-__device__ __forceinline__ Vec8 load8<__nv_bfloat16>(const __nv_bfloat16 *p)
-{
-    const uint4 u = *reinterpret_cast<const uint4 *>(p);
-    Vec8 r;
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        r.v[2 * i] = __uint_as_float(w[i] << 16);
-        r.v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-    return r;
 }
 __device__ __forceinline__ void store8(float *p, const Vec8 &v)
 {
@@ -58,7 +71,17 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *p, const Vec8 &v)
     *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ Vec8 fill8(float a) { return Vec8{{a, a, a, a, a, a, a, a}}; }
-__device__ __forceinline__ Vec8 opt8(const float *p, int c, float other) { return p ? load8(p + c) : fill8(other); }
+// Weights of a lane's channels: from shared memory, row w of [rows][WPR * 256], or, where a row group has one row only and
+// staging would just add its latency, straight from the caller's vector.
+__device__ __forceinline__ Vec8 weight8(bool staged, const float *s_w, int row, int width, int c, bool live, const float *from, float other)
+{
+    if (staged) return load8(s_w + row * width + c);
+    return live && from ? load8(from + c) : fill8(other);
+}
+__device__ __forceinline__ void stage_weight(float *to, const float *from, float other, int D, int width)
+{
+    for (int c = threadIdx.x; c < width; c += blockDim.x) to[c] = from && c < D ? from[c] : other;
+}
 
 __device__ __forceinline__ float act_f(float u, int act) { return act == 0 ? u : (act == 1 ? u * sigmoid_acc(u) : sigmoid_acc(u)); }
 __device__ __forceinline__ float d_act_f(float u, int act)
@@ -101,98 +124,89 @@ struct RowSum {
 
 // ------------------------------------------------------------------------------------------------ forward
 
-template <typename TI, typename TR, typename TO, int WPR, int VPT>
-__global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256) blocknorm_fwd_kernel(const NormParams p)
+template <typename TI, typename TR, typename TO, int WPR>
+__global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 3) blocknorm_fwd_kernel(const NormParams p)
 {
-    constexpr int GROUPS = WPR > 8 ? 1 : 8 / WPR;
+    constexpr int GROUPS = WPR > 8 ? 1 : 8 / WPR, WIDTH = WPR * 256;
     __shared__ float buf[GROUPS * 2 * WPR];
+    extern __shared__ __align__(16) float s_w[];   // w_post, b_post, scale, w_pre, b_pre [WIDTH], those that are used
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / WPR, wr = warp % WPR;
     RowSum<WPR, 1> sum = {buf, 0, group, wr, lane};
     const float inv_d = 1.f / p.D;
+    const int c = 8 * (wr * 32 + lane);
+    const bool live = c < p.D, post = p.y != nullptr, pre = p.o != nullptr, gated = p.gate != nullptr;
+    const bool staged = (long long)gridDim.x * GROUPS < p.T;
+    if (post && staged) {
+        stage_weight(s_w, p.w_post, 1.f, p.D, WIDTH);
+        stage_weight(s_w + WIDTH, p.b_post, 0.f, p.D, WIDTH);
+        stage_weight(s_w + 2 * WIDTH, p.scale, 1.f, p.D, WIDTH);
+    }
+    if (pre && staged) {
+        stage_weight(s_w + 3 * WIDTH, p.w_pre, 1.f, p.D, WIDTH);
+        stage_weight(s_w + 4 * WIDTH, p.b_pre, 0.f, p.D, WIDTH);
+    }
+    if (staged) __syncthreads();
 
-    for (long long row = (long long)blockIdx.x * GROUPS + group; row < p.T; row += (long long)gridDim.x * GROUPS) {
-        Vec8 r[VPT];
-        auto col = [&](int k) { return 8 * ((k * WPR + wr) * 32 + lane); };
-        auto normalise = [&](Vec8 (&x)[VPT], int kind) {
-            if (kind == CHELA_NORM_NONE) return;
-            float s[1];
-            if (kind == CHELA_NORM_LAYER) {
-                s[0] = 0.f;
-#pragma unroll
-                for (int k = 0; k < VPT; ++k)
-                    if (col(k) < p.D)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) s[0] += x[k].v[e];
-                sum(s);
-                const float mean = s[0] * inv_d;
-#pragma unroll
-                for (int k = 0; k < VPT; ++k)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[k].v[e] -= mean;
-            }
+    auto normalise = [&](Vec8 &x, int kind) {
+        if (kind == CHELA_NORM_NONE) return;
+        float s[1];
+        if (kind == CHELA_NORM_LAYER) {
             s[0] = 0.f;
 #pragma unroll
-            for (int k = 0; k < VPT; ++k)
-                if (col(k) < p.D)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) s[0] = fmaf(x[k].v[e], x[k].v[e], s[0]);
+            for (int e = 0; e < 8; ++e) s[0] += x.v[e];
             sum(s);
-            const float inv = 1.0f / sqrtf(fmaf(s[0], inv_d, p.eps));
+            const float mean = live ? s[0] * inv_d : 0.f;
 #pragma unroll
-            for (int k = 0; k < VPT; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[k].v[e] *= inv;
-        };
-
-#pragma unroll
-        for (int k = 0; k < VPT; ++k) {
-            r[k] = fill8(0.f);
-            if (p.res && col(k) < p.D) r[k] = load8(static_cast<const TR *>(p.res) + (size_t)row * p.rs + col(k));
+            for (int e = 0; e < 8; ++e) x.v[e] -= mean;
         }
-        if (p.y) {
-            Vec8 v[VPT], g[VPT];
+        s[0] = 0.f;
 #pragma unroll
-            for (int k = 0; k < VPT; ++k) {
-                v[k] = fill8(0.f);
-                g[k] = fill8(1.f);
-                if (col(k) < p.D) {
-                    v[k] = load8(static_cast<const TI *>(p.y) + (size_t)row * p.ys + col(k));
-                    if (p.gate) {
-                        g[k] = load8(static_cast<const TI *>(p.gate) + (size_t)row * p.gs + col(k));
+        for (int e = 0; e < 8; ++e) s[0] = fmaf(x.v[e], x.v[e], s[0]);
+        sum(s);
+        const float inv = 1.0f / sqrtf(fmaf(s[0], inv_d, p.eps));
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            g[k].v[e] = act_f(g[k].v[e], p.gate_act);
-                            if (!p.gate_after) v[k].v[e] *= g[k].v[e];
-                        }
-                    }
+        for (int e = 0; e < 8; ++e) x.v[e] *= inv;
+    };
+
+    const long long stride = (long long)gridDim.x * GROUPS;
+    long long row = (long long)blockIdx.x * GROUPS + group;
+    Raw8<TR> rr;
+    Raw8<TI> ry, rg;
+    auto fetch = [&](long long at) {
+        const bool ok = live && at < p.T;
+        if (ok && p.res) rr.load(static_cast<const TR *>(p.res) + (size_t)at * p.rs + c); else rr.zero();
+        if (ok && post) ry.load(static_cast<const TI *>(p.y) + (size_t)at * p.ys + c); else ry.zero();
+        if (ok && gated) rg.load(static_cast<const TI *>(p.gate) + (size_t)at * p.gs + c); else rg.zero();
+    };
+    fetch(row);
+    for (; row < p.T; row += stride) {
+        Vec8 r = rr.get(), v = ry.get(), g = rg.get();
+        fetch(row + stride);
+        if (post) {
+            if (gated) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    g.v[e] = act_f(g.v[e], p.gate_act);
+                    if (!p.gate_after) v.v[e] *= g.v[e];
                 }
             }
             normalise(v, p.norm_post);
+            const Vec8 w = weight8(staged, s_w, 0, WIDTH, c, live, p.w_post, 1.f), b = weight8(staged, s_w, 1, WIDTH, c, live, p.b_post, 0.f),
+                       s = weight8(staged, s_w, 2, WIDTH, c, live, p.scale, 1.f);
 #pragma unroll
-            for (int k = 0; k < VPT; ++k) {
-                if (col(k) < p.D) {
-                    const Vec8 w = opt8(p.w_post, col(k), 1.f), b = opt8(p.b_post, col(k), 0.f), s = opt8(p.scale, col(k), 1.f);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        float m = fmaf(v[k].v[e], w.v[e], b.v[e]);
-                        if (p.gate && p.gate_after) m *= g[k].v[e];
-                        r[k].v[e] = fmaf(s.v[e], m, r[k].v[e]);
-                    }
-                    if (p.res_out) store8(static_cast<TR *>(p.res_out) + (size_t)row * p.D + col(k), r[k]);
-                }
+            for (int e = 0; e < 8; ++e) {
+                float m = fmaf(v.v[e], w.v[e], b.v[e]);
+                if (gated && p.gate_after) m *= g.v[e];
+                r.v[e] = live ? fmaf(s.v[e], m, r.v[e]) : 0.f;
             }
+            if (live && p.res_out) store8(static_cast<TR *>(p.res_out) + (size_t)row * p.D + c, r);
         }
-        if (p.o) {
+        if (pre) {
             normalise(r, p.norm_pre);
+            const Vec8 w = weight8(staged, s_w, 3, WIDTH, c, live, p.w_pre, 1.f), b = weight8(staged, s_w, 4, WIDTH, c, live, p.b_pre, 0.f);
 #pragma unroll
-            for (int k = 0; k < VPT; ++k) {
-                if (col(k) < p.D) {
-                    const Vec8 w = opt8(p.w_pre, col(k), 1.f), b = opt8(p.b_pre, col(k), 0.f);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) r[k].v[e] = fmaf(r[k].v[e], w.v[e], b.v[e]);
-                    store8(static_cast<TO *>(p.o) + (size_t)row * p.D + col(k), r[k]);
-                }
-            }
+            for (int e = 0; e < 8; ++e) r.v[e] = fmaf(r.v[e], w.v[e], b.v[e]);
+            if (live) store8(static_cast<TO *>(p.o) + (size_t)row * p.D + c, r);
         }
     }
 }
@@ -203,17 +217,19 @@ struct NormBwdParams {
     NormParams f;   // res = r'
     const void *d_o, *d_ro;
     void *d_res, *d_y, *d_gate;
-    float *part;    // [row groups of the grid][5][D]: w_post, b_post, scale, w_pre, b_pre
+    float *part;    // [CTAs][5][D]: w_post, b_post, scale, w_pre, b_pre
 };
 
 // One vector of 8 channels a lane, so that the five parameter gradients of its channels (40 registers) stay in registers
 // over all rows the group walks; D <= 256 WPR.
 template <typename TI, typename TR, typename TG, int WPR>
-__global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, 1) blocknorm_bwd_kernel(const NormBwdParams q)
+__global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 2) blocknorm_bwd_kernel(const NormBwdParams q)
 {
     constexpr int GROUPS = WPR > 8 ? 1 : 8 / WPR;
     const NormParams &p = q.f;
+    constexpr int WIDTH = WPR * 256;
     __shared__ float buf[GROUPS * 2 * WPR * 2];
+    extern __shared__ __align__(16) float s_w[];   // w_post, b_post, scale, w_pre [WIDTH]; in the end the groups' sums
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / WPR, wr = warp % WPR;
     RowSum<WPR, 2> sum = {buf, 0, group, wr, lane};
     const float inv_d = 1.f / p.D;
@@ -222,25 +238,41 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, 1) blocknorm_bwd_ker
     Vec8 acc[5];
 #pragma unroll
     for (int k = 0; k < 5; ++k) acc[k] = fill8(0.f);
-    const bool post = p.y != nullptr, pre = q.d_o != nullptr;
+    const bool post = p.y != nullptr, pre = q.d_o != nullptr, gated = p.gate != nullptr;
+    stage_weight(s_w, p.w_post, 1.f, p.D, WIDTH);
+    stage_weight(s_w + WIDTH, p.b_post, 0.f, p.D, WIDTH);
+    stage_weight(s_w + 2 * WIDTH, p.scale, 1.f, p.D, WIDTH);
+    stage_weight(s_w + 3 * WIDTH, p.w_pre, 1.f, p.D, WIDTH);
+    __syncthreads();
 
-    for (long long row = (long long)blockIdx.x * GROUPS + group; row < p.T; row += (long long)gridDim.x * GROUPS) {
-        Vec8 hat = fill8(0.f), v = fill8(0.f), y = fill8(0.f), gr = fill8(0.f), ga = fill8(1.f), d_o = fill8(0.f), d_r = fill8(0.f);
-        if (live) {
-            if (q.d_ro) d_r = load8(static_cast<const TR *>(q.d_ro) + (size_t)row * p.D + c);
-            if (pre) {
-                d_o = load8(static_cast<const TI *>(q.d_o) + (size_t)row * p.D + c);
-                hat = load8(static_cast<const TR *>(p.res) + (size_t)row * p.rs + c);
-            }
-            if (post) {
-                y = load8(static_cast<const TI *>(p.y) + (size_t)row * p.ys + c);
-                if (p.gate) {
-                    gr = load8(static_cast<const TI *>(p.gate) + (size_t)row * p.gs + c);
+    const long long stride = (long long)gridDim.x * GROUPS;
+    long long row = (long long)blockIdx.x * GROUPS + group;
+    Raw8<TR> rr, rd;
+    Raw8<TI> ro, ry, rg;
+    auto fetch = [&](long long at) {
+        const bool ok = live && at < p.T;
+        if (ok && q.d_ro) rd.load(static_cast<const TR *>(q.d_ro) + (size_t)at * p.D + c); else rd.zero();
+        if (ok && pre) {
+            ro.load(static_cast<const TI *>(q.d_o) + (size_t)at * p.D + c);
+            rr.load(static_cast<const TR *>(p.res) + (size_t)at * p.rs + c);
+        } else {
+            ro.zero();
+            rr.zero();
+        }
+        if (ok && post) ry.load(static_cast<const TI *>(p.y) + (size_t)at * p.ys + c); else ry.zero();
+        if (ok && gated) rg.load(static_cast<const TI *>(p.gate) + (size_t)at * p.gs + c); else rg.zero();
+    };
+    fetch(row);
+    for (; row < p.T; row += stride) {
+        Vec8 hat = rr.get(), d_o = ro.get(), d_r = rd.get(), v, ga = fill8(1.f);
+        const Raw8<TI> ky = ry, kg = rg;   // unpacked again where they are wanted, half the registers until then
+        fetch(row + stride);
+        {
+            const Vec8 y = ky.get(), gr = kg.get();
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) ga.v[e] = act_f(gr.v[e], p.gate_act);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v.v[e] = p.gate_after ? y.v[e] : y.v[e] * ga.v[e];
+            for (int e = 0; e < 8; ++e) {
+                if (gated) ga.v[e] = act_f(gr.v[e], p.gate_act);
+                v.v[e] = p.gate_after ? y.v[e] : y.v[e] * ga.v[e];
             }
         }
         // statistics of both norms together: [0] = r', [1] = v
@@ -274,7 +306,7 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, 1) blocknorm_bwd_ker
         if (pre) {
             Vec8 dh = fill8(0.f);
             s[0] = s[1] = 0.f;
-            const Vec8 w = live ? opt8(p.w_pre, c, 1.f) : fill8(0.f);
+            const Vec8 w = load8(s_w + 3 * WIDTH + c);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 hat.v[e] *= i0;
@@ -299,7 +331,7 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, 1) blocknorm_bwd_ker
             Vec8 dn = fill8(0.f), dm = fill8(0.f), n = fill8(0.f);
             s[0] = s[1] = 0.f;
             if (live) {
-                const Vec8 w = opt8(p.w_post, c, 1.f), b = opt8(p.b_post, c, 0.f), sc = opt8(p.scale, c, 1.f);
+                const Vec8 w = load8(s_w + c), b = load8(s_w + WIDTH + c), sc = load8(s_w + 2 * WIDTH + c);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     v.v[e] *= i1;
@@ -322,6 +354,7 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, 1) blocknorm_bwd_ker
                 for (int e = 0; e < 8; ++e) dn.v[e] = i1 * (fmaf(-v.v[e], k0, dn.v[e]) - k1);
             }
             if (live) {
+                const Vec8 y = ky.get(), gr = kg.get();
                 Vec8 out;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) out.v[e] = p.gate_after ? dn.v[e] : dn.v[e] * ga.v[e];
@@ -335,8 +368,25 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, 1) blocknorm_bwd_ker
             }
         }
     }
-    if (live) {
-        float *o = q.part + ((size_t)blockIdx.x * GROUPS + group) * 5 * p.D + c;
+    // sums of the CTA's row groups, one partial row per CTA
+    if (GROUPS > 1) {
+#pragma unroll
+        for (int k = 0; k < 5; ++k) {
+            __syncthreads();
+            if (group > 0) store8(s_w + (group - 1) * WIDTH + c, acc[k]);
+            __syncthreads();
+            if (group == 0) {
+#pragma unroll
+                for (int w = 0; w < GROUPS - 1; ++w) {
+                    const Vec8 v = load8(s_w + w * WIDTH + c);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) acc[k].v[e] += v.v[e];
+                }
+            }
+        }
+    }
+    if (live && group == 0) {
+        float *o = q.part + (size_t)blockIdx.x * 5 * p.D + c;
 #pragma unroll
         for (int k = 0; k < 5; ++k) store8(o + (size_t)k * p.D, acc[k]);
     }
@@ -345,7 +395,7 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, 1) blocknorm_bwd_ker
 struct NormSums {
     float *out[5];
 };
-// sums over the row groups in two fixed steps: 8 warps take every eighth partial, then meet in shared memory
+// sums over the CTAs in two fixed steps: 8 warps take every eighth partial, then meet in shared memory
 __global__ void __launch_bounds__(256) blocknorm_sum_kernel(const float *part, NormSums sums, int nparts, int D)
 {
     __shared__ float red[8][33];
@@ -364,57 +414,67 @@ __global__ void __launch_bounds__(256) blocknorm_sum_kernel(const float *part, N
     }
 }
 
-template <typename TI, typename TR, typename TO>
-chela_status_t fwd_d(const NormParams &p, cudaStream_t stream)
-{
-#define CHELA_NORM_FWD(WPR, VPT)                                                                                   \
-    do {                                                                                                           \
-        constexpr int groups = WPR > 8 ? 1 : 8 / WPR;                                                              \
-        const long long need = ((long long)p.T + groups - 1) / groups;                                             \
-        const unsigned grid = (unsigned)(need < 148 * 64 ? need : 148 * 64);                                       \
-        blocknorm_fwd_kernel<TI, TR, TO, WPR, VPT><<<grid, WPR > 8 ? 32 * WPR : 256, 0, stream>>>(p);              \
-    } while (0)
-    if (p.D <= 256) CHELA_NORM_FWD(1, 1);
-    else if (p.D <= 512) CHELA_NORM_FWD(1, 2);
-    else if (p.D <= 1024) CHELA_NORM_FWD(2, 2);
-    else if (p.D <= 2048) CHELA_NORM_FWD(4, 2);
-    else if (p.D <= 4096) CHELA_NORM_FWD(8, 2);
-    else CHELA_NORM_FWD(16, 2);
-#undef CHELA_NORM_FWD
-    return last_launch_status();
-}
-
-int bwd_wpr(int D)
+int row_warps(int D)
 {
     int w = 1;
     while (w * 256 < D) w <<= 1;
     return w;
 }
-int bwd_groups(int wpr) { return wpr > 8 ? 1 : 8 / wpr; }
-int bwd_grid(int T, int D)
+int row_groups(int wpr) { return wpr > 8 ? 1 : 8 / wpr; }
+// CTAs that walk the rows: as many as are resident, no more than there are row groups
+int row_grid(int T, int D, int per_sm)
 {
-    const int g = bwd_groups(bwd_wpr(D)), need = (int)(((long long)T + g - 1) / g);
-    return need < 148 * 4 ? need : 148 * 4;
+    const int g = row_groups(row_warps(D)), need = (int)(((long long)T + g - 1) / g);
+    return need < 148 * per_sm ? need : 148 * per_sm;
+}
+constexpr int kFwdPerSm = 3, kBwdPerSm = 2;
+
+template <typename K, typename P>
+chela_status_t norm_launch(K kern, const P &p, int grid, int threads, size_t smem, cudaStream_t stream)
+{
+    if (smem > 47 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return cuda_status(e);
+    }
+    kern<<<grid, threads, smem, stream>>>(p);
+    return last_launch_status();
+}
+
+template <typename TI, typename TR, typename TO>
+chela_status_t fwd_d(const NormParams &p, cudaStream_t stream)
+{
+    const int wpr = row_warps(p.D), grid = row_grid(p.T, p.D, kFwdPerSm);
+    const size_t smem = (size_t)5 * wpr * 256 * 4;
+    switch (wpr) {
+    case 1: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 1>, p, grid, 256, smem, stream);
+    case 2: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 2>, p, grid, 256, smem, stream);
+    case 4: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 4>, p, grid, 256, smem, stream);
+    case 8: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 8>, p, grid, 256, smem, stream);
+    case 16: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 16>, p, grid, 512, smem, stream);
+    default: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 32>, p, grid, 1024, smem, stream);
+    }
 }
 
 template <typename TI, typename TR, typename TG>
 chela_status_t bwd_d(const NormBwdParams &q, const NormSums &sums, cudaStream_t stream)
 {
     const NormParams &p = q.f;
-    const int wpr = bwd_wpr(p.D), grid = bwd_grid(p.T, p.D);
+    const int wpr = row_warps(p.D), grid = row_grid(p.T, p.D, kBwdPerSm);
+    const int rows = row_groups(wpr) - 1 > 4 ? row_groups(wpr) - 1 : 4;
+    const size_t smem = (size_t)rows * wpr * 256 * 4;
+    chela_status_t st;
     switch (wpr) {
-    case 1: blocknorm_bwd_kernel<TI, TR, TG, 1><<<grid, 256, 0, stream>>>(q); break;
-    case 2: blocknorm_bwd_kernel<TI, TR, TG, 2><<<grid, 256, 0, stream>>>(q); break;
-    case 4: blocknorm_bwd_kernel<TI, TR, TG, 4><<<grid, 256, 0, stream>>>(q); break;
-    case 8: blocknorm_bwd_kernel<TI, TR, TG, 8><<<grid, 256, 0, stream>>>(q); break;
-    case 16: blocknorm_bwd_kernel<TI, TR, TG, 16><<<grid, 512, 0, stream>>>(q); break;
-    default: blocknorm_bwd_kernel<TI, TR, TG, 32><<<grid, 1024, 0, stream>>>(q); break;
+    case 1: st = norm_launch(blocknorm_bwd_kernel<TI, TR, TG, 1>, q, grid, 256, smem, stream); break;
+    case 2: st = norm_launch(blocknorm_bwd_kernel<TI, TR, TG, 2>, q, grid, 256, smem, stream); break;
+    case 4: st = norm_launch(blocknorm_bwd_kernel<TI, TR, TG, 4>, q, grid, 256, smem, stream); break;
+    case 8: st = norm_launch(blocknorm_bwd_kernel<TI, TR, TG, 8>, q, grid, 256, smem, stream); break;
+    case 16: st = norm_launch(blocknorm_bwd_kernel<TI, TR, TG, 16>, q, grid, 512, smem, stream); break;
+    default: st = norm_launch(blocknorm_bwd_kernel<TI, TR, TG, 32>, q, grid, 1024, smem, stream); break;
     }
-    chela_status_t st = last_launch_status();
     bool any = false;
     for (int k = 0; k < 5; ++k) any = any || sums.out[k];
     if (st == CHELA_OK && any) {
-        blocknorm_sum_kernel<<<dim3((p.D + 31) / 32, 5), 256, 0, stream>>>(q.part, sums, grid * bwd_groups(wpr), p.D);
+        blocknorm_sum_kernel<<<dim3((p.D + 31) / 32, 5), 256, 0, stream>>>(q.part, sums, grid, p.D);
         st = last_launch_status();
     }
     return st;
@@ -451,7 +511,7 @@ chela_status_t launch_blocknorm_fwd(const chela_blocknorm_args_t &a, void *res_o
 
 size_t blocknorm_bwd_workspace_bytes(int T, int D)
 {
-    return align_up((size_t)bwd_grid(T, D) * bwd_groups(bwd_wpr(D)) * 5 * D * sizeof(float), 256);
+    return align_up((size_t)row_grid(T, D, kBwdPerSm) * 5 * D * sizeof(float), 256);
 }
 
 chela_status_t launch_blocknorm_bwd(const chela_blocknorm_args_t &a, const void *d_o, const void *d_res_out, void *d_res, void *d_y,

@@ -150,6 +150,8 @@ chela_status_t launch_gate_combine(const float *o, const void *g_a, const void *
 chela_status_t launch_shortconv_carry(const void *x, long long x_stride, const float *w, const float *bias, void *y,
                                       const void *state_in, void *state_out, const int *seq_offsets, int S, int T, int D, int width,
                                       int act, chela_dtype_t io_dtype, cudaStream_t stream);
+chela_status_t launch_shortconv_step(const void *x, long long x_stride, const float *w, const float *bias, void *y, const void *state_in,
+                                     void *state_out, int S, int D, int width, int act, chela_dtype_t io_dtype, cudaStream_t stream);
 size_t shortconv_bwd_workspace_bytes(int T, int D, int width);
 chela_status_t launch_shortconv_bwd(const void *x, long long x_stride, const float *w, const float *bias, const void *d_y,
                                     long long d_y_stride, const void *state_in, const void *d_state_out, void *d_x, float *d_w,

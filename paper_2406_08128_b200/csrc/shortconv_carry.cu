@@ -59,55 +59,125 @@ __device__ __forceinline__ void store_state(const ConvParams &p, int s, const Se
     }
 }
 
+// taps[j] = (w[c][j], w[c+1][j], w[c+2][j], w[c+3][j]).  Four channels' taps are 4 width contiguous floats from a multiple
+// of 16 bytes on, read as vectors where the width is a template argument.
 template <int W>
 __device__ __forceinline__ void load_taps(const float *w, int width, int c, float4 (&taps)[W])
 {
+    if (width == W) {
+        float f[4 * W];
 #pragma unroll
-    for (int j = 0; j < W; ++j)
-        taps[j] = j < width ? make_float4(w[(size_t)c * width + j], w[(size_t)(c + 1) * width + j], w[(size_t)(c + 2) * width + j],
-                                          w[(size_t)(c + 3) * width + j])
-                            : zero4();
+        for (int j = 0; j < W; ++j) {
+            const float4 v = reinterpret_cast<const float4 *>(w + (size_t)c * W)[j];
+            f[4 * j] = v.x; f[4 * j + 1] = v.y; f[4 * j + 2] = v.z; f[4 * j + 3] = v.w;
+        }
+#pragma unroll
+        for (int j = 0; j < W; ++j) taps[j] = make_float4(f[j], f[W + j], f[2 * W + j], f[3 * W + j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+            taps[j] = j < width ? make_float4(w[(size_t)c * width + j], w[(size_t)(c + 1) * width + j], w[(size_t)(c + 2) * width + j],
+                                              w[(size_t)(c + 3) * width + j])
+                                : zero4();
+    }
+}
+
+// (item / nvec, item % nvec) without a 64-bit division where 32 bits do
+__device__ __forceinline__ void split_item(long long item, long long items, int nvec, long long &blk, int &cv)
+{
+    if (items <= 0x7fffffffLL) {
+        blk = (unsigned)item / (unsigned)nvec;
+        cv = (int)((unsigned)item % (unsigned)nvec);
+    } else {
+        blk = item / nvec;
+        cv = (int)(item % nvec);
+    }
 }
 
 // W: taps held in registers (the width itself up to 4; 8 and 16 for the widths up to those, their extra taps zero).
+// kTok tokens in groups of SUB whose loads are in flight while the group before is computed: with four loads a thread the
+// kernel reached 29 % of the measured HBM rate (65536 x 1024, bf16).
 template <typename T, int W>
-__global__ void __launch_bounds__(256) conv_carry_kernel(const ConvParams p, long long items)
+__global__ void __launch_bounds__(256, W <= 4 ? (sizeof(T) == 2 ? 4 : 3) : 1) conv_carry_kernel(const ConvParams p, long long items)
 {
     constexpr int SUB = 4;
     const int nvec = p.D / 4;
     for (long long idx = blockIdx.x * (long long)blockDim.x + threadIdx.x; idx < items; idx += (long long)gridDim.x * blockDim.x) {
-        const int c = 4 * (int)(idx % nvec);
-        const long long blk = idx / nvec;
+        long long blk;
+        int cv;
+        split_item(idx, items, nvec, blk, cv);
+        const int c = 4 * cv;
         const int s = packed_block_seq(p.off, p.S, p.T, kTok, blk);
         const SeqRange sr = seq_range(p.off, s, p.S, p.T);
         const int b = (int)(blk - (sr.start / kTok + s)), t0 = b * kTok;
         if (b < 0) continue;
         if (t0 < sr.len) {
-            float4 taps[W], in[SUB + W - 1];
+            const int end = min(t0 + kTok, sr.len);
+            const T *px = static_cast<const T *>(p.x) + (size_t)(sr.start + t0) * p.xs + c;
+            T *py = static_cast<T *>(p.y) + (size_t)(sr.start + t0) * p.D + c;
+            Raw4<T> raw[SUB];
+            auto fetch = [&](int t) {
+#pragma unroll
+                for (int i = 0; i < SUB; ++i)
+                    if (t + i < end) raw[i].load(px + (size_t)i * p.xs); else raw[i].zero();
+                px += (size_t)SUB * p.xs;
+            };
+            fetch(t0);
+            float4 taps[W], in[W];   // in[j] = x_{t-j}
             load_taps<W>(p.w, p.width, c, taps);
             const float4 bias = p.bias ? load4(p.bias + c) : zero4();
 #pragma unroll
-            for (int i = 0; i < W - 1; ++i) in[i] = row_at<T>(p, s, sr.start, sr.len, t0 - (W - 1) + i, c);
+            for (int j = 1; j < W; ++j) in[j - 1] = row_at<T>(p, s, sr.start, sr.len, t0 - j, c);
 #pragma unroll 1
-            for (int t = t0; t < min(t0 + kTok, sr.len); t += SUB) {
+            for (int t = t0; t < end; t += SUB) {
+                Raw4<T> cur[SUB];
 #pragma unroll
-                for (int i = 0; i < SUB; ++i) in[W - 1 + i] = row_at<T>(p, s, sr.start, sr.len, t + i, c);
+                for (int i = 0; i < SUB; ++i) cur[i] = raw[i];
+                if (t + SUB < end) fetch(t + SUB);
 #pragma unroll
                 for (int i = 0; i < SUB; ++i) {
-                    if (t + i < sr.len) {
-                        float4 u = bias;
 #pragma unroll
-                        for (int j = 0; j < W; ++j) u = fma4(taps[j], in[W - 1 + i - j], u);
-                        if (p.act) u = make_float4(silu_acc(u.x), silu_acc(u.y), silu_acc(u.z), silu_acc(u.w));
-                        store4(static_cast<T *>(p.y) + (size_t)(sr.start + t + i) * p.D + c, u);
-                    }
+                    for (int j = W - 1; j > 0; --j) in[j] = in[j - 1];
+                    in[0] = cur[i].get();
+                    float4 u = bias;
+#pragma unroll
+                    for (int j = 0; j < W; ++j) u = fma4(taps[j], in[j], u);
+                    if (p.act) u = make_float4(silu_acc(u.x), silu_acc(u.y), silu_acc(u.z), silu_acc(u.w));
+                    if (t + i < end) store4(py + (size_t)i * p.D, u);
                 }
-#pragma unroll
-                for (int i = 0; i < W - 1; ++i) in[i] = in[SUB + i];
+                py += (size_t)SUB * p.D;
             }
         }
         if (b == 0 && p.state_out) store_state<T>(p, s, sr, c);
     }
+}
+
+// One token per sequence: a thread reads its channels' carried rows and the new one, writes the output and the rows moved on.
+template <typename T, int W>
+__global__ void __launch_bounds__(128) conv_step_kernel(const ConvParams p)
+{
+    const int nvec = p.D / 4;
+    const long long idx = blockIdx.x * (long long)blockDim.x + threadIdx.x;
+    if (idx >= (long long)p.S * nvec) return;
+    long long row;
+    int cv;
+    split_item(idx, (long long)p.S * nvec, nvec, row, cv);
+    const int c = 4 * cv, s = (int)row, n = p.width - 1;
+    float4 in[W], taps[W];
+    in[0] = load4(static_cast<const T *>(p.x) + (size_t)s * p.xs + c);
+    const T *held = static_cast<const T *>(p.state_in) + ((size_t)s * n) * p.D + c;
+#pragma unroll
+    for (int j = 1; j < W; ++j) in[j] = j <= n ? load4(held + (size_t)(n - j) * p.D) : zero4();
+    load_taps<W>(p.w, p.width, c, taps);
+    float4 u = p.bias ? load4(p.bias + c) : zero4();
+#pragma unroll
+    for (int j = 0; j < W; ++j) u = fma4(taps[j], in[j], u);
+    if (p.act) u = make_float4(silu_acc(u.x), silu_acc(u.y), silu_acc(u.z), silu_acc(u.w));
+    store4(static_cast<T *>(p.y) + (size_t)s * p.D + c, u);
+    T *keep = static_cast<T *>(p.state_out) + ((size_t)s * n) * p.D + c;
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j)
+        if (j < n) store4(keep + (size_t)(n - 1 - j) * p.D, in[j]);
 }
 
 // ------------------------------------------------------------------------------------------------ backward
@@ -121,28 +191,14 @@ struct ConvBwdParams {
     float *part;   // [gridDim.y][width + 1][D]: taps, bias
 };
 
-// d_u at position t: d_y act'(u), zero outside the sequence
-template <typename T, int W>
-__device__ __forceinline__ float4 d_u_at(const ConvBwdParams &q, const SeqRange &sr, int t, int c, const float4 (&taps)[W], float4 bias,
-                                         const float4 *in /* in[j] = x_{t-W+1+j} */)
-{
-    if (t >= sr.len) return zero4();
-    float4 d = load4(static_cast<const T *>(q.dy) + (size_t)(sr.start + t) * q.dys + c);
-    if (q.f.act) {
-        float4 u = bias;
-#pragma unroll
-        for (int j = 0; j < W; ++j) u = fma4(taps[j], in[W - 1 - j], u);
-        d = make_float4(d.x * d_silu(u.x), d.y * d_silu(u.y), d.z * d_silu(u.z), d.w * d_silu(u.w));
-    }
-    return d;
-}
-
 // A CTA: 32 lanes x 4 channels, 8 warps that walk work items of kBwdTok tokens; the taps' gradients stay in registers until
 // the end, are added over the warps in shared memory and leave as one partial sum per CTA row (a fixed order, no atomics).
-// d_x_t = sum_j w_j d_u_{t+j}: a thread evaluates the d_u of its tokens and of the W - 1 behind them.
+// d_x_t = sum_j w_j d_u_{t+j}: a thread evaluates the d_u of its tokens and of the W - 1 behind them.  x and d_y of SUB
+// tokens are in flight while the SUB before are computed.
 template <typename T, typename TG, int W>
-__global__ void __launch_bounds__(256) conv_bwd_kernel(const ConvBwdParams q, long long nblocks)
+__global__ void __launch_bounds__(256, W <= 4 ? 2 : 1) conv_bwd_kernel(const ConvBwdParams q, long long nblocks)
 {
+    constexpr int SUB = W <= 4 ? 4 : 2;
     const ConvParams &p = q.f;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = (blockIdx.x * 32 + lane) * 4;
@@ -158,35 +214,71 @@ __global__ void __launch_bounds__(256) conv_bwd_kernel(const ConvBwdParams q, lo
             const SeqRange sr = seq_range(p.off, s, p.S, p.T);
             const int b = (int)(blk - (sr.start / kBwdTok + s)), t0 = b * kBwdTok;
             if (b < 0 || t0 >= sr.len) continue;
-            const int end = min(t0 + kBwdTok, sr.len);
-            float4 in[W], du[W];   // in[j] = x_{t-W+1+j}; du[j] = d_u_{t-j}
+            const int end = min(t0 + kBwdTok, sr.len), stop = end + W - 1;
+            const T *px = static_cast<const T *>(p.x) + (size_t)(sr.start + t0) * p.xs + c;
+            const T *pd = static_cast<const T *>(q.dy) + (size_t)(sr.start + t0) * q.dys + c;
+            Raw4<T> rx[SUB], rd[SUB];
+            auto fetch = [&](int t) {
+#pragma unroll
+                for (int i = 0; i < SUB; ++i) {
+                    if (t + i < sr.len && t + i < stop) {
+                        rx[i].load(px + (size_t)i * p.xs);
+                        rd[i].load(pd + (size_t)i * q.dys);
+                    } else {
+                        rx[i].zero();
+                        rd[i].zero();   // d_u is zero behind the sequence
+                    }
+                }
+                px += (size_t)SUB * p.xs;
+                pd += (size_t)SUB * q.dys;
+            };
+            fetch(t0);
+            float4 in[W], du[W];   // in[j] = x_{t-j}; du[j] = d_u_{t-j}
 #pragma unroll
             for (int j = 0; j < W; ++j) du[j] = zero4();
 #pragma unroll
-            for (int j = 1; j < W; ++j) in[j] = row_at<T>(p, s, sr.start, sr.len, t0 - W + j, c);
-            in[0] = zero4();
-#pragma unroll 2
-            for (int t = t0; t < end + W - 1; ++t) {
+            for (int j = 1; j < W; ++j) in[j - 1] = row_at<T>(p, s, sr.start, sr.len, t0 - j, c);
+#pragma unroll 1
+            for (int tg = t0; tg < stop; tg += SUB) {
+                Raw4<T> cx[SUB], cd[SUB];
 #pragma unroll
-                for (int j = 0; j < W - 1; ++j) in[j] = in[j + 1];
-                in[W - 1] = row_at<T>(p, s, sr.start, sr.len, t, c);
-#pragma unroll
-                for (int j = W - 1; j > 0; --j) du[j] = du[j - 1];
-                du[0] = d_u_at<T, W>(q, sr, t, c, taps, bias, in);
-                if (t < end) {
-#pragma unroll
-                    for (int j = 0; j < W; ++j) dw[j] = fma4(du[0], in[W - 1 - j], dw[j]);
-                    db = add4(db, du[0]);
+                for (int i = 0; i < SUB; ++i) {
+                    cx[i] = rx[i];
+                    cd[i] = rd[i];
                 }
-                const int tx = t - (W - 1);   // all terms of d_x at this position are there now
-                if (tx >= t0) {
-                    float4 dx = zero4();
+                if (tg + SUB < stop) fetch(tg + SUB);
 #pragma unroll
-                    for (int j = 0; j < W; ++j) dx = fma4(taps[j], du[W - 1 - j], dx);
-                    const int r = tx - (sr.len - (p.width - 1));
-                    if (q.d_state_out && r >= 0)
-                        dx = add4(dx, load4(static_cast<const T *>(q.d_state_out) + ((size_t)s * (p.width - 1) + r) * p.D + c));
-                    store4(static_cast<TG *>(q.d_x) + (size_t)(sr.start + tx) * p.D + c, dx);
+                for (int i = 0; i < SUB; ++i) {
+                    const int t = tg + i;
+#pragma unroll
+                    for (int j = W - 1; j > 0; --j) {
+                        in[j] = in[j - 1];
+                        du[j] = du[j - 1];
+                    }
+                    in[0] = cx[i].get();
+                    float4 d = cd[i].get();
+                    if (p.act) {
+                        float4 u = bias;
+#pragma unroll
+                        for (int j = 0; j < W; ++j) u = fma4(taps[j], in[j], u);
+                        d = make_float4(d.x * d_silu(u.x), d.y * d_silu(u.y), d.z * d_silu(u.z), d.w * d_silu(u.w));
+                    }
+                    du[0] = t < sr.len ? d : zero4();
+                    if (t < end) {
+#pragma unroll
+                        for (int j = 0; j < W; ++j) dw[j] = fma4(du[0], in[j], dw[j]);
+                        db = add4(db, du[0]);
+                    }
+                    const int tx = t - (W - 1);   // all terms of d_x at this position are there now
+                    if (tx >= t0 && tx < end) {
+                        float4 dx = zero4();
+#pragma unroll
+                        for (int j = 0; j < W; ++j) dx = fma4(taps[j], du[W - 1 - j], dx);
+                        const int r = tx - (sr.len - (p.width - 1));
+                        if (q.d_state_out && r >= 0)
+                            dx = add4(dx, load4(static_cast<const T *>(q.d_state_out) + ((size_t)s * (p.width - 1) + r) * p.D + c));
+                        store4(static_cast<TG *>(q.d_x) + (size_t)(sr.start + tx) * p.D + c, dx);
+                    }
                 }
             }
         }
@@ -243,13 +335,20 @@ __global__ void __launch_bounds__(128) conv_bwd_state_kernel(const ConvBwdParams
     store4(static_cast<TG *>(q.d_state_in) + ((size_t)s * n + r) * p.D + c, acc);
 }
 
+// Partial sums of the CTA rows in a fixed order: 8 warps take every eighth, then meet in shared memory.
 __global__ void __launch_bounds__(256) conv_bwd_sum_kernel(const float *part, float *d_w, float *d_bias, int nparts, int D, int width)
 {
-    const int i = blockIdx.x * blockDim.x + threadIdx.x;   // j * D + c
-    if (i >= (width + 1) * D) return;
+    __shared__ float red[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, j = blockIdx.y;
     float o = 0.f;
-    for (int k = 0; k < nparts; ++k) o += part[(size_t)k * (width + 1) * D + i];
-    const int j = i / D, c = i % D;
+    if (c < D)
+        for (int k = warp; k < nparts; k += 8) o += part[((size_t)k * (width + 1) + j) * D + c];
+    red[warp][lane] = o;
+    __syncthreads();
+    if (warp != 0 || c >= D) return;
+    o = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) o += red[k][lane];
     if (j < width) {
         if (d_w) d_w[(size_t)c * width + j] = o;
     } else if (d_bias) {
@@ -259,9 +358,10 @@ __global__ void __launch_bounds__(256) conv_bwd_sum_kernel(const float *part, fl
 
 int conv_bwd_rows(int T, int D)
 {
-    // CTA rows that walk the work items: about four CTAs per SM over all channel columns, no more than there are items
+    // CTA rows that walk the work items: about two CTAs per SM (as many as are resident) over all channel columns, no
+    // more than there are items
     const int cols = (D / 4 + 31) / 32;
-    const int want = (148 * 4 + cols - 1) / cols, most = (T / kBwdTok + 8) / 8;
+    const int want = (148 * 2 + cols - 1) / cols, most = (T / kBwdTok + 8) / 8;
     return want < most ? want : (most < 1 ? 1 : most);
 }
 
@@ -278,6 +378,23 @@ chela_status_t fwd_w(const ConvParams &p, cudaStream_t stream)
     case 4: conv_carry_kernel<T, 4><<<grid, 256, 0, stream>>>(p, items); break;
     case 5: case 6: case 7: case 8: conv_carry_kernel<T, 8><<<grid, 256, 0, stream>>>(p, items); break;
     default: conv_carry_kernel<T, 16><<<grid, 256, 0, stream>>>(p, items); break;
+    }
+    return last_launch_status();
+}
+
+template <typename T>
+chela_status_t step_w(const ConvParams &p, cudaStream_t stream)
+{
+    const long long need = ((long long)p.S * (p.D / 4) + 127) / 128;
+    if (need > 0x7fffffffLL) return CHELA_ERR_UNSUPPORTED;
+    const unsigned grid = (unsigned)need;
+    switch (p.width) {
+    case 1: conv_step_kernel<T, 1><<<grid, 128, 0, stream>>>(p); break;
+    case 2: conv_step_kernel<T, 2><<<grid, 128, 0, stream>>>(p); break;
+    case 3: conv_step_kernel<T, 3><<<grid, 128, 0, stream>>>(p); break;
+    case 4: conv_step_kernel<T, 4><<<grid, 128, 0, stream>>>(p); break;
+    case 5: case 6: case 7: case 8: conv_step_kernel<T, 8><<<grid, 128, 0, stream>>>(p); break;
+    default: conv_step_kernel<T, 16><<<grid, 128, 0, stream>>>(p); break;
     }
     return last_launch_status();
 }
@@ -299,7 +416,7 @@ chela_status_t bwd_w(const ConvBwdParams &q, float *d_w, float *d_bias, cudaStre
     }
     chela_status_t st = last_launch_status();
     if (st == CHELA_OK && q.part) {
-        conv_bwd_sum_kernel<<<((p.width + 1) * p.D + 255) / 256, 256, 0, stream>>>(q.part, d_w, d_bias, rows, p.D, p.width);
+        conv_bwd_sum_kernel<<<dim3((p.D + 31) / 32, p.width + 1), 256, 0, stream>>>(q.part, d_w, d_bias, rows, p.D, p.width);
         st = last_launch_status();
     }
     if (st == CHELA_OK && q.d_state_in) {
@@ -319,6 +436,13 @@ chela_status_t launch_shortconv_carry(const void *x, long long x_stride, const f
     const bool held = width > 1;
     const ConvParams p = {x, x_stride, w, bias, y, held ? state_in : nullptr, held ? state_out : nullptr, seq_offsets, S, T, D, width, act};
     return io_dtype == CHELA_F32 ? fwd_w<float>(p, stream) : fwd_w<__nv_bfloat16>(p, stream);
+}
+
+chela_status_t launch_shortconv_step(const void *x, long long x_stride, const float *w, const float *bias, void *y, const void *state_in,
+                                     void *state_out, int S, int D, int width, int act, chela_dtype_t io_dtype, cudaStream_t stream)
+{
+    const ConvParams p = {x, x_stride, w, bias, y, state_in, state_out, nullptr, S, S, D, width, act};
+    return io_dtype == CHELA_F32 ? step_w<float>(p, stream) : step_w<__nv_bfloat16>(p, stream);
 }
 
 size_t shortconv_bwd_workspace_bytes(int T, int D, int width)
