@@ -391,7 +391,7 @@ typedef struct {
 
 /*
  * y : [T, D] out_dtype.  state_out : [S, D, N] fp32 or NULL, may be state_in's buffer.  checkpoints: NULL, or a device
- * buffer of chela_selscan_checkpoint_bytes that receives the states at every 32nd token of each sequence, which
+ * buffer of chela_selscan_checkpoint_bytes that receives the states at every 8th token of each sequence, which
  * chela_selscan_bwd then need not compute again.  y may be NULL when only state_out or checkpoints are wanted.
  * workspace: chela_selscan_workspace_bytes (0 unless there are so few sequences and channels that the sequences are split
  * into segments, whose states it holds).

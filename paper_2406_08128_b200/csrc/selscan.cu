@@ -15,7 +15,7 @@
 namespace chela {
 namespace {
 
-constexpr int kCkptTok = 32;   // tokens between checkpoints; also the tile of the backward kernel
+constexpr int kCkptTok = 8;   // tokens between checkpoints; also the tile of the backward kernel
 
 struct ScanParams {
     const void *x, *dt, *b, *c, *z;
@@ -439,312 +439,401 @@ struct ScanBwdParams {
     float *part_d;      // [S][2][D]: d_skip, d_dt_bias
 };
 
-// Tiles of kCkptTok tokens from the last to the first.  With e_t = a_t g_t, the gradient that reaches h_{t-1},
-//   g_t = c_t dy_t + e_{t+1},   e_t = exp(dt_t a) g_t,
-// which is the forward recurrence run backwards, so the slices of a tile meet in the same way in both directions.  h is
-// scanned again from the tile's checkpoint; decays and states of a slice (8 tokens x 4 states each) stay in registers.
-// The sums over channels that dB and dC need are folded over the warp's channel lanes by halves (each fold sends one half
-// of the values away and keeps the other), then over the CTA's channel warps in shared memory, and leave as one partial
-// sum per channel block for selscan_bc_kernel: no atomics, so equal calls give equal bits.
-template <typename TI, typename TG, int N, int WD>
-__global__ void __launch_bounds__(32 * WD * 4) selscan_bwd_kernel(const ScanBwdParams q)
-{
-    constexpr int WT = 4, TOK = 8, TILE = WT * TOK;
-    static_assert(TILE == kCkptTok, "one tile per checkpoint");
-    constexpr int R = N / 4, CPW = 32 / R, DC = CPW * WD, NT = 32 * WD * WT;
-    constexpr int NV = TILE * DC / 4, VPT = (NV + NT - 1) / NT;
-    constexpr int NB = TILE * N / 4, BPT = (NB + NT - 1) / NT;
-    constexpr int YP = TILE * DC + 8;
-    constexpr int LEFT = CPW >= 8 ? 1 : 8 / CPW;                        // dB, dC values a lane is left with
-    const ScanParams &p = q.f;
-    extern __shared__ __align__(16) unsigned char smem[];
-    float4 *s_in = reinterpret_cast<float4 *>(smem);                   // [TILE][DC] dt, dt x, dy silu(z), -
-    float *s_b = reinterpret_cast<float *>(s_in + TILE * DC);          // [TILE][N]
-    float *s_c = s_b + TILE * N;
-    float *s_y = s_c + TILE * N;                                       // [3][R][YP]: <c,h>, <g,b>, sum g a h_prev A
-    float4 *s_p = reinterpret_cast<float4 *>(s_y + 3 * R * YP);        // [WT][WD * 32]
-    float4 *s_h = s_p + WT * WD * 32;
-    float4 *s_e = s_h + WT * WD * 32;
-    float *s_bc = reinterpret_cast<float *>(s_e + WT * WD * 32);       // [WD][TILE][2 N]
-    static_assert((R * YP) % 4 == 0, "16-byte aligned planes");
+template <typename TI, int N, int CH>
+struct BwdShape {
+    static constexpr int NS = 8, NP = 4, R = N / NS, CPW = 32 / R * CH, E16 = 16 / (int)sizeof(TI), WT = 12, TOK = kCkptTok, SUB = 2;
+    static constexpr int LPC = R / CH;                                  // lanes of one channel
+    static constexpr int TS = SUB < LPC ? SUB : LPC, PT = SUB / TS, DUP = LPC / TS;   // see tok0
+    static constexpr int XC = CPW / E16, BC = N / E16;
+    static constexpr int CHUNKS = TOK * (4 * XC + 2 * BC), CPL = (CHUNKS + 31) / 32;
+    static constexpr int RAW_E = CHUNKS * E16, PREP_F = 3 * TOK * CPW, BC_F = 2 * TOK * N, STATE_F = 32 * CH * NS;
+    static constexpr int WARP_B = RAW_E * (int)sizeof(TI) + (PREP_F + BC_F + (TOK / SUB - 1) * STATE_F + STATE_F) * 4;
+    static constexpr size_t SMEM = (size_t)WT * WARP_B;
+};
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int wd = warp % WD, wt = warp / WD;
-    const int nblk = (p.D + DC - 1) / DC;
-    const int s = blockIdx.x / nblk, cb = blockIdx.x % nblk, c0 = cb * DC;
-    const int cl_ = lane / R, chl = wd * CPW + cl_, r = lane % R, ch = c0 + chl;
-    const bool live = ch < p.D;
+// With e_t = exp(dt_t a) g_t, the gradient that reaches h_{t-1}:  g_t = c_t dy_t + e_{t+1}.
+// One CTA is a chain: CPW channels of a sequence, whose tiles of kCkptTok tokens its WT warps take in turn from the last
+// to the first.  A warp runs its tile's states forwards from the checkpoint, keeping every second one in shared memory,
+// and sums at the same time what the tile adds to the gradient that leaves its front, sum_t (prod_{s<=t} exp(dt_s a)) c_t
+// dy_t, and the tile's whole decay.  When the gradient behind the tile has come in from the warp with the tile behind, the
+// one before it (one multiply-add per state) goes on to the next warp, and the tile is run backwards two tokens at a
+// time with their decays and states computed again in registers.  So the only serial part is that one step a tile, and
+// few chains still fill the SMs; the second evaluation of the exponentials costs less than keeping the decays would.
+// Lanes as in the forward kernel: 8 states of CH channels, so that the sums over channels that dB and dC need are begun in
+// the lane; they are folded over the other lanes (each exchange sends one half of the values away and keeps the other) and
+// leave as one partial sum per channel block for selscan_bc_kernel: no atomics, so equal calls give equal bits.
+template <typename TI, typename TG, int N, int CH>
+__global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams q_)
+{
+    using Sh = BwdShape<TI, N, CH>;
+    constexpr int NS = Sh::NS, R = Sh::R, NP = Sh::NP, CPW = Sh::CPW, E16 = Sh::E16, XC = Sh::XC, BC = Sh::BC, CPL = Sh::CPL, PT = Sh::PT;
+    constexpr int WT = Sh::WT, TOK = Sh::TOK, SUB = Sh::SUB, DUP = Sh::DUP, LPC = Sh::LPC;
+    static_assert(XC >= 1 && BC >= 1 && R >= CH && SUB == 2 && TOK % LPC == 0 && WT <= 15, "shapes");
+    const ScanParams &p = q_.f;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ longlong2 s_src[6];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    unsigned char *s_mine = smem + warp * Sh::WARP_B;
+    TI *s_raw = reinterpret_cast<TI *>(s_mine);                          // x, dt, z, dy [TOK][CPW], b, c [TOK][N]
+    float *s_dt = reinterpret_cast<float *>(s_mine + Sh::RAW_E * sizeof(TI)), *s_dx = s_dt + TOK * CPW, *s_dg = s_dx + TOK * CPW;
+    float *s_bc = s_dt + Sh::PREP_F;                                     // b, c [TOK][N] in fp32
+    float4 *s_keep = reinterpret_cast<float4 *>(s_bc + Sh::BC_F);        // states before tokens 2, 4, 6: [CH NS / 4][32] each
+    constexpr int HAND = Sh::WARP_B - Sh::STATE_F * 4;
+    float4 *s_down = reinterpret_cast<float4 *>(s_mine + HAND);          // the gradient handed down
+
+    const int nblk = (p.D + CPW - 1) / CPW;
+    const int s = blockIdx.x / nblk, cb = blockIdx.x % nblk, c0 = cb * CPW;
+    const int q = lane % R, grp = lane / R;
+    const int chl = grp * CH + q % CH, ch = c0 + chl, n0 = NS * q;
+    const int tok0 = (q / CH / DUP) * PT;   // of two tokens, the first whose outputs this lane writes (DUP lanes have the same)
+    const bool live = ch < p.D, writer = live && (q / CH) % DUP == 0;
     const SeqRange sr = seq_range(p.off, s, p.S, p.T);
     const int g_ = p.G == 1 ? 0 : c0 / (p.D / p.G);
-    const int slot = wd * 32 + lane;
 
-    const TI *px = static_cast<const TI *>(p.x), *pdt = static_cast<const TI *>(p.dt), *pz = static_cast<const TI *>(p.z);
-    const TI *pdy = static_cast<const TI *>(q.dy);
-    const TI *pb = static_cast<const TI *>(p.b) + g_ * N, *pc = static_cast<const TI *>(p.c) + g_ * N;
-
-    float4 a = zero4(), ar = zero4(), ecarry = zero4();
-    float2 da01 = make_float2(0.f, 0.f), da23 = da01;
-    const size_t st = ((size_t)s * p.D + ch) * N + 4 * r;
-    if (live) {
-        ar = *reinterpret_cast<const float4 *>(p.a + (size_t)ch * N + 4 * r);
-        a = make_float4(decay_rate(ar.x), decay_rate(ar.y), decay_rate(ar.z), decay_rate(ar.w));
-        if (q.d_state_out) ecarry = *reinterpret_cast<const float4 *>(q.d_state_out + st);
+    if (threadIdx.x < 6) {
+        const int w = threadIdx.x;
+        const void *base = w == 0 ? p.x : w == 1 ? p.dt : w == 2 ? p.z : w == 3 ? q_.dy : w == 4 ? p.b : p.c;
+        const long long stride = w == 0 ? p.xs : w == 1 ? p.dts : w == 2 ? p.zs : w == 3 ? q_.dys : w == 4 ? p.bs : p.cs;
+        const long long at = (long long)sr.start * stride + (w < 4 ? c0 : g_ * N);
+        s_src[w] = base ? make_longlong2((long long)base + at * (long long)sizeof(TI), stride * (long long)sizeof(TI)) : make_longlong2(0, 0);
     }
-    const float2 a01 = make_float2(a.x, a.y), a23 = make_float2(a.z, a.w);
-    float4 acc_d[VPT], acc_b[VPT];
+    auto states_from = [&](const float *from, float2 (&v)[CH][NP]) {   // this lane's states of a [D][N] array
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) acc_d[i] = acc_b[i] = zero4();
+        for (int j = 0; j < CH; ++j) {
+            float4 u = zero4(), w = u;
+            if ((ch ^ j) < p.D) {
+                const float4 *o = reinterpret_cast<const float4 *>(from + (size_t)(ch ^ j) * N + n0);
+                u = o[0];
+                w = o[1];
+            }
+            v[j][0] = make_float2(u.x, u.y); v[j][1] = make_float2(u.z, u.w);
+            v[j][2] = make_float2(w.x, w.y); v[j][3] = make_float2(w.z, w.w);
+        }
+    };
+    auto states_to = [&](float *to, const float2 (&v)[CH][NP]) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            if ((ch ^ j) < p.D) {
+                float4 *o = reinterpret_cast<float4 *>(to + (size_t)(ch ^ j) * N + n0);
+                o[0] = make_float4(v[j][0].x, v[j][0].y, v[j][1].x, v[j][1].y);
+                o[1] = make_float4(v[j][2].x, v[j][2].y, v[j][3].x, v[j][3].y);
+            }
+        }
+    };
+    auto put = [&](float4 *to, const float2 (&v)[CH][NP]) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int k = 0; k < NP; k += 2) to[(j * NP / 2 + k / 2) * 32 + lane] = make_float4(v[j][k].x, v[j][k].y, v[j][k + 1].x, v[j][k + 1].y);
+    };
+    auto take = [&](const float4 *from, float2 (&v)[CH][NP]) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int k = 0; k < NP; k += 2) {
+                const float4 u = from[(j * NP / 2 + k / 2) * 32 + lane];
+                v[j][k] = make_float2(u.x, u.y);
+                v[j][k + 1] = make_float2(u.z, u.w);
+            }
+    };
+    auto clear = [&](float2 (&v)[CH][NP]) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int k = 0; k < NP; ++k) v[j][k] = make_float2(0.f, 0.f);
+    };
+    float2 a[CH][NP], da[CH][NP];   // decay rates a log2(e); gradient of a
+    states_from(p.a, a);
+#pragma unroll
+    for (int j = 0; j < CH; ++j)
+#pragma unroll
+        for (int k = 0; k < NP; ++k) a[j][k] = make_float2(decay_rate(a[j][k].x), decay_rate(a[j][k].y));
+    clear(da);
+    const float bias = live && p.bias ? p.bias[ch] : 0.f, skip = live && p.dsk ? p.dsk[ch] : 0.f;
+    float sum_skip = 0.f, sum_bias = 0.f;
+    __syncthreads();
 
-    const int ntile = (sr.len + TILE - 1) / TILE;
-    for (int tile = ntile - 1; tile >= 0; --tile) {
-        const int t0 = tile * TILE;
-        float4 kx[VPT], kz[VPT], kdy[VPT], kraw[VPT];
-        __syncthreads();   // the previous tile's readers of shared memory are done
+    const int ntile = (sr.len + TOK - 1) / TOK;
+    for (int tile = ntile - 1 - warp; tile >= 0; tile -= WT) {
+        const int t0 = tile * TOK;
+        float2 h[CH][NP];
+        states_from(p.ckpt + ((size_t)(sr.start / kCkptTok) + s + tile) * p.D * N, h);
+        __syncwarp();   // the tile before is done with shared memory
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const int v = tid + i * NT, t = t0 + v / (DC / 4), cl = 4 * (v % (DC / 4));
-            kx[i] = kz[i] = kdy[i] = kraw[i] = zero4();
-            if (v < NV) {
-                float4 d = zero4(), dg = zero4();
-                if (t < sr.len && c0 + cl < p.D) {
-                    const size_t row = (size_t)(sr.start + t);
-                    kx[i] = load4(px + row * p.xs + c0 + cl);
-                    kdy[i] = load4(pdy + row * q.dys + c0 + cl);
-                    d = load4(pdt + row * p.dts + c0 + cl);
-                    const float4 bias = opt4(p.bias, c0 + cl, 0.f);
-                    d = make_float4(d.x + bias.x, d.y + bias.y, d.z + bias.z, d.w + bias.w);
-                    kraw[i] = d;
-                    if (p.softplus) d = make_float4(softplus_acc(d.x), softplus_acc(d.y), softplus_acc(d.z), softplus_acc(d.w));
-                    dg = kdy[i];
-                    if (pz) {
-                        kz[i] = load4(pz + row * p.zs + c0 + cl);
-                        dg = make_float4(dg.x * gate_f(kz[i].x), dg.y * gate_f(kz[i].y), dg.z * gate_f(kz[i].z), dg.w * gate_f(kz[i].w));
+        for (int i = 0; i < CPL; ++i) {
+            int id = lane + 32 * i;
+            if (id < Sh::CHUNKS) {
+                void *to = s_raw + id * E16;
+                const bool in_x = id < 4 * TOK * XC;
+                const int which = in_x ? id / (TOK * XC) : 4 + (id - 4 * TOK * XC) / (TOK * BC);
+                id = in_x ? id % (TOK * XC) : (id - 4 * TOK * XC) % (TOK * BC);
+                const int per = in_x ? XC : BC, t = id / per;
+                const longlong2 from = s_src[which];
+                const bool ok = from.x && t0 + t < sr.len && (!in_x || c0 + (id % per) * E16 < p.D);
+                copy16(to, reinterpret_cast<const char *>(ok ? from.x + (long long)(t0 + t) * from.y + (id % per) * 16 : (long long)p.x), ok);
+            }
+        }
+        asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < (Sh::BC_F / 4 + 31) / 32; ++i)
+            if (lane + 32 * i < Sh::BC_F / 4) reinterpret_cast<float4 *>(s_bc)[lane + 32 * i] = load4(s_raw + 4 * TOK * CPW + 4 * (lane + 32 * i));
+        // time step, input and gated gradient of every token and channel
+#pragma unroll
+        for (int i0 = 0; i0 < TOK / LPC; i0 += 2) {
+            float d[2];
+            int at[2], tt[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                tt[k] = q / CH + LPC * (i0 + k < TOK / LPC ? i0 + k : i0);
+                at[k] = tt[k] * CPW + chl;
+                d[k] = load1(s_raw + TOK * CPW + at[k]) + bias;
+            }
+            if (p.softplus) {
+                const float2 v = softplus_acc(make_float2(d[0], d[1]));
+                d[0] = v.x;
+                d[1] = v.y;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if (t0 + tt[k] >= sr.len) d[k] = 0.f;   // past the end: decay 1, no input
+                float dg = load1(s_raw + 3 * TOK * CPW + at[k]);
+                if (p.z) dg *= gate_f(load1(s_raw + 2 * TOK * CPW + at[k]));
+                s_dt[at[k]] = d[k];
+                s_dx[at[k]] = d[k] * load1(s_raw + at[k]);
+                s_dg[at[k]] = dg;
+            }
+        }
+        __syncwarp();
+        auto row_of = [&](const float *m, float2 (&o)[NP]) {
+            const float4 u = reinterpret_cast<const float4 *>(m)[0], v = reinterpret_cast<const float4 *>(m)[1];
+            o[0] = make_float2(u.x, u.y); o[1] = make_float2(u.z, u.w);
+            o[2] = make_float2(v.x, v.y); o[3] = make_float2(v.z, v.w);
+        };
+        const float *s_b = s_bc + n0, *s_c = s_b + TOK * N;
+
+        // forwards: states; what the tile adds to the gradient before it
+        float2 add[CH][NP], whole[CH][NP];
+        clear(add);
+#pragma unroll
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int k = 0; k < NP; ++k) whole[j][k] = make_float2(1.f, 1.f);
+#pragma unroll 1
+        for (int u = 0; u < TOK; u += SUB) {
+            if (u) put(s_keep + (u / SUB - 1) * (Sh::STATE_F / 4), h);
+#pragma unroll
+            for (int i = 0; i < SUB; ++i) {
+                float2 bv[NP], cv[NP];
+                row_of(s_b + (u + i) * N, bv);
+                row_of(s_c + (u + i) * N, cv);
+#pragma unroll
+                for (int j = 0; j < CH; ++j) {
+                    const int at = (u + i) * CPW + (chl ^ j);
+                    const float2 d = splat2(s_dt[at]), x = splat2(s_dx[at]), y = splat2(s_dg[at]);
+#pragma unroll
+                    for (int k = 0; k < NP; ++k) {
+                        const float2 v = mul2v(a[j][k], d), e = make_float2(ex2(v.x), ex2(v.y));
+                        h[j][k] = fma2v(e, h[j][k], mul2v(x, bv[k]));
+                        whole[j][k] = mul2v(whole[j][k], e);
+                        add[j][k] = fma2v(whole[j][k], mul2v(cv[k], y), add[j][k]);
                     }
                 }
-                float4 *o = s_in + (v / (DC / 4)) * DC + cl;
-                o[0] = make_float4(d.x, d.x * kx[i].x, dg.x, 0.f);
-                o[1] = make_float4(d.y, d.y * kx[i].y, dg.y, 0.f);
-                o[2] = make_float4(d.z, d.z * kx[i].z, dg.z, 0.f);
-                o[3] = make_float4(d.w, d.w * kx[i].w, dg.w, 0.f);
             }
+        }
+        // the gradient behind the tile comes in, the one before it goes on
+        float2 g[CH][NP];
+        if (tile < ntile - 1) {
+            const int from = (warp + WT - 1) % WT;
+            named_sync(1 + from);
+            take(reinterpret_cast<const float4 *>(smem + from * Sh::WARP_B + HAND), g);
+        } else if (q_.d_state_out) {
+            states_from(q_.d_state_out + (size_t)s * p.D * N, g);
+        } else {
+            clear(g);
         }
 #pragma unroll
-        for (int i = 0; i < BPT; ++i) {
-            const int v = tid + i * NT, t = t0 + v / (N / 4), n = 4 * (v % (N / 4));
-            if (v < NB) {
-                float4 bv = zero4(), cv = zero4();
-                if (t < sr.len) {
-                    const size_t row = (size_t)(sr.start + t);
-                    bv = load4(pb + row * p.bs + n);
-                    cv = load4(pc + row * p.cs + n);
-                }
-                reinterpret_cast<float4 *>(s_b)[v] = bv;
-                reinterpret_cast<float4 *>(s_c)[v] = cv;
-            }
+        for (int j = 0; j < CH; ++j)
+#pragma unroll
+            for (int k = 0; k < NP; ++k) add[j][k] = fma2v(whole[j][k], g[j][k], add[j][k]);
+        if (tile > 0) {
+            put(s_down, add);
+            named_arrive(1 + warp);
+        } else if (q_.d_state_in) {
+            states_to(q_.d_state_in + (size_t)s * p.D * N, add);
         }
-        float4 hin = zero4();
-        if (live) hin = *reinterpret_cast<const float4 *>(p.ckpt + (((size_t)(sr.start / kCkptTok) + s + tile) * p.D + ch) * N + 4 * r);
-        __syncthreads();
 
-        // states of this slice from zero; the gradient that leaves its front, likewise
-        float2 e01[TOK], e23[TOK], h01[TOK], h23[TOK];
-        float2 hh01 = make_float2(0.f, 0.f), hh23 = hh01, p01 = make_float2(1.f, 1.f), p23 = p01;
+        // backwards, two tokens at a time
+        float *part = q_.part_bc + ((size_t)cb * p.T + sr.start + t0) * (2 * N);   // [token][dB N | dC N]
+#pragma unroll 1
+        for (int u = TOK - SUB; u >= 0; u -= SUB) {
+            if (u) take(s_keep + (u / SUB - 1) * (Sh::STATE_F / 4), h);
+            else states_from(p.ckpt + ((size_t)(sr.start / kCkptTok) + s + tile) * p.D * N, h);
+            auto fold_channels = [&](float (&v)[8], float *to) {
+                // this lane's 8 states summed over the 32 / R lanes of other channels; 8 values halve three times at most
+                int first = 0, n = 8;
 #pragma unroll
-        for (int i = 0; i < TOK; ++i) {
-            const int t = wt * TOK + i;
-            const float4 in = s_in[t * DC + chl];
-            const float4 bv = *reinterpret_cast<const float4 *>(s_b + t * N + 4 * r);
-            float2 x01 = mul2v(a01, splat2(in.x)), x23 = mul2v(a23, splat2(in.x));
-            e01[i] = make_float2(ex2(x01.x), ex2(x01.y));
-            e23[i] = make_float2(ex2(x23.x), ex2(x23.y));
-            hh01 = fma2v(e01[i], hh01, mul2v(splat2(in.y), make_float2(bv.x, bv.y)));
-            hh23 = fma2v(e23[i], hh23, mul2v(splat2(in.y), make_float2(bv.z, bv.w)));
-            h01[i] = hh01;
-            h23[i] = hh23;
-            p01 = mul2v(p01, e01[i]);
-            p23 = mul2v(p23, e23[i]);
-        }
-        float2 g01 = make_float2(0.f, 0.f), g23 = g01;
+                for (int o = 16; o >= R; o >>= 1) {
+                    if (n > 1) {
+                        n >>= 1;
+                        const bool up = lane & o;
 #pragma unroll
-        for (int i = TOK - 1; i >= 0; --i) {
-            const int t = wt * TOK + i;
-            const float dg = reinterpret_cast<const float *>(s_in + t * DC + chl)[2];
-            const float4 cv = *reinterpret_cast<const float4 *>(s_c + t * N + 4 * r);
-            g01 = mul2v(e01[i], fma2v(make_float2(cv.x, cv.y), splat2(dg), g01));
-            g23 = mul2v(e23[i], fma2v(make_float2(cv.z, cv.w), splat2(dg), g23));
-        }
-        s_p[wt * (WD * 32) + slot] = make_float4(p01.x, p01.y, p23.x, p23.y);
-        s_h[wt * (WD * 32) + slot] = make_float4(hh01.x, hh01.y, hh23.x, hh23.y);
-        s_e[wt * (WD * 32) + slot] = make_float4(g01.x, g01.y, g23.x, g23.y);
-        __syncthreads();
-        // state before this slice, gradient behind it
-#pragma unroll
-        for (int w = 0; w < WT - 1; ++w) {
-            if (w < wt) {
-                const float4 pw = s_p[w * (WD * 32) + slot], hw = s_h[w * (WD * 32) + slot];
-                hin = make_float4(fmaf(pw.x, hin.x, hw.x), fmaf(pw.y, hin.y, hw.y), fmaf(pw.z, hin.z, hw.z), fmaf(pw.w, hin.w, hw.w));
-            }
-        }
-        float4 ein = ecarry;
-#pragma unroll
-        for (int w = WT - 1; w >= 0; --w) {
-            if (w == wt) ein = ecarry;
-            const float4 pw = s_p[w * (WD * 32) + slot], ew = s_e[w * (WD * 32) + slot];
-            ecarry = make_float4(fmaf(pw.x, ecarry.x, ew.x), fmaf(pw.y, ecarry.y, ew.y), fmaf(pw.z, ecarry.z, ew.z),
-                                 fmaf(pw.w, ecarry.w, ew.w));
-        }
-        const float2 in01 = make_float2(hin.x, hin.y), in23 = make_float2(hin.z, hin.w);
-        float2 f01 = in01, f23 = in23;
-#pragma unroll
-        for (int i = 0; i < TOK; ++i) {
-            const int t = wt * TOK + i;
-            const float4 cv = *reinterpret_cast<const float4 *>(s_c + t * N + 4 * r);
-            f01 = mul2v(f01, e01[i]);
-            f23 = mul2v(f23, e23[i]);
-            h01[i] = add2v(h01[i], f01);
-            h23[i] = add2v(h23[i], f23);
-            const float2 yy = fma2v(make_float2(cv.z, cv.w), h23[i], mul2v(make_float2(cv.x, cv.y), h01[i]));
-            s_y[r * YP + t * DC + chl] = yy.x + yy.y;
-        }
-        g01 = make_float2(ein.x, ein.y);
-        g23 = make_float2(ein.z, ein.w);
-#pragma unroll
-        for (int i = TOK - 1; i >= 0; --i) {
-            const int t = wt * TOK + i;
-            const float4 in = s_in[t * DC + chl];
-            const float4 bv = *reinterpret_cast<const float4 *>(s_b + t * N + 4 * r);
-            const float4 cv = *reinterpret_cast<const float4 *>(s_c + t * N + 4 * r);
-            g01 = fma2v(make_float2(cv.x, cv.y), splat2(in.z), g01);
-            g23 = fma2v(make_float2(cv.z, cv.w), splat2(in.z), g23);
-            float v[8];
-            {
-                const float2 d01 = mul2v(g01, splat2(in.y)), d23 = mul2v(g23, splat2(in.y));
-                const float2 k01 = mul2v(h01[i], splat2(in.z)), k23 = mul2v(h23[i], splat2(in.z));
-                v[0] = d01.x; v[1] = d01.y; v[2] = d23.x; v[3] = d23.y;
-                v[4] = k01.x; v[5] = k01.y; v[6] = k23.x; v[7] = k23.y;
-            }
-            const float2 gb = fma2v(g23, make_float2(bv.z, bv.w), mul2v(g01, make_float2(bv.x, bv.y)));
-            g01 = mul2v(g01, e01[i]);   // e_t
-            g23 = mul2v(g23, e23[i]);
-            const float2 k01 = mul2v(g01, i ? h01[i ? i - 1 : 0] : in01), k23 = mul2v(g23, i ? h23[i ? i - 1 : 0] : in23);
-            const float2 sa = fma2v(k23, make_float2(ar.z, ar.w), mul2v(k01, make_float2(ar.x, ar.y)));
-            da01 = fma2v(k01, splat2(in.x), da01);
-            da23 = fma2v(k23, splat2(in.x), da23);
-            s_y[(R + r) * YP + t * DC + chl] = gb.x + gb.y;
-            s_y[(2 * R + r) * YP + t * DC + chl] = sa.x + sa.y;
-            // fold the 8 sums over the warp's channels
-            int first = 0, n = 8;
-#pragma unroll
-            for (int o = 16; o >= R; o >>= 1) {
-                if (n > 1) {
-                    n >>= 1;
-                    const bool up = lane & o;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (j < n) {
-                            const float send = up ? v[j] : v[j + n], keep = up ? v[j + n] : v[j];
-                            v[j] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+                        for (int k = 0; k < 4; ++k) {
+                            if (k < n) {
+                                const float send = up ? v[k] : v[k + n], keep = up ? v[k + n] : v[k];
+                                v[k] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+                            }
                         }
-                    }
-                    if (up) first += n;
-                } else {
-                    v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
-                }
-            }
-            if (CPW <= 8 || (cl_ & (CPW / 8 - 1)) == 0) {
-#pragma unroll
-                for (int j = 0; j < LEFT; ++j) {
-                    const int k = first + j;
-                    s_bc[(wd * TILE + t) * (2 * N) + (k >> 2) * N + 4 * r + (k & 3)] = v[j];
-                }
-            }
-        }
-        __syncthreads();
-        for (int v = tid; v < TILE * 2 * N / 4; v += NT) {
-            const int t = v / (2 * N / 4);
-            if (t0 + t >= sr.len) break;
-            float4 o = reinterpret_cast<const float4 *>(s_bc)[v];
-#pragma unroll
-            for (int w = 1; w < WD; ++w) {
-                const float4 k = reinterpret_cast<const float4 *>(s_bc + w * TILE * 2 * N)[v];
-                o.x += k.x; o.y += k.y; o.z += k.z; o.w += k.w;
-            }
-            *reinterpret_cast<float4 *>(q.part_bc + ((size_t)cb * p.T + sr.start + t0) * (2 * N) + 4 * (size_t)v) = o;
-        }
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const int v = tid + i * NT, t = t0 + v / (DC / 4), cl = 4 * (v % (DC / 4));
-            if (v < NV && t < sr.len && c0 + cl < p.D) {
-                float4 sums[3];
-#pragma unroll
-                for (int k = 0; k < 3; ++k) {
-                    sums[k] = zero4();
-#pragma unroll
-                    for (int j = 0; j < R; ++j) {
-                        const float4 part = *reinterpret_cast<const float4 *>(s_y + (k * R + j) * YP + 4 * v);
-                        sums[k].x += part.x; sums[k].y += part.y; sums[k].z += part.z; sums[k].w += part.w;
+                        if (up) first += n;
+                    } else {
+                        v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
                     }
                 }
-                const float4 dv = opt4(p.dsk, c0 + cl, 0.f);
-                const size_t o = (size_t)(sr.start + t) * p.D + c0 + cl;
-                float4 ox, odt, oz;
-                auto one = [&](float x, float z, float dy, float raw, float dsk, float yh, float gb, float sa, float &rx, float &rdt,
-                               float &rz, float &sd, float &sbias) {
-                    float dg = dy;
-                    if (pz) {
-                        const float sg = sigmoid_acc(z);
-                        dg = dy * (z * sg);
-                        rz = dy * fmaf(dsk, x, yh) * (sg * fmaf(z, 1.f - sg, 1.f));
+                constexpr int GR = 32 / R, KEEP = GR >= 8 ? 1 : 8 / GR;
+                if (to && (GR <= 8 || grp % (GR / 8) == 0)) {
+#pragma unroll
+                    for (int k = 0; k < KEEP; ++k) to[n0 + first + k] = v[k];
+                }
+            };
+            float2 e[SUB][CH][NP], h0[CH][NP];   // decays; the state behind the first token
+            float dts[SUB][CH], dxs[SUB][CH], dgs[SUB][CH];
+            float yh[SUB], gb[SUB], ga[SUB];     // of this lane's channel: sum_n c h, g b, e h_prev a
+            {
+                float2 hh[CH][NP];
+#pragma unroll
+                for (int i = 0; i < SUB; ++i) {
+                    float2 bv[NP], cv[NP];
+                    row_of(s_b + (u + i) * N, bv);
+                    row_of(s_c + (u + i) * N, cv);
+                    float own[CH], v[8];
+#pragma unroll
+                    for (int j = 0; j < CH; ++j) {
+                        const int at = (u + i) * CPW + (chl ^ j);
+                        dts[i][j] = s_dt[at];
+                        dxs[i][j] = s_dx[at];
+                        dgs[i][j] = s_dg[at];
+                        float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+                        for (int k = 0; k < NP; ++k) {
+                            const float2 w = mul2v(a[j][k], splat2(dts[i][j]));
+                            e[i][j][k] = make_float2(ex2(w.x), ex2(w.y));
+                            hh[j][k] = fma2v(e[i][j][k], i ? h0[j][k] : h[j][k], mul2v(splat2(dxs[i][j]), bv[k]));
+                            if (i == 0) h0[j][k] = hh[j][k];
+                            sum = k ? fma2v(cv[k], hh[j][k], sum) : mul2v(cv[k], hh[j][k]);
+                            v[2 * k] = j ? fmaf(dgs[i][j], hh[j][k].x, v[2 * k]) : dgs[i][j] * hh[j][k].x;
+                            v[2 * k + 1] = j ? fmaf(dgs[i][j], hh[j][k].y, v[2 * k + 1]) : dgs[i][j] * hh[j][k].y;
+                        }
+                        own[j] = sum.x + sum.y;
                     }
-                    const float dt = p.softplus ? softplus_acc(raw) : raw;
-                    rx = fmaf(dt, gb, dsk * dg);
-                    rdt = fmaf(x, gb, sa);
-                    if (p.softplus) rdt *= sigmoid_acc(raw);
-                    sd = fmaf(dg, x, sd);
-                    sbias += rdt;
-                };
-                one(kx[i].x, kz[i].x, kdy[i].x, kraw[i].x, dv.x, sums[0].x, sums[1].x, sums[2].x, ox.x, odt.x, oz.x, acc_d[i].x, acc_b[i].x);
-                one(kx[i].y, kz[i].y, kdy[i].y, kraw[i].y, dv.y, sums[0].y, sums[1].y, sums[2].y, ox.y, odt.y, oz.y, acc_d[i].y, acc_b[i].y);
-                one(kx[i].z, kz[i].z, kdy[i].z, kraw[i].z, dv.z, sums[0].z, sums[1].z, sums[2].z, ox.z, odt.z, oz.z, acc_d[i].z, acc_b[i].z);
-                one(kx[i].w, kz[i].w, kdy[i].w, kraw[i].w, dv.w, sums[0].w, sums[1].w, sums[2].w, ox.w, odt.w, oz.w, acc_d[i].w, acc_b[i].w);
-                store4(static_cast<TG *>(q.d_x) + o, ox);
-                store4(static_cast<TG *>(q.d_dt) + o, odt);
-                if (pz) store4(static_cast<TG *>(q.d_z) + o, oz);
+                    yh[i] = CH == 1 ? own[0] : own[0] + __shfl_xor_sync(0xffffffffu, own[CH - 1], 1);
+                    fold_channels(v, t0 + u + i < sr.len ? part + (size_t)(u + i) * 2 * N + N : nullptr);
+                }
+            }
+#pragma unroll
+            for (int i = SUB - 1; i >= 0; --i) {
+                float2 bv[NP], cv[NP];
+                row_of(s_b + (u + i) * N, bv);
+                row_of(s_c + (u + i) * N, cv);
+                float ogb[CH], oga[CH], v[8];
+#pragma unroll
+                for (int j = 0; j < CH; ++j) {
+                    float2 ub = make_float2(0.f, 0.f), ua = ub;
+#pragma unroll
+                    for (int k = 0; k < NP; ++k) {
+                        g[j][k] = fma2v(cv[k], splat2(dgs[i][j]), g[j][k]);
+                        ub = k ? fma2v(g[j][k], bv[k], ub) : mul2v(g[j][k], bv[k]);
+                        v[2 * k] = j ? fmaf(dxs[i][j], g[j][k].x, v[2 * k]) : dxs[i][j] * g[j][k].x;
+                        v[2 * k + 1] = j ? fmaf(dxs[i][j], g[j][k].y, v[2 * k + 1]) : dxs[i][j] * g[j][k].y;
+                        g[j][k] = mul2v(g[j][k], e[i][j][k]);   // e_t
+                        const float2 through = mul2v(g[j][k], i ? h0[j][k] : h[j][k]);
+                        ua = k ? fma2v(through, a[j][k], ua) : mul2v(through, a[j][k]);
+                        da[j][k] = fma2v(through, splat2(dts[i][j]), da[j][k]);
+                    }
+                    ogb[j] = ub.x + ub.y;
+                    oga[j] = ua.x + ua.y;
+                }
+                gb[i] = CH == 1 ? ogb[0] : ogb[0] + __shfl_xor_sync(0xffffffffu, ogb[CH - 1], 1);
+                ga[i] = CH == 1 ? oga[0] : oga[0] + __shfl_xor_sync(0xffffffffu, oga[CH - 1], 1);
+                fold_channels(v, t0 + u + i < sr.len ? part + (size_t)(u + i) * 2 * N : nullptr);
+            }
+            // the other lanes of a channel hold other states: halve the tokens at the first exchange, then add
+            if (R > CH) {
+                int n = SUB;
+#pragma unroll
+                for (int o = R / 2; o >= CH; o >>= 1) {
+                    const bool up = lane & o;
+                    if (n > 1) {
+                        n >>= 1;
+                        auto turn = [&](float (&w)[SUB]) {
+                            const float send = up ? w[0] : w[1], mine = up ? w[1] : w[0];
+                            w[0] = mine + __shfl_xor_sync(0xffffffffu, send, o);
+                        };
+                        turn(yh);
+                        turn(gb);
+                        turn(ga);
+                    } else {
+                        yh[0] += __shfl_xor_sync(0xffffffffu, yh[0], o);
+                        gb[0] += __shfl_xor_sync(0xffffffffu, gb[0], o);
+                        ga[0] += __shfl_xor_sync(0xffffffffu, ga[0], o);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < PT; ++i) {
+                const int t = u + tok0 + i, at = t * CPW + chl;
+                if (writer && t0 + t < sr.len) {
+                    const float x = load1(s_raw + at), dy = load1(s_raw + 3 * TOK * CPW + at), dg = s_dg[at];
+                    const size_t o = (size_t)(sr.start + t0 + t) * p.D + ch;
+                    if (p.z) {
+                        const float z = load1(s_raw + 2 * TOK * CPW + at), sg = sigmoid_acc(z);
+                        store1(static_cast<TG *>(q_.d_z) + o, dy * fmaf(skip, x, yh[i]) * (sg * fmaf(z, 1.f - sg, 1.f)));
+                    }
+                    store1(static_cast<TG *>(q_.d_x) + o, fmaf(s_dt[at], gb[i], skip * dg));
+                    float ddt = fmaf(x, gb[i], 0.6931471805599453f * ga[i]);   // the rates are a log2(e)
+                    if (p.softplus) ddt *= sigmoid_acc(load1(s_raw + TOK * CPW + at) + bias);
+                    store1(static_cast<TG *>(q_.d_dt) + o, ddt);
+                    sum_skip = fmaf(dg, x, sum_skip);
+                    sum_bias += ddt;
+                }
             }
         }
     }
-    if (q.d_state_in && live && wt == 0) *reinterpret_cast<float4 *>(q.d_state_in + st) = ecarry;
-    // this sequence's share of the parameters' gradients
+    if (ntile == 0 && q_.d_state_in && warp == 0) {
+        float2 g[CH][NP];
+        clear(g);
+        if (q_.d_state_out) states_from(q_.d_state_out + (size_t)s * p.D * N, g);
+        states_to(q_.d_state_in + (size_t)s * p.D * N, g);
+    }
+    // this sequence's share of the parameters' gradients: over the warps, then over a channel's lanes
     __syncthreads();
-    s_p[wt * (WD * 32) + slot] = make_float4(da01.x, da01.y, da23.x, da23.y);
-    float4 *s_acc = reinterpret_cast<float4 *>(s_y);   // [2][NT * VPT]
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        const int v = tid + i * NT;
-        if (v < NV) {
-            s_acc[v] = acc_d[i];
-            s_acc[NV + v] = acc_b[i];
-        }
-    }
+    put(s_keep, da);
+    float *s_sum = reinterpret_cast<float *>(s_down);
+    s_sum[lane] = sum_skip;
+    s_sum[32 + lane] = sum_bias;
     __syncthreads();
-    if (live && wt == 0) {
-        float4 o = zero4();
+    if (warp == 0) {
+#pragma unroll 1
+        for (int w = 1; w < WT; ++w) {
+            const unsigned char *other = smem + w * Sh::WARP_B;
+            float2 v[CH][NP];
+            take(reinterpret_cast<const float4 *>(other + Sh::RAW_E * sizeof(TI) + (Sh::PREP_F + Sh::BC_F) * 4), v);
 #pragma unroll
-        for (int w = 0; w < WT; ++w) {
-            const float4 k = s_p[w * (WD * 32) + slot];
-            o.x += k.x; o.y += k.y; o.z += k.z; o.w += k.w;
+            for (int j = 0; j < CH; ++j)
+#pragma unroll
+                for (int k = 0; k < NP; ++k) da[j][k] = add2v(da[j][k], v[j][k]);
+            const float *o = reinterpret_cast<const float *>(other + HAND);
+            sum_skip += o[lane];
+            sum_bias += o[32 + lane];
         }
-        *reinterpret_cast<float4 *>(q.part_a + st) = o;
-    }
-    for (int v = tid; v < 2 * DC / 4; v += NT) {
-        const int which = v / (DC / 4), cq = v % (DC / 4);
-        if (c0 + 4 * cq < p.D) {
-            float4 o = zero4();
-            for (int t = 0; t < TILE; ++t) {
-                const float4 k = s_acc[which * NV + t * (DC / 4) + cq];
-                o.x += k.x; o.y += k.y; o.z += k.z; o.w += k.w;
-            }
-            *reinterpret_cast<float4 *>(q.part_d + ((size_t)s * 2 + which) * p.D + c0 + 4 * cq) = o;
+        states_to(q_.part_a + (size_t)s * p.D * N, da);
+#pragma unroll
+        for (int o = CH; o < R; o <<= 1) {
+            sum_skip += __shfl_xor_sync(0xffffffffu, sum_skip, o);
+            sum_bias += __shfl_xor_sync(0xffffffffu, sum_bias, o);
+        }
+        if (live && q < CH) {
+            q_.part_d[((size_t)s * 2) * p.D + ch] = sum_skip;
+            q_.part_d[((size_t)s * 2 + 1) * p.D + ch] = sum_bias;
         }
     }
 }
@@ -846,23 +935,23 @@ chela_status_t step_n(const ScanParams &p, int N, cudaStream_t stream)
     return last_launch_status();
 }
 
-constexpr int bwd_wd(int N) { return N == 8 ? 2 : 4; }
-constexpr int bwd_channels(int N) { return 32 / (N / 4) * bwd_wd(N); }   // channels of a CTA: 32, 32, 16, 8
+constexpr int bwd_ch(int N) { return N == 8 ? 1 : 2; }
+constexpr int bwd_channels(int N) { return 32 / (N / 8) * bwd_ch(N); }   // channels of a CTA: 32, 32, 16, 8
 
 template <typename TI, typename TG, int N>
 chela_status_t bwd_launch(const ScanBwdParams &q, void *d_b, void *d_c, float *d_a, float *d_skip, float *d_bias, cudaStream_t stream)
 {
     const ScanParams &p = q.f;
-    constexpr int WD = bwd_wd(N), R = N / 4, DC = bwd_channels(N), TILE = kCkptTok, WT = 4;
-    constexpr size_t smem = (size_t)TILE * DC * 16 + 2 * TILE * N * 4 + 3 * R * (TILE * DC + 8) * 4 + 3 * WT * WD * 32 * 16 +
-                            (size_t)WD * TILE * 2 * N * 4;
-    const auto kern = selscan_bwd_kernel<TI, TG, N, WD>;
+    using Sh = BwdShape<TI, N, bwd_ch(N)>;
+    constexpr int DC = Sh::CPW;
+    constexpr size_t smem = Sh::SMEM;
+    const auto kern = selscan_bwd_kernel<TI, TG, N, bwd_ch(N)>;
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return cuda_status(e);
     const int nblk = (p.D + DC - 1) / DC;
     const long long blocks = (long long)p.S * nblk;
     if (blocks > 0x7fffffffLL) return CHELA_ERR_UNSUPPORTED;
-    kern<<<(unsigned)blocks, 32 * WD * WT, smem, stream>>>(q);
+    kern<<<(unsigned)blocks, 32 * Sh::WT, smem, stream>>>(q);
     chela_status_t st = last_launch_status();
     if (st != CHELA_OK) return st;
     const size_t items = (size_t)p.T * p.G * (2 * N / 4);
