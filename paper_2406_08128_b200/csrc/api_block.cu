@@ -115,7 +115,7 @@ chela_status_t chela_shortconv_bwd(const void *x, long long x_stride, const floa
 
 size_t chela_selscan_checkpoint_bytes(int T, int S, int D, int N)
 {
-    if (T < 1 || S < 1 || D < 1 || N < 1) return 0;
+    if (T < 1 || S < 1 || D < 1 || (N != 8 && N != 16 && N != 32 && N != 64)) return 0;
     return selscan_checkpoint_bytes(T, S, D, N);
 }
 

@@ -46,6 +46,15 @@ __device__ __forceinline__ float decay_rate(float a)
 }
 __device__ __forceinline__ float gate_f(float z) { return z * sigmoid_acc(z); }
 
+// Channels of a warp (and of a chain) in both kernels, and the checkpoints' layout, which is the warps' own: for each
+// checkpoint and chain, [CH NS / 4][32 lanes] vectors of four states, so that a warp writes and reads whole lines.
+constexpr int chain_ch(int N) { return N == 8 ? 1 : 2; }
+constexpr int chain_channels(int N) { return 32 / (N / 8) * chain_ch(N); }   // 32, 32, 16, 8
+__device__ __forceinline__ float4 *ckpt_at(float *ckpt, size_t index, int chains, int chain, int per_lane)
+{
+    return reinterpret_cast<float4 *>(ckpt) + (index * chains + chain) * (size_t)(per_lane * 32);
+}
+
 // ------------------------------------------------------------------------------------------------ forward
 
 __device__ __forceinline__ void named_sync(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
@@ -294,7 +303,13 @@ __global__ void __launch_bounds__(32 * WT, OCC) selscan_fwd_kernel(const ScanPar
                 keep(p.state_out + (size_t)s * p.D * N, v);
             }
         };
-        if (p.ckpt && t0 % kCkptTok == 0) keep(p.ckpt + ((size_t)(sr.start / kCkptTok) + s + t0 / kCkptTok) * p.D * N, h);
+        if (p.ckpt && t0 % kCkptTok == 0) {
+            float4 *o = ckpt_at(p.ckpt, (size_t)(sr.start / kCkptTok) + s + t0 / kCkptTok, nblk, blockIdx.x % nblk, CH * NP / 2) + lane;
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+#pragma unroll
+                for (int k = 0; k < NP; k += 2) o[(j * NP / 2 + k / 2) * 32] = make_float4(h[j][k].x, h[j][k].y, h[j][k + 1].x, h[j][k + 1].y);
+        }
 #pragma unroll
         for (int i = 0; i < TOK; ++i) {
             float2 bv[NP];
@@ -441,13 +456,14 @@ struct ScanBwdParams {
 
 template <typename TI, int N, int CH>
 struct BwdShape {
-    static constexpr int NS = 8, NP = 4, R = N / NS, CPW = 32 / R * CH, E16 = 16 / (int)sizeof(TI), WT = 12, TOK = kCkptTok, SUB = 2;
+    static constexpr int NS = 8, NP = 4, R = N / NS, CPW = 32 / R * CH, E16 = 16 / (int)sizeof(TI), WT = 8, TOK = kCkptTok, SUB = 2;
     static constexpr int LPC = R / CH;                                  // lanes of one channel
     static constexpr int TS = SUB < LPC ? SUB : LPC, PT = SUB / TS, DUP = LPC / TS;   // see tok0
     static constexpr int XC = CPW / E16, BC = N / E16;
     static constexpr int CHUNKS = TOK * (4 * XC + 2 * BC), CPL = (CHUNKS + 31) / 32;
     static constexpr int RAW_E = CHUNKS * E16, PREP_F = 3 * TOK * CPW, BC_F = 2 * TOK * N, STATE_F = 32 * CH * NS;
-    static constexpr int WARP_B = RAW_E * (int)sizeof(TI) + (PREP_F + BC_F + (TOK / SUB - 1) * STATE_F + STATE_F) * 4;
+    static constexpr int RAW_B = 2 * RAW_E * (int)sizeof(TI);           // two tiles, the next one's copy under way
+    static constexpr int WARP_B = RAW_B + (PREP_F + BC_F + TOK / SUB * STATE_F + STATE_F) * 4;
     static constexpr size_t SMEM = (size_t)WT * WARP_B;
 };
 
@@ -459,11 +475,13 @@ struct BwdShape {
 // one before it (one multiply-add per state) goes on to the next warp, and the tile is run backwards two tokens at a
 // time with their decays and states computed again in registers.  So the only serial part is that one step a tile, and
 // few chains still fill the SMs; the second evaluation of the exponentials costs less than keeping the decays would.
+// Eight warps an SM with 240 registers and no spills: twelve warps, which have 168 registers each and spill 170 to 230
+// bytes, took 640 to 740 us where eight take 490 (4 x 4096 x 1024).
 // Lanes as in the forward kernel: 8 states of CH channels, so that the sums over channels that dB and dC need are begun in
 // the lane; they are folded over the other lanes (each exchange sends one half of the values away and keeps the other) and
 // leave as one partial sum per channel block for selscan_bc_kernel: no atomics, so equal calls give equal bits.
 template <typename TI, typename TG, int N, int CH>
-__global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams q_)
+__global__ void __launch_bounds__(32 * BwdShape<TI, N, CH>::WT, 1) selscan_bwd_kernel(const ScanBwdParams q_)
 {
     using Sh = BwdShape<TI, N, CH>;
     constexpr int NS = Sh::NS, R = Sh::R, NP = Sh::NP, CPW = Sh::CPW, E16 = Sh::E16, XC = Sh::XC, BC = Sh::BC, CPL = Sh::CPL, PT = Sh::PT;
@@ -474,10 +492,10 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
     __shared__ longlong2 s_src[6];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     unsigned char *s_mine = smem + warp * Sh::WARP_B;
-    TI *s_raw = reinterpret_cast<TI *>(s_mine);                          // x, dt, z, dy [TOK][CPW], b, c [TOK][N]
-    float *s_dt = reinterpret_cast<float *>(s_mine + Sh::RAW_E * sizeof(TI)), *s_dx = s_dt + TOK * CPW, *s_dg = s_dx + TOK * CPW;
+    TI *s_raw2 = reinterpret_cast<TI *>(s_mine);                         // two tiles: x, dt, z, dy [TOK][CPW], b, c [TOK][N]
+    float *s_dt = reinterpret_cast<float *>(s_mine + Sh::RAW_B), *s_dx = s_dt + TOK * CPW, *s_dg = s_dx + TOK * CPW;
     float *s_bc = s_dt + Sh::PREP_F;                                     // b, c [TOK][N] in fp32
-    float4 *s_keep = reinterpret_cast<float4 *>(s_bc + Sh::BC_F);        // states before tokens 2, 4, 6: [CH NS / 4][32] each
+    float4 *s_keep = reinterpret_cast<float4 *>(s_bc + Sh::BC_F);        // states before tokens 0, 2, 4, 6: [CH NS / 4][32] each
     constexpr int HAND = Sh::WARP_B - Sh::STATE_F * 4;
     float4 *s_down = reinterpret_cast<float4 *>(s_mine + HAND);          // the gradient handed down
 
@@ -485,6 +503,7 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
     const int s = blockIdx.x / nblk, cb = blockIdx.x % nblk, c0 = cb * CPW;
     const int q = lane % R, grp = lane / R;
     const int chl = grp * CH + q % CH, ch = c0 + chl, n0 = NS * q;
+    const int half = (lane >> 4) * 4;   // of its 8 states, the four that a lane holds first: the lower ones in lanes 0 .. 15
     const int tok0 = (q / CH / DUP) * PT;   // of two tokens, the first whose outputs this lane writes (DUP lanes have the same)
     const bool live = ch < p.D, writer = live && (q / CH) % DUP == 0;
     const SeqRange sr = seq_range(p.off, s, p.S, p.T);
@@ -502,9 +521,9 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
         for (int j = 0; j < CH; ++j) {
             float4 u = zero4(), w = u;
             if ((ch ^ j) < p.D) {
-                const float4 *o = reinterpret_cast<const float4 *>(from + (size_t)(ch ^ j) * N + n0);
-                u = o[0];
-                w = o[1];
+                const float *o = from + (size_t)(ch ^ j) * N + n0;
+                u = *reinterpret_cast<const float4 *>(o + half);
+                w = *reinterpret_cast<const float4 *>(o + (half ^ 4));
             }
             v[j][0] = make_float2(u.x, u.y); v[j][1] = make_float2(u.z, u.w);
             v[j][2] = make_float2(w.x, w.y); v[j][3] = make_float2(w.z, w.w);
@@ -514,9 +533,9 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             if ((ch ^ j) < p.D) {
-                float4 *o = reinterpret_cast<float4 *>(to + (size_t)(ch ^ j) * N + n0);
-                o[0] = make_float4(v[j][0].x, v[j][0].y, v[j][1].x, v[j][1].y);
-                o[1] = make_float4(v[j][2].x, v[j][2].y, v[j][3].x, v[j][3].y);
+                float *o = to + (size_t)(ch ^ j) * N + n0;
+                *reinterpret_cast<float4 *>(o + half) = make_float4(v[j][0].x, v[j][0].y, v[j][1].x, v[j][1].y);
+                *reinterpret_cast<float4 *>(o + (half ^ 4)) = make_float4(v[j][2].x, v[j][2].y, v[j][3].x, v[j][3].y);
             }
         }
     };
@@ -554,26 +573,41 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
     __syncthreads();
 
     const int ntile = (sr.len + TOK - 1) / TOK;
-    for (int tile = ntile - 1 - warp; tile >= 0; tile -= WT) {
-        const int t0 = tile * TOK;
-        float2 h[CH][NP];
-        states_from(p.ckpt + ((size_t)(sr.start / kCkptTok) + s + tile) * p.D * N, h);
-        __syncwarp();   // the tile before is done with shared memory
+    const size_t ck0 = (size_t)(sr.start / kCkptTok) + s;
+    auto fetch = [&](int tile, TI *to) {   // raw operands of a tile
 #pragma unroll
         for (int i = 0; i < CPL; ++i) {
             int id = lane + 32 * i;
             if (id < Sh::CHUNKS) {
-                void *to = s_raw + id * E16;
+                TI *at = to + id * E16;
                 const bool in_x = id < 4 * TOK * XC;
                 const int which = in_x ? id / (TOK * XC) : 4 + (id - 4 * TOK * XC) / (TOK * BC);
                 id = in_x ? id % (TOK * XC) : (id - 4 * TOK * XC) % (TOK * BC);
-                const int per = in_x ? XC : BC, t = id / per;
+                const int per = in_x ? XC : BC, t = tile * TOK + id / per;
                 const longlong2 from = s_src[which];
-                const bool ok = from.x && t0 + t < sr.len && (!in_x || c0 + (id % per) * E16 < p.D);
-                copy16(to, reinterpret_cast<const char *>(ok ? from.x + (long long)(t0 + t) * from.y + (id % per) * 16 : (long long)p.x), ok);
+                const bool ok = from.x && t < sr.len && (!in_x || c0 + (id % per) * E16 < p.D);
+                const char *src = reinterpret_cast<const char *>(ok ? from.x + (long long)t * from.y + (id % per) * 16 : (long long)p.x);
+                copy16(at, src, ok);
             }
         }
-        asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    // the tile's checkpoint into the first of the kept states; the forward kernel's order of states in a lane
+    auto fetch_state = [&](int tile) {
+        const float4 *from = ckpt_at(p.ckpt, ck0 + tile, nblk, cb, CH * NP / 2) + lane;
+#pragma unroll
+        for (int i = 0; i < CH * NP / 2; ++i) copy16(s_keep + i * 32 + lane, from + (i ^ (half >> 2)) * 32, true);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int stage = 0;
+    if (ntile - 1 - warp >= 0) {
+        fetch(ntile - 1 - warp, s_raw2);
+        fetch_state(ntile - 1 - warp);
+    }
+    for (int tile = ntile - 1 - warp; tile >= 0; tile -= WT) {
+        const int t0 = tile * TOK;
+        const TI *s_raw = s_raw2 + stage * Sh::RAW_E;
+        asm volatile("cp.async.wait_group 1;" ::: "memory");   // the operands; the checkpoint may still be under way
         __syncwarp();
 #pragma unroll
         for (int i = 0; i < (Sh::BC_F / 4 + 31) / 32; ++i)
@@ -606,12 +640,20 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
         }
         __syncwarp();
         auto row_of = [&](const float *m, float2 (&o)[NP]) {
-            const float4 u = reinterpret_cast<const float4 *>(m)[0], v = reinterpret_cast<const float4 *>(m)[1];
+            const float4 u = *reinterpret_cast<const float4 *>(m + half), v = *reinterpret_cast<const float4 *>(m + (half ^ 4));
             o[0] = make_float2(u.x, u.y); o[1] = make_float2(u.z, u.w);
             o[2] = make_float2(v.x, v.y); o[3] = make_float2(v.z, v.w);
         };
         const float *s_b = s_bc + n0, *s_c = s_b + TOK * N;
 
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        float2 h[CH][NP];
+        take(s_keep, h);
+        if (tile >= WT) {
+            stage ^= 1;
+            fetch(tile - WT, s_raw2 + stage * Sh::RAW_E);
+            if (lane < CH * NP) asm volatile("prefetch.global.L2 [%0];" ::"l"(ckpt_at(p.ckpt, ck0 + tile - WT, nblk, cb, CH * NP / 2) + lane * 8));
+        }
         // forwards: states; what the tile adds to the gradient before it
         float2 add[CH][NP], whole[CH][NP];
         clear(add);
@@ -619,9 +661,9 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
         for (int j = 0; j < CH; ++j)
 #pragma unroll
             for (int k = 0; k < NP; ++k) whole[j][k] = make_float2(1.f, 1.f);
-#pragma unroll 1
+#pragma unroll
         for (int u = 0; u < TOK; u += SUB) {
-            if (u) put(s_keep + (u / SUB - 1) * (Sh::STATE_F / 4), h);
+            if (u) put(s_keep + u / SUB * (Sh::STATE_F / 4), h);
 #pragma unroll
             for (int i = 0; i < SUB; ++i) {
                 float2 bv[NP], cv[NP];
@@ -667,18 +709,23 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
         float *part = q_.part_bc + ((size_t)cb * p.T + sr.start + t0) * (2 * N);   // [token][dB N | dC N]
 #pragma unroll 1
         for (int u = TOK - SUB; u >= 0; u -= SUB) {
-            if (u) take(s_keep + (u / SUB - 1) * (Sh::STATE_F / 4), h);
-            else states_from(p.ckpt + ((size_t)(sr.start / kCkptTok) + s + tile) * p.D * N, h);
-            auto fold_channels = [&](float (&v)[8], float *to) {
-                // this lane's 8 states summed over the 32 / R lanes of other channels; 8 values halve three times at most
-                int first = 0, n = 8;
+            take(s_keep + u / SUB * (Sh::STATE_F / 4), h);
+            auto fold_channels = [&](const float2 (&w)[NP], float *to) {
+                // this lane's 8 states summed over the 32 / R lanes of other channels; 8 values halve three times at most.
+                // Lanes 16 .. 31 hold the upper four first, so the first halving sends the last four everywhere.
+                float v[4];
+                v[0] = w[0].x + __shfl_xor_sync(0xffffffffu, w[2].x, 16);
+                v[1] = w[0].y + __shfl_xor_sync(0xffffffffu, w[2].y, 16);
+                v[2] = w[1].x + __shfl_xor_sync(0xffffffffu, w[3].x, 16);
+                v[3] = w[1].y + __shfl_xor_sync(0xffffffffu, w[3].y, 16);
+                int first = 0, n = 4;
 #pragma unroll
-                for (int o = 16; o >= R; o >>= 1) {
+                for (int o = 8; o >= R; o >>= 1) {
                     if (n > 1) {
                         n >>= 1;
                         const bool up = lane & o;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
+                        for (int k = 0; k < 2; ++k) {
                             if (k < n) {
                                 const float send = up ? v[k] : v[k + n], keep = up ? v[k + n] : v[k];
                                 v[k] = keep + __shfl_xor_sync(0xffffffffu, send, o);
@@ -692,7 +739,7 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
                 constexpr int GR = 32 / R, KEEP = GR >= 8 ? 1 : 8 / GR;
                 if (to && (GR <= 8 || grp % (GR / 8) == 0)) {
 #pragma unroll
-                    for (int k = 0; k < KEEP; ++k) to[n0 + first + k] = v[k];
+                    for (int k = 0; k < KEEP; ++k) to[n0 + half + first + k] = v[k];
                 }
             };
             float2 e[SUB][CH][NP], h0[CH][NP];   // decays; the state behind the first token
@@ -705,7 +752,8 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
                     float2 bv[NP], cv[NP];
                     row_of(s_b + (u + i) * N, bv);
                     row_of(s_c + (u + i) * N, cv);
-                    float own[CH], v[8];
+                    float own[CH];
+                    float2 v[NP];
 #pragma unroll
                     for (int j = 0; j < CH; ++j) {
                         const int at = (u + i) * CPW + (chl ^ j);
@@ -720,8 +768,7 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
                             hh[j][k] = fma2v(e[i][j][k], i ? h0[j][k] : h[j][k], mul2v(splat2(dxs[i][j]), bv[k]));
                             if (i == 0) h0[j][k] = hh[j][k];
                             sum = k ? fma2v(cv[k], hh[j][k], sum) : mul2v(cv[k], hh[j][k]);
-                            v[2 * k] = j ? fmaf(dgs[i][j], hh[j][k].x, v[2 * k]) : dgs[i][j] * hh[j][k].x;
-                            v[2 * k + 1] = j ? fmaf(dgs[i][j], hh[j][k].y, v[2 * k + 1]) : dgs[i][j] * hh[j][k].y;
+                            v[k] = j ? fma2v(splat2(dgs[i][j]), hh[j][k], v[k]) : mul2v(splat2(dgs[i][j]), hh[j][k]);
                         }
                         own[j] = sum.x + sum.y;
                     }
@@ -734,7 +781,8 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
                 float2 bv[NP], cv[NP];
                 row_of(s_b + (u + i) * N, bv);
                 row_of(s_c + (u + i) * N, cv);
-                float ogb[CH], oga[CH], v[8];
+                float ogb[CH], oga[CH];
+                float2 v[NP];
 #pragma unroll
                 for (int j = 0; j < CH; ++j) {
                     float2 ub = make_float2(0.f, 0.f), ua = ub;
@@ -742,8 +790,7 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
                     for (int k = 0; k < NP; ++k) {
                         g[j][k] = fma2v(cv[k], splat2(dgs[i][j]), g[j][k]);
                         ub = k ? fma2v(g[j][k], bv[k], ub) : mul2v(g[j][k], bv[k]);
-                        v[2 * k] = j ? fmaf(dxs[i][j], g[j][k].x, v[2 * k]) : dxs[i][j] * g[j][k].x;
-                        v[2 * k + 1] = j ? fmaf(dxs[i][j], g[j][k].y, v[2 * k + 1]) : dxs[i][j] * g[j][k].y;
+                        v[k] = j ? fma2v(splat2(dxs[i][j]), g[j][k], v[k]) : mul2v(splat2(dxs[i][j]), g[j][k]);
                         g[j][k] = mul2v(g[j][k], e[i][j][k]);   // e_t
                         const float2 through = mul2v(g[j][k], i ? h0[j][k] : h[j][k]);
                         ua = k ? fma2v(through, a[j][k], ua) : mul2v(through, a[j][k]);
@@ -797,6 +844,8 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
                 }
             }
         }
+        __syncwarp();   // done with the tile's shared memory
+        if (tile >= WT) fetch_state(tile - WT);
     }
     if (ntile == 0 && q_.d_state_in && warp == 0) {
         float2 g[CH][NP];
@@ -816,7 +865,7 @@ __global__ void __launch_bounds__(384, 1) selscan_bwd_kernel(const ScanBwdParams
         for (int w = 1; w < WT; ++w) {
             const unsigned char *other = smem + w * Sh::WARP_B;
             float2 v[CH][NP];
-            take(reinterpret_cast<const float4 *>(other + Sh::RAW_E * sizeof(TI) + (Sh::PREP_F + Sh::BC_F) * 4), v);
+            take(reinterpret_cast<const float4 *>(other + Sh::RAW_B + (Sh::PREP_F + Sh::BC_F) * 4), v);
 #pragma unroll
             for (int j = 0; j < CH; ++j)
 #pragma unroll
@@ -874,7 +923,7 @@ __global__ void __launch_bounds__(256) sum_rows_kernel(const float *part, float 
 // times the exponentials), so it pays only where the chains leave more than half of the SMs without work.
 int fwd_segment(int T, int S, int D, int N)
 {
-    const int cpw = N <= 16 ? 32 : 512 / N;
+    const int cpw = chain_channels(N);
     const long long cols = (D + cpw - 1) / cpw, chains = cols * S;
     if (chains * 2 > 148 || T / S < 512) return 0;
     const long long want = (2 * 148 + cols - 1) / cols;   // segments in all
@@ -935,17 +984,14 @@ chela_status_t step_n(const ScanParams &p, int N, cudaStream_t stream)
     return last_launch_status();
 }
 
-constexpr int bwd_ch(int N) { return N == 8 ? 1 : 2; }
-constexpr int bwd_channels(int N) { return 32 / (N / 8) * bwd_ch(N); }   // channels of a CTA: 32, 32, 16, 8
-
 template <typename TI, typename TG, int N>
 chela_status_t bwd_launch(const ScanBwdParams &q, void *d_b, void *d_c, float *d_a, float *d_skip, float *d_bias, cudaStream_t stream)
 {
     const ScanParams &p = q.f;
-    using Sh = BwdShape<TI, N, bwd_ch(N)>;
+    using Sh = BwdShape<TI, N, chain_ch(N)>;
     constexpr int DC = Sh::CPW;
     constexpr size_t smem = Sh::SMEM;
-    const auto kern = selscan_bwd_kernel<TI, TG, N, bwd_ch(N)>;
+    const auto kern = selscan_bwd_kernel<TI, TG, N, chain_ch(N)>;
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return cuda_status(e);
     const int nblk = (p.D + DC - 1) / DC;
@@ -998,7 +1044,7 @@ struct ScanBwdPlan {
 ScanBwdPlan bwd_plan(int T, int S, int D, int N, bool have_ckpt)
 {
     ScanBwdPlan p;
-    const int dc = bwd_channels(N);
+    const int dc = chain_channels(N);
     p.off_ckpt = 0;
     p.off_fwd = have_ckpt ? 0 : align_up(selscan_checkpoint_bytes(T, S, D, N), 256);
     p.off_bc = p.off_fwd + (have_ckpt ? 0 : selscan_workspace_bytes(T, S, D, N));
@@ -1012,7 +1058,8 @@ ScanBwdPlan bwd_plan(int T, int S, int D, int N, bool have_ckpt)
 
 size_t selscan_checkpoint_bytes(int T, int S, int D, int N)
 {
-    return (packed_blocks(T, S, kCkptTok)) * D * N * sizeof(float);
+    const int cpw = chain_channels(N);
+    return packed_blocks(T, S, kCkptTok) * ((D + cpw - 1) / cpw) * cpw * N * sizeof(float);
 }
 
 size_t selscan_workspace_bytes(int T, int S, int D, int N)
