@@ -48,8 +48,8 @@ __device__ __forceinline__ float gate_f(float z) { return z * sigmoid_acc(z); }
 
 // Channels of a warp (and of a chain) in both kernels, and the checkpoints' layout, which is the warps' own: for each
 // checkpoint and chain, [CH NS / 4][32 lanes] vectors of four states, so that a warp writes and reads whole lines.
-constexpr int chain_ch(int N) { return N == 8 ? 1 : 2; }
-constexpr int chain_channels(int N) { return 32 / (N / 8) * chain_ch(N); }   // 32, 32, 16, 8
+__host__ __device__ constexpr int chain_ch(int N) { return N == 8 ? 1 : 2; }
+__host__ __device__ constexpr int chain_channels(int N) { return 32 / (N / 8) * chain_ch(N); }   // 32, 32, 16, 8
 __device__ __forceinline__ float4 *ckpt_at(float *ckpt, size_t index, int chains, int chain, int per_lane)
 {
     return reinterpret_cast<float4 *>(ckpt) + (index * chains + chain) * (size_t)(per_lane * 32);
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(32 * WT, OCC) selscan_fwd_kernel(const ScanPar
         // value of the token i, slot j, from the lane that prepared it
         auto of = [&](const float (&v)[PT], int i, int j) -> float {
             if (R == 1) return v[i % PT];
-            if (R == 2) return j == 0 ? v[i % PT] : __shfl_xor_sync(0xffffffffu, v[i % PT], 1);
+            if (R == 2 && CH == 2) return j == 0 ? v[i % PT] : __shfl_xor_sync(0xffffffffu, v[i % PT], 1);
             return __shfl_sync(0xffffffffu, v[i % PT], (lane & ~(R - 1)) + ((q % CH) ^ j) + CH * (i / PT));
         };
         float2 e[TOK][CH][NP];
@@ -304,11 +304,21 @@ __global__ void __launch_bounds__(32 * WT, OCC) selscan_fwd_kernel(const ScanPar
             }
         };
         if (p.ckpt && t0 % kCkptTok == 0) {
-            float4 *o = ckpt_at(p.ckpt, (size_t)(sr.start / kCkptTok) + s + t0 / kCkptTok, nblk, blockIdx.x % nblk, CH * NP / 2) + lane;
+            // the backward kernel's chain, lane and slot of this channel
+            constexpr int BCH = chain_ch(N), BCPW = chain_channels(N);
+            const int chains = (p.D + BCPW - 1) / BCPW, c = ch % BCPW;
+            float4 *o = ckpt_at(p.ckpt, (size_t)(sr.start / kCkptTok) + s + t0 / kCkptTok, chains, ch / BCPW, BCH * NP / 2);
+            if (BCH == CH) {
+                o += lane;
 #pragma unroll
-            for (int j = 0; j < CH; ++j)
+                for (int j = 0; j < CH; ++j)
 #pragma unroll
-                for (int k = 0; k < NP; k += 2) o[(j * NP / 2 + k / 2) * 32] = make_float4(h[j][k].x, h[j][k].y, h[j][k + 1].x, h[j][k + 1].y);
+                    for (int k = 0; k < NP; k += 2) o[(j * NP / 2 + k / 2) * 32] = make_float4(h[j][k].x, h[j][k].y, h[j][k + 1].x, h[j][k + 1].y);
+            } else if (live) {   // one channel here, two a lane there: slot 0 where the channel's parity is the lane's
+                o += ((c ^ q) & 1) * (NP / 2) * 32 + c / 2 * R + q;
+#pragma unroll
+                for (int k = 0; k < NP; k += 2) o[(k / 2) * 32] = make_float4(h[0][k].x, h[0][k].y, h[0][k + 1].x, h[0][k + 1].y);
+            }
         }
 #pragma unroll
         for (int i = 0; i < TOK; ++i) {
@@ -596,7 +606,7 @@ __global__ void __launch_bounds__(32 * BwdShape<TI, N, CH>::WT, 1) selscan_bwd_k
     auto fetch_state = [&](int tile) {
         const float4 *from = ckpt_at(p.ckpt, ck0 + tile, nblk, cb, CH * NP / 2) + lane;
 #pragma unroll
-        for (int i = 0; i < CH * NP / 2; ++i) copy16(s_keep + i * 32 + lane, from + (i ^ (half >> 2)) * 32, true);
+        for (int i = 0; i < CH * NP / 2; ++i) copy16(s_keep + i * 32 + lane, from + (i ^ (half >> 2)) * 32, (ch ^ (i / 2)) < p.D);
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     int stage = 0;
@@ -958,13 +968,18 @@ chela_status_t fwd_launch(ScanParams p, cudaStream_t stream)
     return last_launch_status();
 }
 
+// Half as many channels a chain and twice the tokens a slice (one channel a lane): twice the chains, half the steps of each.
+// Every b and c is then read for one channel instead of two, so it pays only while there is no more than one chain of the
+// full width per SM (4 x 4096 x 1024: 152 us against 226; 8 x 8192 x 1024, two chains an SM: 581 against 553).
+bool fwd_narrow(const ScanParams &p, int N) { return !p.seg && (long long)p.S * ((p.D + chain_channels(N) - 1) / chain_channels(N)) <= 148; }
+
 template <typename TI, typename TO>
 chela_status_t fwd_n(const ScanParams &p, int N, cudaStream_t stream)
 {
     switch (N) {
     case 8: return fwd_launch<TI, TO, 8, 1, 8, 8, 2>(p, stream);
-    case 16: return fwd_launch<TI, TO, 16, 2, 4, 8, 2>(p, stream);
-    case 32: return fwd_launch<TI, TO, 32, 2, 4, 8, 2>(p, stream);
+    case 16: return fwd_narrow(p, N) ? fwd_launch<TI, TO, 16, 1, 8, 8, 2>(p, stream) : fwd_launch<TI, TO, 16, 2, 4, 8, 2>(p, stream);
+    case 32: return fwd_narrow(p, N) ? fwd_launch<TI, TO, 32, 1, 8, 8, 2>(p, stream) : fwd_launch<TI, TO, 32, 2, 4, 8, 2>(p, stream);
     default: return fwd_launch<TI, TO, 64, 2, 4, 8, 2>(p, stream);
     }
 }
