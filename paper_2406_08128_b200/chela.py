@@ -420,49 +420,58 @@ def _need(ok, where, what):
         raise err
 
 
-def _rows(t, where, name, lead, dtype, device, inner):
-    """Pointer and token stride of a token tensor [*lead, *inner]; the inner axes contiguous, one step between tokens."""
+def _raw_stream(index):
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _rows(t, where, name, lead, dtype, index, inner):
+    """Address and token stride of a token tensor [*lead, *inner]; the inner axes contiguous, one step between tokens."""
     n = len(lead)
-    _need(t.dtype == dtype and t.device == device and tuple(t.shape) == (*lead, *inner), where,
-          "%s must be a %s tensor %s on %s" % (name, dtype, (*lead, *inner), device))
+    if t.dtype is not dtype or t.get_device() != index or t.shape != lead + inner:
+        _need(False, where, "%s must be a %s tensor %s on device %d" % (name, dtype, lead + inner, index))
     strides, step = t.stride(), 1
-    for i in range(len(t.shape) - 1, n - 1, -1):
-        _need(t.shape[i] == 1 or strides[i] == step, where, "%s: a token's values must be contiguous" % name)
-        step *= t.shape[i]
+    for i in range(len(inner) - 1, -1, -1):
+        if strides[n + i] != step and inner[i] != 1:
+            _need(False, where, "%s: a token's values must be contiguous" % name)
+        step *= inner[i]
     if n == 1:
         stride = strides[0] if lead[0] > 1 else -(-step // 8) * 8
     else:
         stride = strides[1] if lead[1] > 1 else (strides[0] if lead[0] > 1 else -(-step // 8) * 8)
-        _need(lead[0] == 1 or strides[0] == lead[1] * stride, where, "%s: tokens must be a fixed distance apart" % name)
-    return _vp(t.data_ptr()), stride
+        if strides[0] != lead[1] * stride and lead[0] != 1:
+            _need(False, where, "%s: tokens must be a fixed distance apart" % name)
+    return t.data_ptr(), stride
 
 
-def _flat(t, where, name, shape, dtype, device):
-    """Pointer of an optional contiguous tensor of the given shape."""
+def _flat(t, where, name, shape, dtype, index):
+    """Address of an optional contiguous tensor of the given shape."""
     if t is None:
         return None
-    _need(t.dtype == dtype and t.device == device and tuple(t.shape) == tuple(shape) and t.is_contiguous(), where,
-          "%s must be a contiguous %s tensor %s on %s" % (name, dtype, tuple(shape), device))
-    return _vp(t.data_ptr())
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous():
+        _need(False, where, "%s must be a contiguous %s tensor %s on device %d" % (name, dtype, tuple(shape), index))
+    return t.data_ptr()
 
 
 def _seqs(x, seq_offsets, where):
-    """(leading shape, S, T, offsets pointer) of a token tensor."""
-    _need(x.dtype in _DTYPES and x.dim() in (2, 3), where, "tokens must be [T, D] or [B, L, D] of float32 or bfloat16")
-    _need(x.is_cuda, where, "tensors must be on a CUDA device (there is no CPU fallback)")
-    lead = tuple(x.shape[:-1])
+    """(leading shape, S, T, address of the offsets, device) of a token tensor."""
+    lead = x.shape[:-1]
+    if x.dtype not in _DTYPES or len(lead) not in (1, 2):
+        _need(False, where, "tokens must be [T, D] or [B, L, D] of float32 or bfloat16")
+    if not x.is_cuda:
+        _need(False, where, "tensors must be on a CUDA device (there is no CPU fallback)")
+    index = x.get_device()
     if seq_offsets is None:
-        return lead, lead[0] if len(lead) == 2 else 1, lead[0] * lead[1] if len(lead) == 2 else lead[0], None
+        return (lead, 1, lead[0], None, index) if len(lead) == 1 else (lead, lead[0], lead[0] * lead[1], None, index)
     _need(len(lead) == 1 and seq_offsets.dim() == 1 and seq_offsets.shape[0] >= 2, where,
           "seq_offsets [S + 1] goes with packed tokens [T, D]")
-    return lead, seq_offsets.shape[0] - 1, lead[0], _flat(seq_offsets, where, "seq_offsets", (seq_offsets.shape[0],), torch.int32, x.device)
+    return lead, seq_offsets.shape[0] - 1, lead[0], _flat(seq_offsets, where, "seq_offsets", seq_offsets.shape, torch.int32, index), index
 
 
 class _on:
     """The device of a call's tensors as the current one (no switch where it is already)."""
 
-    def __init__(self, device):
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    def __init__(self, index):
+        self.guard = None if index == torch.cuda.current_device() else torch.cuda.device(index)
 
     def __enter__(self):
         if self.guard:
@@ -473,88 +482,100 @@ class _on:
             self.guard.__exit__(*exc)
 
 
-def _new(out, where, name, shape, dtype, device):
+def _new(out, where, name, shape, dtype, device, index):
     if out is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    _flat(out, where, name, shape, dtype, device)
+    _flat(out, where, name, shape, dtype, index)
     return out
+
+
+def _scratch(need, workspace, device, where, index):
+    """(address, bytes) of a call's workspace, allocated here unless the caller brings one."""
+    if workspace is None:
+        if need == 0:
+            return None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        _need(False, where, "workspace must be contiguous and on device %d" % index)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def shortconv_carry_fwd(x, w, bias=None, act=True, state_in=None, state_out=None, seq_offsets=None, out=None):
     """chela_shortconv_carry_fwd: (y, state_out).  x [T,D] or [B,L,D]; w [D,width] f32; states [S,width-1,D] like x."""
-    where = "chela_shortconv_carry_fwd"
-    lead, S, T, off = _seqs(x, seq_offsets, where)
-    D, width, dev = x.shape[-1], w.shape[-1], x.device
-    px, xs = _rows(x, where, "x", lead, x.dtype, dev, (D,))
-    y = _new(out, where, "out", x.shape, x.dtype, dev)
-    state_out = _new(state_out, where, "state_out", (S, width - 1, D), x.dtype, dev)
+    where, f32 = "chela_shortconv_carry_fwd", torch.float32
+    lead, S, T, off, dev = _seqs(x, seq_offsets, where)
+    D, width, dt = x.shape[-1], w.shape[-1], x.dtype
+    px, xs = _rows(x, where, "x", lead, dt, dev, (D,))
+    y = _new(out, where, "out", x.shape, dt, x.device, dev)
+    held = (S, width - 1, D)
+    state_out = _new(state_out, where, "state_out", held, dt, x.device, dev)
     with _on(dev):
         _check(lib().chela_shortconv_carry_fwd(
-            px, xs, _flat(w, where, "w", (D, width), torch.float32, dev), _flat(bias, where, "bias", (D,), torch.float32, dev),
-            _ptr(y), _flat(state_in, where, "state_in", (S, width - 1, D), x.dtype, dev), _ptr(state_out), off, S, T, D, width,
-            int(bool(act)), _dt(x), _stream()), where)
+            px, xs, _flat(w, where, "w", (D, width), f32, dev), _flat(bias, where, "bias", (D,), f32, dev), y.data_ptr(),
+            _flat(state_in, where, "state_in", held, dt, dev), state_out.data_ptr() or None, off, S, T, D, width, int(bool(act)),
+            _DTYPES[dt], _raw_stream(dev)), where)
     return y, state_out
 
 
 def shortconv_step(x, w, state, bias=None, act=True, state_out=None, out=None):
     """chela_shortconv_step: y [S,D] for one new token per sequence; state [S,width-1,D] is updated in place unless
     state_out is given."""
-    where = "chela_shortconv_step"
-    lead, _, S, _ = _seqs(x, None, where)
+    where, f32 = "chela_shortconv_step", torch.float32
+    lead, _, S, _, dev = _seqs(x, None, where)
     _need(len(lead) == 1, where, "x must be [S, D]")
-    D, width, dev = x.shape[-1], w.shape[-1], x.device
-    px, xs = _rows(x, where, "x", lead, x.dtype, dev, (D,))
-    y = _new(out, where, "out", x.shape, x.dtype, dev)
-    state_out = state if state_out is None else state_out
+    D, width, dt = x.shape[-1], w.shape[-1], x.dtype
+    px, xs = _rows(x, where, "x", lead, dt, dev, (D,))
+    y = _new(out, where, "out", x.shape, dt, x.device, dev)
+    held = (S, width - 1, D)
+    before = _flat(state, where, "state", held, dt, dev)
+    after = before if state_out is None else _flat(state_out, where, "state_out", held, dt, dev)
     with _on(dev):
         _check(lib().chela_shortconv_step(
-            px, xs, _flat(w, where, "w", (D, width), torch.float32, dev), _flat(bias, where, "bias", (D,), torch.float32, dev),
-            _ptr(y), _flat(state, where, "state", (S, width - 1, D), x.dtype, dev),
-            _flat(state_out, where, "state_out", (S, width - 1, D), x.dtype, dev), S, D, width, int(bool(act)), _dt(x), _stream()), where)
+            px, xs, _flat(w, where, "w", (D, width), f32, dev), _flat(bias, where, "bias", (D,), f32, dev), y.data_ptr(), before or None,
+            after or None, S, D, width, int(bool(act)), _DTYPES[dt], _raw_stream(dev)), where)
     return y
 
 
 def shortconv_bwd(x, w, d_y, bias=None, act=True, state_in=None, d_state_out=None, seq_offsets=None, grad_dtype=F32,
                   want_d_state=False, workspace=None):
     """chela_shortconv_bwd: ShortconvGrads; d_x (and d_state_in, if wanted) of grad_dtype, d_w and d_bias f32."""
-    where = "chela_shortconv_bwd"
-    lead, S, T, off = _seqs(x, seq_offsets, where)
-    D, width, dev, gt = x.shape[-1], w.shape[-1], x.device, _tdtype(grad_dtype)
-    px, xs = _rows(x, where, "x", lead, x.dtype, dev, (D,))
-    pdy, dys = _rows(d_y, where, "d_y", lead, x.dtype, dev, (D,))
-    d_x = torch.empty(x.shape, dtype=gt, device=dev)
-    d_w = torch.empty((D, width), dtype=torch.float32, device=dev)
-    d_bias = torch.empty((D,), dtype=torch.float32, device=dev)
+    where, f32 = "chela_shortconv_bwd", torch.float32
+    lead, S, T, off, dev = _seqs(x, seq_offsets, where)
+    D, width, dt, gt, device = x.shape[-1], w.shape[-1], x.dtype, _tdtype(grad_dtype), x.device
+    px, xs = _rows(x, where, "x", lead, dt, dev, (D,))
+    pdy, dys = _rows(d_y, where, "d_y", lead, dt, dev, (D,))
     held = (S, width - 1, D)
-    d_state = torch.empty(held, dtype=gt, device=dev) if want_d_state else None
-    if workspace is None:
-        workspace = _workspace(int(lib().chela_shortconv_bwd_workspace_bytes(T, D, width)), dev)
+    g = ShortconvGrads(torch.empty(x.shape, dtype=gt, device=device), torch.empty((D, width), dtype=f32, device=device),
+                       torch.empty((D,), dtype=f32, device=device), torch.empty(held, dtype=gt, device=device) if want_d_state else None)
+    ws, nbytes = _scratch(lib().chela_shortconv_bwd_workspace_bytes(T, D, width), workspace, device, where, dev)
     with _on(dev):
         _check(lib().chela_shortconv_bwd(
-            px, xs, _flat(w, where, "w", (D, width), torch.float32, dev), _flat(bias, where, "bias", (D,), torch.float32, dev), pdy, dys,
-            _flat(state_in, where, "state_in", held, x.dtype, dev), _flat(d_state_out, where, "d_state_out", held, x.dtype, dev),
-            _ptr(d_x), _ptr(d_w), _ptr(d_bias), _ptr(d_state), off, S, T, D, width, int(bool(act)), _dt(x), int(grad_dtype),
-            _ptr(workspace), workspace.numel(), _stream()), where)
-    return ShortconvGrads(d_x, d_w, d_bias, d_state)
+            px, xs, _flat(w, where, "w", (D, width), f32, dev), _flat(bias, where, "bias", (D,), f32, dev), pdy, dys,
+            _flat(state_in, where, "state_in", held, dt, dev), _flat(d_state_out, where, "d_state_out", held, dt, dev),
+            g.d_x.data_ptr(), g.d_w.data_ptr(), g.d_bias.data_ptr(), _ptr(g.d_state_in), off, S, T, D, width, int(bool(act)), _DTYPES[dt],
+            int(grad_dtype), ws, nbytes, _raw_stream(dev)), where)
+    return g
 
 
-def _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state_in, seq_offsets):
-    lead, S, T, off = _seqs(x, seq_offsets, where)
-    D, dev, f32 = x.shape[-1], x.device, torch.float32
-    _need(a.dim() == 2 and b.dim() == len(lead) + 2, where, "a is [D, N], b and c are [..., G, N]")
-    G, N = b.shape[-2], b.shape[-1]
-    r = SelscanArgs()
-    r.x, r.x_stride = _rows(x, where, "x", lead, x.dtype, dev, (D,))
-    r.dt, r.dt_stride = _rows(dt, where, "dt", lead, x.dtype, dev, (D,))
-    r.b, r.b_stride = _rows(b, where, "b", lead, x.dtype, dev, (G, N))
-    r.c, r.c_stride = _rows(c, where, "c", lead, x.dtype, dev, (G, N))
-    if z is not None:
-        r.z, r.z_stride = _rows(z, where, "z", lead, x.dtype, dev, (D,))
-    r.a = _flat(a, where, "a", (D, N), f32, dev)
-    r.d_skip, r.dt_bias = _flat(d_skip, where, "d_skip", (D,), f32, dev), _flat(dt_bias, where, "dt_bias", (D,), f32, dev)
-    r.state_in, r.seq_offsets = _flat(state_in, where, "state_in", (S, D, N), f32, dev), off
-    r.S, r.T, r.D, r.N, r.G, r.softplus, r.in_dtype = S, T, D, N, G, int(bool(softplus)), _dt(x)
-    return r
+def _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state_in, seq_offsets, step=False):
+    """(SelscanArgs, device): step = one token per sequence, the state required."""
+    lead, S, T, off, dev = _seqs(x, seq_offsets, where)
+    kind, f32, D = x.dtype, torch.float32, x.shape[-1]
+    if a.dim() != 2 or b.dim() != len(lead) + 2:
+        _need(False, where, "a is [D, N], b and c are [..., G, N]")
+    if step:
+        _need(len(lead) == 1, where, "x must be [S, D]")
+        S = T
+    G, N = gn = b.shape[-2:]
+    row = (D,)
+    px, xs = _rows(x, where, "x", lead, kind, dev, row)
+    pdt, dts = _rows(dt, where, "dt", lead, kind, dev, row)
+    pb, bs = _rows(b, where, "b", lead, kind, dev, gn)
+    pc, cs = _rows(c, where, "c", lead, kind, dev, gn)
+    pz, zs = (None, 0) if z is None else _rows(z, where, "z", lead, kind, dev, row)
+    return SelscanArgs(px, pdt, pb, pc, pz, xs, dts, bs, cs, zs, _flat(a, where, "a", (D, N), f32, dev),
+                       _flat(d_skip, where, "d_skip", row, f32, dev), _flat(dt_bias, where, "dt_bias", row, f32, dev),
+                       _flat(state_in, where, "state", (S, D, N), f32, dev), off, S, T, D, N, G, int(bool(softplus)), _DTYPES[kind]), dev
 
 
 def selscan_checkpoints(T, S, D, N, device):
@@ -562,28 +583,26 @@ def selscan_checkpoints(T, S, D, N, device):
     return torch.empty(int(lib().chela_selscan_checkpoint_bytes(T, S, D, N)) // 4, dtype=torch.float32, device=device)
 
 
-def _checkpoints(t, where, r, device):
+def _checkpoints(t, where, r, dev):
     if t is None:
         return None
     need = int(lib().chela_selscan_checkpoint_bytes(r.T, r.S, r.D, r.N)) // 4
     _need(t.dim() == 1 and t.shape[0] >= need, where, "checkpoints must come from selscan_checkpoints for these sizes")
-    return _flat(t, where, "checkpoints", (t.shape[0],), torch.float32, device)
+    return _flat(t, where, "checkpoints", t.shape, torch.float32, dev)
 
 
 def selscan_fwd(x, dt, a, b, c, d_skip=None, z=None, dt_bias=None, softplus=True, state_in=None, state_out=None,
                 seq_offsets=None, checkpoints=None, out_dtype=None, out=None, workspace=None):
     """chela_selscan_fwd: (y, state_out).  x, dt, z [T,D] or [B,L,D]; a [D,N] f32; b, c [...,G,N]; states [S,D,N] f32."""
     where = "chela_selscan_fwd"
-    r = _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state_in, seq_offsets)
-    y = _new(out, where, "out", x.shape, x.dtype if out_dtype is None else _tdtype(out_dtype), x.device)
-    state_out = _new(state_out, where, "state_out", (r.S, r.D, r.N), torch.float32, x.device)
-    ckpt = _checkpoints(checkpoints, where, r, x.device)
-    if workspace is None:
-        need = int(lib().chela_selscan_workspace_bytes(r.T, r.S, r.D, r.N))
-        workspace = _workspace(need, x.device) if need else None
-    with _on(x.device):
-        _check(lib().chela_selscan_fwd(ctypes.byref(r), _ptr(y), _ptr(state_out), ckpt, _dt(y), _ptr(workspace),
-                                       0 if workspace is None else workspace.numel(), _stream()), where)
+    r, dev = _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state_in, seq_offsets)
+    y = _new(out, where, "out", x.shape, x.dtype if out_dtype is None else _tdtype(out_dtype), x.device, dev)
+    state_out = _new(state_out, where, "state_out", (r.S, r.D, r.N), torch.float32, x.device, dev)
+    ckpt = _checkpoints(checkpoints, where, r, dev)
+    ws, nbytes = _scratch(lib().chela_selscan_workspace_bytes(r.T, r.S, r.D, r.N), workspace, x.device, where, dev)
+    with _on(dev):
+        _check(lib().chela_selscan_fwd(ctypes.byref(r), y.data_ptr(), state_out.data_ptr(), ckpt, _DTYPES[y.dtype], ws, nbytes,
+                                       _raw_stream(dev)), where)
     return y, state_out
 
 
@@ -592,16 +611,11 @@ def selscan_step(x, dt, a, b, c, state, d_skip=None, z=None, dt_bias=None, softp
     """chela_selscan_step: y [S,D] for one new token per sequence; state [S,D,N] f32 is updated in place unless state_out
     is given."""
     where = "chela_selscan_step"
-    _need(x.dim() == 2, where, "x must be [S, D]")
-    r = _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, None, None)
-    r.S = r.T
-    held = (r.S, r.D, r.N)
-    r.state_in = _flat(state, where, "state", held, torch.float32, x.device)
-    y = _new(out, where, "out", x.shape, x.dtype if out_dtype is None else _tdtype(out_dtype), x.device)
-    state_out = state if state_out is None else state_out
-    with _on(x.device):
-        _check(lib().chela_selscan_step(ctypes.byref(r), _ptr(y), _flat(state_out, where, "state_out", held, torch.float32, x.device),
-                                        _dt(y), _stream()), where)
+    r, dev = _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state, None, True)
+    y = _new(out, where, "out", x.shape, x.dtype if out_dtype is None else _tdtype(out_dtype), x.device, dev)
+    after = state.data_ptr() if state_out is None else _flat(state_out, where, "state_out", (r.S, r.D, r.N), torch.float32, dev)
+    with _on(dev):
+        _check(lib().chela_selscan_step(ctypes.byref(r), y.data_ptr(), after, _DTYPES[y.dtype], _raw_stream(dev)), where)
     return y
 
 
@@ -609,49 +623,45 @@ def selscan_bwd(x, dt, a, b, c, d_y, d_skip=None, z=None, dt_bias=None, softplus
                 checkpoints=None, d_state_out=None, grad_dtype=F32, want_d_state=False, workspace=None):
     """chela_selscan_bwd: SelscanGrads; d_x, d_dt, d_b, d_c, d_z of grad_dtype, the others f32 (None where not given)."""
     where = "chela_selscan_bwd"
-    r = _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state_in, seq_offsets)
-    dev, gt, f32, held = x.device, _tdtype(grad_dtype), torch.float32, (r.S, r.D, r.N)
-    pdy, dys = _rows(d_y, where, "d_y", tuple(x.shape[:-1]), x.dtype, dev, (r.D,))
+    r, dev = _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state_in, seq_offsets)
+    device, gt, f32, held = x.device, _tdtype(grad_dtype), torch.float32, (r.S, r.D, r.N)
+    pdy, dys = _rows(d_y, where, "d_y", x.shape[:-1], x.dtype, dev, (r.D,))
     ckpt = _checkpoints(checkpoints, where, r, dev)
-    g = SelscanGrads(d_x=torch.empty(x.shape, dtype=gt, device=dev), d_dt=torch.empty(x.shape, dtype=gt, device=dev),
-                     d_a=torch.empty(a.shape, dtype=f32, device=dev), d_b=torch.empty(b.shape, dtype=gt, device=dev),
-                     d_c=torch.empty(c.shape, dtype=gt, device=dev),
-                     d_skip=None if d_skip is None else torch.empty((r.D,), dtype=f32, device=dev),
-                     d_z=None if z is None else torch.empty(x.shape, dtype=gt, device=dev),
-                     d_dt_bias=None if dt_bias is None else torch.empty((r.D,), dtype=f32, device=dev),
-                     d_state_in=torch.empty(held, dtype=f32, device=dev) if want_d_state else None)
-    if workspace is None:
-        workspace = _workspace(int(lib().chela_selscan_bwd_workspace_bytes(r.T, r.S, r.D, r.N, int(ckpt is not None))), dev)
+    new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=device)  # noqa: E731
+    g = SelscanGrads(d_x=new(x.shape, gt), d_dt=new(x.shape, gt), d_a=new(a.shape, f32), d_b=new(b.shape, gt), d_c=new(c.shape, gt),
+                     d_skip=None if d_skip is None else new((r.D,), f32), d_z=None if z is None else new(x.shape, gt),
+                     d_dt_bias=None if dt_bias is None else new((r.D,), f32), d_state_in=new(held, f32) if want_d_state else None)
+    ws, nbytes = _scratch(lib().chela_selscan_bwd_workspace_bytes(r.T, r.S, r.D, r.N, int(ckpt is not None)), workspace, device, where, dev)
     with _on(dev):
         _check(lib().chela_selscan_bwd(ctypes.byref(r), pdy, dys, _flat(d_state_out, where, "d_state_out", held, f32, dev), ckpt,
                                        _ptr(g.d_x), _ptr(g.d_dt), _ptr(g.d_a), _ptr(g.d_b), _ptr(g.d_c), _ptr(g.d_skip), _ptr(g.d_z),
-                                       _ptr(g.d_dt_bias), _ptr(g.d_state_in), int(grad_dtype), _ptr(workspace), workspace.numel(),
-                                       _stream()), where)
+                                       _ptr(g.d_dt_bias), _ptr(g.d_state_in), int(grad_dtype), ws, nbytes, _raw_stream(dev)), where)
     return g
 
 
-def _blocknorm_args(where, res, y, gate, w_post, b_post, norm_post, scale, w_pre, b_pre, norm_pre, gate_act, gate_after, eps, in_dtype):
+def _blocknorm_args(where, res, y, gate, w_post, b_post, norm_post, scale, w_pre, b_pre, norm_pre, gate_act, gate_after, eps):
+    """(BlocknormArgs, the tensor that gives shape and residual dtype, device)"""
     first = res if res is not None else y
     _need(first is not None, where, "res or y must be given")
-    lead, _, _, _ = _seqs(first, None, where)
-    D, dev, f32 = first.shape[-1], first.device, torch.float32
-    r = BlocknormArgs()
-    if res is not None:
-        _need(res.dtype in _DTYPES, where, "res must be float32 or bfloat16")
-        r.res, r.res_stride = _rows(res, where, "res", lead, res.dtype, dev, (D,))
+    lead, _, _, _, dev = _seqs(first, None, where)
+    D, f32 = first.shape[-1], torch.float32
+    row = (D,)
+    pr, rs = (None, 0) if res is None else _rows(res, where, "res", lead, res.dtype, dev, row)
+    py = pg = None
+    ys = gs = 0
+    kind = first.dtype
     if y is not None:
-        _need(y.dtype in _DTYPES, where, "y must be float32 or bfloat16")
-        r.y, r.y_stride = _rows(y, where, "y", lead, y.dtype, dev, (D,))
+        kind = y.dtype
+        _need(kind in _DTYPES, where, "y must be float32 or bfloat16")
+        py, ys = _rows(y, where, "y", lead, kind, dev, row)
     if gate is not None:
         _need(y is not None, where, "gate goes with y")
-        r.gate, r.gate_stride = _rows(gate, where, "gate", lead, y.dtype, dev, (D,))
-    for name, t in (("w_post", w_post), ("b_post", b_post), ("scale", scale), ("w_pre", w_pre), ("b_pre", b_pre)):
-        setattr(r, name, _flat(t, where, name, (D,), f32, dev))
-    r.T, r.D = first.numel() // D if D else 0, D
-    r.gate_act, r.gate_after, r.norm_post, r.norm_pre, r.eps = int(gate_act), int(bool(gate_after)), int(norm_post), int(norm_pre), float(eps)
-    r.in_dtype = _dt(y) if y is not None else in_dtype
-    r.res_dtype = _dt(first)
-    return r, first
+        pg, gs = _rows(gate, where, "gate", lead, kind, dev, row)
+    T = lead[0] if len(lead) == 1 else lead[0] * lead[1]
+    return BlocknormArgs(pr, py, pg, rs, ys, gs, _flat(w_post, where, "w_post", row, f32, dev), _flat(b_post, where, "b_post", row, f32, dev),
+                         _flat(scale, where, "scale", row, f32, dev), _flat(w_pre, where, "w_pre", row, f32, dev),
+                         _flat(b_pre, where, "b_pre", row, f32, dev), T, D, int(gate_act), int(bool(gate_after)), int(norm_post),
+                         int(norm_pre), float(eps), _DTYPES[kind], _DTYPES[first.dtype]), first, dev
 
 
 def blocknorm_fwd(res, y=None, gate=None, w_post=None, b_post=None, norm_post=NORM_RMS, scale=None, w_pre=None, b_pre=None,
@@ -659,19 +669,19 @@ def blocknorm_fwd(res, y=None, gate=None, w_post=None, b_post=None, norm_post=NO
     """chela_blocknorm_fwd: (r', o).  y=None: only the norm before a block (r' is res itself); pre=False: only gate, norm,
     scale and residual behind one (o is None).  o is of out_dtype, or y's (without y: res's) dtype."""
     where = "chela_blocknorm_fwd"
-    r, first = _blocknorm_args(where, res, y, gate, w_post, b_post, norm_post, scale, w_pre, b_pre, norm_pre, gate_act, gate_after, eps,
-                               F32 if res is None or res.dtype == torch.float32 else BF16)
+    r, first, dev = _blocknorm_args(where, res, y, gate, w_post, b_post, norm_post, scale, w_pre, b_pre, norm_pre, gate_act, gate_after, eps)
     _need(pre or y is not None, where, "nothing to compute")
-    dev = first.device
     if y is not None:
-        res_out = _new(res_out, where, "res_out", first.shape, first.dtype, dev)
+        res_out = _new(res_out, where, "res_out", first.shape, first.dtype, first.device, dev)
     else:
         _need(res_out is None, where, "res_out goes with y")
-    o = None
+    o, code = None, F32
     if pre:
-        o = _new(out, where, "out", first.shape, (y.dtype if y is not None else res.dtype) if out_dtype is None else _tdtype(out_dtype), dev)
+        dt = (y if y is not None else res).dtype if out_dtype is None else _tdtype(out_dtype)
+        o, code = _new(out, where, "out", first.shape, dt, first.device, dev), _DTYPES[dt]
     with _on(dev):
-        _check(lib().chela_blocknorm_fwd(ctypes.byref(r), _ptr(res_out), _ptr(o), F32 if o is None else _dt(o), _stream()), where)
+        _check(lib().chela_blocknorm_fwd(ctypes.byref(r), None if res_out is None else res_out.data_ptr(), None if o is None else o.data_ptr(),
+                                         code, _raw_stream(dev)), where)
     return res_out if y is not None else res, o
 
 
@@ -680,21 +690,18 @@ def blocknorm_bwd(res_out, y=None, gate=None, d_o=None, d_res_out=None, w_post=N
     """chela_blocknorm_bwd: BlocknormGrads from r' (as blocknorm_fwd returned it), y and gate; d_o of y's dtype (without y:
     res_out's), d_res_out of res_out's dtype, either may be None.  d_res is of res_out's dtype, d_y and d_gate of grad_dtype."""
     where = "chela_blocknorm_bwd"
-    r, first = _blocknorm_args(where, res_out, y, gate, w_post, b_post, norm_post, scale, w_pre, b_pre, norm_pre, gate_act, gate_after, eps,
-                               F32 if res_out.dtype == torch.float32 else BF16)
-    dev, shape, gt, D = first.device, first.shape, _tdtype(grad_dtype), r.D
-    in_dtype = torch.float32 if r.in_dtype == F32 else torch.bfloat16
-    vec = lambda on: torch.empty((D,), dtype=torch.float32, device=dev) if on else None  # noqa: E731
-    g = BlocknormGrads(d_res=torch.empty(shape, dtype=first.dtype, device=dev),
-                       d_y=None if y is None else torch.empty(shape, dtype=gt, device=dev),
-                       d_gate=None if gate is None else torch.empty(shape, dtype=gt, device=dev),
-                       d_w_post=vec(w_post is not None), d_b_post=vec(b_post is not None), d_scale=vec(scale is not None),
-                       d_w_pre=vec(w_pre is not None), d_b_pre=vec(b_pre is not None))
-    if workspace is None:
-        workspace = _workspace(int(lib().chela_blocknorm_bwd_workspace_bytes(r.T, D)), dev)
+    r, first, dev = _blocknorm_args(where, res_out, y, gate, w_post, b_post, norm_post, scale, w_pre, b_pre, norm_pre, gate_act, gate_after, eps)
+    device, shape, gt, D = first.device, first.shape, _tdtype(grad_dtype), r.D
+    kind = first.dtype if y is None else y.dtype
+    vec = lambda w: None if w is None else torch.empty((D,), dtype=torch.float32, device=device)  # noqa: E731
+    g = BlocknormGrads(d_res=torch.empty(shape, dtype=first.dtype, device=device),
+                       d_y=None if y is None else torch.empty(shape, dtype=gt, device=device),
+                       d_gate=None if gate is None else torch.empty(shape, dtype=gt, device=device),
+                       d_w_post=vec(w_post), d_b_post=vec(b_post), d_scale=vec(scale), d_w_pre=vec(w_pre), d_b_pre=vec(b_pre))
+    ws, nbytes = _scratch(lib().chela_blocknorm_bwd_workspace_bytes(r.T, D), workspace, device, where, dev)
     with _on(dev):
-        _check(lib().chela_blocknorm_bwd(ctypes.byref(r), _flat(d_o, where, "d_o", shape, in_dtype, dev),
+        _check(lib().chela_blocknorm_bwd(ctypes.byref(r), _flat(d_o, where, "d_o", shape, kind, dev),
                                          _flat(d_res_out, where, "d_res_out", shape, first.dtype, dev), _ptr(g.d_res), _ptr(g.d_y),
                                          _ptr(g.d_gate), _ptr(g.d_w_post), _ptr(g.d_b_post), _ptr(g.d_scale), _ptr(g.d_w_pre),
-                                         _ptr(g.d_b_pre), int(grad_dtype), _ptr(workspace), workspace.numel(), _stream()), where)
+                                         _ptr(g.d_b_pre), int(grad_dtype), ws, nbytes, _raw_stream(dev)), where)
     return g

@@ -969,9 +969,10 @@ chela_status_t fwd_launch(ScanParams p, cudaStream_t stream)
 }
 
 // Half as many channels a chain and twice the tokens a slice (one channel a lane): twice the chains, half the steps of each.
-// Every b and c is then read for one channel instead of two, so it pays only while there is no more than one chain of the
-// full width per SM (4 x 4096 x 1024: 152 us against 226; 8 x 8192 x 1024, two chains an SM: 581 against 553).
-bool fwd_narrow(const ScanParams &p, int N) { return !p.seg && (long long)p.S * ((p.D + chain_channels(N) - 1) / chain_channels(N)) <= 148; }
+// Every b and c is then read for one channel instead of two, so it pays while the SM with the most chains has fewer half
+// ones than whole ones' halves: up to one and a half chains of the full width per SM (4 x 4096 x 1024, 128 chains: 152 us
+// against 226; 8 x 8192 x 1024, 256 chains: 581 against 553).
+bool fwd_narrow(const ScanParams &p, int N) { return !p.seg && (long long)p.S * ((p.D + chain_channels(N) - 1) / chain_channels(N)) <= 222; }
 
 template <typename TI, typename TO>
 chela_status_t fwd_n(const ScanParams &p, int N, cudaStream_t stream)

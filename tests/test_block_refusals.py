@@ -115,7 +115,7 @@ def test_the_binding_refuses_what_does_not_fit(lib):
         with pytest.raises(chela.ChelaError, match="no CPU fallback") as e:
             call()
         assert e.value.status == chela.ERR_INVALID_ARG
-    where, d, f = "here", x.device, torch.float32
+    where, d, f = "here", -1, torch.float32
     rows = lambda t, lead, inner: chela._rows(t, where, "t", lead, f, d, inner)[1]  # noqa: E731
     assert rows(torch.zeros(4, 128)[:, 64:], (4,), (64,)) == 128
     assert rows(torch.zeros(2, 4, 128)[..., :64], (2, 4), (64,)) == 128
