@@ -44,6 +44,19 @@ struct Raw8 {
         lo.zero();
         hi.zero();
     }
+    // from 16-byte vectors `step` vectors apart
+    __device__ __forceinline__ void from(const uint4 *p, int step)
+    {
+        const uint4 u = p[0];
+        if constexpr (sizeof(T) == 2) {
+            lo.v = make_uint2(u.x, u.y);
+            hi.v = make_uint2(u.z, u.w);
+        } else {
+            const uint4 w = p[step];
+            lo.v = make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
+            hi.v = make_float4(__uint_as_float(w.x), __uint_as_float(w.y), __uint_as_float(w.z), __uint_as_float(w.w));
+        }
+    }
     __device__ __forceinline__ Vec8 get() const
     {
         const float4 a = lo.get(), b = hi.get();
@@ -83,42 +96,57 @@ __device__ __forceinline__ void stage_weight(float *to, const float *from, float
     for (int c = threadIdx.x; c < width; c += blockDim.x) to[c] = from && c < D ? from[c] : other;
 }
 
-__device__ __forceinline__ float act_f(float u, int act) { return act == 0 ? u : (act == 1 ? u * sigmoid_acc(u) : sigmoid_acc(u)); }
-__device__ __forceinline__ float d_act_f(float u, int act)
+// act(u) in place; act is the same for all threads, so the branch is taken once and not per element
+__device__ __forceinline__ void activate8(Vec8 &u, int act)
 {
-    if (act == 0) return 1.f;
-    const float s = sigmoid_acc(u);
-    return act == 1 ? s * fmaf(u, 1.f - s, 1.f) : s * (1.f - s);
+    if (act == 1) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u.v[e] *= sigmoid_acc(u.v[e]);
+    } else if (act == 2) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u.v[e] = sigmoid_acc(u.v[e]);
+    }
 }
 
-// Sum of K values over the lanes of a row (WPR warps); every lane gets the result.  `buf` holds 2 x WPR x K floats per
-// row group, the halves used in turn so that one barrier per sum is enough.
-template <int WPR, int K>
+// Sums over the lanes of a row (WPR warps); every lane gets the result.  `buf` holds 2 x WPR pairs per row group, the
+// halves used in turn so that one barrier per sum is enough.  A pair of sums takes 5 exchanges, not 10: the first one gives
+// one value to each half of the warp.
+template <int WPR>
 struct RowSum {
-    float *buf;
+    float2 *buf;
     int parity, group, wr, lane;
-    __device__ __forceinline__ void operator()(float (&v)[K])
+    __device__ __forceinline__ float2 meet(float2 mine, bool writer, bool second)   // second: this lane writes .y
+    {
+        float2 *b = buf + (group * 2 + parity) * WPR;
+        parity ^= 1;
+        if (writer) reinterpret_cast<float *>(b + wr)[second] = second ? mine.y : mine.x;
+        asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(WPR * 32) : "memory");
+        float2 t = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < WPR; w += 2) {
+            const float4 v = *reinterpret_cast<const float4 *>(b + w);
+            t.x += v.x + v.z;
+            t.y += v.y + v.w;
+        }
+        return t;
+    }
+    __device__ __forceinline__ float one(float v)
     {
 #pragma unroll
-        for (int k = 0; k < K; ++k)
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        return WPR == 1 ? v : meet(make_float2(v, 0.f), lane == 0, false).x;
+    }
+    __device__ __forceinline__ float2 two(float a, float b)
+    {
+        const bool up = lane & 16;
+        float v = (up ? b : a) + __shfl_xor_sync(0xffffffffu, up ? a : b, 16);
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-        if (WPR > 1) {
-            float *b = buf + (group * 2 + parity) * WPR * K;
-            parity ^= 1;
-            if (lane == 0) {
-#pragma unroll
-                for (int k = 0; k < K; ++k) b[wr * K + k] = v[k];
-            }
-            asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(WPR * 32) : "memory");
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                float t = 0.f;
-#pragma unroll
-                for (int w = 0; w < WPR; ++w) t += b[w * K + k];
-                v[k] = t;
-            }
+        for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (WPR == 1) {
+            const float w = __shfl_xor_sync(0xffffffffu, v, 16);
+            return make_float2(up ? w : v, up ? v : w);
         }
+        return meet(make_float2(v, v), (lane & 15) == 0, up);
     }
 };
 
@@ -128,10 +156,10 @@ template <typename TI, typename TR, typename TO, int WPR>
 __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 3) blocknorm_fwd_kernel(const NormParams p)
 {
     constexpr int GROUPS = WPR > 8 ? 1 : 8 / WPR, WIDTH = WPR * 256;
-    __shared__ float buf[GROUPS * 2 * WPR];
+    __shared__ __align__(16) float2 buf[GROUPS * 2 * WPR];
     extern __shared__ __align__(16) float s_w[];   // w_post, b_post, scale, w_pre, b_pre [WIDTH], those that are used
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / WPR, wr = warp % WPR;
-    RowSum<WPR, 1> sum = {buf, 0, group, wr, lane};
+    RowSum<WPR> sum = {buf, 0, group, wr, lane};
     const float inv_d = 1.f / p.D;
     const int c = 8 * (wr * 32 + lane);
     const bool live = c < p.D, post = p.y != nullptr, pre = p.o != nullptr, gated = p.gate != nullptr;
@@ -149,21 +177,19 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 3) blo
 
     auto normalise = [&](Vec8 &x, int kind) {
         if (kind == CHELA_NORM_NONE) return;
-        float s[1];
         if (kind == CHELA_NORM_LAYER) {
-            s[0] = 0.f;
+            float s = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[0] += x.v[e];
-            sum(s);
-            const float mean = live ? s[0] * inv_d : 0.f;
+            for (int e = 0; e < 8; ++e) s += x.v[e];
+            s = sum.one(s);
+            const float mean = live ? s * inv_d : 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) x.v[e] -= mean;
         }
-        s[0] = 0.f;
+        float s = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[0] = fmaf(x.v[e], x.v[e], s[0]);
-        sum(s);
-        const float inv = 1.0f / sqrtf(fmaf(s[0], inv_d, p.eps));
+        for (int e = 0; e < 8; ++e) s = fmaf(x.v[e], x.v[e], s);
+        const float inv = 1.0f / sqrtf(fmaf(sum.one(s), inv_d, p.eps));
 #pragma unroll
         for (int e = 0; e < 8; ++e) x.v[e] *= inv;
     };
@@ -184,21 +210,24 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 3) blo
         fetch(row + stride);
         if (post) {
             if (gated) {
+                activate8(g, p.gate_act);
+                if (!p.gate_after) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    g.v[e] = act_f(g.v[e], p.gate_act);
-                    if (!p.gate_after) v.v[e] *= g.v[e];
+                    for (int e = 0; e < 8; ++e) v.v[e] *= g.v[e];
                 }
             }
             normalise(v, p.norm_post);
             const Vec8 w = weight8(staged, s_w, 0, WIDTH, c, live, p.w_post, 1.f), b = weight8(staged, s_w, 1, WIDTH, c, live, p.b_post, 0.f),
                        s = weight8(staged, s_w, 2, WIDTH, c, live, p.scale, 1.f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float m = fmaf(v.v[e], w.v[e], b.v[e]);
-                if (gated && p.gate_after) m *= g.v[e];
-                r.v[e] = live ? fmaf(s.v[e], m, r.v[e]) : 0.f;
+            for (int e = 0; e < 8; ++e) v.v[e] = fmaf(v.v[e], w.v[e], b.v[e]);
+            if (gated && p.gate_after) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v.v[e] *= g.v[e];
             }
+            const float on = live ? 1.f : 0.f;   // channels past D stay zero for the next norm's sums
+#pragma unroll
+            for (int e = 0; e < 8; ++e) r.v[e] = fmaf(s.v[e] * on, v.v[e], r.v[e]);
             if (live && p.res_out) store8(static_cast<TR *>(p.res_out) + (size_t)row * p.D + c, r);
         }
         if (pre) {
@@ -221,17 +250,18 @@ struct NormBwdParams {
 };
 
 // One vector of 8 channels a lane, so that the five parameter gradients of its channels (40 registers) stay in registers
-// over all rows the group walks; D <= 256 WPR.
+// over all rows the group walks; D <= 256 WPR.  Channels past D have zero operands, and zero weights where that is not
+// enough, so they add nothing to the sums.
 template <typename TI, typename TR, typename TG, int WPR>
 __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 2) blocknorm_bwd_kernel(const NormBwdParams q)
 {
     constexpr int GROUPS = WPR > 8 ? 1 : 8 / WPR;
     const NormParams &p = q.f;
     constexpr int WIDTH = WPR * 256;
-    __shared__ float buf[GROUPS * 2 * WPR * 2];
+    __shared__ __align__(16) float2 buf[GROUPS * 2 * WPR];
     extern __shared__ __align__(16) float s_w[];   // w_post, b_post, scale, w_pre [WIDTH]; in the end the groups' sums
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / WPR, wr = warp % WPR;
-    RowSum<WPR, 2> sum = {buf, 0, group, wr, lane};
+    RowSum<WPR> sum = {buf, 0, group, wr, lane};
     const float inv_d = 1.f / p.D;
     const int c = 8 * (wr * 32 + lane);
     const bool live = c < p.D;
@@ -245,127 +275,183 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 2) blo
     stage_weight(s_w + 3 * WIDTH, p.w_pre, 1.f, p.D, WIDTH);
     __syncthreads();
 
+    // Operands of a row.  Up to 2048 channels they are copied to shared memory one row ahead, every lane what it will read
+    // itself, so nothing but its own copies has to be waited for and registers are not held meanwhile; wider rows are read
+    // where they are wanted.
+    constexpr bool AHEAD = WPR <= 8;
+    constexpr int NR = sizeof(TR) / 2, NI = sizeof(TI) / 2, SLOTS = 2 * NR + 3 * NI;   // 16-byte vectors of r', d r', d o, y, gate
+    uint4 *s_row = reinterpret_cast<uint4 *>(s_w + (GROUPS > 5 ? GROUPS - 1 : 4) * WIDTH) + warp * (2 * SLOTS * 32) + lane;
     const long long stride = (long long)gridDim.x * GROUPS;
     long long row = (long long)blockIdx.x * GROUPS + group;
-    Raw8<TR> rr, rd;
-    Raw8<TI> ro, ry, rg;
-    auto fetch = [&](long long at) {
+    auto fetch = [&](long long at, int stage) {
         const bool ok = live && at < p.T;
-        if (ok && q.d_ro) rd.load(static_cast<const TR *>(q.d_ro) + (size_t)at * p.D + c); else rd.zero();
-        if (ok && pre) {
-            ro.load(static_cast<const TI *>(q.d_o) + (size_t)at * p.D + c);
-            rr.load(static_cast<const TR *>(p.res) + (size_t)at * p.rs + c);
-        } else {
-            ro.zero();
-            rr.zero();
-        }
-        if (ok && post) ry.load(static_cast<const TI *>(p.y) + (size_t)at * p.ys + c); else ry.zero();
-        if (ok && gated) rg.load(static_cast<const TI *>(p.gate) + (size_t)at * p.gs + c); else rg.zero();
-    };
-    fetch(row);
-    for (; row < p.T; row += stride) {
-        Vec8 hat = rr.get(), d_o = ro.get(), d_r = rd.get(), v, ga = fill8(1.f);
-        const Raw8<TI> ky = ry, kg = rg;   // unpacked again where they are wanted, half the registers until then
-        fetch(row + stride);
-        {
-            const Vec8 y = ky.get(), gr = kg.get();
+        uint4 *to = s_row + stage * SLOTS * 32;
+        auto vectors = [&](int slot, const char *from, int n, bool used) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (gated) ga.v[e] = act_f(gr.v[e], p.gate_act);
-                v.v[e] = p.gate_after ? y.v[e] : y.v[e] * ga.v[e];
+            for (int i = 0; i < 2; ++i)
+                if (i < n) copy16(to + (slot + i) * 32, from + 16 * i, ok && used);
+        };
+        const size_t t = ok ? (size_t)at : 0, k = ok ? c : 0;
+        const bool grad = q.d_ro != nullptr;
+        vectors(0, reinterpret_cast<const char *>(static_cast<const TR *>(pre ? p.res : q.d_res) + t * (pre ? p.rs : p.D) + k), NR, pre);
+        vectors(NR, reinterpret_cast<const char *>(static_cast<const TR *>(grad ? q.d_ro : q.d_res) + t * p.D + k), NR, grad);
+        vectors(2 * NR, static_cast<const char *>(pre ? q.d_o : q.d_res) + (t * p.D + k) * sizeof(TI), NI, pre);
+        vectors(2 * NR + NI, static_cast<const char *>(post ? p.y : q.d_res) + (post ? (t * p.ys + k) * sizeof(TI) : 0), NI, post);
+        vectors(2 * NR + 2 * NI, static_cast<const char *>(gated ? p.gate : q.d_res) + (gated ? (t * p.gs + k) * sizeof(TI) : 0), NI, gated);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int stage = 0;
+    if (AHEAD) fetch(row, 0);
+    for (; row < p.T; row += stride) {
+        if (AHEAD) {
+            fetch(row + stride, stage ^ 1);
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+        }
+        const uint4 *now = s_row + stage * SLOTS * 32;
+        stage ^= 1;
+        auto res_like = [&](int slot, const void *from, long long step, bool used) -> Vec8 {
+            Raw8<TR> r;
+            if (AHEAD) r.from(now + slot * 32, 32);
+            else if (live && used) r.load(static_cast<const TR *>(from) + (size_t)row * step + c);
+            else r.zero();
+            return r.get();
+        };
+        auto in_like = [&](int slot, const void *from, long long step, bool used) -> Vec8 {
+            Raw8<TI> r;
+            if (AHEAD) r.from(now + slot * 32, 32);
+            else if (live && used) r.load(static_cast<const TI *>(from) + (size_t)row * step + c);
+            else r.zero();
+            return r.get();
+        };
+        auto read_y = [&]() { return in_like(2 * NR + NI, p.y, p.ys, post); };
+        auto read_gate = [&]() { return in_like(2 * NR + 2 * NI, p.gate, p.gs, gated); };
+        Vec8 hat = res_like(0, p.res, p.rs, pre), v = read_y(), ga;
+        if (gated) {
+            ga = read_gate();
+            activate8(ga, p.gate_act);
+            if (!p.gate_after) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v.v[e] *= ga.v[e];
             }
         }
-        // statistics of both norms together: [0] = r', [1] = v
-        float s[2];
+        // statistics of both norms together: r' and v
+        float2 s;
         const bool l0 = pre && p.norm_pre == CHELA_NORM_LAYER, l1 = post && p.norm_post == CHELA_NORM_LAYER;
         if (l0 || l1) {
-            s[0] = s[1] = 0.f;
+            float a = 0.f, b = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                s[0] += hat.v[e];
-                s[1] += v.v[e];
+                a += hat.v[e];
+                b += v.v[e];
             }
-            sum(s);
-            const float m0 = l0 && live ? s[0] * inv_d : 0.f, m1 = l1 && live ? s[1] * inv_d : 0.f;
+            s = sum.two(a, b);
+            const float m0 = l0 && live ? s.x * inv_d : 0.f, m1 = l1 && live ? s.y * inv_d : 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 hat.v[e] -= m0;
                 v.v[e] -= m1;
             }
         }
-        s[0] = s[1] = 0.f;
+        {
+            float a = 0.f, b = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            s[0] = fmaf(hat.v[e], hat.v[e], s[0]);
-            s[1] = fmaf(v.v[e], v.v[e], s[1]);
+            for (int e = 0; e < 8; ++e) {
+                a = fmaf(hat.v[e], hat.v[e], a);
+                b = fmaf(v.v[e], v.v[e], b);
+            }
+            s = sum.two(a, b);
         }
-        sum(s);
-        const float i0 = p.norm_pre == CHELA_NORM_NONE ? 1.f : 1.0f / sqrtf(fmaf(s[0], inv_d, p.eps));
-        const float i1 = p.norm_post == CHELA_NORM_NONE ? 1.f : 1.0f / sqrtf(fmaf(s[1], inv_d, p.eps));
+        const float i0 = p.norm_pre == CHELA_NORM_NONE ? 1.f : 1.0f / sqrtf(fmaf(s.x, inv_d, p.eps));
+        const float i1 = p.norm_post == CHELA_NORM_NONE ? 1.f : 1.0f / sqrtf(fmaf(s.y, inv_d, p.eps));
         // norm before the next block: d hat, then d r'
+        Vec8 d_r = res_like(NR, q.d_ro, p.D, q.d_ro != nullptr);
         if (pre) {
-            Vec8 dh = fill8(0.f);
-            s[0] = s[1] = 0.f;
             const Vec8 w = load8(s_w + 3 * WIDTH + c);
+            Vec8 d_o = in_like(2 * NR, q.d_o, p.D, pre);
+            float a = 0.f, b = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 hat.v[e] *= i0;
                 acc[3].v[e] = fmaf(d_o.v[e], hat.v[e], acc[3].v[e]);
                 acc[4].v[e] += d_o.v[e];
-                dh.v[e] = d_o.v[e] * w.v[e];
-                s[0] = fmaf(dh.v[e], hat.v[e], s[0]);
-                s[1] += dh.v[e];
+                d_o.v[e] *= w.v[e];
+                a = fmaf(d_o.v[e], hat.v[e], a);
+                b += d_o.v[e];
             }
             if (p.norm_pre != CHELA_NORM_NONE) {
-                sum(s);
-                const float k0 = s[0] * inv_d, k1 = l0 ? s[1] * inv_d : 0.f;
+                s = sum.two(a, b);
+                const float k0 = -s.x * inv_d, k1 = l0 && live ? s.y * inv_d : 0.f;   // channels past D stay zero
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d_r.v[e] = fmaf(i0, fmaf(-hat.v[e], k0, dh.v[e]) - k1, d_r.v[e]);
+                for (int e = 0; e < 8; ++e) d_r.v[e] = fmaf(i0, fmaf(hat.v[e], k0, d_o.v[e]) - k1, d_r.v[e]);
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d_r.v[e] += dh.v[e];
+                for (int e = 0; e < 8; ++e) d_r.v[e] += d_o.v[e];
             }
         }
         if (live) store8(static_cast<TR *>(q.d_res) + (size_t)row * p.D + c, d_r);
         if (post) {
-            Vec8 dn = fill8(0.f), dm = fill8(0.f), n = fill8(0.f);
-            s[0] = s[1] = 0.f;
-            if (live) {
-                const Vec8 w = load8(s_w + c), b = load8(s_w + WIDTH + c), sc = load8(s_w + 2 * WIDTH + c);
+            // d_r becomes d m, then d n, then d hat, then d v
+            const Vec8 w = load8(s_w + c), sc = load8(s_w + 2 * WIDTH + c);
+            Vec8 n = load8(s_w + WIDTH + c);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v.v[e] *= i1;
+                n.v[e] = fmaf(v.v[e], w.v[e], n.v[e]);
+            }
+            Vec8 dg;   // gradient of act(gate)
+            if (gated && p.gate_after) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    v.v[e] *= i1;
-                    n.v[e] = fmaf(v.v[e], w.v[e], b.v[e]);
-                    dm.v[e] = d_r.v[e] * sc.v[e];
-                    const float after = p.gate_after ? ga.v[e] : 1.f;
-                    acc[2].v[e] = fmaf(d_r.v[e], n.v[e] * after, acc[2].v[e]);
-                    const float d_n = dm.v[e] * after;
-                    acc[0].v[e] = fmaf(d_n, v.v[e], acc[0].v[e]);
-                    acc[1].v[e] += d_n;
-                    dn.v[e] = d_n * w.v[e];
-                    s[0] = fmaf(dn.v[e], v.v[e], s[0]);
-                    s[1] += dn.v[e];
+                    acc[2].v[e] = fmaf(d_r.v[e], n.v[e] * ga.v[e], acc[2].v[e]);
+                    d_r.v[e] *= sc.v[e];
+                    dg.v[e] = d_r.v[e] * n.v[e];
+                    d_r.v[e] *= ga.v[e];
                 }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    acc[2].v[e] = fmaf(d_r.v[e], n.v[e], acc[2].v[e]);
+                    d_r.v[e] *= sc.v[e];
+                }
+            }
+            float a = 0.f, b = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                acc[0].v[e] = fmaf(d_r.v[e], v.v[e], acc[0].v[e]);
+                acc[1].v[e] += d_r.v[e];
+                d_r.v[e] *= w.v[e];
+                a = fmaf(d_r.v[e], v.v[e], a);
+                b += d_r.v[e];
             }
             if (p.norm_post != CHELA_NORM_NONE) {
-                sum(s);
-                const float k0 = s[0] * inv_d, k1 = l1 ? s[1] * inv_d : 0.f;
+                s = sum.two(a, b);
+                const float k0 = -s.x * inv_d, k1 = l1 ? s.y * inv_d : 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dn.v[e] = i1 * (fmaf(-v.v[e], k0, dn.v[e]) - k1);
+                for (int e = 0; e < 8; ++e) d_r.v[e] = i1 * (fmaf(v.v[e], k0, d_r.v[e]) - k1);
             }
-            if (live) {
-                const Vec8 y = ky.get(), gr = kg.get();
-                Vec8 out;
+            if (gated) {
+                const Vec8 gr = read_gate();
+                if (!p.gate_after) {
+                    const Vec8 y = read_y();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) out.v[e] = p.gate_after ? dn.v[e] : dn.v[e] * ga.v[e];
-                store8(static_cast<TG *>(q.d_y) + (size_t)row * p.D + c, out);
-                if (p.gate) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        out.v[e] = (p.gate_after ? dm.v[e] * n.v[e] : dn.v[e] * y.v[e]) * d_act_f(gr.v[e], p.gate_act);
-                    store8(static_cast<TG *>(q.d_gate) + (size_t)row * p.D + c, out);
+                    for (int e = 0; e < 8; ++e) {
+                        dg.v[e] = d_r.v[e] * y.v[e];
+                        d_r.v[e] *= ga.v[e];
+                    }
                 }
+                if (p.gate_act == 1) {   // slope sg (1 + u (1 - sg)) = sg + act (1 - sg)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float sg = sigmoid_acc(gr.v[e]);
+                        dg.v[e] *= fmaf(ga.v[e], 1.f - sg, sg);
+                    }
+                } else if (p.gate_act == 2) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) dg.v[e] *= fmaf(-ga.v[e], ga.v[e], ga.v[e]);
+                }
+                if (live) store8(static_cast<TG *>(q.d_gate) + (size_t)row * p.D + c, dg);
             }
+            if (live) store8(static_cast<TG *>(q.d_y) + (size_t)row * p.D + c, d_r);
         }
     }
     // sums of the CTA's row groups, one partial row per CTA
@@ -460,8 +546,10 @@ chela_status_t bwd_d(const NormBwdParams &q, const NormSums &sums, cudaStream_t 
 {
     const NormParams &p = q.f;
     const int wpr = row_warps(p.D), grid = row_grid(p.T, p.D, kBwdPerSm);
+    // weights (in the end the row groups' sums); two rows of operands a warp where they are fetched ahead
     const int rows = row_groups(wpr) - 1 > 4 ? row_groups(wpr) - 1 : 4;
-    const size_t smem = (size_t)rows * wpr * 256 * 4;
+    const size_t ahead = wpr <= 8 ? (size_t)8 * 2 * (sizeof(TR) + 3 * sizeof(TI) / 2) * 32 * 16 : 0;
+    const size_t smem = (size_t)rows * wpr * 256 * 4 + ahead;
     chela_status_t st;
     switch (wpr) {
     case 1: st = norm_launch(blocknorm_bwd_kernel<TI, TR, TG, 1>, q, grid, 256, smem, stream); break;

@@ -124,4 +124,11 @@ struct Raw4<__nv_bfloat16> {
     }
 };
 
+// 16 bytes from global to shared memory, asynchronously; zeros where ok is false (the address is then not read)
+__device__ __forceinline__ void copy16(void *dst, const void *src, bool ok)
+{
+    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+
 }  // namespace chela

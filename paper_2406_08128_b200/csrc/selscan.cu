@@ -59,13 +59,6 @@ __device__ __forceinline__ float4 *ckpt_at(float *ckpt, size_t index, int chains
 
 __device__ __forceinline__ void named_sync(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
 __device__ __forceinline__ void named_arrive(int id) { asm volatile("bar.arrive %0, 64;" ::"r"(id) : "memory"); }
-// 16 bytes from global to shared memory, zeros where ok is false (the address is then not read)
-__device__ __forceinline__ void copy16(void *dst, const void *src, bool ok)
-{
-    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(ok ? 16 : 0) : "memory");
-}
-
 // NS = 8 states and CH channels a lane; R = N / 8 lanes share CH channels.
 template <typename TI, int N, int CH, int TOK>
 struct FwdShape {

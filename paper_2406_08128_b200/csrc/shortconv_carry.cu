@@ -10,7 +10,7 @@ namespace chela {
 namespace {
 
 constexpr int kTok = 32;      // tokens of one forward work item
-constexpr int kBwdTok = 32;   // tokens of one backward work item
+constexpr int kBwdTok = 64;   // tokens of one backward work item
 
 struct ConvParams {
     const void *x;
