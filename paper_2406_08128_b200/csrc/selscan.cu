@@ -44,6 +44,13 @@ __device__ __forceinline__ float decay_rate(float a)
     const float v = a * kLog2e;
     return v < -3.0e38f ? -3.0e38f : v;
 }
+// sum += v with the digits that the sum loses carried along (Kahan): a long sequence adds thousands of tiles to one lane
+__device__ __forceinline__ void compensated(float &sum, float &lost, float v)
+{
+    const float y = __fsub_rn(v, lost), t = __fadd_rn(sum, y);
+    lost = __fsub_rn(__fsub_rn(t, sum), y);
+    sum = t;
+}
 __device__ __forceinline__ float gate_f(float z) { return z * sigmoid_acc(z); }
 
 // Channels of a warp (and of a chain) in both kernels, and the checkpoints' layout, which is the warps' own: for each
@@ -258,7 +265,7 @@ __global__ void __launch_bounds__(32 * WT, OCC) selscan_fwd_kernel(const ScanPar
                 const float d = of(dt, i, j);
 #pragma unroll
                 for (int k = 0; k < NP; ++k) {
-                    const float2 v = mul2v(a[k], splat2(d));
+                    const float2 v = fma2v(a[k], splat2(d), splat2(kDecayShift));
                     e[i][j][k] = make_float2(ex2(v.x), ex2(v.y));
                 }
             }
@@ -427,10 +434,10 @@ __global__ void __launch_bounds__(256) selscan_step_kernel(const ScanParams p)
     if (p.softplus) dt = softplus_acc(dt);
     const float dx = dt * x;
     float4 n;
-    n.x = fmaf(ex2(dt * decay_rate(a.x)), h.x, dx * b.x);
-    n.y = fmaf(ex2(dt * decay_rate(a.y)), h.y, dx * b.y);
-    n.z = fmaf(ex2(dt * decay_rate(a.z)), h.z, dx * b.z);
-    n.w = fmaf(ex2(dt * decay_rate(a.w)), h.w, dx * b.w);
+    n.x = fmaf(ex2(fmaf(dt, decay_rate(a.x), kDecayShift)), h.x, dx * b.x);
+    n.y = fmaf(ex2(fmaf(dt, decay_rate(a.y), kDecayShift)), h.y, dx * b.y);
+    n.z = fmaf(ex2(fmaf(dt, decay_rate(a.z), kDecayShift)), h.z, dx * b.z);
+    n.w = fmaf(ex2(fmaf(dt, decay_rate(a.w), kDecayShift)), h.w, dx * b.w);
     float y = fmaf(c.x, n.x, c.y * n.y) + fmaf(c.z, n.z, c.w * n.w);
 #pragma unroll
     for (int o = 1; o < R; o <<= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
@@ -572,7 +579,7 @@ __global__ void __launch_bounds__(32 * BwdShape<TI, N, CH>::WT, 1) selscan_bwd_k
         for (int k = 0; k < NP; ++k) a[j][k] = make_float2(decay_rate(a[j][k].x), decay_rate(a[j][k].y));
     clear(da);
     const float bias = live && p.bias ? p.bias[ch] : 0.f, skip = live && p.dsk ? p.dsk[ch] : 0.f;
-    float sum_skip = 0.f, sum_bias = 0.f;
+    float sum_skip = 0.f, sum_bias = 0.f, lost_skip = 0.f, lost_bias = 0.f;
     __syncthreads();
 
     const int ntile = (sr.len + TOK - 1) / TOK;
@@ -678,7 +685,7 @@ __global__ void __launch_bounds__(32 * BwdShape<TI, N, CH>::WT, 1) selscan_bwd_k
                     const float2 d = splat2(s_dt[at]), x = splat2(s_dx[at]), y = splat2(s_dg[at]);
 #pragma unroll
                     for (int k = 0; k < NP; ++k) {
-                        const float2 v = mul2v(a[j][k], d), e = make_float2(ex2(v.x), ex2(v.y));
+                        const float2 v = fma2v(a[j][k], d, splat2(kDecayShift)), e = make_float2(ex2(v.x), ex2(v.y));
                         h[j][k] = fma2v(e, h[j][k], mul2v(x, bv[k]));
                         whole[j][k] = mul2v(whole[j][k], e);
                         add[j][k] = fma2v(whole[j][k], mul2v(cv[k], y), add[j][k]);
@@ -709,6 +716,7 @@ __global__ void __launch_bounds__(32 * BwdShape<TI, N, CH>::WT, 1) selscan_bwd_k
         }
 
         // backwards, two tokens at a time
+        float tile_skip = 0.f, tile_bias = 0.f;
         float *part = q_.part_bc + ((size_t)cb * p.T + sr.start + t0) * (2 * N);   // [token][dB N | dC N]
 #pragma unroll 1
         for (int u = TOK - SUB; u >= 0; u -= SUB) {
@@ -766,7 +774,7 @@ __global__ void __launch_bounds__(32 * BwdShape<TI, N, CH>::WT, 1) selscan_bwd_k
                         float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
                         for (int k = 0; k < NP; ++k) {
-                            const float2 w = mul2v(a[j][k], splat2(dts[i][j]));
+                            const float2 w = fma2v(a[j][k], splat2(dts[i][j]), splat2(kDecayShift));
                             e[i][j][k] = make_float2(ex2(w.x), ex2(w.y));
                             hh[j][k] = fma2v(e[i][j][k], i ? h0[j][k] : h[j][k], mul2v(splat2(dxs[i][j]), bv[k]));
                             if (i == 0) h0[j][k] = hh[j][k];
@@ -842,11 +850,13 @@ __global__ void __launch_bounds__(32 * BwdShape<TI, N, CH>::WT, 1) selscan_bwd_k
                     float ddt = fmaf(x, gb[i], 0.6931471805599453f * ga[i]);   // the rates are a log2(e)
                     if (p.softplus) ddt *= sigmoid_acc(load1(s_raw + TOK * CPW + at) + bias);
                     store1(static_cast<TG *>(q_.d_dt) + o, ddt);
-                    sum_skip = fmaf(dg, x, sum_skip);
-                    sum_bias += ddt;
+                    tile_skip = fmaf(dg, x, tile_skip);
+                    tile_bias += ddt;
                 }
             }
         }
+        compensated(sum_skip, lost_skip, tile_skip);
+        compensated(sum_bias, lost_bias, tile_bias);
         __syncwarp();   // done with the tile's shared memory
         if (tile >= WT) fetch_state(tile - WT);
     }
