@@ -35,6 +35,25 @@ __device__ __forceinline__ int packed_block_seq(const int *off, int S, int T, in
     return lo;
 }
 
+// The sequence with the `rank`-th most tokens, for kernels whose CTAs walk whole sequences: the CTAs that start first get
+// the long ones, so that none of those is left for the end.  Packed sequences only, and no more of them than the CTA has
+// threads (else rank itself: the order of the array).  All threads call it; s_len has blockDim.x + 1 ints.
+__device__ __forceinline__ int seq_by_length(const int *off, int S, int T, int rank, int *s_len)
+{
+    if (!off || S == 1 || S > (int)blockDim.x) return rank;
+    const int tid = threadIdx.x;
+    if (tid < S) s_len[tid] = seq_range(off, tid, S, T).len;
+    __syncthreads();
+    if (tid < S) {
+        const int mine = s_len[tid];
+        int longer = 0;
+        for (int j = 0; j < S; ++j) longer += s_len[j] > mine || (s_len[j] == mine && j < tid);
+        if (longer == rank) s_len[blockDim.x] = tid;
+    }
+    __syncthreads();
+    return s_len[blockDim.x];
+}
+
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float ex2(float x)

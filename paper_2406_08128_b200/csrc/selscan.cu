@@ -113,8 +113,10 @@ __global__ void __launch_bounds__(32 * WT, OCC) selscan_fwd_kernel(const ScanPar
         sr = seq_range(p.off, s, p.S, p.T);
         b = (int)(blk - (sr.start / p.seg + s));
         if (b < 0 || (b > 0 && b * p.seg >= sr.len)) return;
+        if (p.seg_sum && b * p.seg + p.seg >= sr.len) return;   // what a sequence's last segment ends with starts nothing
     } else {
-        s = (int)blk;
+        __shared__ int s_len[32 * WT + 1];
+        s = seq_by_length(p.off, p.S, p.T, (int)blk, s_len);
         sr = seq_range(p.off, s, p.S, p.T);
     }
     const int begin = b * p.seg, end = p.seg ? min(begin + p.seg, sr.len) : sr.len;   // tokens of the sequence
@@ -406,9 +408,10 @@ __global__ void __launch_bounds__(128) selscan_segments_kernel(const ScanParams 
     size_t k = (size_t)(sr.start / p.seg) + s;
     for (int t = 0; t < sr.len; t += p.seg, ++k) {
         float *m = p.seg_state + (k * p.D + ch) * N + n;
-        const float own = *m;
+        const bool more = t + p.seg < sr.len;
+        const float own = more ? *m : 0.f, time = more ? p.seg_sum[k * p.D + ch] : 0.f;
         *m = h;
-        h = fmaf(ex2(a * p.seg_sum[k * p.D + ch]), h, own);
+        h = fmaf(ex2(a * time), h, own);
     }
 }
 
@@ -510,7 +513,8 @@ __global__ void __launch_bounds__(32 * BwdShape<TI, N, CH>::WT, 1) selscan_bwd_k
     float4 *s_down = reinterpret_cast<float4 *>(s_mine + HAND);          // the gradient handed down
 
     const int nblk = (p.D + CPW - 1) / CPW;
-    const int s = blockIdx.x / nblk, cb = blockIdx.x % nblk, c0 = cb * CPW;
+    __shared__ int s_len[32 * WT + 1];
+    const int s = seq_by_length(p.off, p.S, p.T, blockIdx.x / nblk, s_len), cb = blockIdx.x % nblk, c0 = cb * CPW;
     const int q = lane % R, grp = lane / R;
     const int chl = grp * CH + q % CH, ch = c0 + chl, n0 = NS * q;
     const int half = (lane >> 4) * 4;   // of its 8 states, the four that a lane holds first: the lower ones in lanes 0 .. 15
@@ -950,7 +954,7 @@ chela_status_t fwd_launch(ScanParams p, cudaStream_t stream)
     using Sh = FwdShape<TI, N, CH, TOK>;
     constexpr size_t smem = (size_t)WT * Sh::WARP_B;
     const auto kern = selscan_fwd_kernel<TI, TO, N, CH, TOK, WT, OCC>;
-    if (smem > 47 * 1024) {
+    if (smem > 40 * 1024) {   // with the static part, past the 48 KB that need no asking
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return cuda_status(e);
     }
@@ -960,6 +964,7 @@ chela_status_t fwd_launch(ScanParams p, cudaStream_t stream)
     if (p.seg) {
         ScanParams q = p;
         q.y = nullptr;
+        q.c = q.z = nullptr;
         q.ckpt = q.state_out = nullptr;
         kern<<<(unsigned)blocks, 32 * WT, smem, stream>>>(q);
         const long long n = ((long long)p.S * p.D * N + 127) / 128;
