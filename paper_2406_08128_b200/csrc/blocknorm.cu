@@ -4,8 +4,7 @@
 //
 // Bound by HBM: every operand is read once and every result written once; rows stay in registers between the two norms.
 // A lane holds 8 consecutive channels (16 bytes of bf16), WPR warps share a row; sums over a row are fp32 shuffles and, for
-// WPR > 1, one exchange through shared memory.  The next row's operands are loaded while a row is worked on, and the
-// per-channel weights wait in shared memory.  Layer statistics are two-pass (mean first) on the registers, so a large
+// WPR > 1, one exchange through shared memory.  The next row's operands are loaded while a row is worked on.  Layer statistics are two-pass (mean first) on the registers, so a large
 // mean costs no digits.
 #include "packed.cuh"
 
@@ -84,13 +83,6 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *p, const Vec8 &v)
     *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 __device__ __forceinline__ Vec8 fill8(float a) { return Vec8{{a, a, a, a, a, a, a, a}}; }
-// Weights of a lane's channels: from shared memory, row w of [rows][WPR * 256], or, where a row group has one row only and
-// staging would just add its latency, straight from the caller's vector.
-__device__ __forceinline__ Vec8 weight8(bool staged, const float *s_w, int row, int width, int c, bool live, const float *from, float other)
-{
-    if (staged) return load8(s_w + row * width + c);
-    return live && from ? load8(from + c) : fill8(other);
-}
 __device__ __forceinline__ void stage_weight(float *to, const float *from, float other, int D, int width)
 {
     for (int c = threadIdx.x; c < width; c += blockDim.x) to[c] = from && c < D ? from[c] : other;
@@ -152,28 +144,34 @@ struct RowSum {
 
 // ------------------------------------------------------------------------------------------------ forward
 
-template <typename TI, typename TR, typename TO, int WPR>
-__global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 3) blocknorm_fwd_kernel(const NormParams p)
+template <typename TI, typename TR, typename TO, int WPR, bool kBias>
+__global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : (kBias ? 2 : 3)) blocknorm_fwd_kernel(const NormParams p)
 {
-    constexpr int GROUPS = WPR > 8 ? 1 : 8 / WPR, WIDTH = WPR * 256;
+    constexpr int GROUPS = WPR > 8 ? 1 : 8 / WPR;
     __shared__ __align__(16) float2 buf[GROUPS * 2 * WPR];
-    extern __shared__ __align__(16) float s_w[];   // w_post, b_post, scale, w_pre, b_pre [WIDTH], those that are used
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / WPR, wr = warp % WPR;
     RowSum<WPR> sum = {buf, 0, group, wr, lane};
     const float inv_d = 1.f / p.D;
     const int c = 8 * (wr * 32 + lane);
     const bool live = c < p.D, post = p.y != nullptr, pre = p.o != nullptr, gated = p.gate != nullptr;
-    const bool staged = (long long)gridDim.x * GROUPS < p.T;
-    if (post && staged) {
-        stage_weight(s_w, p.w_post, 1.f, p.D, WIDTH);
-        stage_weight(s_w + WIDTH, p.b_post, 0.f, p.D, WIDTH);
-        stage_weight(s_w + 2 * WIDTH, p.scale, 1.f, p.D, WIDTH);
+    // this lane's weights, in registers for all its rows: from shared memory they kept the load pipe 80 % busy.  scale is
+    // folded into the post norm's weight and bias; channels past D get zeros there and stay zero in r'.
+    Vec8 w_post = fill8(0.f), b_post, w_pre = fill8(0.f), b_pre;
+    if (live && post) {
+        const Vec8 sc = p.scale ? load8(p.scale + c) : fill8(1.f);
+        w_post = p.w_post ? load8(p.w_post + c) : fill8(1.f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w_post.v[e] *= sc.v[e];
+        if (kBias) {
+            b_post = p.b_post ? load8(p.b_post + c) : fill8(0.f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) b_post.v[e] *= sc.v[e];
+        }
+    } else if (kBias) {
+        b_post = fill8(0.f);
     }
-    if (pre && staged) {
-        stage_weight(s_w + 3 * WIDTH, p.w_pre, 1.f, p.D, WIDTH);
-        stage_weight(s_w + 4 * WIDTH, p.b_pre, 0.f, p.D, WIDTH);
-    }
-    if (staged) __syncthreads();
+    if (live && pre) w_pre = p.w_pre ? load8(p.w_pre + c) : fill8(1.f);
+    if (kBias) b_pre = live && pre && p.b_pre ? load8(p.b_pre + c) : fill8(0.f);
 
     auto normalise = [&](Vec8 &x, int kind) {
         if (kind == CHELA_NORM_NONE) return;
@@ -217,24 +215,21 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 3) blo
                 }
             }
             normalise(v, p.norm_post);
-            const Vec8 w = weight8(staged, s_w, 0, WIDTH, c, live, p.w_post, 1.f), b = weight8(staged, s_w, 1, WIDTH, c, live, p.b_post, 0.f),
-                       s = weight8(staged, s_w, 2, WIDTH, c, live, p.scale, 1.f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v.v[e] = fmaf(v.v[e], w.v[e], b.v[e]);
+            for (int e = 0; e < 8; ++e) v.v[e] = kBias ? fmaf(v.v[e], w_post.v[e], b_post.v[e]) : v.v[e] * w_post.v[e];
             if (gated && p.gate_after) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v.v[e] *= g.v[e];
-            }
-            const float on = live ? 1.f : 0.f;   // channels past D stay zero for the next norm's sums
+                for (int e = 0; e < 8; ++e) r.v[e] = fmaf(v.v[e], g.v[e], r.v[e]);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) r.v[e] = fmaf(s.v[e] * on, v.v[e], r.v[e]);
+                for (int e = 0; e < 8; ++e) r.v[e] += v.v[e];
+            }
             if (live && p.res_out) store8(static_cast<TR *>(p.res_out) + (size_t)row * p.D + c, r);
         }
         if (pre) {
             normalise(r, p.norm_pre);
-            const Vec8 w = weight8(staged, s_w, 3, WIDTH, c, live, p.w_pre, 1.f), b = weight8(staged, s_w, 4, WIDTH, c, live, p.b_pre, 0.f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) r.v[e] = fmaf(r.v[e], w.v[e], b.v[e]);
+            for (int e = 0; e < 8; ++e) r.v[e] = kBias ? fmaf(r.v[e], w_pre.v[e], b_pre.v[e]) : r.v[e] * w_pre.v[e];
             if (live) store8(static_cast<TO *>(p.o) + (size_t)row * p.D + c, r);
         }
     }
@@ -513,7 +508,7 @@ int row_grid(int T, int D, int per_sm)
     const int g = row_groups(row_warps(D)), need = (int)(((long long)T + g - 1) / g);
     return need < 148 * per_sm ? need : 148 * per_sm;
 }
-constexpr int kFwdPerSm = 3, kBwdPerSm = 2;
+constexpr int kBwdPerSm = 2;
 
 template <typename K, typename P>
 chela_status_t norm_launch(K kern, const P &p, int grid, int threads, size_t smem, cudaStream_t stream)
@@ -526,19 +521,24 @@ chela_status_t norm_launch(K kern, const P &p, int grid, int threads, size_t sme
     return last_launch_status();
 }
 
+template <typename TI, typename TR, typename TO, bool kBias>
+chela_status_t fwd_bias(const NormParams &p, cudaStream_t stream)
+{
+    const int wpr = row_warps(p.D), grid = row_grid(p.T, p.D, kBias ? 2 : 3);
+    switch (wpr) {
+    case 1: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 1, kBias>, p, grid, 256, 0, stream);
+    case 2: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 2, kBias>, p, grid, 256, 0, stream);
+    case 4: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 4, kBias>, p, grid, 256, 0, stream);
+    case 8: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 8, kBias>, p, grid, 256, 0, stream);
+    case 16: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 16, kBias>, p, grid, 512, 0, stream);
+    default: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 32, kBias>, p, grid, 1024, 0, stream);
+    }
+}
+
 template <typename TI, typename TR, typename TO>
 chela_status_t fwd_d(const NormParams &p, cudaStream_t stream)
 {
-    const int wpr = row_warps(p.D), grid = row_grid(p.T, p.D, kFwdPerSm);
-    const size_t smem = (size_t)5 * wpr * 256 * 4;
-    switch (wpr) {
-    case 1: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 1>, p, grid, 256, smem, stream);
-    case 2: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 2>, p, grid, 256, smem, stream);
-    case 4: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 4>, p, grid, 256, smem, stream);
-    case 8: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 8>, p, grid, 256, smem, stream);
-    case 16: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 16>, p, grid, 512, smem, stream);
-    default: return norm_launch(blocknorm_fwd_kernel<TI, TR, TO, 32>, p, grid, 1024, smem, stream);
-    }
+    return p.b_post || p.b_pre ? fwd_bias<TI, TR, TO, true>(p, stream) : fwd_bias<TI, TR, TO, false>(p, stream);
 }
 
 template <typename TI, typename TR, typename TG>

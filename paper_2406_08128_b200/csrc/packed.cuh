@@ -155,4 +155,13 @@ __device__ __forceinline__ void copy16(void *dst, const void *src, bool ok)
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
 
+// Four elements (8 or 16 bytes) of one lane, asynchronously; zeros where ok is false.  The lane that copied reads them.
+template <typename T>
+__device__ __forceinline__ void copy_raw4(Raw4<T> *dst, const T *src, bool ok)
+{
+    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+    if (sizeof(T) == 4) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(ok ? 16 : 0) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(d), "l"(src), "r"(ok ? 8 : 0) : "memory");
+}
+
 }  // namespace chela

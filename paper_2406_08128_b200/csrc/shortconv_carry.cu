@@ -95,12 +95,15 @@ __device__ __forceinline__ void split_item(long long item, long long items, int 
 }
 
 // W: taps held in registers (the width itself up to 4; 8 and 16 for the widths up to those, their extra taps zero).
-// kTok tokens in groups of SUB whose loads are in flight while the group before is computed: with four loads a thread the
-// kernel reached 29 % of the measured HBM rate (65536 x 1024, bf16).
+// The tokens of a work item are copied to shared memory in groups of SUB, two groups ahead of the arithmetic, every thread
+// the 8 or 16 bytes that it will use itself: nothing but its own copies has to be waited for, and the loads in flight
+// cost no registers.  (65536 x 1024, bf16: four loads a thread in registers 140 us, eight 68 us.)
 template <typename T, int W>
-__global__ void __launch_bounds__(256, W <= 4 ? (sizeof(T) == 2 ? 4 : 3) : 1) conv_carry_kernel(const ConvParams p, long long items)
+__global__ void __launch_bounds__(256, W <= 4 ? 3 : 1) conv_carry_kernel(const ConvParams p, long long items)
 {
-    constexpr int SUB = 4;
+    constexpr int SUB = 8;
+    extern __shared__ __align__(16) unsigned char smem[];
+    Raw4<T> *ring = reinterpret_cast<Raw4<T> *>(smem) + threadIdx.x;   // [2][SUB][256]
     const int nvec = p.D / 4;
     for (long long idx = blockIdx.x * (long long)blockDim.x + threadIdx.x; idx < items; idx += (long long)gridDim.x * blockDim.x) {
         long long blk;
@@ -115,30 +118,28 @@ __global__ void __launch_bounds__(256, W <= 4 ? (sizeof(T) == 2 ? 4 : 3) : 1) co
             const int end = min(t0 + kTok, sr.len);
             const T *px = static_cast<const T *>(p.x) + (size_t)(sr.start + t0) * p.xs + c;
             T *py = static_cast<T *>(p.y) + (size_t)(sr.start + t0) * p.D + c;
-            Raw4<T> raw[SUB];
-            auto fetch = [&](int t) {
+            auto fetch = [&](int t, int half) {
 #pragma unroll
-                for (int i = 0; i < SUB; ++i)
-                    if (t + i < end) raw[i].load(px + (size_t)i * p.xs); else raw[i].zero();
-                px += (size_t)SUB * p.xs;
+                for (int i = 0; i < SUB; ++i) copy_raw4(ring + (half * SUB + i) * 256, t + i < end ? px + (size_t)i * p.xs : px, t + i < end);
+                px += t + SUB < end ? (size_t)SUB * p.xs : 0;
+                asm volatile("cp.async.commit_group;" ::: "memory");
             };
-            fetch(t0);
+            fetch(t0, 0);
+            fetch(t0 + SUB, 1);
             float4 taps[W], in[W];   // in[j] = x_{t-j}
             load_taps<W>(p.w, p.width, c, taps);
             const float4 bias = p.bias ? load4(p.bias + c) : zero4();
 #pragma unroll
             for (int j = 1; j < W; ++j) in[j - 1] = row_at<T>(p, s, sr.start, sr.len, t0 - j, c);
+            int half = 0;
 #pragma unroll 1
             for (int t = t0; t < end; t += SUB) {
-                Raw4<T> cur[SUB];
-#pragma unroll
-                for (int i = 0; i < SUB; ++i) cur[i] = raw[i];
-                if (t + SUB < end) fetch(t + SUB);
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
 #pragma unroll
                 for (int i = 0; i < SUB; ++i) {
 #pragma unroll
                     for (int j = W - 1; j > 0; --j) in[j] = in[j - 1];
-                    in[0] = cur[i].get();
+                    in[0] = ring[(half * SUB + i) * 256].get();
                     float4 u = bias;
 #pragma unroll
                     for (int j = 0; j < W; ++j) u = fma4(taps[j], in[j], u);
@@ -146,7 +147,10 @@ __global__ void __launch_bounds__(256, W <= 4 ? (sizeof(T) == 2 ? 4 : 3) : 1) co
                     if (t + i < end) store4(py + (size_t)i * p.D, u);
                 }
                 py += (size_t)SUB * p.D;
+                fetch(t + 2 * SUB, half);
+                half ^= 1;
             }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
         }
         if (b == 0 && p.state_out) store_state<T>(p, s, sr, c);
     }
@@ -193,13 +197,15 @@ struct ConvBwdParams {
 
 // A CTA: 32 lanes x 4 channels, 8 warps that walk work items of kBwdTok tokens; the taps' gradients stay in registers until
 // the end, are added over the warps in shared memory and leave as one partial sum per CTA row (a fixed order, no atomics).
-// d_x_t = sum_j w_j d_u_{t+j}: a thread evaluates the d_u of its tokens and of the W - 1 behind them.  x and d_y of SUB
-// tokens are in flight while the SUB before are computed.
+// d_x_t = sum_j w_j d_u_{t+j}: a thread evaluates the d_u of its tokens and of the W - 1 behind them.  x and d_y are
+// copied to shared memory two groups of SUB tokens ahead, as in the forward kernel.
 template <typename T, typename TG, int W>
 __global__ void __launch_bounds__(256, W <= 4 ? 2 : 1) conv_bwd_kernel(const ConvBwdParams q, long long nblocks)
 {
-    constexpr int SUB = W <= 4 ? 4 : 2;
+    constexpr int SUB = 4;
     const ConvParams &p = q.f;
+    extern __shared__ __align__(16) unsigned char smem[];
+    Raw4<T> *ring = reinterpret_cast<Raw4<T> *>(smem) + threadIdx.x;   // [2][SUB][x, d_y][256]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = (blockIdx.x * 32 + lane) * 4;
     const bool live = c < p.D;
@@ -217,22 +223,22 @@ __global__ void __launch_bounds__(256, W <= 4 ? 2 : 1) conv_bwd_kernel(const Con
             const int end = min(t0 + kBwdTok, sr.len), stop = end + W - 1;
             const T *px = static_cast<const T *>(p.x) + (size_t)(sr.start + t0) * p.xs + c;
             const T *pd = static_cast<const T *>(q.dy) + (size_t)(sr.start + t0) * q.dys + c;
-            Raw4<T> rx[SUB], rd[SUB];
-            auto fetch = [&](int t) {
+            const int last = min(sr.len, stop);   // d_u is zero behind the sequence
+            auto fetch = [&](int t, int half) {
 #pragma unroll
                 for (int i = 0; i < SUB; ++i) {
-                    if (t + i < sr.len && t + i < stop) {
-                        rx[i].load(px + (size_t)i * p.xs);
-                        rd[i].load(pd + (size_t)i * q.dys);
-                    } else {
-                        rx[i].zero();
-                        rd[i].zero();   // d_u is zero behind the sequence
-                    }
+                    const bool ok = t + i < last;
+                    Raw4<T> *to = ring + (half * SUB + i) * 512;
+                    copy_raw4(to, ok ? px + (size_t)i * p.xs : px, ok);
+                    copy_raw4(to + 256, ok ? pd + (size_t)i * q.dys : pd, ok);
                 }
-                px += (size_t)SUB * p.xs;
-                pd += (size_t)SUB * q.dys;
+                px += t + SUB < last ? (size_t)SUB * p.xs : 0;
+                pd += t + SUB < last ? (size_t)SUB * q.dys : 0;
+                asm volatile("cp.async.commit_group;" ::: "memory");
             };
-            fetch(t0);
+            fetch(t0, 0);
+            fetch(t0 + SUB, 1);
+            int half = 0;
             float4 in[W], du[W];   // in[j] = x_{t-j}; du[j] = d_u_{t-j}
 #pragma unroll
             for (int j = 0; j < W; ++j) du[j] = zero4();
@@ -240,13 +246,7 @@ __global__ void __launch_bounds__(256, W <= 4 ? 2 : 1) conv_bwd_kernel(const Con
             for (int j = 1; j < W; ++j) in[j - 1] = row_at<T>(p, s, sr.start, sr.len, t0 - j, c);
 #pragma unroll 1
             for (int tg = t0; tg < stop; tg += SUB) {
-                Raw4<T> cx[SUB], cd[SUB];
-#pragma unroll
-                for (int i = 0; i < SUB; ++i) {
-                    cx[i] = rx[i];
-                    cd[i] = rd[i];
-                }
-                if (tg + SUB < stop) fetch(tg + SUB);
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
 #pragma unroll
                 for (int i = 0; i < SUB; ++i) {
                     const int t = tg + i;
@@ -255,8 +255,8 @@ __global__ void __launch_bounds__(256, W <= 4 ? 2 : 1) conv_bwd_kernel(const Con
                         in[j] = in[j - 1];
                         du[j] = du[j - 1];
                     }
-                    in[0] = cx[i].get();
-                    float4 d = cd[i].get();
+                    in[0] = ring[(half * SUB + i) * 512].get();
+                    float4 d = ring[(half * SUB + i) * 512 + 256].get();
                     if (p.act) {
                         float4 u = bias;
 #pragma unroll
@@ -280,7 +280,10 @@ __global__ void __launch_bounds__(256, W <= 4 ? 2 : 1) conv_bwd_kernel(const Con
                         store4(static_cast<TG *>(q.d_x) + (size_t)(sr.start + tx) * p.D + c, dx);
                     }
                 }
+                fetch(tg + 2 * SUB, half);
+                half ^= 1;
             }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
         }
     }
     if (!q.part) return;
@@ -365,21 +368,32 @@ int conv_bwd_rows(int T, int D)
     return want < most ? want : (most < 1 ? 1 : most);
 }
 
+template <typename T, int W>
+chela_status_t fwd_launch(const ConvParams &p, cudaStream_t stream)
+{
+    constexpr size_t smem = 2 * 8 * 256 * sizeof(Raw4<T>);
+    const auto kern = conv_carry_kernel<T, W>;
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return cuda_status(e);
+    }
+    const long long items = (long long)packed_blocks(p.T, p.S, kTok) * (p.D / 4);
+    const long long need = (items + 255) / 256;
+    kern<<<(unsigned)(need < 148 * 64 ? need : 148 * 64), 256, smem, stream>>>(p, items);
+    return last_launch_status();
+}
+
 template <typename T>
 chela_status_t fwd_w(const ConvParams &p, cudaStream_t stream)
 {
-    const long long items = (long long)packed_blocks(p.T, p.S, kTok) * (p.D / 4);
-    const long long need = (items + 255) / 256;
-    const unsigned grid = (unsigned)(need < 148 * 64 ? need : 148 * 64);
     switch (p.width) {
-    case 1: conv_carry_kernel<T, 1><<<grid, 256, 0, stream>>>(p, items); break;
-    case 2: conv_carry_kernel<T, 2><<<grid, 256, 0, stream>>>(p, items); break;
-    case 3: conv_carry_kernel<T, 3><<<grid, 256, 0, stream>>>(p, items); break;
-    case 4: conv_carry_kernel<T, 4><<<grid, 256, 0, stream>>>(p, items); break;
-    case 5: case 6: case 7: case 8: conv_carry_kernel<T, 8><<<grid, 256, 0, stream>>>(p, items); break;
-    default: conv_carry_kernel<T, 16><<<grid, 256, 0, stream>>>(p, items); break;
+    case 1: return fwd_launch<T, 1>(p, stream);
+    case 2: return fwd_launch<T, 2>(p, stream);
+    case 3: return fwd_launch<T, 3>(p, stream);
+    case 4: return fwd_launch<T, 4>(p, stream);
+    case 5: case 6: case 7: case 8: return fwd_launch<T, 8>(p, stream);
+    default: return fwd_launch<T, 16>(p, stream);
     }
-    return last_launch_status();
 }
 
 template <typename T>
@@ -406,15 +420,24 @@ chela_status_t bwd_w(const ConvBwdParams &q, float *d_w, float *d_bias, cudaStre
     const long long nblocks = (long long)packed_blocks(p.T, p.S, kBwdTok);
     const int rows = conv_bwd_rows(p.T, p.D);
     const dim3 grid((p.D / 4 + 31) / 32, rows);
+    constexpr size_t smem = 2 * 4 * 2 * 256 * sizeof(Raw4<T>);
+    auto launch = [&](auto kern) {
+        if (smem > 40 * 1024) {   // with the static part, past the 48 KB that need no asking
+            const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e != cudaSuccess) return cuda_status(e);
+        }
+        kern<<<grid, 256, smem, stream>>>(q, nblocks);
+        return last_launch_status();
+    };
+    chela_status_t st;
     switch (p.width) {
-    case 1: conv_bwd_kernel<T, TG, 1><<<grid, 256, 0, stream>>>(q, nblocks); break;
-    case 2: conv_bwd_kernel<T, TG, 2><<<grid, 256, 0, stream>>>(q, nblocks); break;
-    case 3: conv_bwd_kernel<T, TG, 3><<<grid, 256, 0, stream>>>(q, nblocks); break;
-    case 4: conv_bwd_kernel<T, TG, 4><<<grid, 256, 0, stream>>>(q, nblocks); break;
-    case 5: case 6: case 7: case 8: conv_bwd_kernel<T, TG, 8><<<grid, 256, 0, stream>>>(q, nblocks); break;
-    default: conv_bwd_kernel<T, TG, 16><<<grid, 256, 0, stream>>>(q, nblocks); break;
+    case 1: st = launch(conv_bwd_kernel<T, TG, 1>); break;
+    case 2: st = launch(conv_bwd_kernel<T, TG, 2>); break;
+    case 3: st = launch(conv_bwd_kernel<T, TG, 3>); break;
+    case 4: st = launch(conv_bwd_kernel<T, TG, 4>); break;
+    case 5: case 6: case 7: case 8: st = launch(conv_bwd_kernel<T, TG, 8>); break;
+    default: st = launch(conv_bwd_kernel<T, TG, 16>); break;
     }
-    chela_status_t st = last_launch_status();
     if (st == CHELA_OK && q.part) {
         conv_bwd_sum_kernel<<<dim3((p.D + 31) / 32, p.width + 1), 256, 0, stream>>>(q.part, d_w, d_bias, rows, p.D, p.width);
         st = last_launch_status();
