@@ -417,38 +417,50 @@ __global__ void __launch_bounds__(128) selscan_segments_kernel(const ScanParams 
 
 // ------------------------------------------------------------------------------------------------ single token
 
+// A lane has 8 states of one channel: two 16-byte loads of the state are in flight, which is what this kernel is about
+// (the state is read and written once, 8 bytes of traffic an element against 2 for everything else).
 template <typename TI, typename TO, int N>
 __global__ void __launch_bounds__(256) selscan_step_kernel(const ScanParams p)
 {
-    constexpr int R = N / 4;
+    constexpr int R = N / 8;
     const size_t idx = blockIdx.x * (size_t)blockDim.x + threadIdx.x;
     const size_t row_ch = idx / R;
     const int r = (int)(idx % R);
     const bool live = row_ch < (size_t)p.S * p.D;
     const int s = live ? (int)(row_ch / p.D) : 0, ch = live ? (int)(row_ch % p.D) : 0;
     const int g = p.G == 1 ? 0 : ch / (p.D / p.G);
-    const size_t st = ((size_t)s * p.D + ch) * N + 4 * r;
-    const float4 h = *reinterpret_cast<const float4 *>(p.state_in + st);
-    const float4 a = *reinterpret_cast<const float4 *>(p.a + (size_t)ch * N + 4 * r);
-    const float4 b = load4(static_cast<const TI *>(p.b) + (size_t)s * p.bs + g * N + 4 * r);
-    const float4 c = load4(static_cast<const TI *>(p.c) + (size_t)s * p.cs + g * N + 4 * r);
+    const size_t st = ((size_t)s * p.D + ch) * N + 8 * r;
+    const size_t wt = (size_t)ch * N + 8 * r, bt = (size_t)s * p.bs + g * N + 8 * r, ct = (size_t)s * p.cs + g * N + 8 * r;
+    float4 h[2], a[2], b[2], c[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        h[k] = *reinterpret_cast<const float4 *>(p.state_in + st + 4 * k);
+        a[k] = *reinterpret_cast<const float4 *>(p.a + wt + 4 * k);
+        b[k] = load4(static_cast<const TI *>(p.b) + bt + 4 * k);
+        c[k] = load4(static_cast<const TI *>(p.c) + ct + 4 * k);
+    }
     const float x = load1(static_cast<const TI *>(p.x) + (size_t)s * p.xs + ch);
     float dt = load1(static_cast<const TI *>(p.dt) + (size_t)s * p.dts + ch) + (p.bias ? p.bias[ch] : 0.f);
+    const float z = p.z ? load1(static_cast<const TI *>(p.z) + (size_t)s * p.zs + ch) : 0.f, skip = p.dsk ? p.dsk[ch] : 0.f;
     if (p.softplus) dt = softplus_acc(dt);
     const float dx = dt * x;
-    float4 n;
-    n.x = fmaf(ex2(fmaf(dt, decay_rate(a.x), kDecayShift)), h.x, dx * b.x);
-    n.y = fmaf(ex2(fmaf(dt, decay_rate(a.y), kDecayShift)), h.y, dx * b.y);
-    n.z = fmaf(ex2(fmaf(dt, decay_rate(a.z), kDecayShift)), h.z, dx * b.z);
-    n.w = fmaf(ex2(fmaf(dt, decay_rate(a.w), kDecayShift)), h.w, dx * b.w);
-    float y = fmaf(c.x, n.x, c.y * n.y) + fmaf(c.z, n.z, c.w * n.w);
+    float y = 0.f;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        h[k].x = fmaf(ex2(fmaf(dt, decay_rate(a[k].x), kDecayShift)), h[k].x, dx * b[k].x);
+        h[k].y = fmaf(ex2(fmaf(dt, decay_rate(a[k].y), kDecayShift)), h[k].y, dx * b[k].y);
+        h[k].z = fmaf(ex2(fmaf(dt, decay_rate(a[k].z), kDecayShift)), h[k].z, dx * b[k].z);
+        h[k].w = fmaf(ex2(fmaf(dt, decay_rate(a[k].w), kDecayShift)), h[k].w, dx * b[k].w);
+        y += fmaf(c[k].x, h[k].x, c[k].y * h[k].y) + fmaf(c[k].z, h[k].z, c[k].w * h[k].w);
+    }
 #pragma unroll
     for (int o = 1; o < R; o <<= 1) y += __shfl_xor_sync(0xffffffffu, y, o);
     if (!live) return;
-    *reinterpret_cast<float4 *>(p.state_out + st) = n;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) *reinterpret_cast<float4 *>(p.state_out + st + 4 * k) = h[k];
     if (r == 0) {
-        y = fmaf(p.dsk ? p.dsk[ch] : 0.f, x, y);
-        if (p.z) y *= gate_f(load1(static_cast<const TI *>(p.z) + (size_t)s * p.zs + ch));
+        y = fmaf(skip, x, y);
+        if (p.z) y *= gate_f(z);
         store1(static_cast<TO *>(p.y) + (size_t)s * p.D + ch, y);
     }
 }
@@ -924,14 +936,21 @@ __global__ void __launch_bounds__(256) selscan_bc_kernel(const float *part, void
     }
 }
 
-// sums over the sequences: out[i] = sum_s part[s * stride + i]
-__global__ void __launch_bounds__(256) sum_rows_kernel(const float *part, float *out, int S, size_t stride, size_t n)
+// The parameters' gradients: sums over the sequences of part_a and part_d, the former's elements first
+__global__ void __launch_bounds__(256) selscan_sum_kernel(const float *part_a, const float *part_d, float *d_a, float *d_skip, float *d_bias, int S,
+                                                          int D, int N)
 {
-    const size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x;
-    if (i >= n) return;
+    const size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x, na = (size_t)D * N;
+    if (i >= na + 2 * (size_t)D) return;
+    const bool in_a = i < na;
+    const size_t k = in_a ? i : i - na;   // for the rest [skip | bias][D]
+    float *out = in_a ? d_a + k : (k < (size_t)D ? (d_skip ? d_skip + k : nullptr) : (d_bias ? d_bias + (k - D) : nullptr));
+    if (!out) return;
+    const float *part = in_a ? part_a : part_d;
+    const size_t stride = in_a ? na : 2 * (size_t)D;
     float o = 0.f;
-    for (int s = 0; s < S; ++s) o += part[(size_t)s * stride + i];
-    out[i] = o;
+    for (int s = 0; s < S; ++s) o += part[(size_t)s * stride + k];
+    *out = o;
 }
 
 // ------------------------------------------------------------------------------------------------ launches
@@ -996,7 +1015,7 @@ chela_status_t fwd_n(const ScanParams &p, int N, cudaStream_t stream)
 template <typename TI, typename TO>
 chela_status_t step_n(const ScanParams &p, int N, cudaStream_t stream)
 {
-    const size_t threads = (size_t)p.S * p.D * (N / 4);
+    const size_t threads = (size_t)p.S * p.D * (N / 8);
     const size_t blocks = (threads + 255) / 256;
     if (blocks > 0x7fffffffULL) return CHELA_ERR_UNSUPPORTED;
     switch (N) {
@@ -1028,14 +1047,10 @@ chela_status_t bwd_launch(const ScanBwdParams &q, void *d_b, void *d_c, float *d
     const size_t grid = (items + 255) / 256;
     selscan_bc_kernel<TG, N><<<(unsigned)(grid < 148 * 32 ? grid : 148 * 32), 256, 0, stream>>>(q.part_bc, d_b, d_c, p.off, p.S, p.T, p.G, nblk / p.G);
     st = last_launch_status();
-    auto rows = [&](const float *part, float *out, size_t stride, size_t n) {
-        if (st != CHELA_OK || !out) return;
-        sum_rows_kernel<<<(unsigned)((n + 255) / 256), 256, 0, stream>>>(part, out, p.S, stride, n);
+    if (st == CHELA_OK) {
+        selscan_sum_kernel<<<(unsigned)(((size_t)p.D * (N + 2) + 255) / 256), 256, 0, stream>>>(q.part_a, q.part_d, d_a, d_skip, d_bias, p.S, p.D, N);
         st = last_launch_status();
-    };
-    rows(q.part_a, d_a, (size_t)p.D * N, (size_t)p.D * N);
-    rows(q.part_d, d_skip, (size_t)2 * p.D, p.D);
-    rows(q.part_d + p.D, d_bias, (size_t)2 * p.D, p.D);
+    }
     return st;
 }
 
