@@ -6,6 +6,7 @@ using namespace chela;
 namespace {
 
 constexpr int kNormMaxD = 8192;
+constexpr int kMaxTokens = 0x7fffffff - 4095;   // token positions and the slices past the last one stay within int
 
 bool dtype_ok(chela_dtype_t t) { return t == CHELA_F32 || t == CHELA_BF16; }
 // token stride of an operand whose row has n elements
@@ -16,7 +17,7 @@ chela_status_t check_seqs(const int *seq_offsets, int S, int T)
     if (S < 1 || T < 1) return CHELA_ERR_INVALID_ARG;
     if (!seq_offsets && T % S != 0) return CHELA_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(seq_offsets) & 3u) return CHELA_ERR_INVALID_ARG;
-    return CHELA_OK;
+    return T <= kMaxTokens ? CHELA_OK : CHELA_ERR_UNSUPPORTED;
 }
 
 chela_status_t check_conv(const void *x, long long x_stride, const float *w, const float *bias, const void *state_in,
@@ -60,7 +61,7 @@ chela_status_t check_norm(const chela_blocknorm_args_t *a)
     const void *ptrs[] = {a->res, a->y, a->gate, a->w_post, a->b_post, a->scale, a->w_pre, a->b_pre};
     for (const void *p : ptrs)
         if (!aligned16(p)) return CHELA_ERR_INVALID_ARG;
-    if (a->D % 8 != 0 || a->D > kNormMaxD) return CHELA_ERR_UNSUPPORTED;
+    if (a->D % 8 != 0 || a->D > kNormMaxD || a->T > kMaxTokens) return CHELA_ERR_UNSUPPORTED;
     if ((a->res && !stride_ok(a->res_stride, a->D)) || (a->y && !stride_ok(a->y_stride, a->D)) ||
         (a->gate && !stride_ok(a->gate_stride, a->D)))
         return CHELA_ERR_INVALID_ARG;

@@ -144,7 +144,9 @@ __global__ void __launch_bounds__(32 * WT, OCC) selscan_fwd_kernel(const ScanPar
         const int cj = ch ^ j;   // pairs of channels start at even ones, so the neighbour is ch ^ 1
         const bool ok = cj < p.D;
         const size_t at = (size_t)cj * N + n0;
-        const float *init = p.seg_sum ? nullptr : (b > 0 ? p.seg_state + (size_t)blk * p.D * N : (p.state_in ? p.state_in + (size_t)s * p.D * N : nullptr));
+        // (a segment takes its state from seg_state, the first one too: state_in may be the buffer that the last one writes)
+        const float *init = p.seg_sum ? nullptr : (p.seg && sr.len > 0 ? p.seg_state + (size_t)blk * p.D * N
+                                                                       : (p.state_in ? p.state_in + (size_t)s * p.D * N : nullptr));
 #pragma unroll
         for (int k = 0; k < NP; k += 2) {
             float4 av = zero4(), hv = zero4();
@@ -424,10 +426,12 @@ __global__ void __launch_bounds__(256) selscan_step_kernel(const ScanParams p)
 {
     constexpr int R = N / 8;
     const size_t idx = blockIdx.x * (size_t)blockDim.x + threadIdx.x;
-    const size_t row_ch = idx / R;
+    const size_t row_ch = idx / R, all = (size_t)p.S * p.D;
     const int r = (int)(idx % R);
-    const bool live = row_ch < (size_t)p.S * p.D;
-    const int s = live ? (int)(row_ch / p.D) : 0, ch = live ? (int)(row_ch % p.D) : 0;
+    const bool live = row_ch < all;
+    // 32-bit division where that is enough
+    const int s = !live ? 0 : (all <= 0x7fffffffu ? (int)((unsigned)row_ch / (unsigned)p.D) : (int)(row_ch / p.D));
+    const int ch = live ? (int)(row_ch - (size_t)s * p.D) : 0;
     const int g = p.G == 1 ? 0 : ch / (p.D / p.G);
     const size_t st = ((size_t)s * p.D + ch) * N + 8 * r;
     const size_t wt = (size_t)ch * N + 8 * r, bt = (size_t)s * p.bs + g * N + 8 * r, ct = (size_t)s * p.cs + g * N + 8 * r;

@@ -46,7 +46,7 @@ def test_short_convolution_refusals(lib):
     assert fwd(S=0) == fwd(T=0) == fwd(D=0) == fwd(W=0) == fwd(act=2) == fwd(dt=2) == bad
     assert fwd(T=7) == bad                      # no offsets: T must be a multiple of S
     assert fwd(xs=56) == fwd(xs=68) == bad      # shorter than a row, not a multiple of 8
-    assert fwd(D=60) == fwd(W=17) == chela.ERR_UNSUPPORTED
+    assert fwd(D=60) == fwd(W=17) == fwd(S=1, T=2 ** 31 - 4000) == chela.ERR_UNSUPPORTED
     assert lib.chela_shortconv_step(one, 64, one, null, two, null, two, 2, 64, 4, 1, 1, null) == bad
     assert lib.chela_shortconv_step(one, 64, one, null, two, one, null, 2, 64, 4, 1, 1, null) == bad
 

@@ -281,6 +281,38 @@ def test_scan_segments_and_steps_continue_a_prompt():
     close(state, to_numpy(last), mag_s, 2 * (L + 8) * 2.0 ** -21)
 
 
+@pytest.mark.parametrize("dtype,N,D,G", [("f32", 16, 40, 1), ("bf16", 8, 24, 1), ("bf16", 64, 64, 2), ("f32", 32, 72, 1)])
+@pytest.mark.parametrize("lengths", [[2003], [1500, 0, 701, 1], [640, 640]], ids=str)
+def test_scan_of_few_long_sequences_is_split(dtype, N, D, G, lengths):
+    """So few chains that the sequences are cut into segments: outputs, states (carried in place), checkpoints."""
+    import torch
+    T, S = sum(lengths), len(lengths)
+    form = FORMS[0]
+    v = scan_inputs(T + N, lengths, D, N, G, dtype)
+    split = chela.lib().chela_selscan_workspace_bytes(T, S, D, N) > 0
+    assert split == (T // S >= 512)
+    args, kw = scan_call(v, lengths, dtype, form, 8)
+    want, want_s = scan_ref(v, lengths, form)
+    mag, mag_s = scan_ref(v, lengths, form, mag=True)
+    tol = (max(lengths) + 8) * 2.0 ** -21
+    state = kw.pop("state_in")
+    given = state.clone()
+    ckpt = chela.selscan_checkpoints(T, S, D, N, "cuda")
+    y, last = chela.selscan_fwd(*args, **kw, state_in=state, state_out=state, checkpoints=ckpt)
+    assert last is state
+    close(y, want, mag, tol, dtype)
+    close(last, want_s, mag_s, tol)
+    dy = dev(v["d_y"], dtype, 8)
+    g1 = chela.selscan_bwd(*args, dy, **kw, state_in=given, checkpoints=ckpt, want_d_state=True)
+    g2 = chela.selscan_bwd(*args, dy, **kw, state_in=given, want_d_state=True)
+    for p, q in zip(g1, g2):
+        assert torch.equal(p, q)
+    form_v = dict(v, d_state_out=np.zeros_like(v["d_state_out"]))
+    r, m = scan_ref(form_v, lengths, form, bwd=True), scan_ref(form_v, lengths, form, mag=True, bwd=True)
+    for k, more in (("d_x", 0), ("d_dt", 0), ("d_z", 0), ("d_b", D // G), ("d_c", D // G), ("d_a", T), ("d_skip", T), ("d_dt_bias", T), ("d_state_in", 0)):
+        close(getattr(g1, k), r[k], m[k], 2 * tol + more * 2.0 ** -24)
+
+
 def test_scan_keeps_what_is_not_finite_where_it_is():
     """NaN and infinities of one sequence stay in it; an infinitely fast decay forgets the state and nothing else."""
     lengths, D, N = [20, 33, 9], 16, 16
