@@ -4,6 +4,8 @@
 // Bound by HBM: 2 bytes in and 2 out per bf16 element for 2 width flops.  A thread owns 4 channels (one 8-byte access
 // for bf16, a warp reads 256 contiguous bytes of a token) and kTok consecutive tokens of one sequence with the taps and the
 // previous inputs in registers, so every input is read once plus a halo of width - 1 rows per kTok.
+#include <type_traits>
+
 #include "packed.cuh"
 
 namespace chela {
@@ -244,9 +246,11 @@ __global__ void __launch_bounds__(256, W <= 4 ? 2 : 1) conv_bwd_kernel(const Con
             for (int j = 0; j < W; ++j) du[j] = zero4();
 #pragma unroll
             for (int j = 1; j < W; ++j) in[j - 1] = row_at<T>(p, s, sr.start, sr.len, t0 - j, c);
-#pragma unroll 1
-            for (int tg = t0; tg < stop; tg += SUB) {
-                asm volatile("cp.async.wait_group 1;" ::: "memory");
+            TG *pdx = static_cast<TG *>(q.d_x) + (size_t)(sr.start + t0) * p.D + c;   // of position tg
+            // kEdge: some of the group's tokens, or of the positions whose d_x they complete, lie outside the work item or
+            // pass a gradient on from state_out
+            auto group = [&](auto edge, int tg) {
+                constexpr bool kEdge = decltype(edge)::value;
 #pragma unroll
                 for (int i = 0; i < SUB; ++i) {
                     const int t = tg + i;
@@ -263,23 +267,34 @@ __global__ void __launch_bounds__(256, W <= 4 ? 2 : 1) conv_bwd_kernel(const Con
                         for (int j = 0; j < W; ++j) u = fma4(taps[j], in[j], u);
                         d = make_float4(d.x * d_silu(u.x), d.y * d_silu(u.y), d.z * d_silu(u.z), d.w * d_silu(u.w));
                     }
-                    du[0] = t < sr.len ? d : zero4();
-                    if (t < end) {
+                    du[0] = !kEdge || t < sr.len ? d : zero4();
+                    if (!kEdge || t < end) {
 #pragma unroll
                         for (int j = 0; j < W; ++j) dw[j] = fma4(du[0], in[j], dw[j]);
                         db = add4(db, du[0]);
                     }
                     const int tx = t - (W - 1);   // all terms of d_x at this position are there now
-                    if (tx >= t0 && tx < end) {
+                    if (!kEdge || (tx >= t0 && tx < end)) {
                         float4 dx = zero4();
 #pragma unroll
                         for (int j = 0; j < W; ++j) dx = fma4(taps[j], du[W - 1 - j], dx);
-                        const int r = tx - (sr.len - (p.width - 1));
-                        if (q.d_state_out && r >= 0)
-                            dx = add4(dx, load4(static_cast<const T *>(q.d_state_out) + ((size_t)s * (p.width - 1) + r) * p.D + c));
-                        store4(static_cast<TG *>(q.d_x) + (size_t)(sr.start + tx) * p.D + c, dx);
+                        if (kEdge) {
+                            const int r = tx - (sr.len - (p.width - 1));
+                            if (q.d_state_out && r >= 0)
+                                dx = add4(dx, load4(static_cast<const T *>(q.d_state_out) + ((size_t)s * (p.width - 1) + r) * p.D + c));
+                        }
+                        store4(pdx + (long long)(i - (W - 1)) * p.D, dx);
                     }
                 }
+            };
+#pragma unroll 1
+            for (int tg = t0; tg < stop; tg += SUB) {
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+                if (tg >= t0 + W - 1 && tg + SUB <= end && (!q.d_state_out || tg + SUB <= sr.len - p.width))
+                    group(std::false_type(), tg);
+                else
+                    group(std::true_type(), tg);
+                pdx += (size_t)SUB * p.D;
                 fetch(tg + 2 * SUB, half);
                 half ^= 1;
             }
