@@ -99,11 +99,12 @@ __device__ __forceinline__ void split_item(long long item, long long items, int 
 // W: taps held in registers (the width itself up to 4; 8 and 16 for the widths up to those, their extra taps zero).
 // The tokens of a work item are copied to shared memory in groups of SUB, two groups ahead of the arithmetic, every thread
 // the 8 or 16 bytes that it will use itself: nothing but its own copies has to be waited for, and the loads in flight
-// cost no registers.  (65536 x 1024, bf16: four loads a thread in registers 140 us, eight 68 us.)
+// cost no registers.  (65536 x 1024, bf16: four loads a thread in registers 140 us, eight 68 us, this way 58 us; groups of
+// eight or two CTAs an SM 64 and 68 us.)
 template <typename T, int W>
 __global__ void __launch_bounds__(256, W <= 4 ? 3 : 1) conv_carry_kernel(const ConvParams p, long long items)
 {
-    constexpr int SUB = 8;
+    constexpr int SUB = 4;
     extern __shared__ __align__(16) unsigned char smem[];
     Raw4<T> *ring = reinterpret_cast<Raw4<T> *>(smem) + threadIdx.x;   // [2][SUB][256]
     const int nvec = p.D / 4;
@@ -386,7 +387,7 @@ int conv_bwd_rows(int T, int D)
 template <typename T, int W>
 chela_status_t fwd_launch(const ConvParams &p, cudaStream_t stream)
 {
-    constexpr size_t smem = 2 * 8 * 256 * sizeof(Raw4<T>);
+    constexpr size_t smem = 2 * 4 * 256 * sizeof(Raw4<T>);
     const auto kern = conv_carry_kernel<T, W>;
     if (smem > 48 * 1024) {
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
