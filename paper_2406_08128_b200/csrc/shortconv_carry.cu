@@ -96,7 +96,8 @@ __device__ __forceinline__ void split_item(long long item, long long items, int 
     }
 }
 
-// W: taps held in registers (the width itself up to 4; 8 and 16 for the widths up to those, their extra taps zero).
+// W: taps held in registers (the width itself up to 4; 8 and 16 for the widths up to those, whose extra taps are skipped:
+// zero times an infinity that lies further back than the width would be NaN).
 // The tokens of a work item are copied to shared memory in groups of SUB, two groups ahead of the arithmetic, every thread
 // the 8 or 16 bytes that it will use itself: nothing but its own copies has to be waited for, and the loads in flight
 // cost no registers.  (65536 x 1024, bf16: four loads a thread in registers 140 us, eight 68 us, this way 58 us; groups of
@@ -145,7 +146,8 @@ __global__ void __launch_bounds__(256, W <= 4 ? 3 : 1) conv_carry_kernel(const C
                     in[0] = ring[(half * SUB + i) * 256].get();
                     float4 u = bias;
 #pragma unroll
-                    for (int j = 0; j < W; ++j) u = fma4(taps[j], in[j], u);
+                    for (int j = 0; j < W; ++j)
+                        if (W <= 4 || j < p.width) u = fma4(taps[j], in[j], u);
                     if (p.act) u = make_float4(silu_acc(u.x), silu_acc(u.y), silu_acc(u.z), silu_acc(u.w));
                     if (t + i < end) store4(py + (size_t)i * p.D, u);
                 }
@@ -265,7 +267,8 @@ __global__ void __launch_bounds__(256, W <= 4 ? 2 : 1) conv_bwd_kernel(const Con
                     if (p.act) {
                         float4 u = bias;
 #pragma unroll
-                        for (int j = 0; j < W; ++j) u = fma4(taps[j], in[j], u);
+                        for (int j = 0; j < W; ++j)
+                            if (W <= 4 || j < p.width) u = fma4(taps[j], in[j], u);
                         d = make_float4(d.x * d_silu(u.x), d.y * d_silu(u.y), d.z * d_silu(u.z), d.w * d_silu(u.w));
                     }
                     du[0] = !kEdge || t < sr.len ? d : zero4();
@@ -278,7 +281,8 @@ __global__ void __launch_bounds__(256, W <= 4 ? 2 : 1) conv_bwd_kernel(const Con
                     if (!kEdge || (tx >= t0 && tx < end)) {
                         float4 dx = zero4();
 #pragma unroll
-                        for (int j = 0; j < W; ++j) dx = fma4(taps[j], du[W - 1 - j], dx);
+                        for (int j = 0; j < W; ++j)
+                            if (W <= 4 || j < p.width) dx = fma4(taps[j], du[W - 1 - j], dx);
                         if (kEdge) {
                             const int r = tx - (sr.len - (p.width - 1));
                             if (q.d_state_out && r >= 0)

@@ -126,6 +126,26 @@ def test_conv_steps_continue_a_prompt(dtype):
     assert torch.equal(state, last)
 
 
+@pytest.mark.parametrize("W", [1, 3, 4, 5, 8, 11])
+def test_conv_reaches_no_further_than_its_width(W):
+    """An infinity or NaN in one token's input or gradient: only the outputs and gradients that the width reaches see it."""
+    import torch
+    T, D, at = 100, 16, 40
+    x, w, bias, _, dy, _ = conv_inputs(W, [T], D, W, "f32")
+    wd, bd, off = f32(w), f32(bias), i32([0, T])
+    clean, _ = chela.shortconv_carry_fwd(f32(x), wd, bd, seq_offsets=off)
+    g = chela.shortconv_bwd(f32(x), wd, f32(dy), bd, seq_offsets=off)
+    for value in (np.inf, np.nan):
+        u, du = x.copy(), dy.copy()
+        u[at] = du[at] = value
+        y, _ = chela.shortconv_carry_fwd(f32(u), wd, bd, seq_offsets=off)
+        assert torch.equal(y[:at], clean[:at]) and torch.equal(y[at + W:], clean[at + W:])
+        gd = chela.shortconv_bwd(f32(x), wd, f32(du), bd, seq_offsets=off)
+        assert torch.equal(gd.d_x[:at - W + 1], g.d_x[:at - W + 1]) and torch.equal(gd.d_x[at + 1:], g.d_x[at + 1:])
+        gx = chela.shortconv_bwd(f32(u), wd, f32(dy), bd, seq_offsets=off)   # through act' of the outputs at .. at + W - 1
+        assert torch.equal(gx.d_x[:at - W + 1], g.d_x[:at - W + 1]) and torch.equal(gx.d_x[at + W:], g.d_x[at + W:])
+
+
 # ------------------------------------------------------------------------------------------------ selective scan
 
 def scan_inputs(seed, lengths, D, N, G, dtype, pad=0):
