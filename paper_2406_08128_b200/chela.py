@@ -410,6 +410,7 @@ def mixer_gated_fwd(x, w_short, k_long, w_q, w_k, w_v, w_a, w_o, H, chunk=64, b_
 
 ShortconvGrads = collections.namedtuple("ShortconvGrads", "d_x d_w d_bias d_state_in")
 SelscanGrads = collections.namedtuple("SelscanGrads", "d_x d_dt d_a d_b d_c d_skip d_z d_dt_bias d_state_in")
+_MAX_TOKENS = 2 ** 31 - 4096
 BlocknormGrads = collections.namedtuple("BlocknormGrads", "d_res d_y d_gate d_w_post d_b_post d_scale d_w_pre d_b_pre")
 
 
@@ -457,14 +458,17 @@ def _seqs(x, seq_offsets, where):
     lead = x.shape[:-1]
     if x.dtype not in _DTYPES or len(lead) not in (1, 2):
         _need(False, where, "tokens must be [T, D] or [B, L, D] of float32 or bfloat16")
+    T = lead[0] if len(lead) == 1 else lead[0] * lead[1]
+    if T > _MAX_TOKENS:   # before ctypes cuts it to 32 bits
+        _need(False, where, "%d tokens, at most %d" % (T, _MAX_TOKENS))
     if not x.is_cuda:
         _need(False, where, "tensors must be on a CUDA device (there is no CPU fallback)")
     index = x.get_device()
     if seq_offsets is None:
-        return (lead, 1, lead[0], None, index) if len(lead) == 1 else (lead, lead[0], lead[0] * lead[1], None, index)
+        return lead, 1 if len(lead) == 1 else lead[0], T, None, index
     _need(len(lead) == 1 and seq_offsets.dim() == 1 and seq_offsets.shape[0] >= 2, where,
           "seq_offsets [S + 1] goes with packed tokens [T, D]")
-    return lead, seq_offsets.shape[0] - 1, lead[0], _flat(seq_offsets, where, "seq_offsets", seq_offsets.shape, torch.int32, index), index
+    return lead, seq_offsets.shape[0] - 1, T, _flat(seq_offsets, where, "seq_offsets", seq_offsets.shape, torch.int32, index), index
 
 
 class _on:
@@ -643,7 +647,7 @@ def _blocknorm_args(where, res, y, gate, w_post, b_post, norm_post, scale, w_pre
     """(BlocknormArgs, the tensor that gives shape and residual dtype, device)"""
     first = res if res is not None else y
     _need(first is not None, where, "res or y must be given")
-    lead, _, _, _, dev = _seqs(first, None, where)
+    lead, _, T, _, dev = _seqs(first, None, where)
     D, f32 = first.shape[-1], torch.float32
     row = (D,)
     pr, rs = (None, 0) if res is None else _rows(res, where, "res", lead, res.dtype, dev, row)
@@ -657,7 +661,6 @@ def _blocknorm_args(where, res, y, gate, w_post, b_post, norm_post, scale, w_pre
     if gate is not None:
         _need(y is not None, where, "gate goes with y")
         pg, gs = _rows(gate, where, "gate", lead, kind, dev, row)
-    T = lead[0] if len(lead) == 1 else lead[0] * lead[1]
     return BlocknormArgs(pr, py, pg, rs, ys, gs, _flat(w_post, where, "w_post", row, f32, dev), _flat(b_post, where, "b_post", row, f32, dev),
                          _flat(scale, where, "scale", row, f32, dev), _flat(w_pre, where, "w_pre", row, f32, dev),
                          _flat(b_pre, where, "b_pre", row, f32, dev), T, D, int(gate_act), int(bool(gate_after)), int(norm_post),

@@ -7,6 +7,7 @@ namespace {
 
 constexpr int kNormMaxD = 8192;
 constexpr int kMaxTokens = 0x7fffffff - 4095;   // token positions and the slices past the last one stay within int
+constexpr int kMaxSeqs = 1 << 30;               // and so do the numbers of work items (tokens / 8 + sequences)
 
 bool dtype_ok(chela_dtype_t t) { return t == CHELA_F32 || t == CHELA_BF16; }
 // token stride of an operand whose row has n elements
@@ -17,7 +18,17 @@ chela_status_t check_seqs(const int *seq_offsets, int S, int T)
     if (S < 1 || T < 1) return CHELA_ERR_INVALID_ARG;
     if (!seq_offsets && T % S != 0) return CHELA_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(seq_offsets) & 3u) return CHELA_ERR_INVALID_ARG;
-    return T <= kMaxTokens ? CHELA_OK : CHELA_ERR_UNSUPPORTED;
+    return T <= kMaxTokens && S <= kMaxSeqs ? CHELA_OK : CHELA_ERR_UNSUPPORTED;
+}
+
+// no output may be an operand's buffer: rows of other strides or types would overlap (a null pointer aliases nothing)
+template <size_t A, size_t B>
+bool distinct(const void *const (&outs)[A], const void *const (&operands)[B])
+{
+    for (const void *o : outs)
+        for (const void *i : operands)
+            if (o && o == i) return false;
+    return true;
 }
 
 chela_status_t check_conv(const void *x, long long x_stride, const float *w, const float *bias, const void *state_in,
@@ -134,6 +145,7 @@ chela_status_t chela_selscan_fwd(const chela_selscan_args_t *args, void *y, floa
     if (!dtype_ok(out_dtype) || (!y && !state_out && !checkpoints) || !aligned16(y) || !aligned16(state_out) || !aligned16(checkpoints) ||
         !aligned16(workspace))
         return CHELA_ERR_INVALID_ARG;
+    if (!distinct({y}, {args->x, args->dt, args->b, args->c, args->z})) return CHELA_ERR_INVALID_ARG;
     const size_t need = selscan_workspace_bytes(args->T, args->S, args->D, args->N);
     if (need && (!workspace || workspace_bytes < need)) return CHELA_ERR_WORKSPACE;
     return launch_selscan_fwd(*args, y, state_out, checkpoints, out_dtype, workspace, stream);
@@ -145,7 +157,7 @@ chela_status_t chela_selscan_step(const chela_selscan_args_t *args, void *y, flo
     const chela_status_t st = check_scan(args);
     if (st != CHELA_OK) return st;
     if (args->T != args->S || args->seq_offsets || !args->state_in || !y || !state_out || !dtype_ok(out_dtype) || !aligned16(y) ||
-        !aligned16(state_out))
+        !aligned16(state_out) || !distinct({y}, {args->x, args->dt, args->b, args->c, args->z}))
         return CHELA_ERR_INVALID_ARG;
     return launch_selscan_step(*args, y, state_out, out_dtype, stream);
 }
@@ -169,6 +181,7 @@ chela_status_t chela_selscan_bwd(const chela_selscan_args_t *args, const void *d
     const void *ptrs[] = {d_y, d_state_out, checkpoints, d_x, d_dt, d_a, d_b, d_c, d_skip_grad, d_z, d_dt_bias, d_state_in, workspace};
     for (const void *p : ptrs)
         if (!aligned16(p)) return CHELA_ERR_INVALID_ARG;
+    if (!distinct({d_x, d_dt, d_z, d_b, d_c}, {args->x, args->dt, args->z, args->b, args->c, d_y})) return CHELA_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < selscan_bwd_workspace_bytes(args->T, args->S, args->D, args->N, checkpoints != nullptr))
         return CHELA_ERR_WORKSPACE;
     return launch_selscan_bwd(*args, d_y, d_y_stride, d_state_out, checkpoints, d_x, d_dt, d_a, d_b, d_c, d_skip_grad, d_z, d_dt_bias,
@@ -205,6 +218,8 @@ chela_status_t chela_blocknorm_bwd(const chela_blocknorm_args_t *args, const voi
     const void *ptrs[] = {d_o, d_res_out, d_res, d_y, d_gate, d_w_post, d_b_post, d_scale, d_w_pre, d_b_pre, workspace};
     for (const void *p : ptrs)
         if (!aligned16(p)) return CHELA_ERR_INVALID_ARG;
+    if (!distinct({d_y, d_gate}, {args->res, args->y, args->gate, d_o, d_res_out}) || !distinct({d_res}, {args->res, args->y, args->gate, d_o}))
+        return CHELA_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < blocknorm_bwd_workspace_bytes(args->T, args->D)) return CHELA_ERR_WORKSPACE;
     return launch_blocknorm_bwd(*args, d_o, d_res_out, d_res, d_y, d_gate, d_w_post, d_b_post, d_scale, d_w_pre, d_b_pre, grad_dtype,
                                 workspace, stream);

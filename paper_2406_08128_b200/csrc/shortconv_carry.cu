@@ -116,8 +116,9 @@ __global__ void __launch_bounds__(256, W <= 4 ? 3 : 1) conv_carry_kernel(const C
         const int c = 4 * cv;
         const int s = packed_block_seq(p.off, p.S, p.T, kTok, blk);
         const SeqRange sr = seq_range(p.off, s, p.S, p.T);
-        const int b = (int)(blk - (sr.start / kTok + s)), t0 = b * kTok;
-        if (b < 0) continue;
+        const int b = (int)(blk - (sr.start / kTok + s));
+        if (b < 0 || b > sr.len / kTok) continue;
+        const int t0 = b * kTok;
         if (t0 < sr.len) {
             const int end = min(t0 + kTok, sr.len);
             const T *px = static_cast<const T *>(p.x) + (size_t)(sr.start + t0) * p.xs + c;
@@ -223,8 +224,9 @@ __global__ void __launch_bounds__(256, W <= 4 ? 2 : 1) conv_bwd_kernel(const Con
         for (long long blk = (long long)blockIdx.y * 8 + warp; blk < nblocks; blk += (long long)gridDim.y * 8) {
             const int s = packed_block_seq(p.off, p.S, p.T, kBwdTok, blk);
             const SeqRange sr = seq_range(p.off, s, p.S, p.T);
-            const int b = (int)(blk - (sr.start / kBwdTok + s)), t0 = b * kBwdTok;
-            if (b < 0 || t0 >= sr.len) continue;
+            const int b = (int)(blk - (sr.start / kBwdTok + s));
+            if (b < 0 || sr.len == 0 || b > (sr.len - 1) / kBwdTok) continue;
+            const int t0 = b * kBwdTok;
             const int end = min(t0 + kBwdTok, sr.len), stop = end + W - 1;
             const T *px = static_cast<const T *>(p.x) + (size_t)(sr.start + t0) * p.xs + c;
             const T *pd = static_cast<const T *>(q.dy) + (size_t)(sr.start + t0) * q.dys + c;

@@ -106,6 +106,37 @@ def test_block_norm_refusals(lib):
     assert lib.chela_blocknorm_bwd_workspace_bytes(4, 60) == 0
 
 
+def test_outputs_in_operands_and_sizes_past_the_limits_are_refused(lib):
+    bad, no, huge = chela.ERR_INVALID_ARG, chela.ERR_UNSUPPORTED, 2 ** 30 + 1
+    ptrs = {"x": 4096, "dt": 8192, "b": 12288, "c": 16384, "z": 20480, "z_stride": 64}
+    at = ctypes.c_void_p
+    for k in ("x", "dt", "b", "c", "z"):
+        assert lib.chela_selscan_fwd(scan_args(**ptrs), at(ptrs[k]), null, null, 0, null, 0, null) == bad
+        assert lib.chela_selscan_step(scan_args(**ptrs, S=4, state_in=256), at(ptrs[k]), two, 0, null) == bad
+    grads = [24576, 28672, 32768, 36864, 40960]   # d_x, d_dt, d_b, d_c, d_z
+    dy = 45056
+
+    def bwd(n=16, **kw):
+        p = dict(zip(("d_x", "d_dt", "d_b", "d_c", "d_z"), grads)) | kw
+        return lib.chela_selscan_bwd(scan_args(**ptrs), at(dy), 64, null, null, at(p["d_x"]), at(p["d_dt"]), one, at(p["d_b"]), at(p["d_c"]),
+                                     null, at(p["d_z"]), null, null, 0, one, n, null)
+    assert bwd() == chela.ERR_WORKSPACE
+    for k in ("d_x", "d_dt", "d_b", "d_c", "d_z"):
+        assert bwd(**{k: dy}) == bwd(**{k: ptrs["x"]}) == bwd(**{k: ptrs["c"]}) == bad
+
+    def norm(d_res=three, d_y=at(2048), d_gate=at(2304), d_o=at(2560), d_r=at(2816)):
+        return lib.chela_blocknorm_bwd(norm_args(gate=1024), d_o, d_r, d_res, d_y, d_gate, null, null, null, null, null, 0, one, 16, null)
+    assert norm() == norm(d_res=at(2816)) == chela.ERR_WORKSPACE   # d_res may be d_res_out
+    assert norm(d_res=one) == norm(d_res=at(2560)) == norm(d_y=two) == norm(d_y=at(2816)) == norm(d_gate=at(1024)) == bad
+
+    assert lib.chela_shortconv_carry_fwd(one, 64, one, null, two, null, null, one, huge, 8, 64, 4, 1, 1, null) == no
+    assert lib.chela_selscan_fwd(scan_args(S=huge, seq_offsets=256), two, null, null, 0, null, 0, null) == no
+    # sizes that pass 32 bits: T / 8 + S checkpoints, of 64 x 64 states and of 32 x 8
+    T, S = 2 ** 31 - 4096, 2 ** 30
+    assert lib.chela_selscan_checkpoint_bytes(T, S, 64, 64) == (T // 8 + S) * 64 * 64 * 4
+    assert lib.chela_selscan_checkpoint_bytes(T, 2 ** 31 - 1, 8, 8) == (T // 8 + 2 ** 31 - 1) * 32 * 8 * 4
+
+
 def test_the_binding_refuses_what_does_not_fit(lib):
     import torch
     x = torch.zeros(4, 64)
@@ -115,6 +146,10 @@ def test_the_binding_refuses_what_does_not_fit(lib):
         with pytest.raises(chela.ChelaError, match="no CPU fallback") as e:
             call()
         assert e.value.status == chela.ERR_INVALID_ARG
+    many = torch.zeros(1).expand(2 ** 32 + 64, 8)   # 64 tokens if cut to 32 bits
+    for call in (lambda: chela.blocknorm_fwd(many), lambda: chela.shortconv_carry_fwd(many.expand(2, -1, -1), torch.zeros(8, 4))):
+        with pytest.raises(chela.ChelaError, match="tokens, at most"):
+            call()
     where, d, f = "here", -1, torch.float32
     rows = lambda t, lead, inner: chela._rows(t, where, "t", lead, f, d, inner)[1]  # noqa: E731
     assert rows(torch.zeros(4, 128)[:, 64:], (4,), (64,)) == 128

@@ -333,6 +333,24 @@ def test_scan_of_few_long_sequences_is_split(dtype, N, D, G, lengths):
         close(getattr(g1, k), r[k], m[k], 2 * tol + more * 2.0 ** -24)
 
 
+def test_scan_of_a_split_sequence_with_growing_states():
+    """Rates above zero: a segment's whole growth is infinite in single precision, but there is nothing to grow before the
+    last ten tokens."""
+    T, D, N = 2003, 16, 16
+    form = (False, False, False, False, False)
+    v = scan_inputs(1, [T], D, N, 1, "f32")
+    v["a"] = np.abs(v["a"]) * np.float32(0.1)
+    v["dt"] = np.abs(v["dt"])
+    v["x"][:-10] = 0.0
+    args, kw = scan_call(v, [T], "f32", form)
+    assert chela.lib().chela_selscan_workspace_bytes(T, 1, D, N) > 0
+    y, s = chela.selscan_fwd(*args, **kw)
+    (want, want_s), (mag, mag_s) = scan_ref(v, [T], form), scan_ref(v, [T], form, mag=True)
+    # ten decays exp(u), u up to 1.6 x 4 x 4: the exponent's rounding is u 2^-24 of the result, so 10 (2 + 26) 2^-24 in all
+    close(y, want, mag, 512 * 2.0 ** -24)
+    close(s, want_s, mag_s, 512 * 2.0 ** -24)
+
+
 def test_scan_keeps_what_is_not_finite_where_it_is():
     """NaN and infinities of one sequence stay in it; an infinitely fast decay forgets the state and nothing else."""
     lengths, D, N = [20, 33, 9], 16, 16
