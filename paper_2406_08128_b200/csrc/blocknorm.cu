@@ -4,8 +4,8 @@
 //
 // Bound by HBM: every operand is read once and every result written once; rows stay in registers between the two norms.
 // A lane holds 8 consecutive channels (16 bytes of bf16), WPR warps share a row; sums over a row are fp32 shuffles and, for
-// WPR > 1, one exchange through shared memory.  The next row's operands are loaded while a row is worked on.  Layer statistics are two-pass (mean first) on the registers, so a large
-// mean costs no digits.
+// WPR > 1, one exchange through shared memory.  The next row's operands are loaded while a row is worked on.  Layer
+// statistics are two-pass (mean first) on the registers, so a large mean costs no digits.
 #include "packed.cuh"
 
 namespace chela {
@@ -18,6 +18,7 @@ struct NormParams {
     int T, D, gate_act, gate_after, norm_post, norm_pre;
     float eps;
     void *res_out, *o;
+    bool wide;   // all fp32 tensors lie on 32-byte boundaries: 8 values are one access
 };
 
 struct Vec8 {
@@ -27,12 +28,16 @@ struct Vec8 {
 template <typename T>
 struct Raw8 {
     Raw4<T> lo, hi;
-    __device__ __forceinline__ void load(const T *p)
+    __device__ __forceinline__ void load(const T *p, bool wide)
     {
         if constexpr (sizeof(T) == 2) {
             const uint4 u = *reinterpret_cast<const uint4 *>(p);
             lo.v = make_uint2(u.x, u.y);
             hi.v = make_uint2(u.z, u.w);
+        } else if (wide) {   // a whole sector at once
+            asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=f"(lo.v.x), "=f"(lo.v.y), "=f"(lo.v.z), "=f"(lo.v.w), "=f"(hi.v.x), "=f"(hi.v.y), "=f"(hi.v.z), "=f"(hi.v.w)
+                         : "l"(p) : "memory");
         } else {
             lo.load(p);
             hi.load(p + 4);
@@ -72,7 +77,18 @@ __device__ __forceinline__ void store8(float *p, const Vec8 &v)
     store4(p, make_float4(v.v[0], v.v[1], v.v[2], v.v[3]));
     store4(p + 4, make_float4(v.v[4], v.v[5], v.v[6], v.v[7]));
 }
-__device__ __forceinline__ void store8(__nv_bfloat16 *p, const Vec8 &v)
+// 8 values to a tensor.  In two stores of 16 bytes each a warp would touch every sector twice, which costs L2 twice the
+// requests: forward of 16384 x 2048 in fp32 121 us, in one store (and load) 105.  The backward kernel is not bound by
+// them and is 2 % slower with them.
+__device__ __forceinline__ void put8(float *p, const Vec8 &v, bool wide)
+{
+    if (wide)
+        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(v.v[0]), "f"(v.v[1]), "f"(v.v[2]), "f"(v.v[3]),
+                     "f"(v.v[4]), "f"(v.v[5]), "f"(v.v[6]), "f"(v.v[7]) : "memory");
+    else
+        store8(p, v);
+}
+__device__ __forceinline__ void put8(__nv_bfloat16 *p, const Vec8 &v, bool)
 {
     uint32_t w[4];
 #pragma unroll
@@ -82,10 +98,65 @@ __device__ __forceinline__ void store8(__nv_bfloat16 *p, const Vec8 &v)
     }
     *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ Vec8 fill8(float a) { return Vec8{{a, a, a, a, a, a, a, a}}; }
-__device__ __forceinline__ void stage_weight(float *to, const float *from, float other, int D, int width)
+// elementwise, in pairs: half the instructions
+__device__ __forceinline__ Vec8 mul8(const Vec8 &a, const Vec8 &b)
 {
-    for (int c = threadIdx.x; c < width; c += blockDim.x) to[c] = from && c < D ? from[c] : other;
+    Vec8 o;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const float2 t = mul2v(make_float2(a.v[e], a.v[e + 1]), make_float2(b.v[e], b.v[e + 1]));
+        o.v[e] = t.x;
+        o.v[e + 1] = t.y;
+    }
+    return o;
+}
+__device__ __forceinline__ Vec8 add8(const Vec8 &a, const Vec8 &b)
+{
+    Vec8 o;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const float2 t = add2v(make_float2(a.v[e], a.v[e + 1]), make_float2(b.v[e], b.v[e + 1]));
+        o.v[e] = t.x;
+        o.v[e + 1] = t.y;
+    }
+    return o;
+}
+__device__ __forceinline__ Vec8 fma8(const Vec8 &a, const Vec8 &b, const Vec8 &c)
+{
+    Vec8 o;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const float2 t = fma2v(make_float2(a.v[e], a.v[e + 1]), make_float2(b.v[e], b.v[e + 1]), make_float2(c.v[e], c.v[e + 1]));
+        o.v[e] = t.x;
+        o.v[e + 1] = t.y;
+    }
+    return o;
+}
+__device__ __forceinline__ float dot8(const Vec8 &a, const Vec8 &b)
+{
+    float2 t = mul2v(make_float2(a.v[0], a.v[1]), make_float2(b.v[0], b.v[1]));
+#pragma unroll
+    for (int e = 2; e < 8; e += 2) t = fma2v(make_float2(a.v[e], a.v[e + 1]), make_float2(b.v[e], b.v[e + 1]), t);
+    return t.x + t.y;
+}
+__device__ __forceinline__ float sum8(const Vec8 &a)
+{
+    float2 t = make_float2(a.v[0], a.v[1]);
+#pragma unroll
+    for (int e = 2; e < 8; e += 2) t = add2v(t, make_float2(a.v[e], a.v[e + 1]));
+    return t.x + t.y;
+}
+__device__ __forceinline__ Vec8 fill8(float a) { return Vec8{{a, a, a, a, a, a, a, a}}; }
+__device__ __forceinline__ void stage_weight(float *to, const float *from, float other, const float *scale, int D, int width)
+{
+    // of each warp's 256 channels the even groups of four first, so that 32 lanes read 8 channels each without bank conflicts
+    for (int c = threadIdx.x; c < width; c += blockDim.x) to[(c & ~255) + (c & 4) * 32 + (c >> 3 & 31) * 4 + (c & 3)] = (from && c < D ? from[c] : other) * (scale && c < D ? scale[c] : 1.f);
+}
+
+__device__ __forceinline__ Vec8 staged8(const float *p)   // of a lane's own vectors
+{
+    const float4 a = load4(p), b = load4(p + 128);
+    return Vec8{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
 }
 
 // act(u) in place; act is the same for all threads, so the branch is taken once and not per element
@@ -198,9 +269,9 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : (kBias
     Raw8<TI> ry, rg;
     auto fetch = [&](long long at) {
         const bool ok = live && at < p.T;
-        if (ok && p.res) rr.load(static_cast<const TR *>(p.res) + (size_t)at * p.rs + c); else rr.zero();
-        if (ok && post) ry.load(static_cast<const TI *>(p.y) + (size_t)at * p.ys + c); else ry.zero();
-        if (ok && gated) rg.load(static_cast<const TI *>(p.gate) + (size_t)at * p.gs + c); else rg.zero();
+        if (ok && p.res) rr.load(static_cast<const TR *>(p.res) + (size_t)at * p.rs + c, p.wide); else rr.zero();
+        if (ok && post) ry.load(static_cast<const TI *>(p.y) + (size_t)at * p.ys + c, p.wide); else ry.zero();
+        if (ok && gated) rg.load(static_cast<const TI *>(p.gate) + (size_t)at * p.gs + c, p.wide); else rg.zero();
     };
     fetch(row);
     for (; row < p.T; row += stride) {
@@ -224,13 +295,13 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : (kBias
 #pragma unroll
                 for (int e = 0; e < 8; ++e) r.v[e] += v.v[e];
             }
-            if (live && p.res_out) store8(static_cast<TR *>(p.res_out) + (size_t)row * p.D + c, r);
+            if (live && p.res_out) put8(static_cast<TR *>(p.res_out) + (size_t)row * p.D + c, r, p.wide);
         }
         if (pre) {
             normalise(r, p.norm_pre);
 #pragma unroll
             for (int e = 0; e < 8; ++e) r.v[e] = kBias ? fmaf(r.v[e], w_pre.v[e], b_pre.v[e]) : r.v[e] * w_pre.v[e];
-            if (live) store8(static_cast<TO *>(p.o) + (size_t)row * p.D + c, r);
+            if (live) put8(static_cast<TO *>(p.o) + (size_t)row * p.D + c, r, p.wide);
         }
     }
 }
@@ -241,11 +312,16 @@ struct NormBwdParams {
     NormParams f;   // res = r'
     const void *d_o, *d_ro;
     void *d_res, *d_y, *d_gate;
-    float *part;    // [CTAs][5][D]: w_post, b_post, scale, w_pre, b_pre
+    float *part;    // [CTAs][4][D]: sums over the rows of d n hat / scale and d n / scale, of d o hat' and d o
 };
 
-// One vector of 8 channels a lane, so that the five parameter gradients of its channels (40 registers) stay in registers
-// over all rows the group walks; D <= 256 WPR.  Channels past D have zero operands, and zero weights where that is not
+// One vector of 8 channels a lane, so that the sums that the parameters' gradients are made of (32 registers) stay in
+// registers over all rows the group walks; D <= 256 WPR.  With P = sum d n hat / scale and Q = sum d n / scale, where d n /
+// scale is d r' (times the gate behind the norm): d_w_post = scale P, d_b_post = scale Q, d_scale = w_post P + b_post Q.
+// 16 warps an SM of 128 registers and three or four dependent sums over the row: the chain of these, not HBM, bounds it
+// (32749 x 1024, layer norms, gate, bf16 beside an fp32 residual: 159 us for 113 us of traffic; one operation a channel
+// and five sums instead of pairs and four: 197).  Two rows a warp at a time need 168 registers, 12 warps: 158 us where one
+// takes 165 at 1024 channels, but 215 at 512 and 379 against 271 in fp32, whose operands then fill shared memory.  Channels past D have zero operands, and zero weights where that is not
 // enough, so they add nothing to the sums.
 template <typename TI, typename TR, typename TG, int WPR>
 __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 2) blocknorm_bwd_kernel(const NormBwdParams q)
@@ -254,20 +330,19 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 2) blo
     const NormParams &p = q.f;
     constexpr int WIDTH = WPR * 256;
     __shared__ __align__(16) float2 buf[GROUPS * 2 * WPR];
-    extern __shared__ __align__(16) float s_w[];   // w_post, b_post, scale, w_pre [WIDTH]; in the end the groups' sums
+    extern __shared__ __align__(16) float s_w[];   // w_post scale, b_post scale, w_pre [WIDTH]; in the end the groups' sums
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp / WPR, wr = warp % WPR;
     RowSum<WPR> sum = {buf, 0, group, wr, lane};
     const float inv_d = 1.f / p.D;
     const int c = 8 * (wr * 32 + lane);
     const bool live = c < p.D;
-    Vec8 acc[5];
+    Vec8 acc[4];
 #pragma unroll
-    for (int k = 0; k < 5; ++k) acc[k] = fill8(0.f);
+    for (int k = 0; k < 4; ++k) acc[k] = fill8(0.f);
     const bool post = p.y != nullptr, pre = q.d_o != nullptr, gated = p.gate != nullptr;
-    stage_weight(s_w, p.w_post, 1.f, p.D, WIDTH);
-    stage_weight(s_w + WIDTH, p.b_post, 0.f, p.D, WIDTH);
-    stage_weight(s_w + 2 * WIDTH, p.scale, 1.f, p.D, WIDTH);
-    stage_weight(s_w + 3 * WIDTH, p.w_pre, 1.f, p.D, WIDTH);
+    stage_weight(s_w, p.w_post, 1.f, p.scale, p.D, WIDTH);
+    stage_weight(s_w + WIDTH, p.b_post, 0.f, p.scale, p.D, WIDTH);
+    stage_weight(s_w + 2 * WIDTH, p.w_pre, 1.f, nullptr, p.D, WIDTH);
     __syncthreads();
 
     // Operands of a row.  Up to 2048 channels they are copied to shared memory one row ahead, every lane what it will read
@@ -275,7 +350,8 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 2) blo
     // where they are wanted.
     constexpr bool AHEAD = WPR <= 8;
     constexpr int NR = sizeof(TR) / 2, NI = sizeof(TI) / 2, SLOTS = 2 * NR + 3 * NI;   // 16-byte vectors of r', d r', d o, y, gate
-    uint4 *s_row = reinterpret_cast<uint4 *>(s_w + (GROUPS > 5 ? GROUPS - 1 : 4) * WIDTH) + warp * (2 * SLOTS * 32) + lane;
+    uint4 *s_row = reinterpret_cast<uint4 *>(s_w + (GROUPS > 4 ? GROUPS - 1 : 3) * WIDTH) + warp * (2 * SLOTS * 32) + lane;
+    const float *s_lane = s_w + wr * 256 + 4 * lane;
     const long long stride = (long long)gridDim.x * GROUPS;
     long long row = (long long)blockIdx.x * GROUPS + group;
     auto fetch = [&](long long at, int stage) {
@@ -307,14 +383,14 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 2) blo
         auto res_like = [&](int slot, const void *from, long long step, bool used) -> Vec8 {
             Raw8<TR> r;
             if (AHEAD) r.from(now + slot * 32, 32);
-            else if (live && used) r.load(static_cast<const TR *>(from) + (size_t)row * step + c);
+            else if (live && used) r.load(static_cast<const TR *>(from) + (size_t)row * step + c, p.wide);
             else r.zero();
             return r.get();
         };
         auto in_like = [&](int slot, const void *from, long long step, bool used) -> Vec8 {
             Raw8<TI> r;
             if (AHEAD) r.from(now + slot * 32, 32);
-            else if (live && used) r.load(static_cast<const TI *>(from) + (size_t)row * step + c);
+            else if (live && used) r.load(static_cast<const TI *>(from) + (size_t)row * step + c, p.wide);
             else r.zero();
             return r.get();
         };
@@ -324,135 +400,79 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 2) blo
         if (gated) {
             ga = read_gate();
             activate8(ga, p.gate_act);
-            if (!p.gate_after) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v.v[e] *= ga.v[e];
-            }
+            if (!p.gate_after) v = mul8(v, ga);
         }
         // statistics of both norms together: r' and v
         float2 s;
         const bool l0 = pre && p.norm_pre == CHELA_NORM_LAYER, l1 = post && p.norm_post == CHELA_NORM_LAYER;
         if (l0 || l1) {
-            float a = 0.f, b = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                a += hat.v[e];
-                b += v.v[e];
-            }
-            s = sum.two(a, b);
-            const float m0 = l0 && live ? s.x * inv_d : 0.f, m1 = l1 && live ? s.y * inv_d : 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                hat.v[e] -= m0;
-                v.v[e] -= m1;
-            }
+            s = sum.two(sum8(hat), sum8(v));
+            hat = add8(hat, fill8(l0 && live ? -s.x * inv_d : 0.f));
+            v = add8(v, fill8(l1 && live ? -s.y * inv_d : 0.f));
         }
-        {
-            float a = 0.f, b = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                a = fmaf(hat.v[e], hat.v[e], a);
-                b = fmaf(v.v[e], v.v[e], b);
-            }
-            s = sum.two(a, b);
-        }
+        s = sum.two(dot8(hat, hat), dot8(v, v));
         const float i0 = p.norm_pre == CHELA_NORM_NONE ? 1.f : 1.0f / sqrtf(fmaf(s.x, inv_d, p.eps));
         const float i1 = p.norm_post == CHELA_NORM_NONE ? 1.f : 1.0f / sqrtf(fmaf(s.y, inv_d, p.eps));
         // norm before the next block: d hat, then d r'
         Vec8 d_r = res_like(NR, q.d_ro, p.D, q.d_ro != nullptr);
         if (pre) {
-            const Vec8 w = load8(s_w + 3 * WIDTH + c);
             Vec8 d_o = in_like(2 * NR, q.d_o, p.D, pre);
-            float a = 0.f, b = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                hat.v[e] *= i0;
-                acc[3].v[e] = fmaf(d_o.v[e], hat.v[e], acc[3].v[e]);
-                acc[4].v[e] += d_o.v[e];
-                d_o.v[e] *= w.v[e];
-                a = fmaf(d_o.v[e], hat.v[e], a);
-                b += d_o.v[e];
-            }
+            hat = mul8(hat, fill8(i0));
+            acc[2] = fma8(d_o, hat, acc[2]);
+            acc[3] = add8(acc[3], d_o);
+            d_o = mul8(d_o, staged8(s_lane + 2 * WIDTH));
             if (p.norm_pre != CHELA_NORM_NONE) {
-                s = sum.two(a, b);
-                const float k0 = -s.x * inv_d, k1 = l0 && live ? s.y * inv_d : 0.f;   // channels past D stay zero
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d_r.v[e] = fmaf(i0, fmaf(hat.v[e], k0, d_o.v[e]) - k1, d_r.v[e]);
+                s = sum.two(dot8(d_o, hat), sum8(d_o));
+                const float k0 = -s.x * inv_d * i0, k1 = l0 && live ? -s.y * inv_d * i0 : 0.f;   // channels past D stay zero
+                d_r = fma8(fill8(i0), d_o, d_r);
+                d_r = fma8(hat, fill8(k0), d_r);
+                if (l0) d_r = add8(d_r, fill8(k1));
             } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d_r.v[e] += d_o.v[e];
+                d_r = add8(d_r, d_o);
             }
         }
-        if (live) store8(static_cast<TR *>(q.d_res) + (size_t)row * p.D + c, d_r);
+        if (live) put8(static_cast<TR *>(q.d_res) + (size_t)row * p.D + c, d_r, false);
         if (post) {
-            // d_r becomes d m, then d n, then d hat, then d v
-            const Vec8 w = load8(s_w + c), sc = load8(s_w + 2 * WIDTH + c);
-            Vec8 n = load8(s_w + WIDTH + c);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v.v[e] *= i1;
-                n.v[e] = fmaf(v.v[e], w.v[e], n.v[e]);
-            }
+            // d_r becomes d n / scale, then d hat, then d v
+            const Vec8 w = staged8(s_lane);
+            v = mul8(v, fill8(i1));
             Vec8 dg;   // gradient of act(gate)
             if (gated && p.gate_after) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    acc[2].v[e] = fmaf(d_r.v[e], n.v[e] * ga.v[e], acc[2].v[e]);
-                    d_r.v[e] *= sc.v[e];
-                    dg.v[e] = d_r.v[e] * n.v[e];
-                    d_r.v[e] *= ga.v[e];
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    acc[2].v[e] = fmaf(d_r.v[e], n.v[e], acc[2].v[e]);
-                    d_r.v[e] *= sc.v[e];
-                }
+                dg = mul8(d_r, fma8(v, w, staged8(s_lane + WIDTH)));
+                d_r = mul8(d_r, ga);
             }
-            float a = 0.f, b = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                acc[0].v[e] = fmaf(d_r.v[e], v.v[e], acc[0].v[e]);
-                acc[1].v[e] += d_r.v[e];
-                d_r.v[e] *= w.v[e];
-                a = fmaf(d_r.v[e], v.v[e], a);
-                b += d_r.v[e];
-            }
+            acc[0] = fma8(d_r, v, acc[0]);
+            acc[1] = add8(acc[1], d_r);
+            d_r = mul8(d_r, w);
             if (p.norm_post != CHELA_NORM_NONE) {
-                s = sum.two(a, b);
-                const float k0 = -s.x * inv_d, k1 = l1 ? s.y * inv_d : 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d_r.v[e] = i1 * (fmaf(v.v[e], k0, d_r.v[e]) - k1);
+                s = sum.two(dot8(d_r, v), sum8(d_r));
+                d_r = mul8(d_r, fill8(i1));
+                d_r = fma8(v, fill8(-s.x * inv_d * i1), d_r);
+                if (l1) d_r = add8(d_r, fill8(-s.y * inv_d * i1));
             }
             if (gated) {
                 const Vec8 gr = read_gate();
                 if (!p.gate_after) {
-                    const Vec8 y = read_y();
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        dg.v[e] = d_r.v[e] * y.v[e];
-                        d_r.v[e] *= ga.v[e];
-                    }
+                    dg = mul8(d_r, read_y());
+                    d_r = mul8(d_r, ga);
                 }
                 if (p.gate_act == 1) {   // slope sg (1 + u (1 - sg)) = sg + act (1 - sg)
+                    Vec8 sg;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float sg = sigmoid_acc(gr.v[e]);
-                        dg.v[e] *= fmaf(ga.v[e], 1.f - sg, sg);
-                    }
+                    for (int e = 0; e < 8; ++e) sg.v[e] = sigmoid_acc(gr.v[e]);
+                    dg = mul8(dg, fma8(ga, fma8(sg, fill8(-1.f), fill8(1.f)), sg));
                 } else if (p.gate_act == 2) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) dg.v[e] *= fmaf(-ga.v[e], ga.v[e], ga.v[e]);
+                    dg = mul8(dg, fma8(mul8(ga, fill8(-1.f)), ga, ga));
                 }
-                if (live) store8(static_cast<TG *>(q.d_gate) + (size_t)row * p.D + c, dg);
+                if (live) put8(static_cast<TG *>(q.d_gate) + (size_t)row * p.D + c, dg, false);
             }
-            if (live) store8(static_cast<TG *>(q.d_y) + (size_t)row * p.D + c, d_r);
+            if (live) put8(static_cast<TG *>(q.d_y) + (size_t)row * p.D + c, d_r, false);
         }
     }
     // sums of the CTA's row groups, one partial row per CTA
     if (GROUPS > 1) {
 #pragma unroll
-        for (int k = 0; k < 5; ++k) {
+        for (int k = 0; k < 4; ++k) {
             __syncthreads();
             if (group > 0) store8(s_w + (group - 1) * WIDTH + c, acc[k]);
             __syncthreads();
@@ -467,31 +487,46 @@ __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : 2) blo
         }
     }
     if (live && group == 0) {
-        float *o = q.part + (size_t)blockIdx.x * 5 * p.D + c;
+        float *o = q.part + (size_t)blockIdx.x * 4 * p.D + c;
 #pragma unroll
-        for (int k = 0; k < 5; ++k) store8(o + (size_t)k * p.D, acc[k]);
+        for (int k = 0; k < 4; ++k) store8(o + (size_t)k * p.D, acc[k]);
     }
 }
 
 struct NormSums {
-    float *out[5];
+    float *d_w_post, *d_b_post, *d_scale, *d_w_pre, *d_b_pre;
+    const float *w_post, *b_post, *scale;
 };
-// sums over the CTAs in two fixed steps: 8 warps take every eighth partial, then meet in shared memory
-__global__ void __launch_bounds__(256) blocknorm_sum_kernel(const float *part, NormSums sums, int nparts, int D)
+// sums over the CTAs in two fixed steps: 32 warps take every 32nd partial, then meet in shared memory.  blockIdx.y: P and Q
+// of the post norm, or the two of the pre norm
+__global__ void __launch_bounds__(1024) blocknorm_sum_kernel(const float *part, NormSums sums, int nparts, int D)
 {
-    __shared__ float red[8][33];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, k = blockIdx.y;
-    if (!sums.out[k]) return;
-    float o = 0.f;
-    if (c < D)
-        for (int i = warp; i < nparts; i += 8) o += part[((size_t)i * 5 + k) * D + c];
+    __shared__ float2 red[32][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, k = 2 * blockIdx.y;
+    if (k == 0 ? !sums.d_w_post && !sums.d_b_post && !sums.d_scale : !sums.d_w_pre && !sums.d_b_pre) return;
+    float2 o = make_float2(0.f, 0.f);
+    if (c < D) {
+#pragma unroll 4
+        for (int i = warp; i < nparts; i += 32) {
+            const float *at = part + ((size_t)i * 4 + k) * D + c;
+            o.x += at[0];
+            o.y += at[D];
+        }
+    }
     red[warp][lane] = o;
     __syncthreads();
-    if (warp == 0 && c < D) {
-        o = 0.f;
+    if (warp != 0 || c >= D) return;
+    o = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < 8; ++w) o += red[w][lane];
-        sums.out[k][c] = o;
+    for (int w = 0; w < 32; ++w) o = add2v(o, red[w][lane]);
+    if (k == 0) {
+        const float sc = sums.scale ? sums.scale[c] : 1.f;
+        if (sums.d_w_post) sums.d_w_post[c] = sc * o.x;
+        if (sums.d_b_post) sums.d_b_post[c] = sc * o.y;
+        if (sums.d_scale) sums.d_scale[c] = fmaf(sums.w_post ? sums.w_post[c] : 1.f, o.x, sums.b_post ? sums.b_post[c] * o.y : 0.f);
+    } else {
+        if (sums.d_w_pre) sums.d_w_pre[c] = o.x;
+        if (sums.d_b_pre) sums.d_b_pre[c] = o.y;
     }
 }
 
@@ -547,7 +582,7 @@ chela_status_t bwd_d(const NormBwdParams &q, const NormSums &sums, cudaStream_t 
     const NormParams &p = q.f;
     const int wpr = row_warps(p.D), grid = row_grid(p.T, p.D, kBwdPerSm);
     // weights (in the end the row groups' sums); two rows of operands a warp where they are fetched ahead
-    const int rows = row_groups(wpr) - 1 > 4 ? row_groups(wpr) - 1 : 4;
+    const int rows = row_groups(wpr) > 4 ? row_groups(wpr) - 1 : 3;
     const size_t ahead = wpr <= 8 ? (size_t)8 * 2 * (sizeof(TR) + 3 * sizeof(TI) / 2) * 32 * 16 : 0;
     const size_t smem = (size_t)rows * wpr * 256 * 4 + ahead;
     chela_status_t st;
@@ -559,18 +594,19 @@ chela_status_t bwd_d(const NormBwdParams &q, const NormSums &sums, cudaStream_t 
     case 16: st = norm_launch(blocknorm_bwd_kernel<TI, TR, TG, 16>, q, grid, 512, smem, stream); break;
     default: st = norm_launch(blocknorm_bwd_kernel<TI, TR, TG, 32>, q, grid, 1024, smem, stream); break;
     }
-    bool any = false;
-    for (int k = 0; k < 5; ++k) any = any || sums.out[k];
-    if (st == CHELA_OK && any) {
-        blocknorm_sum_kernel<<<dim3((p.D + 31) / 32, 5), 256, 0, stream>>>(q.part, sums, grid, p.D);
+    if (st == CHELA_OK && (sums.d_w_post || sums.d_b_post || sums.d_scale || sums.d_w_pre || sums.d_b_pre)) {
+        blocknorm_sum_kernel<<<dim3((p.D + 31) / 32, 2), 1024, 0, stream>>>(q.part, sums, grid, p.D);
         st = last_launch_status();
     }
     return st;
 }
 
+bool on_sector(const void *p, bool is_f32) { return !is_f32 || reinterpret_cast<uintptr_t>(p) % 32 == 0; }
 NormParams norm_params(const chela_blocknorm_args_t &a)
 {
     NormParams p = {};
+    const bool i32 = a.in_dtype == CHELA_F32;
+    p.wide = on_sector(a.res, a.res_dtype == CHELA_F32) && on_sector(a.y, i32) && on_sector(a.gate, i32);
     p.res = a.res; p.y = a.y; p.gate = a.gate;
     p.rs = a.res_stride; p.ys = a.y_stride; p.gs = a.gate_stride;
     p.w_post = a.w_post; p.b_post = a.b_post; p.scale = a.scale; p.w_pre = a.w_pre; p.b_pre = a.b_pre;
@@ -588,6 +624,7 @@ chela_status_t launch_blocknorm_fwd(const chela_blocknorm_args_t &a, void *res_o
     NormParams p = norm_params(a);
     p.res_out = res_out;
     p.o = o;
+    p.wide = p.wide && on_sector(res_out, a.res_dtype == CHELA_F32) && on_sector(o, out_dtype == CHELA_F32);
     const bool i32 = a.in_dtype == CHELA_F32, r32 = a.res_dtype == CHELA_F32, o32 = out_dtype == CHELA_F32;
     if (i32) {
         if (r32) return o32 ? fwd_d<float, float, float>(p, stream) : fwd_d<float, float, bf>(p, stream);
@@ -599,7 +636,7 @@ chela_status_t launch_blocknorm_fwd(const chela_blocknorm_args_t &a, void *res_o
 
 size_t blocknorm_bwd_workspace_bytes(int T, int D)
 {
-    return align_up((size_t)row_grid(T, D, kBwdPerSm) * 5 * D * sizeof(float), 256);
+    return align_up((size_t)row_grid(T, D, kBwdPerSm) * 4 * D * sizeof(float), 256);
 }
 
 chela_status_t launch_blocknorm_bwd(const chela_blocknorm_args_t &a, const void *d_o, const void *d_res_out, void *d_res, void *d_y,
@@ -611,8 +648,10 @@ chela_status_t launch_blocknorm_bwd(const chela_blocknorm_args_t &a, const void 
     q.f = norm_params(a);
     q.d_o = d_o; q.d_ro = d_res_out;
     q.d_res = d_res; q.d_y = d_y; q.d_gate = d_gate;
+    const bool rw = a.res_dtype == CHELA_F32, gw = grad_dtype == CHELA_F32;
+    q.f.wide = q.f.wide && on_sector(d_o, a.in_dtype == CHELA_F32) && on_sector(d_res_out, rw) && on_sector(d_res, rw) && on_sector(d_y, gw) && on_sector(d_gate, gw);
     q.part = static_cast<float *>(workspace);
-    const NormSums sums = {{d_w_post, d_b_post, d_scale, d_w_pre, d_b_pre}};
+    const NormSums sums = {d_w_post, d_b_post, d_scale, d_w_pre, d_b_pre, a.w_post, a.b_post, a.scale};
     const bool i32 = a.in_dtype == CHELA_F32, r32 = a.res_dtype == CHELA_F32, g32 = grad_dtype == CHELA_F32;
     if (i32) {
         if (r32) return g32 ? bwd_d<float, float, float>(q, sums, stream) : bwd_d<float, float, bf>(q, sums, stream);

@@ -537,6 +537,23 @@ def test_block_norm_in_place_constant_and_extreme_rows():
     assert got is res and torch.equal(got, want) and torch.equal(o1, o2)
 
 
+@pytest.mark.parametrize("D", [40, 1000, 4104])
+def test_block_norm_of_tensors_between_sectors(D):
+    """fp32 tensors 16 bytes behind a 32-byte boundary: the same bits as on one."""
+    import torch
+    T = 5
+    off = lambda t: torch.empty(t.numel() + 12, device="cuda", dtype=t.dtype)[4:4 + t.numel()].view(t.shape).copy_(t)  # noqa: E731
+    res, y, gate, d_o, d_r = (torch.randn(T, D, device="cuda") for _ in range(5))
+    r1, o1 = chela.blocknorm_fwd(res, y, gate)
+    empty = lambda: off(torch.zeros(T, D, device="cuda"))  # noqa: E731
+    r2, o2 = chela.blocknorm_fwd(off(res), off(y), off(gate), res_out=empty(), out=empty())
+    assert res.data_ptr() % 32 == 0 and r2.data_ptr() % 32 == 16 and torch.equal(r1, r2) and torch.equal(o1, o2)
+    r3, o3 = chela.blocknorm_fwd(res, y, gate, out=empty())
+    assert torch.equal(r1, r3) and torch.equal(o1, o3)
+    for p, q in zip(chela.blocknorm_bwd(r1, y, gate, d_o, d_r), chela.blocknorm_bwd(off(r1), off(y), off(gate), off(d_o), off(d_r))):
+        assert p is None or torch.equal(p, q)
+
+
 # ------------------------------------------------------------------------------------------------ calls
 
 def test_graph_replay_streams_and_repeated_calls_give_equal_bits():
