@@ -215,6 +215,8 @@ struct RowSum {
 
 // ------------------------------------------------------------------------------------------------ forward
 
+// kBias: without the two bias vectors a lane needs 80 registers and three CTAs are resident, with them two (32768 x 1024
+// with biases and layer norms 85 us, without either 78).
 template <typename TI, typename TR, typename TO, int WPR, bool kBias>
 __global__ void __launch_bounds__(WPR > 8 ? 32 * WPR : 256, WPR > 8 ? 1 : (kBias ? 2 : 3)) blocknorm_fwd_kernel(const NormParams p)
 {
