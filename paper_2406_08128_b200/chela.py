@@ -425,11 +425,14 @@ def _raw_stream(index):
     return torch._C._cuda_getCurrentRawStream(index)
 
 
-def _rows(t, where, name, lead, dtype, index, inner):
-    """Address and token stride of a token tensor [*lead, *inner]; the inner axes contiguous, one step between tokens."""
-    n = len(lead)
-    if t.dtype is not dtype or t.get_device() != index or t.shape != lead + inner:
+def _rows(t, where, name, lead, dtype, index, inner, shape=None):
+    """Address and token stride of a token tensor [*lead, *inner] (= shape, where the caller has it); the inner axes
+    contiguous, one step between tokens."""
+    if t.dtype is not dtype or t.get_device() != index or t.shape != (shape or lead + inner):
         _need(False, where, "%s must be a %s tensor %s on device %d" % (name, dtype, lead + inner, index))
+    if t.is_contiguous():
+        return t.data_ptr(), inner[0] if len(inner) == 1 else inner[0] * inner[1]
+    n = len(lead)
     strides, step = t.stride(), 1
     for i in range(len(inner) - 1, -1, -1):
         if strides[n + i] != step and inner[i] != 1:
@@ -471,25 +474,29 @@ def _seqs(x, seq_offsets, where):
     return lead, seq_offsets.shape[0] - 1, T, _flat(seq_offsets, where, "seq_offsets", seq_offsets.shape, torch.int32, index), index
 
 
-class _on:
-    """The device of a call's tensors as the current one (no switch where it is already)."""
-
-    def __init__(self, index):
-        self.guard = None if index == torch.cuda.current_device() else torch.cuda.device(index)
-
-    def __enter__(self):
-        if self.guard:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard:
-            self.guard.__exit__(*exc)
+def _run(fn, where, index, *args):
+    """fn(*args, stream) on the current stream of the call's device."""
+    if index == torch._C._cuda_getDevice():
+        status = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, _raw_stream(index))
+    if status != OK:
+        raise ChelaError(int(status), where)
 
 
 def _new(out, where, name, shape, dtype, device, index):
     if out is None:
         return torch.empty(shape, dtype=dtype, device=device)
     _flat(out, where, name, shape, dtype, index)
+    return out
+
+
+def _new_like(out, where, name, like, dtype, index):
+    """A contiguous output of like's shape."""
+    if out is None:
+        return torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
+    _flat(out, where, name, like.shape, dtype, index)
     return out
 
 
@@ -509,15 +516,13 @@ def shortconv_carry_fwd(x, w, bias=None, act=True, state_in=None, state_out=None
     where, f32 = "chela_shortconv_carry_fwd", torch.float32
     lead, S, T, off, dev = _seqs(x, seq_offsets, where)
     D, width, dt = x.shape[-1], w.shape[-1], x.dtype
-    px, xs = _rows(x, where, "x", lead, dt, dev, (D,))
-    y = _new(out, where, "out", x.shape, dt, x.device, dev)
+    px, xs = _rows(x, where, "x", lead, dt, dev, (D,), x.shape)
+    y = _new_like(out, where, "out", x, dt, dev)
     held = (S, width - 1, D)
     state_out = _new(state_out, where, "state_out", held, dt, x.device, dev)
-    with _on(dev):
-        _check(lib().chela_shortconv_carry_fwd(
-            px, xs, _flat(w, where, "w", (D, width), f32, dev), _flat(bias, where, "bias", (D,), f32, dev), y.data_ptr(),
-            _flat(state_in, where, "state_in", held, dt, dev), state_out.data_ptr() or None, off, S, T, D, width, int(bool(act)),
-            _DTYPES[dt], _raw_stream(dev)), where)
+    _run(lib().chela_shortconv_carry_fwd, where, dev, px, xs, _flat(w, where, "w", (D, width), f32, dev),
+         _flat(bias, where, "bias", (D,), f32, dev), y.data_ptr(), _flat(state_in, where, "state_in", held, dt, dev),
+         state_out.data_ptr() or None, off, S, T, D, width, int(bool(act)), _DTYPES[dt])
     return y, state_out
 
 
@@ -528,15 +533,13 @@ def shortconv_step(x, w, state, bias=None, act=True, state_out=None, out=None):
     lead, _, S, _, dev = _seqs(x, None, where)
     _need(len(lead) == 1, where, "x must be [S, D]")
     D, width, dt = x.shape[-1], w.shape[-1], x.dtype
-    px, xs = _rows(x, where, "x", lead, dt, dev, (D,))
-    y = _new(out, where, "out", x.shape, dt, x.device, dev)
+    px, xs = _rows(x, where, "x", lead, dt, dev, (D,), x.shape)
+    y = _new_like(out, where, "out", x, dt, dev)
     held = (S, width - 1, D)
     before = _flat(state, where, "state", held, dt, dev)
     after = before if state_out is None else _flat(state_out, where, "state_out", held, dt, dev)
-    with _on(dev):
-        _check(lib().chela_shortconv_step(
-            px, xs, _flat(w, where, "w", (D, width), f32, dev), _flat(bias, where, "bias", (D,), f32, dev), y.data_ptr(), before or None,
-            after or None, S, D, width, int(bool(act)), _DTYPES[dt], _raw_stream(dev)), where)
+    _run(lib().chela_shortconv_step, where, dev, px, xs, _flat(w, where, "w", (D, width), f32, dev),
+         _flat(bias, where, "bias", (D,), f32, dev), y.data_ptr(), before or None, after or None, S, D, width, int(bool(act)), _DTYPES[dt])
     return y
 
 
@@ -546,18 +549,16 @@ def shortconv_bwd(x, w, d_y, bias=None, act=True, state_in=None, d_state_out=Non
     where, f32 = "chela_shortconv_bwd", torch.float32
     lead, S, T, off, dev = _seqs(x, seq_offsets, where)
     D, width, dt, gt, device = x.shape[-1], w.shape[-1], x.dtype, _tdtype(grad_dtype), x.device
-    px, xs = _rows(x, where, "x", lead, dt, dev, (D,))
+    px, xs = _rows(x, where, "x", lead, dt, dev, (D,), x.shape)
     pdy, dys = _rows(d_y, where, "d_y", lead, dt, dev, (D,))
     held = (S, width - 1, D)
     g = ShortconvGrads(torch.empty(x.shape, dtype=gt, device=device), torch.empty((D, width), dtype=f32, device=device),
                        torch.empty((D,), dtype=f32, device=device), torch.empty(held, dtype=gt, device=device) if want_d_state else None)
     ws, nbytes = _scratch(lib().chela_shortconv_bwd_workspace_bytes(T, D, width), workspace, device, where, dev)
-    with _on(dev):
-        _check(lib().chela_shortconv_bwd(
-            px, xs, _flat(w, where, "w", (D, width), f32, dev), _flat(bias, where, "bias", (D,), f32, dev), pdy, dys,
-            _flat(state_in, where, "state_in", held, dt, dev), _flat(d_state_out, where, "d_state_out", held, dt, dev),
-            g.d_x.data_ptr(), g.d_w.data_ptr(), g.d_bias.data_ptr(), _ptr(g.d_state_in), off, S, T, D, width, int(bool(act)), _DTYPES[dt],
-            int(grad_dtype), ws, nbytes, _raw_stream(dev)), where)
+    _run(lib().chela_shortconv_bwd, where, dev, px, xs, _flat(w, where, "w", (D, width), f32, dev),
+         _flat(bias, where, "bias", (D,), f32, dev), pdy, dys, _flat(state_in, where, "state_in", held, dt, dev),
+         _flat(d_state_out, where, "d_state_out", held, dt, dev), g.d_x.data_ptr(), g.d_w.data_ptr(), g.d_bias.data_ptr(),
+         _ptr(g.d_state_in), off, S, T, D, width, int(bool(act)), _DTYPES[dt], int(grad_dtype), ws, nbytes)
     return g
 
 
@@ -571,12 +572,12 @@ def _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state_in,
         _need(len(lead) == 1, where, "x must be [S, D]")
         S = T
     G, N = gn = b.shape[-2:]
-    row = (D,)
-    px, xs = _rows(x, where, "x", lead, kind, dev, row)
-    pdt, dts = _rows(dt, where, "dt", lead, kind, dev, row)
-    pb, bs = _rows(b, where, "b", lead, kind, dev, gn)
-    pc, cs = _rows(c, where, "c", lead, kind, dev, gn)
-    pz, zs = (None, 0) if z is None else _rows(z, where, "z", lead, kind, dev, row)
+    row, shape, g_shape = (D,), x.shape, lead + gn
+    px, xs = _rows(x, where, "x", lead, kind, dev, row, shape)
+    pdt, dts = _rows(dt, where, "dt", lead, kind, dev, row, shape)
+    pb, bs = _rows(b, where, "b", lead, kind, dev, gn, g_shape)
+    pc, cs = _rows(c, where, "c", lead, kind, dev, gn, g_shape)
+    pz, zs = (None, 0) if z is None else _rows(z, where, "z", lead, kind, dev, row, shape)
     return SelscanArgs(px, pdt, pb, pc, pz, xs, dts, bs, cs, zs, _flat(a, where, "a", (D, N), f32, dev),
                        _flat(d_skip, where, "d_skip", row, f32, dev), _flat(dt_bias, where, "dt_bias", row, f32, dev),
                        _flat(state_in, where, "state", (S, D, N), f32, dev), off, S, T, D, N, G, int(bool(softplus)), _DTYPES[kind]), dev
@@ -600,13 +601,11 @@ def selscan_fwd(x, dt, a, b, c, d_skip=None, z=None, dt_bias=None, softplus=True
     """chela_selscan_fwd: (y, state_out).  x, dt, z [T,D] or [B,L,D]; a [D,N] f32; b, c [...,G,N]; states [S,D,N] f32."""
     where = "chela_selscan_fwd"
     r, dev = _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state_in, seq_offsets)
-    y = _new(out, where, "out", x.shape, x.dtype if out_dtype is None else _tdtype(out_dtype), x.device, dev)
+    y = _new_like(out, where, "out", x, x.dtype if out_dtype is None else _tdtype(out_dtype), dev)
     state_out = _new(state_out, where, "state_out", (r.S, r.D, r.N), torch.float32, x.device, dev)
     ckpt = _checkpoints(checkpoints, where, r, dev)
     ws, nbytes = _scratch(lib().chela_selscan_workspace_bytes(r.T, r.S, r.D, r.N), workspace, x.device, where, dev)
-    with _on(dev):
-        _check(lib().chela_selscan_fwd(ctypes.byref(r), y.data_ptr(), state_out.data_ptr(), ckpt, _DTYPES[y.dtype], ws, nbytes,
-                                       _raw_stream(dev)), where)
+    _run(lib().chela_selscan_fwd, where, dev, ctypes.byref(r), y.data_ptr(), state_out.data_ptr(), ckpt, _DTYPES[y.dtype], ws, nbytes)
     return y, state_out
 
 
@@ -616,10 +615,9 @@ def selscan_step(x, dt, a, b, c, state, d_skip=None, z=None, dt_bias=None, softp
     is given."""
     where = "chela_selscan_step"
     r, dev = _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state, None, True)
-    y = _new(out, where, "out", x.shape, x.dtype if out_dtype is None else _tdtype(out_dtype), x.device, dev)
+    y = _new_like(out, where, "out", x, x.dtype if out_dtype is None else _tdtype(out_dtype), dev)
     after = state.data_ptr() if state_out is None else _flat(state_out, where, "state_out", (r.S, r.D, r.N), torch.float32, dev)
-    with _on(dev):
-        _check(lib().chela_selscan_step(ctypes.byref(r), y.data_ptr(), after, _DTYPES[y.dtype], _raw_stream(dev)), where)
+    _run(lib().chela_selscan_step, where, dev, ctypes.byref(r), y.data_ptr(), after, _DTYPES[y.dtype])
     return y
 
 
@@ -636,10 +634,9 @@ def selscan_bwd(x, dt, a, b, c, d_y, d_skip=None, z=None, dt_bias=None, softplus
                      d_skip=None if d_skip is None else new((r.D,), f32), d_z=None if z is None else new(x.shape, gt),
                      d_dt_bias=None if dt_bias is None else new((r.D,), f32), d_state_in=new(held, f32) if want_d_state else None)
     ws, nbytes = _scratch(lib().chela_selscan_bwd_workspace_bytes(r.T, r.S, r.D, r.N, int(ckpt is not None)), workspace, device, where, dev)
-    with _on(dev):
-        _check(lib().chela_selscan_bwd(ctypes.byref(r), pdy, dys, _flat(d_state_out, where, "d_state_out", held, f32, dev), ckpt,
-                                       _ptr(g.d_x), _ptr(g.d_dt), _ptr(g.d_a), _ptr(g.d_b), _ptr(g.d_c), _ptr(g.d_skip), _ptr(g.d_z),
-                                       _ptr(g.d_dt_bias), _ptr(g.d_state_in), int(grad_dtype), ws, nbytes, _raw_stream(dev)), where)
+    _run(lib().chela_selscan_bwd, where, dev, ctypes.byref(r), pdy, dys, _flat(d_state_out, where, "d_state_out", held, f32, dev), ckpt,
+         _ptr(g.d_x), _ptr(g.d_dt), _ptr(g.d_a), _ptr(g.d_b), _ptr(g.d_c), _ptr(g.d_skip), _ptr(g.d_z), _ptr(g.d_dt_bias),
+         _ptr(g.d_state_in), int(grad_dtype), ws, nbytes)
     return g
 
 
@@ -648,19 +645,20 @@ def _blocknorm_args(where, res, y, gate, w_post, b_post, norm_post, scale, w_pre
     first = res if res is not None else y
     _need(first is not None, where, "res or y must be given")
     lead, _, T, _, dev = _seqs(first, None, where)
-    D, f32 = first.shape[-1], torch.float32
+    shape, f32 = first.shape, torch.float32
+    D = shape[-1]
     row = (D,)
-    pr, rs = (None, 0) if res is None else _rows(res, where, "res", lead, res.dtype, dev, row)
+    pr, rs = (None, 0) if res is None else _rows(res, where, "res", lead, res.dtype, dev, row, shape)
     py = pg = None
     ys = gs = 0
     kind = first.dtype
     if y is not None:
         kind = y.dtype
         _need(kind in _DTYPES, where, "y must be float32 or bfloat16")
-        py, ys = _rows(y, where, "y", lead, kind, dev, row)
+        py, ys = _rows(y, where, "y", lead, kind, dev, row, shape)
     if gate is not None:
         _need(y is not None, where, "gate goes with y")
-        pg, gs = _rows(gate, where, "gate", lead, kind, dev, row)
+        pg, gs = _rows(gate, where, "gate", lead, kind, dev, row, shape)
     return BlocknormArgs(pr, py, pg, rs, ys, gs, _flat(w_post, where, "w_post", row, f32, dev), _flat(b_post, where, "b_post", row, f32, dev),
                          _flat(scale, where, "scale", row, f32, dev), _flat(w_pre, where, "w_pre", row, f32, dev),
                          _flat(b_pre, where, "b_pre", row, f32, dev), T, D, int(gate_act), int(bool(gate_after)), int(norm_post),
@@ -675,16 +673,15 @@ def blocknorm_fwd(res, y=None, gate=None, w_post=None, b_post=None, norm_post=NO
     r, first, dev = _blocknorm_args(where, res, y, gate, w_post, b_post, norm_post, scale, w_pre, b_pre, norm_pre, gate_act, gate_after, eps)
     _need(pre or y is not None, where, "nothing to compute")
     if y is not None:
-        res_out = _new(res_out, where, "res_out", first.shape, first.dtype, first.device, dev)
+        res_out = _new_like(res_out, where, "res_out", first, first.dtype, dev)
     else:
         _need(res_out is None, where, "res_out goes with y")
     o, code = None, F32
     if pre:
         dt = (y if y is not None else res).dtype if out_dtype is None else _tdtype(out_dtype)
-        o, code = _new(out, where, "out", first.shape, dt, first.device, dev), _DTYPES[dt]
-    with _on(dev):
-        _check(lib().chela_blocknorm_fwd(ctypes.byref(r), None if res_out is None else res_out.data_ptr(), None if o is None else o.data_ptr(),
-                                         code, _raw_stream(dev)), where)
+        o, code = _new_like(out, where, "out", first, dt, dev), _DTYPES[dt]
+    _run(lib().chela_blocknorm_fwd, where, dev, ctypes.byref(r), None if res_out is None else res_out.data_ptr(),
+         None if o is None else o.data_ptr(), code)
     return res_out if y is not None else res, o
 
 
@@ -702,9 +699,7 @@ def blocknorm_bwd(res_out, y=None, gate=None, d_o=None, d_res_out=None, w_post=N
                        d_gate=None if gate is None else torch.empty(shape, dtype=gt, device=device),
                        d_w_post=vec(w_post), d_b_post=vec(b_post), d_scale=vec(scale), d_w_pre=vec(w_pre), d_b_pre=vec(b_pre))
     ws, nbytes = _scratch(lib().chela_blocknorm_bwd_workspace_bytes(r.T, D), workspace, device, where, dev)
-    with _on(dev):
-        _check(lib().chela_blocknorm_bwd(ctypes.byref(r), _flat(d_o, where, "d_o", shape, kind, dev),
-                                         _flat(d_res_out, where, "d_res_out", shape, first.dtype, dev), _ptr(g.d_res), _ptr(g.d_y),
-                                         _ptr(g.d_gate), _ptr(g.d_w_post), _ptr(g.d_b_post), _ptr(g.d_scale), _ptr(g.d_w_pre),
-                                         _ptr(g.d_b_pre), int(grad_dtype), ws, nbytes, _raw_stream(dev)), where)
+    _run(lib().chela_blocknorm_bwd, where, dev, ctypes.byref(r), _flat(d_o, where, "d_o", shape, kind, dev),
+         _flat(d_res_out, where, "d_res_out", shape, first.dtype, dev), _ptr(g.d_res), _ptr(g.d_y), _ptr(g.d_gate), _ptr(g.d_w_post),
+         _ptr(g.d_b_post), _ptr(g.d_scale), _ptr(g.d_w_pre), _ptr(g.d_b_pre), int(grad_dtype), ws, nbytes)
     return g
