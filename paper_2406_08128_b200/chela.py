@@ -492,10 +492,19 @@ def _new(out, where, name, shape, dtype, device, index):
     return out
 
 
+def _like(t, dtype):
+    """An uninitialised contiguous tensor of t's shape; None for None."""
+    return None if t is None else torch.empty_like(t, dtype=dtype, memory_format=torch.contiguous_format)
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
 def _new_like(out, where, name, like, dtype, index):
     """A contiguous output of like's shape."""
     if out is None:
-        return torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format)
+        return _like(like, dtype)
     _flat(out, where, name, like.shape, dtype, index)
     return out
 
@@ -552,13 +561,13 @@ def shortconv_bwd(x, w, d_y, bias=None, act=True, state_in=None, d_state_out=Non
     px, xs = _rows(x, where, "x", lead, dt, dev, (D,), x.shape)
     pdy, dys = _rows(d_y, where, "d_y", lead, dt, dev, (D,))
     held = (S, width - 1, D)
-    g = ShortconvGrads(torch.empty(x.shape, dtype=gt, device=device), torch.empty((D, width), dtype=f32, device=device),
-                       torch.empty((D,), dtype=f32, device=device), torch.empty(held, dtype=gt, device=device) if want_d_state else None)
+    g = ShortconvGrads(_like(x, gt), _like(w, f32), torch.empty((D,), dtype=f32, device=device),
+                       torch.empty(held, dtype=gt, device=device) if want_d_state else None)
     ws, nbytes = _scratch(lib().chela_shortconv_bwd_workspace_bytes(T, D, width), workspace, device, where, dev)
     _run(lib().chela_shortconv_bwd, where, dev, px, xs, _flat(w, where, "w", (D, width), f32, dev),
          _flat(bias, where, "bias", (D,), f32, dev), pdy, dys, _flat(state_in, where, "state_in", held, dt, dev),
          _flat(d_state_out, where, "d_state_out", held, dt, dev), g.d_x.data_ptr(), g.d_w.data_ptr(), g.d_bias.data_ptr(),
-         _ptr(g.d_state_in), off, S, T, D, width, int(bool(act)), _DTYPES[dt], int(grad_dtype), ws, nbytes)
+         _at(g.d_state_in), off, S, T, D, width, int(bool(act)), _DTYPES[dt], int(grad_dtype), ws, nbytes)
     return g
 
 
@@ -629,14 +638,12 @@ def selscan_bwd(x, dt, a, b, c, d_y, d_skip=None, z=None, dt_bias=None, softplus
     device, gt, f32, held = x.device, _tdtype(grad_dtype), torch.float32, (r.S, r.D, r.N)
     pdy, dys = _rows(d_y, where, "d_y", x.shape[:-1], x.dtype, dev, (r.D,))
     ckpt = _checkpoints(checkpoints, where, r, dev)
-    new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=device)  # noqa: E731
-    g = SelscanGrads(d_x=new(x.shape, gt), d_dt=new(x.shape, gt), d_a=new(a.shape, f32), d_b=new(b.shape, gt), d_c=new(c.shape, gt),
-                     d_skip=None if d_skip is None else new((r.D,), f32), d_z=None if z is None else new(x.shape, gt),
-                     d_dt_bias=None if dt_bias is None else new((r.D,), f32), d_state_in=new(held, f32) if want_d_state else None)
+    g = SelscanGrads(d_x=_like(x, gt), d_dt=_like(dt, gt), d_a=_like(a, f32), d_b=_like(b, gt), d_c=_like(c, gt), d_skip=_like(d_skip, f32),
+                     d_z=_like(z, gt), d_dt_bias=_like(dt_bias, f32),
+                     d_state_in=torch.empty(held, dtype=f32, device=device) if want_d_state else None)
     ws, nbytes = _scratch(lib().chela_selscan_bwd_workspace_bytes(r.T, r.S, r.D, r.N, int(ckpt is not None)), workspace, device, where, dev)
     _run(lib().chela_selscan_bwd, where, dev, ctypes.byref(r), pdy, dys, _flat(d_state_out, where, "d_state_out", held, f32, dev), ckpt,
-         _ptr(g.d_x), _ptr(g.d_dt), _ptr(g.d_a), _ptr(g.d_b), _ptr(g.d_c), _ptr(g.d_skip), _ptr(g.d_z), _ptr(g.d_dt_bias),
-         _ptr(g.d_state_in), int(grad_dtype), ws, nbytes)
+         *map(_at, g), int(grad_dtype), ws, nbytes)
     return g
 
 
@@ -693,13 +700,8 @@ def blocknorm_bwd(res_out, y=None, gate=None, d_o=None, d_res_out=None, w_post=N
     r, first, dev = _blocknorm_args(where, res_out, y, gate, w_post, b_post, norm_post, scale, w_pre, b_pre, norm_pre, gate_act, gate_after, eps)
     device, shape, gt, D = first.device, first.shape, _tdtype(grad_dtype), r.D
     kind = first.dtype if y is None else y.dtype
-    vec = lambda w: None if w is None else torch.empty((D,), dtype=torch.float32, device=device)  # noqa: E731
-    g = BlocknormGrads(d_res=torch.empty(shape, dtype=first.dtype, device=device),
-                       d_y=None if y is None else torch.empty(shape, dtype=gt, device=device),
-                       d_gate=None if gate is None else torch.empty(shape, dtype=gt, device=device),
-                       d_w_post=vec(w_post), d_b_post=vec(b_post), d_scale=vec(scale), d_w_pre=vec(w_pre), d_b_pre=vec(b_pre))
+    g = BlocknormGrads(_like(first, first.dtype), _like(y, gt), _like(gate, gt), *(_like(w, torch.float32) for w in (w_post, b_post, scale, w_pre, b_pre)))
     ws, nbytes = _scratch(lib().chela_blocknorm_bwd_workspace_bytes(r.T, D), workspace, device, where, dev)
     _run(lib().chela_blocknorm_bwd, where, dev, ctypes.byref(r), _flat(d_o, where, "d_o", shape, kind, dev),
-         _flat(d_res_out, where, "d_res_out", shape, first.dtype, dev), _ptr(g.d_res), _ptr(g.d_y), _ptr(g.d_gate), _ptr(g.d_w_post),
-         _ptr(g.d_b_post), _ptr(g.d_scale), _ptr(g.d_w_pre), _ptr(g.d_b_pre), int(grad_dtype), ws, nbytes)
+         _flat(d_res_out, where, "d_res_out", shape, first.dtype, dev), *map(_at, g), int(grad_dtype), ws, nbytes)
     return g
