@@ -650,8 +650,7 @@ chela_status_t launch_blocknorm_bwd(const chela_blocknorm_args_t &a, const void 
     q.f = norm_params(a);
     q.d_o = d_o; q.d_ro = d_res_out;
     q.d_res = d_res; q.d_y = d_y; q.d_gate = d_gate;
-    const bool rw = a.res_dtype == CHELA_F32, gw = grad_dtype == CHELA_F32;
-    q.f.wide = q.f.wide && on_sector(d_o, a.in_dtype == CHELA_F32) && on_sector(d_res_out, rw) && on_sector(d_res, rw) && on_sector(d_y, gw) && on_sector(d_gate, gw);
+    q.f.wide = q.f.wide && on_sector(d_o, a.in_dtype == CHELA_F32) && on_sector(d_res_out, a.res_dtype == CHELA_F32);   // for its loads
     q.part = static_cast<float *>(workspace);
     const NormSums sums = {d_w_post, d_b_post, d_scale, d_w_pre, d_b_pre, a.w_post, a.b_post, a.scale};
     const bool i32 = a.in_dtype == CHELA_F32, r32 = a.res_dtype == CHELA_F32, g32 = grad_dtype == CHELA_F32;

@@ -394,14 +394,10 @@ template <typename T, int W>
 chela_status_t fwd_launch(const ConvParams &p, cudaStream_t stream)
 {
     constexpr size_t smem = 2 * 4 * 256 * sizeof(Raw4<T>);
-    const auto kern = conv_carry_kernel<T, W>;
-    if (smem > 48 * 1024) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return cuda_status(e);
-    }
+    static_assert(smem <= 48 * 1024, "more has to be asked for");
     const long long items = (long long)packed_blocks(p.T, p.S, kTok) * (p.D / 4);
     const long long need = (items + 255) / 256;
-    kern<<<(unsigned)(need < 148 * 64 ? need : 148 * 64), 256, smem, stream>>>(p, items);
+    conv_carry_kernel<T, W><<<(unsigned)(need < 148 * 64 ? need : 148 * 64), 256, smem, stream>>>(p, items);
     return last_launch_status();
 }
 
