@@ -110,13 +110,14 @@ __global__ void __launch_bounds__(32 * WT, OCC) selscan_fwd_kernel(const ScanPar
         sr = seq_range(p.off, s, p.S, p.T);
         b = (int)(blk - (sr.start / p.seg + s));
         if (b < 0 || (b > 0 && b > (sr.len - 1) / p.seg)) return;
-        if (p.seg_sum && b * p.seg + p.seg >= sr.len) return;   // what a sequence's last segment ends with starts nothing
+        if (p.seg_sum && sr.len - b * p.seg <= p.seg) return;   // what a sequence's last segment ends with starts nothing
     } else {
         __shared__ int s_len[32 * WT + 1];
         s = seq_by_length(p.off, p.S, p.T, (int)blk, s_len);
         sr = seq_range(p.off, s, p.S, p.T);
     }
-    const int begin = b * p.seg, end = p.seg ? min(begin + p.seg, sr.len) : sr.len;   // tokens of the sequence
+    // tokens of the sequence (a segment's end past the sequence's could pass 31 bits: the lengths are compared, not the ends)
+    const int begin = b * p.seg, end = p.seg ? begin + min(p.seg, sr.len - begin) : sr.len;
     const bool final = end == sr.len;
     const int q = lane % R, grp = lane / R;
     const int chl = grp * CH + q % CH, ch = c0 + chl, tok0 = (q / CH) * PT;   // this lane's channel, its first token of a slice
@@ -405,9 +406,9 @@ __global__ void __launch_bounds__(128) selscan_segments_kernel(const ScanParams 
     const float a = decay_rate(p.a[(size_t)ch * N + n]);
     float h = p.state_in ? p.state_in[i] : 0.f;
     size_t k = (size_t)(sr.start / p.seg) + s;
-    for (int t = 0; t < sr.len; t += p.seg, ++k) {
+    for (int left = sr.len; left > 0; left -= p.seg, ++k) {   // tokens from here on; counted down, so that nothing passes 31 bits
         float *m = p.seg_state + (k * p.D + ch) * N + n;
-        const bool more = t + p.seg < sr.len;
+        const bool more = left > p.seg;
         const float own = more ? *m : 0.f, time = more ? p.seg_sum[k * p.D + ch] : 0.f;
         *m = h;
         h = h == 0.f ? own : fmaf(ex2(a * time), h, own);   // growth over a segment may be infinite, its product with 0 is not NaN

@@ -351,6 +351,38 @@ def test_scan_of_a_split_sequence_with_growing_states():
     close(s, want_s, mag_s, 512 * 2.0 ** -24)
 
 
+def test_scan_of_a_split_sequence_as_long_as_there_may_be():
+    """One sequence of nearly 2^31 tokens beside two of one token: its last segment ends past 2^31 if it is not cut off first.
+    The states forget what is more than a few hundred tokens back, so the last tokens alone give the same state."""
+    import ctypes
+    import torch
+    T, D, N, tail = 2 ** 31 - 4096, 8, 8, 4096
+    pattern = torch.randn(tail, D, device="cuda").bfloat16()
+    x = torch.empty(T, D, dtype=torch.bfloat16, device="cuda")   # 34 GB: all four operands
+    assert T % tail == 0
+    x.view(-1, tail, D).copy_(pattern)
+    a = -torch.arange(1, N + 1, device="cuda").float().repeat(D, 1)
+
+    def last_states(t, lengths):
+        S, out = len(lengths), torch.zeros(len(lengths), D, N, device="cuda")
+        p, off = t.data_ptr(), i32(ref.offsets(lengths))
+        r = chela.SelscanArgs(p, p, p, p, None, D, D, N, N, 0, a.data_ptr(), None, None, None, off.data_ptr(), S, t.shape[0], D, N, 1, 1,
+                              chela.BF16)
+        need = chela.lib().chela_selscan_workspace_bytes(t.shape[0], S, D, N)
+        ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+        assert chela.lib().chela_selscan_fwd(ctypes.byref(r), None, out.data_ptr(), None, chela.F32, ws.data_ptr(), need,
+                                             torch.cuda.current_stream().cuda_stream) == chela.OK
+        torch.cuda.synchronize()
+        return need, out
+
+    need, got = last_states(x, [T - 2, 1, 1])
+    assert need > 0
+    _, want = last_states(pattern, [tail - 2, 1, 1])
+    # the decays of the first 64 tokens of the tail alone (time steps of 0.8 on average) leave nothing of what was before them;
+    # both runs then apply the same operations to the same operands and what an older rounding left has decayed too
+    assert torch.isfinite(got).all() and (got - want).abs().max().item() <= 2.0 ** -20 * want.abs().max().item()
+
+
 def test_scan_keeps_what_is_not_finite_where_it_is():
     """NaN and infinities of one sequence stay in it; an infinitely fast decay forgets the state and nothing else."""
     lengths, D, N = [20, 33, 9], 16, 16
