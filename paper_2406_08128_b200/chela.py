@@ -510,14 +510,16 @@ def _new_like(out, where, name, like, dtype, index):
 
 
 def _scratch(need, workspace, device, where, index):
-    """(address, bytes) of a call's workspace, allocated here unless the caller brings one."""
+    """A call's workspace (allocated here unless the caller brings one), its address and its bytes.  The caller keeps the
+    tensor until the library's function has returned: that runs without the interpreter's lock, and a block given back
+    before could go to another thread whose work is queued before the call's kernels, or between them."""
     if workspace is None:
         if need == 0:
-            return None, 0
+            return None, None, 0
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
     elif workspace.get_device() != index or not workspace.is_contiguous():
         _need(False, where, "workspace must be contiguous and on device %d" % index)
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def shortconv_carry_fwd(x, w, bias=None, act=True, state_in=None, state_out=None, seq_offsets=None, out=None):
@@ -563,7 +565,7 @@ def shortconv_bwd(x, w, d_y, bias=None, act=True, state_in=None, d_state_out=Non
     held = (S, width - 1, D)
     g = ShortconvGrads(_like(x, gt), _like(w, f32), torch.empty((D,), dtype=f32, device=device),
                        torch.empty(held, dtype=gt, device=device) if want_d_state else None)
-    ws, nbytes = _scratch(lib().chela_shortconv_bwd_workspace_bytes(T, D, width), workspace, device, where, dev)
+    workspace, ws, nbytes = _scratch(lib().chela_shortconv_bwd_workspace_bytes(T, D, width), workspace, device, where, dev)
     _run(lib().chela_shortconv_bwd, where, dev, px, xs, _flat(w, where, "w", (D, width), f32, dev),
          _flat(bias, where, "bias", (D,), f32, dev), pdy, dys, _flat(state_in, where, "state_in", held, dt, dev),
          _flat(d_state_out, where, "d_state_out", held, dt, dev), g.d_x.data_ptr(), g.d_w.data_ptr(), g.d_bias.data_ptr(),
@@ -613,7 +615,7 @@ def selscan_fwd(x, dt, a, b, c, d_skip=None, z=None, dt_bias=None, softplus=True
     y = _new_like(out, where, "out", x, x.dtype if out_dtype is None else _tdtype(out_dtype), dev)
     state_out = _new(state_out, where, "state_out", (r.S, r.D, r.N), torch.float32, x.device, dev)
     ckpt = _checkpoints(checkpoints, where, r, dev)
-    ws, nbytes = _scratch(lib().chela_selscan_workspace_bytes(r.T, r.S, r.D, r.N), workspace, x.device, where, dev)
+    workspace, ws, nbytes = _scratch(lib().chela_selscan_workspace_bytes(r.T, r.S, r.D, r.N), workspace, x.device, where, dev)
     _run(lib().chela_selscan_fwd, where, dev, ctypes.byref(r), y.data_ptr(), state_out.data_ptr(), ckpt, _DTYPES[y.dtype], ws, nbytes)
     return y, state_out
 
@@ -641,7 +643,7 @@ def selscan_bwd(x, dt, a, b, c, d_y, d_skip=None, z=None, dt_bias=None, softplus
     g = SelscanGrads(d_x=_like(x, gt), d_dt=_like(dt, gt), d_a=_like(a, f32), d_b=_like(b, gt), d_c=_like(c, gt), d_skip=_like(d_skip, f32),
                      d_z=_like(z, gt), d_dt_bias=_like(dt_bias, f32),
                      d_state_in=torch.empty(held, dtype=f32, device=device) if want_d_state else None)
-    ws, nbytes = _scratch(lib().chela_selscan_bwd_workspace_bytes(r.T, r.S, r.D, r.N, int(ckpt is not None)), workspace, device, where, dev)
+    workspace, ws, nbytes = _scratch(lib().chela_selscan_bwd_workspace_bytes(r.T, r.S, r.D, r.N, int(ckpt is not None)), workspace, device, where, dev)
     _run(lib().chela_selscan_bwd, where, dev, ctypes.byref(r), pdy, dys, _flat(d_state_out, where, "d_state_out", held, f32, dev), ckpt,
          *map(_at, g), int(grad_dtype), ws, nbytes)
     return g
@@ -701,7 +703,7 @@ def blocknorm_bwd(res_out, y=None, gate=None, d_o=None, d_res_out=None, w_post=N
     device, shape, gt, D = first.device, first.shape, _tdtype(grad_dtype), r.D
     kind = first.dtype if y is None else y.dtype
     g = BlocknormGrads(_like(first, first.dtype), _like(y, gt), _like(gate, gt), *(_like(w, torch.float32) for w in (w_post, b_post, scale, w_pre, b_pre)))
-    ws, nbytes = _scratch(lib().chela_blocknorm_bwd_workspace_bytes(r.T, D), workspace, device, where, dev)
+    workspace, ws, nbytes = _scratch(lib().chela_blocknorm_bwd_workspace_bytes(r.T, D), workspace, device, where, dev)
     _run(lib().chela_blocknorm_bwd, where, dev, ctypes.byref(r), _flat(d_o, where, "d_o", shape, kind, dev),
          _flat(d_res_out, where, "d_res_out", shape, first.dtype, dev), *map(_at, g), int(grad_dtype), ws, nbytes)
     return g

@@ -166,6 +166,40 @@ def test_the_binding_refuses_what_does_not_fit(lib):
         chela._flat(torch.zeros(4, 8)[:, :4], where, "t", (4, 4), f, d)
 
 
+def test_a_workspace_lives_until_the_call_has_returned(lib, monkeypatch):
+    """The library's function runs without the interpreter's lock, so the binding holds what it allocated for it."""
+    import weakref
+    import torch
+
+    class OnDevice(torch.Tensor):   # the checks of a CPU tensor's placement pass; nothing is launched
+        is_cuda = property(lambda self: True)
+
+    made, calls = [], []
+    empty = torch.empty
+
+    def tracked(*args, **kw):
+        t = empty(*args, **kw)
+        if kw.get("dtype") is torch.uint8:
+            made.append((weakref.ref(t), t.data_ptr()))
+        return t
+
+    def run(fn, where, index, *args):
+        (alive, address), = made
+        assert alive() is not None and address in args, where
+        calls.append(where)
+
+    monkeypatch.setattr(torch, "empty", tracked)
+    monkeypatch.setattr(chela, "_run", run)
+    T, D, N = 4096, 64, 16   # split: the forward scan has a workspace too
+    x = torch.zeros(T, D).as_subclass(OnDevice)
+    a, bc, w = torch.zeros(D, N), torch.zeros(T, 1, N), torch.zeros(D, 4)
+    for call in (lambda: chela.shortconv_bwd(x, w, x), lambda: chela.selscan_fwd(x, x, a, bc, bc), lambda: chela.selscan_bwd(x, x, a, bc, bc, x),
+                 lambda: chela.blocknorm_bwd(x, x, d_o=x)):
+        made.clear()
+        call()
+    assert calls == ["chela_shortconv_bwd", "chela_selscan_fwd", "chela_selscan_bwd", "chela_blocknorm_bwd"]
+
+
 def test_plain_forms_agree_with_differences():
     """The float64 gradients of the reference against central differences of its forward forms."""
     rng = np.random.default_rng(0)
