@@ -411,6 +411,7 @@ def mixer_gated_fwd(x, w_short, k_long, w_q, w_k, w_v, w_a, w_o, H, chunk=64, b_
 ShortconvGrads = collections.namedtuple("ShortconvGrads", "d_x d_w d_bias d_state_in")
 SelscanGrads = collections.namedtuple("SelscanGrads", "d_x d_dt d_a d_b d_c d_skip d_z d_dt_bias d_state_in")
 _MAX_TOKENS = 2 ** 31 - 4096
+_MAX_INT = 2 ** 31 - 1   # of the sizes that the C entry points take as int
 BlocknormGrads = collections.namedtuple("BlocknormGrads", "d_res d_y d_gate d_w_post d_b_post d_scale d_w_pre d_b_pre")
 
 
@@ -447,6 +448,13 @@ def _rows(t, where, name, lead, dtype, index, inner, shape=None):
     return t.data_ptr(), stride
 
 
+def _width(w, where):
+    """The number of taps of short kernels [D, width]."""
+    if w.dim() != 2 or not 1 <= w.shape[1] <= _MAX_INT:
+        _need(False, where, "w is [D, width] with a width of at least 1")
+    return w.shape[1]
+
+
 def _flat(t, where, name, shape, dtype, index):
     """Address of an optional contiguous tensor of the given shape."""
     if t is None:
@@ -462,14 +470,14 @@ def _seqs(x, seq_offsets, where):
     if x.dtype not in _DTYPES or len(lead) not in (1, 2):
         _need(False, where, "tokens must be [T, D] or [B, L, D] of float32 or bfloat16")
     T = lead[0] if len(lead) == 1 else lead[0] * lead[1]
-    if T > _MAX_TOKENS:   # before ctypes cuts it to 32 bits
-        _need(False, where, "%d tokens, at most %d" % (T, _MAX_TOKENS))
+    if T > _MAX_TOKENS or x.shape[-1] > _MAX_INT:   # before ctypes cuts them to 32 bits
+        _need(False, where, "%d tokens, at most %d, of %d channels, at most %d" % (T, _MAX_TOKENS, x.shape[-1], _MAX_INT))
     if not x.is_cuda:
         _need(False, where, "tensors must be on a CUDA device (there is no CPU fallback)")
     index = x.get_device()
     if seq_offsets is None:
         return lead, 1 if len(lead) == 1 else lead[0], T, None, index
-    _need(len(lead) == 1 and seq_offsets.dim() == 1 and seq_offsets.shape[0] >= 2, where,
+    _need(len(lead) == 1 and seq_offsets.dim() == 1 and 2 <= seq_offsets.shape[0] <= _MAX_INT, where,
           "seq_offsets [S + 1] goes with packed tokens [T, D]")
     return lead, seq_offsets.shape[0] - 1, T, _flat(seq_offsets, where, "seq_offsets", seq_offsets.shape, torch.int32, index), index
 
@@ -526,7 +534,7 @@ def shortconv_carry_fwd(x, w, bias=None, act=True, state_in=None, state_out=None
     """chela_shortconv_carry_fwd: (y, state_out).  x [T,D] or [B,L,D]; w [D,width] f32; states [S,width-1,D] like x."""
     where, f32 = "chela_shortconv_carry_fwd", torch.float32
     lead, S, T, off, dev = _seqs(x, seq_offsets, where)
-    D, width, dt = x.shape[-1], w.shape[-1], x.dtype
+    D, width, dt = x.shape[-1], _width(w, where), x.dtype
     px, xs = _rows(x, where, "x", lead, dt, dev, (D,), x.shape)
     y = _new_like(out, where, "out", x, dt, dev)
     held = (S, width - 1, D)
@@ -543,7 +551,7 @@ def shortconv_step(x, w, state, bias=None, act=True, state_out=None, out=None):
     where, f32 = "chela_shortconv_step", torch.float32
     lead, _, S, _, dev = _seqs(x, None, where)
     _need(len(lead) == 1, where, "x must be [S, D]")
-    D, width, dt = x.shape[-1], w.shape[-1], x.dtype
+    D, width, dt = x.shape[-1], _width(w, where), x.dtype
     px, xs = _rows(x, where, "x", lead, dt, dev, (D,), x.shape)
     y = _new_like(out, where, "out", x, dt, dev)
     held = (S, width - 1, D)
@@ -559,7 +567,7 @@ def shortconv_bwd(x, w, d_y, bias=None, act=True, state_in=None, d_state_out=Non
     """chela_shortconv_bwd: ShortconvGrads; d_x (and d_state_in, if wanted) of grad_dtype, d_w and d_bias f32."""
     where, f32 = "chela_shortconv_bwd", torch.float32
     lead, S, T, off, dev = _seqs(x, seq_offsets, where)
-    D, width, dt, gt, device = x.shape[-1], w.shape[-1], x.dtype, _tdtype(grad_dtype), x.device
+    D, width, dt, gt, device = x.shape[-1], _width(w, where), x.dtype, _tdtype(grad_dtype), x.device
     px, xs = _rows(x, where, "x", lead, dt, dev, (D,), x.shape)
     pdy, dys = _rows(d_y, where, "d_y", lead, dt, dev, (D,))
     held = (S, width - 1, D)
@@ -583,6 +591,8 @@ def _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state_in,
         _need(len(lead) == 1, where, "x must be [S, D]")
         S = T
     G, N = gn = b.shape[-2:]
+    if G * N > _MAX_INT:
+        _need(False, where, "b and c have %d x %d values a token" % (G, N))
     row, shape, g_shape = (D,), x.shape, lead + gn
     px, xs = _rows(x, where, "x", lead, kind, dev, row, shape)
     pdt, dts = _rows(dt, where, "dt", lead, kind, dev, row, shape)

@@ -200,6 +200,31 @@ def test_a_workspace_lives_until_the_call_has_returned(lib, monkeypatch):
     assert calls == ["chela_shortconv_bwd", "chela_selscan_fwd", "chela_selscan_bwd", "chela_blocknorm_bwd"]
 
 
+def test_sizes_that_ctypes_would_cut_are_refused(lib, monkeypatch):
+    """Channels, sequences, groups and taps past 31 bits: 2^32 + 64 channels would be taken for 64."""
+    import torch
+
+    class OnDevice(torch.Tensor):
+        is_cuda = property(lambda self: True)
+
+    monkeypatch.setattr(chela, "_run", lambda *a: pytest.fail("the library was called"))
+    huge = 2 ** 32 + 64
+    on = lambda t: t.as_subclass(OnDevice)  # noqa: E731
+    x = on(torch.zeros(4, 64))
+    wide = on(torch.zeros(1).expand(4, huge))
+    a, bc = torch.zeros(64, 8), torch.zeros(4, 1, 8)
+    for call in (lambda: chela.blocknorm_fwd(wide),
+                 lambda: chela.shortconv_carry_fwd(wide, torch.zeros(1).expand(huge, 4)),
+                 lambda: chela.shortconv_step(x, torch.zeros(1).expand(64, huge), torch.zeros(4, 3, 64)),
+                 lambda: chela.shortconv_bwd(x, torch.zeros(64, 0), x),
+                 lambda: chela.shortconv_carry_fwd(x, torch.zeros(64)),
+                 lambda: chela.shortconv_carry_fwd(x, torch.zeros(64, 4), seq_offsets=torch.zeros(1, dtype=torch.int32).expand(huge)),
+                 lambda: chela.selscan_fwd(x, x, a, torch.zeros(1).expand(4, huge, 8), bc)):
+        with pytest.raises(chela.ChelaError) as e:
+            call()
+        assert e.value.status == chela.ERR_INVALID_ARG
+
+
 def test_plain_forms_agree_with_differences():
     """The float64 gradients of the reference against central differences of its forward forms."""
     rng = np.random.default_rng(0)
