@@ -42,6 +42,14 @@ chela_status_t check_conv(const void *x, long long x_stride, const float *w, con
     return stride_ok(x_stride, D) ? CHELA_OK : CHELA_ERR_INVALID_ARG;
 }
 
+// y and state_out lie in no operand's buffer, but for state_out in state_in's
+bool conv_outputs_ok(const void *x, const void *w, const void *bias, const void *y, const void *state_in, const void *state_out,
+                     const void *seq_offsets, int width)
+{
+    if (width == 1) state_in = state_out = nullptr;   // ignored
+    return distinct({y, state_out}, {x, w, bias, seq_offsets}) && distinct({y}, {state_in});
+}
+
 chela_status_t check_scan(const chela_selscan_args_t *a)
 {
     if (!a || !a->x || !a->dt || !a->b || !a->c || !a->a || a->D < 1 || a->N < 1 || a->G < 1 || !dtype_ok(a->in_dtype) ||
@@ -59,6 +67,13 @@ chela_status_t check_scan(const chela_selscan_args_t *a)
         (a->z && !stride_ok(a->z_stride, a->D)))
         return CHELA_ERR_INVALID_ARG;
     return CHELA_OK;
+}
+
+// no output lies in the buffer of an operand other than the state
+template <size_t A>
+bool scan_outputs_ok(const chela_selscan_args_t &a, const void *const (&outs)[A])
+{
+    return distinct(outs, {a.x, a.dt, a.b, a.c, a.z, a.a, a.d_skip, a.dt_bias, a.seq_offsets});
 }
 
 bool norm_kind_ok(chela_norm_t n) { return n == CHELA_NORM_NONE || n == CHELA_NORM_RMS || n == CHELA_NORM_LAYER; }
@@ -89,7 +104,7 @@ chela_status_t chela_shortconv_carry_fwd(const void *x, long long x_stride, cons
 {
     const chela_status_t st = check_conv(x, x_stride, w, bias, state_in, state_out, seq_offsets, S, T, D, width, act, io_dtype);
     if (st != CHELA_OK) return st;
-    if (!y || y == x || !aligned16(y)) return CHELA_ERR_INVALID_ARG;
+    if (!y || y == x || !aligned16(y) || !conv_outputs_ok(x, w, bias, y, state_in, state_out, seq_offsets, width)) return CHELA_ERR_INVALID_ARG;
     return launch_shortconv_carry(x, x_stride, w, bias, y, state_in, state_out, seq_offsets, S, T, D, width, act, io_dtype, stream);
 }
 
@@ -99,7 +114,9 @@ chela_status_t chela_shortconv_step(const void *x, long long x_stride, const flo
 {
     const chela_status_t st = check_conv(x, x_stride, w, bias, state_in, state_out, nullptr, S, S, D, width, act, io_dtype);
     if (st != CHELA_OK) return st;
-    if (!y || y == x || !aligned16(y) || (width > 1 && (!state_in || !state_out))) return CHELA_ERR_INVALID_ARG;
+    if (!y || y == x || !aligned16(y) || (width > 1 && (!state_in || !state_out)) ||
+        !conv_outputs_ok(x, w, bias, y, state_in, state_out, nullptr, width))
+        return CHELA_ERR_INVALID_ARG;
     return launch_shortconv_step(x, x_stride, w, bias, y, state_in, state_out, S, D, width, act, io_dtype, stream);
 }
 
@@ -121,6 +138,7 @@ chela_status_t chela_shortconv_bwd(const void *x, long long x_stride, const floa
         !aligned16(d_w) || !aligned16(d_bias) || !aligned16(d_state_in) || !aligned16(workspace))
         return CHELA_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < shortconv_bwd_workspace_bytes(T, D, width)) return CHELA_ERR_WORKSPACE;
+    if (!distinct({d_x, d_w, d_bias, d_state_in}, {x, w, bias, d_y, state_in, d_state_out, seq_offsets})) return CHELA_ERR_INVALID_ARG;
     return launch_shortconv_bwd(x, x_stride, w, bias, d_y, d_y_stride, state_in, d_state_out, d_x, d_w, d_bias, d_state_in, seq_offsets, S,
                                 T, D, width, act, io_dtype, grad_dtype, workspace, stream);
 }
@@ -148,6 +166,7 @@ chela_status_t chela_selscan_fwd(const chela_selscan_args_t *args, void *y, floa
     if (!distinct({y}, {args->x, args->dt, args->b, args->c, args->z})) return CHELA_ERR_INVALID_ARG;
     const size_t need = selscan_workspace_bytes(args->T, args->S, args->D, args->N);
     if (need && (!workspace || workspace_bytes < need)) return CHELA_ERR_WORKSPACE;
+    if (!distinct({y, checkpoints}, {args->state_in}) || !scan_outputs_ok(*args, {y, state_out, checkpoints})) return CHELA_ERR_INVALID_ARG;
     return launch_selscan_fwd(*args, y, state_out, checkpoints, out_dtype, workspace, stream);
 }
 
@@ -157,7 +176,7 @@ chela_status_t chela_selscan_step(const chela_selscan_args_t *args, void *y, flo
     const chela_status_t st = check_scan(args);
     if (st != CHELA_OK) return st;
     if (args->T != args->S || args->seq_offsets || !args->state_in || !y || !state_out || !dtype_ok(out_dtype) || !aligned16(y) ||
-        !aligned16(state_out) || !distinct({y}, {args->x, args->dt, args->b, args->c, args->z}))
+        !aligned16(state_out) || !distinct({y}, {args->state_in}) || !scan_outputs_ok(*args, {y, state_out}))
         return CHELA_ERR_INVALID_ARG;
     return launch_selscan_step(*args, y, state_out, out_dtype, stream);
 }
@@ -184,6 +203,9 @@ chela_status_t chela_selscan_bwd(const chela_selscan_args_t *args, const void *d
     if (!distinct({d_x, d_dt, d_z, d_b, d_c}, {args->x, args->dt, args->z, args->b, args->c, d_y})) return CHELA_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < selscan_bwd_workspace_bytes(args->T, args->S, args->D, args->N, checkpoints != nullptr))
         return CHELA_ERR_WORKSPACE;
+    if (!scan_outputs_ok(*args, {d_x, d_dt, d_a, d_b, d_c, d_skip_grad, d_z, d_dt_bias, d_state_in}) ||
+        !distinct({d_x, d_dt, d_a, d_b, d_c, d_skip_grad, d_z, d_dt_bias, d_state_in}, {args->state_in, d_y, d_state_out, checkpoints}))
+        return CHELA_ERR_INVALID_ARG;
     return launch_selscan_bwd(*args, d_y, d_y_stride, d_state_out, checkpoints, d_x, d_dt, d_a, d_b, d_c, d_skip_grad, d_z, d_dt_bias,
                               d_state_in, grad_dtype, workspace, stream);
 }
@@ -197,6 +219,7 @@ chela_status_t chela_blocknorm_fwd(const chela_blocknorm_args_t *args, void *res
     if (res_out && (res_out == args->y || res_out == args->gate || res_out == o)) return CHELA_ERR_INVALID_ARG;
     if (res_out && res_out == args->res && args->res_stride != args->D) return CHELA_ERR_INVALID_ARG;   // rows would overlap
     if (o && (o == args->res || o == args->y || o == args->gate)) return CHELA_ERR_INVALID_ARG;
+    if (!distinct({res_out, o}, {args->w_post, args->b_post, args->scale, args->w_pre, args->b_pre})) return CHELA_ERR_INVALID_ARG;
     return launch_blocknorm_fwd(*args, res_out, o, out_dtype, stream);
 }
 
@@ -221,6 +244,10 @@ chela_status_t chela_blocknorm_bwd(const chela_blocknorm_args_t *args, const voi
     if (!distinct({d_y, d_gate}, {args->res, args->y, args->gate, d_o, d_res_out}) || !distinct({d_res}, {args->res, args->y, args->gate, d_o}))
         return CHELA_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < blocknorm_bwd_workspace_bytes(args->T, args->D)) return CHELA_ERR_WORKSPACE;
+    if (!distinct({d_res, d_y, d_gate, d_w_post, d_b_post, d_scale, d_w_pre, d_b_pre},
+                  {args->w_post, args->b_post, args->scale, args->w_pre, args->b_pre}) ||
+        !distinct({d_w_post, d_b_post, d_scale, d_w_pre, d_b_pre}, {args->res, args->y, args->gate, d_o, d_res_out}))
+        return CHELA_ERR_INVALID_ARG;
     return launch_blocknorm_bwd(*args, d_o, d_res_out, d_res, d_y, d_gate, d_w_post, d_b_post, d_scale, d_w_pre, d_b_pre, grad_dtype,
                                 workspace, stream);
 }

@@ -137,6 +137,78 @@ def test_outputs_in_operands_and_sizes_past_the_limits_are_refused(lib):
     assert lib.chela_selscan_checkpoint_bytes(T, 2 ** 31 - 1, 8, 8) == (T // 8 + 2 ** 31 - 1) * 32 * 8 * 4
 
 
+def at(i):
+    """The i-th of some addresses of their own."""
+    return ctypes.c_void_p(1 << 20 | i << 12)
+
+
+CONV = ("x", "w", "bias", "y", "state_in", "state_out", "off")
+CONV_BWD = ("x", "w", "bias", "d_y", "state_in", "d_state_out", "off", "d_x", "d_w", "d_bias", "d_state_in")
+SCAN_IN = ("x", "dt", "b", "c", "z", "a", "d_skip", "dt_bias", "state_in", "seq_offsets")
+SCAN_BWD = ("d_y", "d_state_out", "checkpoints", "d_x", "d_dt", "d_a", "d_b", "d_c", "d_skip_grad", "d_z", "d_dt_bias", "d_state_in")
+NORM_IN = ("res", "y", "gate", "w_post", "b_post", "scale", "w_pre", "b_pre")
+NORM_BWD = ("d_o", "d_res_out", "d_res", "d_y", "d_gate", "d_w_post", "d_b_post", "d_scale", "d_w_pre", "d_b_pre")
+
+
+def calls(lib):
+    """name: (call on addresses by name, operands, outputs, pairs that the header allows to be one buffer)."""
+    def conv(p):
+        return lib.chela_shortconv_carry_fwd(p["x"], 64, p["w"], p["bias"], p["y"], p["state_in"], p["state_out"], p["off"], 2, 8, 64, 4, 1, 1, null)
+
+    def conv_step(p):
+        return lib.chela_shortconv_step(p["x"], 64, p["w"], p["bias"], p["y"], p["state_in"], p["state_out"], 2, 64, 4, 1, 1, null)
+
+    def conv_bwd(p):
+        return lib.chela_shortconv_bwd(p["x"], 64, p["w"], p["bias"], p["d_y"], 64, p["state_in"], p["d_state_out"], p["d_x"], p["d_w"],
+                                       p["d_bias"], p["d_state_in"], p["off"], 2, 8, 64, 4, 1, 1, 1, at(60), BIG, null)
+
+    def scan_in(p, **kw):
+        return scan_args(**{k: p[k].value for k in SCAN_IN if k in p}, z_stride=64, **kw)
+
+    def scan(p):
+        return lib.chela_selscan_fwd(scan_in(p), p["y"], p["state_out"], p["checkpoints"], 1, at(60), BIG, null)
+
+    def scan_step(p):
+        return lib.chela_selscan_step(scan_in(p, S=4), p["y"], p["state_out"], 1, null)
+
+    def scan_bwd(p):
+        return lib.chela_selscan_bwd(scan_in(p), p["d_y"], 64, *(p[k] for k in SCAN_BWD[1:]), 0, at(60), BIG, null)
+
+    def norm_in(p):
+        return norm_args(**{k: p[k].value for k in NORM_IN})
+
+    def norm(p):
+        return lib.chela_blocknorm_fwd(norm_in(p), p["res_out"], p["o"], 1, null)
+
+    def norm_bwd(p):
+        return lib.chela_blocknorm_bwd(norm_in(p), *(p[k] for k in NORM_BWD), 0, at(60), BIG, null)
+
+    state = {("state_out", "state_in")}
+    steps = tuple(k for k in SCAN_IN if k != "seq_offsets")
+    return {"conv": (conv, CONV[:3] + ("state_in", "off"), ("y", "state_out"), state),
+            "conv_step": (conv_step, CONV[:3] + ("state_in",), ("y", "state_out"), state),
+            "conv_bwd": (conv_bwd, CONV_BWD[:7], CONV_BWD[7:], set()),
+            "scan": (scan, SCAN_IN, ("y", "state_out", "checkpoints"), state),
+            "scan_step": (scan_step, steps, ("y", "state_out"), state),
+            "scan_bwd": (scan_bwd, SCAN_IN + SCAN_BWD[:3], SCAN_BWD[3:], set()),
+            "norm": (norm, NORM_IN, ("res_out", "o"), {("res_out", "res")}),
+            "norm_bwd": (norm_bwd, NORM_IN + NORM_BWD[:2], NORM_BWD[2:], {("d_res", "d_res_out")})}
+
+
+ENTRY_POINTS = ("conv", "conv_step", "conv_bwd", "scan", "scan_step", "scan_bwd", "norm", "norm_bwd")
+
+
+@pytest.mark.parametrize("entry", ENTRY_POINTS)
+def test_no_output_may_be_an_operand(lib, entry):
+    """Every pair of an output and an operand in one buffer is refused, but for those that the header allows."""
+    call, operands, outputs, allowed = calls(lib)[entry]
+    place = {k: at(i) for i, k in enumerate(operands + outputs)}
+    for o in outputs:
+        for i in operands:
+            if (o, i) not in allowed:
+                assert call(place | {o: place[i]}) == chela.ERR_INVALID_ARG, (o, i)
+
+
 def test_the_binding_refuses_what_does_not_fit(lib):
     import torch
     x = torch.zeros(4, 64)
