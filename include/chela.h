@@ -332,7 +332,8 @@ chela_status_t chela_mixer_prepared_fwd(const void *x, const float *w_short, int
  * left as they were.  The offsets are read on the device; out of range values are clamped to [0, T], so that a bad array
  * gives undefined results but no access outside the tensors.
  * At least one token (T >= 1) and at most 2^31 - 4096; at most 2^30 sequences.  An output is never an operand's buffer,
- * except where the entry point says so.
+ * except where the entry point says so, nor another output's (CHELA_ERR_INVALID_ARG where the addresses are equal; buffers
+ * that overlap otherwise are not noticed).
  * Token strides (`*_stride`, in elements) are the distance between consecutive tokens and at least the row's length,
  * so that an operand can be a column slice of a wider projection; they must be multiples of 8.  Outputs without a
  * stride argument are contiguous.

@@ -31,6 +31,16 @@ bool distinct(const void *const (&outs)[A], const void *const (&operands)[B])
     return true;
 }
 
+// nor may two outputs share one
+template <size_t A>
+bool all_different(const void *const (&outs)[A])
+{
+    for (size_t i = 0; i < A; ++i)
+        for (size_t j = 0; j < i; ++j)
+            if (outs[i] && outs[i] == outs[j]) return false;
+    return true;
+}
+
 chela_status_t check_conv(const void *x, long long x_stride, const float *w, const float *bias, const void *state_in,
                           const void *state_out, const int *seq_offsets, int S, int T, int D, int width, int act, chela_dtype_t io_dtype)
 {
@@ -47,7 +57,7 @@ bool conv_outputs_ok(const void *x, const void *w, const void *bias, const void 
                      const void *seq_offsets, int width)
 {
     if (width == 1) state_in = state_out = nullptr;   // ignored
-    return distinct({y, state_out}, {x, w, bias, seq_offsets}) && distinct({y}, {state_in});
+    return distinct({y, state_out}, {x, w, bias, seq_offsets}) && distinct({y}, {state_in}) && all_different({y, state_out});
 }
 
 chela_status_t check_scan(const chela_selscan_args_t *a)
@@ -69,11 +79,11 @@ chela_status_t check_scan(const chela_selscan_args_t *a)
     return CHELA_OK;
 }
 
-// no output lies in the buffer of an operand other than the state
+// no output lies in the buffer of an operand other than the state, or in another output's
 template <size_t A>
 bool scan_outputs_ok(const chela_selscan_args_t &a, const void *const (&outs)[A])
 {
-    return distinct(outs, {a.x, a.dt, a.b, a.c, a.z, a.a, a.d_skip, a.dt_bias, a.seq_offsets});
+    return distinct(outs, {a.x, a.dt, a.b, a.c, a.z, a.a, a.d_skip, a.dt_bias, a.seq_offsets}) && all_different(outs);
 }
 
 bool norm_kind_ok(chela_norm_t n) { return n == CHELA_NORM_NONE || n == CHELA_NORM_RMS || n == CHELA_NORM_LAYER; }
@@ -138,7 +148,9 @@ chela_status_t chela_shortconv_bwd(const void *x, long long x_stride, const floa
         !aligned16(d_w) || !aligned16(d_bias) || !aligned16(d_state_in) || !aligned16(workspace))
         return CHELA_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < shortconv_bwd_workspace_bytes(T, D, width)) return CHELA_ERR_WORKSPACE;
-    if (!distinct({d_x, d_w, d_bias, d_state_in}, {x, w, bias, d_y, state_in, d_state_out, seq_offsets})) return CHELA_ERR_INVALID_ARG;
+    if (!distinct({d_x, d_w, d_bias, d_state_in}, {x, w, bias, d_y, state_in, d_state_out, seq_offsets}) ||
+        !all_different({d_x, d_w, d_bias, d_state_in}))
+        return CHELA_ERR_INVALID_ARG;
     return launch_shortconv_bwd(x, x_stride, w, bias, d_y, d_y_stride, state_in, d_state_out, d_x, d_w, d_bias, d_state_in, seq_offsets, S,
                                 T, D, width, act, io_dtype, grad_dtype, workspace, stream);
 }
@@ -246,7 +258,8 @@ chela_status_t chela_blocknorm_bwd(const chela_blocknorm_args_t *args, const voi
     if (!workspace || workspace_bytes < blocknorm_bwd_workspace_bytes(args->T, args->D)) return CHELA_ERR_WORKSPACE;
     if (!distinct({d_res, d_y, d_gate, d_w_post, d_b_post, d_scale, d_w_pre, d_b_pre},
                   {args->w_post, args->b_post, args->scale, args->w_pre, args->b_pre}) ||
-        !distinct({d_w_post, d_b_post, d_scale, d_w_pre, d_b_pre}, {args->res, args->y, args->gate, d_o, d_res_out}))
+        !distinct({d_w_post, d_b_post, d_scale, d_w_pre, d_b_pre}, {args->res, args->y, args->gate, d_o, d_res_out}) ||
+        !all_different({d_res, d_y, d_gate, d_w_post, d_b_post, d_scale, d_w_pre, d_b_pre}))
         return CHELA_ERR_INVALID_ARG;
     return launch_blocknorm_bwd(*args, d_o, d_res_out, d_res, d_y, d_gate, d_w_post, d_b_post, d_scale, d_w_pre, d_b_pre, grad_dtype,
                                 workspace, stream);

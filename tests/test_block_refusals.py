@@ -209,6 +209,15 @@ def test_no_output_may_be_an_operand(lib, entry):
                 assert call(place | {o: place[i]}) == chela.ERR_INVALID_ARG, (o, i)
 
 
+@pytest.mark.parametrize("entry", ENTRY_POINTS)
+def test_no_two_outputs_may_be_one_buffer(lib, entry):
+    call, operands, outputs, _ = calls(lib)[entry]
+    place = {k: at(i) for i, k in enumerate(operands + outputs)}
+    for n, o in enumerate(outputs):
+        for other in outputs[:n]:
+            assert call(place | {o: place[other]}) == chela.ERR_INVALID_ARG, (o, other)
+
+
 def test_the_binding_refuses_what_does_not_fit(lib):
     import torch
     x = torch.zeros(4, 64)
