@@ -62,11 +62,47 @@ __device__ __forceinline__ float ex2(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Added to the exponent of a decay 2^x that a recurrence multiplies up.  Measured over a million arguments a range, the
-// approximate exponential is low by 0.29 to 0.43 steps of 2^-24 on average for x in -0.5 .. -0.001 (0.5 to 0.7 rms), and
-// over the thousand tokens that a slow state remembers the average adds up where the rest does not.  0.3 steps of 2^-24,
-// over ln 2, cancel it: the states' error falls by half (gradients of a: 1.6e-6 -> 8e-7), and 2^x at x = 0 stays 1.
-constexpr float kDecayShift = 2.6e-8f;
+// Added to the exponent x of a decay 2^x that a recurrence multiplies up.  Over the tokens that a slow state remembers the
+// mean error of the approximate exponential adds up where the rest of it does not.  Mean errors measured over a million
+// arguments an octave, in steps of 2^-24:
+//     -x                      2^-19 .. 2^-8    2^-8 .. 2^-1    2^-1 .. 1    above 1
+//     as it is                -0.17 .. -0.09   -0.44 .. -0.26  -0.42        -0.83 .. -0.85
+//     kDecayShift             +0.13 .. +0.22   -0.14 .. +0.04  -0.11        -0.53
+//     kSlowDecayShift         -0.05 .. +0.03   -0.33 .. -0.15  -0.30        -0.72
+// so exponents closer to zero than kSlowExponent get the smaller one.  Closer to zero than 2^-19 the mean errors with that
+// one are -0.12 (2^-20), -0.06 (2^-21), -0.22 (2^-22); below 2^-23 the exponential is 1.  Growing states (x > 0, errors of
+// +0.12 and more as it is) get none.  2^x at x = 0 stays 1.
+constexpr float kDecayShift = 2.6e-8f, kSlowDecayShift = 1.0e-8f, kSlowExponent = 0x1p-8f;
+__device__ __forceinline__ float decay(float rate, float dt)
+{
+    const float x = rate * dt, shift = x < -kSlowExponent ? kDecayShift : kSlowDecayShift;
+    return ex2(fmaf(rate, dt, x < 0.f ? shift : 0.f));
+}
+// The same for the states that a lane holds of one channel and for a few tokens in a row, with one choice for all of them:
+// that of the slowest state at the first of the tokens.  A fast state forgets the error; and where the first token is a
+// fast one, every state forgets within a few hundred groups of tokens what the larger shift does to the slower ones.  (8 x
+// 8192 x 1024, N = 16: 550 us, with a choice for every token 556 to 612, with one constant for all exponents 537.)  No shift where one of the rates is above zero; a time step below zero is not
+// looked for.
+struct DecayShift {
+    float slow_below, slow;   // time steps below the first: the second, others kDecayShift
+    template <int NP>
+    __device__ __forceinline__ void set(const float2 (&rates)[NP])
+    {
+        float least = fabsf(rates[0].x), most = rates[0].x;
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+            least = fminf(least, fminf(fabsf(rates[k].x), fabsf(rates[k].y)));
+            most = fmaxf(most, fmaxf(rates[k].x, rates[k].y));
+        }
+        slow_below = most > 0.f ? INFINITY : kSlowExponent / least;
+        slow = most > 0.f ? 0.f : kSlowDecayShift;
+    }
+    __device__ __forceinline__ float2 at(float dt) const
+    {
+        const float v = dt < slow_below ? slow : kDecayShift;
+        return make_float2(v, v);
+    }
+};
 __device__ __forceinline__ float rcp_approx(float x)
 {
     float y;

@@ -136,9 +136,11 @@ __global__ void __launch_bounds__(32 * WT, OCC) selscan_fwd_kernel(const ScanPar
     // decay rates in shared memory, [CH NS / 4][32]: they are wanted before the state is, so that one takes the other's
     // registers
     __shared__ float4 s_a[CH * NP / 2][32];
+    DecayShift shift[CH];
     float2 h[CH][NP];
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
+        float2 rates[NP];
         const int cj = ch ^ j;   // pairs of channels start at even ones, so the neighbour is ch ^ 1
         const bool ok = cj < p.D;
         const size_t at = (size_t)cj * N + n0;
@@ -155,8 +157,11 @@ __global__ void __launch_bounds__(32 * WT, OCC) selscan_fwd_kernel(const ScanPar
             }
             h[j][k] = make_float2(hv.x, hv.y);
             h[j][k + 1] = make_float2(hv.z, hv.w);
+            rates[k] = make_float2(av.x, av.y);
+            rates[k + 1] = make_float2(av.z, av.w);
             if (warp == 0) s_a[j * NP / 2 + k / 2][lane] = av;
         }
+        shift[j].set(rates);
     }
     auto keep = [&](float *to, const float2 (&v)[CH][NP]) {   // states of this lane to a [D][N] array
 #pragma unroll
@@ -262,12 +267,14 @@ __global__ void __launch_bounds__(32 * WT, OCC) selscan_fwd_kernel(const ScanPar
         for (int j = 0; j < CH; ++j) {
             float2 a[NP];
             rates(j, a);
+            float2 near;
 #pragma unroll
             for (int i = 0; i < TOK; ++i) {
                 const float d = of(dt, i, j);
+                if (i == 0) near = shift[j].at(d);
 #pragma unroll
                 for (int k = 0; k < NP; ++k) {
-                    const float2 v = fma2v(a[k], splat2(d), splat2(kDecayShift));
+                    const float2 v = fma2v(a[k], splat2(d), near);
                     e[i][j][k] = make_float2(ex2(v.x), ex2(v.y));
                 }
             }
@@ -449,10 +456,10 @@ __global__ void __launch_bounds__(256) selscan_step_kernel(const ScanParams p)
     float y = 0.f;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        h[k].x = fmaf(ex2(fmaf(dt, decay_rate(a[k].x), kDecayShift)), h[k].x, dx * b[k].x);
-        h[k].y = fmaf(ex2(fmaf(dt, decay_rate(a[k].y), kDecayShift)), h[k].y, dx * b[k].y);
-        h[k].z = fmaf(ex2(fmaf(dt, decay_rate(a[k].z), kDecayShift)), h[k].z, dx * b[k].z);
-        h[k].w = fmaf(ex2(fmaf(dt, decay_rate(a[k].w), kDecayShift)), h[k].w, dx * b[k].w);
+        h[k].x = fmaf(decay(decay_rate(a[k].x), dt), h[k].x, dx * b[k].x);
+        h[k].y = fmaf(decay(decay_rate(a[k].y), dt), h[k].y, dx * b[k].y);
+        h[k].z = fmaf(decay(decay_rate(a[k].z), dt), h[k].z, dx * b[k].z);
+        h[k].w = fmaf(decay(decay_rate(a[k].w), dt), h[k].w, dx * b[k].w);
         y += fmaf(c[k].x, h[k].x, c[k].y * h[k].y) + fmaf(c[k].z, h[k].z, c[k].w * h[k].w);
     }
 #pragma unroll
@@ -596,6 +603,9 @@ __global__ void __launch_bounds__(32 * BwdShape<TI, N, CH>::WT, 1) selscan_bwd_k
 #pragma unroll
         for (int k = 0; k < NP; ++k) a[j][k] = make_float2(decay_rate(a[j][k].x), decay_rate(a[j][k].y));
     clear(da);
+    DecayShift shift[CH];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) shift[j].set(a[j]);
     const float bias = live && p.bias ? p.bias[ch] : 0.f, skip = live && p.dsk ? p.dsk[ch] : 0.f;
     float sum_skip = 0.f, sum_bias = 0.f, lost_skip = 0.f, lost_bias = 0.f;
     __syncthreads();
@@ -689,6 +699,8 @@ __global__ void __launch_bounds__(32 * BwdShape<TI, N, CH>::WT, 1) selscan_bwd_k
         for (int j = 0; j < CH; ++j)
 #pragma unroll
             for (int k = 0; k < NP; ++k) whole[j][k] = make_float2(1.f, 1.f);
+        float time[CH] = {};
+        float2 near[CH];
 #pragma unroll
         for (int u = 0; u < TOK; u += SUB) {
             if (u) put(s_keep + u / SUB * (Sh::STATE_F / 4), h);
@@ -701,14 +713,27 @@ __global__ void __launch_bounds__(32 * BwdShape<TI, N, CH>::WT, 1) selscan_bwd_k
                 for (int j = 0; j < CH; ++j) {
                     const int at = (u + i) * CPW + (chl ^ j);
                     const float2 d = splat2(s_dt[at]), x = splat2(s_dx[at]), y = splat2(s_dg[at]);
+                    if (u == 0 && i == 0) near[j] = shift[j].at(d.x);
+                    time[j] += d.x;
 #pragma unroll
                     for (int k = 0; k < NP; ++k) {
-                        const float2 v = fma2v(a[j][k], d, splat2(kDecayShift)), e = make_float2(ex2(v.x), ex2(v.y));
+                        const float2 v = fma2v(a[j][k], d, near[j]), e = make_float2(ex2(v.x), ex2(v.y));
                         h[j][k] = fma2v(e, h[j][k], mul2v(x, bv[k]));
                         whole[j][k] = mul2v(whole[j][k], e);
                         add[j][k] = fma2v(whole[j][k], mul2v(cv[k], y), add[j][k]);
                     }
                 }
+            }
+        }
+        // The tile's whole decay, from its time.  As a product it would lose k l 2^-48 at each step from (1 - k 2^-24)(1 - l
+        // 2^-24) whenever that is less than half a step, always to the same side: 0.16 steps a token at exponents of 2^-14.
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+            near[j] = shift[j].at(time[j]);
+#pragma unroll
+            for (int k = 0; k < NP; ++k) {
+                const float2 v = fma2v(a[j][k], splat2(time[j]), near[j]);
+                whole[j][k] = make_float2(ex2(v.x), ex2(v.y));
             }
         }
         // the gradient behind the tile comes in, the one before it goes on
@@ -790,9 +815,10 @@ __global__ void __launch_bounds__(32 * BwdShape<TI, N, CH>::WT, 1) selscan_bwd_k
                         dxs[i][j] = s_dx[at];
                         dgs[i][j] = s_dg[at];
                         float2 sum = make_float2(0.f, 0.f);
+                        if (i == 0) near[j] = shift[j].at(dts[i][j]);
 #pragma unroll
                         for (int k = 0; k < NP; ++k) {
-                            const float2 w = fma2v(a[j][k], splat2(dts[i][j]), splat2(kDecayShift));
+                            const float2 w = fma2v(a[j][k], splat2(dts[i][j]), near[j]);
                             e[i][j][k] = make_float2(ex2(w.x), ex2(w.y));
                             hh[j][k] = fma2v(e[i][j][k], i ? h0[j][k] : h[j][k], mul2v(splat2(dxs[i][j]), bv[k]));
                             if (i == 0) h0[j][k] = hh[j][k];

@@ -410,6 +410,38 @@ def test_scan_keeps_what_is_not_finite_where_it_is():
         assert torch.equal(y[25:30, :5], clean[25:30, :5]) and not torch.isfinite(y[31:53]).any()
 
 
+@pytest.mark.parametrize("N", [8, 16, 64])
+def test_slow_states_over_a_long_sequence(N):
+    """16384 decays 2^x with x between -2^-8 and -2^-19 multiplied up, forwards (state_in to state_out) and backwards
+    (d_state_out to d_state_in).  One decay is off by up to a step of 2^-24 or so, but the mean over the tokens may not be: the
+    library claims at most 0.06 of a step for these exponents, and a tenth is allowed here (backwards less is done: a tile's
+    decay comes from its time).  What is left is not one-sided: a rounding of the decay and one of the product or two, of at
+    most a step each, over L independent arguments, so 6 L^(1/2) for six standard deviations of one element, and the mean over
+    the 256 elements or more of an octave within that over 16.  A correction that fits x below -2^-8 only is off by 0.12 to
+    0.22 of a step here, the product of a tile's decays by 0.16 at 2^-14."""
+    import torch
+    S, L, octaves, each = 8, 16384, 11, 32
+    D, step, G = octaves * each, 2.0 ** -24, 1   # enough chains that no sequence is split
+    T = S * L
+    assert chela.lib().chela_selscan_workspace_bytes(T, S, D, N) == 0
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(N)
+    scale = 2.0 ** -torch.arange(9, 9 + octaves, device="cuda", dtype=torch.float32).repeat_interleave(each)
+    dt = (1 + torch.rand(T, D, generator=gen, device="cuda")) * scale       # |x| in 2^-(k+1) .. 2^-k with the rates below
+    a = -0.6931 * (0.98 + 0.02 * torch.rand(D, N, generator=gen, device="cuda"))
+    zero, bc = torch.zeros(T, D, device="cuda"), torch.zeros(T, G, N, device="cuda")
+    one = torch.ones(S, D, N, device="cuda")
+    _, last = chela.selscan_fwd(zero, dt, a, bc, bc, softplus=False, state_in=one, seq_offsets=i32(np.arange(S + 1) * L))
+    g = chela.selscan_bwd(zero, dt, a, bc, bc, zero, softplus=False, state_in=one, d_state_out=one, want_d_state=True,
+                          seq_offsets=i32(np.arange(S + 1) * L))
+    total = dt.view(S, L, D).double().sum(1)
+    want = torch.exp(total[:, :, None] * a.double())
+    for got in (last, g.d_state_in):
+        off = ((got.double() / want - 1) / step).view(S, octaves, each, N)
+        most, mean = off.abs().max().item(), off.mean((0, 2, 3)).abs().max().item()
+        assert most <= 0.1 * L + 6 * L ** 0.5 and mean <= 0.1 * L + 6 * L ** 0.5 / 16
+
+
 def test_scan_time_steps_down_to_tiny_ones():
     """softplus far below and above zero keeps its relative precision: one token from a zero state gives dt x b."""
     raw = np.array([-40.0, -20.0, -12.0, -7.0, -2.0, -0.5, 0.0, 0.5, 3.0, 19.0, 30.0, 88.0, -80.0, 1e-3, -1e-3, 100.0], dtype=np.float32)
