@@ -328,8 +328,9 @@ chela_status_t chela_mixer_prepared_fwd(const void *x, const float *w_short, int
  * tokens (token-major: one token's channels are contiguous).  Sequence s owns the tokens seq_offsets[s] <= t <
  * seq_offsets[s + 1]; seq_offsets is a device array of S + 1 int32, not decreasing, seq_offsets[0] = 0.  With
  * seq_offsets = NULL all sequences have T / S tokens (T a multiple of S).  Sequences may be empty: their state passes
- * through unchanged.  Tokens from seq_offsets[S] to T belong to no sequence: they are not read and their output rows are
- * left as they were.  The offsets are read on the device; out of range values are clamped to [0, T], so that a bad array
+ * through unchanged.  Tokens from seq_offsets[S] to T belong to no sequence: they are not read, their rows of gradients are
+ * zero, and their rows of outputs are left as they were, or zero where CHELA_ZERO_REST is added to the forward call's act
+ * or softplus (the other calls ignore it).  The offsets are read on the device; out of range values are clamped to [0, T], so that a bad array
  * gives undefined results but no access outside the tensors.
  * At least one token (T >= 1) and at most 2^31 - 4096; at most 2^30 sequences.  An output is never an operand's buffer,
  * except where the entry point says so, nor another output's (CHELA_ERR_INVALID_ARG where the addresses are equal; buffers
@@ -338,6 +339,10 @@ chela_status_t chela_mixer_prepared_fwd(const void *x, const float *w_short, int
  * so that an operand can be a column slice of a wider projection; they must be multiples of 8.  Outputs without a
  * stride argument are contiguous.
  *
+ */
+#define CHELA_ZERO_REST 256
+
+/*
  * Short depthwise causal convolution (chela_shortconv_fwd) over packed sequences with the inputs before the first
  * token carried in and the last ones carried out, for evaluation in segments and for decoding:
  *   u[t,c] = bias[c] + sum_{j=0}^{width-1} w[c,j] * x[t-j,c],   y = act(u)      (act: 0 identity, 1 SiLU)

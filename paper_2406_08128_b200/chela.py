@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_HERE, "libchela.so")
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = range(6)
 F32, BF16, BF16_PAIR = 0, 1, 2
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+ZERO_REST = 256   # CHELA_ZERO_REST
 
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 _lib = None
@@ -406,7 +407,8 @@ def mixer_gated_fwd(x, w_short, k_long, w_q, w_k, w_v, w_a, w_o, H, chunk=64, b_
 # Operators over packed sequences.  Token tensors are [T, D] (sequences one behind the other, with seq_offsets) or
 # [B, L, D] (B sequences of L tokens); the channel axis must be contiguous and consecutive tokens a fixed distance
 # apart, so column slices of a wider projection are taken as they are.  All tensors of a call live on one CUDA device;
-# the call runs on that device's current stream.
+# the call runs on that device's current stream.  Rows of tokens behind the last sequence (from seq_offsets[-1] on) are not
+# read; they are zero in the outputs and gradients that a call allocates and left as they were in an ``out`` that it is given.
 
 ShortconvGrads = collections.namedtuple("ShortconvGrads", "d_x d_w d_bias d_state_in")
 SelscanGrads = collections.namedtuple("SelscanGrads", "d_x d_dt d_a d_b d_c d_skip d_z d_dt_bias d_state_in")
@@ -541,7 +543,7 @@ def shortconv_carry_fwd(x, w, bias=None, act=True, state_in=None, state_out=None
     state_out = _new(state_out, where, "state_out", held, dt, x.device, dev)
     _run(lib().chela_shortconv_carry_fwd, where, dev, px, xs, _flat(w, where, "w", (D, width), f32, dev),
          _flat(bias, where, "bias", (D,), f32, dev), y.data_ptr(), _flat(state_in, where, "state_in", held, dt, dev),
-         state_out.data_ptr() or None, off, S, T, D, width, int(bool(act)), _DTYPES[dt])
+         state_out.data_ptr() or None, off, S, T, D, width, int(bool(act)) | (ZERO_REST if out is None else 0), _DTYPES[dt])
     return y, state_out
 
 
@@ -624,6 +626,8 @@ def selscan_fwd(x, dt, a, b, c, d_skip=None, z=None, dt_bias=None, softplus=True
     r, dev = _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state_in, seq_offsets)
     y = _new_like(out, where, "out", x, x.dtype if out_dtype is None else _tdtype(out_dtype), dev)
     state_out = _new(state_out, where, "state_out", (r.S, r.D, r.N), torch.float32, x.device, dev)
+    if out is None:
+        r.softplus |= ZERO_REST
     ckpt = _checkpoints(checkpoints, where, r, dev)
     workspace, ws, nbytes = _scratch(lib().chela_selscan_workspace_bytes(r.T, r.S, r.D, r.N), workspace, x.device, where, dev)
     _run(lib().chela_selscan_fwd, where, dev, ctypes.byref(r), y.data_ptr(), state_out.data_ptr(), ckpt, _DTYPES[y.dtype], ws, nbytes)

@@ -10,6 +10,8 @@ constexpr int kMaxTokens = 0x7fffffff - 4095;   // token positions and the slice
 constexpr int kMaxSeqs = 1 << 30;               // and so do the numbers of work items (tokens / 8 + sequences)
 
 bool dtype_ok(chela_dtype_t t) { return t == CHELA_F32 || t == CHELA_BF16; }
+// act or softplus: 0 or 1, and the flag
+bool switch_ok(int v) { return (v & ~CHELA_ZERO_REST) == 0 || (v & ~CHELA_ZERO_REST) == 1; }
 // token stride of an operand whose row has n elements
 bool stride_ok(long long stride, long long n) { return stride >= n && stride % 8 == 0; }
 
@@ -44,7 +46,7 @@ bool all_different(const void *const (&outs)[A])
 chela_status_t check_conv(const void *x, long long x_stride, const float *w, const float *bias, const void *state_in,
                           const void *state_out, const int *seq_offsets, int S, int T, int D, int width, int act, chela_dtype_t io_dtype)
 {
-    if (!x || !w || D < 1 || width < 1 || !dtype_ok(io_dtype) || (act != 0 && act != 1)) return CHELA_ERR_INVALID_ARG;
+    if (!x || !w || D < 1 || width < 1 || !dtype_ok(io_dtype) || !switch_ok(act)) return CHELA_ERR_INVALID_ARG;
     const chela_status_t st = check_seqs(seq_offsets, S, T);
     if (st != CHELA_OK) return st;
     if (!aligned16(x) || !aligned16(w) || !aligned16(bias) || !aligned16(state_in) || !aligned16(state_out)) return CHELA_ERR_INVALID_ARG;
@@ -63,7 +65,7 @@ bool conv_outputs_ok(const void *x, const void *w, const void *bias, const void 
 chela_status_t check_scan(const chela_selscan_args_t *a)
 {
     if (!a || !a->x || !a->dt || !a->b || !a->c || !a->a || a->D < 1 || a->N < 1 || a->G < 1 || !dtype_ok(a->in_dtype) ||
-        (a->softplus != 0 && a->softplus != 1))
+        !switch_ok(a->softplus))
         return CHELA_ERR_INVALID_ARG;
     const chela_status_t st = check_seqs(a->seq_offsets, a->S, a->T);
     if (st != CHELA_OK) return st;

@@ -35,6 +35,8 @@ __device__ __forceinline__ int packed_block_seq(const int *off, int S, int T, in
     return lo;
 }
 
+// (With S + 1 for S the tokens behind the last sequence count as one more.)
+
 // The sequence with the `rank`-th most tokens, for kernels whose CTAs walk whole sequences: the CTAs that start first get
 // the long ones, so that none of those is left for the end.  Packed sequences only, and no more of them than the CTA has
 // threads (else rank itself: the order of the array).  All threads call it; s_len has blockDim.x + 1 ints.

@@ -944,24 +944,43 @@ __global__ void __launch_bounds__(32 * BwdShape<TI, N, CH>::WT, 1) selscan_bwd_k
     }
 }
 
-// dB, dC: sum of the channel blocks' partial sums, rounded once
-template <typename TG, int N>
-__global__ void __launch_bounds__(256) selscan_bc_kernel(const float *part, void *d_b, void *d_c, const int *off, int S, int T, int G,
-                                                         int blocks_per_group)
+// Zeros in the rows of [T, D] tensors (the last two nullable) that belong to no sequence
+template <typename T_>
+__device__ __forceinline__ void zero_rest(void *a, void *b, void *c, const int *off, int S, int T, int D)
 {
+    const size_t first = (size_t)seq_start(off, S, S, T) * D;
+    for (size_t i = first + 4 * (blockIdx.x * (size_t)blockDim.x + threadIdx.x); i < (size_t)T * D; i += 4 * (size_t)gridDim.x * blockDim.x) {
+        store4(static_cast<T_ *>(a) + i, zero4());
+        if (b) store4(static_cast<T_ *>(b) + i, zero4());
+        if (c) store4(static_cast<T_ *>(c) + i, zero4());
+    }
+}
+template <typename TO>
+__global__ void __launch_bounds__(256) selscan_rest_kernel(void *y, const int *off, int S, int T, int D)
+{
+    zero_rest<TO>(y, nullptr, nullptr, off, S, T, D);
+}
+
+// dB, dC: sum of the channel blocks' partial sums, rounded once; zeros where there is no sequence, in the other gradients too
+template <typename TG, int N>
+__global__ void __launch_bounds__(256) selscan_bc_kernel(const ScanBwdParams q, void *d_b, void *d_c, int blocks_per_group)
+{
+    const float *part = q.part_bc;
+    const int *off = q.f.off, S = q.f.S, T = q.f.T, G = q.f.G;
     const size_t per_tok = (size_t)G * (2 * N / 4);
-    const int end = seq_start(off, S, S, T);
-    for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < (size_t)end * per_tok; i += (size_t)gridDim.x * blockDim.x) {
+    const size_t end = seq_start(off, S, S, T);
+    for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < (size_t)T * per_tok; i += (size_t)gridDim.x * blockDim.x) {
         const size_t t = i / per_tok;
         const int rest = (int)(i % per_tok), g = rest / (2 * N / 4), v = rest % (2 * N / 4);
         float4 o = zero4();
-        for (int k = 0; k < blocks_per_group; ++k) {
+        for (int k = 0; k < (t < end ? blocks_per_group : 0); ++k) {
             const float4 u = *reinterpret_cast<const float4 *>(part + ((size_t)(g * blocks_per_group + k) * T + t) * (2 * N) + 4 * v);
             o.x += u.x; o.y += u.y; o.z += u.z; o.w += u.w;
         }
         const bool is_c = v >= N / 4;
         store4(static_cast<TG *>(is_c ? d_c : d_b) + (t * G + g) * N + 4 * (v - (is_c ? N / 4 : 0)), o);
     }
+    if (off) zero_rest<TG>(q.d_x, q.d_dt, q.d_z, off, S, T, q.f.D);
 }
 
 // The parameters' gradients: sums over the sequences of part_a and part_d, the former's elements first
@@ -1083,7 +1102,7 @@ chela_status_t bwd_launch(const ScanBwdParams &q, void *d_b, void *d_c, float *d
     if (st != CHELA_OK) return st;
     const size_t items = (size_t)p.T * p.G * (2 * N / 4);
     const size_t grid = (items + 255) / 256;
-    selscan_bc_kernel<TG, N><<<(unsigned)(grid < 148 * 32 ? grid : 148 * 32), 256, 0, stream>>>(q.part_bc, d_b, d_c, p.off, p.S, p.T, p.G, nblk / p.G);
+    selscan_bc_kernel<TG, N><<<(unsigned)(grid < 148 * 32 ? grid : 148 * 32), 256, 0, stream>>>(q, d_b, d_c, nblk / p.G);
     st = last_launch_status();
     if (st == CHELA_OK) {
         selscan_sum_kernel<<<(unsigned)(((size_t)p.D * (N + 2) + 255) / 256), 256, 0, stream>>>(q.part_a, q.part_d, d_a, d_skip, d_bias, p.S, p.D, N);
@@ -1111,7 +1130,7 @@ ScanParams scan_params(const chela_selscan_args_t &a)
     p.a = a.a; p.dsk = a.d_skip; p.bias = a.dt_bias;
     p.state_in = a.state_in;
     p.off = a.seq_offsets;
-    p.S = a.S; p.T = a.T; p.D = a.D; p.G = a.G; p.softplus = a.softplus;
+    p.S = a.S; p.T = a.T; p.D = a.D; p.G = a.G; p.softplus = a.softplus & 1;
     return p;
 }
 
@@ -1156,6 +1175,12 @@ chela_status_t launch_selscan_fwd(const chela_selscan_args_t &a, void *y, float 
     if (p.seg) {
         p.seg_state = static_cast<float *>(workspace);
         p.seg_sum = p.seg_state + packed_blocks(a.T, a.S, p.seg) * a.D * a.N;
+    }
+    if (y && a.seq_offsets && (a.softplus & CHELA_ZERO_REST)) {   // mostly no rows or few: one CTA an SM
+        const auto rest = out_dtype == CHELA_F32 ? selscan_rest_kernel<float> : selscan_rest_kernel<__nv_bfloat16>;
+        rest<<<148, 256, 0, stream>>>(y, a.seq_offsets, a.S, a.T, a.D);
+        const chela_status_t st = last_launch_status();
+        if (st != CHELA_OK) return st;
     }
     if (a.in_dtype == CHELA_F32)
         return out_dtype == CHELA_F32 ? fwd_n<float, float>(p, a.N, stream) : fwd_n<float, __nv_bfloat16>(p, a.N, stream);

@@ -23,6 +23,7 @@ struct ConvParams {
     void *state_out;
     const int *off;
     int S, T, D, width, act;
+    int rest;   // 1: the rows of tokens of no sequence become zeros
 };
 
 __device__ __forceinline__ float4 fma4(float4 a, float4 b, float4 c)
@@ -59,6 +60,16 @@ __device__ __forceinline__ void store_state(const ConvParams &p, int s, const Se
         const float4 v = row_at<T>(p, s, sr.start, sr.len, sr.len - n + r, c);
         store4(static_cast<T *>(p.state_out) + ((size_t)s * n + r) * p.D + c, v);
     }
+}
+
+// Zeros in four channels of the rows of a block of K tokens behind the last sequence
+template <typename T>
+__device__ __forceinline__ void zero_rest(const ConvParams &p, void *rows, long long blk, int K, int c)
+{
+    const int end = seq_start(p.off, p.S, p.S, p.T);
+    const long long first = end + (blk - (end / K + p.S)) * K, last = first + K < p.T ? first + K : p.T;
+#pragma unroll 1
+    for (long long t = first; t < last; ++t) store4(static_cast<T *>(rows) + (size_t)t * p.D + c, zero4());
 }
 
 // taps[j] = (w[c][j], w[c+1][j], w[c+2][j], w[c+3][j]).  Four channels' taps are 4 width contiguous floats from a multiple
@@ -114,7 +125,11 @@ __global__ void __launch_bounds__(256, W <= 4 ? 3 : 1) conv_carry_kernel(const C
         int cv;
         split_item(idx, items, nvec, blk, cv);
         const int c = 4 * cv;
-        const int s = packed_block_seq(p.off, p.S, p.T, kTok, blk);
+        const int s = packed_block_seq(p.off, p.S + p.rest, p.T, kTok, blk);
+        if (s == p.S) {
+            zero_rest<T>(p, p.y, blk, kTok, c);
+            continue;
+        }
         const SeqRange sr = seq_range(p.off, s, p.S, p.T);
         const int b = (int)(blk - (sr.start / kTok + s));
         if (b < 0 || b > sr.len / kTok) continue;
@@ -222,7 +237,11 @@ __global__ void __launch_bounds__(256, W <= 4 ? 2 : 1) conv_bwd_kernel(const Con
         load_taps<W>(p.w, p.width, c, taps);
         if (p.bias) bias = load4(p.bias + c);
         for (long long blk = (long long)blockIdx.y * 8 + warp; blk < nblocks; blk += (long long)gridDim.y * 8) {
-            const int s = packed_block_seq(p.off, p.S, p.T, kBwdTok, blk);
+            const int s = packed_block_seq(p.off, p.S + p.rest, p.T, kBwdTok, blk);
+            if (s == p.S) {
+                zero_rest<TG>(p, q.d_x, blk, kBwdTok, c);
+                continue;
+            }
             const SeqRange sr = seq_range(p.off, s, p.S, p.T);
             const int b = (int)(blk - (sr.start / kBwdTok + s));
             if (b < 0 || sr.len == 0 || b > (sr.len - 1) / kBwdTok) continue;
@@ -395,7 +414,7 @@ chela_status_t fwd_launch(const ConvParams &p, cudaStream_t stream)
 {
     constexpr size_t smem = 2 * 4 * 256 * sizeof(Raw4<T>);
     static_assert(smem <= 48 * 1024, "more has to be asked for");
-    const long long items = (long long)packed_blocks(p.T, p.S, kTok) * (p.D / 4);
+    const long long items = (long long)packed_blocks(p.T, p.S + p.rest, kTok) * (p.D / 4);
     const long long need = (items + 255) / 256;
     conv_carry_kernel<T, W><<<(unsigned)(need < 148 * 64 ? need : 148 * 64), 256, smem, stream>>>(p, items);
     return last_launch_status();
@@ -435,7 +454,7 @@ template <typename T, typename TG>
 chela_status_t bwd_w(const ConvBwdParams &q, float *d_w, float *d_bias, cudaStream_t stream)
 {
     const ConvParams &p = q.f;
-    const long long nblocks = (long long)packed_blocks(p.T, p.S, kBwdTok);
+    const long long nblocks = (long long)packed_blocks(p.T, p.S + p.rest, kBwdTok);
     const int rows = conv_bwd_rows(p.T, p.D);
     const dim3 grid((p.D / 4 + 31) / 32, rows);
     constexpr size_t smem = 2 * 4 * 2 * 256 * sizeof(Raw4<T>);
@@ -475,14 +494,15 @@ chela_status_t launch_shortconv_carry(const void *x, long long x_stride, const f
                                       int act, chela_dtype_t io_dtype, cudaStream_t stream)
 {
     const bool held = width > 1;
-    const ConvParams p = {x, x_stride, w, bias, y, held ? state_in : nullptr, held ? state_out : nullptr, seq_offsets, S, T, D, width, act};
+    const ConvParams p = {x, x_stride, w, bias, y, held ? state_in : nullptr, held ? state_out : nullptr, seq_offsets, S, T, D, width,
+                          act & 1, seq_offsets && (act & CHELA_ZERO_REST)};
     return io_dtype == CHELA_F32 ? fwd_w<float>(p, stream) : fwd_w<__nv_bfloat16>(p, stream);
 }
 
 chela_status_t launch_shortconv_step(const void *x, long long x_stride, const float *w, const float *bias, void *y, const void *state_in,
                                      void *state_out, int S, int D, int width, int act, chela_dtype_t io_dtype, cudaStream_t stream)
 {
-    const ConvParams p = {x, x_stride, w, bias, y, state_in, state_out, nullptr, S, S, D, width, act};
+    const ConvParams p = {x, x_stride, w, bias, y, state_in, state_out, nullptr, S, S, D, width, act & 1, 0};
     return io_dtype == CHELA_F32 ? step_w<float>(p, stream) : step_w<__nv_bfloat16>(p, stream);
 }
 
@@ -498,7 +518,7 @@ chela_status_t launch_shortconv_bwd(const void *x, long long x_stride, const flo
 {
     const bool held = width > 1;
     ConvBwdParams q = {};
-    q.f = ConvParams{x, x_stride, w, bias, nullptr, held ? state_in : nullptr, nullptr, seq_offsets, S, T, D, width, act};
+    q.f = ConvParams{x, x_stride, w, bias, nullptr, held ? state_in : nullptr, nullptr, seq_offsets, S, T, D, width, act & 1, seq_offsets != nullptr};
     q.dy = d_y;
     q.dys = d_y_stride;
     q.d_state_out = held ? d_state_out : nullptr;

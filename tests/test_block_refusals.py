@@ -137,6 +137,21 @@ def test_outputs_in_operands_and_sizes_past_the_limits_are_refused(lib):
     assert lib.chela_selscan_checkpoint_bytes(T, 2 ** 31 - 1, 8, 8) == (T // 8 + 2 ** 31 - 1) * 32 * 8 * 4
 
 
+def test_the_flag_on_a_switch_leaves_other_values_refused(lib):
+    """CHELA_ZERO_REST goes with act and softplus, 0 or 1; nothing else does.  (A null stream of work is never reached: y or the
+    workspace is missing.)"""
+    bad, flag = chela.ERR_INVALID_ARG, chela.ZERO_REST
+
+    def conv(act):
+        return lib.chela_shortconv_bwd(one, 64, one, null, two, 64, null, null, three, null, null, null, null, 2, 8, 64, 4, act, 1, 0, null, 0, null)
+
+    def scan(softplus):
+        return lib.chela_selscan_bwd(scan_args(softplus=softplus), one, 64, null, null, two, two, two, two, two, null, null, null, null, 0, null, 0, null)
+    for call in (conv, scan):
+        assert call(0) == call(1) == call(flag) == call(flag + 1) == chela.ERR_WORKSPACE
+        assert call(2) == call(-1) == call(flag + 2) == call(2 * flag) == call(flag + 2 ** 31 - 512) == bad
+
+
 def at(i):
     """The i-th of some addresses of their own."""
     return ctypes.c_void_p(1 << 20 | i << 12)

@@ -620,6 +620,38 @@ def test_block_norm_of_tensors_between_sectors(D):
 
 # ------------------------------------------------------------------------------------------------ calls
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lengths,pad", [([5, 0, 33], 7), ([0, 0], 4), ([64], 1), ([70, 3], 1000), ([12, 9], 0)], ids=str)
+def test_rows_of_no_sequence_are_zero_in_what_a_call_allocates(dtype, lengths, pad):
+    """Outputs and gradients of a padded batch go on into sums over all rows.  The allocator hands back blocks of NaN here."""
+    import torch
+    n, D, N, G = sum(lengths), 64, 16, 2
+    T = n + pad
+    v = scan_inputs(5, lengths, D, N, G, dtype, pad)
+    args, kw = scan_call(v, lengths, dtype, FORMS[0])
+    x, w, bias, state, dy, _ = conv_inputs(6, lengths, D, 4, dtype, pad)
+    conv = (dev(x, dtype), f32(w))
+    off = kw["seq_offsets"]
+
+    def stale(like):
+        held = [torch.full(s, float("nan"), dtype=t, device="cuda") for s in ((T, D), (T, G, N)) for t in (torch.float32, torch.bfloat16)
+                for _ in range(6)]
+        del held
+        return like()
+
+    y, _ = stale(lambda: chela.shortconv_carry_fwd(*conv, f32(bias), state_in=dev(state, dtype), seq_offsets=off))
+    rows = [y]
+    for kind in (chela.F32, chela.BF16):
+        rows.append(stale(lambda: chela.shortconv_bwd(*conv, dev(dy, dtype), seq_offsets=off, grad_dtype=kind)).d_x)
+        rows.append(stale(lambda: chela.selscan_fwd(*args, **kw, out_dtype=kind))[0])
+        g = stale(lambda: chela.selscan_bwd(*args, dev(v["d_y"], dtype), **kw, grad_dtype=kind))
+        rows += [g.d_x, g.d_dt, g.d_b, g.d_c, g.d_z]
+    for t in rows:
+        assert t.shape[0] == T and torch.isfinite(t[:n].float()).all() and not t[n:].float().ne(0).any()
+    given = torch.full((T, D), 7.0, device="cuda")
+    chela.selscan_fwd(*args, **kw, out_dtype=chela.F32, out=given)
+    assert (given[n:] == 7).all()
+
 def test_graph_replay_streams_and_repeated_calls_give_equal_bits():
     import torch
     lengths, D, N = [40, 0, 25, 90], 64, 16
