@@ -551,6 +551,35 @@ def test_block_norms(dtype, res_dtype, T, D, post, pre, gate_act, after):
         close(g.d_b_post, w["d_b_post"], (dm * (ga if after else 1)).sum(0), many)
 
 
+@pytest.mark.parametrize("dtype,res_dtype", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("T,D", [(8003, 40), (4001, 264), (2003, 1000), (1301, 2048), (1001, 4104), (901, 8192)])
+@pytest.mark.parametrize("post,pre,gate_act,after", [(2, 2, 2, True), (1, 1, 1, False)])
+def test_block_norms_of_several_rows_a_warp(dtype, res_dtype, T, D, post, pre, gate_act, after):
+    """More rows than three CTAs an SM hold at once: rows fetched ahead, both stages, sums over rows and CTAs."""
+    warps = next(w for w in (1, 2, 4, 8, 16, 32) if w * 256 >= D)
+    assert T > 148 * 3 * max(8 // warps, 1)
+    test_block_norms(dtype, res_dtype, T, D, post, pre, gate_act, after)
+
+
+def test_block_norm_gradient_in_place_over_several_rows_a_warp():
+    """d_res in d_res_out's buffer, which the C entry point allows, with the next row's operands fetched ahead."""
+    import ctypes
+    import torch
+    for T, D in ((8003, 40), (2003, 1000), (901, 4104)):
+        res, y, gate, d_r = (torch.randn(T, D, device="cuda") for _ in range(4))
+        d_o = torch.randn(T, D, device="cuda")
+        want = chela.blocknorm_bwd(res, y, gate, d_o, d_r, norm_post=chela.NORM_LAYER, norm_pre=chela.NORM_LAYER)
+        r = chela.BlocknormArgs(res.data_ptr(), y.data_ptr(), gate.data_ptr(), D, D, D, None, None, None, None, None, T, D, 1, 0, 2, 2, 1e-6,
+                                chela.F32, chela.F32)
+        d_y, d_gate = torch.empty_like(y), torch.empty_like(y)
+        need = chela.lib().chela_blocknorm_bwd_workspace_bytes(T, D)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        assert chela.lib().chela_blocknorm_bwd(ctypes.byref(r), d_o.data_ptr(), d_r.data_ptr(), d_r.data_ptr(), d_y.data_ptr(), d_gate.data_ptr(),
+                                               None, None, None, None, None, chela.F32, ws.data_ptr(), need,
+                                               torch.cuda.current_stream().cuda_stream) == chela.OK
+        assert torch.equal(d_r, want.d_res) and torch.equal(d_y, want.d_y) and torch.equal(d_gate, want.d_gate)
+
+
 def test_block_norm_parts_alone():
     """The norm before a first block, the norm behind a last one, no residual, one gradient missing, weights left out."""
     T, D, eps = 6, 48, 1e-5
