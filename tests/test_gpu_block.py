@@ -333,6 +333,55 @@ def test_scan_of_few_long_sequences_is_split(dtype, N, D, G, lengths):
         close(getattr(g1, k), r[k], m[k], 2 * tol + more * 2.0 ** -24)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,D,lengths", [(16, 1024, [40, 0, 33, 5, 64, 17, 1]), (16, 520, [9, 21, 0, 8, 1, 30, 16, 17, 2, 0, 5, 12, 33, 7]),
+                                         (32, 1024, [65, 0, 12, 31]), (32, 520, [3, 40, 0, 17, 8, 1, 9])], ids=str)
+def test_scan_of_many_chains(dtype, N, D, lengths):
+    """So many chains that a lane has two channels of 16 or 32 states in whole sequences: outputs, states carried in place,
+    checkpoints, gradients."""
+    import torch
+    S, T, form = len(lengths), sum(lengths), FORMS[0]
+    channels = {16: 32, 32: 16}[N]
+    assert S * -(-D // channels) > 222
+    v = scan_inputs(N + D, lengths, D, N, 1, dtype)
+    args, kw = scan_call(v, lengths, dtype, form, 8)
+    state = kw.pop("state_in")
+    given = state.clone()
+    ckpt = chela.selscan_checkpoints(T, S, D, N, "cuda")
+    y, last = chela.selscan_fwd(*args, **kw, state_in=state, state_out=state, checkpoints=ckpt)
+    (want, want_s), (mag, mag_s) = scan_ref(v, lengths, form), scan_ref(v, lengths, form, mag=True)
+    tol = (max(lengths) + 8) * 2.0 ** -21
+    close(y, want, mag, tol, dtype)
+    close(last, want_s, mag_s, tol)
+    d_so = f32(v["d_state_out"])
+    g1, g2 = (chela.selscan_bwd(*args, dev(v["d_y"], dtype, 8), **kw, state_in=given, checkpoints=c, d_state_out=d_so, want_d_state=True)
+              for c in (ckpt, None))
+    for p, q in zip(g1, g2):
+        assert torch.equal(p, q)
+    r, m = scan_ref(v, lengths, form, bwd=True), scan_ref(v, lengths, form, mag=True, bwd=True)
+    for k, more in (("d_x", 0), ("d_dt", 0), ("d_z", 0), ("d_b", D), ("d_c", D), ("d_a", T), ("d_skip", T), ("d_dt_bias", T), ("d_state_in", 0)):
+        close(getattr(g1, k), r[k], m[k], 2 * tol + more * 2.0 ** -24)
+
+
+def test_scan_gradients_of_b_and_c_over_more_tokens_than_threads():
+    """The kernel that adds the channel blocks' shares takes a second turn: the same bits as the sequences one by one."""
+    import torch
+    lengths, D, N = [30000, 29000], 608, 64
+    assert D // 8 * 2 > 148 and sum(lengths) * 2 * N // 4 > 148 * 32 * 256
+    T = sum(lengths)
+    x, dt, dy = (torch.randn(T, D, device="cuda").bfloat16() for _ in range(3))
+    b, c = (torch.randn(T, 1, N, device="cuda").bfloat16() for _ in range(2))
+    a = -torch.arange(1, N + 1, device="cuda").float().repeat(D, 1)
+    g = chela.selscan_bwd(x, dt, a, b, c, dy, seq_offsets=i32(ref.offsets(lengths)))
+    at = 0
+    for n in lengths:
+        sl = slice(at, at + n)
+        one = chela.selscan_bwd(x[sl], dt[sl], a, b[sl], c[sl], dy[sl], seq_offsets=i32([0, n]))
+        for k in ("d_x", "d_dt", "d_b", "d_c"):
+            assert torch.equal(getattr(g, k)[sl], getattr(one, k)), k
+        at += n
+
+
 def test_scan_of_a_split_sequence_with_growing_states():
     """Rates above zero: a segment's whole growth is infinite in single precision, but there is nothing to grow before the
     last ten tokens."""
