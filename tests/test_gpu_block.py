@@ -146,6 +146,37 @@ def test_conv_reaches_no_further_than_its_width(W):
         assert torch.equal(gx.d_x[:at - W + 1], g.d_x[:at - W + 1]) and torch.equal(gx.d_x[at + W:], g.d_x[at + W:])
 
 
+def test_conv_over_more_work_items_than_warps():
+    """The backward pass's warps each walk several work items and its partial sums come from several rows of CTAs; the forward
+    pass's threads take a second item (against the sequences one by one: the same bits)."""
+    import torch
+    for dtype, D, lengths in (("f32", 8, [2000, 1, 0, 1777, 1501]), ("bf16", 1024, [9000, 40, 10977])):
+        T = sum(lengths)
+        x, w, bias, state, dy, d_so = conv_inputs(D, lengths, D, 4, dtype)
+        off = i32(ref.offsets(lengths))
+        g = chela.shortconv_bwd(dev(x, dtype), f32(w), dev(dy, dtype), f32(bias), state_in=dev(state, dtype), d_state_out=dev(d_so, dtype),
+                                seq_offsets=off, grad_dtype=DT[dtype], want_d_state=True)
+        args = (x, w, bias, dy, lengths, state, d_so)
+        r, m = ref.conv_bwd(*args), ref.conv_bwd(*args, mag=True)
+        sums = (4 + 16 + T) * 2.0 ** -23
+        close(g.d_x, r[0], m[0], 24 * 2.0 ** -23, dtype)
+        close(g.d_w, r[1], m[1], sums)
+        close(g.d_bias, r[2], m[2], sums)
+        close(g.d_state_in, r[3], m[3], 24 * 2.0 ** -23, dtype)
+
+    lengths, D = [100003, 0, 99990, 120007], 1024
+    assert (sum(lengths) // 32) * (D // 4) > 148 * 64 * 256
+    x = torch.randn(sum(lengths), D, device="cuda").bfloat16()
+    w, bias = torch.randn(D, 4, device="cuda"), torch.randn(D, device="cuda")
+    y, last = chela.shortconv_carry_fwd(x, w, bias, seq_offsets=i32(ref.offsets(lengths)))
+    at = 0
+    for s, n in enumerate(lengths):
+        if n:
+            y1, last1 = chela.shortconv_carry_fwd(x[at:at + n], w, bias, seq_offsets=i32([0, n]))
+            assert torch.equal(y[at:at + n], y1) and torch.equal(last[s], last1[0])
+        at += n
+
+
 # ------------------------------------------------------------------------------------------------ selective scan
 
 def scan_inputs(seed, lengths, D, N, G, dtype, pad=0):
