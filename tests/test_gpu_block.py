@@ -727,6 +727,78 @@ def test_block_norm_of_tensors_between_sectors(D):
         assert p is None or torch.equal(p, q)
 
 
+# ------------------------------------------------------------------------------------------------ types
+
+OTHER = {"f32": "bf16", "bf16": "f32"}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_outputs_and_gradients_of_another_type_than_the_operands(dtype):
+    """bf16 results of fp32 operands and fp32 results of bf16 ones against the reference: one rounding, or none."""
+    to = OTHER[dtype]
+    lengths, D, N, G, W = [37, 0, 70, 1], 64, 16, 2, 4
+    off, n, L = i32(ref.offsets(lengths)), sum(lengths), max(lengths)
+    x, w, bias, state, dy, d_so = conv_inputs(31, lengths, D, W, dtype)
+    g = chela.shortconv_bwd(dev(x, dtype), f32(w), dev(dy, dtype), f32(bias), state_in=dev(state, dtype), d_state_out=dev(d_so, dtype),
+                            seq_offsets=off, grad_dtype=DT[to], want_d_state=True)
+    args = (x, w, bias, dy, lengths, state, d_so)
+    r, m = ref.conv_bwd(*args), ref.conv_bwd(*args, mag=True)
+    close(g.d_x, r[0], m[0], (2 * W + 16) * 2.0 ** -23, to)
+    close(g.d_w, r[1], m[1], (W + 16 + n) * 2.0 ** -23)
+    close(g.d_state_in, r[3], m[3], (2 * W + 16) * 2.0 ** -23, to)
+
+    form = FORMS[0]
+    v = scan_inputs(32, lengths, D, N, G, dtype)
+    args, kw = scan_call(v, lengths, dtype, form)
+    tol = (L + 8) * 2.0 ** -21
+    (want, _), (mag, _) = scan_ref(v, lengths, form), scan_ref(v, lengths, form, mag=True)
+    y, _ = chela.selscan_fwd(*args, **kw, out_dtype=DT[to])
+    close(y, want, mag, tol, to)
+    g = chela.selscan_bwd(*args, dev(v["d_y"], dtype), **kw, d_state_out=f32(v["d_state_out"]), grad_dtype=DT[to], want_d_state=True)
+    r, m = scan_ref(v, lengths, form, bwd=True), scan_ref(v, lengths, form, mag=True, bwd=True)
+    for k, more in (("d_x", 0), ("d_dt", 0), ("d_z", 0), ("d_b", D // G), ("d_c", D // G)):
+        close(getattr(g, k), r[k], m[k], 2 * tol + more * 2.0 ** -24, to)
+    one = [1] * 5
+    v = scan_inputs(33, one, D, N, G, dtype)
+    args, kw = scan_call(v, one, dtype, form)
+    kw.pop("seq_offsets")
+    y = chela.selscan_step(*args, kw.pop("state_in"), **kw, out_dtype=DT[to])
+    close(y, scan_ref(v, one, form)[0], scan_ref(v, one, form, mag=True)[0], 2.0 ** -18, to)
+
+
+@pytest.mark.parametrize("dtype,res_dtype", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("D", [40, 1000, 4104])
+def test_block_norm_results_of_every_type(dtype, res_dtype, D):
+    """o and the gradients of y and gate in fp32 and bf16, whatever the operands' types."""
+    T, eps = 5, 1e-6
+    v = norm_inputs(41 + D, T, D, dtype, res_dtype)
+    kw = {"w_post": v["w_post"], "b_post": v["b_post"], "norm_post": 2, "scale": v["scale"], "w_pre": v["w_pre"], "b_pre": v["b_pre"],
+          "norm_pre": 1, "gate_act": 1, "gate_after": False, "eps": eps}
+    dkw = {k: (f32(a) if isinstance(a, np.ndarray) else a) for k, a in kw.items()}
+    want_r, want_o, keep = ref.junction(v["res"], v["y"], v["gate"], **kw)
+    rb = inputs.round_storage(want_r.astype(np.float32), res_dtype)
+    w = ref.junction_bwd(rb, v["y"], v["gate"], v["d_o"], v["d_r"], **kw)
+    # the tolerances of test_block_norms
+    tol = (D / 32 + 64) * 2.0 ** -24
+    size_r = np.abs(v["res"]) + np.abs(v["scale"]) * (np.abs(keep["m"]) + np.abs(keep["ga"]) * 4)
+    inv = ref.normalised(want_r, 1, eps)[1]
+    hat2, inv2 = ref.normalised(rb.astype(np.float64), 1, eps)
+    hat2, top = np.abs(hat2), lambda a: np.abs(a).max(1, keepdims=True)
+    do = np.abs(v["d_o"] * v["w_pre"])
+    size = np.abs(v["d_r"]) + inv2 * (do + (hat2 * top(hat2) + 1) * top(do))
+    ga, hat, dn = np.abs(keep["ga"]), np.abs(keep["hat"]), size * np.abs(v["scale"]) * np.abs(v["w_post"])
+    dv = keep["inv"] * (dn + (hat * top(hat) + 1) * top(dn))
+    for to in ("f32", "bf16"):
+        r, o = chela.blocknorm_fwd(dev(v["res"], res_dtype), dev(v["y"], dtype), dev(v["gate"], dtype), **dkw, out_dtype=DT[to])
+        close(r, want_r, size_r, tol, res_dtype)
+        close(o, want_o, np.abs(want_o) + np.abs(v["w_pre"]) * (size_r * inv + 1) + np.abs(v["b_pre"]), 2 * tol, to)
+        g = chela.blocknorm_bwd(dev(rb, res_dtype), dev(v["y"], dtype), dev(v["gate"], dtype), dev(v["d_o"], dtype), dev(v["d_r"], res_dtype),
+                                **dkw, grad_dtype=DT[to])
+        close(g.d_res, w["d_res"], size, 4 * tol, res_dtype)
+        close(g.d_y, w["d_y"], dv * ga, 8 * tol, to)
+        close(g.d_gate, w["d_gate"], dv * np.abs(v["y"]) * (1.0 + np.abs(v["gate"])), 8 * tol, to)
+
+
 # ------------------------------------------------------------------------------------------------ calls
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
