@@ -641,7 +641,7 @@ def selscan_step(x, dt, a, b, c, state, d_skip=None, z=None, dt_bias=None, softp
     where = "chela_selscan_step"
     r, dev = _selscan_args(where, x, dt, a, b, c, d_skip, z, dt_bias, softplus, state, None, True)
     y = _new_like(out, where, "out", x, x.dtype if out_dtype is None else _tdtype(out_dtype), dev)
-    after = state.data_ptr() if state_out is None else _flat(state_out, where, "state_out", (r.S, r.D, r.N), torch.float32, dev)
+    after = _at(state) if state_out is None else _flat(state_out, where, "state_out", (r.S, r.D, r.N), torch.float32, dev)
     _run(lib().chela_selscan_step, where, dev, ctypes.byref(r), y.data_ptr(), after, _DTYPES[y.dtype])
     return y
 

@@ -296,6 +296,21 @@ def test_a_workspace_lives_until_the_call_has_returned(lib, monkeypatch):
     assert calls == ["chela_shortconv_bwd", "chela_selscan_fwd", "chela_selscan_bwd", "chela_blocknorm_bwd"]
 
 
+def test_a_step_without_a_state_is_refused_like_any_bad_argument(lib, monkeypatch):
+    import torch
+
+    class OnDevice(torch.Tensor):
+        is_cuda = property(lambda self: True)
+
+    monkeypatch.setattr(chela, "_run", lambda fn, where, index, *args: chela._check(fn(*args, None), where))
+    x = torch.zeros(4, 64).as_subclass(OnDevice)
+    for call in (lambda: chela.selscan_step(x, x, torch.zeros(64, 16), torch.zeros(4, 1, 16), torch.zeros(4, 1, 16), None),
+                 lambda: chela.shortconv_step(x, torch.zeros(64, 4), None)):
+        with pytest.raises(chela.ChelaError) as e:
+            call()
+        assert e.value.status == chela.ERR_INVALID_ARG
+
+
 def test_sizes_that_ctypes_would_cut_are_refused(lib, monkeypatch):
     """Channels, sequences, groups and taps past 31 bits: 2^32 + 64 channels would be taken for 64."""
     import torch
