@@ -4,7 +4,7 @@
 // What bounds it: N exponentials a token and channel against 8 bytes of bf16 operands.  An SM evaluates 16 exponentials
 // a cycle, so N = 16 costs 1.2 cycles a token and channel (with softplus and the gate) where its share of the measured
 // HBM rate needs 0.36; beside them 3 N multiply-adds, and the shared memory traffic of b and c, which every channel
-// reads.  8 x 8192 x 1024 in bf16: 285 us of exponentials, 83 us of HBM traffic, 530 to 580 us measured.
+// reads.  8 x 8192 x 1024 in bf16: 285 us of exponentials, 83 us of HBM traffic, 550 us measured.
 //
 // Layout of the work: a lane holds 8 states of one or two channels; the warps of a CTA take turns with short slices of the
 // same channels' tokens.  Everything but the recurrence itself (copies, exponentials, outputs) is done beside the other
@@ -82,9 +82,9 @@ struct FwdShape {
 // A lane prepares (time step, gate, output) PT tokens of one channel, "its" channel, and runs 8 states of all CH
 // channels of its R lanes: slot 0 is its own channel, slot 1 its neighbour's, so that one exchange with lane ^ 1 turns
 // partial outputs around, and one 16-byte read of b or c (2 cycles an SM for 16 broadcast bytes) serves CH channels.
-// Two pools of work run beside each other here and are about equally long, which is why taking away any one part changes
-// the time by a few per cent only: exponentials (8 cycles a warp instruction) with the shared memory traffic behind the
-// same queue, and the multiply-adds.  Two-wide multiply-adds of three different register pairs take 4.2 cycles of a
+// Two pools of work run beside each other here, exponentials (8 cycles a warp instruction) with the shared memory traffic
+// behind the same queue, and the multiply-adds; neither is full (49 and 45 %): the warps wait for their turns (about 515
+// cycles for four tokens), and taking away any one part changes the time by a few per cent only.  Two-wide multiply-adds of three different register pairs take 4.2 cycles of a
 // scheduler, two single ones 2.6 but twice the issue slots; as a whole the two-wide form is 10 % faster.
 template <typename TI, typename TO, int N, int CH, int TOK, int WT, int OCC>
 __global__ void __launch_bounds__(32 * WT, OCC) selscan_fwd_kernel(const ScanParams p)
@@ -509,8 +509,9 @@ struct BwdShape {
 // one before it (one multiply-add per state) goes on to the next warp, and the tile is run backwards two tokens at a
 // time with their decays and states computed again in registers.  So the only serial part is that one step a tile, and
 // few chains still fill the SMs; the second evaluation of the exponentials costs less than keeping the decays would.
-// Eight warps an SM with 240 registers and no spills: twelve warps, which have 168 registers each and spill 170 to 230
-// bytes, took 640 to 740 us where eight take 490 (4 x 4096 x 1024).
+// Eight warps an SM with 252 to 255 registers and no spills: twelve warps, which have 168 registers each and spill 170 to
+// 230 bytes, took 640 to 740 us where eight took 490 (4 x 4096 x 1024).  However few the chains are, a sequence is not split:
+// one of 32768 x 512 takes 3750 us on 16 SMs.
 // Lanes as in the forward kernel: 8 states of CH channels, so that the sums over channels that dB and dC need are begun in
 // the lane; they are folded over the other lanes (each exchange sends one half of the values away and keeps the other) and
 // leave as one partial sum per channel block for selscan_bc_kernel: no atomics, so equal calls give equal bits.
@@ -1003,7 +1004,9 @@ __global__ void __launch_bounds__(256) selscan_sum_kernel(const float *part_a, c
 // ------------------------------------------------------------------------------------------------ launches
 
 // Tokens of a segment, 0 = whole sequences.  A split costs a second pass over x, dt, b (their decays evaluated twice, 1.9
-// times the exponentials), so it pays only where the chains leave more than half of the SMs without work.
+// times the exponentials), so for sequences of equal length it pays only where the chains leave more than half of the SMs
+// without work.  The host does not know the lengths and takes the mean: one long sequence among many short ones is not split
+// (30000 tokens among 39 of 51, 512 channels: 1700 us).
 int fwd_segment(int T, int S, int D, int N)
 {
     const int cpw = chain_channels(N);
@@ -1011,7 +1014,7 @@ int fwd_segment(int T, int S, int D, int N)
     if (chains * 2 > 148 || T / S < 512) return 0;
     // k segments a sequence of average length: as many rounds of two CTAs an SM as it takes, each as long as a segment and
     // what it costs to begin one (about 100 tokens).  A segment too many is a round more: one sequence of 32768 x 512
-    // takes 253 us in 18 segments, 390 in 22, 262 in 37.
+    // takes 255 us in 18 segments, 390 in 22, 262 in 37.
     const long long len = T / S;
     long long best = 0, best_seg = 0;
     for (long long k = 1; k <= 1024 && (k == 1 || len / k >= 256); ++k) {
