@@ -150,6 +150,7 @@ chela_status_t chela_shortconv_bwd(const void *x, long long x_stride, const floa
         !aligned16(d_w) || !aligned16(d_bias) || !aligned16(d_state_in) || !aligned16(workspace))
         return CHELA_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < shortconv_bwd_workspace_bytes(T, D, width)) return CHELA_ERR_WORKSPACE;
+    if (width == 1) state_in = d_state_out = d_state_in = nullptr;   // ignored
     if (!distinct({d_x, d_w, d_bias, d_state_in}, {x, w, bias, d_y, state_in, d_state_out, seq_offsets}) ||
         !all_different({d_x, d_w, d_bias, d_state_in}))
         return CHELA_ERR_INVALID_ARG;

@@ -126,6 +126,25 @@ def test_conv_steps_continue_a_prompt(dtype):
     assert torch.equal(state, last)
 
 
+def test_conv_of_one_tap_ignores_its_states():
+    """One buffer given for every state of a width of one, through the C entry points: neither read nor written, nor refused."""
+    import torch
+    T, D, L = 9, 16, chela.lib()
+    x, w, bias, _, dy, _ = conv_inputs(1, [T], D, 1, "f32")
+    xd, wd, bd, dyd = f32(x), f32(w), f32(bias), f32(dy)
+    y, dx, dw, db, state = (torch.empty(s, device="cuda") for s in ((T, D), (T, D), (D, 1), (D,), (T, D)))
+    state.fill_(5.0)
+    stream, s = torch.cuda.current_stream().cuda_stream, state.data_ptr()
+    need = L.chela_shortconv_bwd_workspace_bytes(T, D, 1)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    assert L.chela_shortconv_carry_fwd(xd.data_ptr(), D, wd.data_ptr(), bd.data_ptr(), y.data_ptr(), s, s, None, 1, T, D, 1, 1, chela.F32,
+                                       stream) == chela.OK
+    assert L.chela_shortconv_bwd(xd.data_ptr(), D, wd.data_ptr(), bd.data_ptr(), dyd.data_ptr(), D, s, s, dx.data_ptr(), dw.data_ptr(),
+                                 db.data_ptr(), s, None, 1, T, D, 1, 1, chela.F32, chela.F32, ws.data_ptr(), need, stream) == chela.OK
+    want, g = chela.shortconv_carry_fwd(xd, wd, bd)[0], chela.shortconv_bwd(xd, wd, dyd, bd)
+    assert torch.equal(y, want) and torch.equal(dx, g.d_x) and torch.equal(dw, g.d_w) and torch.equal(db, g.d_bias) and (state == 5).all()
+
+
 @pytest.mark.parametrize("W", [1, 3, 4, 5, 8, 11])
 def test_conv_reaches_no_further_than_its_width(W):
     """An infinity or NaN in one token's input or gradient: only the outputs and gradients that the width reaches see it."""
