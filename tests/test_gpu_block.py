@@ -541,6 +541,30 @@ def test_slow_states_over_a_long_sequence(N):
         assert most <= 0.1 * L + 6 * L ** 0.5 and mean <= 0.1 * L + 6 * L ** 0.5 / 16
 
 
+@pytest.mark.parametrize("N,D,S", [(8, 24, 3), (16, 40, 3), (16, 1024, 7), (64, 16, 3)])
+def test_scan_rates_and_time_steps_of_either_sign(N, D, S):
+    """Growing, constant and decaying states side by side in a lane, time steps below zero: exponents of up to a few units either
+    way, so that the decays' errors stay at 2^-21 and nothing overflows in 40 tokens."""
+    lengths = [40, 1, 17, 33, 5, 29, 40][:S]
+    form = (True, True, False, True, False)
+    v = scan_inputs(N + D, lengths, D, N, 1, "f32")
+    rng = np.random.default_rng(D)
+    v["a"] = rng.uniform(-1.0, 1.0, (D, N)).astype(np.float32)
+    v["a"][:, ::5] = 0.0
+    v["dt"] = (0.3 * v["dt"]).astype(np.float32)
+    args, kw = scan_call(v, lengths, "f32", form)
+    (want, want_s), (mag, mag_s) = scan_ref(v, lengths, form), scan_ref(v, lengths, form, mag=True)
+    tol = (max(lengths) + 8) * 2.0 ** -21
+    y, last = chela.selscan_fwd(*args, **kw)
+    close(y, want, mag, tol)
+    close(last, want_s, mag_s, tol)
+    g = chela.selscan_bwd(*args, f32(v["d_y"]), **kw, d_state_out=f32(v["d_state_out"]), want_d_state=True)
+    r, m = scan_ref(v, lengths, form, bwd=True), scan_ref(v, lengths, form, mag=True, bwd=True)
+    n = sum(lengths)
+    for k, more in (("d_x", 0), ("d_dt", 0), ("d_z", 0), ("d_b", D), ("d_c", D), ("d_a", n), ("d_skip", n), ("d_state_in", 0)):
+        close(getattr(g, k), r[k], m[k], 2 * tol + more * 2.0 ** -24)
+
+
 def test_scan_time_steps_down_to_tiny_ones():
     """softplus far below and above zero keeps its relative precision: one token from a zero state gives dt x b."""
     raw = np.array([-40.0, -20.0, -12.0, -7.0, -2.0, -0.5, 0.0, 0.5, 3.0, 19.0, 30.0, 88.0, -80.0, 1e-3, -1e-3, 100.0], dtype=np.float32)
@@ -895,6 +919,44 @@ def test_graph_replay_streams_and_repeated_calls_give_equal_bits():
     graph.replay()
     want = chela.selscan_fwd(*args, **kw)[0]
     assert torch.equal(held[0], want) and not torch.equal(held[0], first[0])
+
+
+def test_threads_on_one_stream_do_not_share_workspaces():
+    """Three threads queue calls that need a workspace on the same stream at the same time; each gets what it gets alone."""
+    import threading
+    import torch
+    jobs = []
+    for k in range(3):
+        lengths, D, N = [700 + 40 * k, 900 - 100 * k], 40, 16   # split forward: a workspace there too
+        v = scan_inputs(60 + k, lengths, D, N, 1, "f32")
+        args, kw = scan_call(v, lengths, "f32", FORMS[0])
+        dy = f32(v["d_y"])
+        c = [f32(t) for t in conv_inputs(70 + k, lengths, D, 4, "f32")]
+        nv = {n: f32(t) for n, t in norm_inputs(80 + k, 333 + k, D, "f32", "f32").items()}
+        assert chela.lib().chela_selscan_workspace_bytes(sum(lengths), 2, D, N) > 0
+
+        def job(args=args, kw=kw, dy=dy, c=c, nv=nv):
+            off = kw["seq_offsets"]
+            y, s = chela.selscan_fwd(*args, **kw)
+            cg = chela.shortconv_bwd(c[0], c[1], c[4], c[2], seq_offsets=off)
+            g = chela.selscan_bwd(*args, dy, **kw)
+            ng = chela.blocknorm_bwd(nv["res"], nv["y"], nv["gate"], nv["d_o"], nv["d_r"], w_pre=nv["w_pre"], w_post=nv["w_post"])
+            return [t for t in (y, s, *cg, *g, *ng) if t is not None]
+        jobs.append((job, [t.clone() for t in job()]))
+    wrong, start = [], threading.Barrier(len(jobs))
+
+    def work(job, want):
+        start.wait()
+        for _ in range(40):
+            if not all(torch.equal(p, q) for p, q in zip(job(), want)):
+                wrong.append(job)
+                return
+    threads = [threading.Thread(target=work, args=j) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
 
 
 def test_a_selective_block_decodes_what_its_prompt_computed():
