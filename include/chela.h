@@ -8,7 +8,8 @@
  *     d_k x d_v state and a row normaliser                       (Eq. 2, Sec. 4.1),
  *   - their composition with the Q/K/V formation                 (Eqs. 8, 10-12),
  * and, for layers built around the same short convolution, a selective state space scan, the short convolution with
- * carried inputs and the norms between two blocks, each for prompts, single tokens and training.
+ * carried inputs and the norms between two blocks, each for prompts, single tokens and training, and for the two ends of a
+ * language model the token embedding and the cross entropy over its vocabulary, with their gradients.
  *
  * Conventions common to every entry point
  *   - Every data pointer is a DEVICE pointer owned by the caller; the library never frees or
@@ -463,6 +464,64 @@ size_t chela_blocknorm_bwd_workspace_bytes(int T, int D);
 chela_status_t chela_blocknorm_bwd(const chela_blocknorm_args_t *args, const void *d_o, const void *d_res_out, void *d_res,
                                    void *d_y, void *d_gate, float *d_w_post, float *d_b_post, float *d_scale, float *d_w_pre,
                                    float *d_b_pre, chela_dtype_t grad_dtype, void *workspace, size_t workspace_bytes,
+                                   cudaStream_t stream);
+
+/*
+ * The ends of a language model, on either side of the layers: rows of a table for token ids, and the cross entropy of hidden
+ * rows against a table, which may be the same one.  T tokens in any arrangement (packed sequences or not).  ids and targets
+ * are int32 (wide_ids = 0) or int64 (wide_ids = 1) device arrays of T, aligned to their size.  An id outside [0, V) is
+ * allowed and marks a token that is left out (padding, prompts in training): its row of outputs and gradients is zero, its
+ * rows of operands are not read and it adds nothing to the sums over tokens.
+ * At most 2^31 - 4096 tokens; D a multiple of 8.  The rule on outputs and operands in one buffer is that of the packed
+ * sequences; sums over tokens are taken in a fixed order, so equal calls give equal bits.
+ *
+ * chela_embed_fwd: out[t] = scale * w[ids[t]].  w : [V, D] of w_dtype, rows w_stride elements apart (a multiple of 8, at least
+ * D).  out : [T, D] out_dtype, rounded once.  No workspace.
+ */
+chela_status_t chela_embed_fwd(const void *ids, int wide_ids, const void *w, long long w_stride, void *out, int T, int V, int D,
+                               float scale, chela_dtype_t w_dtype, chela_dtype_t out_dtype, cudaStream_t stream);
+
+/*
+ * Gradient of the table: d_w[v] = d_w_in[v] + scale * sum over the t with ids[t] = v of d_out[t], summed in fp32 and rounded
+ * once.  d_out : [T, D] d_out_dtype with a token stride.  d_w : [V, D] grad_dtype.  d_w_in : the same type, or NULL (zero); it
+ * may be d_w itself, and then only the rows of ids that occur are read and written.
+ */
+size_t chela_embed_bwd_workspace_bytes(int T, int V, int D);
+chela_status_t chela_embed_bwd(const void *ids, int wide_ids, const void *d_out, long long d_out_stride, const void *d_w_in, void *d_w,
+                               int T, int V, int D, float scale, chela_dtype_t d_out_dtype, chela_dtype_t grad_dtype, void *workspace,
+                               size_t workspace_bytes, cudaStream_t stream);
+
+/*
+ * Softmax cross entropy of hidden rows against the rows of a vocabulary, the T x V logits never in memory as a whole:
+ *   z[t,v] = scale <h[t], w[v]>,   lse[t] = log sum_v exp(z[t,v]),   loss[t] = lse[t] - z[t, targets[t]].
+ * h : [T, D], w : [V, D] of in_dtype (F32 or BF16), rows h_stride and w_stride elements apart.  scale > 0 and finite.
+ * loss, lse : [T] fp32 (4-byte aligned), zero for tokens that are left out.  bf16 operands are multiplied on the tensor cores with fp32 sums,
+ * fp32 operands there too, as sums of three bf16 parts each (2^-24 of a product is lost).
+ * workspace: chela_vocabloss_workspace_bytes; chela_async_status reads a wait that gave up from it.
+ */
+typedef struct {
+    const void *h, *w, *targets;
+    long long h_stride, w_stride;
+    int T, V, D, wide_ids;
+    float scale;
+    chela_dtype_t in_dtype;
+} chela_vocabloss_args_t;
+
+size_t chela_vocabloss_workspace_bytes(int T, int V, int D, chela_dtype_t in_dtype);
+chela_status_t chela_vocabloss_fwd(const chela_vocabloss_args_t *args, float *loss, float *lse, void *workspace, size_t workspace_bytes,
+                                   cudaStream_t stream);
+
+/*
+ * Gradients of chela_vocabloss_fwd for the same args and its lse.  d_loss, d_lse : [T] fp32, the gradients of loss and lse, either
+ * may be NULL (zero), not both.  With dz[t,v] = scale ((d_loss[t] + d_lse[t]) exp(z[t,v] - lse[t]) - d_loss[t] [v = targets[t]]),
+ *   d_h = dz w  : [T, D],   d_w = d_w_in + dz^T h  : [V, D],   both of grad_dtype and contiguous.
+ * d_w_in : [V, D] grad_dtype or NULL (zero), may be d_w itself.  With grad_dtype BF16, dz is rounded to bf16 between the
+ * products; with F32 it is kept to 24 bits, at three times their cost.  The vocabulary is walked in pieces whose dz (at most
+ * 512 MB, or 256 columns) lies in the workspace.
+ */
+size_t chela_vocabloss_bwd_workspace_bytes(int T, int V, int D, chela_dtype_t in_dtype, chela_dtype_t grad_dtype);
+chela_status_t chela_vocabloss_bwd(const chela_vocabloss_args_t *args, const float *lse, const float *d_loss, const float *d_lse, void *d_h,
+                                   const void *d_w_in, void *d_w, chela_dtype_t grad_dtype, void *workspace, size_t workspace_bytes,
                                    cudaStream_t stream);
 
 #ifdef __cplusplus

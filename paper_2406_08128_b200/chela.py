@@ -45,6 +45,12 @@ class BlocknormArgs(ctypes.Structure):
         + [(n, _c_int) for n in ("in_dtype", "res_dtype")]
 
 
+class VocablossArgs(ctypes.Structure):
+    """chela_vocabloss_args_t"""
+    _fields_ = [(n, _vp) for n in ("h", "w", "targets")] + [("h_stride", _c_ll), ("w_stride", _c_ll)] \
+        + [(n, _c_int) for n in ("T", "V", "D", "wide_ids")] + [("scale", _c_float), ("in_dtype", _c_int)]
+
+
 _SIGNATURES = {
     "chela_status_string": (ctypes.c_char_p, [_c_int]),
     "chela_version": (_c_int, []),
@@ -100,6 +106,13 @@ _SIGNATURES = {
     "chela_blocknorm_fwd": (_c_int, [_vp] * 3 + [_c_int, _vp]),
     "chela_blocknorm_bwd_workspace_bytes": (_c_size_t, [_c_int] * 2),
     "chela_blocknorm_bwd": (_c_int, [_vp] * 11 + [_c_int, _vp, _c_size_t, _vp]),
+    "chela_embed_fwd": (_c_int, [_vp, _c_int, _vp, _c_ll, _vp] + [_c_int] * 3 + [_c_float, _c_int, _c_int, _vp]),
+    "chela_embed_bwd_workspace_bytes": (_c_size_t, [_c_int] * 3),
+    "chela_embed_bwd": (_c_int, [_vp, _c_int, _vp, _c_ll, _vp, _vp] + [_c_int] * 3 + [_c_float, _c_int, _c_int, _vp, _c_size_t, _vp]),
+    "chela_vocabloss_workspace_bytes": (_c_size_t, [_c_int] * 4),
+    "chela_vocabloss_fwd": (_c_int, [_vp] * 4 + [_c_size_t, _vp]),
+    "chela_vocabloss_bwd_workspace_bytes": (_c_size_t, [_c_int] * 5),
+    "chela_vocabloss_bwd": (_c_int, [_vp] * 7 + [_c_int, _vp, _c_size_t, _vp]),
 }
 
 
@@ -721,3 +734,103 @@ def blocknorm_bwd(res_out, y=None, gate=None, d_o=None, d_res_out=None, w_post=N
     _run(lib().chela_blocknorm_bwd, where, dev, ctypes.byref(r), _flat(d_o, where, "d_o", shape, kind, dev),
          _flat(d_res_out, where, "d_res_out", shape, first.dtype, dev), *map(_at, g), int(grad_dtype), ws, nbytes)
     return g
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# The ends of a language model.  ids and targets are int32 or int64 tensors of any shape, token tensors have that shape and the
+# channel axis behind it.  An id outside [0, V) marks a token that is left out: its rows of outputs and gradients are zero, its
+# rows of operands are not read and it adds nothing to the table's gradient.
+
+VocablossGrads = collections.namedtuple("VocablossGrads", "d_h d_w")
+_IDS = {torch.int32: 0, torch.int64: 1}
+_MAX_VOCAB = 2 ** 30
+
+
+def _ids(ids, where, name):
+    """(address, wide, T, device index) of token ids."""
+    if ids.dtype not in _IDS or not ids.is_contiguous():
+        _need(False, where, "%s must be a contiguous int32 or int64 tensor" % name)
+    T = ids.numel()
+    if T > _MAX_TOKENS:
+        _need(False, where, "%d tokens, at most %d" % (T, _MAX_TOKENS))
+    if not ids.is_cuda:
+        _need(False, where, "tensors must be on a CUDA device (there is no CPU fallback)")
+    return ids.data_ptr(), _IDS[ids.dtype], T, ids.get_device()
+
+
+def _token_rows(t, where, name, lead, D, dtype, index):
+    """Address and token stride of [*lead, D]; one or two token axes unless it is contiguous."""
+    if t.is_contiguous() and t.dtype is dtype and t.get_device() == index and t.shape == (*lead, D):
+        return t.data_ptr(), D
+    _need(len(lead) in (1, 2), where, "%s must be a %s tensor %s on device %d" % (name, dtype, (*lead, D), index))
+    return _rows(t, where, name, lead, dtype, index, (D,))
+
+
+def _table(w, where, name, index):
+    """Address and row stride of a table [V, D]."""
+    if w.dim() != 2 or w.dtype not in _DTYPES or not 1 <= w.shape[0] <= _MAX_VOCAB or not 1 <= w.shape[1] <= _MAX_INT:
+        _need(False, where, "%s must be [V, D] of float32 or bfloat16, with at most 2^30 rows" % name)
+    return _rows(w, where, name, (w.shape[0],), w.dtype, index, (w.shape[1],), w.shape)
+
+
+def embed_fwd(ids, w, scale=1.0, out_dtype=None, out=None):
+    """chela_embed_fwd: scale * w[ids], [*ids.shape, D] of out_dtype (or w's); rows of zeros for ids outside the table w [V, D]."""
+    where = "chela_embed_fwd"
+    pi, wide, T, dev = _ids(ids, where, "ids")
+    pw, ws = _table(w, where, "w", dev)
+    V, D = w.shape
+    dt = w.dtype if out_dtype is None else _tdtype(out_dtype)
+    o = _new(out, where, "out", (*ids.shape, D), dt, ids.device, dev)
+    _run(lib().chela_embed_fwd, where, dev, pi, wide, pw, ws, o.data_ptr(), T, V, D, float(scale), _DTYPES[w.dtype], _DTYPES[dt])
+    return o
+
+
+def embed_bwd(ids, d_out, V, scale=1.0, grad_dtype=F32, d_w_in=None, d_w=None, workspace=None):
+    """chela_embed_bwd: the gradient of the table, [V, D] of grad_dtype: d_w_in (if given) plus scale times the sums of d_out
+    [*ids.shape, D] by id.  d_w may be d_w_in itself: then only the rows of ids that occur are read and written."""
+    where = "chela_embed_bwd"
+    pi, wide, T, dev = _ids(ids, where, "ids")
+    if d_out.dtype not in _DTYPES or d_out.dim() < 1 or not 1 <= int(V) <= _MAX_VOCAB or not 1 <= d_out.shape[-1] <= _MAX_INT:
+        _need(False, where, "d_out must be float32 or bfloat16, V between 1 and 2^30")
+    V, D, gt = int(V), d_out.shape[-1], _tdtype(grad_dtype)
+    pd, ds = _token_rows(d_out, where, "d_out", ids.shape, D, d_out.dtype, dev)
+    before = _flat(d_w_in, where, "d_w_in", (V, D), gt, dev)
+    d_w = _new(d_w, where, "d_w", (V, D), gt, ids.device, dev)
+    workspace, ws, nbytes = _scratch(lib().chela_embed_bwd_workspace_bytes(T, V, D), workspace, ids.device, where, dev)
+    _run(lib().chela_embed_bwd, where, dev, pi, wide, pd, ds, before, d_w.data_ptr(), T, V, D, float(scale), _DTYPES[d_out.dtype], int(grad_dtype), ws, nbytes)
+    return d_w
+
+
+def _vocabloss_args(where, h, w, targets, scale):
+    pt, wide, T, dev = _ids(targets, where, "targets")
+    pw, ws = _table(w, where, "w", dev)
+    V, D = w.shape
+    ph, hs = _token_rows(h, where, "h", targets.shape, D, w.dtype, dev)
+    return VocablossArgs(ph, pw, pt, hs, ws, T, V, D, wide, float(scale), _DTYPES[w.dtype]), dev
+
+
+def vocabloss_fwd(h, w, targets, scale=1.0, loss=None, lse=None, workspace=None):
+    """chela_vocabloss_fwd: (loss, lse), f32 of targets' shape: the cross entropy of scale * h w^T, h [*targets.shape, D], w [V, D],
+    and the logarithm of its normaliser; both zero where the target is outside [0, V)."""
+    where = "chela_vocabloss_fwd"
+    r, dev = _vocabloss_args(where, h, w, targets, scale)
+    loss = _new(loss, where, "loss", targets.shape, torch.float32, targets.device, dev)
+    lse = _new(lse, where, "lse", targets.shape, torch.float32, targets.device, dev)
+    workspace, ws, nbytes = _scratch(lib().chela_vocabloss_workspace_bytes(r.T, r.V, r.D, r.in_dtype), workspace, targets.device, where, dev)
+    _run(lib().chela_vocabloss_fwd, where, dev, ctypes.byref(r), loss.data_ptr(), lse.data_ptr(), ws, nbytes)
+    return loss, lse
+
+
+def vocabloss_bwd(h, w, targets, lse, d_loss, d_lse=None, scale=1.0, grad_dtype=F32, d_w_in=None, d_w=None, workspace=None):
+    """chela_vocabloss_bwd: VocablossGrads of grad_dtype from the lse that vocabloss_fwd returned and the gradients of loss and lse
+    (f32 of targets' shape, either may be None).  d_w is d_w_in (if given) plus the gradient of w; it may be d_w_in itself."""
+    where = "chela_vocabloss_bwd"
+    r, dev = _vocabloss_args(where, h, w, targets, scale)
+    gt, f32, shape = _tdtype(grad_dtype), torch.float32, targets.shape
+    before = _flat(d_w_in, where, "d_w_in", w.shape, gt, dev)
+    d_h = _like(h, gt)
+    d_w = _new(d_w, where, "d_w", w.shape, gt, w.device, dev)
+    workspace, ws, nbytes = _scratch(lib().chela_vocabloss_bwd_workspace_bytes(r.T, r.V, r.D, r.in_dtype, int(grad_dtype)), workspace, targets.device, where, dev)
+    _run(lib().chela_vocabloss_bwd, where, dev, ctypes.byref(r), _flat(lse, where, "lse", shape, f32, dev), _flat(d_loss, where, "d_loss", shape, f32, dev),
+         _flat(d_lse, where, "d_lse", shape, f32, dev), d_h.data_ptr(), before, d_w.data_ptr(), int(grad_dtype), ws, nbytes)
+    return VocablossGrads(d_h, d_w)

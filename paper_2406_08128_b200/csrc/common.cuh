@@ -174,4 +174,19 @@ chela_status_t launch_blocknorm_bwd(const chela_blocknorm_args_t &a, const void 
                                     void *d_gate, float *d_w_post, float *d_b_post, float *d_scale, float *d_w_pre, float *d_b_pre,
                                     chela_dtype_t grad_dtype, void *workspace, cudaStream_t stream);
 
+// ---- the ends of a language model (embed.cu, vocabloss.cu) ---------------------------------------------------------
+
+chela_status_t launch_embed_fwd(const void *ids, bool wide_ids, const void *w, long long w_stride, void *out, int T, int V, int D, float scale,
+                                chela_dtype_t w_dtype, chela_dtype_t out_dtype, cudaStream_t stream);
+size_t embed_bwd_workspace_bytes(int T, int V, int D);
+chela_status_t launch_embed_bwd(const void *ids, bool wide_ids, const void *d_out, long long d_out_stride, const void *d_w_in, void *d_w, int T,
+                                int V, int D, float scale, chela_dtype_t d_out_dtype, chela_dtype_t grad_dtype, void *workspace,
+                                cudaStream_t stream);
+
+size_t vocabloss_workspace_bytes(int T, int V, int D, chela_dtype_t in_dtype);
+chela_status_t launch_vocabloss_fwd(const chela_vocabloss_args_t &a, float *loss, float *lse, void *workspace, cudaStream_t stream);
+size_t vocabloss_bwd_workspace_bytes(int T, int V, int D, chela_dtype_t in_dtype, chela_dtype_t grad_dtype);
+chela_status_t launch_vocabloss_bwd(const chela_vocabloss_args_t &a, const float *lse, const float *d_loss, const float *d_lse, void *d_h,
+                                    const void *d_w_in, void *d_w, chela_dtype_t grad_dtype, void *workspace, cudaStream_t stream);
+
 }  // namespace chela

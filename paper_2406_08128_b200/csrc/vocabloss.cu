@@ -1,0 +1,833 @@
+// Softmax cross entropy of hidden rows against a vocabulary's weight rows, and its gradients, without the T x V logits in
+// memory:
+//   z[t,v] = scale <h_t, w_v>,  lse_t = log sum_v e^z[t,v],  loss_t = lse_t - z[t,y_t],
+//   dz[t,v] = scale ((d_loss_t + d_lse_t) e^(z[t,v] - lse_t) - d_loss_t [v = y_t]),   d_h = dz w,   d_w = dz^T h.
+//
+// Bound by the tensor cores: T V D multiply-adds a product.  The forward pass is one product whose epilogue keeps a running
+// maximum and sum per row.  The backward pass walks the vocabulary in pieces: the logits of a piece once more, their dz to the
+// workspace in bf16, and both gradient products of the piece in one launch, so that the few tiles of the one fill the SMs that
+// the other leaves idle.  Four products for a training step where storing the logits would take three.
+//
+// Left-out rows (target outside the vocabulary) cost nothing and are never read: the kept rows are numbered on the device, all
+// kernels walk those, and h is copied together only where some are left out.
+//
+// bf16 operands go to the tensor cores as they are; dz is rounded to bf16 where the gradients are bf16 (its rounding is as large
+// as theirs and independent between terms) and split in three bf16 planes (24 bits) where they are fp32.  fp32 operands are
+// split in three planes too, and a product of them is the six plane products that reach 2^-24 of the result, the small ones
+// first.  The tensor cores truncate the accumulator at every step, so the fp32 modes end a sum after kSegment columns and add
+// the segments in registers.
+#include "packed.cuh"
+#include "sm100_pair.cuh"
+
+namespace chela {
+namespace {
+
+using namespace sm100;
+
+constexpr int kTile = 256;              // rows and columns of a tile: 128 rows of A and 128 columns of B in each CTA's memory
+constexpr int kStages = 6, kOperand = 128 * 128, kStageBytes = 2 * kOperand;
+constexpr int kEpilogueWarps = 8, kThreads = 64 + 32 * kEpilogueWarps;
+constexpr int kStagingWarp = 32 * 128;  // a box of 32 rows x 128 bytes
+constexpr int kSegment = 4;             // K blocks of 64 that fp32 modes add up in the tensor cores
+constexpr int offStaging = kStages * kStageBytes, offBar = offStaging + kEpilogueWarps * kStagingWarp;
+constexpr int offTmem = offBar + 8 * (2 * kStages + 4), offAbort = offTmem + 8, kSmemBytes = offAbort + 8;
+static_assert(kSmemBytes <= 232448, "shared memory per CTA");
+static_assert(kStagingWarp % 1024 == 0 && offStaging % 1024 == 0, "swizzled boxes start on 1024 bytes");
+
+constexpr size_t kHead = 256;           // workspace header: word 0 the asynchronous status, word 1 the number of kept rows
+constexpr float kLn2 = 0.6931471805599453f;
+
+enum What { kStats, kSlopes, kGrads };
+
+// Planes of A and B of the partial products of one product, small ones first, two bits each.
+struct Terms {
+    int n;
+    uint32_t a, b;
+};
+constexpr Terms kTerms1 = {1, 0, 0};
+constexpr Terms kTerms2 = {2, 0, 1 | 0 << 2};                                                                  // B in planes, two of them
+constexpr Terms kTerms3 = {3, 2 | 1 << 2 | 0 << 4, 0};                                                        // A in planes
+constexpr Terms kTerms6 = {6, 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10, 0 | 2 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 0 << 10};   // both
+
+struct Product {
+    CUtensorMap h, hk, w, dz, dz_out, dh_out, dw_out;
+    Terms terms;
+    int *head;
+    const int *target;              // [Tpad] of kept rows, -1 behind them
+    const float4 *coef;             // [Tpad] {lse log2 e, factor of the softmax, factor of the target, target}
+    float *zt;                      // [Tpad] target's logit log2 e
+    float2 *part;                   // [2 * chunks][Tpad] running maximum (log2 e) and sum of a chunk's column halves
+    const void *dw_in;
+    int T, Tpad, V, D, v0, vc, w_row, per_chunk, first_part, sh, sv, planes;
+    int h_in_planes, dh_add, dw_bf16, dw_in_bf16, dw_sliced;
+    float c2;                       // scale log2 e
+    WaitCtl wc;
+};
+
+// One tile of the product that a launch computes.
+struct Tile {
+    int m0, n0, kb0, kb1;
+    bool dw;       // d_w's product (A is dz taken by columns)
+    int slice;
+};
+
+__device__ __forceinline__ long long units_of(const Product &p, int what, int n)
+{
+    const long long mt = (n + kTile - 1) / kTile, nt = (min(p.vc, p.V - p.v0) + kTile - 1) / kTile, nd = (p.D + kTile - 1) / kTile;
+    if (what == kStats) return mt * ((nt + p.per_chunk - 1) / p.per_chunk);
+    if (what == kSlopes) return mt * nt;
+    return nd * (nt * p.sv + mt * p.sh);
+}
+
+// kStats: a unit is a chunk of per_chunk column tiles of one row tile.  Neighbouring units share their columns: the weights of
+// a chunk are read by all row tiles about the same time.
+__device__ __forceinline__ Tile tile_of(const Product &p, int what, int n, long long u, int j)
+{
+    Tile t{};
+    const int mt = (n + kTile - 1) / kTile, nt = (min(p.vc, p.V - p.v0) + kTile - 1) / kTile, nd = (p.D + kTile - 1) / kTile;
+    if (what != kGrads) {
+        t.m0 = (int)(u % mt) * kTile;
+        t.n0 = ((int)(u / mt) * (what == kStats ? p.per_chunk : 1) + j) * kTile;
+        t.kb1 = (p.D + 63) / 64;
+        return t;
+    }
+    // d_w's tiles first: with many tokens they are the longer ones
+    const long long ndw = (long long)nt * nd * p.sv;
+    t.dw = u < ndw;
+    const long long v = t.dw ? u : u - ndw;
+    const int slices = t.dw ? p.sv : p.sh, kbs = ((t.dw ? n : min(p.vc, p.V - p.v0)) + 63) / 64;
+    t.n0 = (int)(v % nd) * kTile;
+    t.slice = (int)(v / nd % slices);
+    t.m0 = (int)(v / nd / slices) * kTile;
+    t.kb0 = (int)((long long)kbs * t.slice / slices);
+    t.kb1 = (int)((long long)kbs * (t.slice + 1) / slices);
+    return t;
+}
+__device__ __forceinline__ int tiles_in_unit(const Product &p, int what, int n, long long u)
+{
+    if (what != kStats) return 1;
+    const int mt = (n + kTile - 1) / kTile, nt = (min(p.vc, p.V - p.v0) + kTile - 1) / kTile;
+    return min(p.per_chunk, nt - (int)(u / mt) * p.per_chunk);
+}
+
+// Half an operand tile: 128 rows of M or N by 64 of K as two boxes of 64 x 64.
+__device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap *map, uint32_t bar, bool mn_major, int mn, int kb, int plane)
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int at = mn + 64 * i;
+        tma_load_3d_pair(dst + i * 8192, map, bar, mn_major ? at : kb * 64, mn_major ? kb * 64 : at, plane);
+    }
+}
+
+// Two CTAs a tile of 256 x 256, persistent.  Warp 0: TMA producer of its CTA's halves; warp 1 of the even CTA: issuer;
+// warps 2-9: epilogue, each 32 rows x 128 columns.  Accumulators double-buffered in TMEM (2 x 256 columns).
+template <int kWhat, bool kSegments>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ Product p)
+{
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t sbase = smem_u32(smem);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = cluster_rank();
+    const long long pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const uint32_t bar_full = sbase + offBar, bar_empty = bar_full + 8 * kStages, bar_tfull = bar_empty + 8 * kStages, bar_tempty = bar_tfull + 16;
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + offTmem);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + offAbort);
+    if (tid == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(bar_full + 8 * s, 1);
+            mbar_init(bar_empty + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(bar_tfull + 8 * b, 1);
+            mbar_init(bar_tempty + 8 * b, 2 * kEpilogueWarps);
+        }
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == 1) {
+        tmem_alloc_pair(sbase + offTmem, 512);
+        tmem_relinquish_pair();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const int n = min(max(p.head[1], 0), p.T);
+    const long long units = units_of(p, kWhat, n);
+    // h as given when no row is left out, else the kept rows' copy
+    const CUtensorMap *map_h = (n == p.T && !p.h_in_planes) ? &p.h : &p.hk;
+    bool ok = true;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ TMA producer
+        if (lane == 0) {
+            int it = 0;
+            for (long long u = pair; ok && u < units; u += pairs) {
+                const int tiles = tiles_in_unit(p, kWhat, n, u);
+                for (int j = 0; ok && j < tiles; ++j) {
+                    const Tile t = tile_of(p, kWhat, n, u, j);
+                    const bool a_mn = kWhat == kGrads && t.dw, b_mn = kWhat == kGrads;
+                    const CUtensorMap *map_a = kWhat == kGrads ? &p.dz : map_h, *map_b = kWhat == kGrads && t.dw ? map_h : &p.w;
+                    const Terms terms = p.terms;
+                    // weights: rows of the vocabulary are B's columns for logits and its K for d_h
+                    const int b_row = kWhat != kGrads ? p.w_row : 0, b_kb = kWhat == kGrads && !t.dw ? p.w_row / 64 : 0;
+                    const int seg = kSegments ? kSegment : t.kb1 - t.kb0;
+                    for (int kb = t.kb0; ok && kb < t.kb1; kb += seg)
+                        for (int i = 0; ok && i < (kSegments ? terms.n : 1); ++i)
+                            for (int k = kb; k < min(kb + seg, t.kb1); ++k, ++it) {
+                                const int s = it % kStages;
+                                ok = mbar_wait(bar_empty + 8 * s, ((it / kStages) & 1) ^ 1, abort_flag, p.wc.limit);
+                                if (!ok) break;
+                                const uint32_t bar = bar_full + 8 * s, dst = sbase + s * kStageBytes, to = map_to_rank(bar, 0);
+                                if (rank == 0) mbar_expect_tx(bar, 2 * kStageBytes);
+                                load_operand(dst, map_a, to, a_mn, t.m0 + (int)rank * 128, k, kSegments ? terms.a >> 2 * i & 3 : 0);
+                                load_operand(dst + kOperand, map_b, to, b_mn, t.n0 + b_row + (int)rank * 128, k + b_kb, kSegments ? terms.b >> 2 * i & 3 : 0);
+                            }
+                }
+            }
+            if (!ok) {
+                *abort_flag = 1;
+                atomicExch(p.head, (int)CHELA_ERR_TIMEOUT);
+                // loads in flight land in shared memory: wait for them as far as this CTA can (bounded)
+                if (rank == 0)
+                    for (int c = it > kStages ? it - kStages : 0; c < it; ++c) mbar_wait(bar_full + 8 * (c % kStages), (c / kStages) & 1, nullptr, p.wc.limit);
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer
+        if (lane == 0 && rank == 0) {
+            int it = 0, gs = 0;
+            for (long long u = pair; ok && u < units; u += pairs) {
+                const int tiles = tiles_in_unit(p, kWhat, n, u);
+                for (int j = 0; ok && j < tiles; ++j) {
+                    const Tile t = tile_of(p, kWhat, n, u, j);
+                    const bool a_mn = kWhat == kGrads && t.dw;
+                    constexpr bool b_mn = kWhat == kGrads;
+                    const int nterms = kSegments ? p.terms.n : 1;
+                    const uint32_t idesc = make_idesc(kTile, kTile, a_mn, b_mn);
+                    // K step of 16: 32 bytes along a K-major row, 16 rows of an MN-major tile (two atoms of 64 columns)
+                    const uint32_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;
+                    const int seg = kSegments ? kSegment : t.kb1 - t.kb0;
+                    for (int kb = t.kb0; ok && kb < t.kb1; kb += seg, ++gs) {
+                        const int buf = gs & 1;
+                        ok = mbar_wait(bar_tempty + 8 * buf, ((gs >> 1) & 1) ^ 1, abort_flag, p.wc.limit);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const int steps = (min(kb + seg, t.kb1) - kb) * nterms;
+                        for (int k = 0; k < steps; ++k, ++it) {
+                            const int s = it % kStages;
+                            ok = mbar_wait(bar_full + 8 * s, (it / kStages) & 1, abort_flag, p.wc.limit);
+                            if (!ok) break;
+                            tc_fence_after();
+                            const uint32_t st = sbase + s * kStageBytes;
+                            const uint32_t a = a_mn ? desc_lo(st, 8192) : desc_lo(st), b = b_mn ? desc_lo(st + kOperand, 8192) : desc_lo(st + kOperand);
+#pragma unroll
+                            for (int q = 0; q < 4; ++q)
+                                umma_bf16_pair(tmem + buf * kTile, a + a_step * q, b + b_step * q, idesc, (k > 0 || q > 0) ? 1u : 0u);
+                            umma_commit_pair(bar_empty + 8 * s);
+                        }
+                        if (ok) umma_commit_pair(bar_tfull + 8 * buf);
+                    }
+                }
+            }
+            if (!ok) {
+                *abort_flag = 1;
+                atomicExch(p.head, (int)CHELA_ERR_TIMEOUT);
+            }
+        }
+    } else {
+        // ------------------------------------------------------------------ epilogue
+        // TMEM lanes are a warp's by its number modulo 4; of the two warps of a lane quarter each takes half the columns
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const int row = (int)rank * 128 + quarter * 32 + lane, row0 = (int)rank * 128 + quarter * 32;
+        const uint32_t t_at = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
+        uint8_t *stg = smem + offStaging + (warp - 2) * kStagingWarp;
+        const uint32_t stg_u32 = sbase + offStaging + (warp - 2) * kStagingWarp;
+        const uint32_t leader_tempty = map_to_rank(bar_tempty, 0);
+        int gs = 0;
+        for (long long u = pair; ok && u < units; u += pairs) {
+            const int tiles = tiles_in_unit(p, kWhat, n, u);
+            float run_m = -INFINITY, run_s = 0.f;
+            for (int j = 0; ok && j < tiles; ++j) {
+                const Tile t = tile_of(p, kWhat, n, u, j);
+                const int seg = kSegments ? kSegment : max(t.kb1 - t.kb0, 1);
+                float z[128];
+                if (kWhat == kGrads && t.kb0 == t.kb1) {   // an empty slice
+#pragma unroll
+                    for (int c = 0; c < 128; ++c) z[c] = 0.f;
+                }
+                for (int kb = t.kb0; kb < t.kb1; kb += seg, ++gs) {
+                    const int buf = gs & 1;
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar_tfull + 8 * buf, (gs >> 1) & 1, abort_flag, p.wc.limit));
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (!kSegments || kb == t.kb0) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) tmem_ld32(t_at + buf * kTile + 32 * c, *reinterpret_cast<float(*)[32]>(&z[32 * c]));
+                        tmem_ld_wait();
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            float more[32];
+                            tmem_ld32(t_at + buf * kTile + 32 * c, more);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) z[32 * c + e] += more[e];
+                        }
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    // (test hook: the first hand-back of CTA 0 left out, so that the issuer's wait for it runs out)
+                    if (lane == 0 && !(p.wc.skip_arrival && blockIdx.x == 0 && gs == 0 && warp == 2)) mbar_arrive_cluster(leader_tempty + 8 * buf);
+                }
+                if (!ok) break;
+                const int c0 = t.n0 + half * 128;   // first column of this thread's 128, in the piece
+                if (kWhat == kStats) {
+                    const int y = p.target[t.m0 + row] - p.v0 - c0;
+                    if (c0 + 128 > p.V - p.v0) {
+#pragma unroll
+                        for (int c = 0; c < 128; ++c)
+                            if (c0 + c >= p.V - p.v0) z[c] = -INFINITY;
+                    }
+                    float m4[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+                    for (int c = 4; c < 128; ++c) m4[c & 3] = fmaxf(m4[c & 3], z[c]);
+                    const float m = fmaxf(run_m, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.c2);
+                    if (m != -INFINITY) {
+                        float s4[4] = {run_s * ex2(run_m - m), 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int c = 0; c < 128; ++c) s4[c & 3] += ex2(fmaf(z[c], p.c2, -m));
+                        run_s = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                        run_m = m;
+                    }
+                    if (__any_sync(0xffffffffu, y >= 0 && y < 128)) {
+                        float zy = 0.f;
+#pragma unroll
+                        for (int c = 0; c < 128; ++c) zy = c == y ? z[c] : zy;
+                        if (y >= 0 && y < 128) p.zt[t.m0 + row] = zy * p.c2;
+                    }
+                } else if (kWhat == kSlopes) {
+                    const float4 cf = p.coef[t.m0 + row];
+                    const int y = __float_as_int(cf.w) - p.v0 - c0;
+                    const bool here = __any_sync(0xffffffffu, y >= 0 && y < 128);
+#pragma unroll
+                    for (int c = 0; c < 128; ++c) z[c] = cf.y * ex2(fmaf(z[c], p.c2, -cf.x));
+                    if (here) {
+#pragma unroll
+                        for (int c = 0; c < 128; ++c) z[c] = c == y ? z[c] - cf.z : z[c];
+                    }
+                    if (c0 + 128 > p.V - p.v0 || t.m0 + kTile > n) {
+#pragma unroll
+                        for (int c = 0; c < 128; ++c)
+                            if (c0 + c >= p.V - p.v0 || t.m0 + row >= n) z[c] = 0.f;
+                    }
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        for (int plane = 0; plane < p.planes; ++plane) {
+                            uint32_t v[32];
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                const __nv_bfloat162 hh = __floats2bfloat162_rn(z[64 * c + 2 * e], z[64 * c + 2 * e + 1]);
+                                v[e] = *reinterpret_cast<const uint32_t *>(&hh);
+                                if (p.planes > 1) {   // what is left for the next plane
+                                    const float2 f = __bfloat1622float2(hh);
+                                    z[64 * c + 2 * e] -= f.x;
+                                    z[64 * c + 2 * e + 1] -= f.y;
+                                }
+                            }
+                            if (lane == 0) bulk_wait_read0();
+                            __syncwarp();
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4 *>(stg + sw128(lane, e)) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                            fence_proxy_async();
+                            __syncwarp();
+                            if (lane == 0 && c0 + 64 * c < p.vc) {
+                                tma_store_3d(&p.dz_out, stg_u32, c0 + 64 * c, t.m0 + row0, plane);
+                                bulk_commit();
+                            }
+                        }
+                } else {
+                    const bool wide = t.dw && p.dw_bf16 && !p.dw_sliced;   // bf16: 64 columns a box, else 32
+                    const int out_row = t.dw && !p.dw_sliced ? p.v0 + t.m0 + row : t.m0 + row;
+                    if (t.dw && !p.dw_sliced && p.dw_in && out_row < p.V) {
+                        const size_t at = (size_t)out_row * p.D;
+#pragma unroll
+                        for (int c = 0; c < 128; c += 4)
+                            if (c0 + c < p.D) {
+                                const float4 o = p.dw_in_bf16 ? load4(reinterpret_cast<const __nv_bfloat16 *>(p.dw_in) + at + c0 + c)
+                                                              : load4(reinterpret_cast<const float *>(p.dw_in) + at + c0 + c);
+                                z[c] += o.x, z[c + 1] += o.y, z[c + 2] += o.z, z[c + 3] += o.w;
+                            }
+                    }
+                    const int first = out_row - lane, rows = t.dw ? (p.dw_sliced ? p.vc : p.V) : p.Tpad;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if (wide && (c & 1)) continue;
+                        if (lane == 0) bulk_wait_read0();
+                        __syncwarp();
+                        if (wide) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                uint32_t v[4];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) v[i] = pack_bf16(z[(32 * c + 8 * e + 2 * i) & 127], z[(32 * c + 8 * e + 2 * i + 1) & 127]);
+                                *reinterpret_cast<uint4 *>(stg + sw128(lane, e)) = make_uint4(v[0], v[1], v[2], v[3]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                *reinterpret_cast<float4 *>(stg + sw128(lane, e)) = make_float4(z[32 * c + 4 * e], z[32 * c + 4 * e + 1], z[32 * c + 4 * e + 2], z[32 * c + 4 * e + 3]);
+                        }
+                        fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0 && c0 + 32 * c < p.D && first < rows) {
+                            if (t.dw) tma_store_3d(&p.dw_out, stg_u32, c0 + 32 * c, first, p.dw_sliced ? t.slice : 0);
+                            else if (p.dh_add) tma_add_3d(&p.dh_out, stg_u32, c0 + 32 * c, first, t.slice);
+                            else tma_store_3d(&p.dh_out, stg_u32, c0 + 32 * c, first, t.slice);
+                            bulk_commit();
+                        }
+                    }
+                }
+            }
+            if (ok && kWhat == kStats) {
+                const int chunk = p.first_part + (int)(u / ((n + kTile - 1) / kTile));
+                const int m0 = (int)(u % ((n + kTile - 1) / kTile)) * kTile;
+                p.part[(size_t)(2 * chunk + half) * p.Tpad + m0 + row] = make_float2(run_m, run_s);
+            }
+        }
+        if (!ok && lane == 0) {
+            *abort_flag = 1;
+            atomicExch(p.head, (int)CHELA_ERR_TIMEOUT);
+        }
+        if (lane == 0) bulk_wait0();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();   // the other CTA's arrivals, loads and products that touch this CTA's memory are behind it
+    if (warp == 1) tmem_dealloc_pair(tmem, 512);
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ void split3(float x, __nv_bfloat16 (&o)[3])
+{
+    o[0] = __float2bfloat16_rn(x);
+    const float r = x - __bfloat162float(o[0]);
+    o[1] = __float2bfloat16_rn(r);
+    o[2] = __float2bfloat16_rn(r - __bfloat162float(o[1]));
+}
+// Eight elements of a row: bf16 as they are, fp32 in three planes `plane` elements apart.
+__device__ __forceinline__ void copy8(const __nv_bfloat16 *src, __nv_bfloat16 *dst, size_t) { *reinterpret_cast<uint4 *>(dst) = *reinterpret_cast<const uint4 *>(src); }
+__device__ __forceinline__ void copy8(const float *src, __nv_bfloat16 *dst, size_t plane)
+{
+    const float4 a = load4(src), b = load4(src + 4);
+    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    __nv_bfloat16 o[3][8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        __nv_bfloat16 t[3];
+        split3(x[e], t);
+        o[0][e] = t[0], o[1][e] = t[1], o[2][e] = t[2];
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) *reinterpret_cast<uint4 *>(dst + i * plane) = *reinterpret_cast<const uint4 *>(o[i]);
+}
+
+struct Rows {
+    const void *targets, *h;
+    long long h_stride;
+    int T, Tpad, V, D, per_cta, planes;
+    int *head, *row_of, *pos_of, *target;    // row_of (forward), pos_of (backward), target (forward): nullable
+    float4 *coef;                            // backward
+    const float *lse, *d_loss, *d_lse;
+    float scale;
+    float *loss_out, *lse_out;               // forward
+    __nv_bfloat16 *hk;
+};
+
+// Numbers the kept rows in the order of the tokens, lays out what the products' epilogues read of them, and copies the kept
+// rows of h together where some row is left out or h is split in planes.  Every CTA counts the kept rows before its own by
+// itself: the targets are few bytes, and a second launch costs more.
+template <typename Idx, typename TH>
+__global__ void __launch_bounds__(256) rows_kernel(const Rows r)
+{
+    __shared__ int s_sum[2][8], s_pos[256], s_warp[8];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const Idx *targets = reinterpret_cast<const Idx *>(r.targets);
+    const TH *h = reinterpret_cast<const TH *>(r.h);
+    const long long begin = (long long)blockIdx.x * r.per_cta, end = min(begin + r.per_cta, (long long)r.T);
+    int before = 0, total = 0;
+    for (long long t = tid; t < r.T; t += 256) {
+        const Idx y = targets[t];
+        const int kept = y >= 0 && y < (Idx)r.V;
+        total += kept;
+        before += kept && t < begin;
+    }
+    for (int o = 16; o; o >>= 1) {
+        before += __shfl_xor_sync(0xffffffffu, before, o);
+        total += __shfl_xor_sync(0xffffffffu, total, o);
+    }
+    if (lane == 0) s_sum[0][warp] = before, s_sum[1][warp] = total;
+    __syncthreads();
+    int base = 0, n = 0;
+    for (int w = 0; w < 8; ++w) base += s_sum[0][w], n += s_sum[1][w];
+    const bool copy = n < r.T || r.planes > 1;
+    const size_t plane = (size_t)r.Tpad * r.D;
+    if (blockIdx.x == 0 && tid == 0) r.head[0] = 0, r.head[1] = n;
+    for (long long t0 = begin; t0 < end; t0 += 256) {
+        const long long t = t0 + tid;
+        const Idx y = t < end ? targets[t] : (Idx)-1;
+        const bool kept = y >= 0 && y < (Idx)r.V;
+        const unsigned votes = __ballot_sync(0xffffffffu, kept);
+        if (lane == 0) s_warp[warp] = __popc(votes);
+        __syncthreads();
+        int pos = base + __popc(votes & ((1u << lane) - 1u));
+        for (int w = 0; w < 8; ++w) {
+            if (w < warp) pos += s_warp[w];
+            base += s_warp[w];
+        }
+        s_pos[tid] = kept ? pos : -1;
+        if (t < end) {
+            if (r.pos_of) r.pos_of[t] = kept ? pos : -1;
+            if (kept) {
+                if (r.row_of) r.row_of[pos] = (int)t;
+                if (r.target) r.target[pos] = (int)y;
+                if (r.coef) {
+                    const float g = r.d_loss ? r.d_loss[t] : 0.f;
+                    r.coef[pos] = make_float4(r.lse[t] * kLog2e, r.scale * (g + (r.d_lse ? r.d_lse[t] : 0.f)), r.scale * g, __int_as_float((int)y));
+                }
+            } else {
+                if (r.loss_out) r.loss_out[t] = 0.f;
+                if (r.lse_out) r.lse_out[t] = 0.f;
+            }
+        }
+        __syncthreads();
+        if (copy)
+            for (int i = warp; i < 256 && t0 + i < end; i += 8) {
+                const int at = s_pos[i];
+                if (at < 0) continue;
+                for (int c = lane * 8; c < r.D; c += 256) copy8(h + (size_t)(t0 + i) * r.h_stride + c, r.hk + (size_t)at * r.D + c, plane);
+            }
+        __syncthreads();
+    }
+    // behind the last kept row, to the end of its tile
+    const int padded = min(r.Tpad, (n + kTile - 1) / kTile * kTile);
+    for (int i = n + blockIdx.x; i < padded; i += gridDim.x) {
+        if (tid == 0) {
+            if (r.target) r.target[i] = -1;
+            if (r.coef) r.coef[i] = make_float4(0.f, 0.f, 0.f, __int_as_float(-1));
+        }
+        if (copy)
+            for (int pl = 0; pl < r.planes; ++pl)
+                for (int c = tid * 8; c < r.D; c += 256 * 8) *reinterpret_cast<uint4 *>(r.hk + pl * plane + (size_t)i * r.D + c) = make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
+// Rows v0 ... v0 + vc of fp32 weights as three bf16 planes [3][vc][D], zero past V.
+__global__ void __launch_bounds__(256) planes_kernel(const float *w, long long w_stride, __nv_bfloat16 *out, int v0, int vc, int V, int D)
+{
+    const long long per_row = D / 8, items = per_row * vc;
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < items; i += gridDim.x * 256LL) {
+        const int v = (int)(i / per_row), c = (int)(i % per_row) * 8;
+        __nv_bfloat16 *dst = out + (size_t)v * D + c;
+        if (v0 + v < V) copy8(w + (size_t)(v0 + v) * w_stride + c, dst, (size_t)vc * D);
+        else
+            for (int pl = 0; pl < 3; ++pl) *reinterpret_cast<uint4 *>(dst + (size_t)pl * vc * D) = make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
+// lse = (m + log2 s) ln 2 over a row's parts; the loss from the differences to the largest logit, so that it keeps its digits
+// where the target has nearly all the weight.
+__global__ void __launch_bounds__(512) join_kernel(const int *head, const int *row_of, const float *zt, const float2 *part, int parts, int T, int Tpad, float *loss, float *lse)
+{
+    __shared__ float2 s_part[16][33];
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
+    const int n = min(max(head[1], 0), T);
+    if ((int)blockIdx.x * 32 >= n) return;
+    float m = -INFINITY, s = 0.f;
+    if (i < n)
+        for (int q = group; q < parts; q += 16) {
+            const float2 v = part[(size_t)q * Tpad + i];
+            const float mm = fmaxf(m, v.x);
+            if (mm != -INFINITY) s = s * ex2(m - mm) + v.y * ex2(v.x - mm), m = mm;
+        }
+    s_part[group][lane] = make_float2(m, s);
+    __syncthreads();
+    if (group == 0 && i < n) {
+        float mm = m;
+        for (int g = 1; g < 16; ++g) mm = fmaxf(mm, s_part[g][lane].x);
+        float sum = 0.f;
+        for (int g = 0; g < 16; ++g) sum += s_part[g][lane].x == -INFINITY ? 0.f : s_part[g][lane].y * ex2(s_part[g][lane].x - mm);
+        const int t = row_of[i];
+        const float log_s = log1pf(sum - 1.f);   // the largest term is 1
+        lse[t] = fmaf(mm, kLn2, log_s);
+        loss[t] = fmaf(mm - zt[i], kLn2, log_s);
+    }
+}
+
+__device__ __forceinline__ void add4(float4 &a, const float4 b) { a.x += b.x, a.y += b.y, a.z += b.z, a.w += b.w; }
+
+// d_h: the slices of a kept row added up in their order and laid where the row came from; zero for rows that were left out.
+template <typename TO>
+__global__ void __launch_bounds__(256) spread_kernel(const int *pos_of, const float *dh, int slices, int T, int Tpad, int D, TO *d_h)
+{
+    const long long per_row = D / 4, items = per_row * T;
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < items; i += gridDim.x * 256LL) {
+        const long long t = i / per_row;
+        const int c = (int)(i % per_row) * 4, at = pos_of[t];
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (at >= 0)
+            for (int s = 0; s < slices; ++s) add4(v, load4(dh + ((size_t)s * Tpad + at) * D + c));
+        store4(d_h + t * D + c, v);
+    }
+}
+
+// d_w's rows v0 ... : its slices added up in their order, on top of dw_in.
+template <typename TO>
+__global__ void __launch_bounds__(256) add_slices_kernel(const float *part, int slices, int vc, int rows, int D, const TO *dw_in, TO *d_w)
+{
+    const long long items = (long long)rows * D / 4, slice = (long long)vc * D;
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < items; i += gridDim.x * 256LL) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < slices; ++s) add4(v, load4(part + s * slice + 4 * i));
+        if (dw_in) add4(v, load4(dw_in + 4 * i));
+        store4(d_w + 4 * i, v);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+
+int sm_count()
+{
+    int sms = 0, dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0) sms = 148;
+    return sms;
+}
+
+int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+
+// How a call is cut, from its sizes alone, and where its parts lie in the workspace.
+struct Plan {
+    int pairs, Tpad, vc, pieces, per_chunk, chunks, sh, sv, planes_in, planes_dz;
+    size_t row_of, pos_of, target, coef, zt, part, hk, wk, dz, dhp, dwp, bytes;
+};
+
+constexpr size_t kPieceBytes = (size_t)512 << 20;    // dz (or the weights' planes) of one piece of the vocabulary
+constexpr size_t kSliceBytes = (size_t)256 << 20;    // the gradients' slices
+
+// Time of the gradient launch in K blocks: pairs take the units in turn, d_w's before d_h's, and a round lasts as long as its
+// longest unit, its K blocks and about eight for the epilogue.
+long long grad_rounds(long long ndw, long long kdw, long long ndh, long long kdh, int pairs)
+{
+    const long long mixed = ndw % pairs ? pairs - ndw % pairs : 0;   // units of d_h in d_w's last round
+    long long sum = ndw / pairs * (8 + kdw);
+    if (mixed) sum += 8 + (kdh > kdw && ndh ? kdh : kdw);
+    if (ndh > mixed) sum += (ndh - mixed + pairs - 1) / pairs * (8 + kdh);
+    return sum;
+}
+
+Plan make_plan(int T, int V, int D, chela_dtype_t in_dtype, chela_dtype_t grad_dtype, bool bwd)
+{
+    Plan q{};
+    q.pairs = sm_count() / 2;
+    q.Tpad = ceil_div(T, kTile) * kTile;
+    q.planes_in = in_dtype == CHELA_F32 ? 3 : 1;
+    q.planes_dz = grad_dtype == CHELA_F32 ? 3 : 1;
+    const int nt = ceil_div(V, kTile), mt = q.Tpad / kTile, nd = ceil_div(D, kTile);
+    size_t tile_bytes = 0;   // of the piece-wise buffers, by column tile
+    if (bwd) tile_bytes = (size_t)q.Tpad * kTile * 2 * q.planes_dz;
+    if (q.planes_in > 1 && tile_bytes < (size_t)3 * kTile * D * 2) tile_bytes = (size_t)3 * kTile * D * 2;
+    long long most = tile_bytes ? (long long)(kPieceBytes / tile_bytes) : nt;
+    if (most < 1) most = 1;
+    q.pieces = ceil_div(nt, most);
+    const int tiles = ceil_div(nt, q.pieces);
+    q.pieces = ceil_div(nt, tiles);
+    q.vc = tiles * kTile;
+    size_t at = kHead;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += align_up(bytes, 1024);
+        return here;
+    };
+    q.hk = take((size_t)q.planes_in * q.Tpad * D * 2);
+    if (q.planes_in > 1) q.wk = take((size_t)3 * q.vc * D * 2);
+    if (!bwd) {
+        // at least about six units a pair, so that the last round weighs little, and at most 16 column tiles a unit
+        long long per = (long long)mt * tiles / (6LL * q.pairs);
+        q.per_chunk = (int)(per < 1 ? 1 : per > 16 ? 16 : per);
+        q.chunks = ceil_div(tiles, q.per_chunk);
+        q.row_of = take((size_t)q.Tpad * 4);
+        q.target = take((size_t)q.Tpad * 4);
+        q.zt = take((size_t)q.Tpad * 4);
+        q.part = take((size_t)2 * q.chunks * q.pieces * q.Tpad * 8);
+    } else {
+        // slices of the gradients' sums: the cheapest launch by grad_rounds, with as few slices as it takes
+        long long best = -1;
+        for (int sv = 1; sv <= 64; sv *= 2)
+            for (int sh = 1; sh <= 64; sh *= 2) {
+                if (sv > 1 && (size_t)sv * q.vc * D * 4 > kSliceBytes) continue;
+                if (sh > 1 && (size_t)sh * q.Tpad * D * 4 > kSliceBytes) continue;
+                const long long kdw = ceil_div(ceil_div(T, 64), sv), kdh = ceil_div(q.vc / 64, sh);
+                long long cost = grad_rounds((long long)tiles * nd * sv, kdw, (long long)mt * nd * sh, kdh, q.pairs);
+                cost += cost * (sv + sh - 2) / 200;   // the slices' own traffic
+                if (best < 0 || cost < best) best = cost, q.sv = sv, q.sh = sh;
+            }
+        q.pos_of = take((size_t)T * 4);
+        q.coef = take((size_t)q.Tpad * 16);
+        q.dz = take((size_t)q.planes_dz * q.Tpad * q.vc * 2);
+        q.dhp = take((size_t)q.sh * q.Tpad * D * 4);
+        if (q.sv > 1) q.dwp = take((size_t)q.sv * q.vc * D * 4);
+    }
+    q.bytes = at;
+    return q;
+}
+
+bool map_3d(CUtensorMap *map, const void *ptr, bool f32, long long cols, long long rows, long long planes, long long row_bytes, long long plane_bytes, int box_cols, int box_rows)
+{
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+    const cuuint64_t strides[2] = {(cuuint64_t)row_bytes, (cuuint64_t)plane_bytes};
+    const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1};
+    return make_map_sw128(map, ptr, f32, 3, dims, strides, box);
+}
+
+template <int kWhat, bool kSegments>
+chela_status_t launch_product(const Product &p, int pairs, cudaStream_t stream)
+{
+    if (cudaFuncSetAttribute(product_kernel<kWhat, kSegments>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess) return CHELA_ERR_CUDA;
+    product_kernel<kWhat, kSegments><<<2 * pairs, kThreads, kSmemBytes, stream>>>(p);
+    return last_launch_status();
+}
+
+chela_status_t launch_rows(Rows &r, chela_dtype_t in_dtype, bool wide_ids, int sms, cudaStream_t stream)
+{
+    int grid = ceil_div(r.T, 32);
+    if (grid > 2 * sms) grid = 2 * sms;
+    r.per_cta = ceil_div(r.T, grid);
+    if (in_dtype == CHELA_F32) {
+        if (wide_ids) rows_kernel<long long, float><<<grid, 256, 0, stream>>>(r);
+        else rows_kernel<int, float><<<grid, 256, 0, stream>>>(r);
+    } else {
+        if (wide_ids) rows_kernel<long long, __nv_bfloat16><<<grid, 256, 0, stream>>>(r);
+        else rows_kernel<int, __nv_bfloat16><<<grid, 256, 0, stream>>>(r);
+    }
+    return last_launch_status();
+}
+
+// The products' operands that both passes share.
+bool set_operands(Product &p, const chela_vocabloss_args_t &a, const Plan &q, uint8_t *ws)
+{
+    const size_t hk_plane = (size_t)q.Tpad * a.D * 2;
+    p.head = reinterpret_cast<int *>(ws);
+    p.T = a.T, p.Tpad = q.Tpad, p.V = a.V, p.D = a.D, p.vc = q.vc;
+    p.h_in_planes = q.planes_in > 1;
+    p.c2 = a.scale * kLog2e;
+    p.wc = current_wait_ctl();
+    p.per_chunk = q.per_chunk, p.sh = q.sh, p.sv = q.sv, p.planes = q.planes_dz;
+    if (!map_3d(&p.hk, ws + q.hk, false, a.D, q.Tpad, q.planes_in, (long long)a.D * 2, (long long)hk_plane, 64, 64)) return false;
+    if (q.planes_in > 1) {
+        p.h = p.hk;
+        return map_3d(&p.w, ws + q.wk, false, a.D, q.vc, 3, (long long)a.D * 2, (long long)q.vc * a.D * 2, 64, 64);
+    }
+    return map_3d(&p.h, a.h, false, a.D, a.T, 1, a.h_stride * 2, a.h_stride * 2, 64, 64) &&
+           map_3d(&p.w, a.w, false, a.D, a.V, 1, a.w_stride * 2, a.w_stride * 2, 64, 64);
+}
+
+// The weights of the piece that starts at v0: rows of w's map, or planes of them.
+chela_status_t set_piece(Product &p, const chela_vocabloss_args_t &a, const Plan &q, uint8_t *ws, int v0, int sms, cudaStream_t stream)
+{
+    p.v0 = v0;
+    p.w_row = q.planes_in > 1 ? 0 : v0;
+    if (q.planes_in > 1) {
+        planes_kernel<<<4 * sms, 256, 0, stream>>>((const float *)a.w, a.w_stride, (__nv_bfloat16 *)(ws + q.wk), v0, q.vc, a.V, a.D);
+        return last_launch_status();
+    }
+    return CHELA_OK;
+}
+
+}  // namespace
+
+size_t vocabloss_workspace_bytes(int T, int V, int D, chela_dtype_t in_dtype) { return make_plan(T, V, D, in_dtype, CHELA_BF16, false).bytes; }
+size_t vocabloss_bwd_workspace_bytes(int T, int V, int D, chela_dtype_t in_dtype, chela_dtype_t grad_dtype)
+{
+    return make_plan(T, V, D, in_dtype, grad_dtype, true).bytes;
+}
+
+chela_status_t launch_vocabloss_fwd(const chela_vocabloss_args_t &a, float *loss, float *lse, void *workspace, cudaStream_t stream)
+{
+    const Plan q = make_plan(a.T, a.V, a.D, a.in_dtype, CHELA_BF16, false);
+    uint8_t *ws = reinterpret_cast<uint8_t *>(workspace);
+    const int sms = 2 * q.pairs;
+    Product p{};
+    if (!set_operands(p, a, q, ws)) return CHELA_ERR_CUDA;
+    Rows r{};
+    r.targets = a.targets, r.h = a.h, r.h_stride = a.h_stride, r.T = a.T, r.Tpad = q.Tpad, r.V = a.V, r.D = a.D, r.planes = q.planes_in;
+    r.head = p.head, r.row_of = (int *)(ws + q.row_of), r.target = (int *)(ws + q.target), r.loss_out = loss, r.lse_out = lse, r.hk = (__nv_bfloat16 *)(ws + q.hk);
+    chela_status_t st = launch_rows(r, a.in_dtype, a.wide_ids != 0, sms, stream);
+    p.target = r.target, p.zt = (float *)(ws + q.zt), p.part = (float2 *)(ws + q.part);
+    p.terms = q.planes_in > 1 ? kTerms6 : kTerms1;
+    int parts = 0;
+    for (int i = 0; st == CHELA_OK && i < q.pieces; ++i) {
+        const int v0 = i * q.vc, tiles = ceil_div((a.V - v0 < q.vc ? a.V - v0 : q.vc), kTile);
+        st = set_piece(p, a, q, ws, v0, sms, stream);
+        if (st != CHELA_OK) return st;
+        p.first_part = parts;
+        parts += ceil_div(tiles, q.per_chunk);
+        st = q.planes_in > 1 ? launch_product<kStats, true>(p, q.pairs, stream) : launch_product<kStats, false>(p, q.pairs, stream);
+    }
+    if (st != CHELA_OK) return st;
+    join_kernel<<<q.Tpad / 32, 512, 0, stream>>>(p.head, r.row_of, p.zt, p.part, 2 * parts, a.T, q.Tpad, loss, lse);
+    return last_launch_status();
+}
+
+chela_status_t launch_vocabloss_bwd(const chela_vocabloss_args_t &a, const float *lse, const float *d_loss, const float *d_lse, void *d_h, const void *d_w_in, void *d_w,
+                                    chela_dtype_t grad_dtype, void *workspace, cudaStream_t stream)
+{
+    const Plan q = make_plan(a.T, a.V, a.D, a.in_dtype, grad_dtype, true);
+    uint8_t *ws = reinterpret_cast<uint8_t *>(workspace);
+    const int sms = 2 * q.pairs;
+    const bool f32 = grad_dtype == CHELA_F32;
+    Product p{};
+    if (!set_operands(p, a, q, ws)) return CHELA_ERR_CUDA;
+    const long long dz_row = (long long)q.vc * 2, es = f32 ? 4 : 2;
+    if (!map_3d(&p.dz, ws + q.dz, false, q.vc, q.Tpad, q.planes_dz, dz_row, dz_row * q.Tpad, 64, 64) ||
+        !map_3d(&p.dz_out, ws + q.dz, false, q.vc, q.Tpad, q.planes_dz, dz_row, dz_row * q.Tpad, 64, 32) ||
+        !map_3d(&p.dh_out, ws + q.dhp, true, a.D, q.Tpad, q.sh, a.D * 4LL, (long long)q.Tpad * a.D * 4, 32, 32))
+        return CHELA_ERR_CUDA;
+    if (q.sv > 1 ? !map_3d(&p.dw_out, ws + q.dwp, true, a.D, q.vc, q.sv, a.D * 4LL, (long long)q.vc * a.D * 4, 32, 32)
+                 : !map_3d(&p.dw_out, d_w, f32, a.D, a.V, 1, a.D * es, a.D * es, f32 ? 32 : 64, 32))
+        return CHELA_ERR_CUDA;
+    Rows r{};
+    r.targets = a.targets, r.h = a.h, r.h_stride = a.h_stride, r.T = a.T, r.Tpad = q.Tpad, r.V = a.V, r.D = a.D, r.planes = q.planes_in;
+    r.head = p.head, r.pos_of = (int *)(ws + q.pos_of), r.coef = (float4 *)(ws + q.coef), r.hk = (__nv_bfloat16 *)(ws + q.hk);
+    r.lse = lse, r.d_loss = d_loss, r.d_lse = d_lse, r.scale = a.scale;
+    chela_status_t st = launch_rows(r, a.in_dtype, a.wide_ids != 0, sms, stream);
+    p.coef = r.coef;
+    p.dw_in = d_w_in, p.dw_bf16 = p.dw_in_bf16 = !f32, p.dw_sliced = q.sv > 1;
+    for (int i = 0; st == CHELA_OK && i < q.pieces; ++i) {
+        const int v0 = i * q.vc, rows = a.V - v0 < q.vc ? a.V - v0 : q.vc;
+        st = set_piece(p, a, q, ws, v0, sms, stream);
+        if (st != CHELA_OK) return st;
+        p.terms = q.planes_in > 1 ? kTerms6 : kTerms1;
+        st = q.planes_in > 1 ? launch_product<kSlopes, true>(p, q.pairs, stream) : launch_product<kSlopes, false>(p, q.pairs, stream);
+        if (st != CHELA_OK) return st;
+        p.terms = q.planes_in > 1 ? (f32 ? kTerms6 : kTerms2) : f32 ? kTerms3 : kTerms1;
+        p.dh_add = i > 0;
+        st = f32 || q.planes_in > 1 ? launch_product<kGrads, true>(p, q.pairs, stream) : launch_product<kGrads, false>(p, q.pairs, stream);
+        if (st == CHELA_OK && q.sv > 1) {
+            const size_t off = (size_t)v0 * a.D;
+            const float *part = (const float *)(ws + q.dwp);
+            if (f32) add_slices_kernel<float><<<4 * sms, 256, 0, stream>>>(part, q.sv, q.vc, rows, a.D, d_w_in ? (const float *)d_w_in + off : nullptr, (float *)d_w + off);
+            else add_slices_kernel<__nv_bfloat16><<<4 * sms, 256, 0, stream>>>(part, q.sv, q.vc, rows, a.D, d_w_in ? (const __nv_bfloat16 *)d_w_in + off : nullptr, (__nv_bfloat16 *)d_w + off);
+            st = last_launch_status();
+        }
+    }
+    if (st != CHELA_OK) return st;
+    const float *dhp = (const float *)(ws + q.dhp);
+    if (f32) spread_kernel<float><<<8 * sms, 256, 0, stream>>>((const int *)(ws + q.pos_of), dhp, q.sh, a.T, q.Tpad, a.D, (float *)d_h);
+    else spread_kernel<__nv_bfloat16><<<8 * sms, 256, 0, stream>>>((const int *)(ws + q.pos_of), dhp, q.sh, a.T, q.Tpad, a.D, (__nv_bfloat16 *)d_h);
+    return last_launch_status();
+}
+
+}  // namespace chela
