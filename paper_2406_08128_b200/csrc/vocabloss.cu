@@ -58,44 +58,58 @@ struct Product {
     float *zt;                      // [Tpad] target's logit log2 e
     float2 *part;                   // [2 * chunks][Tpad] running maximum (log2 e) and sum of a chunk's column halves
     const void *dw_in;
+    const int *row_of;              // [Tpad] tokens of the kept rows
+    void *d_h;
+    const float *dh_before;         // d_h's sum over the pieces before, where dh_last
     int T, Tpad, V, D, v0, vc, w_row, per_chunk, first_part, sh, sv, planes;
-    int h_in_planes, dh_add, dw_bf16, dw_in_bf16, dw_sliced;
+    int h_in_planes, dh_add, dh_last, grad_bf16, dw_sliced;
     float c2;                       // scale log2 e
     WaitCtl wc;
 };
 
 // One tile of the product that a launch computes.
 struct Tile {
-    int m0, n0, kb0, kb1;
+    int m0, n0, kb0, kb1, boxes;   // boxes: of 64 columns that B has
     bool dw;       // d_w's product (A is dz taken by columns)
     int slice;
 };
 
+__device__ __forceinline__ int row_tiles(int n) { return (n + kTile - 1) / kTile; }
+__device__ __forceinline__ int piece_boxes(const Product &p) { return (min(p.vc, p.V - p.v0) + 63) / 64; }
+
 __device__ __forceinline__ long long units_of(const Product &p, int what, int n)
 {
-    const long long mt = (n + kTile - 1) / kTile, nt = (min(p.vc, p.V - p.v0) + kTile - 1) / kTile, nd = (p.D + kTile - 1) / kTile;
-    if (what == kStats) return mt * ((nt + p.per_chunk - 1) / p.per_chunk);
+    const long long mt = row_tiles(n), boxes = piece_boxes(p), nt = (boxes + 3) / 4, nd = (p.D + kTile - 1) / kTile;
+    if (what == kStats) return mt * ((boxes + p.per_chunk - 1) / p.per_chunk);
     if (what == kSlopes) return mt * nt;
     return nd * (nt * p.sv + mt * p.sh);
 }
 
-// kStats: a unit is a chunk of per_chunk column tiles of one row tile.  Neighbouring units share their columns: the weights of
-// a chunk are read by all row tiles about the same time.
+// kStats: a unit is a chunk of per_chunk boxes of 64 columns of one row tile, four boxes a tile.  Neighbouring units share their
+// columns: the weights of a chunk are read by all row tiles about the same time.
 __device__ __forceinline__ Tile tile_of(const Product &p, int what, int n, long long u, int j)
 {
     Tile t{};
-    const int mt = (n + kTile - 1) / kTile, nt = (min(p.vc, p.V - p.v0) + kTile - 1) / kTile, nd = (p.D + kTile - 1) / kTile;
+    const int mt = row_tiles(n), nd = (p.D + kTile - 1) / kTile;
+    t.boxes = 4;
     if (what != kGrads) {
+        const int at = (int)(u / mt);
         t.m0 = (int)(u % mt) * kTile;
-        t.n0 = ((int)(u / mt) * (what == kStats ? p.per_chunk : 1) + j) * kTile;
         t.kb1 = (p.D + 63) / 64;
+        if (what == kSlopes) {
+            t.n0 = at * kTile;
+            return t;
+        }
+        const int box = at * p.per_chunk + 4 * j;
+        t.n0 = box * 64;
+        t.boxes = min(4, min((at + 1) * p.per_chunk, piece_boxes(p)) - box);
         return t;
     }
     // d_w's tiles first: with many tokens they are the longer ones
-    const long long ndw = (long long)nt * nd * p.sv;
+    const long long ndw = (long long)((piece_boxes(p) + 3) / 4) * nd * p.sv;
     t.dw = u < ndw;
     const long long v = t.dw ? u : u - ndw;
-    const int slices = t.dw ? p.sv : p.sh, kbs = ((t.dw ? n : min(p.vc, p.V - p.v0)) + 63) / 64;
+    const int slices = t.dw ? p.sv : p.sh, kbs = t.dw ? (n + 63) / 64 : piece_boxes(p);
     t.n0 = (int)(v % nd) * kTile;
     t.slice = (int)(v / nd % slices);
     t.m0 = (int)(v / nd / slices) * kTile;
@@ -106,15 +120,16 @@ __device__ __forceinline__ Tile tile_of(const Product &p, int what, int n, long 
 __device__ __forceinline__ int tiles_in_unit(const Product &p, int what, int n, long long u)
 {
     if (what != kStats) return 1;
-    const int mt = (n + kTile - 1) / kTile, nt = (min(p.vc, p.V - p.v0) + kTile - 1) / kTile;
-    return min(p.per_chunk, nt - (int)(u / mt) * p.per_chunk);
+    const int at = (int)(u / row_tiles(n));
+    return (min((at + 1) * p.per_chunk, piece_boxes(p)) - at * p.per_chunk + 3) / 4;
 }
 
-// Half an operand tile: 128 rows of M or N by 64 of K as two boxes of 64 x 64.
-__device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap *map, uint32_t bar, bool mn_major, int mn, int kb, int plane)
+// Half an operand tile: 128 rows of M or N by 64 of K as two boxes of 64 x 64 (or fewer, the rest left as it is).
+__device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap *map, uint32_t bar, bool mn_major, int mn, int kb, int plane, int boxes)
 {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
+        if (i >= boxes) break;
         const int at = mn + 64 * i;
         tma_load_3d_pair(dst + i * 8192, map, bar, mn_major ? at : kb * 64, mn_major ? kb * 64 : at, plane);
     }
@@ -154,6 +169,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    griddep_launch_dependents();
+    griddep_wait();   // up to here the kernel before this one may still run
     const int n = min(max(p.head[1], 0), p.T);
     const long long units = units_of(p, kWhat, n);
     // h as given when no row is left out, else the kept rows' copy
@@ -181,9 +198,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                                 ok = mbar_wait(bar_empty + 8 * s, ((it / kStages) & 1) ^ 1, abort_flag, p.wc.limit);
                                 if (!ok) break;
                                 const uint32_t bar = bar_full + 8 * s, dst = sbase + s * kStageBytes, to = map_to_rank(bar, 0);
-                                if (rank == 0) mbar_expect_tx(bar, 2 * kStageBytes);
-                                load_operand(dst, map_a, to, a_mn, t.m0 + (int)rank * 128, k, kSegments ? terms.a >> 2 * i & 3 : 0);
-                                load_operand(dst + kOperand, map_b, to, b_mn, t.n0 + b_row + (int)rank * 128, k + b_kb, kSegments ? terms.b >> 2 * i & 3 : 0);
+                                if (rank == 0) mbar_expect_tx(bar, 2 * kOperand + t.boxes * 8192);
+                                load_operand(dst, map_a, to, a_mn, t.m0 + (int)rank * 128, k, kSegments ? terms.a >> 2 * i & 3 : 0, 2);
+                                load_operand(dst + kOperand, map_b, to, b_mn, t.n0 + b_row + (int)rank * 128, k + b_kb, kSegments ? terms.b >> 2 * i & 3 : 0, t.boxes - 2 * (int)rank);
                             }
                 }
             }
@@ -285,11 +302,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                 if (!ok) break;
                 const int c0 = t.n0 + half * 128;   // first column of this thread's 128, in the piece
                 if (kWhat == kStats) {
-                    const int y = p.target[t.m0 + row] - p.v0 - c0;
-                    if (c0 + 128 > p.V - p.v0) {
+                    int y = p.target[t.m0 + row] - p.v0 - c0;
+                    if (y + c0 >= t.n0 + 64 * t.boxes) y = -1;   // a later chunk's
+                    const int end = min(t.n0 + 64 * t.boxes, p.V - p.v0);
+                    if (c0 + 128 > end) {
 #pragma unroll
                         for (int c = 0; c < 128; ++c)
-                            if (c0 + c >= p.V - p.v0) z[c] = -INFINITY;
+                            if (c0 + c >= end) z[c] = -INFINITY;
                     }
                     float m4[4] = {z[0], z[1], z[2], z[3]};
 #pragma unroll
@@ -349,19 +368,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                             }
                         }
                 } else {
-                    const bool wide = t.dw && p.dw_bf16 && !p.dw_sliced;   // bf16: 64 columns a box, else 32
+                    // a final gradient, of its type, or a sum in fp32 that goes on
+                    const bool final = t.dw ? !p.dw_sliced : p.dh_last, wide = final && p.grad_bf16;   // boxes of 64 bf16 or 32 fp32 columns
                     const int out_row = t.dw && !p.dw_sliced ? p.v0 + t.m0 + row : t.m0 + row;
-                    if (t.dw && !p.dw_sliced && p.dw_in && out_row < p.V) {
+                    const float *before32 = t.dw ? (const float *)p.dw_in : p.dh_before;
+                    if (final && before32 && out_row < (t.dw ? p.V : p.Tpad)) {
                         const size_t at = (size_t)out_row * p.D;
+                        const bool half_width = t.dw && p.grad_bf16;
 #pragma unroll
                         for (int c = 0; c < 128; c += 4)
                             if (c0 + c < p.D) {
-                                const float4 o = p.dw_in_bf16 ? load4(reinterpret_cast<const __nv_bfloat16 *>(p.dw_in) + at + c0 + c)
-                                                              : load4(reinterpret_cast<const float *>(p.dw_in) + at + c0 + c);
+                                const float4 o = half_width ? load4(reinterpret_cast<const __nv_bfloat16 *>(p.dw_in) + at + c0 + c) : load4(before32 + at + c0 + c);
                                 z[c] += o.x, z[c + 1] += o.y, z[c + 2] += o.z, z[c + 3] += o.w;
                             }
                     }
                     const int first = out_row - lane, rows = t.dw ? (p.dw_sliced ? p.vc : p.V) : p.Tpad;
+                    const int token = !t.dw && final && t.m0 + row < n ? p.row_of[t.m0 + row] : -1;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         if (wide && (c & 1)) continue;
@@ -380,6 +402,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                             for (int e = 0; e < 8; ++e)
                                 *reinterpret_cast<float4 *>(stg + sw128(lane, e)) = make_float4(z[32 * c + 4 * e], z[32 * c + 4 * e + 1], z[32 * c + 4 * e + 2], z[32 * c + 4 * e + 3]);
                         }
+                        if (!t.dw && final) {
+                            // rows go to where their tokens are: eight lanes a row of 128 bytes
+                            __syncwarp();
+                            const int es = wide ? 2 : 4, col = c0 + 32 * c + (lane & 7) * (16 / es);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const int r = e * 4 + (lane >> 3), to = __shfl_sync(0xffffffffu, token, r);
+                                const uint4 v = *reinterpret_cast<const uint4 *>(stg + sw128(r, lane & 7));
+                                if (to >= 0 && col < p.D) *reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(p.d_h) + ((size_t)to * p.D + col) * es) = v;
+                            }
+                            __syncwarp();
+                            continue;
+                        }
                         fence_proxy_async();
                         __syncwarp();
                         if (lane == 0 && c0 + 32 * c < p.D && first < rows) {
@@ -392,8 +427,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                 }
             }
             if (ok && kWhat == kStats) {
-                const int chunk = p.first_part + (int)(u / ((n + kTile - 1) / kTile));
-                const int m0 = (int)(u % ((n + kTile - 1) / kTile)) * kTile;
+                const int chunk = p.first_part + (int)(u / row_tiles(n)), m0 = (int)(u % row_tiles(n)) * kTile;
                 p.part[(size_t)(2 * chunk + half) * p.Tpad + m0 + row] = make_float2(run_m, run_s);
             }
         }
@@ -439,7 +473,9 @@ struct Rows {
     const void *targets, *h;
     long long h_stride;
     int T, Tpad, V, D, per_cta, planes;
-    int *head, *row_of, *pos_of, *target;    // row_of (forward), pos_of (backward), target (forward): nullable
+    int *head, *row_of, *pos_of, *target;    // pos_of, target (forward): nullable
+    void *d_h;                               // backward without slices: zero for rows that are left out
+    int d_h_bytes;                           // of a row
     float4 *coef;                            // backward
     const float *lse, *d_loss, *d_lse;
     float scale;
@@ -447,19 +483,22 @@ struct Rows {
     __nv_bfloat16 *hk;
 };
 
+constexpr int kRowsThreads = 512, kRowsWarps = kRowsThreads / 32;
 // Numbers the kept rows in the order of the tokens, lays out what the products' epilogues read of them, and copies the kept
 // rows of h together where some row is left out or h is split in planes.  Every CTA counts the kept rows before its own by
 // itself: the targets are few bytes, and a second launch costs more.
 template <typename Idx, typename TH>
-__global__ void __launch_bounds__(256) rows_kernel(const Rows r)
+__global__ void __launch_bounds__(kRowsThreads) rows_kernel(const Rows r)
 {
-    __shared__ int s_sum[2][8], s_pos[256], s_warp[8];
+    __shared__ int s_sum[2][kRowsWarps], s_pos[kRowsThreads], s_warp[kRowsWarps];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const Idx *targets = reinterpret_cast<const Idx *>(r.targets);
     const TH *h = reinterpret_cast<const TH *>(r.h);
     const long long begin = (long long)blockIdx.x * r.per_cta, end = min(begin + r.per_cta, (long long)r.T);
     int before = 0, total = 0;
-    for (long long t = tid; t < r.T; t += 256) {
+    griddep_launch_dependents();
+#pragma unroll 8
+    for (long long t = tid; t < r.T; t += kRowsThreads) {
         const Idx y = targets[t];
         const int kept = y >= 0 && y < (Idx)r.V;
         total += kept;
@@ -472,11 +511,11 @@ __global__ void __launch_bounds__(256) rows_kernel(const Rows r)
     if (lane == 0) s_sum[0][warp] = before, s_sum[1][warp] = total;
     __syncthreads();
     int base = 0, n = 0;
-    for (int w = 0; w < 8; ++w) base += s_sum[0][w], n += s_sum[1][w];
+    for (int w = 0; w < kRowsWarps; ++w) base += s_sum[0][w], n += s_sum[1][w];
     const bool copy = n < r.T || r.planes > 1;
     const size_t plane = (size_t)r.Tpad * r.D;
     if (blockIdx.x == 0 && tid == 0) r.head[0] = 0, r.head[1] = n;
-    for (long long t0 = begin; t0 < end; t0 += 256) {
+    for (long long t0 = begin; t0 < end; t0 += kRowsThreads) {
         const long long t = t0 + tid;
         const Idx y = t < end ? targets[t] : (Idx)-1;
         const bool kept = y >= 0 && y < (Idx)r.V;
@@ -484,7 +523,7 @@ __global__ void __launch_bounds__(256) rows_kernel(const Rows r)
         if (lane == 0) s_warp[warp] = __popc(votes);
         __syncthreads();
         int pos = base + __popc(votes & ((1u << lane) - 1u));
-        for (int w = 0; w < 8; ++w) {
+        for (int w = 0; w < kRowsWarps; ++w) {
             if (w < warp) pos += s_warp[w];
             base += s_warp[w];
         }
@@ -492,7 +531,7 @@ __global__ void __launch_bounds__(256) rows_kernel(const Rows r)
         if (t < end) {
             if (r.pos_of) r.pos_of[t] = kept ? pos : -1;
             if (kept) {
-                if (r.row_of) r.row_of[pos] = (int)t;
+                r.row_of[pos] = (int)t;
                 if (r.target) r.target[pos] = (int)y;
                 if (r.coef) {
                     const float g = r.d_loss ? r.d_loss[t] : 0.f;
@@ -504,10 +543,15 @@ __global__ void __launch_bounds__(256) rows_kernel(const Rows r)
             }
         }
         __syncthreads();
-        if (copy)
-            for (int i = warp; i < 256 && t0 + i < end; i += 8) {
+        if (copy || r.d_h)
+            for (int i = warp; i < kRowsThreads && t0 + i < end; i += kRowsWarps) {
                 const int at = s_pos[i];
-                if (at < 0) continue;
+                if (at < 0) {
+                    if (r.d_h)
+                        for (int c = lane * 16; c < r.d_h_bytes; c += 512) *reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(r.d_h) + (size_t)(t0 + i) * r.d_h_bytes + c) = make_uint4(0u, 0u, 0u, 0u);
+                    continue;
+                }
+                if (!copy) continue;
                 for (int c = lane * 8; c < r.D; c += 256) copy8(h + (size_t)(t0 + i) * r.h_stride + c, r.hk + (size_t)at * r.D + c, plane);
             }
         __syncthreads();
@@ -521,13 +565,15 @@ __global__ void __launch_bounds__(256) rows_kernel(const Rows r)
         }
         if (copy)
             for (int pl = 0; pl < r.planes; ++pl)
-                for (int c = tid * 8; c < r.D; c += 256 * 8) *reinterpret_cast<uint4 *>(r.hk + pl * plane + (size_t)i * r.D + c) = make_uint4(0u, 0u, 0u, 0u);
+                for (int c = tid * 8; c < r.D; c += kRowsThreads * 8) *reinterpret_cast<uint4 *>(r.hk + pl * plane + (size_t)i * r.D + c) = make_uint4(0u, 0u, 0u, 0u);
     }
 }
 
 // Rows v0 ... v0 + vc of fp32 weights as three bf16 planes [3][vc][D], zero past V.
 __global__ void __launch_bounds__(256) planes_kernel(const float *w, long long w_stride, __nv_bfloat16 *out, int v0, int vc, int V, int D)
 {
+    griddep_launch_dependents();
+    griddep_wait();
     const long long per_row = D / 8, items = per_row * vc;
     for (long long i = blockIdx.x * 256LL + threadIdx.x; i < items; i += gridDim.x * 256LL) {
         const int v = (int)(i / per_row), c = (int)(i % per_row) * 8;
@@ -540,26 +586,33 @@ __global__ void __launch_bounds__(256) planes_kernel(const float *w, long long w
 
 // lse = (m + log2 s) ln 2 over a row's parts; the loss from the differences to the largest logit, so that it keeps its digits
 // where the target has nearly all the weight.
-__global__ void __launch_bounds__(512) join_kernel(const int *head, const int *row_of, const float *zt, const float2 *part, int parts, int T, int Tpad, float *loss, float *lse)
+// A CTA's 256 threads are `groups` threads a row, next to one another rows of one part.
+__global__ void __launch_bounds__(256) join_kernel(const int *head, const int *row_of, const float *zt, const float2 *part, int parts, int T, int Tpad, int groups, float *loss, float *lse)
 {
-    __shared__ float2 s_part[16][33];
-    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
+    __shared__ float2 s_part[256];
+    const int rows = 256 / groups, lane = threadIdx.x % rows, group = threadIdx.x / rows;
+    const long long i = (long long)blockIdx.x * rows + lane;
+    griddep_wait();
     const int n = min(max(head[1], 0), T);
-    if ((int)blockIdx.x * 32 >= n) return;
+    if ((long long)blockIdx.x * rows >= n) return;
     float m = -INFINITY, s = 0.f;
     if (i < n)
-        for (int q = group; q < parts; q += 16) {
+#pragma unroll 4
+        for (int q = group; q < parts; q += groups) {
             const float2 v = part[(size_t)q * Tpad + i];
             const float mm = fmaxf(m, v.x);
             if (mm != -INFINITY) s = s * ex2(m - mm) + v.y * ex2(v.x - mm), m = mm;
         }
-    s_part[group][lane] = make_float2(m, s);
+    s_part[threadIdx.x] = make_float2(m, s);
     __syncthreads();
     if (group == 0 && i < n) {
         float mm = m;
-        for (int g = 1; g < 16; ++g) mm = fmaxf(mm, s_part[g][lane].x);
+        for (int g = 1; g < groups; ++g) mm = fmaxf(mm, s_part[g * rows + lane].x);
         float sum = 0.f;
-        for (int g = 0; g < 16; ++g) sum += s_part[g][lane].x == -INFINITY ? 0.f : s_part[g][lane].y * ex2(s_part[g][lane].x - mm);
+        for (int g = 0; g < groups; ++g) {
+            const float2 v = s_part[g * rows + lane];
+            sum += v.x == -INFINITY ? 0.f : v.y * ex2(v.x - mm);
+        }
         const int t = row_of[i];
         const float log_s = log1pf(sum - 1.f);   // the largest term is 1
         lse[t] = fmaf(mm, kLn2, log_s);
@@ -573,6 +626,7 @@ __device__ __forceinline__ void add4(float4 &a, const float4 b) { a.x += b.x, a.
 template <typename TO>
 __global__ void __launch_bounds__(256) spread_kernel(const int *pos_of, const float *dh, int slices, int T, int Tpad, int D, TO *d_h)
 {
+    griddep_wait();
     const long long per_row = D / 4, items = per_row * T;
     for (long long i = blockIdx.x * 256LL + threadIdx.x; i < items; i += gridDim.x * 256LL) {
         const long long t = i / per_row;
@@ -588,6 +642,7 @@ __global__ void __launch_bounds__(256) spread_kernel(const int *pos_of, const fl
 template <typename TO>
 __global__ void __launch_bounds__(256) add_slices_kernel(const float *part, int slices, int vc, int rows, int D, const TO *dw_in, TO *d_w)
 {
+    griddep_wait();
     const long long items = (long long)rows * D / 4, slice = (long long)vc * D;
     for (long long i = blockIdx.x * 256LL + threadIdx.x; i < items; i += gridDim.x * 256LL) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -610,7 +665,7 @@ int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 // How a call is cut, from its sizes alone, and where its parts lie in the workspace.
 struct Plan {
-    int pairs, Tpad, vc, pieces, per_chunk, chunks, sh, sv, planes_in, planes_dz;
+    int pairs, Tpad, vc, pieces, per_chunk, chunks, sh, sv, planes_in, planes_dz;   // per_chunk: boxes of 64 columns
     size_t row_of, pos_of, target, coef, zt, part, hk, wk, dz, dhp, dwp, bytes;
 };
 
@@ -651,14 +706,26 @@ Plan make_plan(int T, int V, int D, chela_dtype_t in_dtype, chela_dtype_t grad_d
         at += align_up(bytes, 1024);
         return here;
     };
+    q.row_of = take((size_t)q.Tpad * 4);
     q.hk = take((size_t)q.planes_in * q.Tpad * D * 2);
     if (q.planes_in > 1) q.wk = take((size_t)3 * q.vc * D * 2);
     if (!bwd) {
-        // at least about six units a pair, so that the last round weighs little, and at most 16 column tiles a unit
-        long long per = (long long)mt * tiles / (6LL * q.pairs);
-        q.per_chunk = (int)(per < 1 ? 1 : per > 16 ? 16 : per);
-        q.chunks = ceil_div(tiles, q.per_chunk);
-        q.row_of = take((size_t)q.Tpad * 4);
+        // chunks of which the pairs get about the same number of boxes, each a box's worth of overhead; more than two row tiles
+        // are bound by whole tiles of four boxes, fewer by the weights that are read
+        const int boxes = ceil_div(q.pieces > 1 ? q.vc : V, 64);
+        long long best = -1;
+        for (int rounds = 1; rounds <= 64; ++rounds) {
+            long long chunks = (long long)rounds * q.pairs / mt;
+            if (chunks < 1) continue;
+            if (chunks > boxes) chunks = boxes;
+            int per = ceil_div(boxes, chunks);
+            if (mt > 2) per = ceil_div(per, 4) * 4;
+            const long long cost = ceil_div((long long)mt * ceil_div(boxes, per), q.pairs) * (long long)(per + 1);
+            if (best < 0 || cost < best) best = cost, q.per_chunk = per;
+            if (chunks == boxes) break;
+        }
+        if (best < 0) q.per_chunk = boxes < 64 ? boxes : 64;   // many row tiles
+        q.chunks = ceil_div(boxes, q.per_chunk);
         q.target = take((size_t)q.Tpad * 4);
         q.zt = take((size_t)q.Tpad * 4);
         q.part = take((size_t)2 * q.chunks * q.pieces * q.Tpad * 8);
@@ -671,13 +738,15 @@ Plan make_plan(int T, int V, int D, chela_dtype_t in_dtype, chela_dtype_t grad_d
                 if (sh > 1 && (size_t)sh * q.Tpad * D * 4 > kSliceBytes) continue;
                 const long long kdw = ceil_div(ceil_div(T, 64), sv), kdh = ceil_div(q.vc / 64, sh);
                 long long cost = grad_rounds((long long)tiles * nd * sv, kdw, (long long)mt * nd * sh, kdh, q.pairs);
-                cost += cost * (sv + sh - 2) / 200;   // the slices' own traffic
+                // the slices' own traffic, in K blocks of a pair (0.27 us) at 6 TB/s: written, read, and a launch
+                if (sv > 1) cost += (long long)sv * q.vc * D / 200000 + 8;
+                if (sh > 1) cost += ((long long)sh * q.Tpad * D / 200000 + 8) / q.pieces;
                 if (best < 0 || cost < best) best = cost, q.sv = sv, q.sh = sh;
             }
-        q.pos_of = take((size_t)T * 4);
+        if (q.sh > 1) q.pos_of = take((size_t)T * 4);
         q.coef = take((size_t)q.Tpad * 16);
         q.dz = take((size_t)q.planes_dz * q.Tpad * q.vc * 2);
-        q.dhp = take((size_t)q.sh * q.Tpad * D * 4);
+        if (q.sh > 1 || q.pieces > 1) q.dhp = take((size_t)q.sh * q.Tpad * D * 4);
         if (q.sv > 1) q.dwp = take((size_t)q.sv * q.vc * D * 4);
     }
     q.bytes = at;
@@ -692,25 +761,37 @@ bool map_3d(CUtensorMap *map, const void *ptr, bool f32, long long cols, long lo
     return make_map_sw128(map, ptr, f32, 3, dims, strides, box);
 }
 
+// Launch as a programmatic dependent of the kernel before it in the stream, which it waits for by griddep_wait.
+template <typename... P, typename... A>
+chela_status_t launch_after(void (*kernel)(P...), int grid, int threads, int smem, cudaStream_t stream, const A &...args)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(grid), cfg.blockDim = dim3(threads), cfg.dynamicSmemBytes = smem, cfg.stream = stream;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr, cfg.numAttrs = 1;
+    return cuda_status(cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...));
+}
+
 template <int kWhat, bool kSegments>
 chela_status_t launch_product(const Product &p, int pairs, cudaStream_t stream)
 {
     if (cudaFuncSetAttribute(product_kernel<kWhat, kSegments>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess) return CHELA_ERR_CUDA;
-    product_kernel<kWhat, kSegments><<<2 * pairs, kThreads, kSmemBytes, stream>>>(p);
-    return last_launch_status();
+    return launch_after(product_kernel<kWhat, kSegments>, 2 * pairs, kThreads, kSmemBytes, stream, p);
 }
 
 chela_status_t launch_rows(Rows &r, chela_dtype_t in_dtype, bool wide_ids, int sms, cudaStream_t stream)
 {
-    int grid = ceil_div(r.T, 32);
+    int grid = ceil_div(r.T, 32);   // a row or more a warp
     if (grid > 2 * sms) grid = 2 * sms;
     r.per_cta = ceil_div(r.T, grid);
     if (in_dtype == CHELA_F32) {
-        if (wide_ids) rows_kernel<long long, float><<<grid, 256, 0, stream>>>(r);
-        else rows_kernel<int, float><<<grid, 256, 0, stream>>>(r);
+        if (wide_ids) rows_kernel<long long, float><<<grid, kRowsThreads, 0, stream>>>(r);
+        else rows_kernel<int, float><<<grid, kRowsThreads, 0, stream>>>(r);
     } else {
-        if (wide_ids) rows_kernel<long long, __nv_bfloat16><<<grid, 256, 0, stream>>>(r);
-        else rows_kernel<int, __nv_bfloat16><<<grid, 256, 0, stream>>>(r);
+        if (wide_ids) rows_kernel<long long, __nv_bfloat16><<<grid, kRowsThreads, 0, stream>>>(r);
+        else rows_kernel<int, __nv_bfloat16><<<grid, kRowsThreads, 0, stream>>>(r);
     }
     return last_launch_status();
 }
@@ -740,8 +821,7 @@ chela_status_t set_piece(Product &p, const chela_vocabloss_args_t &a, const Plan
     p.v0 = v0;
     p.w_row = q.planes_in > 1 ? 0 : v0;
     if (q.planes_in > 1) {
-        planes_kernel<<<4 * sms, 256, 0, stream>>>((const float *)a.w, a.w_stride, (__nv_bfloat16 *)(ws + q.wk), v0, q.vc, a.V, a.D);
-        return last_launch_status();
+        return launch_after(planes_kernel, 4 * sms, 256, 0, stream, (const float *)a.w, a.w_stride, (__nv_bfloat16 *)(ws + q.wk), v0, q.vc, a.V, a.D);
     }
     return CHELA_OK;
 }
@@ -769,16 +849,16 @@ chela_status_t launch_vocabloss_fwd(const chela_vocabloss_args_t &a, float *loss
     p.terms = q.planes_in > 1 ? kTerms6 : kTerms1;
     int parts = 0;
     for (int i = 0; st == CHELA_OK && i < q.pieces; ++i) {
-        const int v0 = i * q.vc, tiles = ceil_div((a.V - v0 < q.vc ? a.V - v0 : q.vc), kTile);
+        const int v0 = i * q.vc, boxes = ceil_div((a.V - v0 < q.vc ? a.V - v0 : q.vc), 64);
         st = set_piece(p, a, q, ws, v0, sms, stream);
         if (st != CHELA_OK) return st;
         p.first_part = parts;
-        parts += ceil_div(tiles, q.per_chunk);
+        parts += ceil_div(boxes, q.per_chunk);
         st = q.planes_in > 1 ? launch_product<kStats, true>(p, q.pairs, stream) : launch_product<kStats, false>(p, q.pairs, stream);
     }
     if (st != CHELA_OK) return st;
-    join_kernel<<<q.Tpad / 32, 512, 0, stream>>>(p.head, r.row_of, p.zt, p.part, 2 * parts, a.T, q.Tpad, loss, lse);
-    return last_launch_status();
+    const int groups = parts <= 2 ? 1 : parts <= 32 ? 8 : 32;   // threads a row, by the parts (two a chunk)
+    return launch_after(join_kernel, q.Tpad / (256 / groups), 256, 0, stream, p.head, r.row_of, p.zt, p.part, 2 * parts, a.T, q.Tpad, groups, loss, lse);
 }
 
 chela_status_t launch_vocabloss_bwd(const chela_vocabloss_args_t &a, const float *lse, const float *d_loss, const float *d_lse, void *d_h, const void *d_w_in, void *d_w,
@@ -791,20 +871,22 @@ chela_status_t launch_vocabloss_bwd(const chela_vocabloss_args_t &a, const float
     Product p{};
     if (!set_operands(p, a, q, ws)) return CHELA_ERR_CUDA;
     const long long dz_row = (long long)q.vc * 2, es = f32 ? 4 : 2;
+    const bool sums = q.sh > 1 || q.pieces > 1;   // d_h passes through fp32 sums
     if (!map_3d(&p.dz, ws + q.dz, false, q.vc, q.Tpad, q.planes_dz, dz_row, dz_row * q.Tpad, 64, 64) ||
         !map_3d(&p.dz_out, ws + q.dz, false, q.vc, q.Tpad, q.planes_dz, dz_row, dz_row * q.Tpad, 64, 32) ||
-        !map_3d(&p.dh_out, ws + q.dhp, true, a.D, q.Tpad, q.sh, a.D * 4LL, (long long)q.Tpad * a.D * 4, 32, 32))
+        (sums && !map_3d(&p.dh_out, ws + q.dhp, true, a.D, q.Tpad, q.sh, a.D * 4LL, (long long)q.Tpad * a.D * 4, 32, 32)))
         return CHELA_ERR_CUDA;
     if (q.sv > 1 ? !map_3d(&p.dw_out, ws + q.dwp, true, a.D, q.vc, q.sv, a.D * 4LL, (long long)q.vc * a.D * 4, 32, 32)
                  : !map_3d(&p.dw_out, d_w, f32, a.D, a.V, 1, a.D * es, a.D * es, f32 ? 32 : 64, 32))
         return CHELA_ERR_CUDA;
     Rows r{};
     r.targets = a.targets, r.h = a.h, r.h_stride = a.h_stride, r.T = a.T, r.Tpad = q.Tpad, r.V = a.V, r.D = a.D, r.planes = q.planes_in;
-    r.head = p.head, r.pos_of = (int *)(ws + q.pos_of), r.coef = (float4 *)(ws + q.coef), r.hk = (__nv_bfloat16 *)(ws + q.hk);
+    r.head = p.head, r.row_of = (int *)(ws + q.row_of), r.pos_of = q.sh > 1 ? (int *)(ws + q.pos_of) : nullptr, r.coef = (float4 *)(ws + q.coef), r.hk = (__nv_bfloat16 *)(ws + q.hk);
     r.lse = lse, r.d_loss = d_loss, r.d_lse = d_lse, r.scale = a.scale;
+    if (q.sh == 1) r.d_h = d_h, r.d_h_bytes = a.D * (int)es;
     chela_status_t st = launch_rows(r, a.in_dtype, a.wide_ids != 0, sms, stream);
     p.coef = r.coef;
-    p.dw_in = d_w_in, p.dw_bf16 = p.dw_in_bf16 = !f32, p.dw_sliced = q.sv > 1;
+    p.row_of = r.row_of, p.d_h = d_h, p.dw_in = d_w_in, p.grad_bf16 = !f32, p.dw_sliced = q.sv > 1;
     for (int i = 0; st == CHELA_OK && i < q.pieces; ++i) {
         const int v0 = i * q.vc, rows = a.V - v0 < q.vc ? a.V - v0 : q.vc;
         st = set_piece(p, a, q, ws, v0, sms, stream);
@@ -814,20 +896,20 @@ chela_status_t launch_vocabloss_bwd(const chela_vocabloss_args_t &a, const float
         if (st != CHELA_OK) return st;
         p.terms = q.planes_in > 1 ? (f32 ? kTerms6 : kTerms2) : f32 ? kTerms3 : kTerms1;
         p.dh_add = i > 0;
+        p.dh_last = q.sh == 1 && i + 1 == q.pieces;
+        p.dh_before = i > 0 ? (const float *)(ws + q.dhp) : nullptr;
         st = f32 || q.planes_in > 1 ? launch_product<kGrads, true>(p, q.pairs, stream) : launch_product<kGrads, false>(p, q.pairs, stream);
         if (st == CHELA_OK && q.sv > 1) {
             const size_t off = (size_t)v0 * a.D;
             const float *part = (const float *)(ws + q.dwp);
-            if (f32) add_slices_kernel<float><<<4 * sms, 256, 0, stream>>>(part, q.sv, q.vc, rows, a.D, d_w_in ? (const float *)d_w_in + off : nullptr, (float *)d_w + off);
-            else add_slices_kernel<__nv_bfloat16><<<4 * sms, 256, 0, stream>>>(part, q.sv, q.vc, rows, a.D, d_w_in ? (const __nv_bfloat16 *)d_w_in + off : nullptr, (__nv_bfloat16 *)d_w + off);
-            st = last_launch_status();
+            if (f32) st = launch_after(add_slices_kernel<float>, 4 * sms, 256, 0, stream, part, q.sv, q.vc, rows, a.D, d_w_in ? (const float *)d_w_in + off : nullptr, (float *)d_w + off);
+            else st = launch_after(add_slices_kernel<__nv_bfloat16>, 4 * sms, 256, 0, stream, part, q.sv, q.vc, rows, a.D, d_w_in ? (const __nv_bfloat16 *)d_w_in + off : nullptr, (__nv_bfloat16 *)d_w + off);
         }
     }
-    if (st != CHELA_OK) return st;
+    if (st != CHELA_OK || q.sh == 1) return st;
     const float *dhp = (const float *)(ws + q.dhp);
-    if (f32) spread_kernel<float><<<8 * sms, 256, 0, stream>>>((const int *)(ws + q.pos_of), dhp, q.sh, a.T, q.Tpad, a.D, (float *)d_h);
-    else spread_kernel<__nv_bfloat16><<<8 * sms, 256, 0, stream>>>((const int *)(ws + q.pos_of), dhp, q.sh, a.T, q.Tpad, a.D, (__nv_bfloat16 *)d_h);
-    return last_launch_status();
+    if (f32) return launch_after(spread_kernel<float>, 8 * sms, 256, 0, stream, (const int *)(ws + q.pos_of), dhp, q.sh, a.T, q.Tpad, a.D, (float *)d_h);
+    return launch_after(spread_kernel<__nv_bfloat16>, 8 * sms, 256, 0, stream, (const int *)(ws + q.pos_of), dhp, q.sh, a.T, q.Tpad, a.D, (__nv_bfloat16 *)d_h);
 }
 
 }  // namespace chela
