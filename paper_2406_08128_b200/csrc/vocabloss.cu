@@ -25,14 +25,14 @@ namespace {
 using namespace sm100;
 
 constexpr int kTile = 256;              // rows and columns of a tile: 128 rows of A and 128 columns of B in each CTA's memory
-constexpr int kStages = 6, kOperand = 128 * 128, kStageBytes = 2 * kOperand;
+constexpr int kStages = 5, kOperand = 128 * 128, kStageBytes = 2 * kOperand;
 constexpr int kEpilogueWarps = 8, kThreads = 64 + 32 * kEpilogueWarps;
-constexpr int kStagingWarp = 32 * 128;  // a box of 32 rows x 128 bytes
+constexpr int kBox = 32 * 128, kStagingWarp = 2 * kBox;   // two boxes of 32 rows x 128 bytes: one is filled while the other is stored
 constexpr int kSegment = 4;             // K blocks of 64 that fp32 modes add up in the tensor cores
 constexpr int offStaging = kStages * kStageBytes, offBar = offStaging + kEpilogueWarps * kStagingWarp;
 constexpr int offTmem = offBar + 8 * (2 * kStages + 4), offAbort = offTmem + 8, kSmemBytes = offAbort + 8;
 static_assert(kSmemBytes <= 232448, "shared memory per CTA");
-static_assert(kStagingWarp % 1024 == 0 && offStaging % 1024 == 0, "swizzled boxes start on 1024 bytes");
+static_assert(kBox % 1024 == 0 && offStaging % 1024 == 0, "swizzled boxes start on 1024 bytes");
 
 constexpr size_t kHead = 256;           // workspace header: word 0 the asynchronous status, word 1 the number of kept rows
 constexpr float kLn2 = 0.6931471805599453f;
@@ -69,7 +69,7 @@ struct Product {
 
 // One tile of the product that a launch computes.
 struct Tile {
-    int m0, n0, kb0, kb1, boxes;   // boxes: of 64 columns that B has
+    int m0, n0, kb0, kb1, a_boxes, b_boxes;   // boxes of 64 rows of A and columns of B that exist; the others are not loaded
     bool dw;       // d_w's product (A is dz taken by columns)
     int slice;
 };
@@ -77,9 +77,9 @@ struct Tile {
 __device__ __forceinline__ int row_tiles(int n) { return (n + kTile - 1) / kTile; }
 __device__ __forceinline__ int piece_boxes(const Product &p) { return (min(p.vc, p.V - p.v0) + 63) / 64; }
 
-__device__ __forceinline__ long long units_of(const Product &p, int what, int n)
+__device__ __forceinline__ int units_of(const Product &p, int what, int n)
 {
-    const long long mt = row_tiles(n), boxes = piece_boxes(p), nt = (boxes + 3) / 4, nd = (p.D + kTile - 1) / kTile;
+    const int mt = row_tiles(n), boxes = piece_boxes(p), nt = (boxes + 3) / 4, nd = (p.D + kTile - 1) / kTile;
     if (what == kStats) return mt * ((boxes + p.per_chunk - 1) / p.per_chunk);
     if (what == kSlopes) return mt * nt;
     return nd * (nt * p.sv + mt * p.sh);
@@ -87,40 +87,41 @@ __device__ __forceinline__ long long units_of(const Product &p, int what, int n)
 
 // kStats: a unit is a chunk of per_chunk boxes of 64 columns of one row tile, four boxes a tile.  Neighbouring units share their
 // columns: the weights of a chunk are read by all row tiles about the same time.
-__device__ __forceinline__ Tile tile_of(const Product &p, int what, int n, long long u, int j)
+__device__ __forceinline__ Tile tile_of(const Product &p, int what, int n, int u, int j)
 {
     Tile t{};
     const int mt = row_tiles(n), nd = (p.D + kTile - 1) / kTile;
-    t.boxes = 4;
     if (what != kGrads) {
-        const int at = (int)(u / mt);
-        t.m0 = (int)(u % mt) * kTile;
+        const int at = u / mt;
+        t.m0 = u % mt * kTile;
         t.kb1 = (p.D + 63) / 64;
-        if (what == kSlopes) {
-            t.n0 = at * kTile;
-            return t;
-        }
-        const int box = at * p.per_chunk + 4 * j;
+        const int per = what == kSlopes ? 4 : p.per_chunk, box = at * per + 4 * j;
         t.n0 = box * 64;
-        t.boxes = min(4, min((at + 1) * p.per_chunk, piece_boxes(p)) - box);
+        t.a_boxes = min(4, (n - t.m0 + 63) / 64);
+        t.b_boxes = min(4, min((at + 1) * per, piece_boxes(p)) - box);
         return t;
     }
     // d_w's tiles first: with many tokens they are the longer ones
-    const long long ndw = (long long)((piece_boxes(p) + 3) / 4) * nd * p.sv;
+    const int ndw = (piece_boxes(p) + 3) / 4 * nd * p.sv;
     t.dw = u < ndw;
-    const long long v = t.dw ? u : u - ndw;
+    const int v = t.dw ? u : u - ndw, tile = v / nd;
     const int slices = t.dw ? p.sv : p.sh, kbs = t.dw ? (n + 63) / 64 : piece_boxes(p);
-    t.n0 = (int)(v % nd) * kTile;
-    t.slice = (int)(v / nd % slices);
-    t.m0 = (int)(v / nd / slices) * kTile;
-    t.kb0 = (int)((long long)kbs * t.slice / slices);
-    t.kb1 = (int)((long long)kbs * (t.slice + 1) / slices);
+    t.n0 = (v - tile * nd) * kTile;
+    t.m0 = tile / slices * kTile;
+    t.slice = tile % slices;
+    t.kb1 = kbs;
+    if (slices > 1) {
+        t.kb0 = (int)((long long)kbs * t.slice / slices);
+        t.kb1 = (int)((long long)kbs * (t.slice + 1) / slices);
+    }
+    t.a_boxes = min(4, t.dw ? piece_boxes(p) - t.m0 / 64 : (n - t.m0 + 63) / 64);
+    t.b_boxes = min(4, (p.D - t.n0 + 63) / 64);
     return t;
 }
-__device__ __forceinline__ int tiles_in_unit(const Product &p, int what, int n, long long u)
+__device__ __forceinline__ int tiles_in_unit(const Product &p, int what, int n, int u)
 {
     if (what != kStats) return 1;
-    const int at = (int)(u / row_tiles(n));
+    const int at = u / row_tiles(n);
     return (min((at + 1) * p.per_chunk, piece_boxes(p)) - at * p.per_chunk + 3) / 4;
 }
 
@@ -144,7 +145,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     const uint32_t sbase = smem_u32(smem);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = cluster_rank();
-    const long long pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const uint32_t bar_full = sbase + offBar, bar_empty = bar_full + 8 * kStages, bar_tfull = bar_empty + 8 * kStages, bar_tempty = bar_tfull + 16;
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + offTmem);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + offAbort);
@@ -172,7 +173,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     griddep_launch_dependents();
     griddep_wait();   // up to here the kernel before this one may still run
     const int n = min(max(p.head[1], 0), p.T);
-    const long long units = units_of(p, kWhat, n);
+    const int units = units_of(p, kWhat, n);
     // h as given when no row is left out, else the kept rows' copy
     const CUtensorMap *map_h = (n == p.T && !p.h_in_planes) ? &p.h : &p.hk;
     bool ok = true;
@@ -181,7 +182,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         // ------------------------------------------------------------------ TMA producer
         if (lane == 0) {
             int it = 0;
-            for (long long u = pair; ok && u < units; u += pairs) {
+            for (int u = pair; ok && u < units; u += pairs) {
                 const int tiles = tiles_in_unit(p, kWhat, n, u);
                 for (int j = 0; ok && j < tiles; ++j) {
                     const Tile t = tile_of(p, kWhat, n, u, j);
@@ -198,9 +199,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                                 ok = mbar_wait(bar_empty + 8 * s, ((it / kStages) & 1) ^ 1, abort_flag, p.wc.limit);
                                 if (!ok) break;
                                 const uint32_t bar = bar_full + 8 * s, dst = sbase + s * kStageBytes, to = map_to_rank(bar, 0);
-                                if (rank == 0) mbar_expect_tx(bar, 2 * kOperand + t.boxes * 8192);
-                                load_operand(dst, map_a, to, a_mn, t.m0 + (int)rank * 128, k, kSegments ? terms.a >> 2 * i & 3 : 0, 2);
-                                load_operand(dst + kOperand, map_b, to, b_mn, t.n0 + b_row + (int)rank * 128, k + b_kb, kSegments ? terms.b >> 2 * i & 3 : 0, t.boxes - 2 * (int)rank);
+                                if (rank == 0) mbar_expect_tx(bar, (t.a_boxes + t.b_boxes) * 8192);
+                                load_operand(dst, map_a, to, a_mn, t.m0 + (int)rank * 128, k, kSegments ? terms.a >> 2 * i & 3 : 0, t.a_boxes - 2 * (int)rank);
+                                load_operand(dst + kOperand, map_b, to, b_mn, t.n0 + b_row + (int)rank * 128, k + b_kb, kSegments ? terms.b >> 2 * i & 3 : 0, t.b_boxes - 2 * (int)rank);
                             }
                 }
             }
@@ -216,7 +217,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         // ------------------------------------------------------------------ MMA issuer
         if (lane == 0 && rank == 0) {
             int it = 0, gs = 0;
-            for (long long u = pair; ok && u < units; u += pairs) {
+            for (int u = pair; ok && u < units; u += pairs) {
                 const int tiles = tiles_in_unit(p, kWhat, n, u);
                 for (int j = 0; ok && j < tiles; ++j) {
                     const Tile t = tile_of(p, kWhat, n, u, j);
@@ -263,8 +264,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         uint8_t *stg = smem + offStaging + (warp - 2) * kStagingWarp;
         const uint32_t stg_u32 = sbase + offStaging + (warp - 2) * kStagingWarp;
         const uint32_t leader_tempty = map_to_rank(bar_tempty, 0);
-        int gs = 0;
-        for (long long u = pair; ok && u < units; u += pairs) {
+        int gs = 0, boxes = 0;
+        for (int u = pair; ok && u < units; u += pairs) {
             const int tiles = tiles_in_unit(p, kWhat, n, u);
             float run_m = -INFINITY, run_s = 0.f;
             for (int j = 0; ok && j < tiles; ++j) {
@@ -300,11 +301,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     if (lane == 0 && !(p.wc.skip_arrival && blockIdx.x == 0 && gs == 0 && warp == 2)) mbar_arrive_cluster(leader_tempty + 8 * buf);
                 }
                 if (!ok) break;
+                if (kWhat != kGrads && row0 >= 64 * t.a_boxes) continue;   // rows of no token, not even loaded
                 const int c0 = t.n0 + half * 128;   // first column of this thread's 128, in the piece
                 if (kWhat == kStats) {
                     int y = p.target[t.m0 + row] - p.v0 - c0;
-                    if (y + c0 >= t.n0 + 64 * t.boxes) y = -1;   // a later chunk's
-                    const int end = min(t.n0 + 64 * t.boxes, p.V - p.v0);
+                    if (y + c0 >= t.n0 + 64 * t.b_boxes) y = -1;   // a later chunk's
+                    const int end = min(t.n0 + 64 * t.b_boxes, p.V - p.v0);
                     if (c0 + 128 > end) {
 #pragma unroll
                         for (int c = 0; c < 128; ++c)
@@ -337,10 +339,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
 #pragma unroll
                         for (int c = 0; c < 128; ++c) z[c] = c == y ? z[c] - cf.z : z[c];
                     }
-                    if (c0 + 128 > p.V - p.v0 || t.m0 + kTile > n) {
+                    // (rows behind the last token are zero: h is, to the end of its 64, and so are their factors)
+                    if (c0 + 128 > p.V - p.v0) {
 #pragma unroll
                         for (int c = 0; c < 128; ++c)
-                            if (c0 + c >= p.V - p.v0 || t.m0 + row >= n) z[c] = 0.f;
+                            if (c0 + c >= p.V - p.v0) z[c] = 0.f;
                     }
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
@@ -356,14 +359,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                                     z[64 * c + 2 * e + 1] -= f.y;
                                 }
                             }
-                            if (lane == 0) bulk_wait_read0();
+                            // (every box is a bulk group, stored or not, so that the last but one has left this buffer)
+                            const uint32_t buf = (boxes++ & 1) * kBox;
+                            if (lane == 0) bulk_wait_read1();
                             __syncwarp();
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4 *>(stg + sw128(lane, e)) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                            for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4 *>(stg + buf + sw128(lane, e)) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
                             fence_proxy_async();
                             __syncwarp();
-                            if (lane == 0 && c0 + 64 * c < p.vc) {
-                                tma_store_3d(&p.dz_out, stg_u32, c0 + 64 * c, t.m0 + row0, plane);
+                            if (lane == 0) {
+                                if (c0 + 64 * c < p.vc) tma_store_3d(&p.dz_out, stg_u32 + buf, c0 + 64 * c, t.m0 + row0, plane);
                                 bulk_commit();
                             }
                         }
@@ -382,12 +387,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                                 z[c] += o.x, z[c + 1] += o.y, z[c + 2] += o.z, z[c + 3] += o.w;
                             }
                     }
-                    const int first = out_row - lane, rows = t.dw ? (p.dw_sliced ? p.vc : p.V) : p.Tpad;
+                    const int first = out_row - lane, rows = t.dw ? (p.dw_sliced ? p.vc : p.V) : n;
                     const int token = !t.dw && final && t.m0 + row < n ? p.row_of[t.m0 + row] : -1;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         if (wide && (c & 1)) continue;
-                        if (lane == 0) bulk_wait_read0();
+                        const uint32_t buf = (boxes++ & 1) * kBox;
+                        if (lane == 0) bulk_wait_read1();
                         __syncwarp();
                         if (wide) {
 #pragma unroll
@@ -395,12 +401,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                                 uint32_t v[4];
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) v[i] = pack_bf16(z[(32 * c + 8 * e + 2 * i) & 127], z[(32 * c + 8 * e + 2 * i + 1) & 127]);
-                                *reinterpret_cast<uint4 *>(stg + sw128(lane, e)) = make_uint4(v[0], v[1], v[2], v[3]);
+                                *reinterpret_cast<uint4 *>(stg + buf + sw128(lane, e)) = make_uint4(v[0], v[1], v[2], v[3]);
                             }
                         } else {
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
-                                *reinterpret_cast<float4 *>(stg + sw128(lane, e)) = make_float4(z[32 * c + 4 * e], z[32 * c + 4 * e + 1], z[32 * c + 4 * e + 2], z[32 * c + 4 * e + 3]);
+                                *reinterpret_cast<float4 *>(stg + buf + sw128(lane, e)) = make_float4(z[32 * c + 4 * e], z[32 * c + 4 * e + 1], z[32 * c + 4 * e + 2], z[32 * c + 4 * e + 3]);
                         }
                         if (!t.dw && final) {
                             // rows go to where their tokens are: eight lanes a row of 128 bytes
@@ -409,25 +415,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
 #pragma unroll
                             for (int e = 0; e < 8; ++e) {
                                 const int r = e * 4 + (lane >> 3), to = __shfl_sync(0xffffffffu, token, r);
-                                const uint4 v = *reinterpret_cast<const uint4 *>(stg + sw128(r, lane & 7));
+                                const uint4 v = *reinterpret_cast<const uint4 *>(stg + buf + sw128(r, lane & 7));
                                 if (to >= 0 && col < p.D) *reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(p.d_h) + ((size_t)to * p.D + col) * es) = v;
                             }
                             __syncwarp();
+                            if (lane == 0) bulk_commit();
                             continue;
                         }
                         fence_proxy_async();
                         __syncwarp();
-                        if (lane == 0 && c0 + 32 * c < p.D && first < rows) {
-                            if (t.dw) tma_store_3d(&p.dw_out, stg_u32, c0 + 32 * c, first, p.dw_sliced ? t.slice : 0);
-                            else if (p.dh_add) tma_add_3d(&p.dh_out, stg_u32, c0 + 32 * c, first, t.slice);
-                            else tma_store_3d(&p.dh_out, stg_u32, c0 + 32 * c, first, t.slice);
+                        if (lane == 0) {
+                            if (c0 + 32 * c < p.D && first < rows) {
+                                if (t.dw) tma_store_3d(&p.dw_out, stg_u32 + buf, c0 + 32 * c, first, p.dw_sliced ? t.slice : 0);
+                                else if (p.dh_add) tma_add_3d(&p.dh_out, stg_u32 + buf, c0 + 32 * c, first, t.slice);
+                                else tma_store_3d(&p.dh_out, stg_u32 + buf, c0 + 32 * c, first, t.slice);
+                            }
                             bulk_commit();
                         }
                     }
                 }
             }
             if (ok && kWhat == kStats) {
-                const int chunk = p.first_part + (int)(u / row_tiles(n)), m0 = (int)(u % row_tiles(n)) * kTile;
+                const int chunk = p.first_part + u / row_tiles(n), m0 = u % row_tiles(n) * kTile;
                 p.part[(size_t)(2 * chunk + half) * p.Tpad + m0 + row] = make_float2(run_m, run_s);
             }
         }
@@ -556,17 +565,15 @@ __global__ void __launch_bounds__(kRowsThreads) rows_kernel(const Rows r)
             }
         __syncthreads();
     }
-    // behind the last kept row, to the end of its tile
-    const int padded = min(r.Tpad, (n + kTile - 1) / kTile * kTile);
-    for (int i = n + blockIdx.x; i < padded; i += gridDim.x) {
-        if (tid == 0) {
-            if (r.target) r.target[i] = -1;
-            if (r.coef) r.coef[i] = make_float4(0.f, 0.f, 0.f, __int_as_float(-1));
-        }
-        if (copy)
-            for (int pl = 0; pl < r.planes; ++pl)
-                for (int c = tid * 8; c < r.D; c += kRowsThreads * 8) *reinterpret_cast<uint4 *>(r.hk + pl * plane + (size_t)i * r.D + c) = make_uint4(0u, 0u, 0u, 0u);
+    // behind the last kept row: no targets to the end of its tile, zeros of h to the end of its 64 (d_w's sums read so many)
+    for (int i = n + blockIdx.x * kRowsThreads + tid; i < min(r.Tpad, (n + kTile - 1) / kTile * kTile); i += gridDim.x * kRowsThreads) {
+        if (r.target) r.target[i] = -1;
+        if (r.coef) r.coef[i] = make_float4(0.f, 0.f, 0.f, __int_as_float(-1));
     }
+    if (copy)
+        for (int i = n + blockIdx.x * kRowsWarps + warp; i < (n + 63) / 64 * 64; i += gridDim.x * kRowsWarps)
+            for (int pl = 0; pl < r.planes; ++pl)
+                for (int c = lane * 8; c < r.D; c += 256) *reinterpret_cast<uint4 *>(r.hk + pl * plane + (size_t)i * r.D + c) = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // Rows v0 ... v0 + vc of fp32 weights as three bf16 planes [3][vc][D], zero past V.
@@ -783,7 +790,7 @@ chela_status_t launch_product(const Product &p, int pairs, cudaStream_t stream)
 
 chela_status_t launch_rows(Rows &r, chela_dtype_t in_dtype, bool wide_ids, int sms, cudaStream_t stream)
 {
-    int grid = ceil_div(r.T, 32);   // a row or more a warp
+    int grid = ceil_div(r.T, 16);   // a row or more a warp
     if (grid > 2 * sms) grid = 2 * sms;
     r.per_cta = ceil_div(r.T, grid);
     if (in_dtype == CHELA_F32) {
