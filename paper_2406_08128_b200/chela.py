@@ -814,8 +814,8 @@ def vocabloss_fwd(h, w, targets, scale=1.0, loss=None, lse=None, workspace=None)
     and the logarithm of its normaliser; both zero where the target is outside [0, V)."""
     where = "chela_vocabloss_fwd"
     r, dev = _vocabloss_args(where, h, w, targets, scale)
-    loss = _new(loss, where, "loss", targets.shape, torch.float32, targets.device, dev)
-    lse = _new(lse, where, "lse", targets.shape, torch.float32, targets.device, dev)
+    loss = _new_like(loss, where, "loss", targets, torch.float32, dev)
+    lse = _new_like(lse, where, "lse", targets, torch.float32, dev)
     workspace, ws, nbytes = _scratch(lib().chela_vocabloss_workspace_bytes(r.T, r.V, r.D, r.in_dtype), workspace, targets.device, where, dev)
     _run(lib().chela_vocabloss_fwd, where, dev, ctypes.byref(r), loss.data_ptr(), lse.data_ptr(), ws, nbytes)
     return loss, lse
@@ -829,7 +829,7 @@ def vocabloss_bwd(h, w, targets, lse, d_loss, d_lse=None, scale=1.0, grad_dtype=
     gt, f32, shape = _tdtype(grad_dtype), torch.float32, targets.shape
     before = _flat(d_w_in, where, "d_w_in", w.shape, gt, dev)
     d_h = _like(h, gt)
-    d_w = _new(d_w, where, "d_w", w.shape, gt, w.device, dev)
+    d_w = _new_like(d_w, where, "d_w", w, gt, dev)
     workspace, ws, nbytes = _scratch(lib().chela_vocabloss_bwd_workspace_bytes(r.T, r.V, r.D, r.in_dtype, int(grad_dtype)), workspace, targets.device, where, dev)
     _run(lib().chela_vocabloss_bwd, where, dev, ctypes.byref(r), _flat(lse, where, "lse", shape, f32, dev), _flat(d_loss, where, "d_loss", shape, f32, dev),
          _flat(d_lse, where, "d_lse", shape, f32, dev), d_h.data_ptr(), before, d_w.data_ptr(), int(grad_dtype), ws, nbytes)

@@ -2,6 +2,8 @@
 // code here.
 #include <math.h>
 
+#include <atomic>
+
 #include "common.cuh"
 
 using namespace chela;
@@ -44,6 +46,22 @@ chela_status_t check_loss(const chela_vocabloss_args_t *a)
 bool query_ok(int T, int V, int D) { return check_sizes(T, V, D) == CHELA_OK; }
 
 }  // namespace
+
+namespace chela {
+
+int current_sm_count()
+{
+    static std::atomic<int> counts[64];   // of a device, once asked for: it does not change
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return 148;
+    int n = dev < 64 ? counts[dev].load(std::memory_order_relaxed) : 0;
+    if (n > 0) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return 148;
+    if (dev < 64) counts[dev].store(n, std::memory_order_relaxed);
+    return n;
+}
+
+}  // namespace chela
 
 extern "C" {
 

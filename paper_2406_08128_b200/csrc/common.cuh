@@ -45,6 +45,9 @@ __device__ __forceinline__ float load1(const __nv_bfloat16 *p) { return __bfloat
 __device__ __forceinline__ void store1(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
+// Multiprocessors of the current device (148 where the runtime does not say).
+int current_sm_count();
+
 // How long a device-side wait may last, and the test hook that makes one run out: the tensor-core kernels take this
 // by value.  `limit` is in SM cycles; `skip_arrival` != 0 asks CTA 0 to leave out one mbarrier arrival (the role that
 // waits for it then gives up after `limit` cycles, records CHELA_ERR_TIMEOUT and the kernel returns by itself).

@@ -521,12 +521,6 @@ __global__ void __launch_bounds__(256) other_rows_kernel(const unsigned *present
     }
 }
 
-int sm_count()
-{
-    int sms = 0, dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0) sms = 148;
-    return sms;
-}
 int grid_for(long long items, long long per_cta, int most) { const long long g = (items + per_cta - 1) / per_cta; return (int)(g < most ? g : most); }
 
 struct Plan {
@@ -603,7 +597,7 @@ template <typename Idx, typename TI, typename TO>
 chela_status_t embed_bwd(const Idx *ids, const TI *d_out, long long d_out_stride, const TO *d_w_in, TO *d_w, int T, int V, int D, float scale, uint8_t *ws, cudaStream_t stream)
 {
     const Plan q = make_plan(T, V, D);
-    const int sms = sm_count();
+    const int sms = current_sm_count();
     const chela_status_t st = arrange(ids, T, V, D, d_w_in, d_w, q, ws, sms, stream);
     if (st != CHELA_OK) return st;
     const int *keys = (const int *)(ws + q.keys[0]), *from = (const int *)(ws + q.from[0]);
@@ -630,7 +624,7 @@ chela_status_t embed_bwd(const void *ids, bool wide_ids, const void *d_out, long
 template <typename Idx, typename TI>
 void embed_to(const void *ids, const void *w, long long w_stride, void *out, int T, int V, int D, float scale, chela_dtype_t out_dtype, cudaStream_t stream)
 {
-    const int grid = grid_for((long long)T * ((D + 255) / 256), 8, 16 * sm_count());
+    const int grid = grid_for((long long)T * ((D + 255) / 256), 8, 16 * current_sm_count());
     if (out_dtype == CHELA_F32) embed_kernel<Idx, TI, float><<<grid, 256, 0, stream>>>((const Idx *)ids, (const TI *)w, w_stride, (float *)out, T, V, D, scale);
     else embed_kernel<Idx, TI, __nv_bfloat16><<<grid, 256, 0, stream>>>((const Idx *)ids, (const TI *)w, w_stride, (__nv_bfloat16 *)out, T, V, D, scale);
 }

@@ -18,6 +18,7 @@
 // the segments in registers.
 #include "packed.cuh"
 #include "sm100_pair.cuh"
+#include "vocabloss.cuh"
 
 namespace chela {
 namespace {
@@ -316,13 +317,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
 #pragma unroll
                     for (int c = 4; c < 128; ++c) m4[c & 3] = fmaxf(m4[c & 3], z[c]);
                     const float m = fmaxf(run_m, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.c2);
-                    if (m != -INFINITY) {
-                        float s4[4] = {run_s * ex2(run_m - m), 0.f, 0.f, 0.f};
+                    const float shift = m == -INFINITY ? 0.f : m;
+                    float s4[4] = {run_s * rescale(run_m, m), 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int c = 0; c < 128; ++c) s4[c & 3] += ex2(fmaf(z[c], p.c2, -m));
-                        run_s = (s4[0] + s4[1]) + (s4[2] + s4[3]);
-                        run_m = m;
-                    }
+                    for (int c = 0; c < 128; ++c) s4[c & 3] += ex2(fmaf(z[c], p.c2, -shift));
+                    run_s = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    run_m = m;
                     if (__any_sync(0xffffffffu, y >= 0 && y < 128)) {
                         float zy = 0.f;
 #pragma unroll
@@ -608,7 +608,7 @@ __global__ void __launch_bounds__(256) join_kernel(const int *head, const int *r
         for (int q = group; q < parts; q += groups) {
             const float2 v = part[(size_t)q * Tpad + i];
             const float mm = fmaxf(m, v.x);
-            if (mm != -INFINITY) s = s * ex2(m - mm) + v.y * ex2(v.x - mm), m = mm;
+            s = s * rescale(m, mm) + v.y * rescale(v.x, mm), m = mm;
         }
     s_part[threadIdx.x] = make_float2(m, s);
     __syncthreads();
@@ -618,7 +618,7 @@ __global__ void __launch_bounds__(256) join_kernel(const int *head, const int *r
         float sum = 0.f;
         for (int g = 0; g < groups; ++g) {
             const float2 v = s_part[g * rows + lane];
-            sum += v.x == -INFINITY ? 0.f : v.y * ex2(v.x - mm);
+            sum += v.y * rescale(v.x, mm);
         }
         const int t = row_of[i];
         const float log_s = log1pf(sum - 1.f);   // the largest term is 1
@@ -661,13 +661,6 @@ __global__ void __launch_bounds__(256) add_slices_kernel(const float *part, int 
 
 // ---------------------------------------------------------------------------------------------------------------------
 
-int sm_count()
-{
-    int sms = 0, dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0) sms = 148;
-    return sms;
-}
-
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 // How a call is cut, from its sizes alone, and where its parts lie in the workspace.
@@ -693,7 +686,7 @@ long long grad_rounds(long long ndw, long long kdw, long long ndh, long long kdh
 Plan make_plan(int T, int V, int D, chela_dtype_t in_dtype, chela_dtype_t grad_dtype, bool bwd)
 {
     Plan q{};
-    q.pairs = sm_count() / 2;
+    q.pairs = current_sm_count() / 2;
     q.Tpad = ceil_div(T, kTile) * kTile;
     q.planes_in = in_dtype == CHELA_F32 ? 3 : 1;
     q.planes_dz = grad_dtype == CHELA_F32 ? 3 : 1;
@@ -835,14 +828,20 @@ chela_status_t set_piece(Product &p, const chela_vocabloss_args_t &a, const Plan
 
 }  // namespace
 
-size_t vocabloss_workspace_bytes(int T, int V, int D, chela_dtype_t in_dtype) { return make_plan(T, V, D, in_dtype, CHELA_BF16, false).bytes; }
+size_t vocabloss_workspace_bytes(int T, int V, int D, chela_dtype_t in_dtype)
+{
+    const size_t few = vocabloss_few_workspace_bytes(T, V, D, in_dtype, false);
+    return few ? few : make_plan(T, V, D, in_dtype, CHELA_BF16, false).bytes;
+}
 size_t vocabloss_bwd_workspace_bytes(int T, int V, int D, chela_dtype_t in_dtype, chela_dtype_t grad_dtype)
 {
-    return make_plan(T, V, D, in_dtype, grad_dtype, true).bytes;
+    const size_t few = vocabloss_few_workspace_bytes(T, V, D, in_dtype, true);
+    return few ? few : make_plan(T, V, D, in_dtype, grad_dtype, true).bytes;
 }
 
 chela_status_t launch_vocabloss_fwd(const chela_vocabloss_args_t &a, float *loss, float *lse, void *workspace, cudaStream_t stream)
 {
+    if (vocabloss_few_workspace_bytes(a.T, a.V, a.D, a.in_dtype, false)) return launch_vocabloss_few_fwd(a, loss, lse, workspace, stream);
     const Plan q = make_plan(a.T, a.V, a.D, a.in_dtype, CHELA_BF16, false);
     uint8_t *ws = reinterpret_cast<uint8_t *>(workspace);
     const int sms = 2 * q.pairs;
@@ -871,6 +870,7 @@ chela_status_t launch_vocabloss_fwd(const chela_vocabloss_args_t &a, float *loss
 chela_status_t launch_vocabloss_bwd(const chela_vocabloss_args_t &a, const float *lse, const float *d_loss, const float *d_lse, void *d_h, const void *d_w_in, void *d_w,
                                     chela_dtype_t grad_dtype, void *workspace, cudaStream_t stream)
 {
+    if (vocabloss_few_workspace_bytes(a.T, a.V, a.D, a.in_dtype, true)) return launch_vocabloss_few_bwd(a, lse, d_loss, d_lse, d_h, d_w_in, d_w, grad_dtype, workspace, stream);
     const Plan q = make_plan(a.T, a.V, a.D, a.in_dtype, grad_dtype, true);
     uint8_t *ws = reinterpret_cast<uint8_t *>(workspace);
     const int sms = 2 * q.pairs;
