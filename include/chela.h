@@ -515,7 +515,7 @@ chela_status_t chela_vocabloss_fwd(const chela_vocabloss_args_t *args, float *lo
  * Gradients of chela_vocabloss_fwd for the same args and its lse.  d_loss, d_lse : [T] fp32, the gradients of loss and lse, either
  * may be NULL (zero), not both.  With dz[t,v] = scale ((d_loss[t] + d_lse[t]) exp(z[t,v] - lse[t]) - d_loss[t] [v = targets[t]]),
  *   d_h = dz w  : [T, D],   d_w = d_w_in + dz^T h  : [V, D],   both of grad_dtype and contiguous.
- * d_w_in : [V, D] grad_dtype or NULL (zero), may be d_w itself.  With grad_dtype BF16, dz is rounded to bf16 between the
+ * d_w_in : [V, D] grad_dtype or NULL (zero), may be d_w itself.  With grad_dtype BF16, dz may be rounded to bf16 between the
  * products; with F32 it is kept to 24 bits, at three times their cost.  The vocabulary is walked in pieces whose dz (at most
  * 512 MB, or 256 columns) lies in the workspace.
  */

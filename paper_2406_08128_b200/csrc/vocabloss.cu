@@ -11,11 +11,11 @@
 // Left-out rows (target outside the vocabulary) cost nothing and are never read: the kept rows are numbered on the device, all
 // kernels walk those, and h is copied together only where some are left out.
 //
-// bf16 operands go to the tensor cores as they are; dz is rounded to bf16 where the gradients are bf16 (its rounding is as large
-// as theirs and independent between terms) and split in three bf16 planes (24 bits) where they are fp32.  fp32 operands are
-// split in three planes too, and a product of them is the six plane products that reach 2^-24 of the result, the small ones
-// first.  The tensor cores truncate the accumulator at every step, so the fp32 modes end a sum after kSegment columns and add
-// the segments in registers.
+// bf16 operands go to the tensor cores as they are; dz is rounded to bf16 where the gradients are bf16 and their sums have many
+// terms (its rounding is as large as theirs and independent between terms), and split in bf16 planes otherwise: two, or three
+// (24 bits) where the gradients are fp32.  fp32 operands are split in three planes too, and a product of
+// them is the six plane products that reach 2^-24 of the result, the small ones first.  The tensor cores truncate the
+// accumulator at every step, so the fp32 modes end a sum after kSegment blocks and add the segments in registers.
 #include "packed.cuh"
 #include "sm100_pair.cuh"
 #include "vocabloss.cuh"
@@ -29,7 +29,7 @@ constexpr int kTile = 256;              // rows and columns of a tile: 128 rows 
 constexpr int kStages = 5, kOperand = 128 * 128, kStageBytes = 2 * kOperand;
 constexpr int kEpilogueWarps = 8, kThreads = 64 + 32 * kEpilogueWarps;
 constexpr int kBox = 32 * 128, kStagingWarp = 2 * kBox;   // two boxes of 32 rows x 128 bytes: one is filled while the other is stored
-constexpr int kSegment = 4;             // K blocks of 64 that fp32 modes add up in the tensor cores
+constexpr int kSegment = 4, kLongSegment = 16;   // K blocks of 64 that the tensor cores add up: fp32 gradients and logits; bf16 ones
 constexpr int offStaging = kStages * kStageBytes, offBar = offStaging + kEpilogueWarps * kStagingWarp;
 constexpr int offTmem = offBar + 8 * (2 * kStages + 4), offAbort = offTmem + 8, kSmemBytes = offAbort + 8;
 static_assert(kSmemBytes <= 232448, "shared memory per CTA");
@@ -46,7 +46,8 @@ struct Terms {
     uint32_t a, b;
 };
 constexpr Terms kTerms1 = {1, 0, 0};
-constexpr Terms kTerms2 = {2, 0, 1 | 0 << 2};                                                                  // B in planes, two of them
+constexpr Terms kTerms2A = {2, 1 | 0 << 2, 0};                                                                 // A in planes, two of them
+constexpr Terms kTerms3B = {3, 0 | 1 << 2 | 0 << 4, 1 | 0 << 2 | 0 << 4};                                      // both, two of them
 constexpr Terms kTerms3 = {3, 2 | 1 << 2 | 0 << 4, 0};                                                        // A in planes
 constexpr Terms kTerms6 = {6, 2 | 0 << 2 | 1 << 4 | 1 << 6 | 0 << 8 | 0 << 10, 0 | 2 << 2 | 1 << 4 | 0 << 6 | 1 << 8 | 0 << 10};   // both
 
@@ -63,7 +64,7 @@ struct Product {
     void *d_h;
     const float *dh_before;         // d_h's sum over the pieces before, where dh_last
     int T, Tpad, V, D, v0, vc, w_row, per_chunk, first_part, sh, sv, planes;
-    int h_in_planes, dh_add, dh_last, grad_bf16, dw_sliced;
+    int h_in_planes, dh_add, dh_last, grad_bf16, dw_sliced, segment;
     float c2;                       // scale log2 e
     WaitCtl wc;
 };
@@ -125,6 +126,9 @@ __device__ __forceinline__ int tiles_in_unit(const Product &p, int what, int n, 
     const int at = u / row_tiles(n);
     return (min((at + 1) * p.per_chunk, piece_boxes(p)) - at * p.per_chunk + 3) / 4;
 }
+
+// Columns of a tile that a CTA's half of B has: the product is as wide as the boxes that exist, and each CTA brings half of it.
+__device__ __forceinline__ int b_half(const Tile &t) { return 32 * t.b_boxes; }
 
 // Half an operand tile: 128 rows of M or N by 64 of K as two boxes of 64 x 64 (or fewer, the rest left as it is).
 __device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap *map, uint32_t bar, bool mn_major, int mn, int kb, int plane, int boxes)
@@ -192,7 +196,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     const Terms terms = p.terms;
                     // weights: rows of the vocabulary are B's columns for logits and its K for d_h
                     const int b_row = kWhat != kGrads ? p.w_row : 0, b_kb = kWhat == kGrads && !t.dw ? p.w_row / 64 : 0;
-                    const int seg = kSegments ? kSegment : t.kb1 - t.kb0;
+                    const int seg = kSegments ? p.segment : t.kb1 - t.kb0;
                     for (int kb = t.kb0; ok && kb < t.kb1; kb += seg)
                         for (int i = 0; ok && i < (kSegments ? terms.n : 1); ++i)
                             for (int k = kb; k < min(kb + seg, t.kb1); ++k, ++it) {
@@ -200,9 +204,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                                 ok = mbar_wait(bar_empty + 8 * s, ((it / kStages) & 1) ^ 1, abort_flag, p.wc.limit);
                                 if (!ok) break;
                                 const uint32_t bar = bar_full + 8 * s, dst = sbase + s * kStageBytes, to = map_to_rank(bar, 0);
-                                if (rank == 0) mbar_expect_tx(bar, (t.a_boxes + t.b_boxes) * 8192);
+                                if (rank == 0) mbar_expect_tx(bar, (t.a_boxes + 2 * ((t.b_boxes + 1) / 2)) * 8192);
                                 load_operand(dst, map_a, to, a_mn, t.m0 + (int)rank * 128, k, kSegments ? terms.a >> 2 * i & 3 : 0, t.a_boxes - 2 * (int)rank);
-                                load_operand(dst + kOperand, map_b, to, b_mn, t.n0 + b_row + (int)rank * 128, k + b_kb, kSegments ? terms.b >> 2 * i & 3 : 0, t.b_boxes - 2 * (int)rank);
+                                load_operand(dst + kOperand, map_b, to, b_mn, t.n0 + b_row + (int)rank * b_half(t), k + b_kb, kSegments ? terms.b >> 2 * i & 3 : 0, (t.b_boxes + 1) / 2);
                             }
                 }
             }
@@ -225,10 +229,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     const bool a_mn = kWhat == kGrads && t.dw;
                     constexpr bool b_mn = kWhat == kGrads;
                     const int nterms = kSegments ? p.terms.n : 1;
-                    const uint32_t idesc = make_idesc(kTile, kTile, a_mn, b_mn);
+                    const uint32_t idesc = make_idesc(kTile, 64 * t.b_boxes, a_mn, b_mn);
                     // K step of 16: 32 bytes along a K-major row, 16 rows of an MN-major tile (two atoms of 64 columns)
                     const uint32_t a_step = a_mn ? 128 : 2, b_step = b_mn ? 128 : 2;
-                    const int seg = kSegments ? kSegment : t.kb1 - t.kb0;
+                    const int seg = kSegments ? p.segment : t.kb1 - t.kb0;
                     for (int kb = t.kb0; ok && kb < t.kb1; kb += seg, ++gs) {
                         const int buf = gs & 1;
                         ok = mbar_wait(bar_tempty + 8 * buf, ((gs >> 1) & 1) ^ 1, abort_flag, p.wc.limit);
@@ -271,7 +275,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             float run_m = -INFINITY, run_s = 0.f;
             for (int j = 0; ok && j < tiles; ++j) {
                 const Tile t = tile_of(p, kWhat, n, u, j);
-                const int seg = kSegments ? kSegment : max(t.kb1 - t.kb0, 1);
+                const int seg = kSegments ? p.segment : max(t.kb1 - t.kb0, 1);
                 float z[128];
                 if (kWhat == kGrads && t.kb0 == t.kb1) {   // an empty slice
 #pragma unroll
@@ -689,7 +693,10 @@ Plan make_plan(int T, int V, int D, chela_dtype_t in_dtype, chela_dtype_t grad_d
     q.pairs = current_sm_count() / 2;
     q.Tpad = ceil_div(T, kTile) * kTile;
     q.planes_in = in_dtype == CHELA_F32 ? 3 : 1;
-    q.planes_dz = grad_dtype == CHELA_F32 ? 3 : 1;
+    // bf16 gradients: one plane of dz, but two beside fp32 operands, and for up to 64 tokens and 2^25 weights, where the launches
+    // bound the call: sums of few terms keep the whole of dz's rounding (21 tokens: relative error of d_w 0.0028 with one plane,
+    // 0.0017 with two; 42 x 197413 x 1328: 253 us for the gradients with one, 411 with two)
+    q.planes_dz = grad_dtype == CHELA_F32 ? 3 : q.planes_in > 1 || (T <= 64 && (long long)V * D <= 1LL << 25) ? 2 : 1;
     const int nt = ceil_div(V, kTile), mt = q.Tpad / kTile, nd = ceil_div(D, kTile);
     size_t tile_bytes = 0;   // of the piece-wise buffers, by column tile
     if (bwd) tile_bytes = (size_t)q.Tpad * kTile * 2 * q.planes_dz;
@@ -805,6 +812,7 @@ bool set_operands(Product &p, const chela_vocabloss_args_t &a, const Plan &q, ui
     p.h_in_planes = q.planes_in > 1;
     p.c2 = a.scale * kLog2e;
     p.wc = current_wait_ctl();
+    p.segment = kSegment;
     p.per_chunk = q.per_chunk, p.sh = q.sh, p.sv = q.sv, p.planes = q.planes_dz;
     if (!map_3d(&p.hk, ws + q.hk, false, a.D, q.Tpad, q.planes_in, (long long)a.D * 2, (long long)hk_plane, 64, 64)) return false;
     if (q.planes_in > 1) {
@@ -899,13 +907,15 @@ chela_status_t launch_vocabloss_bwd(const chela_vocabloss_args_t &a, const float
         st = set_piece(p, a, q, ws, v0, sms, stream);
         if (st != CHELA_OK) return st;
         p.terms = q.planes_in > 1 ? kTerms6 : kTerms1;
+        p.segment = kSegment;
         st = q.planes_in > 1 ? launch_product<kSlopes, true>(p, q.pairs, stream) : launch_product<kSlopes, false>(p, q.pairs, stream);
         if (st != CHELA_OK) return st;
-        p.terms = q.planes_in > 1 ? (f32 ? kTerms6 : kTerms2) : f32 ? kTerms3 : kTerms1;
+        p.terms = q.planes_in > 1 ? (f32 ? kTerms6 : kTerms3B) : f32 ? kTerms3 : q.planes_dz > 1 ? kTerms2A : kTerms1;
+        p.segment = f32 ? kSegment : kLongSegment;
         p.dh_add = i > 0;
         p.dh_last = q.sh == 1 && i + 1 == q.pieces;
         p.dh_before = i > 0 ? (const float *)(ws + q.dhp) : nullptr;
-        st = f32 || q.planes_in > 1 ? launch_product<kGrads, true>(p, q.pairs, stream) : launch_product<kGrads, false>(p, q.pairs, stream);
+        st = p.terms.n > 1 ? launch_product<kGrads, true>(p, q.pairs, stream) : launch_product<kGrads, false>(p, q.pairs, stream);
         if (st == CHELA_OK && q.sv > 1) {
             const size_t off = (size_t)v0 * a.D;
             const float *part = (const float *)(ws + q.dwp);
