@@ -276,6 +276,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             for (int j = 0; ok && j < tiles; ++j) {
                 const Tile t = tile_of(p, kWhat, n, u, j);
                 const int seg = kSegments ? p.segment : max(t.kb1 - t.kb0, 1);
+                // what the row brings along, asked for before the wait for its products
+                int target = -1;
+                float4 cf = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (kWhat == kStats) target = p.target[t.m0 + row];
+                if (kWhat == kSlopes) cf = p.coef[t.m0 + row];
                 float z[128];
                 if (kWhat == kGrads && t.kb0 == t.kb1) {   // an empty slice
 #pragma unroll
@@ -309,7 +314,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                 if (kWhat != kGrads && row0 >= 64 * t.a_boxes) continue;   // rows of no token, not even loaded
                 const int c0 = t.n0 + half * 128;   // first column of this thread's 128, in the piece
                 if (kWhat == kStats) {
-                    int y = p.target[t.m0 + row] - p.v0 - c0;
+                    int y = target - p.v0 - c0;
                     if (y + c0 >= t.n0 + 64 * t.b_boxes) y = -1;   // a later chunk's
                     const int end = min(t.n0 + 64 * t.b_boxes, p.V - p.v0);
                     if (c0 + 128 > end) {
@@ -334,7 +339,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                         if (y >= 0 && y < 128) p.zt[t.m0 + row] = zy * p.c2;
                     }
                 } else if (kWhat == kSlopes) {
-                    const float4 cf = p.coef[t.m0 + row];
                     const int y = __float_as_int(cf.w) - p.v0 - c0;
                     const bool here = __any_sync(0xffffffffu, y >= 0 && y < 128);
 #pragma unroll
@@ -351,30 +355,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     }
 #pragma unroll
                     for (int c = 0; c < 2; ++c)
-                        for (int plane = 0; plane < p.planes; ++plane) {
-                            uint32_t v[32];
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) {
-                                const __nv_bfloat162 hh = __floats2bfloat162_rn(z[64 * c + 2 * e], z[64 * c + 2 * e + 1]);
-                                v[e] = *reinterpret_cast<const uint32_t *>(&hh);
-                                if (p.planes > 1) {   // what is left for the next plane
-                                    const float2 f = __bfloat1622float2(hh);
-                                    z[64 * c + 2 * e] -= f.x;
-                                    z[64 * c + 2 * e + 1] -= f.y;
-                                }
-                            }
+                        for (int plane = 0;;) {
                             // (every box is a bulk group, stored or not, so that the last but one has left this buffer)
                             const uint32_t buf = (boxes++ & 1) * kBox;
                             if (lane == 0) bulk_wait_read1();
                             __syncwarp();
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4 *>(stg + buf + sw128(lane, e)) = make_uint4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                            for (int e = 0; e < 8; ++e) {
+                                const float *x = &z[64 * c + 8 * e];
+                                *reinterpret_cast<uint4 *>(stg + buf + sw128(lane, e)) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+                            }
                             fence_proxy_async();
                             __syncwarp();
                             if (lane == 0) {
                                 if (c0 + 64 * c < p.vc) tma_store_3d(&p.dz_out, stg_u32 + buf, c0 + 64 * c, t.m0 + row0, plane);
                                 bulk_commit();
                             }
+                            if (++plane == p.planes) break;
+#pragma unroll
+                            for (int e = 0; e < 64; ++e) z[64 * c + e] -= __bfloat162float(__float2bfloat16_rn(z[64 * c + e]));   // what is left for the next plane
                         }
                 } else {
                     // a final gradient, of its type, or a sum in fp32 that goes on
