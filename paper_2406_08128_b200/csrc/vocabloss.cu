@@ -57,7 +57,7 @@ struct Product {
     int *head;
     const int *target;              // [Tpad] of kept rows, -1 behind them
     const float4 *coef;             // [Tpad] {lse log2 e, factor of the softmax, factor of the target, target}
-    float *zt;                      // [Tpad] target's logit log2 e
+    float *zt;                      // [Tpad] target's product with h
     float2 *part;                   // [2 * chunks][Tpad] running maximum (log2 e) and sum of a chunk's column halves
     const void *dw_in;
     const int *row_of;              // [Tpad] tokens of the kept rows
@@ -336,7 +336,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                         float zy = 0.f;
 #pragma unroll
                         for (int c = 0; c < 128; ++c) zy = c == y ? z[c] : zy;
-                        if (y >= 0 && y < 128) p.zt[t.m0 + row] = zy * p.c2;
+                        if (y >= 0 && y < 128) p.zt[t.m0 + row] = zy;
                     }
                 } else if (kWhat == kSlopes) {
                     const int y = __float_as_int(cf.w) - p.v0 - c0;
@@ -597,7 +597,7 @@ __global__ void __launch_bounds__(256) planes_kernel(const float *w, long long w
 // lse = (m + log2 s) ln 2 over a row's parts; the loss from the differences to the largest logit, so that it keeps its digits
 // where the target has nearly all the weight.
 // A CTA's 256 threads are `groups` threads a row, next to one another rows of one part.
-__global__ void __launch_bounds__(256) join_kernel(const int *head, const int *row_of, const float *zt, const float2 *part, int parts, int T, int Tpad, int groups, float *loss, float *lse)
+__global__ void __launch_bounds__(256) join_kernel(const int *head, const int *row_of, const float *zt, const float2 *part, int parts, int T, int Tpad, int groups, float c2, float *loss, float *lse)
 {
     __shared__ float2 s_part[256];
     const int rows = 256 / groups, lane = threadIdx.x % rows, group = threadIdx.x / rows;
@@ -626,7 +626,9 @@ __global__ void __launch_bounds__(256) join_kernel(const int *head, const int *r
         const int t = row_of[i];
         const float log_s = log1pf(sum - 1.f);   // the largest term is 1
         lse[t] = fmaf(mm, kLn2, log_s);
-        loss[t] = fmaf(mm - zt[i], kLn2, log_s);
+        // (the product with c2 unrounded, as in the exponents: where the target has the largest logit, what rounding took from
+        // the maximum is in log_s and cancels)
+        loss[t] = fmaf(fmaf(-zt[i], c2, mm), kLn2, log_s);
     }
 }
 
@@ -780,10 +782,16 @@ chela_status_t launch_after(void (*kernel)(P...), int grid, int threads, int sme
     return cuda_status(cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...));
 }
 
+// Shared memory for a product.  Before the tensor maps: this runtime call also makes the device's context the thread's, which
+// the driver's call that encodes them needs and a new thread does not have yet.
+template <int kWhat, bool kSegments>
+bool prepare_product()
+{
+    return cudaFuncSetAttribute(product_kernel<kWhat, kSegments>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) == cudaSuccess;
+}
 template <int kWhat, bool kSegments>
 chela_status_t launch_product(const Product &p, int pairs, cudaStream_t stream)
 {
-    if (cudaFuncSetAttribute(product_kernel<kWhat, kSegments>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) != cudaSuccess) return CHELA_ERR_CUDA;
     return launch_after(product_kernel<kWhat, kSegments>, 2 * pairs, kThreads, kSmemBytes, stream, p);
 }
 
@@ -853,7 +861,7 @@ chela_status_t launch_vocabloss_fwd(const chela_vocabloss_args_t &a, float *loss
     uint8_t *ws = reinterpret_cast<uint8_t *>(workspace);
     const int sms = 2 * q.pairs;
     Product p{};
-    if (!set_operands(p, a, q, ws)) return CHELA_ERR_CUDA;
+    if (!(q.planes_in > 1 ? prepare_product<kStats, true>() : prepare_product<kStats, false>()) || !set_operands(p, a, q, ws)) return CHELA_ERR_CUDA;
     Rows r{};
     r.targets = a.targets, r.h = a.h, r.h_stride = a.h_stride, r.T = a.T, r.Tpad = q.Tpad, r.V = a.V, r.D = a.D, r.planes = q.planes_in;
     r.head = p.head, r.row_of = (int *)(ws + q.row_of), r.target = (int *)(ws + q.target), r.loss_out = loss, r.lse_out = lse, r.hk = (__nv_bfloat16 *)(ws + q.hk);
@@ -871,7 +879,7 @@ chela_status_t launch_vocabloss_fwd(const chela_vocabloss_args_t &a, float *loss
     }
     if (st != CHELA_OK) return st;
     const int groups = parts <= 2 ? 1 : parts <= 32 ? 8 : 32;   // threads a row, by the parts (two a chunk)
-    return launch_after(join_kernel, q.Tpad / (256 / groups), 256, 0, stream, p.head, r.row_of, p.zt, p.part, 2 * parts, a.T, q.Tpad, groups, loss, lse);
+    return launch_after(join_kernel, q.Tpad / (256 / groups), 256, 0, stream, p.head, r.row_of, p.zt, p.part, 2 * parts, a.T, q.Tpad, groups, p.c2, loss, lse);
 }
 
 chela_status_t launch_vocabloss_bwd(const chela_vocabloss_args_t &a, const float *lse, const float *d_loss, const float *d_lse, void *d_h, const void *d_w_in, void *d_w,
@@ -883,7 +891,10 @@ chela_status_t launch_vocabloss_bwd(const chela_vocabloss_args_t &a, const float
     const int sms = 2 * q.pairs;
     const bool f32 = grad_dtype == CHELA_F32;
     Product p{};
-    if (!set_operands(p, a, q, ws)) return CHELA_ERR_CUDA;
+    const Terms terms = q.planes_in > 1 ? (f32 ? kTerms6 : kTerms3B) : f32 ? kTerms3 : q.planes_dz > 1 ? kTerms2A : kTerms1;   // of the gradients
+    if (!(q.planes_in > 1 ? prepare_product<kSlopes, true>() : prepare_product<kSlopes, false>()) ||
+        !(terms.n > 1 ? prepare_product<kGrads, true>() : prepare_product<kGrads, false>()) || !set_operands(p, a, q, ws))
+        return CHELA_ERR_CUDA;
     const long long dz_row = (long long)q.vc * 2, es = f32 ? 4 : 2;
     const bool sums = q.sh > 1 || q.pieces > 1;   // d_h passes through fp32 sums
     if (!map_3d(&p.dz, ws + q.dz, false, q.vc, q.Tpad, q.planes_dz, dz_row, dz_row * q.Tpad, 64, 64) ||
@@ -909,7 +920,7 @@ chela_status_t launch_vocabloss_bwd(const chela_vocabloss_args_t &a, const float
         p.segment = kSegment;
         st = q.planes_in > 1 ? launch_product<kSlopes, true>(p, q.pairs, stream) : launch_product<kSlopes, false>(p, q.pairs, stream);
         if (st != CHELA_OK) return st;
-        p.terms = q.planes_in > 1 ? (f32 ? kTerms6 : kTerms3B) : f32 ? kTerms3 : q.planes_dz > 1 ? kTerms2A : kTerms1;
+        p.terms = terms;
         p.segment = f32 ? kSegment : kLongSegment;
         p.dh_add = i > 0;
         p.dh_last = q.sh == 1 && i + 1 == q.pieces;

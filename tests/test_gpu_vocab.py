@@ -120,3 +120,333 @@ def test_loss_and_gradients(T, V, D, it, gt, left_out):
     assert (got.d_h[~ref.kept_of(targets, V)] == 0).all()
     again = chela.vocabloss_bwd(h, w, targets, lse, d_loss, d_lse, scale=scale, grad_dtype=CODE[gt])
     assert torch.equal(again.d_h, got.d_h) and torch.equal(again.d_w, got.d_w)
+
+
+@pytest.mark.parametrize("gt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,V,D,it", [(5, 700, 64, "bf16"), (100, 900, 72, "f32"), (300, 4000, 264, "bf16")])
+def test_loss_gradient_on_top_of_another(T, V, D, it, gt):
+    g = gen(T * V)
+    targets = token_ids(g, T, V, 0.1)
+    h, w = hidden(g, T, V, D, DT[it], targets)
+    d_lse = normal(g, T, std=1.0 / T)
+    d_w_in = normal(g, V, D, dtype=DT[gt], std=0.1)
+    r = ref.loss(h, w, targets, 1.3, None, d_lse, d_w_in)   # of lse alone
+    _, lse = chela.vocabloss_fwd(h, w, targets, scale=1.3)
+    bounds = ref.grad_bounds(r, T, V, D, DT[it], DT[gt])
+    other = chela.vocabloss_bwd(h, w, targets, lse, None, d_lse, scale=1.3, grad_dtype=CODE[gt], d_w_in=d_w_in)
+    buf = d_w_in.clone()
+    same = chela.vocabloss_bwd(h, w, targets, lse, None, d_lse, scale=1.3, grad_dtype=CODE[gt], d_w_in=buf, d_w=buf)
+    assert same.d_w is buf and torch.equal(buf, other.d_w) and torch.equal(same.d_h, other.d_h)
+    for name, a, b in zip(("d_h", "d_w"), other, bounds):
+        within(a, r[name], b, name)
+
+
+@pytest.mark.parametrize("T,V,D,gt", [(65536, 4500, 64, "bf16"), (40000, 3000, 40, "f32")])
+def test_loss_of_several_pieces_of_the_vocabulary(T, V, D, gt):
+    """More dz than a piece holds: the pieces' sums of d_h go on top of each other."""
+    g = gen(T)
+    targets = token_ids(g, T, V, 0.05)
+    h, w = hidden(g, T, V, D, torch.bfloat16, targets)
+    d_loss = torch.rand(T, generator=g, device="cuda") / T
+    r = ref.loss(h, w, targets, 1.0, d_loss)
+    loss, lse = chela.vocabloss_fwd(h, w, targets)
+    within(loss, r["loss"], ref.lse_bound(r, D, torch.bfloat16) + ref.z_bound(r, D, torch.bfloat16), "loss")
+    got = chela.vocabloss_bwd(h, w, targets, lse, d_loss, grad_dtype=CODE[gt])
+    for name, a, b in zip(("d_h", "d_w"), got, ref.grad_bounds(r, T, V, D, torch.bfloat16, DT[gt])):
+        within(a, r[name], b, name)
+
+
+def test_fp32_weights_of_several_pieces():
+    """The weights' parts are laid out a piece at a time: 90000 x 2048 take more than one, forward and backward."""
+    T, V, D = 24, 90000, 2048
+    g = gen(3)
+    targets = token_ids(g, T, V)
+    h, w = hidden(g, T, V, D, torch.float32, targets)
+    d_loss = torch.rand(T, generator=g, device="cuda")
+    r = ref.loss(h, w, targets, 1.0, d_loss)
+    loss, lse = chela.vocabloss_fwd(h, w, targets)
+    within(lse, r["lse"], ref.lse_bound(r, D, torch.float32), "lse")
+    got = chela.vocabloss_bwd(h, w, targets, lse, d_loss)
+    for name, a, b in zip(("d_h", "d_w"), got, ref.grad_bounds(r, T, V, D, torch.float32, torch.float32)):
+        within(a, r[name], b, name)
+
+
+@pytest.mark.parametrize("T", [4, 70, 700])
+def test_gradients_against_differences_of_the_definition(T):
+    V, D, eps = 150, 48, 1e-5
+    g = gen(T + 1)
+    targets = token_ids(g, T, V, 0.2)
+    h, w = hidden(g, T, V, D, torch.float32, targets)
+    a, b = torch.rand(T, generator=g, device="cuda"), normal(g, T, std=0.3)
+    _, lse = chela.vocabloss_fwd(h, w, targets, scale=0.9)
+    got = chela.vocabloss_bwd(h, w, targets, lse, a, b, scale=0.9)
+    bounds = ref.grad_bounds(ref.loss(h, w, targets, 0.9, a, b), T, V, D, torch.float32, torch.float32)
+
+    def value(dh, dw):
+        r = ref.loss(h.double() + dh, w.double() + dw, targets, 0.9)
+        return float((a * r["loss"] + b * r["lse"]).sum())
+    for k in range(3):
+        u, v = normal(g, T, D).double(), normal(g, V, D).double()
+        slope = (value(eps * u, eps * v) - value(-eps * u, -eps * v)) / (2 * eps)
+        mine = float((got.d_h.double() * u).sum() + (got.d_w.double() * v).sum())
+        allowed = float((bounds[0] * u.abs()).sum() + (bounds[1] * v.abs()).sum())
+        # the quotient: third derivatives (eps^2 of at most the cube of the directions' logits) and 2^-52 of the values over eps
+        assert abs(slope - mine) <= allowed + 1e-4 * (1 + abs(slope)), (k, slope, mine)
+
+
+def test_slices_batches_and_scalars():
+    """Column slices of wider tensors, tokens by batch and position, ids of any shape, one-dimensional and none."""
+    g = gen(11)
+    B, L, V, D = 3, 50, 333, 72
+    wide_h, wide_w = normal(g, B, L, 200, dtype=torch.bfloat16), normal(g, V, 96, dtype=torch.bfloat16, std=0.1)
+    h, w = wide_h[:, :, 64:64 + D], wide_w[:, 16:16 + D]
+    targets = token_ids(g, B * L, V, 0.1).view(B, L)
+    loss, lse = chela.vocabloss_fwd(h, w, targets)
+    dense = chela.vocabloss_fwd(h.contiguous().view(-1, D), w.contiguous(), targets.view(-1))
+    assert loss.shape == (B, L) and torch.equal(loss.view(-1), dense[0]) and torch.equal(lse.view(-1), dense[1])
+    d_loss = torch.rand(B, L, generator=g, device="cuda")
+    got = chela.vocabloss_bwd(h, w, targets, lse, d_loss)
+    flat = chela.vocabloss_bwd(h.contiguous().view(-1, D), w.contiguous(), targets.view(-1), lse.view(-1), d_loss.view(-1))
+    assert got.d_h.shape == (B, L, D) and torch.equal(got.d_h.view(-1, D), flat.d_h) and torch.equal(got.d_w, flat.d_w)
+    rows = chela.embed_fwd(targets, w, scale=2.0)
+    assert rows.shape == (B, L, D) and torch.equal(rows, chela.embed_fwd(targets.view(2, 3, 25), w.contiguous(), scale=2.0).view(B, L, D))
+    d_w = chela.embed_bwd(targets, h, V)
+    assert torch.equal(d_w, chela.embed_bwd(targets.view(-1), h.contiguous().view(-1, D), V))
+    one = torch.tensor(7, device="cuda")
+    assert torch.equal(chela.embed_fwd(one, w), w[7]) and chela.vocabloss_fwd(h[0, 0].contiguous(), w, one)[0].shape == ()
+    few = chela.vocabloss_fwd(h[0, :5], w, targets[0, :5].contiguous())     # the path for a few tokens, with strides
+    assert torch.allclose(few[0], loss[0, :5], atol=1e-4)
+
+
+def test_tables_beyond_32_bits_of_elements():
+    V, D, T = 2200000, 1032, 40
+    g = gen(5)
+    w = torch.empty(V, D, dtype=torch.bfloat16, device="cuda")
+    for part in w.split(100000):
+        part.copy_(torch.randn(part.shape, generator=g, device="cuda") * 0.03)
+    ids = torch.cat([torch.tensor([V - 1, 0, V, -1, V - 2], device="cuda"), torch.randint(V // 2, V, (T - 5,), generator=g, device="cuda")])
+    out = chela.embed_fwd(ids, w)
+    assert torch.equal(out, torch.where(ref.kept_of(ids, V)[:, None], w[ids.clamp(0, V - 1)], 0))
+    for count in (3, T):
+        h, y = out[:count] + 0.5 * normal(g, count, D, dtype=torch.bfloat16), ids[:count]
+        loss, lse = chela.vocabloss_fwd(h, w, y)
+        z = torch.cat([torch.mm(h.double(), part.double().t()) for part in w.split(100000)], 1)
+        kept = ref.kept_of(y, V)
+        true = torch.where(kept, torch.logsumexp(z, 1), 0.0)
+        m_z = torch.cat([torch.mm(h.double().abs(), part.double().abs().t()).amax(1, keepdim=True) for part in w.split(100000)], 1).amax(1)
+        within(lse, true, ref.lse_bound({"m_z": m_z, "lse": true}, D, torch.bfloat16), "lse")
+        d_loss = torch.ones(count, device="cuda")
+        got = chela.vocabloss_bwd(h, w, y, lse, d_loss, grad_dtype=chela.BF16)
+        dz = torch.exp(z - torch.logsumexp(z, 1, keepdim=True))
+        dz[torch.arange(count, device="cuda"), y.clamp(0, V - 1)] -= 1
+        dz = torch.where(kept[:, None], dz, 0.0)
+        rows = torch.cat([torch.arange(50, device="cuda"), torch.arange(V - 50, V, device="cuda"), ids[:count].clamp(0, V - 1)])
+        true_w = dz[:, rows].t() @ torch.where(kept[:, None], h.double(), 0.0)
+        mag = dz[:, rows].abs().t() @ torch.where(kept[:, None], h.double(), 0.0).abs()
+        rel = float((2 * ref.z_bound({"m_z": m_z}, D, torch.bfloat16)).amax()) + 2.0 ** -19
+        within(got.d_w[rows], true_w, (rel + 2 * 2.0 ** -8) * mag + 2.0 ** -8 * true_w.abs() + 1e-37, "d_w")
+        del got, z, dz
+    d_w = chela.embed_bwd(ids, out, V, grad_dtype=chela.BF16)
+    within(d_w[V - 3:], ref.embed_bwd(torch.where(ids >= V - 3, ids - (V - 3), -1), out, 3, 1.0), 2.0 ** -7 * out.double().abs().amax() * T, "d_w")
+    assert float(d_w[:100].float().abs().sum()) == float(out[ids.eq(0)].float().abs().sum())
+
+
+@pytest.mark.parametrize("T", [6, 300])
+def test_what_is_not_finite_stays_with_its_token(T):
+    V, D = 500, 64
+    g = gen(T)
+    targets = token_ids(g, T, V)
+    h, w = hidden(g, T, V, D, torch.bfloat16, targets)
+    clean = chela.vocabloss_fwd(h, w, targets)
+    h[1, 3], h[2, 5] = float("nan"), float("inf")
+    loss, lse = chela.vocabloss_fwd(h, w, targets)
+    bad = torch.zeros(T, dtype=torch.bool, device="cuda")
+    bad[1:3] = True
+    assert not torch.isfinite(loss[bad]).any() and not torch.isfinite(lse[bad]).any()
+    assert torch.equal(loss[~bad], clean[0][~bad]) and torch.equal(lse[~bad], clean[1][~bad])
+    got = chela.vocabloss_bwd(h, w, targets, lse, torch.ones(T, device="cuda"))
+    assert torch.isfinite(got.d_h[~bad]).all() and torch.isnan(got.d_h[1]).all() and torch.isnan(got.d_w).any(0).all()
+    # left out, they reach nothing
+    targets[1], targets[2] = -1, V
+    got = chela.vocabloss_bwd(h, w, targets, clean[1], torch.full((T,), 1.0, device="cuda"))
+    assert torch.isfinite(got.d_h).all() and torch.isfinite(got.d_w).all() and (got.d_h[bad] == 0).all()
+    d_w = chela.embed_bwd(targets, h, V)
+    assert torch.isfinite(d_w).all()
+
+
+def test_large_logits_and_a_certain_target():
+    """Logits of hundreds, and tokens whose target has all the weight: the loss keeps its digits near zero."""
+    T, V, D = 200, 1000, 64
+    g = gen(2)
+    targets = token_ids(g, T, V, skew=False)
+    w = normal(g, V, D, std=3.0)
+    h = w[targets] * torch.linspace(0.02, 3.0, T, device="cuda")[:, None]
+    r = ref.loss(h, w, targets, 1.0)
+    loss, lse = chela.vocabloss_fwd(h, w, targets)
+    within(lse, r["lse"], ref.lse_bound(r, D, torch.float32), "lse")
+    within(loss, r["loss"], ref.lse_bound(r, D, torch.float32) + ref.z_bound(r, D, torch.float32), "loss")
+    # a certain target's loss is the logarithm of an approximate exponential of next to nothing, off by at most 2^-22, its
+    # rounding and that of the maximum's difference to the target, which is itself
+    certain = r["loss"] < 1e-9
+    assert int(certain.sum()) > T // 2 and float(loss[certain].abs().amax()) <= 2.0 ** -21
+
+
+# ------------------------------------------------------------------------------------------------ streams, graphs, threads
+
+def calls(ids, h, w, d_loss, grads=chela.BF16):
+    V = w.shape[0]
+    loss, lse = chela.vocabloss_fwd(h, w, ids)
+    g = chela.vocabloss_bwd(h, w, ids, lse, d_loss, grad_dtype=grads)
+    x = chela.embed_fwd(ids, w, scale=0.5)
+    d_w = chela.embed_bwd(ids, g.d_h, V, grad_dtype=grads, d_w_in=g.d_w)
+    return loss, lse, g.d_h, g.d_w, x, d_w
+
+
+@pytest.mark.parametrize("T", [3, 40, 900])
+def test_graph_replay_and_side_streams_give_equal_bits(T):
+    V, D = 2500, 136
+    g = gen(T)
+    sets = []
+    for _ in range(2):
+        ids = token_ids(g, T, V, 0.2)
+        h, w = hidden(g, T, V, D, torch.bfloat16, ids)
+        sets.append((ids, h, w, torch.rand(T, generator=g, device="cuda")))
+    eager = [calls(*s) for s in sets]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for s, e in zip(sets, eager):
+            for a, b in zip(calls(*s), e):
+                assert torch.equal(a, b)
+    torch.cuda.current_stream().wait_stream(side)
+    held = tuple(t.clone() for t in sets[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = calls(*held)
+    for s, e in list(zip(sets, eager)) * 2:
+        for t, v in zip(held, s):
+            t.copy_(v)
+        graph.replay()
+        for a, b in zip(out, e):
+            assert torch.equal(a, b)
+
+
+def test_two_streams_at_once():
+    """Calls of different sizes side by side on two streams, each as if it were alone."""
+    g = gen(9)
+    sizes = [(700, 5000, 256), (30, 9000, 512)]
+    data, alone = [], []
+    for T, V, D in sizes:
+        ids = token_ids(g, T, V)
+        h, w = hidden(g, T, V, D, torch.bfloat16, ids)
+        data.append((ids, h, w, torch.rand(T, generator=g, device="cuda")))
+        alone.append(calls(*data[-1]))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sizes]
+    got = [[], []]
+    for _ in range(8):
+        for k, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[k].append(calls(*data[k]))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for out in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(out, alone[k]))
+
+
+def test_threads_on_one_stream():
+    import threading
+    g = gen(13)
+    data, alone = [], []
+    for T, V, D in [(300, 3000, 128), (5, 700, 64), (4000, 200, 72), (64, 20000, 256)]:
+        ids = token_ids(g, T, V)
+        h, w = hidden(g, T, V, D, torch.bfloat16, ids)
+        data.append((ids, h, w, torch.rand(T, generator=g, device="cuda")))
+        alone.append(calls(*data[-1]))
+    torch.cuda.synchronize()
+    right = []
+
+    def work(k):
+        for _ in range(30):
+            out = calls(*data[k])
+            torch.cuda.current_stream().synchronize()
+            if all(torch.equal(a, b) for a, b in zip(out, alone[k])):
+                right.append(k)
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(len(data))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert sorted(right) == sorted(list(range(len(data))) * 30)   # no call refused, none wrong
+
+
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_clean():
+    g = gen(21)
+    T, V, D = 600, 60000, 64   # enough units that the first CTA comes back to the buffer whose hand-back was left out
+    ids = token_ids(g, T, V)
+    h, w = hidden(g, T, V, D, torch.bfloat16, ids)
+    clean = chela.vocabloss_fwd(h, w, ids)
+    ws = torch.zeros(int(chela.lib().chela_vocabloss_workspace_bytes(T, V, D, chela.BF16)), dtype=torch.uint8, device="cuda")
+    try:
+        chela.debug_wait_control(6_000_000, 1)
+        chela.vocabloss_fwd(h, w, ids, workspace=ws)
+        assert chela.async_status(ws) == chela.ERR_TIMEOUT
+    finally:
+        chela.debug_wait_control(0, 0)
+    got = chela.vocabloss_fwd(h, w, ids, workspace=ws)
+    assert chela.async_status(ws) == chela.OK
+    assert torch.equal(got[0], clean[0]) and torch.equal(got[1], clean[1])
+
+
+# ------------------------------------------------------------------------------------------------ together
+
+def test_a_language_model_with_tied_weights_trains_as_its_definition_says():
+    """ids -> embedding -> norm -> short convolution -> residual and norm -> loss against the same table, and back: every gradient
+    against automatic differentiation of the same formulas in 64 bits.  Two packed sequences, padding behind them."""
+    T, pad, V, D, W, scale, eps = 150, 10, 700, 64, 4, 8.0, 1e-6
+    g = gen(31)
+    ids = token_ids(g, T + pad, V)
+    ids[T:] = -100
+    off = torch.tensor([0, 90, T], dtype=torch.int32, device="cuda")
+    targets = torch.full_like(ids, -100)
+    targets[:T - 1] = ids[1:T]
+    targets[89] = -100   # the first sequence's last token has nothing to foretell
+    table, taps = normal(g, V, D, std=D ** -0.5), normal(g, D, W, std=0.5)
+    w_in, w_out = 1 + 0.1 * normal(g, D), 1 + 0.1 * normal(g, D)
+    weight = torch.where(ref.kept_of(targets, V), 1.0, 0.0) / float(ref.kept_of(targets, V).sum())
+
+    x = chela.embed_fwd(ids, table, scale=scale)
+    _, o = chela.blocknorm_fwd(x, w_pre=w_in, eps=eps)
+    y, _ = chela.shortconv_carry_fwd(o, taps, seq_offsets=off)
+    res, top = chela.blocknorm_fwd(x, y=y, norm_post=chela.NORM_NONE, w_pre=w_out, eps=eps)
+    loss, lse = chela.vocabloss_fwd(top, table, targets)
+    gl = chela.vocabloss_bwd(top, table, targets, lse, weight)
+    gt = chela.blocknorm_bwd(res, y=y, d_o=gl.d_h, norm_post=chela.NORM_NONE, w_pre=w_out, eps=eps)
+    gc = chela.shortconv_bwd(o, taps, gt.d_y, seq_offsets=off)
+    gi = chela.blocknorm_bwd(x, d_o=gc.d_x, d_res_out=gt.d_res, w_pre=w_in, eps=eps)
+    d_table = chela.embed_bwd(ids, gi.d_res, V, scale=scale, d_w_in=gl.d_w, d_w=gl.d_w)
+    assert d_table is gl.d_w
+
+    leaves = [t.double().requires_grad_() for t in (table, taps, w_in, w_out)]
+    tab, tap, wi, wo = leaves
+
+    def norm(v, weights):
+        return v * torch.rsqrt((v * v).mean(-1, keepdim=True) + eps) * weights
+    kept = ref.kept_of(ids, V)
+    e = torch.where(kept[:, None], scale * tab[torch.where(kept, ids, 0)], 0.0)
+    n = norm(e, wi)
+    parts = []
+    for a, b in ((0, 90), (90, T)):
+        padded = torch.cat([torch.zeros(W - 1, D, dtype=torch.float64, device="cuda"), n[a:b]])
+        u = sum(tap[:, j] * padded[W - 1 - j:W - 1 - j + b - a] for j in range(W))
+        parts.append(u * torch.sigmoid(u))
+    parts.append(torch.zeros(pad, D, dtype=torch.float64, device="cuda"))
+    z = norm(e + torch.cat(parts), wo) @ tab.t()
+    rows = torch.where(ref.kept_of(targets, V), torch.logsumexp(z, 1) - z.gather(1, targets.clamp(0)[:, None])[:, 0], 0.0)
+    total = (rows * weight.double()).sum()
+    total.backward()
+    assert abs(float((loss * weight).sum()) - total.item()) <= 1e-5 * total.item()
+    # fp32 throughout: each of some ten stages adds up at most a few hundred roundings of 2^-24 of its majorant
+    for name, got, leaf in zip(("table", "taps", "w_in", "w_out"), (d_table, gc.d_w, gi.d_w_pre, gt.d_w_pre), leaves):
+        far = float((got.double() - leaf.grad).norm() / leaf.grad.norm())
+        assert far <= 2e-5, (name, far)
