@@ -1,7 +1,5 @@
 // C ABI entry points of the token embedding and the vocabulary's cross entropy: argument validation and dispatch.  No kernel
 // code here.
-#include <math.h>
-
 #include <atomic>
 
 #include "common.cuh"
@@ -14,6 +12,8 @@ constexpr int kMaxTokens = 0x7fffffff - 4095;
 constexpr long long kMaxStride = 1LL << 36;   // a row's distance in elements: within a tensor map's strides
 constexpr int kMaxRows = 1 << 30, kMaxCols = 1 << 20;
 
+constexpr float kMaxScale = 1e30f;            // its product with log2 e stays finite
+
 bool dtype_ok(chela_dtype_t t) { return t == CHELA_F32 || t == CHELA_BF16; }
 bool stride_ok(long long stride, long long n) { return stride >= n && stride % 8 == 0 && stride <= kMaxStride; }
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }   // arrays of one value a token
@@ -25,6 +25,9 @@ chela_status_t check_sizes(int T, int V, int D)
     if (T < 1 || V < 1 || D < 1) return CHELA_ERR_INVALID_ARG;
     return T <= kMaxTokens && V <= kMaxRows && D <= kMaxCols && D % 8 == 0 ? CHELA_OK : CHELA_ERR_UNSUPPORTED;
 }
+
+// the tiles of the logits, 256 tokens by 64 words, are counted in 32 bits
+bool loss_sizes_ok(int T, int V) { return (T / 256 + 1LL) * (V / 64 + 1LL) <= 0x7fffffff; }
 
 template <size_t A, size_t B>
 bool distinct(const void *const (&outs)[A], const void *const (&operands)[B])
@@ -40,10 +43,12 @@ chela_status_t check_loss(const chela_vocabloss_args_t *a)
     if (!a || !a->h || !a->w || !ids_ok(a->targets, a->wide_ids) || !dtype_ok(a->in_dtype) || !aligned16(a->h) || !aligned16(a->w)) return CHELA_ERR_INVALID_ARG;
     const chela_status_t st = check_sizes(a->T, a->V, a->D);
     if (st != CHELA_OK) return st;
-    return stride_ok(a->h_stride, a->D) && stride_ok(a->w_stride, a->D) && a->scale > 0.f && isfinite(a->scale) ? CHELA_OK : CHELA_ERR_INVALID_ARG;
+    if (!loss_sizes_ok(a->T, a->V)) return CHELA_ERR_UNSUPPORTED;
+    return stride_ok(a->h_stride, a->D) && stride_ok(a->w_stride, a->D) && a->scale > 0.f && a->scale <= kMaxScale ? CHELA_OK : CHELA_ERR_INVALID_ARG;
 }
 
 bool query_ok(int T, int V, int D) { return check_sizes(T, V, D) == CHELA_OK; }
+bool loss_query_ok(int T, int V, int D) { return query_ok(T, V, D) && loss_sizes_ok(T, V); }
 
 }  // namespace
 
@@ -91,7 +96,7 @@ chela_status_t chela_embed_bwd(const void *ids, int wide_ids, const void *d_out,
 
 size_t chela_vocabloss_workspace_bytes(int T, int V, int D, chela_dtype_t in_dtype)
 {
-    return query_ok(T, V, D) && dtype_ok(in_dtype) ? vocabloss_workspace_bytes(T, V, D, in_dtype) : 0;
+    return loss_query_ok(T, V, D) && dtype_ok(in_dtype) ? vocabloss_workspace_bytes(T, V, D, in_dtype) : 0;
 }
 
 chela_status_t chela_vocabloss_fwd(const chela_vocabloss_args_t *args, float *loss, float *lse, void *workspace, size_t workspace_bytes, cudaStream_t stream)
@@ -107,7 +112,7 @@ chela_status_t chela_vocabloss_fwd(const chela_vocabloss_args_t *args, float *lo
 
 size_t chela_vocabloss_bwd_workspace_bytes(int T, int V, int D, chela_dtype_t in_dtype, chela_dtype_t grad_dtype)
 {
-    return query_ok(T, V, D) && dtype_ok(in_dtype) && dtype_ok(grad_dtype) ? vocabloss_bwd_workspace_bytes(T, V, D, in_dtype, grad_dtype) : 0;
+    return loss_query_ok(T, V, D) && dtype_ok(in_dtype) && dtype_ok(grad_dtype) ? vocabloss_bwd_workspace_bytes(T, V, D, in_dtype, grad_dtype) : 0;
 }
 
 chela_status_t chela_vocabloss_bwd(const chela_vocabloss_args_t *args, const float *lse, const float *d_loss, const float *d_lse, void *d_h, const void *d_w_in, void *d_w,

@@ -465,20 +465,44 @@ __device__ __forceinline__ void split3(float x, __nv_bfloat16 (&o)[3])
     o[2] = __float2bfloat16_rn(r - __bfloat162float(o[1]));
 }
 // Eight elements of a row: bf16 as they are, fp32 in three planes `plane` elements apart.
-__device__ __forceinline__ void copy8(const __nv_bfloat16 *src, __nv_bfloat16 *dst, size_t) { *reinterpret_cast<uint4 *>(dst) = *reinterpret_cast<const uint4 *>(src); }
-__device__ __forceinline__ void copy8(const float *src, __nv_bfloat16 *dst, size_t plane)
-{
-    const float4 a = load4(src), b = load4(src + 4);
-    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    __nv_bfloat16 o[3][8];
+struct Eight16 {
+    uint4 u;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *src) { u = *reinterpret_cast<const uint4 *>(src); }
+    __device__ __forceinline__ void store(__nv_bfloat16 *dst, size_t) const { *reinterpret_cast<uint4 *>(dst) = u; }
+};
+struct Eight32 {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float *src) { a = load4(src), b = load4(src + 4); }
+    __device__ __forceinline__ void store(__nv_bfloat16 *dst, size_t plane) const
+    {
+        const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        __align__(16) __nv_bfloat16 o[3][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        __nv_bfloat16 t[3];
-        split3(x[e], t);
-        o[0][e] = t[0], o[1][e] = t[1], o[2][e] = t[2];
+        for (int e = 0; e < 8; ++e) {
+            __nv_bfloat16 t[3];
+            split3(x[e], t);
+            o[0][e] = t[0], o[1][e] = t[1], o[2][e] = t[2];
+        }
+#pragma unroll
+        for (int i = 0; i < 3; ++i) *reinterpret_cast<uint4 *>(dst + i * plane) = *reinterpret_cast<const uint4 *>(o[i]);
     }
+};
+__device__ __forceinline__ Eight16 eight(const __nv_bfloat16 *) { return Eight16(); }
+__device__ __forceinline__ Eight32 eight(const float *) { return Eight32(); }
+
+// A row by a warp, four vectors a lane at once.
+template <typename TH>
+__device__ __forceinline__ void copy_row(const TH *src, __nv_bfloat16 *dst, size_t plane, int D, int lane)
+{
+    for (int c = lane * 8; c < D; c += 1024) {
+        decltype(eight(src)) x[4];
 #pragma unroll
-    for (int i = 0; i < 3; ++i) *reinterpret_cast<uint4 *>(dst + i * plane) = *reinterpret_cast<const uint4 *>(o[i]);
+        for (int k = 0; k < 4; ++k)
+            if (c + 256 * k < D) x[k].load(src + c + 256 * k);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (c + 256 * k < D) x[k].store(dst + c + 256 * k, plane);
+    }
 }
 
 struct Rows {
@@ -509,13 +533,23 @@ __global__ void __launch_bounds__(kRowsThreads) rows_kernel(const Rows r)
     const long long begin = (long long)blockIdx.x * r.per_cta, end = min(begin + r.per_cta, (long long)r.T);
     int before = 0, total = 0;
     griddep_launch_dependents();
-#pragma unroll 8
-    for (long long t = tid; t < r.T; t += kRowsThreads) {
-        const Idx y = targets[t];
+    const auto count = [&](long long t, Idx y) {
         const int kept = y >= 0 && y < (Idx)r.V;
         total += kept;
         before += kept && t < begin;
+    };
+    // 16 bytes at a time between the ends that are not aligned to them
+    constexpr int kVec = 16 / sizeof(Idx);
+    const long long head = min((long long)r.T, (long long)((16 - ((uintptr_t)targets & 15)) % 16 / sizeof(Idx))), vecs = (r.T - head) / kVec;
+#pragma unroll 4
+    for (long long i = tid; i < vecs; i += kRowsThreads) {
+        const uint4 u = *reinterpret_cast<const uint4 *>(targets + head + i * kVec);
+        const Idx *y = reinterpret_cast<const Idx *>(&u);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) count(head + i * kVec + e, y[e]);
     }
+    if (tid < head) count(tid, targets[tid]);
+    for (long long t = head + vecs * kVec + tid; t < r.T; t += kRowsThreads) count(t, targets[t]);
     for (int o = 16; o; o >>= 1) {
         before += __shfl_xor_sync(0xffffffffu, before, o);
         total += __shfl_xor_sync(0xffffffffu, total, o);
@@ -564,7 +598,7 @@ __global__ void __launch_bounds__(kRowsThreads) rows_kernel(const Rows r)
                     continue;
                 }
                 if (!copy) continue;
-                for (int c = lane * 8; c < r.D; c += 256) copy8(h + (size_t)(t0 + i) * r.h_stride + c, r.hk + (size_t)at * r.D + c, plane);
+                copy_row(h + (size_t)(t0 + i) * r.h_stride, r.hk + (size_t)at * r.D, plane, r.D, lane);
             }
         __syncthreads();
     }
@@ -588,8 +622,11 @@ __global__ void __launch_bounds__(256) planes_kernel(const float *w, long long w
     for (long long i = blockIdx.x * 256LL + threadIdx.x; i < items; i += gridDim.x * 256LL) {
         const int v = (int)(i / per_row), c = (int)(i % per_row) * 8;
         __nv_bfloat16 *dst = out + (size_t)v * D + c;
-        if (v0 + v < V) copy8(w + (size_t)(v0 + v) * w_stride + c, dst, (size_t)vc * D);
-        else
+        if (v0 + v < V) {
+            Eight32 x;
+            x.load(w + (size_t)(v0 + v) * w_stride + c);
+            x.store(dst, (size_t)vc * D);
+        } else
             for (int pl = 0; pl < 3; ++pl) *reinterpret_cast<uint4 *>(dst + (size_t)pl * vc * D) = make_uint4(0u, 0u, 0u, 0u);
     }
 }

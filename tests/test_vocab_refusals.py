@@ -63,6 +63,7 @@ def test_loss_refusals(lib):
             assert call(scale=scale) == bad
         assert call(D=60) == call(T=2 ** 31 - 4000) == call(V=2 ** 30 + 1) == no
         assert call(ws=null) == call(n=64) == small
+        assert call(T=2 ** 31 - 4097, V=2 ** 24) == no and call(scale=2e30) == bad
         for T in (3, 20):   # both paths
             assert call(T=T, n=64) == call(T=T, in_dtype=0, n=64) == small
     assert fwd(loss=null) == fwd(lse=null) == fwd(lse=four) == fwd(loss=one) == fwd(lse=two) == fwd(loss=ctypes.c_void_p(1025)) == fwd(ws=odd) == fwd(ws=four) == fwd(ws=one) == bad
@@ -73,6 +74,7 @@ def test_loss_refusals(lib):
     qf, qb = lib.chela_vocabloss_workspace_bytes, lib.chela_vocabloss_bwd_workspace_bytes
     assert qf(0, 10, 64, 1) == qf(4, 10, 60, 1) == qf(4, 10, 64, 2) == qb(4, 10, 64, 1, 2) == qb(4, 0, 64, 1, 1) == 0
     assert 0 < qf(20, 10, 64, 1) < qf(20, 10, 64, 0) and 0 < qb(300, 10, 64, 1, 1) < qb(300, 10, 64, 1, 0)
+    assert qf(2 ** 31 - 4097, 2 ** 24, 64, 1) == 0 < qf(2 ** 31 - 4097, 2 ** 12, 64, 1)
     # dz of a piece is bounded, however large the vocabulary
     assert qb(16384, 2 ** 20, 1024, 1, 1) < 2 << 30
 
