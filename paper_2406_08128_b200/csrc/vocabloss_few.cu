@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(kThreads, two_ctas(kTokens, kQuads, kGrad) ? 2
         if (kGrad) {
             __syncthreads();
             if (set < sets)
-#pragma unroll 1
+#pragma unroll 2
                 for (int r = set; r < rows && (long long)i * rows + r < p.V; r += sets) {
                     const long long v = (long long)i * rows + r;
 #pragma unroll
