@@ -26,19 +26,25 @@ namespace {
 using namespace sm100;
 
 constexpr int kTile = 256;              // rows and columns of a tile: 128 rows of A and 128 columns of B in each CTA's memory
-constexpr int kStages = 5, kOperand = 128 * 128, kStageBytes = 2 * kOperand;
+constexpr int kOperand = 128 * 128, kStageBytes = 2 * kOperand;
 constexpr int kEpilogueWarps = 8, kThreads = 64 + 32 * kEpilogueWarps;
 constexpr int kBox = 32 * 128, kStagingWarp = 2 * kBox;   // two boxes of 32 rows x 128 bytes: one is filled while the other is stored
 constexpr int kSegment = 4, kLongSegment = 16;   // K blocks of 64 that the tensor cores add up: fp32 gradients and logits; bf16 ones
-constexpr int offStaging = kStages * kStageBytes, offBar = offStaging + kEpilogueWarps * kStagingWarp;
-constexpr int offTmem = offBar + 8 * (2 * kStages + 4), offAbort = offTmem + 8, kSmemBytes = offAbort + 8;
-static_assert(kSmemBytes <= 232448, "shared memory per CTA");
-static_assert(kBox % 1024 == 0 && offStaging % 1024 == 0, "swizzled boxes start on 1024 bytes");
+enum What { kStats, kSlopes, kGrads };
+
+// The ring of operands, and what the epilogue stages; kStats stages nothing and has the room for two stages more (48 tokens
+// against 50000 x 1024, bound by the weights that are on their way: the call 34.7 us with five, 33.7 with seven).
+template <bool kStaging>
+struct Layout {
+    static constexpr int stages = kStaging ? 5 : 7, staging = stages * kStageBytes, bar = staging + (kStaging ? kEpilogueWarps * kStagingWarp : 0);
+    static constexpr int tmem = bar + 8 * (2 * stages + 4), abort = tmem + 8, bytes = abort + 8;
+    static_assert(bytes <= 232448, "shared memory per CTA");
+};
+static_assert(kBox % 1024 == 0 && kStageBytes % 1024 == 0, "swizzled boxes start on 1024 bytes");
 
 constexpr size_t kHead = 256;           // workspace header: word 0 the asynchronous status, word 1 the number of kept rows
 constexpr float kLn2 = 0.6931471805599453f;
 
-enum What { kStats, kSlopes, kGrads };
 
 // Planes of A and B of the partial products of one product, small ones first, two bits each.
 struct Terms {
@@ -147,13 +153,15 @@ template <int kWhat, bool kSegments>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ Product p)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
+    using Smem = Layout<kWhat != kStats>;
+    constexpr int kStages = Smem::stages;
     const uint32_t sbase = smem_u32(smem);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint32_t rank = cluster_rank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const uint32_t bar_full = sbase + offBar, bar_empty = bar_full + 8 * kStages, bar_tfull = bar_empty + 8 * kStages, bar_tempty = bar_tfull + 16;
-    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + offTmem);
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + offAbort);
+    const uint32_t bar_full = sbase + Smem::bar, bar_empty = bar_full + 8 * kStages, bar_tfull = bar_empty + 8 * kStages, bar_tempty = bar_tfull + 16;
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + Smem::tmem);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + Smem::abort);
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
             mbar_init(bar_full + 8 * s, 1);
@@ -167,7 +175,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         fence_barrier_init();
     }
     if (warp == 1) {
-        tmem_alloc_pair(sbase + offTmem, 512);
+        tmem_alloc_pair(sbase + Smem::tmem, 512);
         tmem_relinquish_pair();
     }
     tc_fence_before();
@@ -266,8 +274,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         const int row = (int)rank * 128 + quarter * 32 + lane, row0 = (int)rank * 128 + quarter * 32;
         const uint32_t t_at = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
-        uint8_t *stg = smem + offStaging + (warp - 2) * kStagingWarp;
-        const uint32_t stg_u32 = sbase + offStaging + (warp - 2) * kStagingWarp;
+        uint8_t *stg = smem + Smem::staging + (warp - 2) * kStagingWarp;
+        const uint32_t stg_u32 = sbase + Smem::staging + (warp - 2) * kStagingWarp;
         const uint32_t leader_tempty = map_to_rank(bar_tempty, 0);
         int gs = 0, boxes = 0;
         for (int u = pair; ok && u < units; u += pairs) {
@@ -824,12 +832,12 @@ chela_status_t launch_after(void (*kernel)(P...), int grid, int threads, int sme
 template <int kWhat, bool kSegments>
 bool prepare_product()
 {
-    return cudaFuncSetAttribute(product_kernel<kWhat, kSegments>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes) == cudaSuccess;
+    return cudaFuncSetAttribute(product_kernel<kWhat, kSegments>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<kWhat != kStats>::bytes) == cudaSuccess;
 }
 template <int kWhat, bool kSegments>
 chela_status_t launch_product(const Product &p, int pairs, cudaStream_t stream)
 {
-    return launch_after(product_kernel<kWhat, kSegments>, 2 * pairs, kThreads, kSmemBytes, stream, p);
+    return launch_after(product_kernel<kWhat, kSegments>, 2 * pairs, kThreads, Layout<kWhat != kStats>::bytes, stream, p);
 }
 
 chela_status_t launch_rows(Rows &r, chela_dtype_t in_dtype, bool wide_ids, int sms, cudaStream_t stream)
