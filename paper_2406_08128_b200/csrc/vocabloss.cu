@@ -45,7 +45,6 @@ static_assert(kBox % 1024 == 0 && kStageBytes % 1024 == 0, "swizzled boxes start
 constexpr size_t kHead = 256;           // workspace header: word 0 the asynchronous status, word 1 the number of kept rows
 constexpr float kLn2 = 0.6931471805599453f;
 
-
 // Planes of A and B of the partial products of one product, small ones first, two bits each.
 struct Terms {
     int n;
@@ -785,8 +784,8 @@ Plan make_plan(int T, int V, int D, chela_dtype_t in_dtype, chela_dtype_t grad_d
     } else {
         // slices of the gradients' sums: the cheapest launch by grad_rounds, with as few slices as it takes
         long long best = -1;
-        for (int sv = 1; sv <= 64; sv *= 2)
-            for (int sh = 1; sh <= 64; sh *= 2) {
+        for (int sv = 1; sv == 1 || (sv <= 64 && sv <= T / 64); sv *= 2)
+            for (int sh = 1; sh == 1 || (sh <= 64 && sh <= q.vc / 64); sh *= 2) {
                 if (sv > 1 && (size_t)sv * q.vc * D * 4 > kSliceBytes) continue;
                 if (sh > 1 && (size_t)sh * q.Tpad * D * 4 > kSliceBytes) continue;
                 const long long kdw = ceil_div(ceil_div(T, 64), sv), kdh = ceil_div(q.vc / 64, sh);

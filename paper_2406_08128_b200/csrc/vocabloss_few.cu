@@ -1,13 +1,15 @@
-// The vocabulary's cross entropy and its gradients for a few tokens (fp32 up to 16, bf16 up to 8): the weights are read once in each pass, on the
-// plain fp32 pipes.  A tile of 256 rows of tensor-core operands would be nearly empty; the backward pass needs the logits of a weight row, its own gradient and its share of d_h
-// while the row is in shared memory, where the tensor-core path reads the weights twice and passes dz through memory.  fp32
-// operands keep all their bits without being split.
+// The vocabulary's cross entropy and its gradients for a few tokens (up to 16; bf16 while the weights are few): the weights are
+// read once in each pass, on the plain fp32 pipes.  A tile of 256 rows of tensor-core operands would be nearly empty; the
+// backward pass needs the logits of a weight row, its own gradient and its share of d_h while the row is in shared memory, where
+// the tensor-core path reads the weights twice and passes dz through memory.  fp32 operands keep all their bits without being
+// split.
 //
 // A persistent CTA walks tiles of weight rows, copied two tiles ahead by bulk copies.  Few rows are bound by the instructions that
-// they take, so the sums are two-wide (one instruction a pair of columns).  A warp takes 32 / kTokens rows and a share of the columns:
-// 32 sums a lane, transposed and added over the lanes in 31 exchanges, after which lane i has the logit of row i / kTokens
-// and token i % kTokens.  Backward, a thread then owns columns: with the tokens' values of its columns in registers it writes
-// the rows' gradients and keeps its share of d_h.
+// they take, so the sums are two-wide (one instruction a pair of columns).  A warp takes 32 / kTokens rows and a share of the
+// columns: 32 sums a lane, transposed and added over the lanes in 31 exchanges, after which lane i has the logit of row
+// i / kTokens and token i % kTokens.  Backward, a thread then owns columns: with the tokens' values of its columns in registers
+// it writes the rows' gradients and keeps its share of d_h.  (6 x 91800 x 352 fp32: 35 us forward, 88 backward, where the weights
+// take 20 once and their gradients as long again; 467 us for both on the tensor cores.)
 #include "packed.cuh"
 #include "sm100_ptx.cuh"
 #include "vocabloss.cuh"
@@ -251,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, two_ctas(kTokens, kQuads, kGrad) ? 2
 #pragma unroll
             for (int t = 0; t < kTokens; ++t) {
                 const int c = (quad + j * kThreads) * 4;
-                if (c < D) store4(p.dhp + ((size_t)blockIdx.x * kTokens + t) * D + c, make_float4(acc_lo[j][t].x, acc_lo[j][t].y, acc_hi[j][t].x, acc_hi[j][t].y));
+                if (c < D && set < sets) store4(p.dhp + ((size_t)blockIdx.x * kTokens + t) * D + c, make_float4(acc_lo[j][t].x, acc_lo[j][t].y, acc_hi[j][t].x, acc_hi[j][t].y));
             }
     } else {
         // the sets' shares in order, through the tokens' place in shared memory
@@ -331,10 +333,10 @@ struct Plan {
 
 bool make_plan(Plan &q, int T, int V, int D, chela_dtype_t in_dtype, bool grad)
 {
-    // fp32: 91800 x 352, forward and backward, 14 tokens 228 us here and 20 tokens 443 us on the tensor cores.  bf16: the tensor
-    // cores' path takes 60 us and 1.5 us for a million weights, this one 15 us and 2.7 (up to 8 tokens) or 1.9 (up to 4).
-    const long long weights = (long long)V * D;
-    if (T > (in_dtype == CHELA_F32 ? 16 : 8) || (in_dtype != CHELA_F32 && weights > (T > 4 ? 32LL << 20 : 128LL << 20))) return false;
+    // fp32: 91800 x 352, forward and backward, 14 tokens 226 us here and 20 tokens 443 us on the tensor cores.  bf16: the tensor
+    // cores' path takes 60 us and 1.5 us for a million weights, this one 15 us and 1.9 (up to 4 tokens), 2.7 (8) or 7 (16).
+    const long long weights = (long long)V * D, most = T <= 4 ? 128LL << 20 : T <= 8 ? 32LL << 20 : 4LL << 20;
+    if (T > 16 || (in_dtype != CHELA_F32 && weights > most)) return false;
     q.tokens = T <= 4 ? 4 : T <= 8 ? 8 : 16;
     q.quads = D <= 1024 ? 1 : D <= 2048 ? 2 : 4;
     if (D > 4096 || q.quads * q.tokens > 16) return false;   // 64 registers of sums and 64 of tokens a thread

@@ -87,10 +87,12 @@ def hidden(g, T, V, D, dtype, targets, lean=4.0):
 
 
 LOSSES = [
-    # a few tokens: their own kernels, by 4, 8 and (fp32) 16, up to 1024, 2048 and 4096 channels
+    # a few tokens: their own kernels, by 4, 8 and 16, up to 1024, 2048 and 4096 channels
     (3, 5, 8, "bf16", "f32", 0.3), (4, 3000, 1024, "f32", "f32", 0), (4, 700, 2056, "bf16", "bf16", 0), (4, 50, 4096, "bf16", "f32", 0.5), (8, 9999, 264, "bf16", "bf16", 0),
     (8, 4001, 2048, "bf16", "bf16", 0.2), (7, 333, 1032, "f32", "bf16", 0), (16, 2500, 344, "f32", "f32", 0.1), (16, 1, 16, "f32", "f32", 0), (9, 130, 1024, "f32", "f32", 0),
-    (1, 40000, 72, "bf16", "bf16", 0), (5, 600, 520, "f32", "f32", 1.0), (8, 20, 4104, "bf16", "f32", 0), (16, 700, 2048, "f32", "f32", 0), (16, 700, 256, "bf16", "bf16", 0),
+    (1, 40000, 72, "bf16", "bf16", 0), (5, 600, 520, "f32", "f32", 1.0), (8, 20, 4104, "bf16", "f32", 0), (16, 700, 2048, "f32", "f32", 0), (16, 700, 256, "bf16", "bf16", 0), (13, 519, 232, "bf16", "bf16", 0.1), (16, 8200, 512, "bf16", "bf16", 0),
+    (4, 2001, 544, "bf16", "bf16", 0.1), (8, 900, 776, "f32", "f32", 0), (16, 400, 1000, "f32", "bf16", 0), (2, 800, 516 + 4, "bf16", "f32", 0),
+    (3, 500, 2000, "f32", "f32", 0), (4, 300, 3000, "bf16", "f32", 0), (7, 640, 1536, "bf16", "f32", 0), (6, 77, 40, "f32", "f32", 0),
     # T, V, D, operands, gradients, left out
     (1, 1, 8, "bf16", "bf16", 0), (1, 2, 8, "f32", "f32", 0), (2, 300, 64, "bf16", "f32", 0), (48, 5000, 1024, "bf16", "bf16", 0),
     (127, 255, 72, "bf16", "bf16", 0.3), (128, 256, 128, "f32", "f32", 0.2), (129, 257, 136, "bf16", "f32", 0), (255, 511, 264, "f32", "bf16", 0.5),
