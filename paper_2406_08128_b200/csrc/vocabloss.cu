@@ -27,23 +27,16 @@ using namespace sm100;
 
 constexpr int kTile = 256;              // rows and columns of a tile: 128 rows of A and 128 columns of B in each CTA's memory
 constexpr int kOperand = 128 * 128, kStageBytes = 2 * kOperand;
-constexpr int kEpilogueWarps = 8;       // of a tile: 32 rows x 128 columns each
-constexpr int kBox = 32 * 128;          // a box of 32 rows x 128 bytes
+constexpr int kEpilogueWarps = 8, kThreads = 64 + 32 * kEpilogueWarps;
+constexpr int kBox = 32 * 128, kStagingWarp = 2 * kBox;   // two boxes of 32 rows x 128 bytes: one is filled while the other is stored
 constexpr int kSegment = 4, kLongSegment = 16;   // K blocks of 64 that the tensor cores add up: fp32 gradients and logits; bf16 ones
 enum What { kStats, kSlopes, kGrads };
-
-// Tiles whose epilogues run side by side, each by its own eight warps on its own TMEM buffer: two for dz of single products, whose
-// epilogue is the longest (16384 x 12544 x 1024: 314 -> 307 us, 42 x 197413 x 256: 36 -> 32), one elsewhere: the gradients' warps
-// then have two boxes each to fill, and sums of several segments take the registers.
-__host__ __device__ constexpr int groups_of(int what, bool segments) { return what == kSlopes && !segments ? 2 : 1; }
-__host__ __device__ constexpr int threads_of(int what, bool segments) { return 64 + 32 * kEpilogueWarps * groups_of(what, segments); }
-constexpr int kStagingBytes = 2 * kEpilogueWarps * kBox;   // two boxes a warp, or one a warp of two groups
 
 // The ring of operands, and what the epilogue stages; kStats stages nothing and has the room for two stages more (48 tokens
 // against 50000 x 1024, bound by the weights that are on their way: the call 34.7 us with five, 33.7 with seven).
 template <bool kStaging>
 struct Layout {
-    static constexpr int stages = kStaging ? 5 : 7, staging = stages * kStageBytes, bar = staging + (kStaging ? kStagingBytes : 0);
+    static constexpr int stages = kStaging ? 5 : 7, staging = stages * kStageBytes, bar = staging + (kStaging ? kEpilogueWarps * kStagingWarp : 0);
     static constexpr int tmem = bar + 8 * (2 * stages + 4), abort = tmem + 8, bytes = abort + 8;
     static_assert(bytes <= 232448, "shared memory per CTA");
 };
@@ -154,9 +147,9 @@ __device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap *ma
 }
 
 // Two CTAs a tile of 256 x 256, persistent.  Warp 0: TMA producer of its CTA's halves; warp 1 of the even CTA: issuer;
-// warps 2 and up: epilogue, each 32 rows x 128 columns.  Accumulators double-buffered in TMEM (2 x 256 columns).
+// warps 2-9: epilogue, each 32 rows x 128 columns.  Accumulators double-buffered in TMEM (2 x 256 columns).
 template <int kWhat, bool kSegments>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kWhat, kSegments), 1) product_kernel(const __grid_constant__ Product p)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ Product p)
 {
     extern __shared__ __align__(1024) uint8_t smem[];
     using Smem = Layout<kWhat != kStats>;
@@ -276,221 +269,181 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(threads_of(kWhat, kS
         }
     } else {
         // ------------------------------------------------------------------ epilogue
-        // TMEM lanes are a warp's by its number modulo 4; of a group's two warps of a lane quarter each takes half the columns
-        constexpr int kGroups = groups_of(kWhat, kSegments), kChunk = kGroups > 1 ? 64 : 128;   // columns in registers at a time
-        constexpr int kBoxes = kStagingBytes / (kGroups * kEpilogueWarps * kBox);
-        const int quarter = warp & 3, half = ((warp - 2) >> 2) & 1, group = (warp - 2) / kEpilogueWarps;
+        // TMEM lanes are a warp's by its number modulo 4; of the two warps of a lane quarter each takes half the columns
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
         const int row = (int)rank * 128 + quarter * 32 + lane, row0 = (int)rank * 128 + quarter * 32;
         const uint32_t t_at = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
-        uint8_t *stg = smem + Smem::staging + (warp - 2) * kBoxes * kBox;
-        const uint32_t stg_u32 = sbase + Smem::staging + (warp - 2) * kBoxes * kBox;
+        uint8_t *stg = smem + Smem::staging + (warp - 2) * kStagingWarp;
+        const uint32_t stg_u32 = sbase + Smem::staging + (warp - 2) * kStagingWarp;
         const uint32_t leader_tempty = map_to_rank(bar_tempty, 0);
         int gs = 0, boxes = 0;
-        // The next box to fill.  Every box is a bulk group, stored or not, so that with two the last but one has been read.
-        const auto next_box = [&]() {
-            const uint32_t at = kBoxes > 1 ? (boxes++ & 1) * kBox : 0;
-            if (lane == 0) {
-                if (kBoxes > 1) bulk_wait_read1();
-                else bulk_wait_read0();
-            }
-            __syncwarp();
-            return at;
-        };
         for (int u = pair; ok && u < units; u += pairs) {
             const int tiles = tiles_in_unit(p, kWhat, n, u);
             float run_m = -INFINITY, run_s = 0.f;
             for (int j = 0; ok && j < tiles; ++j) {
                 const Tile t = tile_of(p, kWhat, n, u, j);
                 const int seg = kSegments ? p.segment : max(t.kb1 - t.kb0, 1);
-                const bool empty = kWhat == kGrads && t.kb0 == t.kb1;   // a slice of nothing
-                if (kGroups > 1) {
-                    const bool mine = (empty ? 0 : gs & 1) == group;
-                    if (!mine) {
-                        gs += !empty;
-                        continue;
-                    }
-                }
                 // what the row brings along, asked for before the wait for its products
                 int target = -1;
                 float4 cf = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (kWhat == kStats) target = p.target[t.m0 + row];
                 if (kWhat == kSlopes) cf = p.coef[t.m0 + row];
-                const bool idle = kWhat != kGrads && row0 >= 64 * t.a_boxes;   // rows of no token, not even loaded
-                const auto hand_back = [&](int buf) {
+                float z[128];
+                if (kWhat == kGrads && t.kb0 == t.kb1) {   // an empty slice
+#pragma unroll
+                    for (int c = 0; c < 128; ++c) z[c] = 0.f;
+                }
+                for (int kb = t.kb0; kb < t.kb1; kb += seg, ++gs) {
+                    const int buf = gs & 1;
+                    ok = __all_sync(0xffffffffu, mbar_wait(bar_tfull + 8 * buf, (gs >> 1) & 1, abort_flag, p.wc.limit));
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (!kSegments || kb == t.kb0) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) tmem_ld32(t_at + buf * kTile + 32 * c, *reinterpret_cast<float(*)[32]>(&z[32 * c]));
+                        tmem_ld_wait();
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            float more[32];
+                            tmem_ld32(t_at + buf * kTile + 32 * c, more);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) z[32 * c + e] += more[e];
+                        }
+                    }
                     tc_fence_before();
                     __syncwarp();
                     // (test hook: the first hand-back of CTA 0 left out, so that the issuer's wait for it runs out)
                     if (lane == 0 && !(p.wc.skip_arrival && blockIdx.x == 0 && gs == 0 && warp == 2)) mbar_arrive_cluster(leader_tempty + 8 * buf);
-                };
-                float z[kChunk];
-                if (kSegments) {
-                    if (empty) {
-#pragma unroll
-                        for (int c = 0; c < kChunk; ++c) z[c] = 0.f;
-                    }
-                    for (int kb = t.kb0; kb < t.kb1; kb += seg, ++gs) {
-                        const int buf = gs & 1;
-                        ok = __all_sync(0xffffffffu, mbar_wait(bar_tfull + 8 * buf, (gs >> 1) & 1, abort_flag, p.wc.limit));
-                        if (!ok) break;
-                        tc_fence_after();
-                        if (kb == t.kb0) {
-#pragma unroll
-                            for (int c = 0; c < kChunk / 32; ++c) tmem_ld32(t_at + buf * kTile + 32 * c, *reinterpret_cast<float(*)[32]>(&z[32 * c]));
-                            tmem_ld_wait();
-                        } else {
-#pragma unroll
-                            for (int c = 0; c < kChunk / 32; ++c) {
-                                float more[32];
-                                tmem_ld32(t_at + buf * kTile + 32 * c, more);
-                                tmem_ld_wait();
-#pragma unroll
-                                for (int e = 0; e < 32; ++e) z[32 * c + e] += more[e];
-                            }
-                        }
-                        hand_back(buf);
-                    }
-                    if (!ok) break;
-                } else if (!empty) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(bar_tfull + 8 * (gs & 1), (gs >> 1) & 1, abort_flag, p.wc.limit));
-                    if (!ok) break;
-                    tc_fence_after();
                 }
-                // final gradients, of their type, or sums in fp32 that go on
-                const bool final = t.dw ? !p.dw_sliced : p.dh_last, wide = final && p.grad_bf16;   // boxes of 64 bf16 or 32 fp32 columns
-                const int out_row = t.dw && !p.dw_sliced ? p.v0 + t.m0 + row : t.m0 + row;
-                const int token = kWhat == kGrads && !t.dw && final && t.m0 + row < n ? p.row_of[t.m0 + row] : -1;
+                if (!ok) break;
+                if (kWhat != kGrads && row0 >= 64 * t.a_boxes) continue;   // rows of no token, not even loaded
+                const int c0 = t.n0 + half * 128;   // first column of this thread's 128, in the piece
+                if (kWhat == kStats) {
+                    int y = target - p.v0 - c0;
+                    if (y + c0 >= t.n0 + 64 * t.b_boxes) y = -1;   // a later chunk's
+                    const int end = min(t.n0 + 64 * t.b_boxes, p.V - p.v0);
+                    if (c0 + 128 > end) {
 #pragma unroll
-                for (int ch = 0; ch < 128 / kChunk; ++ch) {
-                    if (!kSegments) {
-                        if (empty) {
-#pragma unroll
-                            for (int c = 0; c < kChunk; ++c) z[c] = 0.f;
-                        } else {
-#pragma unroll
-                            for (int c = 0; c < kChunk / 32; ++c)
-                                tmem_ld32(t_at + (gs & 1) * kTile + kChunk * ch + 32 * c, *reinterpret_cast<float(*)[32]>(&z[32 * c]));
-                            tmem_ld_wait();
-                            if (ch == 128 / kChunk - 1) hand_back(gs & 1);
-                        }
+                        for (int c = 0; c < 128; ++c)
+                            if (c0 + c >= end) z[c] = -INFINITY;
                     }
-                    if (idle) continue;
-                    const int c0 = t.n0 + half * 128 + ch * kChunk;   // first of the columns in z, in the piece
-                    if (kWhat == kStats) {
-                        const int end = min(t.n0 + 64 * t.b_boxes, p.V - p.v0), y = target - p.v0 < end ? target - p.v0 - c0 : -1;
-                        if (c0 + kChunk > end) {
+                    float m4[4] = {z[0], z[1], z[2], z[3]};
 #pragma unroll
-                            for (int c = 0; c < kChunk; ++c)
-                                if (c0 + c >= end) z[c] = -INFINITY;
-                        }
-                        float m4[4] = {z[0], z[1], z[2], z[3]};
+                    for (int c = 4; c < 128; ++c) m4[c & 3] = fmaxf(m4[c & 3], z[c]);
+                    const float m = fmaxf(run_m, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.c2);
+                    const float shift = m == -INFINITY ? 0.f : m;
+                    float s4[4] = {run_s * rescale(run_m, m), 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int c = 4; c < kChunk; ++c) m4[c & 3] = fmaxf(m4[c & 3], z[c]);
-                        const float m = fmaxf(run_m, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.c2);
-                        const float shift = m == -INFINITY ? 0.f : m;
-                        float s4[4] = {run_s * rescale(run_m, m), 0.f, 0.f, 0.f};
+                    for (int c = 0; c < 128; ++c) s4[c & 3] += ex2(fmaf(z[c], p.c2, -shift));
+                    run_s = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    run_m = m;
+                    if (__any_sync(0xffffffffu, y >= 0 && y < 128)) {
+                        float zy = 0.f;
 #pragma unroll
-                        for (int c = 0; c < kChunk; ++c) s4[c & 3] += ex2(fmaf(z[c], p.c2, -shift));
-                        run_s = (s4[0] + s4[1]) + (s4[2] + s4[3]);
-                        run_m = m;
-                        if (__any_sync(0xffffffffu, y >= 0 && y < kChunk)) {
-                            float zy = 0.f;
+                        for (int c = 0; c < 128; ++c) zy = c == y ? z[c] : zy;
+                        if (y >= 0 && y < 128) p.zt[t.m0 + row] = zy;
+                    }
+                } else if (kWhat == kSlopes) {
+                    const int y = __float_as_int(cf.w) - p.v0 - c0;
+                    const bool here = __any_sync(0xffffffffu, y >= 0 && y < 128);
 #pragma unroll
-                            for (int c = 0; c < kChunk; ++c) zy = c == y ? z[c] : zy;
-                            if (y >= 0 && y < kChunk) p.zt[t.m0 + row] = zy;
-                        }
-                    } else if (kWhat == kSlopes) {
-                        const int y = __float_as_int(cf.w) - p.v0 - c0;
-                        const bool here = __any_sync(0xffffffffu, y >= 0 && y < kChunk);
+                    for (int c = 0; c < 128; ++c) z[c] = cf.y * ex2(fmaf(z[c], p.c2, -cf.x));
+                    if (here) {
 #pragma unroll
-                        for (int c = 0; c < kChunk; ++c) z[c] = cf.y * ex2(fmaf(z[c], p.c2, -cf.x));
-                        if (here) {
+                        for (int c = 0; c < 128; ++c) z[c] = c == y ? z[c] - cf.z : z[c];
+                    }
+                    // (rows behind the last token are zero: h is, to the end of its 64, and so are their factors)
+                    if (c0 + 128 > p.V - p.v0) {
 #pragma unroll
-                            for (int c = 0; c < kChunk; ++c) z[c] = c == y ? z[c] - cf.z : z[c];
-                        }
-                        // (rows behind the last token are zero: h is, to the end of its 64, and so are their factors)
-                        if (c0 + kChunk > p.V - p.v0) {
+                        for (int c = 0; c < 128; ++c)
+                            if (c0 + c >= p.V - p.v0) z[c] = 0.f;
+                    }
 #pragma unroll
-                            for (int c = 0; c < kChunk; ++c)
-                                if (c0 + c >= p.V - p.v0) z[c] = 0.f;
-                        }
+                    for (int c = 0; c < 2; ++c)
+                        for (int plane = 0;;) {
+                            // (every box is a bulk group, stored or not, so that the last but one has left this buffer)
+                            const uint32_t buf = (boxes++ & 1) * kBox;
+                            if (lane == 0) bulk_wait_read1();
+                            __syncwarp();
 #pragma unroll
-                        for (int c = 0; c < kChunk; c += 64)
-                            for (int plane = 0;;) {
-                                const uint32_t box = next_box();
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    const float *x = &z[c + 8 * e];
-                                    *reinterpret_cast<uint4 *>(stg + box + sw128(lane, e)) =
-                                        make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-                                }
-                                fence_proxy_async();
-                                __syncwarp();
-                                if (lane == 0) {
-                                    if (c0 + c < p.vc) tma_store_3d(&p.dz_out, stg_u32 + box, c0 + c, t.m0 + row0, plane);
-                                    bulk_commit();
-                                }
-                                if (++plane == p.planes) break;
-#pragma unroll
-                                for (int e = 0; e < 64; ++e) z[c + e] -= __bfloat162float(__float2bfloat16_rn(z[c + e]));   // what is left for the next plane
-                            }
-                    } else {
-                        const float *before32 = t.dw ? (const float *)p.dw_in : p.dh_before;
-                        if (final && before32 && out_row < (t.dw ? p.V : p.Tpad)) {
-                            const size_t at = (size_t)out_row * p.D;
-                            const bool half_width = t.dw && p.grad_bf16;
-#pragma unroll
-                            for (int c = 0; c < kChunk; c += 4)
-                                if (c0 + c < p.D) {
-                                    const float4 o = half_width ? load4(reinterpret_cast<const __nv_bfloat16 *>(p.dw_in) + at + c0 + c) : load4(before32 + at + c0 + c);
-                                    z[c] += o.x, z[c + 1] += o.y, z[c + 2] += o.z, z[c + 3] += o.w;
-                                }
-                        }
-                        const int first = out_row - lane, rows = t.dw ? (p.dw_sliced ? p.vc : p.V) : n;
-#pragma unroll
-                        for (int c = 0; c < kChunk; c += 32) {
-                            if (wide && (c & 32)) continue;
-                            const uint32_t box = next_box();
-                            if (wide) {
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    uint32_t v[4];
-#pragma unroll
-                                    for (int i = 0; i < 4; ++i) v[i] = pack_bf16(z[(c + 8 * e + 2 * i) % kChunk], z[(c + 8 * e + 2 * i + 1) % kChunk]);
-                                    *reinterpret_cast<uint4 *>(stg + box + sw128(lane, e)) = make_uint4(v[0], v[1], v[2], v[3]);
-                                }
-                            } else {
-#pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    *reinterpret_cast<float4 *>(stg + box + sw128(lane, e)) = make_float4(z[c + 4 * e], z[c + 4 * e + 1], z[c + 4 * e + 2], z[c + 4 * e + 3]);
-                            }
-                            if (!t.dw && final) {
-                                // rows go to where their tokens are: eight lanes a row of 128 bytes
-                                __syncwarp();
-                                const int es = wide ? 2 : 4, col = c0 + c + (lane & 7) * (16 / es);
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    const int r = e * 4 + (lane >> 3), to = __shfl_sync(0xffffffffu, token, r);
-                                    const uint4 v = *reinterpret_cast<const uint4 *>(stg + box + sw128(r, lane & 7));
-                                    if (to >= 0 && col < p.D) *reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(p.d_h) + ((size_t)to * p.D + col) * es) = v;
-                                }
-                                __syncwarp();
-                                if (lane == 0) bulk_commit();
-                                continue;
+                            for (int e = 0; e < 8; ++e) {
+                                const float *x = &z[64 * c + 8 * e];
+                                *reinterpret_cast<uint4 *>(stg + buf + sw128(lane, e)) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
                             }
                             fence_proxy_async();
                             __syncwarp();
                             if (lane == 0) {
-                                if (c0 + c < p.D && first < rows) {
-                                    if (t.dw) tma_store_3d(&p.dw_out, stg_u32 + box, c0 + c, first, p.dw_sliced ? t.slice : 0);
-                                    else if (p.dh_add) tma_add_3d(&p.dh_out, stg_u32 + box, c0 + c, first, t.slice);
-                                    else tma_store_3d(&p.dh_out, stg_u32 + box, c0 + c, first, t.slice);
-                                }
+                                if (c0 + 64 * c < p.vc) tma_store_3d(&p.dz_out, stg_u32 + buf, c0 + 64 * c, t.m0 + row0, plane);
                                 bulk_commit();
                             }
+                            if (++plane == p.planes) break;
+#pragma unroll
+                            for (int e = 0; e < 64; ++e) z[64 * c + e] -= __bfloat162float(__float2bfloat16_rn(z[64 * c + e]));   // what is left for the next plane
+                        }
+                } else {
+                    // a final gradient, of its type, or a sum in fp32 that goes on
+                    const bool final = t.dw ? !p.dw_sliced : p.dh_last, wide = final && p.grad_bf16;   // boxes of 64 bf16 or 32 fp32 columns
+                    const int out_row = t.dw && !p.dw_sliced ? p.v0 + t.m0 + row : t.m0 + row;
+                    const float *before32 = t.dw ? (const float *)p.dw_in : p.dh_before;
+                    if (final && before32 && out_row < (t.dw ? p.V : p.Tpad)) {
+                        const size_t at = (size_t)out_row * p.D;
+                        const bool half_width = t.dw && p.grad_bf16;
+#pragma unroll
+                        for (int c = 0; c < 128; c += 4)
+                            if (c0 + c < p.D) {
+                                const float4 o = half_width ? load4(reinterpret_cast<const __nv_bfloat16 *>(p.dw_in) + at + c0 + c) : load4(before32 + at + c0 + c);
+                                z[c] += o.x, z[c + 1] += o.y, z[c + 2] += o.z, z[c + 3] += o.w;
+                            }
+                    }
+                    const int first = out_row - lane, rows = t.dw ? (p.dw_sliced ? p.vc : p.V) : n;
+                    const int token = !t.dw && final && t.m0 + row < n ? p.row_of[t.m0 + row] : -1;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if (wide && (c & 1)) continue;
+                        const uint32_t buf = (boxes++ & 1) * kBox;
+                        if (lane == 0) bulk_wait_read1();
+                        __syncwarp();
+                        if (wide) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                uint32_t v[4];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) v[i] = pack_bf16(z[(32 * c + 8 * e + 2 * i) & 127], z[(32 * c + 8 * e + 2 * i + 1) & 127]);
+                                *reinterpret_cast<uint4 *>(stg + buf + sw128(lane, e)) = make_uint4(v[0], v[1], v[2], v[3]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                *reinterpret_cast<float4 *>(stg + buf + sw128(lane, e)) = make_float4(z[32 * c + 4 * e], z[32 * c + 4 * e + 1], z[32 * c + 4 * e + 2], z[32 * c + 4 * e + 3]);
+                        }
+                        if (!t.dw && final) {
+                            // rows go to where their tokens are: eight lanes a row of 128 bytes
+                            __syncwarp();
+                            const int es = wide ? 2 : 4, col = c0 + 32 * c + (lane & 7) * (16 / es);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const int r = e * 4 + (lane >> 3), to = __shfl_sync(0xffffffffu, token, r);
+                                const uint4 v = *reinterpret_cast<const uint4 *>(stg + buf + sw128(r, lane & 7));
+                                if (to >= 0 && col < p.D) *reinterpret_cast<uint4 *>(reinterpret_cast<uint8_t *>(p.d_h) + ((size_t)to * p.D + col) * es) = v;
+                            }
+                            __syncwarp();
+                            if (lane == 0) bulk_commit();
+                            continue;
+                        }
+                        fence_proxy_async();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (c0 + 32 * c < p.D && first < rows) {
+                                if (t.dw) tma_store_3d(&p.dw_out, stg_u32 + buf, c0 + 32 * c, first, p.dw_sliced ? t.slice : 0);
+                                else if (p.dh_add) tma_add_3d(&p.dh_out, stg_u32 + buf, c0 + 32 * c, first, t.slice);
+                                else tma_store_3d(&p.dh_out, stg_u32 + buf, c0 + 32 * c, first, t.slice);
+                            }
+                            bulk_commit();
                         }
                     }
                 }
-                if (!kSegments) gs += !empty;
             }
             if (ok && kWhat == kStats) {
                 const int chunk = p.first_part + u / row_tiles(n), m0 = u % row_tiles(n) * kTile;
@@ -883,7 +836,7 @@ bool prepare_product()
 template <int kWhat, bool kSegments>
 chela_status_t launch_product(const Product &p, int pairs, cudaStream_t stream)
 {
-    return launch_after(product_kernel<kWhat, kSegments>, 2 * pairs, threads_of(kWhat, kSegments), Layout<kWhat != kStats>::bytes, stream, p);
+    return launch_after(product_kernel<kWhat, kSegments>, 2 * pairs, kThreads, Layout<kWhat != kStats>::bytes, stream, p);
 }
 
 chela_status_t launch_rows(Rows &r, chela_dtype_t in_dtype, bool wide_ids, int sms, cudaStream_t stream)
@@ -969,9 +922,8 @@ chela_status_t launch_vocabloss_fwd(const chela_vocabloss_args_t &a, float *loss
         st = q.planes_in > 1 ? launch_product<kStats, true>(p, q.pairs, stream) : launch_product<kStats, false>(p, q.pairs, stream);
     }
     if (st != CHELA_OK) return st;
-    parts *= 2;
-    const int groups = parts <= 4 ? 1 : parts <= 64 ? 8 : 32;   // threads a row
-    return launch_after(join_kernel, q.Tpad / (256 / groups), 256, 0, stream, p.head, r.row_of, p.zt, p.part, parts, a.T, q.Tpad, groups, p.c2, loss, lse);
+    const int groups = parts <= 2 ? 1 : parts <= 32 ? 8 : 32;   // threads a row, by the parts (two a chunk)
+    return launch_after(join_kernel, q.Tpad / (256 / groups), 256, 0, stream, p.head, r.row_of, p.zt, p.part, 2 * parts, a.T, q.Tpad, groups, p.c2, loss, lse);
 }
 
 chela_status_t launch_vocabloss_bwd(const chela_vocabloss_args_t &a, const float *lse, const float *d_loss, const float *d_lse, void *d_h, const void *d_w_in, void *d_w,
