@@ -610,12 +610,13 @@ __global__ void __launch_bounds__(kRowsThreads) rows_kernel(const Rows r)
         __syncthreads();
     }
     // behind the last kept row: no targets to the end of its tile, zeros of h to the end of its 64 (d_w's sums read so many)
-    for (int i = n + blockIdx.x * kRowsThreads + tid; i < min(r.Tpad, (n + kTile - 1) / kTile * kTile); i += gridDim.x * kRowsThreads) {
+    // (counted in 64 bits: a CTA's place behind a number of tokens near 2^31 is past it)
+    for (long long i = n + (long long)blockIdx.x * kRowsThreads + tid; i < min(r.Tpad, (n + kTile - 1) / kTile * kTile); i += gridDim.x * kRowsThreads) {
         if (r.target) r.target[i] = -1;
         if (r.coef) r.coef[i] = make_float4(0.f, 0.f, 0.f, __int_as_float(-1));
     }
     if (copy)
-        for (int i = n + blockIdx.x * kRowsWarps + warp; i < (n + 63) / 64 * 64; i += gridDim.x * kRowsWarps)
+        for (long long i = n + (long long)blockIdx.x * kRowsWarps + warp; i < (n + 63) / 64 * 64; i += gridDim.x * kRowsWarps)
             for (int pl = 0; pl < r.planes; ++pl)
                 for (int c = lane * 8; c < r.D; c += 256) *reinterpret_cast<uint4 *>(r.hk + pl * plane + (size_t)i * r.D + c) = make_uint4(0u, 0u, 0u, 0u);
 }

@@ -253,6 +253,33 @@ def test_tables_beyond_32_bits_of_elements():
     assert float(d_w[:100].float().abs().sum()) == float(out[ids.eq(0)].float().abs().sum())
 
 
+def test_loss_of_as_many_tokens_as_there_may_be():
+    """2^31 - 4096 tokens, all but a few of them kept: 4096 tokens and their losses over and over."""
+    T, V, D, tail = 2 ** 31 - 4096, 24, 8, 4096
+    torch.cuda.empty_cache()
+    need = int(chela.lib().chela_vocabloss_workspace_bytes(T, V, D, chela.BF16)) + T * (2 * D + 4 + 8)
+    if torch.cuda.mem_get_info()[0] < need + (4 << 30):
+        pytest.skip("needs %d GB" % (need >> 30))
+    g = gen(17)
+    y = token_ids(g, tail, V, skew=False, dtype=torch.int32)
+    some, w = hidden(g, tail, V, D, torch.bfloat16, y)
+    true = chela.vocabloss_fwd(some, w, y)
+    h, targets = torch.empty(T, D, dtype=torch.bfloat16, device="cuda"), torch.empty(T, dtype=torch.int32, device="cuda")
+    h.view(-1, tail, D).copy_(some)
+    targets.view(-1, tail).copy_(y)
+    out = torch.tensor([5, T // 2, T - 2, T - 1], device="cuda")
+    targets[out] = -1
+    got = chela.vocabloss_fwd(h, w, targets)
+    for a, b in zip(got, true):
+        assert (a[out] == 0).all()
+        for i in out.tolist():
+            a[i] = b[i % tail]
+        for part in a.view(-1, tail).split(65536):
+            assert bool((part == b).all())
+    del h, targets, got, a, part
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("T", [6, 300])
 def test_what_is_not_finite_stays_with_its_token(T):
     V, D = 500, 64
