@@ -374,7 +374,8 @@ template <typename TW, typename TG, int kTokens, int kQuads, bool kGrad>
 chela_status_t launch_few(const Few &p, const Plan &q, cudaStream_t stream)
 {
     auto kern = few_kernel<TW, TG, kTokens, kQuads, kGrad>;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, q.smem) != cudaSuccess) return CHELA_ERR_CUDA;
+    // (the limit is the function's, not the thread's: set to what this call takes, it would refuse another thread's wider rows)
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost) != cudaSuccess) return CHELA_ERR_CUDA;
     kern<<<q.ctas, kThreads, q.smem, stream>>>(p);
     return last_launch_status();
 }

@@ -409,6 +409,37 @@ def test_threads_on_one_stream():
     assert sorted(right) == sorted(list(range(len(data))) * 30)   # no call refused, none wrong
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_threads_with_rows_of_different_widths(dt):
+    """The kernels of a few tokens take shared memory by the width of the rows: threads with narrow and wide ones at once."""
+    import threading
+    g = gen(19)
+    data, alone = [], []
+    for D in (64, 512, 1024, 8, 960, 128):
+        ids = token_ids(g, 4, 3000)
+        h, w = hidden(g, 4, 3000, D, DT[dt], ids)
+        data.append((ids, h, w, torch.rand(4, generator=g, device="cuda")))
+        alone.append(calls(*data[-1]))
+    torch.cuda.synchronize()
+    right, refused = [], []
+
+    def work(k):
+        for _ in range(300):
+            try:
+                out = calls(*data[k])
+            except chela.ChelaError as e:
+                refused.append((k, e))
+                return
+            if all(torch.equal(a, b) for a, b in zip(out, alone[k])):
+                right.append(k)
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(len(data))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not refused and sorted(right) == sorted(list(range(len(data))) * 300)
+
+
 def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_clean():
     g = gen(21)
     T, V, D = 600, 60000, 64   # enough units that the first CTA comes back to the buffer whose hand-back was left out
