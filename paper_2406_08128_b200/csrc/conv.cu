@@ -786,7 +786,7 @@ LongconvPlan longconv_plan(int B, int L, int D)
     p.total = p.nb > 1 ? align_up(p.off_xspec + (size_t)B * D * p.nb * (p.M + 2) * sizeof(float2), 256) : p.off_xspec;
     return p;
 }
-const size_t kBlockSmem = (size_t)(kBlockM + 256) * sizeof(float2);
+const size_t kBlockSmem = (size_t)(kBlockM + 256) * sizeof(float2);   // also the most that fft_conv_kernel takes
 chela_status_t block_kernels_ready()
 {
     if (cudaFuncSetAttribute(fft_block_spectrum_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBlockSmem) != cudaSuccess ||
@@ -840,7 +840,8 @@ chela_status_t launch_longconv_prepare(const float *k_long, int L, int D, void *
     const size_t smem = (size_t)(p.M + 256) * sizeof(float2);
     int threads = p.M / 16;
     threads = threads < 32 ? 32 : (threads > 1024 ? 1024 : threads);
-    if (cudaFuncSetAttribute(fft_conv_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return CHELA_ERR_CUDA;
+    // (the limit is the function's, not the thread's: one for all sizes, or a shorter call would refuse another thread's)
+    if (cudaFuncSetAttribute(fft_conv_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBlockSmem) != cudaSuccess) return CHELA_ERR_CUDA;
     fft_conv_kernel<0><<<D, threads, smem, stream>>>(const_cast<float *>(k_long), L, L, D, p.M, p.logM, tw, spec, spec_stride);
     return last_launch_status();
 }
@@ -900,9 +901,9 @@ chela_status_t launch_longconv(const void *x, const float *k_long, const float *
     const size_t smem = (size_t)(p.M + 256) * sizeof(float2);
     int threads = p.M / 16;
     threads = threads < 32 ? 32 : (threads > 1024 ? 1024 : threads);
-    cudaError_t e = cudaFuncSetAttribute(fft_conv_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = cudaFuncSetAttribute(fft_conv_kernel<0>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBlockSmem);
     if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(fft_conv_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        e = cudaFuncSetAttribute(fft_conv_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBlockSmem);
     if (e != cudaSuccess) return CHELA_ERR_CUDA;
     if (!spectrum) fft_conv_kernel<0><<<D, threads, smem, stream>>>(const_cast<float *>(k_long), L, L, D, p.M, p.logM, tw, spec, spec_stride);
     fft_conv_kernel<1><<<B * D, threads, smem, stream>>>(at, p.Ls, L, D, p.M, p.logM, tw, spec, spec_stride);

@@ -101,3 +101,33 @@ def test_reparameterised_short_kernels_match_the_parallel_pair():
     k_long = (rng.standard_normal((D, L), dtype=np.float32) * np.exp(-0.001 * np.arange(L))).astype(np.float32)
     z = to_numpy(chela.longconv_fwd(to_device(x, "bf16"), dev_f32(k_long), merged))
     assert rel_err(z, oracle.longconv_fft(ref, k_long)) <= 2e-5
+
+
+def test_threads_with_long_kernels_of_different_lengths():
+    """The transform of short sequences takes shared memory by their length: threads with several lengths at once."""
+    import threading
+    import torch
+    B, D = 2, 16
+    data, alone = [], []
+    for L in (7, 40, 100, 200, 400, 512):
+        g = torch.Generator(device="cuda").manual_seed(L)
+        data.append((torch.randn(B, L, D, generator=g, device="cuda"), torch.randn(D, L, generator=g, device="cuda")))
+        alone.append(chela.longconv_fwd(*data[-1]))
+    torch.cuda.synchronize()
+    right, refused = [], []
+
+    def work(k):
+        for _ in range(300):
+            try:
+                out = chela.longconv_fwd(*data[k])
+            except chela.ChelaError as e:
+                refused.append((k, e))
+                return
+            if torch.equal(out, alone[k]):
+                right.append(k)
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(len(data))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not refused and sorted(right) == sorted(list(range(len(data))) * 300)
