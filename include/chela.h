@@ -497,8 +497,8 @@ chela_status_t chela_embed_bwd(const void *ids, int wide_ids, const void *d_out,
  * h : [T, D], w : [V, D] of in_dtype (F32 or BF16), rows h_stride and w_stride elements apart.  0 < scale <= 1e30.  At most
  * 2^45 logits.
  * loss, lse : [T] fp32 (4-byte aligned), zero for tokens that are left out.  bf16 operands are multiplied on the tensor cores
- * with fp32 sums, fp32 operands there too, as sums of three bf16 parts each (2^-24 of a product is lost); a few tokens are
- * multiplied in fp32.
+ * with fp32 sums, fp32 operands there too, as sums of three bf16 parts each (2^-24 of a product is lost; an infinite operand, or
+ * one past the largest bf16, has no such parts and gives NaN); a few tokens are multiplied in fp32.
  * workspace: chela_vocabloss_workspace_bytes; chela_async_status reads a wait that gave up from it.
  */
 typedef struct {

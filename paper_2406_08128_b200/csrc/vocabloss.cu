@@ -346,7 +346,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                         if (y >= 0 && y < 128) p.zt[t.m0 + row] = zy;
                     }
                 } else if (kWhat == kSlopes) {
-                    const int y = __float_as_int(cf.w) - p.v0 - c0;
+                    const int word = __float_as_int(cf.w), y = word - p.v0 - c0;
                     const bool here = __any_sync(0xffffffffu, y >= 0 && y < 128);
 #pragma unroll
                     for (int c = 0; c < 128; ++c) z[c] = cf.y * ex2(fmaf(z[c], p.c2, -cf.x));
@@ -354,11 +354,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
 #pragma unroll
                         for (int c = 0; c < 128; ++c) z[c] = c == y ? z[c] - cf.z : z[c];
                     }
-                    // (rows behind the last token are zero: h is, to the end of its 64, and so are their factors)
-                    if (c0 + 128 > p.V - p.v0) {
+                    // rows behind the last token: zero whatever the weights hold (an infinite one times their h of zero is none)
+                    if (word < 0 || c0 + 128 > p.V - p.v0) {
 #pragma unroll
                         for (int c = 0; c < 128; ++c)
-                            if (c0 + c >= p.V - p.v0) z[c] = 0.f;
+                            if (word < 0 || c0 + c >= p.V - p.v0) z[c] = 0.f;
                     }
 #pragma unroll
                     for (int c = 0; c < 2; ++c)

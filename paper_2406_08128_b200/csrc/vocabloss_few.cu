@@ -193,7 +193,8 @@ __global__ void __launch_bounds__(kThreads, two_ctas(kTokens, kQuads, kGrad) ? 2
             } else {
                 float dz = s_g1[t] * ex2(z - s_lse[t]);
                 if (v == s_target[t]) dz -= s_g0[t];
-                s_dz[tid] = v < p.V ? splat2(dz) : splat2(0.f);
+                // (a token that is left out by choice, not by its factor of zero: the weights may hold infinities)
+                s_dz[tid] = v < p.V && s_target[t] >= 0 ? splat2(dz) : splat2(0.f);
             }
         }
         if (kGrad) {
@@ -301,15 +302,17 @@ __global__ void __launch_bounds__(kThreads) few_join_kernel(const Few p, int cta
     }
 }
 
-// d_h: the CTAs' shares added up, 32 columns of a token a CTA, 32 shares side by side and then in order.
+// d_h: the CTAs' shares added up, 32 columns of a token a CTA, 32 shares side by side and then in order; zero where it is left out
+// (its shares are sums of zeros, but of zeros times the weights).
 template <typename TG>
 __global__ void __launch_bounds__(kThreads) few_spread_kernel(const Few p, int ctas, int tokens, TG *d_h)
 {
     __shared__ float4 s_sum[32][8];
     const int t = blockIdx.y, quad = threadIdx.x & 7, lot = threadIdx.x >> 3, c = blockIdx.x * 32 + quad * 4;
+    const long long y = target_of(p, t);
     griddep_wait();
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (c < p.D)
+    if (c < p.D && y >= 0 && y < p.V)
 #pragma unroll 4
         for (int q = lot; q < ctas; q += 32) {
             const float4 x = load4(p.dhp + ((size_t)q * tokens + t) * p.D + c);

@@ -303,6 +303,44 @@ def test_what_is_not_finite_stays_with_its_token(T):
     assert torch.isfinite(d_w).all()
 
 
+@pytest.mark.parametrize("it", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 7, 13, 21, 300])
+def test_tokens_left_out_take_nothing_from_weights_that_are_not_finite(T, it):
+    V, D = 500, 64
+    g = gen(T + 40)
+    targets = token_ids(g, T, V)
+    h, w = hidden(g, T, V, D, DT[it], targets)
+    w[3], w[77, 5], w[V - 1, 9] = float("nan"), float("inf"), float("-inf")
+    targets[::3] = -1
+    left = ~ref.kept_of(targets, V)
+    d_w_in = normal(g, V, D)
+    for y in (targets, torch.full_like(targets, V)):   # some, and all of them
+        loss, lse = chela.vocabloss_fwd(h, w, y)
+        got = chela.vocabloss_bwd(h, w, y, lse, torch.ones(T, device="cuda"), d_w_in=d_w_in)
+        assert (loss[left] == 0).all() and (lse[left] == 0).all() and (got.d_h[left] == 0).all()
+        if y is not targets:
+            assert (got.d_h == 0).all() and torch.equal(got.d_w, d_w_in)
+
+
+@pytest.mark.parametrize("T,it", [(5, "bf16"), (5, "f32"), (11, "f32"), (21, "bf16"), (70, "bf16"), (300, "bf16")])
+def test_a_word_that_its_weights_rule_out(T, it):
+    """A logit of minus infinity for every token: the word has no probability, and its gradient is zero."""
+    V, D, out = 400, 64, 123
+    g = gen(T + 50)
+    targets = token_ids(g, T, V)
+    targets[targets == out] = 0
+    h, w = hidden(g, T, V, D, DT[it], targets)
+    h = h.abs()
+    w[out] = float("-inf")
+    _, lse = chela.vocabloss_fwd(h, w, targets)
+    some = torch.arange(V, device="cuda") != out
+    r = ref.loss(h, w[some], targets - (targets > out).to(targets.dtype), 1.0, torch.ones(T, device="cuda"))
+    within(lse, r["lse"], ref.lse_bound(r, D, DT[it]), "lse")
+    d_w = chela.vocabloss_bwd(h, w, targets, lse, torch.ones(T, device="cuda")).d_w
+    assert (d_w[out] == 0).all()
+    within(d_w[some], r["d_w"], ref.grad_bounds(r, T, V, D, DT[it], torch.float32)[1], "d_w")
+
+
 def test_large_logits_and_a_certain_target():
     """Logits of hundreds, and tokens whose target has all the weight: the loss keeps its digits near zero."""
     T, V, D = 200, 1000, 64
