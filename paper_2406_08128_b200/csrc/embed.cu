@@ -76,10 +76,12 @@ __global__ void __launch_bounds__(256) embed_kernel(const Idx *ids, const TI *w,
             const int c = (int)(i % chunks) * 256 + lane * 8;
             if (c >= D) continue;
             uint4 u = make_uint4(0u, 0u, 0u, 0u);
-            if (kept) u = *reinterpret_cast<const uint4 *>(row + c);
-            uint32_t *v = reinterpret_cast<uint32_t *>(&u);
+            if (kept) {
+                u = *reinterpret_cast<const uint4 *>(row + c);
+                uint32_t *v = reinterpret_cast<uint32_t *>(&u);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = sm100::pack_bf16(__uint_as_float(v[e] << 16) * scale, __uint_as_float(v[e] & 0xffff0000u) * scale);
+                for (int e = 0; e < 4; ++e) v[e] = sm100::pack_bf16(__uint_as_float(v[e] << 16) * scale, __uint_as_float(v[e] & 0xffff0000u) * scale);
+            }
             *reinterpret_cast<uint4 *>(out + t * D + c) = u;
             continue;
         }

@@ -53,6 +53,15 @@ def test_embedding(T, V, D, wt, ot, left_out, ids):
     within(out, true, (2.0 ** -23 + ref.HALF[DT[ot]]) * true.abs(), "out")   # the scale as fp32, its product, the output
 
 
+@pytest.mark.parametrize("wt,ot", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16"), ("f32", "f32")])
+def test_rows_left_out_are_zero_whatever_the_scale(wt, ot):
+    w = normal(gen(1), 10, 520, dtype=DT[wt])
+    ids = torch.tensor([3, -1, 10, 0], device="cuda")
+    for scale in (-2.0, float("inf"), float("nan")):
+        rows = chela.embed_fwd(ids, w, scale=scale, out_dtype=CODE[ot])[1:3].float()
+        assert (rows == 0).all() and not torch.signbit(rows).any()
+
+
 @pytest.mark.parametrize("T,V,D,it,gt,left_out,skew", [
     (1, 1, 8, "bf16", "f32", 0, True), (2, 300, 8, "f32", "bf16", 0, True), (63, 10, 24, "bf16", "bf16", 0.3, True), (64, 1, 1024, "bf16", "f32", 0, True),
     (65, 1, 264, "f32", "f32", 0, True), (129, 2, 256, "bf16", "f32", 0.1, False), (1000, 511, 520, "bf16", "bf16", 0.5, True),
