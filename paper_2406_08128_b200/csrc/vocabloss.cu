@@ -15,7 +15,8 @@
 // terms (its rounding is as large as theirs and independent between terms), and split in bf16 planes otherwise: two, or three
 // (24 bits) where the gradients are fp32.  fp32 operands are split in three planes too, and a product of
 // them is the six plane products that reach 2^-24 of the result, the small ones first.  The tensor cores truncate the
-// accumulator at every step, so the fp32 modes end a sum after kSegment blocks and add the segments in registers.
+// accumulator at every step, so long sums are cut in segments that the epilogue adds up in registers: however long a sum, the
+// truncations take no more of it than those of one segment take of that.
 #include "packed.cuh"
 #include "sm100_pair.cuh"
 #include "vocabloss.cuh"
@@ -29,7 +30,12 @@ constexpr int kTile = 256;              // rows and columns of a tile: 128 rows 
 constexpr int kOperand = 128 * 128, kStageBytes = 2 * kOperand;
 constexpr int kEpilogueWarps = 8, kThreads = 64 + 32 * kEpilogueWarps;
 constexpr int kBox = 32 * 128, kStagingWarp = 2 * kBox;   // two boxes of 32 rows x 128 bytes: one is filled while the other is stored
-constexpr int kSegment = 4, kLongSegment = 16;   // K blocks of 64 that the tensor cores add up: fp32 gradients and logits; bf16 ones
+// K blocks of 64 (four truncated steps of up to 2^-23 each) that the tensor cores add up at most.  fp32 logits and gradients: 2^-19
+// of a plane product's segment.  bf16 operands' logits, and bf16 gradients of dz in planes: 2^-17, the same for any D (uncut, the
+// logits of 8192 positive products were 3.0e-5 too small, of 524288 3.3e-3; 7e-7 now.  4096 x 50000 x 2048: 558 -> 576 us, with
+// gradients 2311 -> 2368).  bf16 gradients of dz in one plane: 2^-13, a sixteenth of half a step of dz and of the result (uncut, 65536
+// products of a slice 3.9e-4 too small, 8e-5 now; no difference in time).
+constexpr int kSegment = 4, kLongSegment = 16, kWholeSegment = 256;
 enum What { kStats, kSlopes, kGrads };
 
 // The ring of operands, and what the epilogue stages; kStats stages nothing and has the room for two stages more (48 tokens
@@ -864,7 +870,6 @@ bool set_operands(Product &p, const chela_vocabloss_args_t &a, const Plan &q, ui
     p.h_in_planes = q.planes_in > 1;
     p.c2 = a.scale * kLog2e;
     p.wc = current_wait_ctl();
-    p.segment = kSegment;
     p.per_chunk = q.per_chunk, p.sh = q.sh, p.sv = q.sv, p.planes = q.planes_dz;
     if (!map_3d(&p.hk, ws + q.hk, false, a.D, q.Tpad, q.planes_in, (long long)a.D * 2, (long long)hk_plane, 64, 64)) return false;
     if (q.planes_in > 1) {
@@ -874,6 +879,10 @@ bool set_operands(Product &p, const chela_vocabloss_args_t &a, const Plan &q, ui
     return map_3d(&p.h, a.h, false, a.D, a.T, 1, a.h_stride * 2, a.h_stride * 2, 64, 64) &&
            map_3d(&p.w, a.w, false, a.D, a.V, 1, a.w_stride * 2, a.w_stride * 2, 64, 64);
 }
+
+// Logits whose sums are cut: those of fp32 operands, and of bf16 ones over more columns than one segment takes.
+int logit_segment(const Plan &q) { return q.planes_in > 1 ? kSegment : kLongSegment; }
+bool logits_cut(const Plan &q, int D) { return q.planes_in > 1 || ceil_div(D, 64) > kLongSegment; }
 
 // The weights of the piece that starts at v0: rows of w's map, or planes of them.
 chela_status_t set_piece(Product &p, const chela_vocabloss_args_t &a, const Plan &q, uint8_t *ws, int v0, int sms, cudaStream_t stream)
@@ -905,14 +914,16 @@ chela_status_t launch_vocabloss_fwd(const chela_vocabloss_args_t &a, float *loss
     const Plan q = make_plan(a.T, a.V, a.D, a.in_dtype, CHELA_BF16, false);
     uint8_t *ws = reinterpret_cast<uint8_t *>(workspace);
     const int sms = 2 * q.pairs;
+    const bool cut = logits_cut(q, a.D);
     Product p{};
-    if (!(q.planes_in > 1 ? prepare_product<kStats, true>() : prepare_product<kStats, false>()) || !set_operands(p, a, q, ws)) return CHELA_ERR_CUDA;
+    if (!(cut ? prepare_product<kStats, true>() : prepare_product<kStats, false>()) || !set_operands(p, a, q, ws)) return CHELA_ERR_CUDA;
     Rows r{};
     r.targets = a.targets, r.h = a.h, r.h_stride = a.h_stride, r.T = a.T, r.Tpad = q.Tpad, r.V = a.V, r.D = a.D, r.planes = q.planes_in;
     r.head = p.head, r.row_of = (int *)(ws + q.row_of), r.target = (int *)(ws + q.target), r.loss_out = loss, r.lse_out = lse, r.hk = (__nv_bfloat16 *)(ws + q.hk);
     chela_status_t st = launch_rows(r, a.in_dtype, a.wide_ids != 0, sms, stream);
     p.target = r.target, p.zt = (float *)(ws + q.zt), p.part = (float2 *)(ws + q.part);
     p.terms = q.planes_in > 1 ? kTerms6 : kTerms1;
+    p.segment = logit_segment(q);
     int parts = 0;
     for (int i = 0; st == CHELA_OK && i < q.pieces; ++i) {
         const int v0 = i * q.vc, boxes = ceil_div((a.V - v0 < q.vc ? a.V - v0 : q.vc), 64);
@@ -920,7 +931,7 @@ chela_status_t launch_vocabloss_fwd(const chela_vocabloss_args_t &a, float *loss
         if (st != CHELA_OK) return st;
         p.first_part = parts;
         parts += ceil_div(boxes, q.per_chunk);
-        st = q.planes_in > 1 ? launch_product<kStats, true>(p, q.pairs, stream) : launch_product<kStats, false>(p, q.pairs, stream);
+        st = cut ? launch_product<kStats, true>(p, q.pairs, stream) : launch_product<kStats, false>(p, q.pairs, stream);
     }
     if (st != CHELA_OK) return st;
     const int groups = parts <= 2 ? 1 : parts <= 32 ? 8 : 32;   // threads a row, by the parts (two a chunk)
@@ -937,8 +948,10 @@ chela_status_t launch_vocabloss_bwd(const chela_vocabloss_args_t &a, const float
     const bool f32 = grad_dtype == CHELA_F32;
     Product p{};
     const Terms terms = q.planes_in > 1 ? (f32 ? kTerms6 : kTerms3B) : f32 ? kTerms3 : q.planes_dz > 1 ? kTerms2A : kTerms1;   // of the gradients
-    if (!(q.planes_in > 1 ? prepare_product<kSlopes, true>() : prepare_product<kSlopes, false>()) ||
-        !(terms.n > 1 ? prepare_product<kGrads, true>() : prepare_product<kGrads, false>()) || !set_operands(p, a, q, ws))
+    // gradients whose sums are cut: those of several terms, and those over more tokens or words than one segment takes
+    const bool cut = logits_cut(q, a.D), cut_grads = terms.n > 1 || ceil_div(ceil_div(a.T, 64), q.sv) > kWholeSegment || ceil_div(q.vc / 64, q.sh) > kWholeSegment;
+    if (!(cut ? prepare_product<kSlopes, true>() : prepare_product<kSlopes, false>()) || !(cut_grads ? prepare_product<kGrads, true>() : prepare_product<kGrads, false>()) ||
+        !set_operands(p, a, q, ws))
         return CHELA_ERR_CUDA;
     const long long dz_row = (long long)q.vc * 2, es = f32 ? 4 : 2;
     const bool sums = q.sh > 1 || q.pieces > 1;   // d_h passes through fp32 sums
@@ -962,15 +975,15 @@ chela_status_t launch_vocabloss_bwd(const chela_vocabloss_args_t &a, const float
         st = set_piece(p, a, q, ws, v0, sms, stream);
         if (st != CHELA_OK) return st;
         p.terms = q.planes_in > 1 ? kTerms6 : kTerms1;
-        p.segment = kSegment;
-        st = q.planes_in > 1 ? launch_product<kSlopes, true>(p, q.pairs, stream) : launch_product<kSlopes, false>(p, q.pairs, stream);
+        p.segment = logit_segment(q);
+        st = cut ? launch_product<kSlopes, true>(p, q.pairs, stream) : launch_product<kSlopes, false>(p, q.pairs, stream);
         if (st != CHELA_OK) return st;
         p.terms = terms;
-        p.segment = f32 ? kSegment : kLongSegment;
+        p.segment = f32 ? kSegment : terms.n > 1 ? kLongSegment : kWholeSegment;
         p.dh_add = i > 0;
         p.dh_last = q.sh == 1 && i + 1 == q.pieces;
         p.dh_before = i > 0 ? (const float *)(ws + q.dhp) : nullptr;
-        st = p.terms.n > 1 ? launch_product<kGrads, true>(p, q.pairs, stream) : launch_product<kGrads, false>(p, q.pairs, stream);
+        st = cut_grads ? launch_product<kGrads, true>(p, q.pairs, stream) : launch_product<kGrads, false>(p, q.pairs, stream);
         if (st == CHELA_OK && q.sv > 1) {
             const size_t off = (size_t)v0 * a.D;
             const float *part = (const float *)(ws + q.dwp);

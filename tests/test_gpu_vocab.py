@@ -182,6 +182,66 @@ def test_fp32_weights_of_several_pieces():
         within(a, r[name], b, name)
 
 
+def positive(g, rows, D):
+    """bf16 values between 1 and 4, larger towards the last columns, so that rounded sums of a column have mantissas of every kind."""
+    out, slope = torch.empty(rows, D, dtype=torch.bfloat16, device="cuda"), 1 + torch.arange(D, device="cuda") / D
+    for part in out.split(8192):
+        part.copy_((1 + torch.rand(part.shape, generator=g, device="cuda")) * slope)
+    return out
+
+
+def relative_mean(got, true):
+    """Mean of the signed relative errors, which rounding to nearest leaves near zero and truncation does not."""
+    return float(((got.double() - true) / true).mean())
+
+
+@pytest.mark.parametrize("D", [1024, 1032, 8192, 65536])
+@pytest.mark.parametrize("it", ["bf16", "f32"])
+def test_logits_of_many_columns(D, it):
+    """Products of one sign, so that the truncated sums lose from all of them: no more for many columns than for 1024."""
+    T, V = 40, 300
+    g = gen(D)
+    h, w = positive(g, T, D).to(DT[it]), positive(g, V, D).to(DT[it])
+    y = torch.arange(T, device="cuda")
+    loss, lse = chela.vocabloss_fwd(h, w, y, scale=1.0 / 64)
+    z = torch.cat([part.double() @ w.double().t() for part in h.split(8)]) / 64
+    true = torch.logsumexp(z, 1)
+    # 64 steps of 2^-23 (fp32: 16 and, for small terms, next to nothing, and what six products leave out, 3 2^-24), as many fp32
+    # sums as there are segments, and some roundings
+    steps, sums = (64, D / 1024) if it == "bf16" else (17 + 2, D / 256)
+    bound = (steps * 2.0 ** -23 + (sums + 8) * 2.0 ** -24) * z.amax(1) + 2.0 ** -20
+    within(lse, true, bound, "lse")
+    within(loss, true - z[y, y], 2 * bound, "loss")
+
+
+def test_gradients_of_many_tokens_lose_nothing_to_truncation():
+    """d_w in bf16 over 2^18 tokens, all terms of one sign and every dz a bf16 value: half a step, and the truncations of 16384 terms,
+    1024 of at most 2^-23, of the mean."""
+    T, V, D = 2 ** 18, 1024, 8192
+    g = gen(41)
+    h, d_lse = positive(g, T, D), positive(g, T, 1)[:, 0].float()
+    w, y = torch.zeros(V, D, dtype=torch.bfloat16, device="cuda"), torch.zeros(T, dtype=torch.int32, device="cuda")
+    _, lse = chela.vocabloss_fwd(h, w, y)
+    got = chela.vocabloss_bwd(h, w, y, lse, None, d_lse, grad_dtype=chela.BF16).d_w
+    true = sum((a.double() * b.double()[:, None]).sum(0) for a, b in zip(h.split(8192), d_lse.split(8192))) / V
+    within(got[1], true, (2.0 ** -8 + 2.0 ** -13) * true, "d_w")
+    # beside the truncations: the mean of D roundings, each off by at most 2^-8 (0.42 of that in the quadratic mean)
+    assert abs(relative_mean(got[1], true)) <= 2.0 ** -13 + 5 * 0.42 * 2.0 ** -8 / D ** 0.5
+
+
+def test_gradients_over_many_words_lose_nothing_to_truncation():
+    """The same of d_h over 2^16 words."""
+    T, V, D = 512, 2 ** 16, 16384
+    g = gen(42)
+    w, d_lse = positive(g, V, D), positive(g, T, 1)[:, 0].float()
+    h, y = torch.zeros(T, D, dtype=torch.bfloat16, device="cuda"), torch.zeros(T, dtype=torch.int32, device="cuda")
+    _, lse = chela.vocabloss_fwd(h, w, y)
+    got = chela.vocabloss_bwd(h, w, y, lse, None, d_lse, grad_dtype=chela.BF16).d_h
+    true = d_lse.double()[:, None] * (sum(part.double().sum(0) for part in w.split(8192)) / V)
+    within(got, true, (2.0 ** -8 + 2.0 ** -13) * true, "d_h")
+    assert abs(relative_mean(got, true)) <= 2.0 ** -13 + 5 * 0.42 * 2.0 ** -8 / D ** 0.5
+
+
 @pytest.mark.parametrize("T", [4, 70, 700])
 def test_gradients_against_differences_of_the_definition(T):
     V, D, eps = 150, 48, 1e-5
