@@ -210,10 +210,11 @@ chela_status_t chela_async_status(const void *workspace, cudaStream_t stream);
 /*
  * Test hook for the bounded waits (the paper has no counterpart).  Every device-side wait of the tensor-core kernels
  * gives up after `limit_cycles` SM cycles (<= 0: the default, about one second) and then ends as chela_async_status
- * describes.  skip_arrival != 0 makes the first CTA of the d = 64 linear-attention kernels and of the tensor-core
- * projection leave out one mbarrier arrival, so that the role waiting for it runs into the limit: the kernel returns by
- * itself, records CHELA_ERR_TIMEOUT, and words 8..11 of the workspace header keep the site of the wait, the CTA, the
- * chunk and the grid size.  Process-wide, not thread-safe, read by every later launch: set it, launch, set it back.
+ * describes.  skip_arrival != 0 makes the first CTA of the d = 64 linear-attention kernels, of the tensor-core
+ * projection and of the vocabulary loss's kernels leave out one mbarrier arrival, so that the role waiting for it runs into
+ * the limit: the kernel returns by itself, records CHELA_ERR_TIMEOUT, and words 8..11 of the workspace header keep the site of
+ * the wait, the CTA, the chunk and the grid size (the vocabulary loss keeps the status alone).  Process-wide, not thread-safe,
+ * read by every later launch: set it, launch, set it back.
  */
 void chela_debug_wait_control(long long limit_cycles, int skip_arrival);
 

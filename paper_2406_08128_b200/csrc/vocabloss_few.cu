@@ -108,7 +108,8 @@ __global__ void __launch_bounds__(kThreads, two_ctas(kTokens, kQuads, kGrad) ? 2
         sm100::mbar_init(bars + 8, 1);
         sm100::fence_barrier_init();
         sm100::fence_proxy_async();
-        for (int k = 0; k < 2 && blockIdx.x + k * gridDim.x < count; ++k)
+        // (test hook: the first copy of CTA 0 left out, so that the wait for it runs out)
+        for (int k = p.wc.skip_arrival && blockIdx.x == 0; k < 2 && blockIdx.x + k * gridDim.x < count; ++k)
             load_tile(tiles + (size_t)k * rows * D, bars + 8 * k, p, (blockIdx.x + (long long)k * gridDim.x) * rows, rows);
     }
     if (tid < kTokens) {

@@ -565,6 +565,33 @@ def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_clean():
     assert torch.equal(got[0], clean[0]) and torch.equal(got[1], clean[1])
 
 
+@pytest.mark.parametrize("T,V,D,it,gt", [(4, 30000, 256, "bf16", "bf16"), (14, 30000, 520, "f32", "f32"),   # a few tokens
+                                         (600, 60000, 64, "bf16", "bf16"), (600, 60000, 64, "bf16", "f32")])
+def test_waits_that_run_out_forward_and_backward(T, V, D, it, gt):
+    """CTA 0 leaves out an arrival: the status says so, later launches of the call end too, and the next call is clean."""
+    g = gen(23)
+    ids = token_ids(g, T, V)
+    h, w = hidden(g, T, V, D, DT[it], ids)
+    d_loss = torch.rand(T, generator=g, device="cuda")
+    _, lse = clean = chela.vocabloss_fwd(h, w, ids)
+    grads = chela.vocabloss_bwd(h, w, ids, lse, d_loss, grad_dtype=CODE[gt])
+    lib = chela.lib()
+    for call, need, want in (
+            (lambda ws: chela.vocabloss_fwd(h, w, ids, workspace=ws), lib.chela_vocabloss_workspace_bytes(T, V, D, CODE[it]), clean),
+            (lambda ws: chela.vocabloss_bwd(h, w, ids, lse, d_loss, grad_dtype=CODE[gt], workspace=ws),
+             lib.chela_vocabloss_bwd_workspace_bytes(T, V, D, CODE[it], CODE[gt]), grads)):
+        ws = torch.zeros(int(need), dtype=torch.uint8, device="cuda")
+        try:
+            chela.debug_wait_control(6_000_000, 1)
+            call(ws)
+            assert chela.async_status(ws) == chela.ERR_TIMEOUT
+        finally:
+            chela.debug_wait_control(0, 0)
+        got = call(ws)
+        assert chela.async_status(ws) == chela.OK
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 # ------------------------------------------------------------------------------------------------ together
 
 def test_a_language_model_with_tied_weights_trains_as_its_definition_says():
