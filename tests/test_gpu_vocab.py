@@ -167,6 +167,55 @@ def test_loss_of_several_pieces_of_the_vocabulary(T, V, D, gt):
         within(a, r[name], b, name)
 
 
+@pytest.mark.parametrize("T,V,D,it,gt", [
+    (65536, 4500, 64, "bf16", "bf16"), (40000, 3000, 40, "bf16", "f32"),     # d_w in slices, added up by a kernel of their own
+    (16384, 20000, 1024, "bf16", "bf16"), (9000, 50001, 264, "bf16", "f32"),  # in whole sums, from the products' epilogues
+    (300, 90000, 2048, "f32", "bf16"), (24, 90000, 2048, "f32", "f32")])      # the same, and d_h in slices over the pieces
+def test_pieces_of_the_vocabulary_on_top_of_another_gradient(T, V, D, it, gt):
+    """Every piece finds its rows of the earlier gradient, in a buffer of its own and in place."""
+    g = gen(T + D)
+    targets = token_ids(g, T, V, 0.05)
+    h, w = hidden(g, T, V, D, DT[it], targets)
+    d_loss = torch.rand(T, generator=g, device="cuda") / T
+    # of a word's own size: rows that are put on top of another word's show
+    d_w_in = (normal(g, V, D) * (1e-3 * (1 + torch.arange(V, device="cuda") % 997))[:, None]).to(DT[gt])
+    _, lse = chela.vocabloss_fwd(h, w, targets)
+    got = chela.vocabloss_bwd(h, w, targets, lse, d_loss, grad_dtype=CODE[gt], d_w_in=d_w_in)
+    held = d_w_in.clone()
+    same = chela.vocabloss_bwd(h, w, targets, lse, d_loss, grad_dtype=CODE[gt], d_w_in=held, d_w=held)
+    assert same.d_w is held and torch.equal(held, got.d_w) and torch.equal(same.d_h, got.d_h)
+    r = ref.loss(h, w, targets, 1.0, d_loss, None, d_w_in)
+    for name, a, b in zip(("d_h", "d_w"), got, ref.grad_bounds(r, T, V, D, DT[it], DT[gt])):
+        within(a, r[name], b, name)
+
+
+@pytest.mark.parametrize("T,V,D,it,left_out", [(2047, 3000, 264, "bf16", 0.1), (4097, 40, 512, "bf16", 0), (300, 20001, 136, "bf16", 0), (700, 3000, 1032, "bf16", 0.5),
+                                               (48, 9000, 256, "bf16", 0), (7, 3000, 256, "bf16", 0), (500, 3000, 200, "f32", 0)])
+def test_bf16_gradients_in_the_norm(T, V, D, it, left_out):
+    """Errors against the norms: dz's rounding where it has one plane and more than 64 tokens, and the result's.  A rounding error
+    is spread over half a step, 2^-8 / sqrt(3) of the value in the quadratic mean at most; those of dz are independent, so that their
+    squares add up, weighted by the other factor's."""
+    g = gen(T + V + D)
+    targets = token_ids(g, T, V, left_out)
+    h, w = hidden(g, T, V, D, DT[it], targets)
+    d_loss = torch.rand(T, generator=g, device="cuda") / T
+    r = ref.loss(h, w, targets, 1.0, d_loss)
+    _, lse = chela.vocabloss_fwd(h, w, targets)
+    got = chela.vocabloss_bwd(h, w, targets, lse, d_loss, grad_dtype=chela.BF16)
+    kept = ref.kept_of(targets, V)
+    hd, wd, y = torch.where(kept[:, None], h.double(), 0.0), w.double(), torch.where(kept, targets, 0)[:, None]
+    dz = torch.softmax(hd @ wd.t(), 1)
+    dz -= torch.zeros_like(dz).scatter_(1, y, 1.0)
+    dz *= torch.where(kept, d_loss.double(), 0.0)[:, None]
+    one_plane = it == "bf16" and T > 64
+    half = 2.0 ** -8 / 3 ** 0.5
+    # what is left: logits and exponentials, 2^-15 of a softmax value or less at these widths; 5 of 100 for the mean of few roundings
+    for name, a, terms in (("d_h", got.d_h, dz.square() @ wd.square()), ("d_w", got.d_w, dz.square().t() @ hd.square())):
+        far, true = float((a.double() - r[name]).norm()), float(r[name].norm())
+        allowed = half * ((float(terms.sum()) if one_plane else 0.0) + true ** 2) ** 0.5 * 1.05 + 2.0 ** -13 * true
+        assert far <= allowed, (name, far / true, allowed / true)
+
+
 def test_fp32_weights_of_several_pieces():
     """The weights' parts are laid out a piece at a time: 90000 x 2048 take more than one, forward and backward."""
     T, V, D = 24, 90000, 2048
