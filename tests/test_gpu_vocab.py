@@ -86,6 +86,34 @@ def test_embedding_gradient(T, V, D, it, gt, left_out, skew, before):
     assert torch.equal(again, got)
 
 
+def test_embedding_of_as_many_tokens_as_there_may_be():
+    """2^31 - 4096 tokens, forward and backward; d_out is zero but for a few whole numbers, so that all sums are exact."""
+    T, V, D, tail = 2 ** 31 - 4096, 5000, 8, 4096
+    torch.cuda.empty_cache()
+    need = int(chela.lib().chela_embed_bwd_workspace_bytes(T, V, D)) + T * (2 * D + 4)
+    if torch.cuda.mem_get_info()[0] < need + (4 << 30):
+        pytest.skip("needs %d GB" % (need >> 30))
+    g = gen(18)
+    some = token_ids(g, tail, V, 0.01, dtype=torch.int32)
+    ids = torch.empty(T, dtype=torch.int32, device="cuda")
+    ids.view(-1, tail).copy_(some)
+    w = normal(g, V, D, dtype=torch.bfloat16)
+    out = chela.embed_fwd(ids, w, scale=0.5)
+    rows = chela.embed_fwd(some, w, scale=0.5)
+    for part in out.view(-1, tail, D).split(16384):
+        assert bool((part == rows).all())
+    d_out = out.zero_()
+    at = torch.cat([torch.randint(0, T, (3000,), generator=g, device="cuda"), torch.arange(T - 500, T, device="cuda"), torch.arange(500, device="cuda")]).unique()
+    values = torch.randint(-3, 4, (len(at), D), generator=g, device="cuda")
+    d_out[at] = values.to(torch.bfloat16)
+    d_w = chela.embed_bwd(ids, d_out, V)
+    kept = ref.kept_of(ids[at], V)
+    true = torch.zeros(V, D, dtype=torch.int64, device="cuda").index_add_(0, ids[at][kept].long(), values[kept])
+    assert int(true.abs().amax()) > 3 and torch.equal(d_w, true.float())
+    del ids, out, part, d_out
+    torch.cuda.empty_cache()
+
+
 # ------------------------------------------------------------------------------------------------ cross entropy
 
 def hidden(g, T, V, D, dtype, targets, lean=4.0):
